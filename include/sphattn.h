@@ -61,7 +61,8 @@ enum {
     SPHATTN_ERR_ALIAS = -7,       /* O overlaps Q, K or V (or mult) */
     SPHATTN_ERR_NORMALIZER = -8,  /* normalizer is not a sphattn_normalizer value */
     SPHATTN_ERR_WORKSPACE = -9,   /* workspace NULL, not 16-byte aligned, or too small */
-    SPHATTN_ERR_SCRATCH = -10     /* sphattn_splitkv_fwd_noalloc: needs more than SPHATTN_NOALLOC_SCRATCH_BYTES */
+    SPHATTN_ERR_SCRATCH = -10,    /* sphattn_splitkv_fwd_noalloc: needs more than SPHATTN_NOALLOC_SCRATCH_BYTES */
+    SPHATTN_ERR_VALUE = -11       /* sphattn_train.h: a number or a choice that the call does not take */
 };
 
 /* Normalizers N(x)_i = a1(x_i) / b(sum_j a2(x_j)) (paper, Appendix A.1, Definition 2). */

@@ -28,6 +28,7 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import math
 import os
 
 from ._build import LIB_PATH, MARSHAL_PATH, build_library
@@ -47,6 +48,10 @@ EXPORTED_SYMBOLS = ("sphattn_fwd", "sphattn_fwd_z", "sphattn_fwd_tile_rows", "sp
                     "sphattn_cross_splitkv_workspace_bytes", "sphattn_cross_splitkv_fwd",
                     "sphattn_bwd", "sphattn_grn_bwd", "sphattn_bwd_workspace_bytes", "sphattn_grn_bwd_split",
                     "sphattn_fp8_workspace_bytes", "sphattn_fp8_fwd", "sphattn_fp8_grn_fwd", "sphattn_fp8_softmax_fwd",
+                    "sphattn_embed_fwd", "sphattn_embed_bwd_workspace_bytes", "sphattn_embed_bwd",
+                    "sphattn_vocab_loss_workspace_bytes", "sphattn_vocab_loss_fwd",
+                    "sphattn_vocab_loss_bwd_workspace_bytes", "sphattn_vocab_loss_bwd",
+                    "sphattn_clip_grads_workspace_bytes", "sphattn_clip_grads",
                     "sphattn_strerror", "sphattn_version")
 
 NORMALIZERS = {"l2": 0, "softmax": 1, "l1": 2, "sqrelu": 3}
@@ -125,6 +130,25 @@ def load_library() -> ctypes.CDLL:
             fn.argtypes = [vp, vp, vp, vp, vp, sz, ip, ip, ip, ip, ip, vp]
         lib.sphattn_fp8_grn_fwd.restype = ip
         lib.sphattn_fp8_grn_fwd.argtypes = [vp, vp, vp, vp, vp, vp, sz, ip, ip, ip, ip, ip, vp]
+        fl = ctypes.c_float
+        lib.sphattn_embed_fwd.restype = ip
+        lib.sphattn_embed_fwd.argtypes = [vp, ip, vp, vp, vp, ip, ip, ip, fl, ip, vp]
+        lib.sphattn_embed_bwd_workspace_bytes.restype = sz
+        lib.sphattn_embed_bwd_workspace_bytes.argtypes = [ip, ip, ip]
+        lib.sphattn_embed_bwd.restype = ip
+        lib.sphattn_embed_bwd.argtypes = [vp, ip, vp, vp, vp, ip, ip, ip, fl, ip, vp, sz, vp]
+        for name in ("sphattn_vocab_loss_workspace_bytes", "sphattn_vocab_loss_bwd_workspace_bytes"):
+            fn = getattr(lib, name)
+            fn.restype = sz
+            fn.argtypes = [ip, ip, ip, ip]
+        lib.sphattn_vocab_loss_fwd.restype = ip
+        lib.sphattn_vocab_loss_fwd.argtypes = [vp, vp, vp, ip, vp, vp, vp, ip, ip, ip, fl, ip, ip, ip, vp, sz, vp]
+        lib.sphattn_vocab_loss_bwd.restype = ip
+        lib.sphattn_vocab_loss_bwd.argtypes = [vp, vp, vp, ip, vp, vp, vp, vp, ip, ip, ip, fl, ip, ip, vp, sz, vp]
+        lib.sphattn_clip_grads_workspace_bytes.restype = sz
+        lib.sphattn_clip_grads_workspace_bytes.argtypes = [ip]
+        lib.sphattn_clip_grads.restype = ip
+        lib.sphattn_clip_grads.argtypes = [vp, vp, vp, vp, ip, fl, vp, vp, sz, vp]
         lib.sphattn_strerror.restype = ctypes.c_char_p
         lib.sphattn_strerror.argtypes = [ip]
         lib.sphattn_version.restype = ip
@@ -697,3 +721,250 @@ def sphattn_bwd(Q, K, V, O, dO, Z, dQ=None, dK=None, dV=None, delta=None, dtype=
     B, H, N, d, H_kv = _check_backward(Q, K, V, None, O, dO, Z, dQ, dK, dV, delta, code)
     _launch_bwd(lib, Q, K, V, None, O, dO, Z, dQ, dK, dV, delta, B, H, H_kv, N, d, code, stream, own_outputs)
     return dQ, dK, dV
+
+
+# ---- what a model that trains with the attention has at its two ends (include/sphattn_train.h) ----------
+#
+# Token embeddings, the cross entropy over a vocabulary, gradient clipping, in the manner of the entry points above.
+# A caller that gives a stream handle brings every output and the workspace too: memory allocated here
+# would belong to the current stream.
+
+REDUCTIONS = {"none": 0, "sum": 1, "mean": 2}
+
+
+@functools.lru_cache(maxsize=None)
+def _codes():
+    import torch
+    return {torch.float32: SPHATTN_F32, torch.bfloat16: SPHATTN_BF16, torch.float16: SPHATTN_F16}
+
+
+@functools.lru_cache(maxsize=None)
+def _id_types():
+    import torch
+    return {torch.int32: 4, torch.int64: 8}
+
+
+def _code_of(name, t):
+    code = _codes().get(t.dtype)
+    if code is None:
+        raise ValueError(f"{name} must have dtype torch.float32 or torch.bfloat16 or torch.float16, got {t.dtype}")
+    return code
+
+
+def _ids(name, t, n=None):
+    """Bytes per id of a one-dimensional tensor of token ids."""
+    if t is None or t.dim() != 1:
+        raise ValueError(f"{name} must be a one-dimensional tensor")
+    _need(name, t, t.shape if n is None else (n,), tuple(_id_types()))
+    return _id_types()[t.dtype]
+
+
+def _matrix(name, t):
+    if t is None or t.dim() != 2:
+        raise ValueError(f"{name} must be a two-dimensional tensor")
+    return int(t.shape[0]), int(t.shape[1])
+
+
+def _f32(name, t, shape, optional=True):
+    import torch
+    _need(name, t, shape, (torch.float32,), optional=optional)
+
+
+def _brought(stream, **needed):
+    if stream is not None:
+        for name, t in needed.items():
+            if t is None:
+                raise ValueError(f"{name} is required with a stream handle")
+
+
+def _scratch(workspace, need, like):
+    """(tensor, bytes): the caller's workspace, or one of `need` bytes."""
+    if workspace is not None:
+        return workspace, _need_workspace(workspace)
+    import torch
+    return torch.empty(need, dtype=torch.uint8, device=like.device), need
+
+
+def _finite(name, x):
+    x = float(x)
+    if not math.isfinite(x):
+        raise ValueError(f"{name} must be finite, got {x}")
+    return x
+
+
+# ---- embedding ------------------------------------------------------------------------------------
+
+def sphattn_embed_fwd(tokens, table, mult=None, scale=1.0, O=None, stream=None):
+    """O[t] = scale * mult[t] * table[tokens[t]]: tokens [T] int32 or int64 (negative: no token, a row of zeros; not below
+    V: a row of NaN), table [V,D] fp32, bf16 or fp16, mult [T] fp32 or None; returns O [T,D]."""
+    import torch
+    lib = load_library()
+    id_bytes = _ids("tokens", tokens)
+    V, D = _matrix("table", table)
+    T, code = int(tokens.shape[0]), _code_of("table", table)
+    _brought(stream, O=O)
+    if O is None:
+        O = torch.empty((T, D), dtype=table.dtype, device=table.device)
+    _need("table", table, (V, D), (table.dtype,))
+    _need("O", O, (T, D), (table.dtype,))
+    _f32("mult", mult, (T,))
+    _on_device(table=table, tokens=tokens, mult=mult, O=O)
+    _raise_on(lib.sphattn_embed_fwd(tokens.data_ptr(), id_bytes, table.data_ptr(), _ptr(mult), O.data_ptr(), T, V, D, float(scale), code,
+                                    _stream_of(table, stream)))
+    return O
+
+
+def sphattn_embed_bwd_workspace_bytes(T, V, D) -> int:
+    return int(load_library().sphattn_embed_bwd_workspace_bytes(T, V, D))
+
+
+def sphattn_embed_bwd(tokens, dO, V, mult=None, scale=1.0, dtable=None, workspace=None, stream=None):
+    """Gradient [V,D] of the table for O = sphattn_embed_fwd(tokens, table, mult, scale) and dO [T,D]; every row is written,
+    the same bits in every run.  `workspace` is a device byte tensor of at least sphattn_embed_bwd_workspace_bytes(T, V, D)."""
+    import torch
+    lib = load_library()
+    id_bytes = _ids("tokens", tokens)
+    T, D = _matrix("dO", dO)
+    V, code = int(V), _code_of("dO", dO)
+    _ids("tokens", tokens, T)
+    _brought(stream, dtable=dtable, workspace=workspace)
+    _need("dO", dO, (T, D), (dO.dtype,))
+    _f32("mult", mult, (T,))
+    _on_device(dO=dO, tokens=tokens, mult=mult, dtable=dtable, workspace=workspace)
+    if dtable is None:
+        dtable = torch.empty((V, D), dtype=dO.dtype, device=dO.device)
+    _need("dtable", dtable, (V, D), (dO.dtype,))
+    ws, ws_bytes = _scratch(workspace, sphattn_embed_bwd_workspace_bytes(T, V, D), dO)
+    _raise_on(lib.sphattn_embed_bwd(tokens.data_ptr(), id_bytes, _ptr(mult), dO.data_ptr(), dtable.data_ptr(), T, V, D, float(scale), code,
+                                    ws.data_ptr(), ws_bytes, _stream_of(dO, stream)))
+    return dtable
+
+
+# ---- cross entropy over the vocabulary -------------------------------------------------------------
+
+def _head(X, W, targets):
+    T, D = _matrix("X", X)
+    V, _ = _matrix("W", W)
+    code = _code_of("X", X)
+    id_bytes = _ids("targets", targets, T)
+    _need("X", X, (T, D), (X.dtype,))
+    _need("W", W, (V, D), (X.dtype,))
+    return T, V, D, code, id_bytes
+
+
+def sphattn_vocab_loss_workspace_bytes(T, V, D, dtype="bf16") -> int:
+    return int(load_library().sphattn_vocab_loss_workspace_bytes(T, V, D, _dtype_code(dtype)))
+
+
+def sphattn_vocab_loss_bwd_workspace_bytes(T, V, D, dtype="bf16") -> int:
+    return int(load_library().sphattn_vocab_loss_bwd_workspace_bytes(T, V, D, _dtype_code(dtype)))
+
+
+def sphattn_vocab_loss_fwd(X, W, targets, scale=1.0, reduction="none", all_rows=True, losses=None, lse=None, mean=None,
+                           workspace=None, stream=None):
+    """-log softmax(scale * X W^T)[targets] without the logits in memory: X [T,D], W [V,D] (fp32, bf16 or fp16), targets [T]
+    int32 or int64; rows with a negative target do not count, a target not below V gives NaN.  Returns (losses [T], lse [T])
+    in fp32, and with reduction "sum" or "mean" (losses, lse, that of the rows that count).  all_rows=False leaves lse out where a
+    row does not count, and the work for it."""
+    import torch
+    lib = load_library()
+    T, V, D, code, id_bytes = _head(X, W, targets)
+    red = REDUCTIONS[reduction]
+    scale = _finite("scale", scale)
+    _brought(stream, losses=losses, lse=lse, workspace=workspace, **({"mean": mean} if red else {}))
+    _on_device(X=X, W=W, targets=targets, losses=losses, lse=lse, mean=mean, workspace=workspace)
+    losses = torch.empty(T, dtype=torch.float32, device=X.device) if losses is None else losses
+    lse = torch.empty(T, dtype=torch.float32, device=X.device) if lse is None else lse
+    if red and mean is None:
+        mean = torch.empty((), dtype=torch.float32, device=X.device)
+    _f32("losses", losses, (T,))
+    _f32("lse", lse, (T,))
+    _f32("mean", mean, ())
+    ws, ws_bytes = _scratch(workspace, lib.sphattn_vocab_loss_workspace_bytes(T, V, D, code), X)
+    _raise_on(lib.sphattn_vocab_loss_fwd(X.data_ptr(), W.data_ptr(), targets.data_ptr(), id_bytes, losses.data_ptr(), lse.data_ptr(),
+                                         _ptr(mean), T, V, D, scale, red, int(bool(all_rows)), code, ws.data_ptr(), ws_bytes,
+                                         _stream_of(X, stream)))
+    return (losses, lse, mean) if red else (losses, lse)
+
+
+def sphattn_vocab_loss_bwd(X, W, targets, lse, dloss, scale=1.0, reduction="none", dX=None, dW=None, want_dX=True, want_dW=True,
+                           workspace=None, stream=None):
+    """Gradients (dX, dW) of the losses of sphattn_vocab_loss_fwd: lse [T] from it; dloss fp32, [T] with reduction "none" and one
+    value with "sum" and "mean".  One of the two may be not wanted (None in its place)."""
+    import torch
+    lib = load_library()
+    T, V, D, code, id_bytes = _head(X, W, targets)
+    red = REDUCTIONS[reduction]
+    scale = _finite("scale", scale)
+    if not want_dX and not want_dW:
+        raise ValueError("neither dX nor dW is wanted")
+    _f32("lse", lse, (T,), optional=False)
+    _f32("dloss", dloss, () if red else (T,), optional=False)
+    _brought(stream, workspace=workspace, **({"dX": dX} if want_dX else {}), **({"dW": dW} if want_dW else {}))
+    _on_device(X=X, W=W, targets=targets, lse=lse, dloss=dloss, dX=dX, dW=dW, workspace=workspace)
+    if want_dX and dX is None:
+        dX = torch.empty_like(X)
+    if want_dW and dW is None:
+        dW = torch.empty_like(W)
+    dX, dW = dX if want_dX else None, dW if want_dW else None
+    _need("dX", dX, (T, D), (X.dtype,), optional=True)
+    _need("dW", dW, (V, D), (X.dtype,), optional=True)
+    ws, ws_bytes = _scratch(workspace, lib.sphattn_vocab_loss_bwd_workspace_bytes(T, V, D, code), X)
+    _raise_on(lib.sphattn_vocab_loss_bwd(X.data_ptr(), W.data_ptr(), targets.data_ptr(), id_bytes, lse.data_ptr(), dloss.data_ptr(),
+                                         _ptr(dX), _ptr(dW), T, V, D, scale, red, code, ws.data_ptr(), ws_bytes, _stream_of(X, stream)))
+    return dX, dW
+
+
+# ---- clipping ----------------------------------------------------------------------------------------
+
+def _dense(t):
+    """Whether the elements lie side by side in some order of the dimensions (then an elementwise step may take them in memory's)."""
+    if t.is_contiguous():
+        return True
+    expected = 1
+    for stride, size in sorted((st, si) for st, si in zip(t.stride(), t.shape) if si != 1):
+        if stride != expected:
+            return False
+        expected *= size
+    return True
+
+
+def sphattn_clip_grads_workspace_bytes(n) -> int:
+    return int(load_library().sphattn_clip_grads_workspace_bytes(n))
+
+
+def sphattn_clip_grads(grads, max_norm, out=None, norm=None, workspace=None, stream=None):
+    """Scale gradients down so that their common 2-norm is at most max_norm: out[i] = grads[i] * min(1, max_norm / (norm + 1e-6)),
+    in place unless `out` (a tensor like each of `grads`) is given.  Tensors of fp32, bf16 and fp16, in any mixture, of any
+    shape, dense in memory.  Returns the norm (before clipping) as an fp32 scalar on the device; nothing waits for it."""
+    import torch
+    lib = load_library()
+    grads = list(grads)
+    outs = grads if out is None else list(out)
+    if len(outs) != len(grads):
+        raise ValueError(f"out must have {len(grads)} tensors, got {len(outs)}")
+    max_norm = float(max_norm)
+    if not max_norm >= 0:
+        raise ValueError(f"max_norm must not be negative, got {max_norm}")
+    if not grads and norm is None:
+        raise ValueError("no gradients: norm is required (there is no device to put it on)")
+    n, codes = len(grads), _codes()
+    device = grads[0].device if grads else norm.device
+    for i in range(n):
+        g, o = grads[i], outs[i]
+        if g.dtype not in codes or g.device != device or not g.is_cuda or not _dense(g):
+            raise ValueError(f"grads[{i}] must be a dense fp32, bf16 or fp16 tensor on {device} (a GPU), got {g.dtype} of strides {g.stride()} on {g.device}")
+        if o is not g and (o.dtype != g.dtype or o.shape != g.shape or o.stride() != g.stride() or o.device != device):
+            raise ValueError(f"out[{i}] must be like grads[{i}]: {g.dtype} {tuple(g.shape)} of strides {g.stride()}, "
+                             f"got {o.dtype} {tuple(o.shape)} of strides {o.stride()} on {o.device}")
+    _brought(stream, norm=norm, workspace=workspace)
+    if norm is None:
+        norm = torch.empty((), dtype=torch.float32, device=device)
+    _f32("norm", norm, ())
+    _on_device(norm=norm, workspace=workspace)
+    ws, ws_bytes = _scratch(workspace, sphattn_clip_grads_workspace_bytes(n), norm)
+    pointers, sizes, types = ctypes.c_void_p * n, ctypes.c_longlong * n, ctypes.c_int * n
+    _raise_on(lib.sphattn_clip_grads(pointers(*[g.data_ptr() for g in grads]), pointers(*[o.data_ptr() for o in outs]),
+                                     sizes(*[g.numel() for g in grads]), types(*[codes[g.dtype] for g in grads]), n, max_norm,
+                                     norm.data_ptr(), ws.data_ptr(), ws_bytes, _stream_of(norm, stream)))
+    return norm

@@ -8,7 +8,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB_PATH = os.path.join(_HERE, "libsphattn.so")
 MARSHAL_PATH = os.path.join(_HERE, "_marshal.so")
-SOURCES = [os.path.join(CSRC, "sphattn_api.hip")]
+SOURCES = [os.path.join(CSRC, name) for name in ("sphattn_api.hip", "sphattn_train.hip")]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

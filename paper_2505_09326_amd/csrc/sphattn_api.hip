@@ -19,7 +19,7 @@ namespace {
 
 using namespace sphattn;
 
-constexpr int kVersion = 510;   // 0.5.1
+constexpr int kVersion = 600;   // 0.6.0
 
 static_assert(kBC == kChoiceTile && kF32Tile == kChoiceF32Tile, "times per tile of the kernels' tiles");
 
@@ -1153,6 +1153,7 @@ const char* sphattn_strerror(int code)
     case SPHATTN_ERR_NORMALIZER: return "normalizer is not a sphattn_normalizer value";
     case SPHATTN_ERR_WORKSPACE: return "workspace is NULL, misaligned or smaller than the entry point's *_workspace_bytes";
     case SPHATTN_ERR_SCRATCH: return "the problem needs more scratch than the library's own array holds (SPHATTN_NOALLOC_SCRATCH_BYTES)";
+    case SPHATTN_ERR_VALUE: return "a number or a choice that the call does not take (scale, max_norm, reduction)";
     default: return "unknown sphattn error code";
     }
 }

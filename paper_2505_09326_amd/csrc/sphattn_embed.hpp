@@ -1,0 +1,378 @@
+// Embedding lookup with scaling and the gradient of the table by sorted tokens, for gfx950.
+//
+//   O[t] = s m_t E[x_t]          dE[v] = s sum_{t : x_t = v} m_t dO[t]
+//
+// Both are bound by memory: the lookup reads and writes T D values, the gradient reads T D and writes
+// V D.  What the gradient needs beside that is an order in which equal tokens are neighbours, without atomics
+// on floats (their order, and with it the result, would change from run to run).
+#pragma once
+#include "sphattn_device.hpp"
+
+namespace sphattn {
+
+// ---- element types --------------------------------------------------------------------------------
+
+enum class Store { F32, Bf16, F16 };
+template <Store S> constexpr int store_bytes() { return S == Store::F32 ? 4 : 2; }
+
+template <Store S> __device__ __forceinline__ float load_el(const void* p, size_t i)
+{
+    if constexpr (S == Store::F32) return ((const float*)p)[i];
+    else if constexpr (S == Store::Bf16) return (float)((const __bf16*)p)[i];
+    else return (float)((const _Float16*)p)[i];
+}
+template <Store S> __device__ __forceinline__ void store_el(void* p, size_t i, float x)
+{
+    if constexpr (S == Store::F32) ((float*)p)[i] = x;
+    else if constexpr (S == Store::Bf16) ((__bf16*)p)[i] = (__bf16)x;
+    else ((_Float16*)p)[i] = (_Float16)x;
+}
+
+// 16 bytes of elements as floats, and back (to nearest even)
+template <Store S> constexpr int per16() { return 16 / store_bytes<S>(); }
+template <Store S> __device__ __forceinline__ void widen16(i32x4 w, float (&x)[per16<S>()])
+{
+    if constexpr (S == Store::F32) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int bits = w[i];                 // (a bit cast of the vector's element itself takes the vector's first)
+            x[i] = __builtin_bit_cast(float, bits);
+        }
+    } else if constexpr (S == Store::Bf16) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[2 * i] = __builtin_bit_cast(float, w[i] << 16);
+            x[2 * i + 1] = __builtin_bit_cast(float, w[i] & (int)0xffff0000);
+        }
+    } else {
+        const f16x8 h = __builtin_bit_cast(f16x8, w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = (float)h[i];
+    }
+}
+template <Store S> __device__ __forceinline__ i32x4 narrow16(const float (&x)[per16<S>()])
+{
+    i32x4 w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (S == Store::F32) w[i] = __builtin_bit_cast(int, x[i]);
+        else w[i] = pack2<S == Store::F16>(x[2 * i], x[2 * i + 1]);
+    }
+    return w;
+}
+
+// Token ids of 4 or 8 bytes as ints: what does not fit an int is no valid id (negative stays negative, the rest too large).
+__device__ __forceinline__ int load_id(const void* ids, int id_bytes, size_t i)
+{
+    if (id_bytes == 4) return ((const int*)ids)[i];
+    const long long x = ((const long long*)ids)[i];
+    return x < 0 ? -1 : x > 0x7fffffff ? 0x7fffffff : (int)x;
+}
+
+// ---- lookup ------------------------------------------------------------------------------------------
+// One wave per row, four rows per workgroup; a lane moves 16 bytes at a time, four of them under way.  WIDE: rows
+// are whole 16-byte pieces from an aligned start on.  Bound by memory, and for few rows by the launch.
+constexpr int kEmbedThreads = 256;
+
+template <Store S, bool WIDE>
+__global__ __launch_bounds__(kEmbedThreads)
+void embed_fwd_kernel(const void* __restrict__ tokens, int id_bytes, const void* __restrict__ table,
+                      const float* __restrict__ mult, void* __restrict__ O, int T, int V, int D, float scale)
+{
+    const int lane = threadIdx.x & 63;
+    const long long row = (long long)blockIdx.x * (kEmbedThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (row >= T) return;
+    const int v = load_id(tokens, id_bytes, row);
+    // no token: zeros; not a token of this table: NaN.  Both without reading the table.
+    const bool in = v >= 0 && v < V;
+    const float f = in ? (mult ? mult[row] * scale : scale) : 0.f;
+    const float fill = v < 0 ? 0.f : __builtin_nanf("");
+    if constexpr (WIDE) {
+        constexpr int N = per16<S>(), AHEAD = 4;
+        const int pieces = D / N;
+        const i32x4* src = (const i32x4*)table + (size_t)(in ? v : 0) * pieces;
+        i32x4* dst = (i32x4*)O + (size_t)row * pieces;
+        for (int c0 = 0; c0 < pieces; c0 += 64 * AHEAD) {
+            i32x4 w[AHEAD];
+#pragma unroll
+            for (int a = 0; a < AHEAD; ++a) {
+                const int c = c0 + a * 64 + lane;
+                w[a] = i32x4{0, 0, 0, 0};
+                if (in && c < pieces) w[a] = src[c];
+            }
+#pragma unroll
+            for (int a = 0; a < AHEAD; ++a) {
+                const int c = c0 + a * 64 + lane;
+                float x[N];
+                widen16<S>(w[a], x);
+#pragma unroll
+                for (int i = 0; i < N; ++i) x[i] = in ? x[i] * f : fill;
+                if (c < pieces) dst[c] = narrow16<S>(x);
+            }
+        }
+    } else {
+        for (int c = lane; c < D; c += 64) {
+            const float x = in ? load_el<S>(table, (size_t)v * D + c) * f : fill;
+            store_el<S>(O, (size_t)row * D + c, x);
+        }
+    }
+}
+
+// ---- gradient: sorting ---------------------------------------------------------------------------------
+// A stable counting sort of the positions by token in one launch: a workgroup owns `ids` neighbouring
+// token ids and reads all T tokens twice (they stay in the caches: 64 bytes a cycle and CU, 0.25 us per 4096
+// of 8 bytes).  First it counts, per wave (each wave has a stretch of t of its own) and id, its own ids, and how many
+// tokens lie below them, which is where its part of the result begins; the second time each position goes to its place:
+// that of its id and wave, plus its rank among the equal tokens before it in the wave.  No workgroup waits for
+// another, no atomic touches global memory.  Then it writes zeros to those rows of the gradient that have no token.
+//   first : [V + 1], where the positions of id v begin in `sorted`;  sorted : [T]
+constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64, kSortMaxIds = 512;
+
+constexpr int sort_lds_bytes(int ids) { return (kSortWaves * ids + 2 * kSortWaves + 2) * 4; }
+
+__device__ __forceinline__ int sum_over_wave(int x)
+{
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) x += __shfl_xor(x, d);
+    return x;
+}
+
+// sum of x over the lanes below, and `total` over all
+__device__ __forceinline__ int exclusive_over_wave(int x, int lane, int& total)
+{
+    int s = x;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int y = __shfl_up(s, d);
+        if (lane >= d) s += y;
+    }
+    total = __shfl(s, 63);
+    return s - x;
+}
+
+__global__ __launch_bounds__(kSortThreads)
+void embed_sort_kernel(const void* __restrict__ tokens, int id_bytes, int* __restrict__ first, int* __restrict__ sorted,
+                       void* __restrict__ dtable, int T, int V, int ids, int row_bytes)
+{
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem_raw[];
+    int* cnt = (int*)smem_raw;                     // [kSortWaves][ids]
+    int* part = cnt + kSortWaves * ids;            // [2][kSortWaves]
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int lo = blockIdx.x * ids, n_ids = min(ids, V - lo);
+    for (int i = tid; i < kSortWaves * ids; i += kSortThreads) cnt[i] = 0;
+    __syncthreads();
+
+    // this wave's tokens: whole batches of 64
+    const long long batches = ((long long)T + 63) / 64, share = (batches + kSortWaves - 1) / kSortWaves;
+    const long long t0 = min((long long)T, wave * share * 64), t1 = min((long long)T, t0 + share * 64);
+    int* mine = cnt + wave * ids;
+    constexpr int AHEAD = 8;
+    int below = 0;
+    for (long long t = t0; t < t1; t += 64 * AHEAD) {
+        int v[AHEAD];
+#pragma unroll
+        for (int a = 0; a < AHEAD; ++a) v[a] = t + a * 64 + lane < t1 ? load_id(tokens, id_bytes, t + a * 64 + lane) : -1;
+#pragma unroll
+        for (int a = 0; a < AHEAD; ++a) {
+            below += v[a] >= 0 && v[a] < lo;
+            if (v[a] >= lo && v[a] < lo + n_ids) atomicAdd(&mine[v[a] - lo], 1);   // (integers, in LDS)
+        }
+    }
+    below = sum_over_wave(below);
+    if (lane == 0) part[wave] = below;
+    __syncthreads();
+
+    // places: ids in order, within an id the waves in order.  Thread i has id i (ids <= kSortThreads).
+    int of_id = 0;
+    if (tid < n_ids)
+        for (int w = 0; w < kSortWaves; ++w) of_id += cnt[w * ids + tid];
+    int of_wave, base = 0;
+    int at = exclusive_over_wave(of_id, lane, of_wave);
+    if (lane == 0) part[kSortWaves + wave] = of_wave;
+    __syncthreads();
+    for (int w = 0; w < kSortWaves; ++w) {
+        base += part[w];
+        if (w < wave) at += part[kSortWaves + w];
+    }
+    at += base;
+    if (tid < n_ids) {
+        first[lo + tid] = at;
+        if (lo + tid == V - 1) first[V] = at + of_id;
+        int p = at;
+        for (int w = 0; w < kSortWaves; ++w) {
+            const int c = cnt[w * ids + tid];
+            cnt[w * ids + tid] = p;
+            p += c;
+        }
+    }
+    __syncthreads();
+
+    for (long long t = t0; t < t1; t += 64 * AHEAD) {
+        int v[AHEAD];
+#pragma unroll
+        for (int a = 0; a < AHEAD; ++a) v[a] = t + a * 64 + lane < t1 ? load_id(tokens, id_bytes, t + a * 64 + lane) : -1;
+#pragma unroll
+        for (int a = 0; a < AHEAD; ++a) {
+            const bool own = v[a] >= lo && v[a] < lo + n_ids;
+            uint64_t left = __ballot(own);
+            while (left) {                         // one round per different id among the 64
+                const int id = __shfl(v[a], __builtin_ctzll(left));
+                const uint64_t same = __ballot(own && v[a] == id);
+                const int p = mine[id - lo];
+                if (own && v[a] == id)
+                    sorted[p + __builtin_amdgcn_mbcnt_hi((uint32_t)(same >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)same, 0))] =
+                        (int)(t + a * 64 + lane);
+                mine[id - lo] = p + __builtin_popcountll(same);   // (every lane the same value)
+                left &= ~same;
+            }
+        }
+    }
+
+    // rows without a token, a wave each; thread i says over LDS how many id i has
+    __syncthreads();
+    if (tid < n_ids) cnt[tid] = of_id;
+    __syncthreads();
+    for (int i = wave; i < n_ids; i += kSortWaves) {
+        if (cnt[i] != 0) continue;
+        unsigned char* row = (unsigned char*)dtable + (size_t)(lo + i) * row_bytes;
+        if ((((uintptr_t)dtable | (unsigned)row_bytes) & 15) == 0) {
+            for (int c = lane; c < row_bytes / 16; c += 64) ((i32x4*)row)[c] = i32x4{0, 0, 0, 0};
+        } else {
+            for (int c = lane; c < row_bytes / 2; c += 64) ((short*)row)[c] = 0;
+        }
+    }
+}
+
+// ---- gradient: sums ------------------------------------------------------------------------------------
+// The sorted positions are cut into pieces of `len`, whatever tokens they hold, so a token that half of all positions have is
+// shared by as many waves as it fills pieces.  A wave adds up a piece's runs of equal tokens over 64 lanes' columns in fp32.  A
+// run that lies inside the piece is a row of the gradient; one that crosses its borders leaves a partial sum: [piece][0] if
+// it began before the piece, [piece][1] if it begins in it and goes on behind it.
+template <Store S, bool WIDE> constexpr int embed_lane_cols() { return WIDE ? per16<S>() : 1; }
+
+template <Store S, bool WIDE>
+__device__ __forceinline__ void store_cols(void* row0, size_t at, const float (&x)[embed_lane_cols<S, WIDE>()])
+{
+    if constexpr (WIDE) ((i32x4*)row0)[at / per16<S>()] = narrow16<S>(x);
+    else store_el<S>(row0, at, x[0]);
+}
+
+template <Store S, bool WIDE>
+__global__ __launch_bounds__(kEmbedThreads)
+void embed_sum_kernel(const void* __restrict__ tokens, int id_bytes, const float* __restrict__ mult, const void* __restrict__ dO,
+                      const int* __restrict__ first, const int* __restrict__ sorted, float* __restrict__ partial,
+                      void* __restrict__ dtable, int V, int D, float scale, int len, int n_pieces)
+{
+    constexpr int C = embed_lane_cols<S, WIDE>(), AHEAD = WIDE ? 8 : 4;
+    const int lane = threadIdx.x & 63;
+    const long long piece = (long long)blockIdx.x * (kEmbedThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (piece >= n_pieces) return;
+    const int total = first[V];
+    const long long p0 = piece * len, p1 = min((long long)total, p0 + len);
+    if (p0 >= p1) return;
+    const int col = ((int)blockIdx.y * 64 + lane) * C;
+    const bool live = col < D;
+    float acc[C];
+#pragma unroll
+    for (int i = 0; i < C; ++i) acc[i] = 0.f;
+    int run = -1;                                  // the id that acc belongs to
+    auto flush = [&](int id) {
+        const int r0 = first[id], r1 = first[id + 1];
+        if (live) {
+            if (r0 >= p0 && r1 <= p1) store_cols<S, WIDE>(dtable, (size_t)id * D + col, acc);
+            else {
+                float* to = partial + ((size_t)piece * 2 + (r0 < p0 ? 0 : 1)) * D + col;
+#pragma unroll
+                for (int i = 0; i < C; ++i) to[i] = acc[i];
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < C; ++i) acc[i] = 0.f;
+    };
+    for (long long b = p0; b < p1; b += 64) {
+        // 64 positions, their tokens and factors, one per lane
+        const int n = (int)min((long long)64, p1 - b);
+        int t = 0, id = 0;
+        float f = 0.f;
+        if (lane < n) {
+            t = sorted[b + lane];
+            id = load_id(tokens, id_bytes, t);
+            f = mult ? mult[t] * scale : scale;
+        }
+        for (int j0 = 0; j0 < n; j0 += AHEAD) {
+            i32x4 w[AHEAD];
+            float s[AHEAD];
+#pragma unroll
+            for (int a = 0; a < AHEAD; ++a) {
+                const size_t at = (size_t)__builtin_amdgcn_readlane(t, min(j0 + a, n - 1)) * D + col;
+                if constexpr (WIDE) {
+                    w[a] = i32x4{0, 0, 0, 0};
+                    if (live) w[a] = ((const i32x4*)dO)[at / C];
+                } else {
+                    s[a] = live ? load_el<S>(dO, at) : 0.f;
+                }
+            }
+#pragma unroll
+            for (int a = 0; a < AHEAD; ++a) {
+                if (j0 + a >= n) break;
+                const int v = __builtin_amdgcn_readlane(id, j0 + a);
+                const float fa = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f), j0 + a));
+                if (v != run) {
+                    if (run >= 0) flush(run);
+                    run = v;
+                }
+                float x[C];
+                if constexpr (WIDE) widen16<S>(w[a], x);
+                else x[0] = s[a];
+#pragma unroll
+                for (int i = 0; i < C; ++i) acc[i] = __builtin_fmaf(x[i], fa, acc[i]);
+            }
+        }
+    }
+    flush(run);
+}
+
+// A row whose run crosses borders: the piece in which it begins adds its partial sums up, eight waves a share of the
+// pieces each, the shares in order behind that.
+constexpr int kJoinThreads = 512, kJoinWaves = kJoinThreads / 64;
+
+template <Store S, bool WIDE>
+__global__ __launch_bounds__(kJoinThreads)
+void embed_join_kernel(const void* __restrict__ tokens, int id_bytes, const int* __restrict__ first, const int* __restrict__ sorted,
+                       const float* __restrict__ partial, void* __restrict__ dtable, int V, int D, int len)
+{
+    constexpr int C = embed_lane_cols<S, WIDE>();
+    __shared__ float shared[kJoinWaves][64 * C];
+    const long long piece = blockIdx.x, p0 = piece * len, p1 = p0 + len;
+    if (p1 >= first[V]) return;                    // nothing behind this piece
+    const int id = load_id(tokens, id_bytes, sorted[p1 - 1]);
+    const int r0 = first[id], r1 = first[id + 1];
+    if (r0 < p0 || r1 <= p1) return;               // its last run began earlier, or ends with it
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int col = ((int)blockIdx.y * 64 + lane) * C;
+    const long long last = (r1 - 1) / len;         // the run's last piece
+    float acc[C];
+#pragma unroll
+    for (int i = 0; i < C; ++i) acc[i] = 0.f;
+    const long long n = last - piece + 1, share = (n + kJoinWaves - 1) / kJoinWaves;
+    const long long q0 = piece + wave * share, q1 = min(last + 1, q0 + share);
+    if (col < D) {
+#pragma unroll 4
+        for (long long q = q0; q < q1; ++q) {
+            const float* from = partial + ((size_t)q * 2 + (q == piece ? 1 : 0)) * D + col;
+#pragma unroll
+            for (int i = 0; i < C; ++i) acc[i] += from[i];
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < C; ++i) shared[wave][lane * C + i] = acc[i];
+    __syncthreads();
+    if (wave == 0 && col < D) {
+        for (int w = 1; w < kJoinWaves; ++w)
+#pragma unroll
+            for (int i = 0; i < C; ++i) acc[i] += shared[w][lane * C + i];
+        store_cols<S, WIDE>(dtable, (size_t)id * D + col, acc);
+    }
+}
+
+}  // namespace sphattn

@@ -1,0 +1,546 @@
+// Host side of the C ABI declared in include/sphattn_train.h: argument checks, choice of tiles, launches on the
+// caller's stream.  Allocates nothing and never synchronises.
+#include "sphattn_embed.hpp"
+#include "sphattn_vocab.hpp"
+#include "sphattn_clip.hpp"
+#include "../../include/sphattn_train.h"
+
+#include <climits>
+#include <cmath>
+#include <stdint.h>
+
+#include <atomic>
+
+namespace {
+
+using namespace sphattn;
+
+constexpr int kCus = 256;
+
+// A range of bytes that a call reads or writes.
+struct Range { const void* at; size_t bytes; };
+
+bool meet(const Range& a, const Range& b)
+{
+    if (!a.at || !b.at || !a.bytes || !b.bytes) return false;
+    const uintptr_t a0 = (uintptr_t)a.at, b0 = (uintptr_t)b.at;
+    return a0 <= b0 ? b0 - a0 < a.bytes : a0 - b0 < b.bytes;
+}
+
+// Each written range against everything else.
+template <int W, int R>
+bool any_meet(const Range (&written)[W], const Range (&read)[R])
+{
+    for (int i = 0; i < W; ++i) {
+        for (int j = i + 1; j < W; ++j)
+            if (meet(written[i], written[j])) return true;
+        for (int j = 0; j < R; ++j)
+            if (meet(written[i], read[j])) return true;
+    }
+    return false;
+}
+
+bool off(const void* p, size_t alignment) { return ((uintptr_t)p & (alignment - 1)) != 0; }
+
+int element_bytes(int dtype)
+{
+    return dtype == SPHATTN_F32 ? 4 : dtype == SPHATTN_BF16 || dtype == SPHATTN_F16 ? 2 : 0;
+}
+
+int launched() { return hipGetLastError() == hipSuccess ? SPHATTN_OK : SPHATTN_ERR_LAUNCH; }
+
+// A kernel with more than 64 KB of LDS needs its limit raised once per device.
+template <typename Kern>
+bool raise_lds_limit(Kern kern, int lds_bytes)
+{
+    static std::atomic<uint64_t> done{0};
+    int dev = 0;
+    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) {
+        (void)hipGetLastError();
+        return false;
+    }
+    const uint64_t bit = 1ull << dev;
+    if (done.load(std::memory_order_acquire) & bit) return true;
+    if (hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes) != hipSuccess) {
+        (void)hipGetLastError();
+        return false;
+    }
+    done.fetch_or(bit, std::memory_order_release);
+    return true;
+}
+
+// Pieces of a workspace, each on a 256-byte line.
+class Carve {
+public:
+    explicit Carve(void* base) : base_((unsigned char*)base) {}
+    template <typename T> T* take(size_t count)
+    {
+        T* p = base_ ? (T*)(base_ + used_) : nullptr;
+        used_ += (count * sizeof(T) + 255) / 256 * 256;
+        return p;
+    }
+    size_t used() const { return used_; }
+private:
+    unsigned char* base_;
+    size_t used_ = 0;
+};
+
+// ---- embedding -------------------------------------------------------------------------------------
+
+bool embed_shape(int T, int V, int D) { return T >= 0 && V >= 1 && V <= 1 << 30 && D >= 1 && D <= 65536; }
+
+int embed_check(const void* tokens, int id_bytes, const float* mult, int T, int V, int D, int dtype)
+{
+    if (!embed_shape(T, V, D)) return SPHATTN_ERR_SHAPE;
+    if (!element_bytes(dtype) || (id_bytes != 4 && id_bytes != 8)) return SPHATTN_ERR_DTYPE;
+    if (T > 0 && !tokens) return SPHATTN_ERR_NULL;
+    if (off(tokens, id_bytes) || off(mult, 4)) return SPHATTN_ERR_ALIGN;
+    return SPHATTN_OK;
+}
+
+struct EmbedPlan {
+    int ids, sort_groups;                          // token ids per sorting workgroup, workgroups
+    int len, pieces;                               // sorted positions per piece, pieces
+    int* first;
+    int* sorted;
+    float* partial;
+    size_t bytes;
+};
+
+EmbedPlan embed_plan(int T, int V, int D, void* workspace)
+{
+    EmbedPlan p;
+    // one sorting workgroup per CU if ids allow it: each reads all tokens whatever its share
+    p.ids = (V + kCus - 1) / kCus;
+    p.ids = p.ids < kSortMaxIds ? p.ids : kSortMaxIds;
+    p.sort_groups = (V + p.ids - 1) / p.ids;
+    // pieces of 16 positions: a wave has 16 rows to add up, eight of them under way; no run has more than 2048 pieces
+    p.len = 16;
+    while ((T + p.len - 1) / p.len > 2048) p.len *= 2;
+    p.pieces = (T + p.len - 1) / p.len;
+    Carve c(workspace);
+    p.first = c.take<int>((size_t)V + 1);
+    p.sorted = c.take<int>(T);
+    p.partial = c.take<float>((size_t)p.pieces * 2 * D);
+    p.bytes = c.used();
+    return p;
+}
+
+template <Store S>
+int run_embed_fwd(const void* tokens, int id_bytes, const void* table, const float* mult, void* O, int T, int V, int D, float scale, hipStream_t stream)
+{
+    const bool wide = !off(table, 16) && !off(O, 16) && D % per16<S>() == 0;
+    const dim3 grid((unsigned)(((long long)T + 3) / 4));
+    if (wide) hipLaunchKernelGGL((embed_fwd_kernel<S, true>), grid, dim3(kEmbedThreads), 0, stream, tokens, id_bytes, table, mult, O, T, V, D, scale);
+    else hipLaunchKernelGGL((embed_fwd_kernel<S, false>), grid, dim3(kEmbedThreads), 0, stream, tokens, id_bytes, table, mult, O, T, V, D, scale);
+    return launched();
+}
+
+template <Store S, bool WIDE>
+int run_embed_sums(const EmbedPlan& p, const void* tokens, int id_bytes, const float* mult, const void* dO, void* dtable, int V, int D, float scale, hipStream_t stream)
+{
+    const unsigned columns = (unsigned)((D + 64 * embed_lane_cols<S, WIDE>() - 1) / (64 * embed_lane_cols<S, WIDE>()));
+    hipLaunchKernelGGL((embed_sum_kernel<S, WIDE>), dim3((unsigned)(p.pieces + 3) / 4, columns), dim3(kEmbedThreads), 0, stream,
+                       tokens, id_bytes, mult, dO, p.first, p.sorted, p.partial, dtable, V, D, scale, p.len, p.pieces);
+    if (p.pieces > 1)
+        hipLaunchKernelGGL((embed_join_kernel<S, WIDE>), dim3((unsigned)p.pieces - 1, columns), dim3(kJoinThreads), 0, stream,
+                           tokens, id_bytes, p.first, p.sorted, p.partial, dtable, V, D, p.len);
+    return launched();
+}
+
+template <Store S>
+int run_embed_bwd(const EmbedPlan& p, const void* tokens, int id_bytes, const float* mult, const void* dO, void* dtable, int T, int V, int D, float scale, hipStream_t stream)
+{
+    hipLaunchKernelGGL(embed_sort_kernel, dim3((unsigned)p.sort_groups), dim3(kSortThreads), (size_t)sort_lds_bytes(p.ids), stream,
+                       tokens, id_bytes, p.first, p.sorted, dtable, T, V, p.ids, D * store_bytes<S>());
+    const int rc = launched();
+    if (rc != SPHATTN_OK || T == 0) return rc;
+    const bool wide = !off(dO, 16) && !off(dtable, 16) && D % per16<S>() == 0;
+    return wide ? run_embed_sums<S, true>(p, tokens, id_bytes, mult, dO, dtable, V, D, scale, stream)
+                : run_embed_sums<S, false>(p, tokens, id_bytes, mult, dO, dtable, V, D, scale, stream);
+}
+
+// ---- vocabulary loss ---------------------------------------------------------------------------------
+
+using Big = Tile<256, 256, 2, 4, 4>;               // eight waves of 128 x 64: one workgroup per CU
+using Mid = Tile<128, 128, 2, 2, 4>;               // four of 64 x 64: two per CU
+using Low = Tile<128, 64, 4, 1, 4>;                // up to 64 rows
+using One = Tile<128, 16, 4, 1, 6>;                // up to 16 rows
+
+constexpr size_t kPieceBytes = 256u << 20;         // of G: what the last-level cache holds
+
+bool vocab_shape(int T, int V, int D) { return T >= 0 && T <= 1 << 20 && V >= 1 && V <= 1 << 24 && D >= 1 && D <= 65536; }
+
+long long up_to(long long x, long long m) { return (x + m - 1) / m * m; }
+
+// The tile of fewest rounds of the CUs' time: a Mid tile takes 0.36 of a Big one's in a CU that runs two of them
+bool big_tiles(long long p, long long q)
+{
+    const long long big = ((p + 255) / 256) * ((q + 255) / 256), mid = ((p + 127) / 128) * ((q + 127) / 128);
+    const double big_time = (double)((big + kCus - 1) / kCus), mid_time = 0.72 * (double)((mid + 2 * kCus - 1) / (2 * kCus));
+    return big_time <= mid_time;
+}
+
+struct Vocab {
+    int T, V, D, parts, ld;                        // ld: elements per packed row
+    int piece, n_pieces, slices;                   // backward: vocabulary ids of a piece of G, slices of dX's sum
+    // workspace
+    VocabInfo* info;
+    int *rows, *place, *g_target;
+    float *g_lse2, *g, *target_logit, *dx;
+    float2* partial;
+    unsigned short *x, *w, *G;
+    size_t bytes;
+};
+
+int logit_tile_p(int T) { return T > 64 && big_tiles(1, 1) ? 256 : 128; }
+
+Vocab vocab_fwd_plan(int T, int V, int D, int dtype, void* workspace)
+{
+    Vocab p{};
+    p.T = T, p.V = V, p.D = D, p.parts = dtype == SPHATTN_F32 ? 3 : 1, p.ld = (int)up_to(D, 8);
+    Carve c(workspace);
+    p.info = c.take<VocabInfo>(1);
+    p.rows = c.take<int>(T);
+    p.place = c.take<int>(T);
+    p.target_logit = c.take<float>(T);
+    p.partial = c.take<float2>((size_t)((V + 127) / 128) * T);
+    p.x = c.take<unsigned short>((size_t)p.parts * T * p.ld);
+    // (W and X with rows that the products can read as they are need no copy, but who asks for the size knows no addresses)
+    p.w = c.take<unsigned short>((size_t)p.parts * V * p.ld);
+    p.bytes = c.used();
+    return p;
+}
+
+Vocab vocab_bwd_plan(int T, int V, int D, int dtype, void* workspace)
+{
+    Vocab p{};
+    p.T = T, p.V = V, p.D = D, p.parts = dtype == SPHATTN_F32 ? 3 : 1, p.ld = (int)up_to(D, 8);
+    const long long row_bytes = 2ll * p.parts * (T > 0 ? T : 1);
+    size_t limit = kPieceBytes;
+    if ((size_t)row_bytes * p.ld > limit) limit = (size_t)row_bytes * p.ld;
+    long long most = (long long)(limit / row_bytes) / 256 * 256;
+    most = most < 256 ? 256 : most > 1 << 18 ? 1 << 18 : most;
+    p.n_pieces = (int)((V + most - 1) / most);
+    p.piece = (int)up_to((V + p.n_pieces - 1) / p.n_pieces, 256);
+    p.n_pieces = (V + p.piece - 1) / p.piece;
+    // few tiles of dX: its sum over the vocabulary in slices
+    p.slices = 1;
+    if (p.n_pieces == 1) {
+        const long long tiles = ((T + 127) / 128) * ((D + 127) / 128);
+        while (p.slices < 64 && tiles * p.slices < kCus && V / (p.slices * 2) >= 512) p.slices *= 2;
+    }
+    Carve c(workspace);
+    p.info = c.take<VocabInfo>(1);
+    p.rows = c.take<int>(T);
+    p.place = c.take<int>(T);
+    p.g_target = c.take<int>(T);
+    p.g_lse2 = c.take<float>(T);
+    p.g = c.take<float>(T);
+    p.x = c.take<unsigned short>((size_t)p.parts * T * p.ld);
+    p.G = c.take<unsigned short>((size_t)p.parts * T * p.piece);
+    p.dx = c.take<float>((size_t)p.slices * T * p.ld);
+    p.w = c.take<unsigned short>((size_t)p.parts * V * p.ld);
+    p.bytes = c.used();
+    return p;
+}
+
+template <class T, Store S, Stage ST>
+int launch_tiles(VocabArgs& a, int p, int q, hipStream_t stream)
+{
+    const auto kern = vocab_tile_kernel<T, S, ST>;
+    if (T::LDS > 65536 && !raise_lds_limit(kern, T::LDS)) return SPHATTN_ERR_LAUNCH;
+    a.tiles_p = (p + T::BP - 1) / T::BP;
+    const long long tiles = (long long)a.tiles_p * ((q + T::BQ - 1) / T::BQ) * a.slices;
+    if (tiles > INT_MAX) return SPHATTN_ERR_SHAPE;
+    if (tiles > 0) hipLaunchKernelGGL(kern, dim3((unsigned)tiles), dim3(T::THREADS), T::LDS, stream, a);
+    return launched();
+}
+
+// logits and G: rows decide the tile
+template <Store S, Stage ST>
+int launch_scores(VocabArgs& a, int V, int T, int& tiles_p, hipStream_t stream)
+{
+    int rc;
+    if (T <= 16) rc = launch_tiles<One, S, ST>(a, V, T, stream);
+    else if (T <= 64) rc = launch_tiles<Low, S, ST>(a, V, T, stream);
+    else if (big_tiles(V, T)) rc = launch_tiles<Big, S, ST>(a, V, T, stream);
+    else rc = launch_tiles<Mid, S, ST>(a, V, T, stream);
+    tiles_p = a.tiles_p;
+    return rc;
+}
+
+template <Store S, Stage ST>
+int launch_gradient(VocabArgs& a, int p, int q, hipStream_t stream)
+{
+    if (a.slices == 1 && big_tiles(p, q)) return launch_tiles<Big, S, ST>(a, p, q, stream);
+    return launch_tiles<Mid, S, ST>(a, p, q, stream);
+}
+
+// whether the products can read rows of D elements at p as they are
+bool ready(const void* p, int D, Store S) { return S != Store::F32 && !off(p, 16) && D % 8 == 0; }
+
+template <Store S>
+Operand pack_w(const Vocab& p, const void* W, hipStream_t stream)
+{
+    if (ready(W, p.D, S)) return Operand{(const unsigned char*)W, 0, p.D * 2, p.V};
+    PackArgs k{};
+    k.in = W, k.out = p.w, k.n = p.V, k.D = p.D, k.ld = p.ld, k.part = (long long)p.V * p.ld;
+    hipLaunchKernelGGL((vocab_pack_kernel<S>), dim3((unsigned)(p.V + 3) / 4), dim3(256), 0, stream, k);
+    return Operand{(const unsigned char*)p.w, k.part * 2, p.ld * 2, p.V};
+}
+
+template <Store S>
+int run_vocab_fwd(const Vocab& p, const void* X, const void* W, const void* targets, int id_bytes, float* losses, float* lse, float* mean,
+                  float scale, int reduction, int all_rows, hipStream_t stream)
+{
+    VocabArgs a{};
+    a.Q = Operand{(const unsigned char*)X, 0, p.D * 2, p.T};
+    if (!all_rows) {
+        hipLaunchKernelGGL(vocab_rows_kernel, dim3(1), dim3(kRowsThreads), 0, stream, targets, id_bytes, p.T, p.rows, p.place, p.info,
+                           (const float*)nullptr, Reduce::None, 1.f, 0);
+        a.info = p.info, a.rows = p.rows;
+    }
+    if (!all_rows || !ready(X, p.D, S)) {
+        PackArgs k{};
+        k.in = X, k.out = p.x, k.n = p.T, k.D = p.D, k.ld = p.ld, k.part = (long long)p.T * p.ld, k.info = a.info, k.rows = a.rows;
+        hipLaunchKernelGGL((vocab_pack_kernel<S>), dim3((unsigned)(p.T + 3) / 4), dim3(256), 0, stream, k);
+        a.Q = Operand{(const unsigned char*)p.x, k.part * 2, p.ld * 2, p.T};
+    }
+    a.P = pack_w<S>(p, W, stream);
+    a.k = p.ld, a.slices = 1, a.V = p.V, a.scale2 = scale * kLog2e;
+    a.targets = targets, a.id_bytes = id_bytes;
+    a.partial = p.partial, a.partial_ld = p.T, a.target_logit = p.target_logit;
+    int tiles = 0;
+    const int rc = launch_scores<S, Stage::Logits>(a, p.V, p.T, tiles, stream);
+    if (rc != SPHATTN_OK) return rc;
+    hipLaunchKernelGGL(vocab_join_kernel, dim3((unsigned)(p.T + 63) / 64), dim3(kJoinLossThreads), 0, stream, p.partial, p.T, tiles, p.target_logit,
+                       targets, id_bytes, all_rows ? (const int*)nullptr : p.place, losses, lse, p.T, p.V);
+    if (mean && reduction != SPHATTN_LOSS_NONE)
+        hipLaunchKernelGGL(vocab_mean_kernel, dim3(1), dim3(1024), 0, stream, losses, targets, id_bytes, p.T, mean, reduction == SPHATTN_LOSS_MEAN);
+    return launched();
+}
+
+template <Store S>
+int run_vocab_bwd(const Vocab& p, const void* X, const void* W, const void* targets, int id_bytes, const float* lse, const float* dloss,
+                  void* dX, void* dW, float scale, int reduction, hipStream_t stream)
+{
+    hipLaunchKernelGGL(vocab_rows_kernel, dim3(1), dim3(kRowsThreads), 0, stream, targets, id_bytes, p.T, p.rows, p.place, p.info,
+                       dloss, (Reduce)reduction, scale, S == Store::F16);
+    PackArgs k{};
+    k.in = X, k.out = p.x, k.n = p.T, k.D = p.D, k.ld = p.ld, k.part = (long long)p.T * p.ld, k.info = p.info, k.rows = p.rows;
+    k.targets = targets, k.id_bytes = id_bytes, k.lse = lse, k.dloss = reduction == SPHATTN_LOSS_NONE ? dloss : nullptr, k.scale = scale;
+    k.g_target = p.g_target, k.g_lse2 = p.g_lse2, k.g = p.g;
+    if (p.T > 0) hipLaunchKernelGGL((vocab_pack_kernel<S>), dim3((unsigned)(p.T + 3) / 4), dim3(256), 0, stream, k);
+    const Operand x{(const unsigned char*)p.x, k.part * 2, p.ld * 2, p.T}, w = pack_w<S>(p, W, stream);
+    int rc = SPHATTN_OK;
+    for (int i = 0; i < p.n_pieces && rc == SPHATTN_OK; ++i) {
+        const int v0 = i * p.piece, n = p.V - v0 < p.piece ? p.V - v0 : p.piece;
+        const Operand wi{w.data + (size_t)v0 * w.ld, w.part, w.ld, n};
+        const Operand G{(const unsigned char*)p.G, (long long)p.T * p.piece * 2, p.piece * 2, 0};
+        VocabArgs a{};
+        a.P = wi, a.Q = x, a.info = p.info, a.k = p.ld, a.slices = 1, a.V = p.V, a.v0 = v0, a.scale2 = scale * kLog2e;
+        a.g_target = p.g_target, a.g_lse2 = p.g_lse2, a.g = p.g;
+        a.G = p.G, a.G_part = (long long)p.T * p.piece, a.G_ld = p.piece;
+        int tiles;
+        if (p.T > 0) rc = launch_scores<S, Stage::G>(a, n, p.T, tiles, stream);
+        if (rc == SPHATTN_OK && dX && p.T > 0) {
+            VocabArgs b{};
+            b.P = Operand{wi.data, wi.part, wi.ld, p.ld};
+            b.Q = G, b.Q.size = p.T, b.info = p.info, b.k = n, b.slices = p.slices;
+            b.out = p.dx, b.out_slice = (long long)p.T * p.ld, b.out_ld = p.ld, b.out_cols = p.ld, b.accumulate = i > 0;
+            rc = launch_gradient<S, Stage::Dx>(b, p.ld, p.T, stream);
+        }
+        if (rc == SPHATTN_OK && dW) {
+            VocabArgs b{};
+            b.P = Operand{x.data, x.part, x.ld, p.ld};
+            b.Q = G, b.Q.size = (int)up_to(n, 8), b.info = p.info, b.slices = 1;
+            b.out = (unsigned char*)dW + (size_t)v0 * p.D * store_bytes<S>(), b.out_ld = p.D, b.out_cols = p.D, b.out_rows = n;
+            rc = launch_gradient<S, Stage::Dw>(b, p.ld, n, stream);
+        }
+    }
+    if (rc == SPHATTN_OK && dX && p.T > 0)
+        hipLaunchKernelGGL((vocab_dx_kernel<S>), dim3((unsigned)(p.T + 3) / 4), dim3(256), 0, stream, p.dx, (long long)p.T * p.ld, p.slices, p.ld,
+                           p.place, p.info, dX, p.T, p.D);
+    return rc == SPHATTN_OK ? launched() : rc;
+}
+
+int vocab_check(const void* X, const void* W, const void* targets, int id_bytes, int T, int V, int D, float scale, int reduction, int dtype)
+{
+    if (!vocab_shape(T, V, D)) return SPHATTN_ERR_SHAPE;
+    if (!element_bytes(dtype) || (id_bytes != 4 && id_bytes != 8)) return SPHATTN_ERR_DTYPE;
+    if (!W || (T > 0 && (!X || !targets))) return SPHATTN_ERR_NULL;
+    if (off(X, element_bytes(dtype)) || off(W, element_bytes(dtype)) || off(targets, id_bytes)) return SPHATTN_ERR_ALIGN;
+    if (!std::isfinite(scale) || reduction < SPHATTN_LOSS_NONE || reduction > SPHATTN_LOSS_MEAN) return SPHATTN_ERR_VALUE;
+    return SPHATTN_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int sphattn_embed_fwd(const void* tokens, int id_bytes, const void* table, const float* mult, void* O,
+                      int T, int V, int D, float scale, int dtype, void* stream)
+{
+    const int rc = embed_check(tokens, id_bytes, mult, T, V, D, dtype);
+    if (rc != SPHATTN_OK) return rc;
+    if (!table || (T > 0 && !O)) return SPHATTN_ERR_NULL;
+    const size_t e = (size_t)element_bytes(dtype);
+    if (off(table, e) || off(O, e)) return SPHATTN_ERR_ALIGN;
+    const Range written[] = {{O, (size_t)T * D * e}};
+    const Range read[] = {{tokens, (size_t)T * id_bytes}, {table, (size_t)V * D * e}, {mult, mult ? (size_t)T * 4 : 0}};
+    if (any_meet(written, read)) return SPHATTN_ERR_ALIAS;
+    if (T == 0) return SPHATTN_OK;
+    const hipStream_t s = (hipStream_t)stream;
+    switch (dtype) {
+    case SPHATTN_F32: return run_embed_fwd<Store::F32>(tokens, id_bytes, table, mult, O, T, V, D, scale, s);
+    case SPHATTN_BF16: return run_embed_fwd<Store::Bf16>(tokens, id_bytes, table, mult, O, T, V, D, scale, s);
+    default: return run_embed_fwd<Store::F16>(tokens, id_bytes, table, mult, O, T, V, D, scale, s);
+    }
+}
+
+size_t sphattn_embed_bwd_workspace_bytes(int T, int V, int D)
+{
+    return embed_shape(T, V, D) ? embed_plan(T, V, D, nullptr).bytes : 0;
+}
+
+int sphattn_embed_bwd(const void* tokens, int id_bytes, const float* mult, const void* dO, void* dtable,
+                      int T, int V, int D, float scale, int dtype,
+                      void* workspace, size_t workspace_bytes, void* stream)
+{
+    const int rc = embed_check(tokens, id_bytes, mult, T, V, D, dtype);
+    if (rc != SPHATTN_OK) return rc;
+    if (!dtable || (T > 0 && !dO)) return SPHATTN_ERR_NULL;
+    const size_t e = (size_t)element_bytes(dtype);
+    if (off(dtable, e) || off(dO, e)) return SPHATTN_ERR_ALIGN;
+    const EmbedPlan p = embed_plan(T, V, D, workspace);
+    if (!workspace || off(workspace, 16) || workspace_bytes < p.bytes) return SPHATTN_ERR_WORKSPACE;
+    const Range written[] = {{dtable, (size_t)V * D * e}, {workspace, p.bytes}};
+    const Range read[] = {{tokens, (size_t)T * id_bytes}, {dO, (size_t)T * D * e}, {mult, mult ? (size_t)T * 4 : 0}};
+    if (any_meet(written, read)) return SPHATTN_ERR_ALIAS;
+    const hipStream_t s = (hipStream_t)stream;
+    switch (dtype) {
+    case SPHATTN_F32: return run_embed_bwd<Store::F32>(p, tokens, id_bytes, mult, dO, dtable, T, V, D, scale, s);
+    case SPHATTN_BF16: return run_embed_bwd<Store::Bf16>(p, tokens, id_bytes, mult, dO, dtable, T, V, D, scale, s);
+    default: return run_embed_bwd<Store::F16>(p, tokens, id_bytes, mult, dO, dtable, T, V, D, scale, s);
+    }
+}
+
+size_t sphattn_vocab_loss_workspace_bytes(int T, int V, int D, int dtype)
+{
+    return vocab_shape(T, V, D) && element_bytes(dtype) ? vocab_fwd_plan(T, V, D, dtype, nullptr).bytes : 0;
+}
+
+int sphattn_vocab_loss_fwd(const void* X, const void* W, const void* targets, int id_bytes,
+                           float* losses, float* lse, float* mean,
+                           int T, int V, int D, float scale, int reduction, int all_rows, int dtype,
+                           void* workspace, size_t workspace_bytes, void* stream)
+{
+    const int rc = vocab_check(X, W, targets, id_bytes, T, V, D, scale, reduction, dtype);
+    if (rc != SPHATTN_OK) return rc;
+    if (T > 0 && !losses) return SPHATTN_ERR_NULL;
+    if (off(losses, 4) || off(lse, 4) || off(mean, 4)) return SPHATTN_ERR_ALIGN;
+    const size_t e = (size_t)element_bytes(dtype);
+    const Vocab p = vocab_fwd_plan(T, V, D, dtype, workspace);
+    if (!workspace || off(workspace, 16) || workspace_bytes < p.bytes) return SPHATTN_ERR_WORKSPACE;
+    const Range written[] = {{losses, (size_t)T * 4}, {lse, lse ? (size_t)T * 4 : 0}, {mean, mean ? (size_t)4 : 0}, {workspace, p.bytes}};
+    const Range read[] = {{X, (size_t)T * D * e}, {W, (size_t)V * D * e}, {targets, (size_t)T * id_bytes}};
+    if (any_meet(written, read)) return SPHATTN_ERR_ALIAS;
+    const hipStream_t s = (hipStream_t)stream;
+    if (T == 0) {
+        if (mean && reduction != SPHATTN_LOSS_NONE)
+            hipLaunchKernelGGL(vocab_mean_kernel, dim3(1), dim3(1024), 0, s, losses, targets, id_bytes, 0, mean, 0);
+        return launched();
+    }
+    switch (dtype) {
+    case SPHATTN_F32: return run_vocab_fwd<Store::F32>(p, X, W, targets, id_bytes, losses, lse, mean, scale, reduction, all_rows, s);
+    case SPHATTN_BF16: return run_vocab_fwd<Store::Bf16>(p, X, W, targets, id_bytes, losses, lse, mean, scale, reduction, all_rows, s);
+    default: return run_vocab_fwd<Store::F16>(p, X, W, targets, id_bytes, losses, lse, mean, scale, reduction, all_rows, s);
+    }
+}
+
+size_t sphattn_vocab_loss_bwd_workspace_bytes(int T, int V, int D, int dtype)
+{
+    return vocab_shape(T, V, D) && element_bytes(dtype) ? vocab_bwd_plan(T, V, D, dtype, nullptr).bytes : 0;
+}
+
+int sphattn_vocab_loss_bwd(const void* X, const void* W, const void* targets, int id_bytes,
+                           const float* lse, const float* dloss, void* dX, void* dW,
+                           int T, int V, int D, float scale, int reduction, int dtype,
+                           void* workspace, size_t workspace_bytes, void* stream)
+{
+    const int rc = vocab_check(X, W, targets, id_bytes, T, V, D, scale, reduction, dtype);
+    if (rc != SPHATTN_OK) return rc;
+    if ((T > 0 && (!lse || !dloss)) || (!dX && !dW)) return SPHATTN_ERR_NULL;
+    const size_t e = (size_t)element_bytes(dtype);
+    if (off(lse, 4) || off(dloss, 4) || off(dX, e) || off(dW, e)) return SPHATTN_ERR_ALIGN;
+    const Vocab p = vocab_bwd_plan(T, V, D, dtype, workspace);
+    if (!workspace || off(workspace, 16) || workspace_bytes < p.bytes) return SPHATTN_ERR_WORKSPACE;
+    const Range written[] = {{dX, (size_t)T * D * e}, {dW, (size_t)V * D * e}, {workspace, p.bytes}};
+    const Range read[] = {{X, (size_t)T * D * e}, {W, (size_t)V * D * e}, {targets, (size_t)T * id_bytes}, {lse, (size_t)T * 4},
+                          {dloss, reduction == SPHATTN_LOSS_NONE ? (size_t)T * 4 : 4}};
+    if (any_meet(written, read)) return SPHATTN_ERR_ALIAS;
+    const hipStream_t s = (hipStream_t)stream;
+    switch (dtype) {
+    case SPHATTN_F32: return run_vocab_bwd<Store::F32>(p, X, W, targets, id_bytes, lse, dloss, dX, dW, scale, reduction, s);
+    case SPHATTN_BF16: return run_vocab_bwd<Store::Bf16>(p, X, W, targets, id_bytes, lse, dloss, dX, dW, scale, reduction, s);
+    default: return run_vocab_bwd<Store::F16>(p, X, W, targets, id_bytes, lse, dloss, dX, dW, scale, reduction, s);
+    }
+}
+
+size_t sphattn_clip_grads_workspace_bytes(int n)
+{
+    return n < 0 ? 0 : (size_t)((n + kClipBatch - 1) / kClipBatch + (n == 0)) * kClipMostGroups * sizeof(double);
+}
+
+int sphattn_clip_grads(const void* const* in, void* const* out, const long long* size, const int* dtype, int n,
+                       float max_norm, float* norm, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (n < 0) return SPHATTN_ERR_SHAPE;
+    if (!norm || (n > 0 && (!in || !out || !size || !dtype))) return SPHATTN_ERR_NULL;
+    if (off(norm, 4)) return SPHATTN_ERR_ALIGN;
+    if (!(max_norm >= 0.f)) return SPHATTN_ERR_VALUE;
+    for (int i = 0; i < n; ++i) {
+        const int e = element_bytes(dtype[i]);
+        if (!e) return SPHATTN_ERR_DTYPE;
+        if (size[i] < 0 || size[i] > (1ll << 40)) return SPHATTN_ERR_SHAPE;
+        if (size[i] > 0 && (!in[i] || !out[i])) return SPHATTN_ERR_NULL;
+        if (off(in[i], e) || off(out[i], e)) return SPHATTN_ERR_ALIGN;
+        const Range a{in[i], (size_t)size[i] * e}, b{out[i], a.bytes};
+        if ((in[i] != out[i] && meet(a, b)) || meet(b, {norm, 4}) || meet(b, {workspace, workspace_bytes}) || meet(a, {workspace, workspace_bytes}))
+            return SPHATTN_ERR_ALIAS;
+    }
+    if (!workspace || off(workspace, 16) || workspace_bytes < sphattn_clip_grads_workspace_bytes(n)) return SPHATTN_ERR_WORKSPACE;
+    if (meet({norm, 4}, {workspace, workspace_bytes})) return SPHATTN_ERR_ALIAS;
+
+    const hipStream_t s = (hipStream_t)stream;
+    double* sums = (double*)workspace;
+    ClipList list;
+    auto fill = [&](int i0) {
+        list.chunks = 0;
+        for (int j = 0; j < kClipBatch; ++j) {
+            const int i = i0 + j;
+            list.first[j] = i < n ? (int)list.chunks : INT_MAX;
+            if (i >= n) continue;
+            list.in[j] = in[i], list.out[j] = out[i], list.size[j] = size[i];
+            const Store t = dtype[i] == SPHATTN_F32 ? Store::F32 : dtype[i] == SPHATTN_BF16 ? Store::Bf16 : Store::F16;
+            list.type[j] = (unsigned char)((int)t | (off(in[i], 16) || off(out[i], 16) ? 0 : 128));
+            list.chunks += (size[i] + kClipChunk - 1) / kClipChunk;
+        }
+        const long long most = kClipMostGroups;
+        return (int)(list.chunks < 1 ? 1 : list.chunks < most ? list.chunks : most);
+    };
+    int n_sums = 0;
+    for (int i = 0; i < n || i == 0; i += kClipBatch) {
+        const int groups = fill(i);
+        hipLaunchKernelGGL(clip_squares_kernel, dim3((unsigned)groups), dim3(kClipThreads), 0, s, list, sums + n_sums);
+        n_sums += groups;
+    }
+    for (int i = 0; i < n || i == 0; i += kClipBatch) {
+        const int groups = fill(i);
+        hipLaunchKernelGGL(clip_scale_kernel, dim3((unsigned)groups), dim3(kClipThreads), 0, s, list, sums, n_sums, max_norm, norm, i == 0);
+    }
+    return launched();
+}
+
+}  // extern "C"

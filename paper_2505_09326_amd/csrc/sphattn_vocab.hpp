@@ -1,0 +1,640 @@
+// Cross entropy over a large vocabulary without keeping the logits, and its gradients, for gfx950.
+//
+//   l_tv = c x_t . w_v      lse_t = log sum_v exp l_tv      loss_t = lse_t - l_{t,y_t}
+//   G_tv = g_t (exp(l_tv - lse_t) - [v = y_t])      dX = c G W      dW = c G^T X
+//
+// Three kinds of matrix product run on one tile kernel:
+//   logits   each tile of T x V is reduced, in registers, to a maximum and a sum of exponentials per row
+//   G        the same tiles again for a piece of the vocabulary, each turned into 16-bit values of G in a workspace
+//   dX, dW   products of that piece with W and X, the operand whose rows run along the sum read from LDS transposed
+// The logits are formed twice (8 T V D operations for a training step instead of 6): a tile costs less than
+// writing it as fp32 and reading it back.  G is rounded to the storage type (once; half a unit in the last place, 2^-9 of a
+// term in bf16, 2^-12 in fp16), sums are in fp32 throughout.
+//
+// fp32 storage: every value is written as three bf16 parts that are exactly it (8 + 8 + 8 bits), and a product is
+// six products of parts, the small ones first, on the same kernel; the three left out come to 2^-25 of a term on
+// average and 2^-21 at most.
+#pragma once
+#include "sphattn_embed.hpp"
+#include "sphattn_pipelined.hpp"
+
+namespace sphattn {
+
+// What the host cannot know: how many rows count, and how their gradients are scaled.
+struct VocabInfo {
+    int rows;                                      // rows with a target
+    float g;                                       // gradient of every row (scalar dloss), or 0 with per-row gradients
+    float up, down;                                // power of two on G, and its inverse: fp16 holds G near 1
+};
+
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+
+// ---- tile products -------------------------------------------------------------------------------------
+
+// out[q][p] = sum_k P[p][k] Q[q][k].  An operand is stored with rows along k ("across": row k holds all p) or with
+// rows of k.  P's index lies along a lane's registers, Q's along the lanes.
+struct Operand {
+    const unsigned char* data;                     // 16-byte aligned
+    long long part;                                // bytes from one part to the next (fp32)
+    int ld;                                        // bytes per row, a multiple of 16
+    int size;                                      // valid p or q (across: columns, a multiple of 8)
+};
+
+template <int BP_, int BQ_, int WAVES_P_, int WAVES_Q_, int NBUF_>
+struct Tile {
+    static constexpr int BP = BP_, BQ = BQ_, WAVES_P = WAVES_P_, WAVES_Q = WAVES_Q_, NBUF = NBUF_;
+    static constexpr int WAVES = WAVES_P * WAVES_Q, THREADS = 64 * WAVES;
+    static constexpr int FP = BP / WAVES_P / 16, FQ = BQ / WAVES_Q / 16;      // fragments of a wave
+    // 1 KB copies per wave and step; where there are fewer blocks than waves several copy the same one (the same bytes)
+    static constexpr int CP = BP / 16 / WAVES, CQ = (BQ / 16 + WAVES - 1) / WAVES, COPIES = CP + CQ;
+    static constexpr int BUF = (BP + BQ) * 64, LDS = NBUF * BUF;
+    static_assert(CP * WAVES * 16 == BP && (CQ * WAVES * 16 == BQ || CQ == 1), "");
+};
+constexpr int kStepK = 32;
+
+// The sum over k runs in steps of 32.  A step's part of the two operands is BP / 16 + BQ / 16 blocks of 1 KB, copied
+// straight into one of NBUF LDS buffers, NBUF - 1 steps ahead; a step's fragments are read from LDS while the matrix
+// instructions of the step before run, so that behind the one barrier per step the matrix pipe has its operands already.
+template <class T, bool HALF, bool PX, bool QX, int PAIRS>
+struct Product {
+    f32x4 acc[T::FP][T::FQ];
+
+    __device__ __forceinline__ void run(const Operand& P, const Operand& Q, int p0, int q0, int k0, int k_end,
+                                        SPH_LDS unsigned char* smem)
+    {
+        const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+        const int n16 = lane & 15, g = lane >> 4;
+        const int wp = wave % T::WAVES_P, wq = wave / T::WAVES_P;
+        const uint32_t lds0 = (uint32_t)(uintptr_t)smem;
+        const int steps = (k_end - k0 + kStepK - 1) / kStepK;
+        const int total = steps * PAIRS;
+
+        // a copy's lane: row lane / 4 of the block, the 16-byte piece of its slot.  Across, slot row s of block h holds
+        // k = 8 (s / 4) + 4 h + s % 4, so that two transposing reads give a lane eight consecutive k.
+        const int row = lane >> 2, piece = block_piece_in_slot(lane);
+        int voff[T::COPIES];
+        uint32_t at[T::COPIES];                    // place in a buffer
+        auto place = [&](bool across, const Operand& A, int a0, int size, int b, int& v) {
+            if (!across) v = (b * 16 + row) * A.ld + piece * 16;
+            else {
+                const int h = b / (size / 32), cb = b % (size / 32), col = a0 + cb * 32 + piece * 8;
+                v = col < A.size ? (8 * (row >> 2) + 4 * h + (row & 3)) * A.ld + col * 2 : 0x7fffffff;
+            }
+        };
+#pragma unroll
+        for (int i = 0; i < T::COPIES; ++i) {
+            const int b = i < T::CP ? wave * T::CP + i : (wave * T::CQ + (i - T::CP)) % (T::BQ / 16);
+            place(i < T::CP ? PX : QX, i < T::CP ? P : Q, i < T::CP ? p0 : q0, i < T::CP ? T::BP : T::BQ, b, voff[i]);
+            at[i] = (i < T::CP ? 0 : T::BP * 64) + b * 1024;
+        }
+        // where the next step's part begins, and (rows of k) how many bytes or (across) how many rows are left.  All of it in
+        // scalar registers, which have no 64-bit comparisons.
+        struct Stream { const unsigned char* base; int left; };
+        auto start = [&](bool across, const Operand& A, int a0, int size, int part) {
+            const int rows = min(size, A.size - a0);
+            return across ? Stream{A.data + part * A.part + (long long)k0 * A.ld, k_end - k0}
+                          : Stream{A.data + part * A.part + (long long)a0 * A.ld + (long long)k0 * 2, rows * A.ld - k0 * 2};
+        };
+        // parts of P and Q by pair, small products first: (2,0) (0,2) (1,1) (1,0) (0,1) (0,0)
+        int pair = 0, step = 0, copied = 0;        // of the next copies
+        Stream sp = start(PX, P, p0, T::BP, PAIRS == 1 ? 0 : 2), sq = start(QX, Q, q0, T::BQ, 0);
+        uint32_t to = lds0;
+        auto words = [&](bool across, const Operand& A, const Stream& s, bool there) {
+            const int left = there ? max(s.left, 0) : 0;
+            return rsrc_words(s.base, (uint32_t)__builtin_amdgcn_readfirstlane(across ? min(left, kStepK) * A.ld : left));
+        };
+        auto copy_step = [&]() {
+            const bool there = copied < total;
+            const i32x4 rp = words(PX, P, sp, there), rq = words(QX, Q, sq, there);
+            const bool past = k0 * 2 + step * 64 + piece * 16 >= k_end * 2;   // pieces behind the end of the sum are zeros
+#pragma unroll
+            for (int i = 0; i < T::COPIES; ++i) {
+                const bool across = i < T::CP ? PX : QX;
+                const int v = !across && past ? 0x7fffffff : voff[i];
+                copy_to_lds(i < T::CP ? rp : rq, to + at[i], v, 0);
+            }
+            ++copied;
+            ++step;
+            to = to == lds0 + (T::NBUF - 1) * T::BUF ? lds0 : to + T::BUF;
+            sp.base += PX ? (long long)kStepK * P.ld : 64;
+            sp.left -= PX ? kStepK : 64;
+            sq.base += QX ? (long long)kStepK * Q.ld : 64;
+            sq.left -= QX ? kStepK : 64;
+            if (PAIRS > 1 && step == steps && copied < total) {
+                step = 0;
+                ++pair;
+                sp = start(PX, P, p0, T::BP, pair == 2 || pair == 3);
+                sq = start(QX, Q, q0, T::BQ, pair == 1 ? 2 : pair == 2 || pair == 4);
+            }
+        };
+
+        i32x4 pf[2][T::FP], qf[2][T::FQ];
+        auto fragment = [&](bool across, const SPH_LDS unsigned char* block0, int size, int i) -> i32x4 {
+            if (!across) return lds_read_b128(block0 + i * 1024 + block_piece_offset(n16, g));
+            const SPH_LDS unsigned char* b = block0 + (i >> 1) * 1024 + block_tr_offset(lane, i & 1);
+            const i32x2 lo = lds_read_tr64(b), hi = lds_read_tr64(b + size / 32 * 1024);
+            return i32x4{lo[0], lo[1], hi[0], hi[1]};
+        };
+        uint32_t from = 0;                         // buffer of the next fragments
+        auto read_step = [&](int set) {
+            const SPH_LDS unsigned char* pb = smem + from + (PX ? wp * T::FP / 2 : wp * T::FP) * 1024;
+            const SPH_LDS unsigned char* qb = smem + from + T::BP * 64 + (QX ? wq * T::FQ / 2 : wq * T::FQ) * 1024;
+#pragma unroll
+            for (int j = 0; j < T::FQ; ++j) qf[set][j] = fragment(QX, qb, T::BQ, j);
+#pragma unroll
+            for (int i = 0; i < T::FP; ++i) pf[set][i] = fragment(PX, pb, T::BP, i);
+            from = from == (T::NBUF - 1) * T::BUF ? 0 : from + T::BUF;
+        };
+        auto multiply = [&](int set) {
+#pragma unroll
+            for (int i = 0; i < T::FP; ++i)
+#pragma unroll
+                for (int j = 0; j < T::FQ; ++j) acc[i][j] = mfma16x16<HALF>(pf[set][i], qf[set][j], acc[i][j]);
+        };
+        constexpr int VM = (T::NBUF - 3) * T::COPIES;   // copies that may still be under way when the next step's have to be there
+        static_assert(T::NBUF >= 3 && VM < 64, "");
+        auto arrive = [&]() {
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_s_waitcnt(0x0F70 | (VM & 15) | ((VM >> 4) << 14));
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+        };
+
+#pragma unroll
+        for (int i = 0; i < T::FP; ++i)
+#pragma unroll
+            for (int j = 0; j < T::FQ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        // (every step is copied, those past the last one as zeros, which add nothing: the loop takes two at a time)
+#pragma unroll
+        for (int s = 0; s < T::NBUF - 2; ++s) copy_step();
+        copy_step();
+        {
+            constexpr int VM0 = (T::NBUF - 2) * T::COPIES;
+            static_assert(VM0 < 64, "");
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_s_waitcnt(0x0F70 | (VM0 & 15) | ((VM0 >> 4) << 14));
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+        }
+        read_step(0);
+        for (int s = 0; s < total; s += 2) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                arrive();                          // step s + u + 1 is there; the fragments of step s + u - 1 are used up
+                copy_step();                       // into that one's buffer
+                read_step(u ^ 1);
+                multiply(u);
+            }
+        }
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(0x0070);        // vmcnt(0), lgkmcnt(0): nothing of this lands in what follows
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    }
+};
+
+// Workgroup -> tile.  Each XCD takes a contiguous range; within it, groups of eight q tiles are walked p by p, so that the
+// workgroups that run together share operand panels in the XCD's L2.
+struct TileAt { int p, q, slice; };
+__device__ __forceinline__ TileAt tile_of(int id, int tiles_p, int tiles_q)
+{
+    constexpr int GROUP = 8;
+    const int per_slice = tiles_p * tiles_q, slice = id / per_slice;
+    id -= slice * per_slice;
+    const int per_group = GROUP * tiles_p, group = id / per_group, in = id - group * per_group;
+    const int rows = min(GROUP, tiles_q - group * GROUP);
+    return TileAt{in / rows, group * GROUP + in % rows, slice};
+}
+
+struct VocabArgs {
+    Operand P, Q;
+    const VocabInfo* info;                         // NULL: all rows of Q count
+    int k;                                         // length of the sum (dW: the rows that count)
+    int tiles_p, slices;
+    // logits and G: the vocabulary ids p0 .. of this launch, V of them in all
+    int V, v0;
+    float scale2;                                  // c log2(e)
+    const void* targets; int id_bytes; const int* rows;   // targets[rows[q]], or targets[q] without rows
+    float2* partial; int partial_ld; float* target_logit; // logits
+    const int* g_target; const float* g_lse2; const float* g;   // G, by row that counts
+    void* G; long long G_part; int G_ld;           // (elements)
+    // dX, dW
+    void* out; long long out_slice; int out_ld; int out_cols, out_rows; int accumulate;
+};
+
+enum class Stage { Logits, G, Dx, Dw };
+
+// A value as three bf16 parts, cut rather than rounded: x = hi + mid + lo exactly.
+__device__ __forceinline__ void split3(float x, uint32_t& hi, uint32_t& mid, uint32_t& lo)
+{
+    const uint32_t bits = __builtin_bit_cast(uint32_t, x);
+    if ((bits & 0x7f800000) == 0x7f800000) {       // infinite or NaN: in the first part
+        hi = (bits & 0x7fffff) ? 0x7fc0 : bits >> 16;
+        mid = lo = 0;
+        return;
+    }
+    hi = bits >> 16;
+    const float r = x - __builtin_bit_cast(float, bits & 0xffff0000);
+    const uint32_t rb = __builtin_bit_cast(uint32_t, r);
+    mid = rb >> 16;
+    lo = __builtin_bit_cast(uint32_t, r - __builtin_bit_cast(float, rb & 0xffff0000)) >> 16;
+}
+
+template <class T, Store S, Stage ST>
+__global__ __launch_bounds__(T::THREADS, 2)
+void vocab_tile_kernel(VocabArgs a)
+{
+    constexpr bool PX = ST == Stage::Dx || ST == Stage::Dw, QX = ST == Stage::Dw;
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem_raw[];
+    SPH_LDS unsigned char* smem = (SPH_LDS unsigned char*)smem_raw;
+    int rows = a.Q.size, k = a.k;
+    float down = 1.f;
+    if (a.info) {
+        rows = __builtin_amdgcn_readfirstlane(a.info->rows);
+        if constexpr (ST == Stage::Dw) down = a.info->down;
+    }
+    Operand Q = a.Q;
+    if constexpr (ST == Stage::Dw) {
+        k = rows;
+        rows = a.Q.size;
+    } else {
+        Q.size = rows;
+    }
+    const int tiles_q = (rows + T::BQ - 1) / T::BQ, n_tiles = a.tiles_p * tiles_q * a.slices;
+    if ((int)blockIdx.x >= n_tiles) return;
+    const TileAt tile = tile_of(xcd_contiguous_id(blockIdx.x, n_tiles), a.tiles_p, tiles_q);
+    // (divisions leave their results in vector registers)
+    const int p0 = __builtin_amdgcn_readfirstlane(tile.p) * T::BP, q0 = __builtin_amdgcn_readfirstlane(tile.q) * T::BQ;
+    const int per_slice = __builtin_amdgcn_readfirstlane(((k + kStepK - 1) / kStepK + a.slices - 1) / a.slices) * kStepK;
+    const int k0 = min(k, __builtin_amdgcn_readfirstlane(tile.slice) * per_slice), k1 = min(k, k0 + per_slice);
+
+    Product<T, S == Store::F16, PX, QX, S == Store::F32 ? 6 : 1> prod;
+    prod.run(a.P, Q, p0, q0, k0, k1, smem);
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int n16 = lane & 15, g = lane >> 4, wp = wave % T::WAVES_P, wq = wave / T::WAVES_P;
+    const int pw = p0 + wp * T::FP * 16, qw = q0 + wq * T::FQ * 16;     // this wave's corner
+    if constexpr (ST == Stage::Logits) {
+        SPH_LDS float* shared = (SPH_LDS float*)smem;                     // [WAVES_P][BQ][2]
+#pragma unroll
+        for (int j = 0; j < T::FQ; ++j) {
+            const int q = qw + 16 * j + n16;
+            float m = -__builtin_inff();
+#pragma unroll
+            for (int i = 0; i < T::FP; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float x = pw + 16 * i + 4 * g + r < a.P.size ? prod.acc[i][j][r] * a.scale2 : -__builtin_inff();
+                    prod.acc[i][j][r] = x;
+                    m = fmaxf(m, x);               // (a NaN is not lost: the sum has it)
+                }
+            m = max_across_groups(m);
+            const float shift = __builtin_fabsf(m) < __builtin_inff() ? m : 0.f;
+            float sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < T::FP; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) sum += __builtin_amdgcn_exp2f(prod.acc[i][j][r] - shift);
+            sum = sum_across_groups(sum);
+            if (g == 0) {
+                shared[(wp * T::BQ + q - q0) * 2] = m;
+                shared[(wp * T::BQ + q - q0) * 2 + 1] = sum;
+            }
+            if (q < rows) {
+                const int y = load_id(a.targets, a.id_bytes, a.rows ? a.rows[q] : q) - a.v0 - pw;
+                if (y >= 0 && y < T::FP * 16 && a.v0 + pw + y < a.V && ((y >> 2) & 3) == g) {
+                    float x = 0.f;
+#pragma unroll
+                    for (int i = 0; i < T::FP; ++i)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            if (y == 16 * i + 4 * g + r) x = prod.acc[i][j][r];
+                    a.target_logit[q] = x;
+                }
+            }
+        }
+        __syncthreads();
+        for (int i = tid; i < T::BQ; i += T::THREADS) {
+            if (q0 + i >= rows) continue;
+            float m = shared[i * 2], sum = 0.f;
+            for (int w = 1; w < T::WAVES_P; ++w) m = fmaxf(m, shared[(w * T::BQ + i) * 2]);
+            const float shift = __builtin_fabsf(m) < __builtin_inff() ? m : 0.f;
+            for (int w = 0; w < T::WAVES_P; ++w) {
+                const float mw = shared[(w * T::BQ + i) * 2], s = shared[(w * T::BQ + i) * 2 + 1];
+                const float sw = __builtin_fabsf(mw) < __builtin_inff() ? mw : 0.f;   // what s is relative to
+                sum += mw == -__builtin_inff() ? s : s * __builtin_amdgcn_exp2f(sw - shift);
+            }
+            a.partial[(size_t)tile.p * a.partial_ld + q0 + i] = float2{m, sum};
+        }
+    } else if constexpr (ST == Stage::G) {
+#pragma unroll
+        for (int j = 0; j < T::FQ; ++j) {
+            const int q = qw + 16 * j + n16;
+            const bool live = q < rows;
+            const int y = live ? a.g_target[q] - a.v0 : -1;
+            const float lse2 = live ? a.g_lse2[q] : 0.f, gq = live ? a.g[q] : 0.f;
+#pragma unroll
+            for (int i = 0; i < T::FP; ++i) {
+                const int v = pw + 16 * i + 4 * g;
+                float d[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float p = __builtin_amdgcn_exp2f(prod.acc[i][j][r] * a.scale2 - lse2);
+                    d[r] = v + r < a.P.size && live ? (p - (v + r == y ? 1.f : 0.f)) * gq : 0.f;
+                }
+                if (!live) continue;
+                const size_t at = (size_t)q * a.G_ld + v;
+                if constexpr (S == Store::F32) {
+                    uint32_t h[4], m[4], l[4];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) split3(d[r], h[r], m[r], l[r]);
+                    unsigned short* to = (unsigned short*)a.G + at;
+                    *(i32x2*)to = i32x2{(int)(h[0] | h[1] << 16), (int)(h[2] | h[3] << 16)};
+                    *(i32x2*)(to + a.G_part) = i32x2{(int)(m[0] | m[1] << 16), (int)(m[2] | m[3] << 16)};
+                    *(i32x2*)(to + 2 * a.G_part) = i32x2{(int)(l[0] | l[1] << 16), (int)(l[2] | l[3] << 16)};
+                } else {
+                    *(i32x2*)((unsigned short*)a.G + at) = i32x2{pack2<S == Store::F16>(d[0], d[1]), pack2<S == Store::F16>(d[2], d[3])};
+                }
+            }
+        }
+    } else {
+        // dX: fp32 sums, one array per slice or one that pieces are added to; dW: rows of the result, in its type
+        const int limit = ST == Stage::Dx ? rows : a.out_rows;
+#pragma unroll
+        for (int j = 0; j < T::FQ; ++j) {
+            const int q = qw + 16 * j + n16;
+            if (q >= limit) continue;
+#pragma unroll
+            for (int i = 0; i < T::FP; ++i) {
+                const int p = pw + 16 * i + 4 * g;
+                if (p >= a.out_cols) continue;
+                if constexpr (ST == Stage::Dx) {   // (out_ld is a multiple of 4)
+                    f32x4* to = (f32x4*)((float*)a.out + tile.slice * a.out_slice + (size_t)q * a.out_ld + p);
+                    f32x4 x = prod.acc[i][j];
+                    if (a.accumulate) x += *to;
+                    *to = x;
+                } else {
+                    const size_t at = (size_t)q * a.out_ld + p;
+                    float x[4];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) x[r] = prod.acc[i][j][r] * down;
+                    constexpr int N = S == Store::F32 ? 16 : 8;
+                    if (p + 4 <= a.out_cols && (((uintptr_t)a.out | (unsigned)(a.out_ld * store_bytes<S>())) & (N - 1)) == 0) {
+                        if constexpr (S == Store::F32) *(f32x4*)((float*)a.out + at) = f32x4{x[0], x[1], x[2], x[3]};
+                        else *(i32x2*)((short*)a.out + at) = i32x2{pack2<S == Store::F16>(x[0], x[1]), pack2<S == Store::F16>(x[2], x[3])};
+                    } else {
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            if (p + r < a.out_cols) store_el<S>(a.out, at + r, x[r]);
+                    }
+                }
+            }
+        }
+    }
+}
+
+// ---- around the products ---------------------------------------------------------------------------------
+
+// Which rows count (target >= 0), in order: rows[m] = t, place[t] = m or -1; and with `dloss` the scale of their gradients.
+// One workgroup: T ids are little beside what follows.
+constexpr int kRowsThreads = 1024;
+enum class Reduce { None, Sum, Mean };             // of dloss: [T], or one value
+
+__global__ __launch_bounds__(kRowsThreads)
+void vocab_rows_kernel(const void* __restrict__ targets, int id_bytes, int T, int* __restrict__ rows, int* __restrict__ place,
+                       VocabInfo* __restrict__ info, const float* __restrict__ dloss, Reduce reduce, float scale, int half)
+{
+    __shared__ int part[2][kRowsThreads / 64];
+    __shared__ float most[kRowsThreads / 64];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    int n = 0;
+    float top = 0.f;
+    // eight consecutive rows a thread
+    constexpr int EACH = 8;
+    int turn = 0;
+    for (long long t0 = 0; t0 < T; t0 += kRowsThreads * EACH, turn ^= 1) {
+        const long long t = t0 + tid * EACH;
+        bool counts[EACH];
+        int c = 0;
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            counts[i] = t + i < T && load_id(targets, id_bytes, t + i) >= 0;
+            c += counts[i];
+        }
+        int of_wave, at = exclusive_over_wave(c, lane, of_wave);
+        if (lane == 0) part[turn][wave] = of_wave;
+        __syncthreads();
+        int all = 0;
+        for (int w = 0; w < kRowsThreads / 64; ++w) {
+            if (w < wave) at += part[turn][w];
+            all += part[turn][w];
+        }
+        at += n;
+        n += all;
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            if (t + i >= T) break;
+            place[t + i] = counts[i] ? at : -1;
+            if (counts[i]) {
+                rows[at++] = (int)(t + i);
+                if (dloss && reduce == Reduce::None) top = fmaxf(top, __builtin_fabsf(dloss[t + i]));
+            }
+        }
+    }
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+    if (lane == 0) most[wave] = top;
+    __syncthreads();
+    if (tid != 0) return;
+    VocabInfo out{n, 0.f, 1.f, 1.f};
+    if (dloss) {
+        if (reduce == Reduce::None) {
+            for (int w = 0; w < kRowsThreads / 64; ++w) out.g = fmaxf(out.g, most[w]);
+        } else {
+            out.g = n ? (reduce == Reduce::Mean ? *dloss / (float)n : *dloss) : 0.f;
+        }
+        if (half) {
+            // the largest |c g| goes to 2^13 .. 2^14: |G| < 2^14 times what exp and 1 differ by, and a probability of 2^-28 is
+            // a normal number still
+            const float x = __builtin_fabsf(out.g * scale);
+            if (x > 0.f && x < __builtin_inff()) {
+                const int e = max(-126, min(126, 13 - (__builtin_amdgcn_frexp_expf(x) - 1)));
+                out.up = __builtin_ldexpf(1.f, e);
+                out.down = __builtin_ldexpf(1.f, -e);
+            }
+        }
+        if (reduce == Reduce::None) out.g = 0.f;
+    }
+    *info = out;
+}
+
+// Rows as the products want them: 16-bit, 16-byte aligned, whole pieces of 8; gathered by `rows` if there; fp32 in
+// three parts.  One wave per row.  With g_target: also what the G stage needs of each row.
+struct PackArgs {
+    const void* in; void* out; int n, D, ld;       // (ld: elements per row of out, a multiple of 8)
+    long long part;                                // elements from part to part
+    const VocabInfo* info; const int* rows;
+    const void* targets; int id_bytes; const float* lse; const float* dloss; float scale;
+    int* g_target; float* g_lse2; float* g;
+};
+
+template <Store S>
+__global__ __launch_bounds__(256)
+void vocab_pack_kernel(PackArgs a)
+{
+    const int lane = threadIdx.x & 63;
+    const long long m = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n = a.info ? a.info->rows : a.n;
+    if (m >= n) return;
+    const long long t = a.rows ? a.rows[m] : m;
+    if (a.g_target && lane == 0) {
+        a.g_target[m] = load_id(a.targets, a.id_bytes, t);
+        a.g_lse2[m] = a.lse[t] * kLog2e;
+        a.g[m] = (a.dloss ? a.dloss[t] : a.info->g) * a.scale * a.info->up;
+    }
+    const size_t from = (size_t)t * a.D, to = (size_t)m * a.ld;
+    constexpr int N = per16<S>();
+    const bool wide = ((uintptr_t)a.in & 15) == 0 && a.D % N == 0;
+    if (S != Store::F32 && wide) {
+        for (int c = lane; c < a.ld / 8; c += 64) ((i32x4*)a.out)[to / 8 + c] = ((const i32x4*)a.in)[from / 8 + c];
+        return;
+    }
+    for (int c = lane * 4; c < a.ld; c += 256) {
+        if constexpr (S == Store::F32) {
+            float x[4] = {0.f, 0.f, 0.f, 0.f};
+            if (wide) {
+                if (c < a.D) *(f32x4*)x = *(const f32x4*)((const float*)a.in + from + c);
+            } else {
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (c + r < a.D) x[r] = ((const float*)a.in)[from + c + r];
+            }
+            uint32_t h[4], md[4], l[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) split3(x[r], h[r], md[r], l[r]);
+            unsigned short* o = (unsigned short*)a.out + to + c;
+            *(i32x2*)o = i32x2{(int)(h[0] | h[1] << 16), (int)(h[2] | h[3] << 16)};
+            *(i32x2*)(o + a.part) = i32x2{(int)(md[0] | md[1] << 16), (int)(md[2] | md[3] << 16)};
+            *(i32x2*)(o + 2 * a.part) = i32x2{(int)(l[0] | l[1] << 16), (int)(l[2] | l[3] << 16)};
+        } else {
+            uint32_t x[4] = {0, 0, 0, 0};
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (c + r < a.D) x[r] = ((const unsigned short*)a.in)[from + c + r];
+            *(i32x2*)((unsigned short*)a.out + to + c) = i32x2{(int)(x[0] | x[1] << 16), (int)(x[2] | x[3] << 16)};
+        }
+    }
+}
+
+// The tiles' maxima and sums joined: 64 rows per workgroup, its waves a share of the tiles each.
+constexpr int kJoinLossThreads = 512;
+
+__global__ __launch_bounds__(kJoinLossThreads)
+void vocab_join_kernel(const float2* __restrict__ partial, int partial_ld, int tiles, const float* __restrict__ target_logit,
+                       const void* __restrict__ targets, int id_bytes, const int* __restrict__ place,
+                       float* __restrict__ losses, float* __restrict__ lse, int T, int V)
+{
+    constexpr int W = kJoinLossThreads / 64;
+    __shared__ float shared[2][W][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const long long t = (long long)blockIdx.x * 64 + lane;
+    const int m = t >= T ? -1 : place ? place[t] : (int)t;
+    float top = -__builtin_inff(), sum = 0.f;
+    if (m >= 0) {
+#pragma unroll 4
+        for (int i = wave; i < tiles; i += W) {
+            const float2 x = partial[(size_t)i * partial_ld + m];
+            const float now = fmaxf(top, x.x);
+            // sums are relative to a finite maximum, or to 0 where it is not finite
+            const float a = __builtin_fabsf(top) < __builtin_inff() ? top : 0.f, b = __builtin_fabsf(x.x) < __builtin_inff() ? x.x : 0.f;
+            const float c = __builtin_fabsf(now) < __builtin_inff() ? now : 0.f;
+            sum = (top == -__builtin_inff() ? sum : sum * __builtin_amdgcn_exp2f(a - c)) +
+                  (x.x == -__builtin_inff() ? x.y : x.y * __builtin_amdgcn_exp2f(b - c));
+            top = now;
+        }
+    }
+    shared[0][wave][lane] = top;
+    shared[1][wave][lane] = sum;
+    __syncthreads();
+    if (wave != 0 || t >= T) return;
+    if (m < 0) {
+        losses[t] = 0.f;
+        if (lse) lse[t] = 0.f;
+        return;
+    }
+    float now = top;
+    for (int w = 1; w < W; ++w) now = fmaxf(now, shared[0][w][lane]);
+    const float c = __builtin_fabsf(now) < __builtin_inff() ? now : 0.f;
+    float all = 0.f;
+    for (int w = 0; w < W; ++w) {
+        const float x = shared[0][w][lane], s = shared[1][w][lane];
+        all += x == -__builtin_inff() ? s : s * __builtin_amdgcn_exp2f((__builtin_fabsf(x) < __builtin_inff() ? x : 0.f) - c);
+    }
+    const float l2 = c + __builtin_amdgcn_logf(all);
+    const int y = load_id(targets, id_bytes, t);
+    if (lse) lse[t] = y >= V ? __builtin_nanf("") : l2 * kLn2;
+    losses[t] = y < 0 ? 0.f : y >= V ? __builtin_nanf("") : (l2 - target_logit[m]) * kLn2;
+}
+
+// Their sum over the rows that count and its mean: one workgroup, in fp64.  No row that counts: 0.
+__global__ __launch_bounds__(1024)
+void vocab_mean_kernel(const float* __restrict__ losses, const void* __restrict__ targets, int id_bytes, int T, float* __restrict__ mean, int divide)
+{
+    __shared__ double shared[2][16];
+    const int tid = threadIdx.x;
+    double sum = 0.0, n = 0.0;
+    for (long long t = tid; t < T; t += 1024) {
+        sum += losses[t];
+        n += load_id(targets, id_bytes, t) >= 0;
+    }
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) {
+        sum += __shfl_xor(sum, d);
+        n += __shfl_xor(n, d);
+    }
+    if ((tid & 63) == 0) {
+        shared[0][tid >> 6] = sum;
+        shared[1][tid >> 6] = n;
+    }
+    __syncthreads();
+    if (tid != 0) return;
+    for (int w = 1; w < 16; ++w) {
+        sum += shared[0][w];
+        n += shared[1][w];
+    }
+    *mean = (float)(!divide ? sum : n > 0.0 ? sum / n : 0.0);
+}
+
+// dX: the slices' sums, in order, scaled back and rounded; zeros for rows that do not count.  One wave per row.
+template <Store S>
+__global__ __launch_bounds__(256)
+void vocab_dx_kernel(const float* __restrict__ part, long long slice, int slices, int ld, const int* __restrict__ place,
+                     const VocabInfo* __restrict__ info, void* __restrict__ dX, int T, int D)
+{
+    const int lane = threadIdx.x & 63;
+    const long long t = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (t >= T) return;
+    const int m = place[t];
+    const float down = info->down;
+    const bool wide = ((uintptr_t)dX & 15) == 0 && D % 4 == 0;
+    for (int c = lane * 4; c < D; c += 256) {
+        f32x4 x = {0.f, 0.f, 0.f, 0.f};
+        if (m >= 0) {
+            const float* from = part + (size_t)m * ld + c;
+            for (int s = 0; s < slices; ++s) x += *(const f32x4*)(from + s * slice);
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x[r] *= down;
+        const size_t at = (size_t)t * D + c;
+        if (wide) {
+            if constexpr (S == Store::F32) *(f32x4*)((float*)dX + at) = x;
+            else *(i32x2*)((short*)dX + at) = i32x2{pack2<S == Store::F16>(x[0], x[1]), pack2<S == Store::F16>(x[2], x[3])};
+        } else {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (c + r < D) store_el<S>(dX, at + r, x[r]);
+        }
+    }
+}
+
+}  // namespace sphattn
