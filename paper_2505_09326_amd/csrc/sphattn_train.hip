@@ -162,7 +162,12 @@ int run_embed_bwd(const EmbedPlan& p, const void* tokens, int id_bytes, const fl
 
 // ---- vocabulary loss ---------------------------------------------------------------------------------
 
-using Big = Tile<256, 256, 2, 4, 4>;               // eight waves of 128 x 64: one workgroup per CU
+#ifdef W4
+using Big = Tile<256, 256, 2, 2, 4>;
+#else
+using Big = Tile<256, 256, 2, 4, 4>; 
+#endif
+//              // eight waves of 128 x 64: one workgroup per CU
 using Mid = Tile<128, 128, 2, 2, 4>;               // four of 64 x 64: two per CU
 using Low = Tile<128, 64, 4, 1, 4>;                // up to 64 rows
 using One = Tile<128, 16, 4, 1, 6>;                // up to 16 rows

@@ -103,16 +103,20 @@ struct Product {
             const int left = there ? max(s.left, 0) : 0;
             return rsrc_words(s.base, (uint32_t)__builtin_amdgcn_readfirstlane(across ? min(left, kStepK) * A.ld : left));
         };
-        auto copy_step = [&]() {
+        // of the step that is copied next
+        i32x4 rp, rq;
+        bool past = false;
+        auto copy_begin = [&]() {
             const bool there = copied < total;
-            const i32x4 rp = words(PX, P, sp, there), rq = words(QX, Q, sq, there);
-            const bool past = k0 * 2 + step * 64 + piece * 16 >= k_end * 2;   // pieces behind the end of the sum are zeros
-#pragma unroll
-            for (int i = 0; i < T::COPIES; ++i) {
-                const bool across = i < T::CP ? PX : QX;
-                const int v = !across && past ? 0x7fffffff : voff[i];
-                copy_to_lds(i < T::CP ? rp : rq, to + at[i], v, 0);
-            }
+            rp = words(PX, P, sp, there);
+            rq = words(QX, Q, sq, there);
+            past = k0 * 2 + step * 64 + piece * 16 >= k_end * 2;   // pieces behind the end of the sum are zeros
+        };
+        auto copy_one = [&](int i) {
+            const bool across = i < T::CP ? PX : QX;
+            copy_to_lds(i < T::CP ? rp : rq, to + at[i], !across && past ? 0x7fffffff : voff[i], 0);
+        };
+        auto copy_end = [&]() {
             ++copied;
             ++step;
             to = to == lds0 + (T::NBUF - 1) * T::BUF ? lds0 : to + T::BUF;
@@ -127,6 +131,12 @@ struct Product {
                 sq = start(QX, Q, q0, T::BQ, pair == 1 ? 2 : pair == 2 || pair == 4);
             }
         };
+        auto copy_step = [&]() {
+            copy_begin();
+#pragma unroll
+            for (int i = 0; i < T::COPIES; ++i) copy_one(i);
+            copy_end();
+        };
 
         i32x4 pf[2][T::FP], qf[2][T::FQ];
         auto fragment = [&](bool across, const SPH_LDS unsigned char* block0, int size, int i) -> i32x4 {
@@ -136,20 +146,14 @@ struct Product {
             return i32x4{lo[0], lo[1], hi[0], hi[1]};
         };
         uint32_t from = 0;                         // buffer of the next fragments
-        auto read_step = [&](int set) {
-            const SPH_LDS unsigned char* pb = smem + from + (PX ? wp * T::FP / 2 : wp * T::FP) * 1024;
-            const SPH_LDS unsigned char* qb = smem + from + T::BP * 64 + (QX ? wq * T::FQ / 2 : wq * T::FQ) * 1024;
-#pragma unroll
-            for (int j = 0; j < T::FQ; ++j) qf[set][j] = fragment(QX, qb, T::BQ, j);
-#pragma unroll
-            for (int i = 0; i < T::FP; ++i) pf[set][i] = fragment(PX, pb, T::BP, i);
-            from = from == (T::NBUF - 1) * T::BUF ? 0 : from + T::BUF;
+        auto read_one = [&](int set, int f) {      // Q's first: every product of the step needs one of them
+            if (f < T::FQ) qf[set][f] = fragment(QX, smem + from + T::BP * 64 + (QX ? wq * T::FQ / 2 : wq * T::FQ) * 1024, T::BQ, f);
+            else pf[set][f - T::FQ] = fragment(PX, smem + from + (PX ? wp * T::FP / 2 : wp * T::FP) * 1024, T::BP, f - T::FQ);
         };
-        auto multiply = [&](int set) {
-#pragma unroll
-            for (int i = 0; i < T::FP; ++i)
-#pragma unroll
-                for (int j = 0; j < T::FQ; ++j) acc[i][j] = mfma16x16<HALF>(pf[set][i], qf[set][j], acc[i][j]);
+        auto read_end = [&]() { from = from == (T::NBUF - 1) * T::BUF ? 0 : from + T::BUF; };
+        auto multiply_one = [&](int set, int m) {
+            const int i = m / T::FQ, j = m % T::FQ;
+            acc[i][j] = mfma16x16<HALF>(pf[set][i], qf[set][j], acc[i][j]);
         };
         constexpr int VM = (T::NBUF - 3) * T::COPIES;   // copies that may still be under way when the next step's have to be there
         static_assert(T::NBUF >= 3 && VM < 64, "");
@@ -176,14 +180,37 @@ struct Product {
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
         }
-        read_step(0);
+        constexpr int FRAGMENTS = T::FP + T::FQ, PRODUCTS = T::FP * T::FQ;
+#pragma unroll
+        for (int f = 0; f < FRAGMENTS; ++f) read_one(0, f);
+        read_end();
         for (int s = 0; s < total; s += 2) {
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 arrive();                          // step s + u + 1 is there; the fragments of step s + u - 1 are used up
-                copy_step();                       // into that one's buffer
-                read_step(u ^ 1);
-                multiply(u);
+                copy_begin();                      // into that one's buffer
+                // One copy, its share of the reads, its share of the products at a time.  All copies behind the barrier would
+                // queue at the memory pipe, eight waves' at once, and the products behind them in the program with them; left to
+                // itself the compiler also puts a read right before the product that needs it.
+#pragma unroll
+                for (int c = 0; c < T::COPIES; ++c) {
+                    copy_one(c);
+                    const int f0 = c * FRAGMENTS / T::COPIES, f1 = (c + 1) * FRAGMENTS / T::COPIES;
+                    const int m0 = c * PRODUCTS / T::COPIES, m1 = (c + 1) * PRODUCTS / T::COPIES;
+#pragma unroll
+                    for (int f = f0; f < f1; ++f) read_one(u ^ 1, f);
+#pragma unroll
+                    for (int m = m0; m < m1; ++m) multiply_one(u, m);
+                    const int reads = (f1 - f0) * (PX || QX ? 2 : 1);
+#pragma unroll
+                    for (int m = m0; m < m1; ++m) {
+                        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                        if (m - m0 < reads) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                copy_end();
+                read_end();
             }
         }
         asm volatile("" ::: "memory");
@@ -241,7 +268,7 @@ __device__ __forceinline__ void split3(float x, uint32_t& hi, uint32_t& mid, uin
 }
 
 template <class T, Store S, Stage ST>
-__global__ __launch_bounds__(T::THREADS, 2)
+__global__ __launch_bounds__(T::THREADS, T::FP * T::FQ > 32 ? 1 : 2)
 void vocab_tile_kernel(VocabArgs a)
 {
     constexpr bool PX = ST == Stage::Dx || ST == Stage::Dw, QX = ST == Stage::Dw;
@@ -274,43 +301,62 @@ void vocab_tile_kernel(VocabArgs a)
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n16 = lane & 15, g = lane >> 4, wp = wave % T::WAVES_P, wq = wave / T::WAVES_P;
     const int pw = p0 + wp * T::FP * 16, qw = q0 + wq * T::FQ * 16;     // this wave's corner
+    // Exponentials are in base 2, the scale and log2(e) in one factor that is not negative.  Eight waves reach the end of a
+    // tile together, so nothing hides these instructions: one maximum, one multiply-add, one exponential (16 cycles) and one addition
+    // (or half a conversion) per logit, and everything that only the vocabulary's last tile or a row's target needs is kept out of that.
+    float scale2 = a.scale2;
+    if (ST != Stage::Dx && ST != Stage::Dw && scale2 < 0.f) {
+        scale2 = -scale2;
+#pragma unroll
+        for (int i = 0; i < T::FP; ++i)
+#pragma unroll
+            for (int j = 0; j < T::FQ; ++j) prod.acc[i][j] = -prod.acc[i][j];
+    }
+    const bool whole = p0 + T::BP <= a.P.size;     // no column behind the end of the vocabulary
+    // logit y of this wave's columns and row block j, for the lane that has it
+    auto pick = [&](int j, int y) {
+        float x = 0.f;
+#pragma unroll
+        for (int i = 0; i < T::FP; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x = y == 16 * i + 4 * g + r ? prod.acc[i][j][r] : x;
+        return x;
+    };
     if constexpr (ST == Stage::Logits) {
         SPH_LDS float* shared = (SPH_LDS float*)smem;                     // [WAVES_P][BQ][2]
+        if (!whole) {
+#pragma unroll
+            for (int i = 0; i < T::FP; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (pw + 16 * i + 4 * g + r >= a.P.size)
+#pragma unroll
+                        for (int j = 0; j < T::FQ; ++j) prod.acc[i][j][r] = -__builtin_inff();
+            if (scale2 == 0.f) scale2 = 1e-38f;    // (so that minus infinity stays one)
+        }
 #pragma unroll
         for (int j = 0; j < T::FQ; ++j) {
             const int q = qw + 16 * j + n16;
-            float m = -__builtin_inff();
+            float m = prod.acc[0][j][0];           // (a NaN may get lost here: the sum has it)
 #pragma unroll
             for (int i = 0; i < T::FP; ++i)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const float x = pw + 16 * i + 4 * g + r < a.P.size ? prod.acc[i][j][r] * a.scale2 : -__builtin_inff();
-                    prod.acc[i][j][r] = x;
-                    m = fmaxf(m, x);               // (a NaN is not lost: the sum has it)
-                }
-            m = max_across_groups(m);
+                for (int r = 0; r < 4; ++r) m = fmaxf(m, prod.acc[i][j][r]);
+            m = max_across_groups(m) * scale2;
             const float shift = __builtin_fabsf(m) < __builtin_inff() ? m : 0.f;
-            float sum = 0.f;
+            float sum[2] = {0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < T::FP; ++i)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) sum += __builtin_amdgcn_exp2f(prod.acc[i][j][r] - shift);
-            sum = sum_across_groups(sum);
+                for (int r = 0; r < 4; ++r) sum[r & 1] += __builtin_amdgcn_exp2f(__builtin_fmaf(prod.acc[i][j][r], scale2, -shift));
+            const float all = sum_across_groups(sum[0] + sum[1]);
             if (g == 0) {
                 shared[(wp * T::BQ + q - q0) * 2] = m;
-                shared[(wp * T::BQ + q - q0) * 2 + 1] = sum;
+                shared[(wp * T::BQ + q - q0) * 2 + 1] = all;
             }
             if (q < rows) {
-                const int y = load_id(a.targets, a.id_bytes, a.rows ? a.rows[q] : q) - a.v0 - pw;
-                if (y >= 0 && y < T::FP * 16 && a.v0 + pw + y < a.V && ((y >> 2) & 3) == g) {
-                    float x = 0.f;
-#pragma unroll
-                    for (int i = 0; i < T::FP; ++i)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            if (y == 16 * i + 4 * g + r) x = prod.acc[i][j][r];
-                    a.target_logit[q] = x;
-                }
+                const int y = load_id(a.targets, a.id_bytes, a.rows ? a.rows[q] : q) - pw;
+                if (y >= 0 && y < T::FP * 16 && pw + y < a.V && ((y >> 2) & 3) == g) a.target_logit[q] = pick(j, y) * scale2;
             }
         }
         __syncthreads();
@@ -327,22 +373,31 @@ void vocab_tile_kernel(VocabArgs a)
             a.partial[(size_t)tile.p * a.partial_ld + q0 + i] = float2{m, sum};
         }
     } else if constexpr (ST == Stage::G) {
+        auto put = [&](size_t at, float d) {       // one element
+            if constexpr (S == Store::F32) {
+                uint32_t h, m, l;
+                split3(d, h, m, l);
+                unsigned short* to = (unsigned short*)a.G + at;
+                to[0] = (unsigned short)h, to[a.G_part] = (unsigned short)m, to[2 * a.G_part] = (unsigned short)l;
+            } else {
+                store_el<S>(a.G, at, d);
+            }
+        };
 #pragma unroll
         for (int j = 0; j < T::FQ; ++j) {
             const int q = qw + 16 * j + n16;
-            const bool live = q < rows;
-            const int y = live ? a.g_target[q] - a.v0 : -1;
-            const float lse2 = live ? a.g_lse2[q] : 0.f, gq = live ? a.g[q] : 0.f;
+            if (q >= rows) continue;
+            const float lse2 = a.g_lse2[q], gq = a.g[q];
+            const int y = a.g_target[q] - a.v0 - pw;
 #pragma unroll
             for (int i = 0; i < T::FP; ++i) {
                 const int v = pw + 16 * i + 4 * g;
                 float d[4];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const float p = __builtin_amdgcn_exp2f(prod.acc[i][j][r] * a.scale2 - lse2);
-                    d[r] = v + r < a.P.size && live ? (p - (v + r == y ? 1.f : 0.f)) * gq : 0.f;
-                }
-                if (!live) continue;
+                for (int r = 0; r < 4; ++r) d[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(prod.acc[i][j][r], scale2, -lse2)) * gq;
+                if (!whole)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) d[r] = v + r < a.P.size ? d[r] : 0.f;
                 const size_t at = (size_t)q * a.G_ld + v;
                 if constexpr (S == Store::F32) {
                     uint32_t h[4], m[4], l[4];
@@ -356,6 +411,9 @@ void vocab_tile_kernel(VocabArgs a)
                     *(i32x2*)((unsigned short*)a.G + at) = i32x2{pack2<S == Store::F16>(d[0], d[1]), pack2<S == Store::F16>(d[2], d[3])};
                 }
             }
+            // the target's own element once more, over what is there
+            if (y >= 0 && y < T::FP * 16 && pw + y < a.P.size && ((y >> 2) & 3) == g)
+                put((size_t)q * a.G_ld + pw + y, (__builtin_amdgcn_exp2f(__builtin_fmaf(pick(j, y), scale2, -lse2)) - 1.f) * gq);
         }
     } else {
         // dX: fp32 sums, one array per slice or one that pieces are added to; dW: rows of the result, in its type
