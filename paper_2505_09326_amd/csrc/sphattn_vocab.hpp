@@ -152,7 +152,7 @@ struct Product {
         };
         auto read_end = [&]() { from = from == (T::NBUF - 1) * T::BUF ? 0 : from + T::BUF; };
         auto multiply_one = [&](int set, int m) {
-            const int i = m / T::FQ, j = m % T::FQ;
+            const int i = m / T::FQ, j = i & 1 ? T::FQ - 1 - m % T::FQ : m % T::FQ;   // to and fro: one operand changes at a time
             acc[i][j] = mfma16x16<HALF>(pf[set][i], qf[set][j], acc[i][j]);
         };
         constexpr int VM = (T::NBUF - 3) * T::COPIES;   // copies that may still be under way when the next step's have to be there
