@@ -52,6 +52,9 @@ struct Tile {
 };
 constexpr int kStepK = 32;
 
+// place of 16-byte piece c in row k of an operand stored across, and the piece in place c
+__device__ __forceinline__ int across_slot(int k, int c) { return c ^ (2 * ((k & 3) | (k >> 1 & 4))); }
+
 // The sum over k runs in steps of 32.  A step's part of the two operands is BP / 16 + BQ / 16 blocks of 1 KB, copied
 // straight into one of NBUF LDS buffers, NBUF - 1 steps ahead; a step's fragments are read from LDS while the matrix
 // instructions of the step before run, so that behind the one barrier per step the matrix pipe has its operands already.
@@ -69,16 +72,17 @@ struct Product {
         const int steps = (k_end - k0 + kStepK - 1) / kStepK;
         const int total = steps * PAIRS;
 
-        // a copy's lane: row lane / 4 of the block, the 16-byte piece of its slot.  Across, slot row s of block h holds
-        // k = 8 (s / 4) + 4 h + s % 4, so that two transposing reads give a lane eight consecutive k.
+        // A copy's lane: rows of k lie in blocks of 16 x 64 bytes, lane l on row l / 4 with the piece of its slot.  Across, the buffer
+        // holds 32 whole rows of the tile, so that a copy fetches whole lines of memory, their 16-byte pieces exchanged by
+        // row (across_slot) so that the transposing reads of eight rows fall on different banks.
         const int row = lane >> 2, piece = block_piece_in_slot(lane);
         int voff[T::COPIES];
         uint32_t at[T::COPIES];                    // place in a buffer
         auto place = [&](bool across, const Operand& A, int a0, int size, int b, int& v) {
             if (!across) v = (b * 16 + row) * A.ld + piece * 16;
             else {
-                const int h = b / (size / 32), cb = b % (size / 32), col = a0 + cb * 32 + piece * 8;
-                v = col < A.size ? (8 * (row >> 2) + 4 * h + (row & 3)) * A.ld + col * 2 : 0x7fffffff;
+                const int slots = size / 8, k = (b * 64 + lane) / slots, col = a0 + across_slot(k, lane % slots) * 8;
+                v = col < A.size ? k * A.ld + col * 2 : 0x7fffffff;
             }
         };
 #pragma unroll
@@ -141,14 +145,16 @@ struct Product {
         i32x4 pf[2][T::FP], qf[2][T::FQ];
         auto fragment = [&](bool across, const SPH_LDS unsigned char* block0, int size, int i) -> i32x4 {
             if (!across) return lds_read_b128(block0 + i * 1024 + block_piece_offset(n16, g));
-            const SPH_LDS unsigned char* b = block0 + (i >> 1) * 1024 + block_tr_offset(lane, i & 1);
-            const i32x2 lo = lds_read_tr64(b), hi = lds_read_tr64(b + size / 32 * 1024);
+            // lane (i, g): rows 8 g + i / 4 and 4 more, columns 4 (i % 4) .. + 3 of the sixteen
+            const int k = 8 * g + (n16 >> 2), at = across_slot(k, 2 * i + ((lane >> 1) & 1)) * 16 + (lane & 1) * 8;
+            const SPH_LDS unsigned char* b = block0 + k * size * 2 + at;
+            const i32x2 lo = lds_read_tr64(b), hi = lds_read_tr64(b + 4 * size * 2);   // (rows k and k + 4 exchange alike)
             return i32x4{lo[0], lo[1], hi[0], hi[1]};
         };
         uint32_t from = 0;                         // buffer of the next fragments
         auto read_one = [&](int set, int f) {      // Q's first: every product of the step needs one of them
-            if (f < T::FQ) qf[set][f] = fragment(QX, smem + from + T::BP * 64 + (QX ? wq * T::FQ / 2 : wq * T::FQ) * 1024, T::BQ, f);
-            else pf[set][f - T::FQ] = fragment(PX, smem + from + (PX ? wp * T::FP / 2 : wp * T::FP) * 1024, T::BP, f - T::FQ);
+            if (f < T::FQ) qf[set][f] = fragment(QX, smem + from + T::BP * 64 + (QX ? 0 : wq * T::FQ * 1024), T::BQ, QX ? wq * T::FQ + f : f);
+            else pf[set][f - T::FQ] = fragment(PX, smem + from + (PX ? 0 : wp * T::FP * 1024), T::BP, PX ? wp * T::FP + f - T::FQ : f - T::FQ);
         };
         auto read_end = [&]() { from = from == (T::NBUF - 1) * T::BUF ? 0 : from + T::BUF; };
         auto multiply_one = [&](int set, int m) {
