@@ -142,7 +142,7 @@ struct Product {
             copy_end();
         };
 
-        i32x4 pf[2][T::FP], qf[2][T::FQ];
+        i32x4 pf[T::FP], qf[2][T::FQ];
         auto fragment = [&](bool across, const SPH_LDS unsigned char* block0, int size, int i) -> i32x4 {
             if (!across) return lds_read_b128(block0 + i * 1024 + block_piece_offset(n16, g));
             // lane (i, g): rows 8 g + i / 4 and 4 more, columns 4 (i % 4) .. + 3 of the sixteen
@@ -151,16 +151,13 @@ struct Product {
             const i32x2 lo = lds_read_tr64(b), hi = lds_read_tr64(b + 4 * size * 2);   // (rows k and k + 4 exchange alike)
             return i32x4{lo[0], lo[1], hi[0], hi[1]};
         };
-        uint32_t from = 0;                         // buffer of the next fragments
-        auto read_one = [&](int set, int f) {      // Q's first: every product of the step needs one of them
-            if (f < T::FQ) qf[set][f] = fragment(QX, smem + from + T::BP * 64 + (QX ? 0 : wq * T::FQ * 1024), T::BQ, QX ? wq * T::FQ + f : f);
-            else pf[set][f - T::FQ] = fragment(PX, smem + from + (PX ? 0 : wp * T::FP * 1024), T::BP, PX ? wp * T::FP + f - T::FQ : f - T::FQ);
+        auto read_p = [&](uint32_t from, int i) {
+            pf[i] = fragment(PX, smem + from + (PX ? 0 : wp * T::FP * 1024), T::BP, PX ? wp * T::FP + i : i);
         };
-        auto read_end = [&]() { from = from == (T::NBUF - 1) * T::BUF ? 0 : from + T::BUF; };
-        auto multiply_one = [&](int set, int m) {
-            const int i = m / T::FQ, j = i & 1 ? T::FQ - 1 - m % T::FQ : m % T::FQ;   // to and fro: one operand changes at a time
-            acc[i][j] = mfma16x16<HALF>(pf[set][i], qf[set][j], acc[i][j]);
+        auto read_q = [&](uint32_t from, int set, int j) {
+            qf[set][j] = fragment(QX, smem + from + T::BP * 64 + (QX ? 0 : wq * T::FQ * 1024), T::BQ, QX ? wq * T::FQ + j : j);
         };
+        auto behind = [](uint32_t from) { return from == (T::NBUF - 1) * T::BUF ? 0u : from + T::BUF; };
         constexpr int VM = (T::NBUF - 3) * T::COPIES;   // copies that may still be under way when the next step's have to be there
         static_assert(T::NBUF >= 3 && VM < 64, "");
         auto arrive = [&]() {
@@ -186,37 +183,46 @@ struct Product {
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
         }
-        constexpr int FRAGMENTS = T::FP + T::FQ, PRODUCTS = T::FP * T::FQ;
+        uint32_t from = 0;                         // buffer of step s
 #pragma unroll
-        for (int f = 0; f < FRAGMENTS; ++f) read_one(0, f);
-        read_end();
+        for (int j = 0; j < T::FQ; ++j) read_q(from, 0, j);
+#pragma unroll
+        for (int i = 0; i < T::FP - 1; ++i) read_p(from, i);
         for (int s = 0; s < total; s += 2) {
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 arrive();                          // step s + u + 1 is there; the fragments of step s + u - 1 are used up
                 copy_begin();                      // into that one's buffer
-                // One copy, its share of the reads, its share of the products at a time.  All copies behind the barrier would
-                // queue at the memory pipe, eight waves' at once, and the products behind them in the program with them; left to
-                // itself the compiler also puts a read right before the product that needs it.
+                const uint32_t next = behind(from);
+                // One P fragment with all of Q at a time, and beside these products a share of the step's copies and of the reads for the
+                // next one.  All copies behind the barrier would queue at the memory pipe, eight waves' at once, and the products
+                // behind them in the program with them; left to itself the compiler also puts a read right before the product that
+                // needs it.  A P fragment is used up when its products are done and makes place for the next step's (the last
+                // one's place is taken a step later); Q's are needed to the end and have two sets.
 #pragma unroll
-                for (int c = 0; c < T::COPIES; ++c) {
-                    copy_one(c);
-                    const int f0 = c * FRAGMENTS / T::COPIES, f1 = (c + 1) * FRAGMENTS / T::COPIES;
-                    const int m0 = c * PRODUCTS / T::COPIES, m1 = (c + 1) * PRODUCTS / T::COPIES;
+                for (int i = 0; i < T::FP; ++i) {
 #pragma unroll
-                    for (int f = f0; f < f1; ++f) read_one(u ^ 1, f);
+                    for (int c = i * T::COPIES / T::FP; c < (i + 1) * T::COPIES / T::FP; ++c) copy_one(c);
+                    if (i == 0) read_p(from, T::FP - 1);
+                    else read_p(next, i - 1);
+                    const int q0f = i * T::FQ / T::FP, q1f = (i + 1) * T::FQ / T::FP;
 #pragma unroll
-                    for (int m = m0; m < m1; ++m) multiply_one(u, m);
-                    const int reads = (f1 - f0) * (PX || QX ? 2 : 1);
+                    for (int j = q0f; j < q1f; ++j) read_q(next, u ^ 1, j);
 #pragma unroll
-                    for (int m = m0; m < m1; ++m) {
+                    for (int j = 0; j < T::FQ; ++j) {   // to and fro: one operand changes at a time
+                        const int jj = i & 1 ? T::FQ - 1 - j : j;
+                        acc[i][jj] = mfma16x16<HALF>(pf[i], qf[u][jj], acc[i][jj]);
+                    }
+                    const int reads = (PX ? 2 : 1) + (q1f - q0f) * (QX ? 2 : 1);
+#pragma unroll
+                    for (int j = 0; j < T::FQ; ++j) {
                         __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-                        if (m - m0 < reads) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                        if (j < reads) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
                     }
                     __builtin_amdgcn_sched_barrier(0);
                 }
                 copy_end();
-                read_end();
+                from = next;
             }
         }
         asm volatile("" ::: "memory");
