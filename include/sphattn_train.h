@@ -88,7 +88,8 @@ int sphattn_vocab_loss_bwd(const void* X, const void* W, const void* targets, in
  * Clipping of gradients by their common 2-norm:
  *   norm = sqrt(sum over all elements of all tensors of in^2)      out[i] = in[i] * min(1, max_norm / (norm + 1e-6))
  *   in, out : host arrays of n device pointers; out[i] may be in[i] (then it is not written where the factor
- *             is 1) and overlaps no other tensor (not checked).  Tensor i has size[i] >= 0 elements of type dtype[i].
+ *             is 1) and overlaps no other tensor (not checked).  Tensor i has size[i] >= 0 elements of type dtype[i],
+ *             2^40 in all at most (SPHATTN_ERR_SHAPE).
  *   norm    : device, one fp32; written by the call.  Squares are added in fp64; a norm that is not
  *             finite gives a factor of 0 (infinite) or NaN, as the formula does.
  *   max_norm: >= 0 (SPHATTN_ERR_VALUE for negative ones and NaN).  n >= 0; the host arrays are read before the call returns.

@@ -12,6 +12,7 @@ namespace sphattn {
 
 constexpr int kClipThreads = 256, kClipBatch = 120;
 constexpr int kClipChunk = 8192;                   // elements that a workgroup takes at a time, of one tensor
+constexpr long long kClipMostElements = 1ll << 40; // of a call: chunk numbers are ints
 constexpr int kClipMostGroups = 1024;              // workgroups of a launch: four per CU
 
 struct ClipList {

@@ -80,40 +80,41 @@ void embed_fwd_kernel(const void* __restrict__ tokens, int id_bytes, const void*
                       const float* __restrict__ mult, void* __restrict__ O, int T, int V, int D, float scale)
 {
     const int lane = threadIdx.x & 63;
-    const long long row = (long long)blockIdx.x * (kEmbedThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if (row >= T) return;
-    const int v = load_id(tokens, id_bytes, row);
-    // no token: zeros; not a token of this table: NaN.  Both without reading the table.
-    const bool in = v >= 0 && v < V;
-    const float f = in ? (mult ? mult[row] * scale : scale) : 0.f;
-    const float fill = v < 0 ? 0.f : __builtin_nanf("");
-    if constexpr (WIDE) {
-        constexpr int N = per16<S>(), AHEAD = 4;
-        const int pieces = D / N;
-        const i32x4* src = (const i32x4*)table + (size_t)(in ? v : 0) * pieces;
-        i32x4* dst = (i32x4*)O + (size_t)row * pieces;
-        for (int c0 = 0; c0 < pieces; c0 += 64 * AHEAD) {
-            i32x4 w[AHEAD];
+    constexpr int WAVES = kEmbedThreads / 64;
+    for (long long row = (long long)blockIdx.x * WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); row < T; row += (long long)gridDim.x * WAVES) {
+        const int v = load_id(tokens, id_bytes, row);
+        // no token: zeros; not a token of this table: NaN.  Both without reading the table.
+        const bool in = v >= 0 && v < V;
+        const float f = in ? (mult ? mult[row] * scale : scale) : 0.f;
+        const float fill = v < 0 ? 0.f : __builtin_nanf("");
+        if constexpr (WIDE) {
+            constexpr int N = per16<S>(), AHEAD = 4;
+            const int pieces = D / N;
+            const i32x4* src = (const i32x4*)table + (size_t)(in ? v : 0) * pieces;
+            i32x4* dst = (i32x4*)O + (size_t)row * pieces;
+            for (int c0 = 0; c0 < pieces; c0 += 64 * AHEAD) {
+                i32x4 w[AHEAD];
 #pragma unroll
-            for (int a = 0; a < AHEAD; ++a) {
-                const int c = c0 + a * 64 + lane;
-                w[a] = i32x4{0, 0, 0, 0};
-                if (in && c < pieces) w[a] = src[c];
+                for (int a = 0; a < AHEAD; ++a) {
+                    const int c = c0 + a * 64 + lane;
+                    w[a] = i32x4{0, 0, 0, 0};
+                    if (in && c < pieces) w[a] = src[c];
+                }
+#pragma unroll
+                for (int a = 0; a < AHEAD; ++a) {
+                    const int c = c0 + a * 64 + lane;
+                    float x[N];
+                    widen16<S>(w[a], x);
+#pragma unroll
+                    for (int i = 0; i < N; ++i) x[i] = in ? x[i] * f : fill;
+                    if (c < pieces) dst[c] = narrow16<S>(x);
+                }
             }
-#pragma unroll
-            for (int a = 0; a < AHEAD; ++a) {
-                const int c = c0 + a * 64 + lane;
-                float x[N];
-                widen16<S>(w[a], x);
-#pragma unroll
-                for (int i = 0; i < N; ++i) x[i] = in ? x[i] * f : fill;
-                if (c < pieces) dst[c] = narrow16<S>(x);
+        } else {
+            for (int c = lane; c < D; c += 64) {
+                const float x = in ? load_el<S>(table, (size_t)v * D + c) * f : fill;
+                store_el<S>(O, (size_t)row * D + c, x);
             }
-        }
-    } else {
-        for (int c = lane; c < D; c += 64) {
-            const float x = in ? load_el<S>(table, (size_t)v * D + c) * f : fill;
-            store_el<S>(O, (size_t)row * D + c, x);
         }
     }
 }

@@ -49,11 +49,11 @@ int element_bytes(int dtype)
 
 int launched() { return hipGetLastError() == hipSuccess ? SPHATTN_OK : SPHATTN_ERR_LAUNCH; }
 
-// A kernel with more than 64 KB of LDS needs its limit raised once per device.
+// A kernel with more than 64 KB of LDS needs its limit raised once per device.  `done` is the kernel's own: kernels of one type
+// share whatever a template over the type keeps.
 template <typename Kern>
-bool raise_lds_limit(Kern kern, int lds_bytes)
+bool raise_lds_limit(Kern kern, int lds_bytes, std::atomic<uint64_t>& done)
 {
-    static std::atomic<uint64_t> done{0};
     int dev = 0;
     if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) {
         (void)hipGetLastError();
@@ -116,8 +116,8 @@ EmbedPlan embed_plan(int T, int V, int D, void* workspace)
     p.sort_groups = (V + p.ids - 1) / p.ids;
     // pieces of 16 positions: a wave has 16 rows to add up, eight of them under way; no run has more than 2048 pieces
     p.len = 16;
-    while ((T + p.len - 1) / p.len > 2048) p.len *= 2;
-    p.pieces = (T + p.len - 1) / p.len;
+    while (((long long)T + p.len - 1) / p.len > 2048) p.len *= 2;
+    p.pieces = (int)(((long long)T + p.len - 1) / p.len);
     Carve c(workspace);
     p.first = c.take<int>((size_t)V + 1);
     p.sorted = c.take<int>(T);
@@ -130,7 +130,8 @@ template <Store S>
 int run_embed_fwd(const void* tokens, int id_bytes, const void* table, const float* mult, void* O, int T, int V, int D, float scale, hipStream_t stream)
 {
     const bool wide = !off(table, 16) && !off(O, 16) && D % per16<S>() == 0;
-    const dim3 grid((unsigned)(((long long)T + 3) / 4));
+    const long long groups = ((long long)T + 3) / 4, most = 1 << 22;   // (a launch has less than 2^32 threads)
+    const dim3 grid((unsigned)(groups < most ? groups : most));
     if (wide) hipLaunchKernelGGL((embed_fwd_kernel<S, true>), grid, dim3(kEmbedThreads), 0, stream, tokens, id_bytes, table, mult, O, T, V, D, scale);
     else hipLaunchKernelGGL((embed_fwd_kernel<S, false>), grid, dim3(kEmbedThreads), 0, stream, tokens, id_bytes, table, mult, O, T, V, D, scale);
     return launched();
@@ -162,12 +163,7 @@ int run_embed_bwd(const EmbedPlan& p, const void* tokens, int id_bytes, const fl
 
 // ---- vocabulary loss ---------------------------------------------------------------------------------
 
-#ifdef W4
-using Big = Tile<256, 256, 2, 2, 4>;
-#else
-using Big = Tile<256, 256, 2, 4, 4>; 
-#endif
-//              // eight waves of 128 x 64: one workgroup per CU
+using Big = Tile<256, 256, 2, 4, 4>;               // eight waves of 128 x 64: one workgroup per CU
 using Mid = Tile<128, 128, 2, 2, 4>;               // four of 64 x 64: two per CU
 using Low = Tile<128, 64, 4, 1, 4>;                // up to 64 rows
 using One = Tile<128, 16, 4, 1, 6>;                // up to 16 rows
@@ -188,7 +184,8 @@ bool big_tiles(long long p, long long q)
 
 struct Vocab {
     int T, V, D, parts, ld;                        // ld: elements per packed row
-    int piece, n_pieces, slices;                   // backward: vocabulary ids of a piece of G, slices of dX's sum
+    int piece, n_pieces;                           // backward: vocabulary ids of a piece of G
+    bool dx_big; int slices;                       // dX: its tile, slices of its sum over a piece
     // workspace
     VocabInfo* info;
     int *rows, *place, *g_target;
@@ -198,7 +195,22 @@ struct Vocab {
     size_t bytes;
 };
 
-int logit_tile_p(int T) { return T > 64 && big_tiles(1, 1) ? 256 : 128; }
+// dX's tile and the slices of its sum over n ids, by the time that its rounds take: in a round of 256 Big tiles each takes 27 ns per id,
+// in one of 512 Mid tiles 20, and every slice is written and read again as fp32.  (8192 rows, width 1024: 512 Mid tiles 338 us per 16384 ids,
+// 256 Big ones in two slices 225.)
+void dx_choice(long long T, long long ld, int n, bool& big, int& slices)
+{
+    double best = 0.0;
+    for (int b = 1; b >= 0; --b) {
+        const int tile = b ? 256 : 128, at_once = b ? kCus : 2 * kCus;
+        const long long tiles = ((T + tile - 1) / tile) * ((ld + tile - 1) / tile);
+        for (int s = 1; s <= 64 && (s == 1 || n / s >= 512); s *= 2) {
+            const double rounds = (double)((tiles * s + at_once - 1) / at_once);
+            const double us = rounds * (n / s) * (b ? 0.027 : 0.020) + s * (double)(T * ld) * 8.0 / 4.5e6;
+            if (best == 0.0 || us < best) best = us, big = b, slices = s;
+        }
+    }
+}
 
 Vocab vocab_fwd_plan(int T, int V, int D, int dtype, void* workspace)
 {
@@ -229,12 +241,7 @@ Vocab vocab_bwd_plan(int T, int V, int D, int dtype, void* workspace)
     p.n_pieces = (int)((V + most - 1) / most);
     p.piece = (int)up_to((V + p.n_pieces - 1) / p.n_pieces, 256);
     p.n_pieces = (V + p.piece - 1) / p.piece;
-    // few tiles of dX: its sum over the vocabulary in slices
-    p.slices = 1;
-    if (p.n_pieces == 1) {
-        const long long tiles = ((T + 127) / 128) * ((D + 127) / 128);
-        while (p.slices < 64 && tiles * p.slices < kCus && V / (p.slices * 2) >= 512) p.slices *= 2;
-    }
+    dx_choice(T > 0 ? T : 1, p.ld, p.piece < V ? p.piece : V, p.dx_big, p.slices);
     Carve c(workspace);
     p.info = c.take<VocabInfo>(1);
     p.rows = c.take<int>(T);
@@ -254,11 +261,17 @@ template <class T, Store S, Stage ST>
 int launch_tiles(VocabArgs& a, int p, int q, hipStream_t stream)
 {
     const auto kern = vocab_tile_kernel<T, S, ST>;
-    if (T::LDS > 65536 && !raise_lds_limit(kern, T::LDS)) return SPHATTN_ERR_LAUNCH;
+    static std::atomic<uint64_t> done{0};
+    if (T::LDS > 65536 && !raise_lds_limit(kern, T::LDS, done)) return SPHATTN_ERR_LAUNCH;
     a.tiles_p = (p + T::BP - 1) / T::BP;
     const long long tiles = (long long)a.tiles_p * ((q + T::BQ - 1) / T::BQ) * a.slices;
     if (tiles > INT_MAX) return SPHATTN_ERR_SHAPE;
-    if (tiles > 0) hipLaunchKernelGGL(kern, dim3((unsigned)tiles), dim3(T::THREADS), T::LDS, stream, a);
+    // (a launch has less than 2^32 threads)
+    constexpr long long MOST = 1 << 22;
+    for (long long first = 0; first < tiles; first += MOST) {
+        a.first = (int)first;
+        hipLaunchKernelGGL(kern, dim3((unsigned)(tiles - first < MOST ? tiles - first : MOST)), dim3(T::THREADS), T::LDS, stream, a);
+    }
     return launched();
 }
 
@@ -273,13 +286,6 @@ int launch_scores(VocabArgs& a, int V, int T, int& tiles_p, hipStream_t stream)
     else rc = launch_tiles<Mid, S, ST>(a, V, T, stream);
     tiles_p = a.tiles_p;
     return rc;
-}
-
-template <Store S, Stage ST>
-int launch_gradient(VocabArgs& a, int p, int q, hipStream_t stream)
-{
-    if (a.slices == 1 && big_tiles(p, q)) return launch_tiles<Big, S, ST>(a, p, q, stream);
-    return launch_tiles<Mid, S, ST>(a, p, q, stream);
 }
 
 // whether the products can read rows of D elements at p as they are
@@ -319,7 +325,10 @@ int run_vocab_fwd(const Vocab& p, const void* X, const void* W, const void* targ
     int tiles = 0;
     const int rc = launch_scores<S, Stage::Logits>(a, p.V, p.T, tiles, stream);
     if (rc != SPHATTN_OK) return rc;
-    hipLaunchKernelGGL(vocab_join_kernel, dim3((unsigned)(p.T + 63) / 64), dim3(kJoinLossThreads), 0, stream, p.partial, p.T, tiles, p.target_logit,
+    int log_rows = 0;                              // rows of a joining workgroup: half a round of the CUs where they are few
+    while (log_rows < 6 && (p.T >> log_rows) > kCus / 2) ++log_rows;
+    hipLaunchKernelGGL(vocab_join_kernel, dim3((unsigned)(p.T + (1 << log_rows) - 1) >> log_rows), dim3(kJoinLossThreads), 0, stream, p.partial, p.T, tiles,
+                       log_rows, p.target_logit,
                        targets, id_bytes, all_rows ? (const int*)nullptr : p.place, losses, lse, p.T, p.V);
     if (mean && reduction != SPHATTN_LOSS_NONE)
         hipLaunchKernelGGL(vocab_mean_kernel, dim3(1), dim3(1024), 0, stream, losses, targets, id_bytes, p.T, mean, reduction == SPHATTN_LOSS_MEAN);
@@ -339,6 +348,7 @@ int run_vocab_bwd(const Vocab& p, const void* X, const void* W, const void* targ
     if (p.T > 0) hipLaunchKernelGGL((vocab_pack_kernel<S>), dim3((unsigned)(p.T + 3) / 4), dim3(256), 0, stream, k);
     const Operand x{(const unsigned char*)p.x, k.part * 2, p.ld * 2, p.T}, w = pack_w<S>(p, W, stream);
     int rc = SPHATTN_OK;
+    const int dx_tile = p.dx_big ? 256 : 128, dx_at_once = p.dx_big ? kCus : 2 * kCus;
     for (int i = 0; i < p.n_pieces && rc == SPHATTN_OK; ++i) {
         const int v0 = i * p.piece, n = p.V - v0 < p.piece ? p.V - v0 : p.piece;
         const Operand wi{w.data + (size_t)v0 * w.ld, w.part, w.ld, n};
@@ -353,20 +363,21 @@ int run_vocab_bwd(const Vocab& p, const void* X, const void* W, const void* targ
             VocabArgs b{};
             b.P = Operand{wi.data, wi.part, wi.ld, p.ld};
             b.Q = G, b.Q.size = p.T, b.info = p.info, b.k = n, b.slices = p.slices;
-            b.out = p.dx, b.out_slice = (long long)p.T * p.ld, b.out_ld = p.ld, b.out_cols = p.ld, b.accumulate = i > 0;
-            rc = launch_gradient<S, Stage::Dx>(b, p.ld, p.T, stream);
+            b.T = p.T, b.target = dx_at_once;
+            b.out = p.dx, b.out_ld = p.ld, b.out_cols = p.ld, b.accumulate = i > 0;
+            rc = p.dx_big ? launch_tiles<Big, S, Stage::Dx>(b, p.ld, p.T, stream) : launch_tiles<Mid, S, Stage::Dx>(b, p.ld, p.T, stream);
         }
         if (rc == SPHATTN_OK && dW) {
             VocabArgs b{};
             b.P = Operand{x.data, x.part, x.ld, p.ld};
             b.Q = G, b.Q.size = (int)up_to(n, 8), b.info = p.info, b.slices = 1;
             b.out = (unsigned char*)dW + (size_t)v0 * p.D * store_bytes<S>(), b.out_ld = p.D, b.out_cols = p.D, b.out_rows = n;
-            rc = launch_gradient<S, Stage::Dw>(b, p.ld, n, stream);
+            rc = big_tiles(p.ld, n) ? launch_tiles<Big, S, Stage::Dw>(b, p.ld, n, stream) : launch_tiles<Mid, S, Stage::Dw>(b, p.ld, n, stream);
         }
     }
     if (rc == SPHATTN_OK && dX && p.T > 0)
-        hipLaunchKernelGGL((vocab_dx_kernel<S>), dim3((unsigned)(p.T + 3) / 4), dim3(256), 0, stream, p.dx, (long long)p.T * p.ld, p.slices, p.ld,
-                           p.place, p.info, dX, p.T, p.D);
+        hipLaunchKernelGGL((vocab_dx_kernel<S>), dim3((unsigned)(p.T + 3) / 4), dim3(256), 0, stream, p.dx, p.slices, p.ld,
+                           dx_tile, (p.ld + dx_tile - 1) / dx_tile, dx_at_once, p.place, p.info, dX, p.T, p.D);
     return rc == SPHATTN_OK ? launched() : rc;
 }
 
@@ -495,7 +506,7 @@ int sphattn_vocab_loss_bwd(const void* X, const void* W, const void* targets, in
 
 size_t sphattn_clip_grads_workspace_bytes(int n)
 {
-    return n < 0 ? 0 : (size_t)((n + kClipBatch - 1) / kClipBatch + (n == 0)) * kClipMostGroups * sizeof(double);
+    return n < 0 ? 0 : (((size_t)n + kClipBatch - 1) / kClipBatch + (n == 0)) * kClipMostGroups * sizeof(double);
 }
 
 int sphattn_clip_grads(const void* const* in, void* const* out, const long long* size, const int* dtype, int n,
@@ -505,14 +516,16 @@ int sphattn_clip_grads(const void* const* in, void* const* out, const long long*
     if (!norm || (n > 0 && (!in || !out || !size || !dtype))) return SPHATTN_ERR_NULL;
     if (off(norm, 4)) return SPHATTN_ERR_ALIGN;
     if (!(max_norm >= 0.f)) return SPHATTN_ERR_VALUE;
+    long long elements = 0;
     for (int i = 0; i < n; ++i) {
         const int e = element_bytes(dtype[i]);
         if (!e) return SPHATTN_ERR_DTYPE;
-        if (size[i] < 0 || size[i] > (1ll << 40)) return SPHATTN_ERR_SHAPE;
+        if (size[i] < 0 || size[i] > kClipMostElements - elements) return SPHATTN_ERR_SHAPE;
+        elements += size[i];
         if (size[i] > 0 && (!in[i] || !out[i])) return SPHATTN_ERR_NULL;
         if (off(in[i], e) || off(out[i], e)) return SPHATTN_ERR_ALIGN;
         const Range a{in[i], (size_t)size[i] * e}, b{out[i], a.bytes};
-        if ((in[i] != out[i] && meet(a, b)) || meet(b, {norm, 4}) || meet(b, {workspace, workspace_bytes}) || meet(a, {workspace, workspace_bytes}))
+        if ((in[i] != out[i] && meet(a, b)) || meet(a, {norm, 4}) || meet(b, {norm, 4}) || meet(b, {workspace, workspace_bytes}) || meet(a, {workspace, workspace_bytes}))
             return SPHATTN_ERR_ALIAS;
     }
     if (!workspace || off(workspace, 16) || workspace_bytes < sphattn_clip_grads_workspace_bytes(n)) return SPHATTN_ERR_WORKSPACE;

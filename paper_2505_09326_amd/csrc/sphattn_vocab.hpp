@@ -2,6 +2,7 @@
 //
 //   l_tv = c x_t . w_v      lse_t = log sum_v exp l_tv      loss_t = lse_t - l_{t,y_t}
 //   G_tv = g_t (exp(l_tv - lse_t) - [v = y_t])      dX = c G W      dW = c G^T X
+// (one g for all rows and c are applied to the sums instead)
 //
 // Three kinds of matrix product run on one tile kernel:
 //   logits   each tile of T x V is reduced, in registers, to a maximum and a sum of exponentials per row
@@ -23,8 +24,8 @@ namespace sphattn {
 // What the host cannot know: how many rows count, and how their gradients are scaled.
 struct VocabInfo {
     int rows;                                      // rows with a target
-    float g;                                       // gradient of every row (scalar dloss), or 0 with per-row gradients
-    float up, down;                                // power of two on G, and its inverse: fp16 holds G near 1
+    float up;                                      // factor of G in the workspace: a power of two (fp16 holds G near 2^14 with it)
+    float down;                                    // factor of the sums behind it
 };
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
@@ -249,7 +250,9 @@ struct VocabArgs {
     Operand P, Q;
     const VocabInfo* info;                         // NULL: all rows of Q count
     int k;                                         // length of the sum (dW: the rows that count)
+    int first;                                     // tile of the launch's first workgroup
     int tiles_p, slices;
+    int T, target;                                 // dX: rows that the slices' arrays are made for, workgroups that the chip runs at once
     // logits and G: the vocabulary ids p0 .. of this launch, V of them in all
     int V, v0;
     float scale2;                                  // c log2(e)
@@ -258,10 +261,21 @@ struct VocabArgs {
     const int* g_target; const float* g_lse2; const float* g;   // G, by row that counts
     void* G; long long G_part; int G_ld;           // (elements)
     // dX, dW
-    void* out; long long out_slice; int out_ld; int out_cols, out_rows; int accumulate;
+    void* out; int out_ld; int out_cols, out_rows; int accumulate;   // (dX: slice after slice, `rows` rows each)
 };
 
 enum class Stage { Logits, G, Dx, Dw };
+
+// Slices of dX's sum over the vocabulary for `rows` rows that count, where a launch for T of them has `slices`: as many more as
+// workgroups and arrays of partial sums are then free, while the chip is not full.  (8000 rows of which 1200 count, 20011 ids, width 1024:
+// dX 84 -> 21 us per half of the ids.)
+__device__ __forceinline__ int dx_slices(int rows, int T, int slices, int tile_q, int tiles_p, int target)
+{
+    const int tq = (rows + tile_q - 1) / tile_q, tq_all = (T + tile_q - 1) / tile_q;
+    if (rows <= 0) return slices;
+    const int room = (int)min((long long)tq_all * slices / tq, (long long)T * slices / rows);
+    return max(slices, min(min(room, 32), target / (tq * tiles_p)));
+}
 
 // A value as three bf16 parts, cut rather than rounded: x = hi + mid + lo exactly.
 __device__ __forceinline__ void split3(float x, uint32_t& hi, uint32_t& mid, uint32_t& lo)
@@ -277,6 +291,16 @@ __device__ __forceinline__ void split3(float x, uint32_t& hi, uint32_t& mid, uin
     const uint32_t rb = __builtin_bit_cast(uint32_t, r);
     mid = rb >> 16;
     lo = __builtin_bit_cast(uint32_t, r - __builtin_bit_cast(float, rb & 0xffff0000)) >> 16;
+}
+
+// Two accumulator fragments' rows of four 16-bit values, lane group g holding columns 4 g .. 4 g + 3 of each: afterwards group g has
+// columns 8 (g / 2) .. + 7 of fragment g % 2.
+__device__ __forceinline__ i32x4 join_fragments(i32x2 a, i32x2 b)
+{
+    int a0 = a[0], a1 = a[1], b0 = b[0], b1 = b[1];
+    // (odd rows of sixteen lanes of the first operand and even rows of the second change places)
+    asm volatile("s_nop 1\n\tv_permlane16_swap_b32 %0, %2\n\tv_permlane16_swap_b32 %1, %3\n\ts_nop 1" : "+v"(a0), "+v"(a1), "+v"(b0), "+v"(b1));
+    return i32x4{a0, a1, b0, b1};
 }
 
 template <class T, Store S, Stage ST>
@@ -299,12 +323,14 @@ void vocab_tile_kernel(VocabArgs a)
     } else {
         Q.size = rows;
     }
-    const int tiles_q = (rows + T::BQ - 1) / T::BQ, n_tiles = a.tiles_p * tiles_q * a.slices;
-    if ((int)blockIdx.x >= n_tiles) return;
-    const TileAt tile = tile_of(xcd_contiguous_id(blockIdx.x, n_tiles), a.tiles_p, tiles_q);
+    const int slices = ST == Stage::Dx ? __builtin_amdgcn_readfirstlane(dx_slices(rows, a.T, a.slices, T::BQ, a.tiles_p, a.target)) : 1;
+    const int tiles_q = (rows + T::BQ - 1) / T::BQ, n_tiles = a.tiles_p * tiles_q * slices;
+    const int id = (int)blockIdx.x + a.first;
+    if (id >= n_tiles) return;
+    const TileAt tile = tile_of(xcd_contiguous_id(id, n_tiles), a.tiles_p, tiles_q);
     // (divisions leave their results in vector registers)
     const int p0 = __builtin_amdgcn_readfirstlane(tile.p) * T::BP, q0 = __builtin_amdgcn_readfirstlane(tile.q) * T::BQ;
-    const int per_slice = __builtin_amdgcn_readfirstlane(((k + kStepK - 1) / kStepK + a.slices - 1) / a.slices) * kStepK;
+    const int per_slice = __builtin_amdgcn_readfirstlane(((k + kStepK - 1) / kStepK + slices - 1) / slices) * kStepK;
     const int k0 = min(k, __builtin_amdgcn_readfirstlane(tile.slice) * per_slice), k1 = min(k, k0 + per_slice);
 
     Product<T, S == Store::F16, PX, QX, S == Store::F32 ? 6 : 1> prod;
@@ -385,61 +411,80 @@ void vocab_tile_kernel(VocabArgs a)
             a.partial[(size_t)tile.p * a.partial_ld + q0 + i] = float2{m, sum};
         }
     } else if constexpr (ST == Stage::G) {
-        auto put = [&](size_t at, float d) {       // one element
-            if constexpr (S == Store::F32) {
-                uint32_t h, m, l;
-                split3(d, h, m, l);
-                unsigned short* to = (unsigned short*)a.G + at;
-                to[0] = (unsigned short)h, to[a.G_part] = (unsigned short)m, to[2 * a.G_part] = (unsigned short)l;
-            } else {
-                store_el<S>(a.G, at, d);
-            }
-        };
 #pragma unroll
         for (int j = 0; j < T::FQ; ++j) {
-            const int q = qw + 16 * j + n16;
-            if (q >= rows) continue;
-            const float lse2 = a.g_lse2[q], gq = a.g[q];
-            const int y = a.g_target[q] - a.v0 - pw;
-#pragma unroll
-            for (int i = 0; i < T::FP; ++i) {
-                const int v = pw + 16 * i + 4 * g;
-                float d[4];
+            const int q = qw + 16 * j + n16, qc = min(q, rows - 1);
+            const float lse2 = a.g_lse2[qc], gq = a.g[qc];
+            const int y = a.g_target[qc] - a.v0 - pw;
+            unsigned short* const row = (unsigned short*)a.G + (size_t)qc * a.G_ld + pw;
+            auto value = [&](int i, float (&d)[4]) {
 #pragma unroll
                 for (int r = 0; r < 4; ++r) d[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(prod.acc[i][j][r], scale2, -lse2)) * gq;
+                if (__ballot(y >> 4 == i)) {       // a target in these sixteen columns (few have one)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (y == 16 * i + 4 * g + r) d[r] = (__builtin_amdgcn_exp2f(__builtin_fmaf(prod.acc[i][j][r], scale2, -lse2)) - 1.f) * gq;
+                }
                 if (!whole)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) d[r] = v + r < a.P.size ? d[r] : 0.f;
-                const size_t at = (size_t)q * a.G_ld + v;
-                if constexpr (S == Store::F32) {
-                    uint32_t h[4], m[4], l[4];
+                    for (int r = 0; r < 4; ++r) d[r] = pw + 16 * i + 4 * g + r < a.P.size ? d[r] : 0.f;
+            };
+            // two fragments at a time: lanes exchange halves, so that each has eight neighbouring columns of one and 16 bytes to store
+            static_assert(T::FP % 2 == 0, "");
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) split3(d[r], h[r], m[r], l[r]);
-                    unsigned short* to = (unsigned short*)a.G + at;
-                    *(i32x2*)to = i32x2{(int)(h[0] | h[1] << 16), (int)(h[2] | h[3] << 16)};
-                    *(i32x2*)(to + a.G_part) = i32x2{(int)(m[0] | m[1] << 16), (int)(m[2] | m[3] << 16)};
-                    *(i32x2*)(to + 2 * a.G_part) = i32x2{(int)(l[0] | l[1] << 16), (int)(l[2] | l[3] << 16)};
+            for (int i = 0; i < T::FP; i += 2) {
+                float d[2][4];
+                value(i, d[0]);
+                value(i + 1, d[1]);
+                unsigned short* to = row + 16 * (i + (g & 1)) + 8 * (g >> 1);
+                if constexpr (S == Store::F32) {
+                    uint32_t w[2][3][4];
+#pragma unroll
+                    for (int f = 0; f < 2; ++f)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) split3(d[f][r], w[f][0][r], w[f][1][r], w[f][2][r]);
+#pragma unroll
+                    for (int part = 0; part < 3; ++part) {
+                        const auto& x = w[0][part];
+                        const auto& z = w[1][part];
+                        const i32x4 o = join_fragments(i32x2{(int)(x[0] | x[1] << 16), (int)(x[2] | x[3] << 16)},
+                                                       i32x2{(int)(z[0] | z[1] << 16), (int)(z[2] | z[3] << 16)});
+                        if (q < rows) *(i32x4*)(to + part * a.G_part) = o;
+                    }
                 } else {
-                    *(i32x2*)((unsigned short*)a.G + at) = i32x2{pack2<S == Store::F16>(d[0], d[1]), pack2<S == Store::F16>(d[2], d[3])};
+                    const i32x4 o = join_fragments(i32x2{pack2<S == Store::F16>(d[0][0], d[0][1]), pack2<S == Store::F16>(d[0][2], d[0][3])},
+                                                   i32x2{pack2<S == Store::F16>(d[1][0], d[1][1]), pack2<S == Store::F16>(d[1][2], d[1][3])});
+                    if (q < rows) *(i32x4*)to = o;
                 }
             }
-            // the target's own element once more, over what is there
-            if (y >= 0 && y < T::FP * 16 && pw + y < a.P.size && ((y >> 2) & 3) == g)
-                put((size_t)q * a.G_ld + pw + y, (__builtin_amdgcn_exp2f(__builtin_fmaf(pick(j, y), scale2, -lse2)) - 1.f) * gq);
         }
     } else {
         // dX: fp32 sums, one array per slice or one that pieces are added to; dW: rows of the result, in its type
         const int limit = ST == Stage::Dx ? rows : a.out_rows;
+        const bool pairs = ST == Stage::Dw && S != Store::F32 && (((uintptr_t)a.out | (unsigned)(a.out_ld * 2)) & 15) == 0 && a.out_cols % 8 == 0;
 #pragma unroll
         for (int j = 0; j < T::FQ; ++j) {
             const int q = qw + 16 * j + n16;
+            if constexpr (ST == Stage::Dw && S != Store::F32) {
+                if (pairs) {                       // (as in G)
+#pragma unroll
+                    for (int i = 0; i < T::FP; i += 2) {
+                        const f32x4 x = prod.acc[i][j] * down, z = prod.acc[i + 1][j] * down;
+                        const i32x4 o = join_fragments(i32x2{pack2<S == Store::F16>(x[0], x[1]), pack2<S == Store::F16>(x[2], x[3])},
+                                                       i32x2{pack2<S == Store::F16>(z[0], z[1]), pack2<S == Store::F16>(z[2], z[3])});
+                        const int p = pw + 16 * (i + (g & 1)) + 8 * (g >> 1);
+                        if (q < limit && p < a.out_cols) *(i32x4*)((short*)a.out + (size_t)q * a.out_ld + p) = o;
+                    }
+                    continue;
+                }
+            }
             if (q >= limit) continue;
 #pragma unroll
             for (int i = 0; i < T::FP; ++i) {
                 const int p = pw + 16 * i + 4 * g;
                 if (p >= a.out_cols) continue;
                 if constexpr (ST == Stage::Dx) {   // (out_ld is a multiple of 4)
-                    f32x4* to = (f32x4*)((float*)a.out + tile.slice * a.out_slice + (size_t)q * a.out_ld + p);
+                    f32x4* to = (f32x4*)((float*)a.out + ((size_t)tile.slice * rows + q) * a.out_ld + p);
                     f32x4 x = prod.acc[i][j];
                     if (a.accumulate) x += *to;
                     *to = x;
@@ -516,24 +561,23 @@ void vocab_rows_kernel(const void* __restrict__ targets, int id_bytes, int T, in
     if (lane == 0) most[wave] = top;
     __syncthreads();
     if (tid != 0) return;
-    VocabInfo out{n, 0.f, 1.f, 1.f};
-    if (dloss) {
-        if (reduce == Reduce::None) {
-            for (int w = 0; w < kRowsThreads / 64; ++w) out.g = fmaxf(out.g, most[w]);
-        } else {
-            out.g = n ? (reduce == Reduce::Mean ? *dloss / (float)n : *dloss) : 0.f;
+    VocabInfo out{n, 1.f, 1.f};
+    if (dloss && reduce != Reduce::None) {
+        // One gradient for all rows comes behind the sums: G is then p - [v = y], and the -1 of a target, which is most of a row's
+        // gradient and of a rare id's, has no rounding (with g in front, g (p - 1) is rounded to the type: 2.6e-3 from 64 bits in bf16 where
+        // few rows count, 1.7e-3 without).  fp16: 2^14 makes a probability of 2^-28 a normal number still.
+        const float g = n ? (reduce == Reduce::Mean ? *dloss / (float)n : *dloss) : 0.f;
+        out.up = half ? 16384.f : 1.f;
+        out.down = g * scale / out.up;
+    } else if (dloss && half) {
+        // the largest |c g| goes to 2^13 .. 2^14
+        for (int w = 1; w < kRowsThreads / 64; ++w) top = fmaxf(top, most[w]);
+        const float x = __builtin_fabsf(fmaxf(top, most[0]) * scale);
+        if (x > 0.f && x < __builtin_inff()) {
+            const int e = max(-126, min(126, 13 - (__builtin_amdgcn_frexp_expf(x) - 1)));
+            out.up = __builtin_ldexpf(1.f, e);
+            out.down = __builtin_ldexpf(1.f, -e);
         }
-        if (half) {
-            // the largest |c g| goes to 2^13 .. 2^14: |G| < 2^14 times what exp and 1 differ by, and a probability of 2^-28 is
-            // a normal number still
-            const float x = __builtin_fabsf(out.g * scale);
-            if (x > 0.f && x < __builtin_inff()) {
-                const int e = max(-126, min(126, 13 - (__builtin_amdgcn_frexp_expf(x) - 1)));
-                out.up = __builtin_ldexpf(1.f, e);
-                out.down = __builtin_ldexpf(1.f, -e);
-            }
-        }
-        if (reduce == Reduce::None) out.g = 0.f;
     }
     *info = out;
 }
@@ -560,7 +604,7 @@ void vocab_pack_kernel(PackArgs a)
     if (a.g_target && lane == 0) {
         a.g_target[m] = load_id(a.targets, a.id_bytes, t);
         a.g_lse2[m] = a.lse[t] * kLog2e;
-        a.g[m] = (a.dloss ? a.dloss[t] : a.info->g) * a.scale * a.info->up;
+        a.g[m] = (a.dloss ? a.dloss[t] * a.scale : 1.f) * a.info->up;
     }
     const size_t from = (size_t)t * a.D, to = (size_t)m * a.ld;
     constexpr int N = per16<S>();
@@ -596,51 +640,49 @@ void vocab_pack_kernel(PackArgs a)
     }
 }
 
-// The tiles' maxima and sums joined: 64 rows per workgroup, its waves a share of the tiles each.
+// The tiles' maxima and sums joined: 2^log_rows rows per workgroup (64 at most), its other lanes and waves a share of the tiles each.
+// One row in a workgroup of one lane per row and wave took 7.8 us for 256 tiles, each wave 32 of them one after another; spread over the lanes
+// it is the latency of a load and nine exchanges.
 constexpr int kJoinLossThreads = 512;
 
+struct LogSum { float top, sum; };                 // sum of exponentials relative to a finite top, or to 0 where it is not finite
+__device__ __forceinline__ LogSum join_sums(LogSum a, LogSum b)
+{
+    auto finite = [](float x) { return __builtin_fabsf(x) < __builtin_inff() ? x : 0.f; };
+    const float now = fmaxf(a.top, b.top), c = finite(now);
+    auto part = [&](LogSum x) { return x.top == -__builtin_inff() ? x.sum : x.sum * __builtin_amdgcn_exp2f(finite(x.top) - c); };
+    return LogSum{now, part(a) + part(b)};
+}
+
 __global__ __launch_bounds__(kJoinLossThreads)
-void vocab_join_kernel(const float2* __restrict__ partial, int partial_ld, int tiles, const float* __restrict__ target_logit,
+void vocab_join_kernel(const float2* __restrict__ partial, int partial_ld, int tiles, int log_rows, const float* __restrict__ target_logit,
                        const void* __restrict__ targets, int id_bytes, const int* __restrict__ place,
                        float* __restrict__ losses, float* __restrict__ lse, int T, int V)
 {
     constexpr int W = kJoinLossThreads / 64;
-    __shared__ float shared[2][W][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const long long t = (long long)blockIdx.x * 64 + lane;
+    __shared__ LogSum shared[W][64];
+    const int tid = threadIdx.x, wave = tid >> 6, R = 1 << log_rows, row = tid & (R - 1);
+    const long long t = ((long long)blockIdx.x << log_rows) + row;
     const int m = t >= T ? -1 : place ? place[t] : (int)t;
-    float top = -__builtin_inff(), sum = 0.f;
+    LogSum s{-__builtin_inff(), 0.f};
     if (m >= 0) {
 #pragma unroll 4
-        for (int i = wave; i < tiles; i += W) {
+        for (int i = tid >> log_rows; i < tiles; i += kJoinLossThreads >> log_rows) {
             const float2 x = partial[(size_t)i * partial_ld + m];
-            const float now = fmaxf(top, x.x);
-            // sums are relative to a finite maximum, or to 0 where it is not finite
-            const float a = __builtin_fabsf(top) < __builtin_inff() ? top : 0.f, b = __builtin_fabsf(x.x) < __builtin_inff() ? x.x : 0.f;
-            const float c = __builtin_fabsf(now) < __builtin_inff() ? now : 0.f;
-            sum = (top == -__builtin_inff() ? sum : sum * __builtin_amdgcn_exp2f(a - c)) +
-                  (x.x == -__builtin_inff() ? x.y : x.y * __builtin_amdgcn_exp2f(b - c));
-            top = now;
+            s = join_sums(s, LogSum{x.x, x.y});
         }
     }
-    shared[0][wave][lane] = top;
-    shared[1][wave][lane] = sum;
+    for (int d = R; d < 64; d <<= 1) s = join_sums(s, LogSum{__shfl_xor(s.top, d), __shfl_xor(s.sum, d)});
+    if ((tid & 63) < R) shared[wave][row] = s;
     __syncthreads();
-    if (wave != 0 || t >= T) return;
+    if (tid >= R || t >= T) return;
     if (m < 0) {
         losses[t] = 0.f;
         if (lse) lse[t] = 0.f;
         return;
     }
-    float now = top;
-    for (int w = 1; w < W; ++w) now = fmaxf(now, shared[0][w][lane]);
-    const float c = __builtin_fabsf(now) < __builtin_inff() ? now : 0.f;
-    float all = 0.f;
-    for (int w = 0; w < W; ++w) {
-        const float x = shared[0][w][lane], s = shared[1][w][lane];
-        all += x == -__builtin_inff() ? s : s * __builtin_amdgcn_exp2f((__builtin_fabsf(x) < __builtin_inff() ? x : 0.f) - c);
-    }
-    const float l2 = c + __builtin_amdgcn_logf(all);
+    for (int w = 1; w < W; ++w) s = join_sums(s, shared[w][row]);
+    const float l2 = (__builtin_fabsf(s.top) < __builtin_inff() ? s.top : 0.f) + __builtin_amdgcn_logf(s.sum);
     const int y = load_id(targets, id_bytes, t);
     if (lse) lse[t] = y >= V ? __builtin_nanf("") : l2 * kLn2;
     losses[t] = y < 0 ? 0.f : y >= V ? __builtin_nanf("") : (l2 - target_logit[m]) * kLn2;
@@ -678,7 +720,7 @@ void vocab_mean_kernel(const float* __restrict__ losses, const void* __restrict_
 // dX: the slices' sums, in order, scaled back and rounded; zeros for rows that do not count.  One wave per row.
 template <Store S>
 __global__ __launch_bounds__(256)
-void vocab_dx_kernel(const float* __restrict__ part, long long slice, int slices, int ld, const int* __restrict__ place,
+void vocab_dx_kernel(const float* __restrict__ part, int slices, int ld, int tile_q, int tiles_p, int target, const int* __restrict__ place,
                      const VocabInfo* __restrict__ info, void* __restrict__ dX, int T, int D)
 {
     const int lane = threadIdx.x & 63;
@@ -686,6 +728,9 @@ void vocab_dx_kernel(const float* __restrict__ part, long long slice, int slices
     if (t >= T) return;
     const int m = place[t];
     const float down = info->down;
+    const int rows = info->rows;
+    const size_t slice = (size_t)rows * ld;
+    slices = dx_slices(rows, T, slices, tile_q, tiles_p, target);
     const bool wide = ((uintptr_t)dX & 15) == 0 && D % 4 == 0;
     for (int c = lane * 4; c < D; c += 256) {
         f32x4 x = {0.f, 0.f, 0.f, 0.f};
