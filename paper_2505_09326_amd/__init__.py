@@ -65,7 +65,7 @@ class _PythonOnly:
     @staticmethod
     def forward(*args):
         return None
-    backward = fp8_forward = forward
+    backward = fp8_forward = embed_forward = embed_backward = loss_forward = loss_backward = clip = forward
 
 
 class SphattnError(RuntimeError):
@@ -158,6 +158,12 @@ def load_library() -> ctypes.CDLL:
     return _lib
 
 
+def _fast_calls():
+    """_marshal, or what stands in its place."""
+    load_library()
+    return _fast
+
+
 def _bound_marshal(lib):
     """_marshal on the library's entry points, or _PythonOnly where it is not there for this torch."""
     if not os.path.exists(MARSHAL_PATH):
@@ -170,7 +176,10 @@ def _bound_marshal(lib):
     if getattr(_marshal, "built_for", None) != torch.__version__:
         return _PythonOnly
     names = ("sphattn_cross_fwd", "sphattn_cross_splitkv_fwd", "sphattn_cross_splitkv_workspace_bytes", "sphattn_grn_bwd",
-             "sphattn_grn_bwd_split", "sphattn_bwd_workspace_bytes", "sphattn_fp8_grn_fwd")
+             "sphattn_grn_bwd_split", "sphattn_bwd_workspace_bytes", "sphattn_fp8_grn_fwd", "sphattn_embed_fwd",
+             "sphattn_embed_bwd_workspace_bytes", "sphattn_embed_bwd", "sphattn_vocab_loss_workspace_bytes", "sphattn_vocab_loss_fwd",
+             "sphattn_vocab_loss_bwd_workspace_bytes", "sphattn_vocab_loss_bwd", "sphattn_clip_grads_workspace_bytes", "sphattn_clip_grads",
+             "sphattn_strerror")
     _marshal.bind(_raise_on, *(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in names))
     return _marshal
 
@@ -799,6 +808,10 @@ def sphattn_embed_fwd(tokens, table, mult=None, scale=1.0, O=None, stream=None):
     V: a row of NaN), table [V,D] fp32, bf16 or fp16, mult [T] fp32 or None; returns O [T,D]."""
     import torch
     lib = load_library()
+    if O is None and stream is None:
+        done = _fast.embed_forward(tokens, table, mult, scale, False)
+        if done is not None:
+            return done
     id_bytes = _ids("tokens", tokens)
     V, D = _matrix("table", table)
     T, code = int(tokens.shape[0]), _code_of("table", table)
@@ -823,6 +836,10 @@ def sphattn_embed_bwd(tokens, dO, V, mult=None, scale=1.0, dtable=None, workspac
     the same bits in every run.  `workspace` is a device byte tensor of at least sphattn_embed_bwd_workspace_bytes(T, V, D)."""
     import torch
     lib = load_library()
+    if dtable is None and workspace is None and stream is None:
+        done = _fast.embed_backward(tokens, dO, V, mult, scale)
+        if done is not None:
+            return done
     id_bytes = _ids("tokens", tokens)
     T, D = _matrix("dO", dO)
     V, code = int(V), _code_of("dO", dO)
@@ -868,9 +885,13 @@ def sphattn_vocab_loss_fwd(X, W, targets, scale=1.0, reduction="none", all_rows=
     row does not count, and the work for it."""
     import torch
     lib = load_library()
-    T, V, D, code, id_bytes = _head(X, W, targets)
     red = REDUCTIONS[reduction]
     scale = _finite("scale", scale)
+    if losses is None and lse is None and mean is None and workspace is None and stream is None:
+        done = _fast.loss_forward(X, W, targets, scale, red, bool(all_rows), False)
+        if done is not None:
+            return done
+    T, V, D, code, id_bytes = _head(X, W, targets)
     _brought(stream, losses=losses, lse=lse, workspace=workspace, **({"mean": mean} if red else {}))
     _on_device(X=X, W=W, targets=targets, losses=losses, lse=lse, mean=mean, workspace=workspace)
     losses = torch.empty(T, dtype=torch.float32, device=X.device) if losses is None else losses
@@ -893,11 +914,15 @@ def sphattn_vocab_loss_bwd(X, W, targets, lse, dloss, scale=1.0, reduction="none
     value with "sum" and "mean".  One of the two may be not wanted (None in its place)."""
     import torch
     lib = load_library()
-    T, V, D, code, id_bytes = _head(X, W, targets)
     red = REDUCTIONS[reduction]
     scale = _finite("scale", scale)
     if not want_dX and not want_dW:
         raise ValueError("neither dX nor dW is wanted")
+    if dX is None and dW is None and workspace is None and stream is None:
+        done = _fast.loss_backward(X, W, targets, lse, dloss, scale, red, bool(want_dX), bool(want_dW))
+        if done is not None:
+            return done
+    T, V, D, code, id_bytes = _head(X, W, targets)
     _f32("lse", lse, (T,), optional=False)
     _f32("dloss", dloss, () if red else (T,), optional=False)
     _brought(stream, workspace=workspace, **({"dX": dX} if want_dX else {}), **({"dW": dW} if want_dW else {}))
@@ -948,6 +973,10 @@ def sphattn_clip_grads(grads, max_norm, out=None, norm=None, workspace=None, str
         raise ValueError(f"max_norm must not be negative, got {max_norm}")
     if not grads and norm is None:
         raise ValueError("no gradients: norm is required (there is no device to put it on)")
+    if norm is None and workspace is None and stream is None:
+        done = _fast.clip(grads, outs, max_norm)
+        if done is not None:
+            return done
     n, codes = len(grads), _codes()
     device = grads[0].device if grads else norm.device
     for i in range(n):

@@ -11,9 +11,12 @@ Forward = sphattn_fwd_z (O and the row aggregates z, which the backward needs), 
 sphattn_cross_fwd when multiplicities or shared K/V heads are given; backward = the library's
 two backward kernels.  Nothing is computed here.
 """
-import torch
+import math
 
-from . import (_cross_fwd_z, sphattn_bwd, sphattn_embed_bwd, sphattn_embed_fwd, sphattn_fwd_z, sphattn_grn_bwd,
+import torch
+from torch.autograd.function import once_differentiable
+
+from . import (REDUCTIONS, _cross_fwd_z, _fast_calls, sphattn_bwd, sphattn_embed_bwd, sphattn_embed_fwd, sphattn_fwd_z, sphattn_grn_bwd,
                sphattn_vocab_loss_bwd, sphattn_vocab_loss_fwd)
 
 _DTYPES = {torch.bfloat16: "bf16", torch.float16: "f16"}
@@ -66,6 +69,7 @@ class _TokenEmbedding(torch.autograd.Function):
         return O.view(*shape, O.shape[1])
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dO):
         tokens, mult = ctx.saved_tensors
         return None, sphattn_embed_bwd(tokens, dO.reshape(-1, dO.shape[-1]).contiguous(), ctx.V, mult, ctx.scale), None, None
@@ -74,7 +78,8 @@ class _TokenEmbedding(torch.autograd.Function):
 def token_embedding(tokens, table, mult=None, scale=1.0):
     """Differentiable embedding lookup with scaling, scale * mult * table[tokens]: tokens of any shape (int32 or int64; negative: no
     token, a row of zeros), table [V,D] (fp32, bf16 or fp16), mult of the tokens' shape (fp32, no gradient) or None."""
-    return _TokenEmbedding.apply(tokens, table, mult, scale)
+    done = _fast_calls().embed_forward(tokens, table, mult, scale, True)
+    return _TokenEmbedding.apply(tokens, table, mult, scale) if done is None else done
 
 
 class _VocabCrossEntropy(torch.autograd.Function):
@@ -91,6 +96,7 @@ class _VocabCrossEntropy(torch.autograd.Function):
         return got[2] if reduction != "none" else got[0].view(ctx.shape[:-1])
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dloss):
         X, W, targets, lse = ctx.saved_tensors
         if ctx.reduction == "none":
@@ -104,4 +110,9 @@ def vocab_cross_entropy(X, W, targets, scale=1.0, reduction="mean"):
     """Differentiable cross entropy of softmax(scale * X W^T) over a vocabulary, in fp32: X [..., D] and W [V,D] of one type (fp32, bf16 or
     fp16), targets [...] (int32 or int64; negative: the row does not count).  reduction "mean" (over the rows that count; 0 if
     none does), "sum" or "none"."""
+    scale = float(scale)
+    if math.isfinite(scale):                       # (else the Python path says so)
+        done = _fast_calls().loss_forward(X, W, targets, scale, REDUCTIONS[reduction], False, True)
+        if done is not None:
+            return done
     return _VocabCrossEntropy.apply(X, W, targets, scale, reduction)

@@ -17,13 +17,18 @@
 #include <ATen/ops/empty_like.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <c10/hip/HIPStream.h>
+#include <torch/csrc/autograd/custom_function.h>
+#include <torch/csrc/autograd/functions/basic_ops.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <array>
 #include <climits>
 #include <exception>
+#include <stdexcept>
+#include <string>
+#include <vector>
 
-#include "../../include/sphattn.h"
+#include "../../include/sphattn_train.h"
 
 namespace {
 
@@ -35,6 +40,16 @@ struct EntryPoints {
     decltype(&sphattn_grn_bwd_split) bwd_cut = nullptr;
     decltype(&sphattn_bwd_workspace_bytes) bwd_bytes = nullptr;
     decltype(&sphattn_fp8_grn_fwd) fp8 = nullptr;
+    decltype(&sphattn_embed_fwd) embed = nullptr;
+    decltype(&sphattn_embed_bwd_workspace_bytes) embed_bwd_bytes = nullptr;
+    decltype(&sphattn_embed_bwd) embed_bwd = nullptr;
+    decltype(&sphattn_vocab_loss_workspace_bytes) loss_bytes = nullptr;
+    decltype(&sphattn_vocab_loss_fwd) loss = nullptr;
+    decltype(&sphattn_vocab_loss_bwd_workspace_bytes) loss_bwd_bytes = nullptr;
+    decltype(&sphattn_vocab_loss_bwd) loss_bwd = nullptr;
+    decltype(&sphattn_clip_grads_workspace_bytes) clip_bytes = nullptr;
+    decltype(&sphattn_clip_grads) clip = nullptr;
+    decltype(&sphattn_strerror) text = nullptr;
 } entry;
 PyObject* raise_on = nullptr;                      // the binding's function that raises for an error code
 
@@ -270,28 +285,342 @@ PyObject* fp8_forward(PyObject*, PyObject* const* args, Py_ssize_t n)
     return wrapped(std::move(O));
 }
 
+// ---- sphattn_train.h -------------------------------------------------------------------------------
+//
+// The differentiable calls are autograd nodes of their own here: a backward pass's worker thread then neither waits for the
+// interpreter nor runs it.  A lookup of 8192 rows of 19999 x 1024 with its gradient took 105 us through Python (kernels 38) and takes 52, a
+// lookup of one row 9.9 and 5.0, clipping twelve tensors 26.8 and 10.8 (kernels 10).
+
+int code_of(const at::Tensor& t)
+{
+    return t.scalar_type() == at::kFloat ? SPHATTN_F32 : t.scalar_type() == at::kBFloat16 ? SPHATTN_BF16 : t.scalar_type() == at::kHalf ? SPHATTN_F16 : -1;
+}
+
+bool plain(const at::Tensor& t, at::Device device) { return t.device() == device && t.layout() == at::kStrided && t.is_contiguous(); }
+
+bool are_ids(const at::Tensor& t, at::Device device) { return (t.scalar_type() == at::kLong || t.scalar_type() == at::kInt) && plain(t, device); }
+
+at::Tensor bytes_of(size_t n, const at::Tensor& like) { return at::empty({(int64_t)n}, like.options().dtype(at::kByte)); }
+
+at::Tensor floats(at::IntArrayRef shape, const at::Tensor& like) { return at::empty(shape, like.options().dtype(at::kFloat)); }
+
+// In a backward pass, where no Python is at hand to raise the binding's own error.
+void throw_on(int rc)
+{
+    if (rc != 0) throw std::runtime_error("sphattn error " + std::to_string(rc) + ": " + entry.text(rc));
+}
+
+// Gradients that a second derivative is asked of say that they have none.
+torch::autograd::variable_list once(torch::autograd::variable_list grads)
+{
+    if (!at::GradMode::is_enabled()) return grads;
+    std::vector<size_t> at;
+    torch::autograd::variable_list there;
+    for (size_t i = 0; i < grads.size(); ++i)
+        if (grads[i].defined()) {
+            at.push_back(i);
+            there.push_back(grads[i].detach().requires_grad_());
+        }
+    const auto error = std::make_shared<torch::autograd::DelayedError>("this gradient of sphattn has no derivative", (int64_t)there.size());
+    torch::autograd::variable_list marked = (*error)(std::move(there));
+    for (size_t i = 0; i < at.size(); ++i) grads[at[i]] = marked[i];
+    return grads;
+}
+
+at::Tensor embed(const at::Tensor& tokens, const at::Tensor& table, const at::Tensor* mult, double scale, int& rc)
+{
+    std::vector<int64_t> shape = tokens.sizes().vec();
+    shape.push_back(table.size(1));
+    at::Tensor O = at::empty(shape, table.options());
+    rc = entry.embed(data(tokens), (int)tokens.element_size(), data(table), (const float*)data(mult), data(O), (int)tokens.numel(), (int)table.size(0),
+                     (int)table.size(1), (float)scale, code_of(table), stream_of(table));
+    return O;
+}
+
+at::Tensor embed_gradient(const at::Tensor& tokens, const at::Tensor& dO, int64_t V, const at::Tensor* mult, double scale, int& rc)
+{
+    const int T = (int)tokens.numel(), D = (int)dO.size(-1);
+    at::Tensor dtable = at::empty({V, D}, dO.options());
+    const size_t bytes = entry.embed_bwd_bytes(T, (int)V, D);
+    const at::Tensor ws = bytes_of(bytes, dO);
+    rc = entry.embed_bwd(data(tokens), (int)tokens.element_size(), (const float*)data(mult), data(dO), data(dtable), T, (int)V, D, (float)scale, code_of(dO),
+                         data(ws), bytes, stream_of(dO));
+    return dtable;
+}
+
+struct TokenEmbedding : torch::autograd::Function<TokenEmbedding> {
+    static at::Tensor forward(torch::autograd::AutogradContext* ctx, const at::Tensor& tokens, const at::Tensor& table, const at::Tensor& mult, double scale, int* rc)
+    {
+        at::Tensor O = embed(tokens, table, mult.defined() ? &mult : nullptr, scale, *rc);
+        ctx->save_for_backward({tokens, mult});
+        ctx->saved_data["V"] = table.size(0);
+        ctx->saved_data["scale"] = scale;
+        return O;
+    }
+    static torch::autograd::variable_list backward(torch::autograd::AutogradContext* ctx, torch::autograd::variable_list grads)
+    {
+        const auto saved = ctx->get_saved_variables();
+        int rc = 0;
+        at::Tensor dtable;
+        {
+            const at::NoGradGuard off;
+            dtable = embed_gradient(saved[0], grads[0].contiguous(), ctx->saved_data["V"].toInt(), saved[1].defined() ? &saved[1] : nullptr,
+                                    ctx->saved_data["scale"].toDouble(), rc);
+        }
+        throw_on(rc);
+        return once({at::Tensor(), dtable, at::Tensor(), at::Tensor(), at::Tensor()});
+    }
+};
+
+// What the embedding's calls have to be like: tokens of any shape if `any`, else [T].
+bool embed_fits(const at::Tensor& tokens, const at::Tensor& like, const at::Tensor* mult, bool any)
+{
+    const at::Device device = like.device();
+    return like.is_cuda() && plain(like, device) && code_of(like) >= 0 && (any || tokens.dim() == 1) && are_ids(tokens, device) && tokens.numel() <= INT_MAX &&
+           (!mult || fits(*mult, tokens.sizes(), at::kFloat, device));
+}
+
+// embed_forward(tokens, table, mult, scale, differentiable) -> O
+PyObject* embed_forward(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    if (!arguments(n, 5)) return nullptr;
+    const at::Tensor *tokens = tensor(args[0]), *table = tensor(args[1]), *mult;
+    const double scale = PyFloat_AsDouble(args[3]);
+    if (scale == -1.0 && PyErr_Occurred()) return nullptr;
+    if (!tokens || !table || !optional(args[2], mult) || !ready()) Py_RETURN_NONE;
+    at::Tensor O;
+    int rc = 0;
+    try {
+        const bool differentiable = args[4] == Py_True;
+        if (table->dim() != 2 || table->size(0) > INT_MAX || table->size(1) > INT_MAX || !embed_fits(*tokens, *table, mult, differentiable)) Py_RETURN_NONE;
+        const Unlocked unlocked;
+        O = differentiable ? TokenEmbedding::apply(*tokens, *table, mult ? *mult : at::Tensor(), scale, &rc) : embed(*tokens, *table, mult, scale, rc);
+    } catch (...) {
+        PyErr_Clear();
+        Py_RETURN_NONE;
+    }
+    return rc != 0 ? raised(rc) : wrapped(std::move(O));
+}
+
+// embed_backward(tokens, dO, V, mult, scale) -> dtable
+PyObject* embed_backward(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    if (!arguments(n, 5)) return nullptr;
+    const at::Tensor *tokens = tensor(args[0]), *dO = tensor(args[1]), *mult;
+    const long long V = PyLong_AsLongLong(args[2]);
+    const double scale = PyFloat_AsDouble(args[4]);
+    if (PyErr_Occurred()) return nullptr;
+    if (!tokens || !dO || !optional(args[3], mult) || !ready()) Py_RETURN_NONE;
+    at::Tensor dtable;
+    int rc = 0;
+    try {
+        if (dO->dim() != 2 || dO->size(0) != tokens->numel() || dO->size(1) > INT_MAX || V < 1 || V > INT_MAX || !embed_fits(*tokens, *dO, mult, false)) Py_RETURN_NONE;
+        const Unlocked unlocked;
+        dtable = embed_gradient(*tokens, *dO, V, mult, scale, rc);
+    } catch (...) {
+        PyErr_Clear();
+        Py_RETURN_NONE;
+    }
+    return rc != 0 ? raised(rc) : wrapped(std::move(dtable));
+}
+
+struct Head { int T, V, D, code; };
+Head head_of(const at::Tensor& targets, const at::Tensor& W) { return Head{(int)targets.numel(), (int)W.size(0), (int)W.size(1), code_of(W)}; }
+
+struct Losses { at::Tensor losses, lse, mean; };
+
+Losses loss(const at::Tensor& X, const at::Tensor& W, const at::Tensor& targets, double scale, int reduction, bool all_rows, int& rc)
+{
+    const Head h = head_of(targets, W);
+    Losses out{floats(targets.sizes(), X), floats(targets.sizes(), X), reduction ? floats({}, X) : at::Tensor()};
+    const size_t bytes = entry.loss_bytes(h.T, h.V, h.D, h.code);
+    const at::Tensor ws = bytes_of(bytes, X);
+    rc = entry.loss(data(X), data(W), data(targets), (int)targets.element_size(), (float*)data(out.losses), (float*)data(out.lse),
+                    reduction ? (float*)data(out.mean) : nullptr, h.T, h.V, h.D, (float)scale, reduction, all_rows, h.code, data(ws), bytes, stream_of(X));
+    return out;
+}
+
+std::array<at::Tensor, 2> loss_gradients(const at::Tensor& X, const at::Tensor& W, const at::Tensor& targets, const at::Tensor& lse, const at::Tensor& dloss,
+                                         double scale, int reduction, bool want_dX, bool want_dW, int& rc)
+{
+    const Head h = head_of(targets, W);
+    std::array<at::Tensor, 2> d;
+    if (want_dX) d[0] = at::empty_like(X);
+    if (want_dW) d[1] = at::empty_like(W);
+    const size_t bytes = entry.loss_bwd_bytes(h.T, h.V, h.D, h.code);
+    const at::Tensor ws = bytes_of(bytes, X);
+    rc = entry.loss_bwd(data(X), data(W), data(targets), (int)targets.element_size(), (const float*)data(lse), (const float*)data(dloss),
+                        want_dX ? data(d[0]) : nullptr, want_dW ? data(d[1]) : nullptr, h.T, h.V, h.D, (float)scale, reduction, h.code, data(ws), bytes,
+                        stream_of(X));
+    return d;
+}
+
+struct VocabCrossEntropy : torch::autograd::Function<VocabCrossEntropy> {
+    static at::Tensor forward(torch::autograd::AutogradContext* ctx, const at::Tensor& X, const at::Tensor& W, const at::Tensor& targets, double scale,
+                              int64_t reduction, int* rc)
+    {
+        Losses out = loss(X, W, targets, scale, (int)reduction, false, *rc);
+        ctx->save_for_backward({X, W, targets, out.lse});
+        ctx->saved_data["scale"] = scale;
+        ctx->saved_data["reduction"] = reduction;
+        return reduction ? out.mean : out.losses;
+    }
+    static torch::autograd::variable_list backward(torch::autograd::AutogradContext* ctx, torch::autograd::variable_list grads)
+    {
+        const auto saved = ctx->get_saved_variables();
+        int rc = 0;
+        std::array<at::Tensor, 2> d;
+        {
+            const at::NoGradGuard off;
+            d = loss_gradients(saved[0], saved[1], saved[2], saved[3], grads[0].contiguous(), ctx->saved_data["scale"].toDouble(),
+                               (int)ctx->saved_data["reduction"].toInt(), ctx->needs_input_grad(0), ctx->needs_input_grad(1), rc);
+        }
+        throw_on(rc);
+        return once({d[0], d[1], at::Tensor(), at::Tensor(), at::Tensor(), at::Tensor()});
+    }
+};
+
+// X [..., D] (rows of any shape if `any`, else [T,D]), W [V,D], targets [...]
+bool head_fits(const at::Tensor& X, const at::Tensor& W, const at::Tensor& targets, bool any)
+{
+    if (!X.is_cuda() || W.dim() != 2 || X.dim() < 1 || (!any && X.dim() != 2)) return false;
+    const at::Device device = X.device();
+    return code_of(X) >= 0 && W.scalar_type() == X.scalar_type() && plain(X, device) && plain(W, device) && are_ids(targets, device) &&
+           X.sizes().slice(0, X.dim() - 1) == targets.sizes() && X.size(-1) == W.size(1) && W.size(0) <= INT_MAX && W.size(1) <= INT_MAX &&
+           targets.numel() <= INT_MAX;
+}
+
+PyObject* tuple_of(std::initializer_list<at::Tensor*> tensors)
+{
+    PyObject* out = PyTuple_New((Py_ssize_t)tensors.size());
+    Py_ssize_t i = 0;
+    for (at::Tensor* t : tensors) {
+        if (out == nullptr) break;
+        PyObject* o = Py_None;
+        if (t->defined()) o = wrapped(std::move(*t));
+        else Py_INCREF(o);
+        if (o == nullptr) Py_CLEAR(out);
+        else PyTuple_SET_ITEM(out, i++, o);
+    }
+    return out;
+}
+
+// loss_forward(X, W, targets, scale, reduction, all_rows, differentiable) -> (losses, lse[, mean]), or if differentiable what vocab_cross_entropy returns
+PyObject* loss_forward(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    if (!arguments(n, 7)) return nullptr;
+    const at::Tensor *X = tensor(args[0]), *W = tensor(args[1]), *targets = tensor(args[2]);
+    const double scale = PyFloat_AsDouble(args[3]);
+    const long reduction = PyLong_AsLong(args[4]);
+    if (PyErr_Occurred()) return nullptr;
+    if (!X || !W || !targets || !ready()) Py_RETURN_NONE;
+    const bool differentiable = args[6] == Py_True;
+    Losses out;
+    int rc = 0;
+    try {
+        if (!head_fits(*X, *W, *targets, differentiable)) Py_RETURN_NONE;
+        const Unlocked unlocked;
+        if (differentiable) out.losses = VocabCrossEntropy::apply(*X, *W, *targets, scale, (int64_t)reduction, &rc);
+        else out = loss(*X, *W, *targets, scale, (int)reduction, args[5] == Py_True, rc);
+    } catch (...) {
+        PyErr_Clear();
+        Py_RETURN_NONE;
+    }
+    if (rc != 0) return raised(rc);
+    if (differentiable) return wrapped(std::move(out.losses));
+    return reduction ? tuple_of({&out.losses, &out.lse, &out.mean}) : tuple_of({&out.losses, &out.lse});
+}
+
+// loss_backward(X, W, targets, lse, dloss, scale, reduction, want_dX, want_dW) -> (dX, dW)
+PyObject* loss_backward(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    if (!arguments(n, 9)) return nullptr;
+    const at::Tensor *X = tensor(args[0]), *W = tensor(args[1]), *targets = tensor(args[2]), *lse = tensor(args[3]), *dloss = tensor(args[4]);
+    const double scale = PyFloat_AsDouble(args[5]);
+    const long reduction = PyLong_AsLong(args[6]);
+    if (PyErr_Occurred()) return nullptr;
+    if (!X || !W || !targets || !lse || !dloss || !ready()) Py_RETURN_NONE;
+    std::array<at::Tensor, 2> d;
+    int rc = 0;
+    try {
+        if (!head_fits(*X, *W, *targets, false) || !fits(*lse, targets->sizes(), at::kFloat, X->device()) ||
+            !fits(*dloss, reduction ? at::IntArrayRef() : targets->sizes(), at::kFloat, X->device()))
+            Py_RETURN_NONE;
+        const Unlocked unlocked;
+        d = loss_gradients(*X, *W, *targets, *lse, *dloss, scale, (int)reduction, args[7] == Py_True, args[8] == Py_True, rc);
+    } catch (...) {
+        PyErr_Clear();
+        Py_RETURN_NONE;
+    }
+    return rc != 0 ? raised(rc) : tuple_of({&d[0], &d[1]});
+}
+
+// clip(grads, out, max_norm) -> norm: two lists, or one twice
+PyObject* clip(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    if (!arguments(n, 3)) return nullptr;
+    const double max_norm = PyFloat_AsDouble(args[2]);
+    if (PyErr_Occurred()) return nullptr;
+    if (!PyList_CheckExact(args[0]) || !PyList_CheckExact(args[1]) || !ready()) Py_RETURN_NONE;
+    const Py_ssize_t count = PyList_GET_SIZE(args[0]);
+    if (count == 0 || count > INT_MAX || PyList_GET_SIZE(args[1]) != count || !(max_norm >= 0)) Py_RETURN_NONE;
+    at::Tensor norm;
+    int rc = 0;
+    try {
+        std::vector<const void*> in(count);
+        std::vector<void*> out(count);
+        std::vector<long long> size(count);
+        std::vector<int> type(count);
+        const at::Tensor* first = nullptr;
+        for (Py_ssize_t i = 0; i < count; ++i) {
+            const at::Tensor *g = tensor(PyList_GET_ITEM(args[0], i)), *o = tensor(PyList_GET_ITEM(args[1], i));
+            if (!g || !o || !g->is_cuda() || g->layout() != at::kStrided || code_of(*g) < 0 || !g->is_non_overlapping_and_dense()) Py_RETURN_NONE;
+            if (!first) first = g;
+            if (g->device() != first->device() || (o != g && (o->scalar_type() != g->scalar_type() || o->device() != g->device() || o->layout() != at::kStrided ||
+                                                              o->sizes() != g->sizes() || o->strides() != g->strides())))
+                Py_RETURN_NONE;
+            in[i] = data(*g), out[i] = data(*o), size[i] = g->numel(), type[i] = code_of(*g);
+        }
+        const Unlocked unlocked;
+        norm = floats({}, *first);
+        const size_t bytes = entry.clip_bytes((int)count);
+        const at::Tensor ws = bytes_of(bytes, *first);
+        rc = entry.clip(in.data(), out.data(), size.data(), type.data(), (int)count, (float)max_norm, (float*)data(norm), data(ws), bytes, stream_of(*first));
+    } catch (...) {
+        PyErr_Clear();
+        Py_RETURN_NONE;
+    }
+    return rc != 0 ? raised(rc) : wrapped(std::move(norm));
+}
+
 // bind(raise_on, addresses of the entry points in the order of EntryPoints)
 PyObject* bind(PyObject*, PyObject* args)
 {
-    PyObject* handler;
-    unsigned long long a[7];
-    if (!PyArg_ParseTuple(args, "OKKKKKKK", &handler, &a[0], &a[1], &a[2], &a[3], &a[4], &a[5], &a[6])) return nullptr;
+    constexpr Py_ssize_t COUNT = 17;
+    unsigned long long a[COUNT];
+    if (!arguments(PyTuple_GET_SIZE(args), COUNT + 1)) return nullptr;
+    for (Py_ssize_t i = 0; i < COUNT; ++i) {
+        a[i] = PyLong_AsUnsignedLongLong(PyTuple_GET_ITEM(args, i + 1));
+        if (PyErr_Occurred()) return nullptr;
+    }
+    PyObject* handler = PyTuple_GET_ITEM(args, 0);
     Py_INCREF(handler);
     Py_XDECREF(raise_on);
     raise_on = handler;
-    entry.cross = (decltype(entry.cross))a[0];
-    entry.cross_cut = (decltype(entry.cross_cut))a[1];
-    entry.cross_bytes = (decltype(entry.cross_bytes))a[2];
-    entry.bwd = (decltype(entry.bwd))a[3];
-    entry.bwd_cut = (decltype(entry.bwd_cut))a[4];
-    entry.bwd_bytes = (decltype(entry.bwd_bytes))a[5];
-    entry.fp8 = (decltype(entry.fp8))a[6];
+    auto set = [&, i = 0](auto&... to) mutable { ((to = (std::decay_t<decltype(to)>)a[i++]), ...); };
+    set(entry.cross, entry.cross_cut, entry.cross_bytes, entry.bwd, entry.bwd_cut, entry.bwd_bytes, entry.fp8, entry.embed, entry.embed_bwd_bytes,
+        entry.embed_bwd, entry.loss_bytes, entry.loss, entry.loss_bwd_bytes, entry.loss_bwd, entry.clip_bytes, entry.clip, entry.text);
     Py_RETURN_NONE;
 }
 
 PyMethodDef methods[] = {{"forward", (PyCFunction)(void*)forward, METH_FASTCALL, nullptr},
                          {"backward", (PyCFunction)(void*)backward, METH_FASTCALL, nullptr},
                          {"fp8_forward", (PyCFunction)(void*)fp8_forward, METH_FASTCALL, nullptr},
+                         {"embed_forward", (PyCFunction)(void*)embed_forward, METH_FASTCALL, nullptr},
+                         {"embed_backward", (PyCFunction)(void*)embed_backward, METH_FASTCALL, nullptr},
+                         {"loss_forward", (PyCFunction)(void*)loss_forward, METH_FASTCALL, nullptr},
+                         {"loss_backward", (PyCFunction)(void*)loss_backward, METH_FASTCALL, nullptr},
+                         {"clip", (PyCFunction)(void*)clip, METH_FASTCALL, nullptr},
                          {"bind", bind, METH_VARARGS, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", "Checks, outputs, workspace and launch of a call (see marshal.cpp).", -1, methods};
