@@ -275,6 +275,23 @@ int launch_tiles(VocabArgs& a, int p, int q, hipStream_t stream)
     return launched();
 }
 
+// dX [q,p] and dW [n,p] at once
+template <class T, Store S>
+int launch_gradients(VocabArgs& dx, VocabArgs& dw, int p, int q, int n, hipStream_t stream)
+{
+    const auto kern = vocab_gradients_kernel<T, S>;
+    static std::atomic<uint64_t> done{0};
+    if (T::LDS > 65536 && !raise_lds_limit(kern, T::LDS, done)) return SPHATTN_ERR_LAUNCH;
+    dx.tiles_p = dw.tiles_p = (p + T::BP - 1) / T::BP;
+    const long long first = (long long)dx.tiles_p * ((q + T::BQ - 1) / T::BQ) * dx.slices, all = first + (long long)dw.tiles_p * ((n + T::BQ - 1) / T::BQ);
+    if (all > 1 << 22) {                           // (a launch has less than 2^32 threads)
+        const int rc = launch_tiles<T, S, Stage::Dx>(dx, p, q, stream);
+        return rc == SPHATTN_OK ? launch_tiles<T, S, Stage::Dw>(dw, p, n, stream) : rc;
+    }
+    hipLaunchKernelGGL(kern, dim3((unsigned)all), dim3(T::THREADS), T::LDS, stream, dx, dw, (int)first);
+    return launched();
+}
+
 // logits and G: rows decide the tile
 template <Store S, Stage ST>
 int launch_scores(VocabArgs& a, int V, int T, int& tiles_p, hipStream_t stream)
@@ -291,14 +308,33 @@ int launch_scores(VocabArgs& a, int V, int T, int& tiles_p, hipStream_t stream)
 // whether the products can read rows of D elements at p as they are
 bool ready(const void* p, int D, Store S) { return S != Store::F32 && !off(p, 16) && D % 8 == 0; }
 
-template <Store S>
-Operand pack_w(const Vocab& p, const void* W, hipStream_t stream)
+RowArgs row_args(const Vocab& p, const void* targets, int id_bytes)
 {
-    if (ready(W, p.D, S)) return Operand{(const unsigned char*)W, 0, p.D * 2, p.V};
-    PackArgs k{};
-    k.in = W, k.out = p.w, k.n = p.V, k.D = p.D, k.ld = p.ld, k.part = (long long)p.V * p.ld;
-    hipLaunchKernelGGL((vocab_pack_kernel<S>), dim3((unsigned)(p.V + 3) / 4), dim3(256), 0, stream, k);
-    return Operand{(const unsigned char*)p.w, k.part * 2, p.ld * 2, p.V};
+    RowArgs r{};
+    r.targets = targets, r.id_bytes = id_bytes, r.T = p.T, r.rows = p.rows, r.place = p.place, r.info = p.info;
+    return r;
+}
+
+// X and W as the products want them; what can be read as it is stays where it is
+template <Store S>
+void pack(const Vocab& p, const void* X, const void* W, bool pack_x, PackArgs k, Operand& x, Operand& w, hipStream_t stream)
+{
+    x = Operand{(const unsigned char*)X, 0, p.D * 2, p.T};
+    w = Operand{(const unsigned char*)W, 0, p.D * 2, p.V};
+    unsigned groups = 0;
+    if (pack_x) {
+        k.x = PackRows{X, p.x, p.T, p.D, p.ld, (long long)p.T * p.ld};
+        k.x_groups = (int)(groups = (unsigned)(p.T + kPackRows - 1) / kPackRows);
+        x = Operand{(const unsigned char*)p.x, k.x.part * 2, p.ld * 2, p.T};
+    }
+    if (!ready(W, p.D, S)) {
+        k.w = PackRows{W, p.w, p.V, p.D, p.ld, (long long)p.V * p.ld};
+        groups += (unsigned)(p.V + kPackRows - 1) / kPackRows;
+        w = Operand{(const unsigned char*)p.w, k.w.part * 2, p.ld * 2, p.V};
+    }
+    k.own_rows = p.T <= kOwnRows;
+    if (k.compact && !k.own_rows) hipLaunchKernelGGL(vocab_rows_kernel, dim3(1), dim3(kRowsThreads), 0, stream, k.r);
+    if (groups) hipLaunchKernelGGL((vocab_pack_kernel<S>), dim3(groups), dim3(kPackThreads), 0, stream, k);
 }
 
 template <Store S>
@@ -306,31 +342,25 @@ int run_vocab_fwd(const Vocab& p, const void* X, const void* W, const void* targ
                   float scale, int reduction, int all_rows, hipStream_t stream)
 {
     VocabArgs a{};
-    a.Q = Operand{(const unsigned char*)X, 0, p.D * 2, p.T};
-    if (!all_rows) {
-        hipLaunchKernelGGL(vocab_rows_kernel, dim3(1), dim3(kRowsThreads), 0, stream, targets, id_bytes, p.T, p.rows, p.place, p.info,
-                           (const float*)nullptr, Reduce::None, 1.f, 0);
-        a.info = p.info, a.rows = p.rows;
-    }
-    if (!all_rows || !ready(X, p.D, S)) {
-        PackArgs k{};
-        k.in = X, k.out = p.x, k.n = p.T, k.D = p.D, k.ld = p.ld, k.part = (long long)p.T * p.ld, k.info = a.info, k.rows = a.rows;
-        hipLaunchKernelGGL((vocab_pack_kernel<S>), dim3((unsigned)(p.T + 3) / 4), dim3(256), 0, stream, k);
-        a.Q = Operand{(const unsigned char*)p.x, k.part * 2, p.ld * 2, p.T};
-    }
-    a.P = pack_w<S>(p, W, stream);
+    PackArgs k{};
+    k.r = row_args(p, targets, id_bytes);
+    k.compact = !all_rows && p.T > Low::BQ;        // (up to one tile's rows cost the same whether they count or not)
+    pack<S>(p, X, W, k.compact || !ready(X, p.D, S), k, a.Q, a.P, stream);
+    if (k.compact) a.info = p.info, a.rows = p.rows;
     a.k = p.ld, a.slices = 1, a.V = p.V, a.scale2 = scale * kLog2e;
     a.targets = targets, a.id_bytes = id_bytes;
     a.partial = p.partial, a.partial_ld = p.T, a.target_logit = p.target_logit;
     int tiles = 0;
     const int rc = launch_scores<S, Stage::Logits>(a, p.V, p.T, tiles, stream);
     if (rc != SPHATTN_OK) return rc;
+    if (reduction == SPHATTN_LOSS_NONE) mean = nullptr;
+    const bool at_once = mean && p.T <= 64 && (long long)tiles * p.T <= 16 * kJoinLossThreads;   // one workgroup, 16 sums per lane at most
     int log_rows = 0;                              // rows of a joining workgroup: half a round of the CUs where they are few
-    while (log_rows < 6 && (p.T >> log_rows) > kCus / 2) ++log_rows;
+    while (log_rows < 6 && (p.T >> log_rows) > (at_once ? 0 : kCus / 2)) ++log_rows;
     hipLaunchKernelGGL(vocab_join_kernel, dim3((unsigned)(p.T + (1 << log_rows) - 1) >> log_rows), dim3(kJoinLossThreads), 0, stream, p.partial, p.T, tiles,
-                       log_rows, p.target_logit,
-                       targets, id_bytes, all_rows ? (const int*)nullptr : p.place, losses, lse, p.T, p.V);
-    if (mean && reduction != SPHATTN_LOSS_NONE)
+                       log_rows, p.target_logit, targets, id_bytes, k.compact ? p.place : (const int*)nullptr, all_rows, losses, lse,
+                       at_once ? mean : (float*)nullptr, reduction == SPHATTN_LOSS_MEAN, p.T, p.V);
+    if (mean && !at_once)
         hipLaunchKernelGGL(vocab_mean_kernel, dim3(1), dim3(1024), 0, stream, losses, targets, id_bytes, p.T, mean, reduction == SPHATTN_LOSS_MEAN);
     return launched();
 }
@@ -339,19 +369,22 @@ template <Store S>
 int run_vocab_bwd(const Vocab& p, const void* X, const void* W, const void* targets, int id_bytes, const float* lse, const float* dloss,
                   void* dX, void* dW, float scale, int reduction, hipStream_t stream)
 {
-    hipLaunchKernelGGL(vocab_rows_kernel, dim3(1), dim3(kRowsThreads), 0, stream, targets, id_bytes, p.T, p.rows, p.place, p.info,
-                       dloss, (Reduce)reduction, scale, S == Store::F16);
     PackArgs k{};
-    k.in = X, k.out = p.x, k.n = p.T, k.D = p.D, k.ld = p.ld, k.part = (long long)p.T * p.ld, k.info = p.info, k.rows = p.rows;
-    k.targets = targets, k.id_bytes = id_bytes, k.lse = lse, k.dloss = reduction == SPHATTN_LOSS_NONE ? dloss : nullptr, k.scale = scale;
-    k.g_target = p.g_target, k.g_lse2 = p.g_lse2, k.g = p.g;
-    if (p.T > 0) hipLaunchKernelGGL((vocab_pack_kernel<S>), dim3((unsigned)(p.T + 3) / 4), dim3(256), 0, stream, k);
-    const Operand x{(const unsigned char*)p.x, k.part * 2, p.ld * 2, p.T}, w = pack_w<S>(p, W, stream);
+    k.r = row_args(p, targets, id_bytes);
+    k.r.dloss = dloss, k.r.reduce = (Reduce)reduction, k.r.scale = scale, k.r.half = S == Store::F16;
+    k.compact = 1, k.lse = lse, k.g_target = p.g_target, k.g_lse2 = p.g_lse2, k.g = p.g;
+    Operand x{}, w{};
+    if (p.T == 0) {                                // (the info of no rows, which one workgroup writes)
+        hipLaunchKernelGGL(vocab_rows_kernel, dim3(1), dim3(kRowsThreads), 0, stream, k.r);
+        x = Operand{(const unsigned char*)p.x, 0, p.ld * 2, 0};
+    } else {
+        pack<S>(p, X, W, true, k, x, w, stream);
+    }
     int rc = SPHATTN_OK;
     const int dx_tile = p.dx_big ? 256 : 128, dx_at_once = p.dx_big ? kCus : 2 * kCus;
     for (int i = 0; i < p.n_pieces && rc == SPHATTN_OK; ++i) {
         const int v0 = i * p.piece, n = p.V - v0 < p.piece ? p.V - v0 : p.piece;
-        const Operand wi{w.data + (size_t)v0 * w.ld, w.part, w.ld, n};
+        const Operand wi{p.T ? w.data + (size_t)v0 * w.ld : nullptr, w.part, w.ld, n};
         const Operand G{(const unsigned char*)p.G, (long long)p.T * p.piece * 2, p.piece * 2, 0};
         VocabArgs a{};
         a.P = wi, a.Q = x, a.info = p.info, a.k = p.ld, a.slices = 1, a.V = p.V, a.v0 = v0, a.scale2 = scale * kLog2e;
@@ -359,21 +392,24 @@ int run_vocab_bwd(const Vocab& p, const void* X, const void* W, const void* targ
         a.G = p.G, a.G_part = (long long)p.T * p.piece, a.G_ld = p.piece;
         int tiles;
         if (p.T > 0) rc = launch_scores<S, Stage::G>(a, n, p.T, tiles, stream);
-        if (rc == SPHATTN_OK && dX && p.T > 0) {
-            VocabArgs b{};
-            b.P = Operand{wi.data, wi.part, wi.ld, p.ld};
-            b.Q = G, b.Q.size = p.T, b.info = p.info, b.k = n, b.slices = p.slices;
-            b.T = p.T, b.target = dx_at_once;
-            b.out = p.dx, b.out_ld = p.ld, b.out_cols = p.ld, b.accumulate = i > 0;
-            rc = p.dx_big ? launch_tiles<Big, S, Stage::Dx>(b, p.ld, p.T, stream) : launch_tiles<Mid, S, Stage::Dx>(b, p.ld, p.T, stream);
+        if (rc != SPHATTN_OK) break;
+        VocabArgs bx{}, bw{};
+        const bool with_dx = dX && p.T > 0, with_dw = dW != nullptr;
+        bx.P = Operand{wi.data, wi.part, wi.ld, p.ld};
+        bx.Q = G, bx.Q.size = p.T, bx.info = p.info, bx.k = n, bx.slices = p.slices;
+        bx.T = p.T, bx.target = dx_at_once;
+        bx.out = p.dx, bx.out_ld = p.ld, bx.out_cols = p.ld, bx.accumulate = i > 0;
+        bw.P = Operand{x.data, x.part, x.ld, p.ld};
+        bw.Q = G, bw.Q.size = (int)up_to(n, 8), bw.info = p.info, bw.slices = 1;
+        bw.out = dW ? (unsigned char*)dW + (size_t)v0 * p.D * store_bytes<S>() : nullptr, bw.out_ld = p.D, bw.out_cols = p.D, bw.out_rows = n;
+        const bool dw_big = big_tiles(p.ld, n);
+        if (with_dx && with_dw && !p.dx_big && !dw_big) {
+            rc = launch_gradients<Mid, S>(bx, bw, p.ld, p.T, n, stream);
+            continue;
         }
-        if (rc == SPHATTN_OK && dW) {
-            VocabArgs b{};
-            b.P = Operand{x.data, x.part, x.ld, p.ld};
-            b.Q = G, b.Q.size = (int)up_to(n, 8), b.info = p.info, b.slices = 1;
-            b.out = (unsigned char*)dW + (size_t)v0 * p.D * store_bytes<S>(), b.out_ld = p.D, b.out_cols = p.D, b.out_rows = n;
-            rc = big_tiles(p.ld, n) ? launch_tiles<Big, S, Stage::Dw>(b, p.ld, n, stream) : launch_tiles<Mid, S, Stage::Dw>(b, p.ld, n, stream);
-        }
+        if (with_dx) rc = p.dx_big ? launch_tiles<Big, S, Stage::Dx>(bx, p.ld, p.T, stream) : launch_tiles<Mid, S, Stage::Dx>(bx, p.ld, p.T, stream);
+        if (rc == SPHATTN_OK && with_dw)
+            rc = dw_big ? launch_tiles<Big, S, Stage::Dw>(bw, p.ld, n, stream) : launch_tiles<Mid, S, Stage::Dw>(bw, p.ld, n, stream);
     }
     if (rc == SPHATTN_OK && dX && p.T > 0)
         hipLaunchKernelGGL((vocab_dx_kernel<S>), dim3((unsigned)(p.T + 3) / 4), dim3(256), 0, stream, p.dx, p.slices, p.ld,

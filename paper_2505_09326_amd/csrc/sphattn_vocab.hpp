@@ -304,12 +304,9 @@ __device__ __forceinline__ i32x4 join_fragments(i32x2 a, i32x2 b)
 }
 
 template <class T, Store S, Stage ST>
-__global__ __launch_bounds__(T::THREADS, T::FP * T::FQ > 32 ? 1 : 2)
-void vocab_tile_kernel(VocabArgs a)
+__device__ __forceinline__ void vocab_tile(const VocabArgs& a, int block, SPH_LDS unsigned char* smem)
 {
     constexpr bool PX = ST == Stage::Dx || ST == Stage::Dw, QX = ST == Stage::Dw;
-    extern __shared__ __attribute__((aligned(16))) unsigned char smem_raw[];
-    SPH_LDS unsigned char* smem = (SPH_LDS unsigned char*)smem_raw;
     int rows = a.Q.size, k = a.k;
     float down = 1.f;
     if (a.info) {
@@ -325,7 +322,7 @@ void vocab_tile_kernel(VocabArgs a)
     }
     const int slices = ST == Stage::Dx ? __builtin_amdgcn_readfirstlane(dx_slices(rows, a.T, a.slices, T::BQ, a.tiles_p, a.target)) : 1;
     const int tiles_q = (rows + T::BQ - 1) / T::BQ, n_tiles = a.tiles_p * tiles_q * slices;
-    const int id = (int)blockIdx.x + a.first;
+    const int id = block + a.first;
     if (id >= n_tiles) return;
     const TileAt tile = tile_of(xcd_contiguous_id(id, n_tiles), a.tiles_p, tiles_q);
     // (divisions leave their results in vector registers)
@@ -508,104 +505,140 @@ void vocab_tile_kernel(VocabArgs a)
     }
 }
 
+template <class T, Store S, Stage ST>
+__global__ __launch_bounds__(T::THREADS, T::FP * T::FQ > 32 ? 1 : 2)
+void vocab_tile_kernel(VocabArgs a)
+{
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem_raw[];
+    vocab_tile<T, S, ST>(a, blockIdx.x, (SPH_LDS unsigned char*)smem_raw);
+}
+
+// dX and dW of a piece, which do not depend on each other, in one launch: dX's tiles first.  For small problems one launch less, and where
+// neither fills the chip its round is shared.
+template <class T, Store S>
+__global__ __launch_bounds__(T::THREADS, T::FP * T::FQ > 32 ? 1 : 2)
+void vocab_gradients_kernel(VocabArgs dx, VocabArgs dw, int dx_blocks)
+{
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem_raw[];
+    if ((int)blockIdx.x < dx_blocks) vocab_tile<T, S, Stage::Dx>(dx, blockIdx.x, (SPH_LDS unsigned char*)smem_raw);
+    else vocab_tile<T, S, Stage::Dw>(dw, (int)blockIdx.x - dx_blocks, (SPH_LDS unsigned char*)smem_raw);
+}
+
 // ---- around the products ---------------------------------------------------------------------------------
 
 // Which rows count (target >= 0), in order: rows[m] = t, place[t] = m or -1; and with `dloss` the scale of their gradients.
-// One workgroup: T ids are little beside what follows.
-constexpr int kRowsThreads = 1024;
 enum class Reduce { None, Sum, Mean };             // of dloss: [T], or one value
+struct RowArgs {
+    const void* targets; int id_bytes; int T;
+    int* rows; int* place; VocabInfo* info;
+    const float* dloss; Reduce reduce; float scale; int half;
+};
 
-__global__ __launch_bounds__(kRowsThreads)
-void vocab_rows_kernel(const void* __restrict__ targets, int id_bytes, int T, int* __restrict__ rows, int* __restrict__ place,
-                       VocabInfo* __restrict__ info, const float* __restrict__ dloss, Reduce reduce, float scale, int half)
+// `top`: the largest |dloss| of a row that counts, where there is one for each
+__device__ __forceinline__ VocabInfo row_scale(const RowArgs& a, int n, float top)
 {
-    __shared__ int part[2][kRowsThreads / 64];
-    __shared__ float most[kRowsThreads / 64];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    int n = 0;
-    float top = 0.f;
-    // eight consecutive rows a thread
-    constexpr int EACH = 8;
-    int turn = 0;
-    for (long long t0 = 0; t0 < T; t0 += kRowsThreads * EACH, turn ^= 1) {
-        const long long t = t0 + tid * EACH;
-        bool counts[EACH];
-        int c = 0;
-#pragma unroll
-        for (int i = 0; i < EACH; ++i) {
-            counts[i] = t + i < T && load_id(targets, id_bytes, t + i) >= 0;
-            c += counts[i];
-        }
-        int of_wave, at = exclusive_over_wave(c, lane, of_wave);
-        if (lane == 0) part[turn][wave] = of_wave;
-        __syncthreads();
-        int all = 0;
-        for (int w = 0; w < kRowsThreads / 64; ++w) {
-            if (w < wave) at += part[turn][w];
-            all += part[turn][w];
-        }
-        at += n;
-        n += all;
-#pragma unroll
-        for (int i = 0; i < EACH; ++i) {
-            if (t + i >= T) break;
-            place[t + i] = counts[i] ? at : -1;
-            if (counts[i]) {
-                rows[at++] = (int)(t + i);
-                if (dloss && reduce == Reduce::None) top = fmaxf(top, __builtin_fabsf(dloss[t + i]));
-            }
-        }
-    }
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-    if (lane == 0) most[wave] = top;
-    __syncthreads();
-    if (tid != 0) return;
     VocabInfo out{n, 1.f, 1.f};
-    if (dloss && reduce != Reduce::None) {
+    if (a.dloss && a.reduce != Reduce::None) {
         // One gradient for all rows comes behind the sums: G is then p - [v = y], and the -1 of a target, which is most of a row's
         // gradient and of a rare id's, has no rounding (with g in front, g (p - 1) is rounded to the type: 2.6e-3 from 64 bits in bf16 where
         // few rows count, 1.7e-3 without).  fp16: 2^14 makes a probability of 2^-28 a normal number still.
-        const float g = n ? (reduce == Reduce::Mean ? *dloss / (float)n : *dloss) : 0.f;
-        out.up = half ? 16384.f : 1.f;
-        out.down = g * scale / out.up;
-    } else if (dloss && half) {
+        const float g = n ? (a.reduce == Reduce::Mean ? *a.dloss / (float)n : *a.dloss) : 0.f;
+        out.up = a.half ? 16384.f : 1.f;
+        out.down = g * a.scale / out.up;
+    } else if (a.dloss && a.half) {
         // the largest |c g| goes to 2^13 .. 2^14
-        for (int w = 1; w < kRowsThreads / 64; ++w) top = fmaxf(top, most[w]);
-        const float x = __builtin_fabsf(fmaxf(top, most[0]) * scale);
+        const float x = __builtin_fabsf(top * a.scale);
         if (x > 0.f && x < __builtin_inff()) {
             const int e = max(-126, min(126, 13 - (__builtin_amdgcn_frexp_expf(x) - 1)));
             out.up = __builtin_ldexpf(1.f, e);
             out.down = __builtin_ldexpf(1.f, -e);
         }
     }
-    *info = out;
+    return out;
 }
 
-// Rows as the products want them: 16-bit, 16-byte aligned, whole pieces of 8; gathered by `rows` if there; fp32 in
-// three parts.  One wave per row.  With g_target: also what the G stage needs of each row.
-struct PackArgs {
+__device__ __forceinline__ float max_over_wave(float x)
+{
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) x = fmaxf(x, __shfl_xor(x, d));
+    return x;
+}
+
+__device__ __forceinline__ int lanes_below(uint64_t mask)
+{
+    return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
+}
+
+// One workgroup, for more rows than kOwnRows: T ids are little beside what follows.
+constexpr int kRowsThreads = 1024;
+
+__global__ __launch_bounds__(kRowsThreads)
+void vocab_rows_kernel(RowArgs a)
+{
+    constexpr int WAVES = kRowsThreads / 64, EACH = 8;      // a wave takes EACH times 64 neighbouring rows at a time
+    __shared__ int part[2][WAVES];
+    __shared__ float most[WAVES];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    int n = 0, turn = 0;
+    float top = 0.f;
+    for (long long t0 = 0; t0 < a.T; t0 += kRowsThreads * EACH, turn ^= 1) {
+        const long long t = t0 + wave * (64 * EACH) + lane;
+        int id[EACH];
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) id[i] = t + i * 64 < a.T ? load_id(a.targets, a.id_bytes, t + i * 64) : -1;
+        uint64_t counts[EACH];
+        int of_wave = 0;
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            counts[i] = __ballot(id[i] >= 0);
+            of_wave += __builtin_popcountll(counts[i]);
+        }
+        if (lane == 0) part[turn][wave] = of_wave;
+        __syncthreads();
+        int at = n;
+        for (int w = 0; w < WAVES; ++w) {
+            if (w < wave) at += part[turn][w];
+            n += part[turn][w];
+        }
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            const int m = at + lanes_below(counts[i]);
+            if (t + i * 64 < a.T) a.place[t + i * 64] = id[i] >= 0 ? m : -1;
+            if (id[i] >= 0) {
+                a.rows[m] = (int)(t + i * 64);
+                if (a.dloss && a.reduce == Reduce::None) top = fmaxf(top, __builtin_fabsf(a.dloss[t + i * 64]));
+            }
+            at += __builtin_popcountll(counts[i]);
+        }
+    }
+    top = max_over_wave(top);
+    if (lane == 0) most[wave] = top;
+    __syncthreads();
+    if (tid != 0) return;
+    for (int w = 1; w < WAVES; ++w) top = fmaxf(top, most[w]);
+    *a.info = row_scale(a, n, top);
+}
+
+// Rows as the products want them: 16-bit, 16-byte aligned, whole pieces of 8; gathered if only some count; fp32 in three
+// parts.  One wave per row; X's and W's in one launch.  For at most kOwnRows rows each workgroup finds out by itself which rows before its
+// own count, which spares a launch of one workgroup in front.
+constexpr int kPackThreads = 256, kPackRows = kPackThreads / 64, kOwnRows = 1024;
+
+struct PackRows {
     const void* in; void* out; int n, D, ld;       // (ld: elements per row of out, a multiple of 8)
     long long part;                                // elements from part to part
-    const VocabInfo* info; const int* rows;
-    const void* targets; int id_bytes; const float* lse; const float* dloss; float scale;
-    int* g_target; float* g_lse2; float* g;
+};
+struct PackArgs {
+    PackRows x, w;
+    int x_groups;                                  // workgroups on X, the rest on W
+    int compact, own_rows;                         // only X's rows that count; found here
+    RowArgs r;
+    const float* lse; int* g_target; float* g_lse2; float* g;   // what the G stage needs of each row, or NULL
 };
 
 template <Store S>
-__global__ __launch_bounds__(256)
-void vocab_pack_kernel(PackArgs a)
+__device__ __forceinline__ void pack_row(const PackRows& a, long long t, long long m, int lane)
 {
-    const int lane = threadIdx.x & 63;
-    const long long m = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int n = a.info ? a.info->rows : a.n;
-    if (m >= n) return;
-    const long long t = a.rows ? a.rows[m] : m;
-    if (a.g_target && lane == 0) {
-        a.g_target[m] = load_id(a.targets, a.id_bytes, t);
-        a.g_lse2[m] = a.lse[t] * kLog2e;
-        a.g[m] = (a.dloss ? a.dloss[t] * a.scale : 1.f) * a.info->up;
-    }
     const size_t from = (size_t)t * a.D, to = (size_t)m * a.ld;
     constexpr int N = per16<S>();
     const bool wide = ((uintptr_t)a.in & 15) == 0 && a.D % N == 0;
@@ -640,9 +673,65 @@ void vocab_pack_kernel(PackArgs a)
     }
 }
 
+template <Store S>
+__global__ __launch_bounds__(kPackThreads)
+void vocab_pack_kernel(PackArgs a)
+{
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    if ((int)blockIdx.x >= a.x_groups) {
+        const long long v = (long long)((int)blockIdx.x - a.x_groups) * kPackRows + wave;
+        if (v < a.w.n) pack_row<S>(a.w, v, v, lane);
+        return;
+    }
+    const long long row = (long long)blockIdx.x * kPackRows + wave;
+    long long t = row, m = row;
+    float up = 1.f;
+    if (a.compact && a.own_rows) {
+        __shared__ int before[kPackRows], all[kPackRows];
+        __shared__ float most[kPackRows];
+        const int t0 = (int)blockIdx.x * kPackRows;
+        int b = 0, n = 0;
+        float top = 0.f;
+        for (int i0 = 0; i0 < a.r.T; i0 += kPackThreads) {
+            const int i = i0 + tid;
+            const bool counts = i < a.r.T && load_id(a.r.targets, a.r.id_bytes, i) >= 0;
+            n += __builtin_popcountll(__ballot(counts));
+            b += __builtin_popcountll(__ballot(counts && i < t0));
+            if (counts && a.r.dloss && a.r.reduce == Reduce::None) top = fmaxf(top, __builtin_fabsf(a.r.dloss[i]));
+        }
+        top = max_over_wave(top);
+        if (lane == 0) before[wave] = b, all[wave] = n, most[wave] = top;
+        __syncthreads();
+        b = n = 0;
+        for (int w = 0; w < kPackRows; ++w) b += before[w], n += all[w], top = fmaxf(top, most[w]);
+        const VocabInfo info = row_scale(a.r, n, top);
+        if (blockIdx.x == 0 && tid == 0) *a.r.info = info;
+        if (row >= a.r.T) return;
+        const bool counts = load_id(a.r.targets, a.r.id_bytes, row) >= 0;
+        m = b;
+        for (int i = t0; i < row; ++i) m += load_id(a.r.targets, a.r.id_bytes, i) >= 0;
+        if (lane == 0) a.r.place[row] = counts ? (int)m : -1;
+        if (!counts) return;
+        if (lane == 0) a.r.rows[m] = (int)row;
+        up = info.up;
+    } else if (a.compact) {
+        if (m >= a.r.info->rows) return;
+        t = a.r.rows[m];
+        up = a.r.info->up;
+    } else if (m >= a.x.n) {
+        return;
+    }
+    if (a.g_target && lane == 0) {
+        a.g_target[m] = load_id(a.r.targets, a.r.id_bytes, t);
+        a.g_lse2[m] = a.lse[t] * kLog2e;
+        a.g[m] = (a.r.reduce == Reduce::None ? a.r.dloss[t] * a.r.scale : 1.f) * up;
+    }
+    pack_row<S>(a.x, t, m, lane);
+}
+
 // The tiles' maxima and sums joined: 2^log_rows rows per workgroup (64 at most), its other lanes and waves a share of the tiles each.
 // One row in a workgroup of one lane per row and wave took 7.8 us for 256 tiles, each wave 32 of them one after another; spread over the lanes
-// it is the latency of a load and nine exchanges.
+// it is the latency of a load and nine exchanges.  One workgroup on all rows also gives their sum or mean.
 constexpr int kJoinLossThreads = 512;
 
 struct LogSum { float top, sum; };                 // sum of exponentials relative to a finite top, or to 0 where it is not finite
@@ -657,7 +746,7 @@ __device__ __forceinline__ LogSum join_sums(LogSum a, LogSum b)
 __global__ __launch_bounds__(kJoinLossThreads)
 void vocab_join_kernel(const float2* __restrict__ partial, int partial_ld, int tiles, int log_rows, const float* __restrict__ target_logit,
                        const void* __restrict__ targets, int id_bytes, const int* __restrict__ place,
-                       float* __restrict__ losses, float* __restrict__ lse, int T, int V)
+                       int all_rows, float* __restrict__ losses, float* __restrict__ lse, float* __restrict__ mean, int divide, int T, int V)
 {
     constexpr int W = kJoinLossThreads / 64;
     __shared__ LogSum shared[W][64];
@@ -675,17 +764,26 @@ void vocab_join_kernel(const float2* __restrict__ partial, int partial_ld, int t
     for (int d = R; d < 64; d <<= 1) s = join_sums(s, LogSum{__shfl_xor(s.top, d), __shfl_xor(s.sum, d)});
     if ((tid & 63) < R) shared[wave][row] = s;
     __syncthreads();
-    if (tid >= R || t >= T) return;
-    if (m < 0) {
-        losses[t] = 0.f;
-        if (lse) lse[t] = 0.f;
-        return;
+    if (wave != 0) return;
+    const int y = tid < R && t < T ? load_id(targets, id_bytes, t) : -1;
+    float of_row = 0.f;
+    if (tid < R && t < T) {
+        float l = 0.f;
+        if (m >= 0 && (all_rows || y >= 0)) {
+            for (int w = 1; w < W; ++w) s = join_sums(s, shared[w][row]);
+            const float l2 = (__builtin_fabsf(s.top) < __builtin_inff() ? s.top : 0.f) + __builtin_amdgcn_logf(s.sum);
+            l = y >= V ? __builtin_nanf("") : l2 * kLn2;
+            if (y >= 0) of_row = y >= V ? __builtin_nanf("") : (l2 - target_logit[m]) * kLn2;
+        }
+        if (lse) lse[t] = l;
+        losses[t] = of_row;
     }
-    for (int w = 1; w < W; ++w) s = join_sums(s, shared[w][row]);
-    const float l2 = (__builtin_fabsf(s.top) < __builtin_inff() ? s.top : 0.f) + __builtin_amdgcn_logf(s.sum);
-    const int y = load_id(targets, id_bytes, t);
-    if (lse) lse[t] = y >= V ? __builtin_nanf("") : l2 * kLn2;
-    losses[t] = y < 0 ? 0.f : y >= V ? __builtin_nanf("") : (l2 - target_logit[m]) * kLn2;
+    if (!mean) return;                             // (with one workgroup only)
+    double sum = of_row;
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+    const int n = __builtin_popcountll(__ballot(y >= 0));
+    if (tid == 0) *mean = (float)(!divide ? sum : n > 0 ? sum / n : 0.0);
 }
 
 // Their sum over the rows that count and its mean: one workgroup, in fp64.  No row that counts: 0.
