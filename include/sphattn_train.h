@@ -56,7 +56,8 @@ int sphattn_embed_bwd(const void* tokens, int id_bytes, const float* mult, const
  *   mean : one fp32, or NULL: the sum of the losses (reduction SPHATTN_LOSS_SUM) or their mean over the rows that
  *          count (SPHATTN_LOSS_MEAN; 0 if none does).  Not looked at with SPHATTN_LOSS_NONE.
  *   all_rows : 1: lse also of rows that do not count; 0: those rows cost nothing and get lse 0.
- * Products in fp32 sums of exact products (SPHATTN_F32: to 2^-25 of a term on average, 2^-21 at most).  T <= 2^20, 1 <= V <= 2^24, 1 <= D <= 65536
+ * fp32 sums of exact products (SPHATTN_F32: the factors to 2^-23 on average and 2^-22 at most, those below 2^-17 of their
+ * tensor's largest element to 2^-40 of that; terms off by 3/4 2^-20 at most).  T <= 2^20, 1 <= V <= 2^24, 1 <= D <= 65536
  * (SPHATTN_ERR_SHAPE); scale finite, reduction a sphattn_reduction (SPHATTN_ERR_VALUE).
  * Workspace sizes are 0 for sizes that the call would reject.
  */
@@ -76,7 +77,7 @@ int sphattn_vocab_loss_fwd(const void* X, const void* W, const void* targets, in
  *           rows that count).
  *   dX : [T,D], dW : [V,D], the dtype of X and W; either may be NULL (not wanted), not both.
  * G is formed a piece of the vocabulary at a time and rounded to the storage type (fp16: scaled by a power of two, so that
- * small gradients keep their bits); sums in fp32, the results rounded once.
+ * small gradients keep their bits; fp32: two fp16 parts, as above); sums in fp32, the results rounded once.
  */
 size_t sphattn_vocab_loss_bwd_workspace_bytes(int T, int V, int D, int dtype);
 int sphattn_vocab_loss_bwd(const void* X, const void* W, const void* targets, int id_bytes,

@@ -24,6 +24,7 @@
 #include <array>
 #include <climits>
 #include <exception>
+#include <optional>
 #include <stdexcept>
 #include <string>
 #include <vector>
@@ -349,10 +350,11 @@ at::Tensor embed_gradient(const at::Tensor& tokens, const at::Tensor& dO, int64_
 }
 
 struct TokenEmbedding : torch::autograd::Function<TokenEmbedding> {
-    static at::Tensor forward(torch::autograd::AutogradContext* ctx, const at::Tensor& tokens, const at::Tensor& table, const at::Tensor& mult, double scale, int* rc)
+    static at::Tensor forward(torch::autograd::AutogradContext* ctx, const at::Tensor& tokens, const at::Tensor& table, const std::optional<at::Tensor>& mult, double scale,
+                              int* rc)
     {
-        at::Tensor O = embed(tokens, table, mult.defined() ? &mult : nullptr, scale, *rc);
-        ctx->save_for_backward({tokens, mult});
+        at::Tensor O = embed(tokens, table, mult ? &*mult : nullptr, scale, *rc);
+        ctx->save_for_backward({tokens, mult.value_or(at::Tensor())});
         ctx->saved_data["V"] = table.size(0);
         ctx->saved_data["scale"] = scale;
         return O;
@@ -394,7 +396,7 @@ PyObject* embed_forward(PyObject*, PyObject* const* args, Py_ssize_t n)
         const bool differentiable = args[4] == Py_True;
         if (table->dim() != 2 || table->size(0) > INT_MAX || table->size(1) > INT_MAX || !embed_fits(*tokens, *table, mult, differentiable)) Py_RETURN_NONE;
         const Unlocked unlocked;
-        O = differentiable ? TokenEmbedding::apply(*tokens, *table, mult ? *mult : at::Tensor(), scale, &rc) : embed(*tokens, *table, mult, scale, rc);
+        O = differentiable ? TokenEmbedding::apply(*tokens, *table, mult ? std::optional<at::Tensor>(*mult) : std::nullopt, scale, &rc) : embed(*tokens, *table, mult, scale, rc);
     } catch (...) {
         PyErr_Clear();
         Py_RETURN_NONE;

@@ -123,7 +123,7 @@ __device__ __forceinline__ void clip_scale(const void* in, void* out, long long 
             widen16<S>(w[r], x);
 #pragma unroll
             for (int i = 0; i < N; ++i) x[i] *= f;
-            if ((c + 1) * N <= n) q[c] = narrow16<S>(x);
+            if ((c + 1) * N <= n) __builtin_nontemporal_store(narrow16<S>(x), &q[c]);
         }
         const int rest = n / N * N + tid;
         if (rest < n) store_el<S>(out, at + rest, load_el<S>(in, at + rest) * f);
@@ -145,7 +145,7 @@ void clip_scale_kernel(ClipList list, const double* __restrict__ sums, int n_sum
     const double ratio = (double)limit / (n + 1e-6);
     const float f = ratio < 1.0 ? (float)ratio : ratio >= 1.0 ? 1.f : __builtin_nanf("");   // (NaN stays NaN)
     if (first_launch && blockIdx.x == 0 && tid == 0) *norm = (float)n;
-    for (long long c = blockIdx.x; c < list.chunks; c += gridDim.x) {
+    for (long long c = list.chunks - 1 - blockIdx.x; c >= 0; c -= gridDim.x) {
         const int k = __builtin_amdgcn_readfirstlane(clip_tensor(list, (int)c, tid & 63));
         if (f == 1.f && list.in[k] == list.out[k]) continue;
         const long long at = (c - list.first[k]) * kClipChunk;

@@ -61,6 +61,52 @@ template <Store S> __device__ __forceinline__ i32x4 narrow16(const float (&x)[pe
     return w;
 }
 
+// per16 elements from element `at` on, `left` of which are wanted (the rest zeros), and back.  WIDE: 16-byte aligned and all wanted;
+// otherwise aligned to an element only, which the memory pipe takes in one access too (with one element a lane 8192 rows of 515 took
+// two to three times as long).  room: elements to the end of the tensor, up to which more than is wanted may be read.
+template <Store S, bool WIDE> __device__ __forceinline__ i32x4 load16(const void* p, size_t at, int left, size_t room)
+{
+    constexpr int N = per16<S>();
+    if constexpr (WIDE) return ((const i32x4*)p)[at / N];
+    i32x4 w = {0, 0, 0, 0};
+    const unsigned char* from = (const unsigned char*)p + at * store_bytes<S>();
+    if (room >= (size_t)N) {
+        __builtin_memcpy(&w, from, 16);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N - 1; ++i) {
+            if (i >= left) break;
+            if constexpr (S == Store::F32) w[i] = ((const int*)from)[i];
+            else w[i / 2] |= (int)((uint32_t)((const unsigned short*)from)[i] << (16 * (i & 1)));
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (S == Store::F32) w[i] = i < left ? w[i] : 0;
+        else w[i] = 2 * i + 1 < left ? w[i] : 2 * i < left ? w[i] & 0xffff : 0;
+    }
+    return w;
+}
+template <Store S, bool WIDE> __device__ __forceinline__ void store16(void* p, size_t at, i32x4 w, int left)
+{
+    constexpr int N = per16<S>();
+    if constexpr (WIDE) {
+        ((i32x4*)p)[at / N] = w;
+        return;
+    }
+    unsigned char* to = (unsigned char*)p + at * store_bytes<S>();
+    if (left >= N) {
+        __builtin_memcpy(to, &w, 16);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N - 1; ++i) {
+            if (i >= left) break;
+            if constexpr (S == Store::F32) ((int*)to)[i] = w[i];
+            else ((unsigned short*)to)[i] = (unsigned short)((uint32_t)w[i / 2] >> (16 * (i & 1)));
+        }
+    }
+}
+
 // Token ids of 4 or 8 bytes as ints: what does not fit an int is no valid id (negative stays negative, the rest too large).
 __device__ __forceinline__ int load_id(const void* ids, int id_bytes, size_t i)
 {
@@ -87,33 +133,24 @@ void embed_fwd_kernel(const void* __restrict__ tokens, int id_bytes, const void*
         const bool in = v >= 0 && v < V;
         const float f = in ? (mult ? mult[row] * scale : scale) : 0.f;
         const float fill = v < 0 ? 0.f : __builtin_nanf("");
-        if constexpr (WIDE) {
-            constexpr int N = per16<S>(), AHEAD = 4;
-            const int pieces = D / N;
-            const i32x4* src = (const i32x4*)table + (size_t)(in ? v : 0) * pieces;
-            i32x4* dst = (i32x4*)O + (size_t)row * pieces;
-            for (int c0 = 0; c0 < pieces; c0 += 64 * AHEAD) {
-                i32x4 w[AHEAD];
+        constexpr int N = per16<S>(), AHEAD = 4;
+        const size_t src = (size_t)(in ? v : 0) * D, dst = (size_t)row * D;
+        for (int c0 = lane * N; c0 < D; c0 += 64 * N * AHEAD) {
+            i32x4 w[AHEAD];
 #pragma unroll
-                for (int a = 0; a < AHEAD; ++a) {
-                    const int c = c0 + a * 64 + lane;
-                    w[a] = i32x4{0, 0, 0, 0};
-                    if (in && c < pieces) w[a] = src[c];
-                }
-#pragma unroll
-                for (int a = 0; a < AHEAD; ++a) {
-                    const int c = c0 + a * 64 + lane;
-                    float x[N];
-                    widen16<S>(w[a], x);
-#pragma unroll
-                    for (int i = 0; i < N; ++i) x[i] = in ? x[i] * f : fill;
-                    if (c < pieces) dst[c] = narrow16<S>(x);
-                }
+            for (int a = 0; a < AHEAD; ++a) {
+                const int c = c0 + a * 64 * N;
+                w[a] = i32x4{0, 0, 0, 0};
+                if (in && c < D) w[a] = load16<S, WIDE>(table, src + c, D - c, (size_t)V * D - src - c);
             }
-        } else {
-            for (int c = lane; c < D; c += 64) {
-                const float x = in ? load_el<S>(table, (size_t)v * D + c) * f : fill;
-                store_el<S>(O, (size_t)row * D + c, x);
+#pragma unroll
+            for (int a = 0; a < AHEAD; ++a) {
+                const int c = c0 + a * 64 * N;
+                float x[N];
+                widen16<S>(w[a], x);
+#pragma unroll
+                for (int i = 0; i < N; ++i) x[i] = in ? x[i] * f : fill;
+                if (c < D) store16<S, WIDE>(O, dst + c, narrow16<S>(x), D - c);
             }
         }
     }
@@ -167,17 +204,40 @@ void embed_sort_kernel(const void* __restrict__ tokens, int id_bytes, int* __res
     const long long batches = ((long long)T + 63) / 64, share = (batches + kSortWaves - 1) / kSortWaves;
     const long long t0 = min((long long)T, wave * share * 64), t1 = min((long long)T, t0 + share * 64);
     int* mine = cnt + wave * ids;
+    // Eight times 64 positions at a time; one round per different own id among them, over all eight.  (One LDS access per id and eight batches
+    // instead of one per batch: each waits for the one before it, and a token at half of 32768 positions made 32 us of them.)
     constexpr int AHEAD = 8;
     int below = 0;
+    auto each_id = [&](const int (&v)[AHEAD], auto&& round) {
+        uint64_t left[AHEAD];
+#pragma unroll
+        for (int a = 0; a < AHEAD; ++a) left[a] = __ballot(v[a] >= lo && v[a] < lo + n_ids);
+#pragma unroll
+        for (int a = 0; a < AHEAD; ++a) {
+            while (left[a]) {
+                const int id = __builtin_amdgcn_readlane(v[a], __builtin_ctzll(left[a]));
+                uint64_t same[AHEAD];
+#pragma unroll
+                for (int k = 0; k < AHEAD; ++k) {
+                    same[k] = k < a ? 0 : __ballot(v[k] == id);
+                    left[k] &= ~same[k];
+                }
+                round(id, same);
+            }
+        }
+    };
     for (long long t = t0; t < t1; t += 64 * AHEAD) {
         int v[AHEAD];
 #pragma unroll
         for (int a = 0; a < AHEAD; ++a) v[a] = t + a * 64 + lane < t1 ? load_id(tokens, id_bytes, t + a * 64 + lane) : -1;
 #pragma unroll
-        for (int a = 0; a < AHEAD; ++a) {
-            below += v[a] >= 0 && v[a] < lo;
-            if (v[a] >= lo && v[a] < lo + n_ids) atomicAdd(&mine[v[a] - lo], 1);   // (integers, in LDS)
-        }
+        for (int a = 0; a < AHEAD; ++a) below += v[a] >= 0 && v[a] < lo;
+        each_id(v, [&](int id, const uint64_t (&same)[AHEAD]) {
+            int n = 0;
+#pragma unroll
+            for (int a = 0; a < AHEAD; ++a) n += __builtin_popcountll(same[a]);
+            if (lane == 0) mine[id - lo] += n;     // (no other wave has this row of counts)
+        });
     }
     below = sum_over_wave(below);
     if (lane == 0) part[wave] = below;
@@ -212,21 +272,15 @@ void embed_sort_kernel(const void* __restrict__ tokens, int id_bytes, int* __res
         int v[AHEAD];
 #pragma unroll
         for (int a = 0; a < AHEAD; ++a) v[a] = t + a * 64 + lane < t1 ? load_id(tokens, id_bytes, t + a * 64 + lane) : -1;
+        each_id(v, [&](int id, const uint64_t (&same)[AHEAD]) {
+            int p = mine[id - lo];
 #pragma unroll
-        for (int a = 0; a < AHEAD; ++a) {
-            const bool own = v[a] >= lo && v[a] < lo + n_ids;
-            uint64_t left = __ballot(own);
-            while (left) {                         // one round per different id among the 64
-                const int id = __shfl(v[a], __builtin_ctzll(left));
-                const uint64_t same = __ballot(own && v[a] == id);
-                const int p = mine[id - lo];
-                if (own && v[a] == id)
-                    sorted[p + __builtin_amdgcn_mbcnt_hi((uint32_t)(same >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)same, 0))] =
-                        (int)(t + a * 64 + lane);
-                mine[id - lo] = p + __builtin_popcountll(same);   // (every lane the same value)
-                left &= ~same;
+            for (int a = 0; a < AHEAD; ++a) {
+                if (v[a] == id) sorted[p + __builtin_amdgcn_mbcnt_hi((uint32_t)(same[a] >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)same[a], 0))] = (int)(t + a * 64 + lane);
+                p += __builtin_popcountll(same[a]);
             }
-        }
+            mine[id - lo] = p;                     // (every lane the same value)
+        });
     }
 
     // rows without a token, a wave each; thread i says over LDS how many id i has
@@ -249,22 +303,13 @@ void embed_sort_kernel(const void* __restrict__ tokens, int id_bytes, int* __res
 // shared by as many waves as it fills pieces.  A wave adds up a piece's runs of equal tokens over 64 lanes' columns in fp32.  A
 // run that lies inside the piece is a row of the gradient; one that crosses its borders leaves a partial sum: [piece][0] if
 // it began before the piece, [piece][1] if it begins in it and goes on behind it.
-template <Store S, bool WIDE> constexpr int embed_lane_cols() { return WIDE ? per16<S>() : 1; }
-
-template <Store S, bool WIDE>
-__device__ __forceinline__ void store_cols(void* row0, size_t at, const float (&x)[embed_lane_cols<S, WIDE>()])
-{
-    if constexpr (WIDE) ((i32x4*)row0)[at / per16<S>()] = narrow16<S>(x);
-    else store_el<S>(row0, at, x[0]);
-}
-
 template <Store S, bool WIDE>
 __global__ __launch_bounds__(kEmbedThreads)
 void embed_sum_kernel(const void* __restrict__ tokens, int id_bytes, const float* __restrict__ mult, const void* __restrict__ dO,
                       const int* __restrict__ first, const int* __restrict__ sorted, float* __restrict__ partial,
-                      void* __restrict__ dtable, int V, int D, float scale, int len, int n_pieces)
+                      void* __restrict__ dtable, int T, int V, int D, float scale, int len, int n_pieces)
 {
-    constexpr int C = embed_lane_cols<S, WIDE>(), AHEAD = WIDE ? 8 : 4;
+    constexpr int C = per16<S>(), AHEAD = 8;
     const int lane = threadIdx.x & 63;
     const long long piece = (long long)blockIdx.x * (kEmbedThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (piece >= n_pieces) return;
@@ -276,15 +321,15 @@ void embed_sum_kernel(const void* __restrict__ tokens, int id_bytes, const float
     float acc[C];
 #pragma unroll
     for (int i = 0; i < C; ++i) acc[i] = 0.f;
-    int run = -1;                                  // the id that acc belongs to
+    int run = -1, r0 = 0, r1 = 0;                  // the id that acc belongs to, and where its positions begin and end
     auto flush = [&](int id) {
-        const int r0 = first[id], r1 = first[id + 1];
         if (live) {
-            if (r0 >= p0 && r1 <= p1) store_cols<S, WIDE>(dtable, (size_t)id * D + col, acc);
+            if (r0 >= p0 && r1 <= p1) store16<S, WIDE>(dtable, (size_t)id * D + col, narrow16<S>(acc), D - col);
             else {
                 float* to = partial + ((size_t)piece * 2 + (r0 < p0 ? 0 : 1)) * D + col;
 #pragma unroll
-                for (int i = 0; i < C; ++i) to[i] = acc[i];
+                for (int i = 0; i < C; ++i)
+                    if (WIDE || col + i < D) to[i] = acc[i];
             }
         }
 #pragma unroll
@@ -293,25 +338,22 @@ void embed_sum_kernel(const void* __restrict__ tokens, int id_bytes, const float
     for (long long b = p0; b < p1; b += 64) {
         // 64 positions, their tokens and factors, one per lane
         const int n = (int)min((long long)64, p1 - b);
-        int t = 0, id = 0;
+        int t = 0, id = 0, begin = 0, end = 0;
         float f = 0.f;
         if (lane < n) {
             t = sorted[b + lane];
             id = load_id(tokens, id_bytes, t);
             f = mult ? mult[t] * scale : scale;
+            begin = first[id];                     // (here for all at once: at a run's end each would be waited for)
+            end = first[id + 1];
         }
         for (int j0 = 0; j0 < n; j0 += AHEAD) {
             i32x4 w[AHEAD];
-            float s[AHEAD];
 #pragma unroll
             for (int a = 0; a < AHEAD; ++a) {
                 const size_t at = (size_t)__builtin_amdgcn_readlane(t, min(j0 + a, n - 1)) * D + col;
-                if constexpr (WIDE) {
-                    w[a] = i32x4{0, 0, 0, 0};
-                    if (live) w[a] = ((const i32x4*)dO)[at / C];
-                } else {
-                    s[a] = live ? load_el<S>(dO, at) : 0.f;
-                }
+                w[a] = i32x4{0, 0, 0, 0};
+                if (live) w[a] = load16<S, WIDE>(dO, at, D - col, (size_t)T * D - at);
             }
 #pragma unroll
             for (int a = 0; a < AHEAD; ++a) {
@@ -321,10 +363,11 @@ void embed_sum_kernel(const void* __restrict__ tokens, int id_bytes, const float
                 if (v != run) {
                     if (run >= 0) flush(run);
                     run = v;
+                    r0 = __builtin_amdgcn_readlane(begin, j0 + a);
+                    r1 = __builtin_amdgcn_readlane(end, j0 + a);
                 }
                 float x[C];
-                if constexpr (WIDE) widen16<S>(w[a], x);
-                else x[0] = s[a];
+                widen16<S>(w[a], x);
 #pragma unroll
                 for (int i = 0; i < C; ++i) acc[i] = __builtin_fmaf(x[i], fa, acc[i]);
             }
@@ -334,7 +377,7 @@ void embed_sum_kernel(const void* __restrict__ tokens, int id_bytes, const float
 }
 
 // A row whose run crosses borders: the piece in which it begins adds its partial sums up, eight waves a share of the
-// pieces each, the shares in order behind that.
+// pieces each, sixteen (eight) pieces' loads under way, the shares in order behind that.
 constexpr int kJoinThreads = 512, kJoinWaves = kJoinThreads / 64;
 
 template <Store S, bool WIDE>
@@ -342,7 +385,7 @@ __global__ __launch_bounds__(kJoinThreads)
 void embed_join_kernel(const void* __restrict__ tokens, int id_bytes, const int* __restrict__ first, const int* __restrict__ sorted,
                        const float* __restrict__ partial, void* __restrict__ dtable, int V, int D, int len)
 {
-    constexpr int C = embed_lane_cols<S, WIDE>();
+    constexpr int C = per16<S>();
     __shared__ float shared[kJoinWaves][64 * C];
     const long long piece = blockIdx.x, p0 = piece * len, p1 = p0 + len;
     if (p1 >= first[V]) return;                    // nothing behind this piece
@@ -358,11 +401,20 @@ void embed_join_kernel(const void* __restrict__ tokens, int id_bytes, const int*
     const long long n = last - piece + 1, share = (n + kJoinWaves - 1) / kJoinWaves;
     const long long q0 = piece + wave * share, q1 = min(last + 1, q0 + share);
     if (col < D) {
-#pragma unroll 4
-        for (long long q = q0; q < q1; ++q) {
-            const float* from = partial + ((size_t)q * 2 + (q == piece ? 1 : 0)) * D + col;
+        constexpr int AHEAD = S == Store::F32 ? 16 : 8;
+        for (long long q = q0; q < q1; q += AHEAD) {
+            float x[AHEAD][C];
 #pragma unroll
-            for (int i = 0; i < C; ++i) acc[i] += from[i];
+            for (int a = 0; a < AHEAD; ++a) {
+                const long long at = min(q + a, q1 - 1);   // (loads without a condition: none waits for another)
+                const float* from = partial + ((size_t)at * 2 + (at == piece ? 1 : 0)) * D + col;
+#pragma unroll
+                for (int i = 0; i < C; ++i) x[a][i] = from[WIDE ? i : min(i, D - 1 - col)];
+            }
+#pragma unroll
+            for (int a = 0; a < AHEAD; ++a)
+#pragma unroll
+                for (int i = 0; i < C; ++i) acc[i] += q + a < q1 ? x[a][i] : 0.f;
         }
     }
 #pragma unroll
@@ -372,7 +424,7 @@ void embed_join_kernel(const void* __restrict__ tokens, int id_bytes, const int*
         for (int w = 1; w < kJoinWaves; ++w)
 #pragma unroll
             for (int i = 0; i < C; ++i) acc[i] += shared[w][lane * C + i];
-        store_cols<S, WIDE>(dtable, (size_t)id * D + col, acc);
+        store16<S, WIDE>(dtable, (size_t)id * D + col, narrow16<S>(acc), D - col);
     }
 }
 

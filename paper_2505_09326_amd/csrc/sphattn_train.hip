@@ -138,11 +138,11 @@ int run_embed_fwd(const void* tokens, int id_bytes, const void* table, const flo
 }
 
 template <Store S, bool WIDE>
-int run_embed_sums(const EmbedPlan& p, const void* tokens, int id_bytes, const float* mult, const void* dO, void* dtable, int V, int D, float scale, hipStream_t stream)
+int run_embed_sums(const EmbedPlan& p, const void* tokens, int id_bytes, const float* mult, const void* dO, void* dtable, int T, int V, int D, float scale, hipStream_t stream)
 {
-    const unsigned columns = (unsigned)((D + 64 * embed_lane_cols<S, WIDE>() - 1) / (64 * embed_lane_cols<S, WIDE>()));
+    const unsigned columns = (unsigned)((D + 64 * per16<S>() - 1) / (64 * per16<S>()));
     hipLaunchKernelGGL((embed_sum_kernel<S, WIDE>), dim3((unsigned)(p.pieces + 3) / 4, columns), dim3(kEmbedThreads), 0, stream,
-                       tokens, id_bytes, mult, dO, p.first, p.sorted, p.partial, dtable, V, D, scale, p.len, p.pieces);
+                       tokens, id_bytes, mult, dO, p.first, p.sorted, p.partial, dtable, T, V, D, scale, p.len, p.pieces);
     if (p.pieces > 1)
         hipLaunchKernelGGL((embed_join_kernel<S, WIDE>), dim3((unsigned)p.pieces - 1, columns), dim3(kJoinThreads), 0, stream,
                            tokens, id_bytes, p.first, p.sorted, p.partial, dtable, V, D, p.len);
@@ -157,8 +157,8 @@ int run_embed_bwd(const EmbedPlan& p, const void* tokens, int id_bytes, const fl
     const int rc = launched();
     if (rc != SPHATTN_OK || T == 0) return rc;
     const bool wide = !off(dO, 16) && !off(dtable, 16) && D % per16<S>() == 0;
-    return wide ? run_embed_sums<S, true>(p, tokens, id_bytes, mult, dO, dtable, V, D, scale, stream)
-                : run_embed_sums<S, false>(p, tokens, id_bytes, mult, dO, dtable, V, D, scale, stream);
+    return wide ? run_embed_sums<S, true>(p, tokens, id_bytes, mult, dO, dtable, T, V, D, scale, stream)
+                : run_embed_sums<S, false>(p, tokens, id_bytes, mult, dO, dtable, T, V, D, scale, stream);
 }
 
 // ---- vocabulary loss ---------------------------------------------------------------------------------
@@ -188,6 +188,8 @@ struct Vocab {
     bool dx_big; int slices;                       // dX: its tile, slices of its sum over a piece
     // workspace
     VocabInfo* info;
+    VocabRange* range;                             // fp32
+    float* most;
     int *rows, *place, *g_target;
     float *g_lse2, *g, *target_logit, *dx;
     float2* partial;
@@ -215,9 +217,11 @@ void dx_choice(long long T, long long ld, int n, bool& big, int& slices)
 Vocab vocab_fwd_plan(int T, int V, int D, int dtype, void* workspace)
 {
     Vocab p{};
-    p.T = T, p.V = V, p.D = D, p.parts = dtype == SPHATTN_F32 ? 3 : 1, p.ld = (int)up_to(D, 8);
+    p.T = T, p.V = V, p.D = D, p.parts = dtype == SPHATTN_F32 ? 2 : 1, p.ld = (int)up_to(D, 8);
     Carve c(workspace);
     p.info = c.take<VocabInfo>(1);
+    p.range = c.take<VocabRange>(1);
+    p.most = c.take<float>(p.parts > 1 ? kRangeGroupsX + kRangeGroupsW : 0);
     p.rows = c.take<int>(T);
     p.place = c.take<int>(T);
     p.target_logit = c.take<float>(T);
@@ -232,7 +236,7 @@ Vocab vocab_fwd_plan(int T, int V, int D, int dtype, void* workspace)
 Vocab vocab_bwd_plan(int T, int V, int D, int dtype, void* workspace)
 {
     Vocab p{};
-    p.T = T, p.V = V, p.D = D, p.parts = dtype == SPHATTN_F32 ? 3 : 1, p.ld = (int)up_to(D, 8);
+    p.T = T, p.V = V, p.D = D, p.parts = dtype == SPHATTN_F32 ? 2 : 1, p.ld = (int)up_to(D, 8);
     const long long row_bytes = 2ll * p.parts * (T > 0 ? T : 1);
     size_t limit = kPieceBytes;
     if ((size_t)row_bytes * p.ld > limit) limit = (size_t)row_bytes * p.ld;
@@ -244,6 +248,8 @@ Vocab vocab_bwd_plan(int T, int V, int D, int dtype, void* workspace)
     dx_choice(T > 0 ? T : 1, p.ld, p.piece < V ? p.piece : V, p.dx_big, p.slices);
     Carve c(workspace);
     p.info = c.take<VocabInfo>(1);
+    p.range = c.take<VocabRange>(1);
+    p.most = c.take<float>(p.parts > 1 ? kRangeGroupsX + kRangeGroupsW : 0);
     p.rows = c.take<int>(T);
     p.place = c.take<int>(T);
     p.g_target = c.take<int>(T);
@@ -317,7 +323,7 @@ RowArgs row_args(const Vocab& p, const void* targets, int id_bytes)
 
 // X and W as the products want them; what can be read as it is stays where it is
 template <Store S>
-void pack(const Vocab& p, const void* X, const void* W, bool pack_x, PackArgs k, Operand& x, Operand& w, hipStream_t stream)
+void pack(const Vocab& p, const void* X, const void* W, bool pack_x, bool all_rows, PackArgs k, Operand& x, Operand& w, hipStream_t stream)
 {
     x = Operand{(const unsigned char*)X, 0, p.D * 2, p.T};
     w = Operand{(const unsigned char*)W, 0, p.D * 2, p.V};
@@ -333,6 +339,11 @@ void pack(const Vocab& p, const void* X, const void* W, bool pack_x, PackArgs k,
         w = Operand{(const unsigned char*)p.w, k.w.part * 2, p.ld * 2, p.V};
     }
     k.own_rows = p.T <= kOwnRows;
+    if (S == Store::F32) {
+        hipLaunchKernelGGL(vocab_range_kernel, dim3(kRangeGroupsX + kRangeGroupsW), dim3(kRangeThreads), 0, stream, (const float*)X, (const float*)W, p.T, p.V, p.D,
+                           k.r.targets, k.r.id_bytes, (int)all_rows, p.most);
+        k.most = p.most, k.range = p.range;
+    }
     if (k.compact && !k.own_rows) hipLaunchKernelGGL(vocab_rows_kernel, dim3(1), dim3(kRowsThreads), 0, stream, k.r);
     if (groups) hipLaunchKernelGGL((vocab_pack_kernel<S>), dim3(groups), dim3(kPackThreads), 0, stream, k);
 }
@@ -345,8 +356,9 @@ int run_vocab_fwd(const Vocab& p, const void* X, const void* W, const void* targ
     PackArgs k{};
     k.r = row_args(p, targets, id_bytes);
     k.compact = !all_rows && p.T > Low::BQ;        // (up to one tile's rows cost the same whether they count or not)
-    pack<S>(p, X, W, k.compact || !ready(X, p.D, S), k, a.Q, a.P, stream);
+    pack<S>(p, X, W, k.compact || !ready(X, p.D, S), all_rows, k, a.Q, a.P, stream);
     if (k.compact) a.info = p.info, a.rows = p.rows;
+    a.range = p.range;
     a.k = p.ld, a.slices = 1, a.V = p.V, a.scale2 = scale * kLog2e;
     a.targets = targets, a.id_bytes = id_bytes;
     a.partial = p.partial, a.partial_ld = p.T, a.target_logit = p.target_logit;
@@ -371,14 +383,14 @@ int run_vocab_bwd(const Vocab& p, const void* X, const void* W, const void* targ
 {
     PackArgs k{};
     k.r = row_args(p, targets, id_bytes);
-    k.r.dloss = dloss, k.r.reduce = (Reduce)reduction, k.r.scale = scale, k.r.half = S == Store::F16;
+    k.r.dloss = dloss, k.r.reduce = (Reduce)reduction, k.r.scale = scale, k.r.half = S != Store::Bf16;
     k.compact = 1, k.lse = lse, k.g_target = p.g_target, k.g_lse2 = p.g_lse2, k.g = p.g;
     Operand x{}, w{};
     if (p.T == 0) {                                // (the info of no rows, which one workgroup writes)
         hipLaunchKernelGGL(vocab_rows_kernel, dim3(1), dim3(kRowsThreads), 0, stream, k.r);
         x = Operand{(const unsigned char*)p.x, 0, p.ld * 2, 0};
     } else {
-        pack<S>(p, X, W, true, k, x, w, stream);
+        pack<S>(p, X, W, true, false, k, x, w, stream);
     }
     int rc = SPHATTN_OK;
     const int dx_tile = p.dx_big ? 256 : 128, dx_at_once = p.dx_big ? kCus : 2 * kCus;
@@ -387,6 +399,7 @@ int run_vocab_bwd(const Vocab& p, const void* X, const void* W, const void* targ
         const Operand wi{p.T ? w.data + (size_t)v0 * w.ld : nullptr, w.part, w.ld, n};
         const Operand G{(const unsigned char*)p.G, (long long)p.T * p.piece * 2, p.piece * 2, 0};
         VocabArgs a{};
+        a.range = p.range;
         a.P = wi, a.Q = x, a.info = p.info, a.k = p.ld, a.slices = 1, a.V = p.V, a.v0 = v0, a.scale2 = scale * kLog2e;
         a.g_target = p.g_target, a.g_lse2 = p.g_lse2, a.g = p.g;
         a.G = p.G, a.G_part = (long long)p.T * p.piece, a.G_ld = p.piece;
@@ -394,6 +407,7 @@ int run_vocab_bwd(const Vocab& p, const void* X, const void* W, const void* targ
         if (p.T > 0) rc = launch_scores<S, Stage::G>(a, n, p.T, tiles, stream);
         if (rc != SPHATTN_OK) break;
         VocabArgs bx{}, bw{};
+        bx.range = bw.range = p.T ? p.range : nullptr;
         const bool with_dx = dX && p.T > 0, with_dw = dW != nullptr;
         bx.P = Operand{wi.data, wi.part, wi.ld, p.ld};
         bx.Q = G, bx.Q.size = p.T, bx.info = p.info, bx.k = n, bx.slices = p.slices;
@@ -412,8 +426,8 @@ int run_vocab_bwd(const Vocab& p, const void* X, const void* W, const void* targ
             rc = dw_big ? launch_tiles<Big, S, Stage::Dw>(bw, p.ld, n, stream) : launch_tiles<Mid, S, Stage::Dw>(bw, p.ld, n, stream);
     }
     if (rc == SPHATTN_OK && dX && p.T > 0)
-        hipLaunchKernelGGL((vocab_dx_kernel<S>), dim3((unsigned)(p.T + 3) / 4), dim3(256), 0, stream, p.dx, p.slices, p.ld,
-                           dx_tile, (p.ld + dx_tile - 1) / dx_tile, dx_at_once, p.place, p.info, dX, p.T, p.D);
+        hipLaunchKernelGGL((vocab_dx_kernel<S>), dim3((unsigned)(p.T + 3) / 4, (unsigned)(p.D + kDxCols - 1) / kDxCols), dim3(256), 0, stream, p.dx, p.slices, p.ld,
+                           dx_tile, (p.ld + dx_tile - 1) / dx_tile, dx_at_once, p.place, p.info, p.range, dX, p.T, p.D);
     return rc == SPHATTN_OK ? launched() : rc;
 }
 
@@ -581,17 +595,19 @@ int sphattn_clip_grads(const void* const* in, void* const* out, const long long*
             list.type[j] = (unsigned char)((int)t | (off(in[i], 16) || off(out[i], 16) ? 0 : 128));
             list.chunks += (size[i] + kClipChunk - 1) / kClipChunk;
         }
-        const long long most = kClipMostGroups;
-        return (int)(list.chunks < 1 ? 1 : list.chunks < most ? list.chunks : most);
     };
+    auto groups_of = [](long long chunks) { return (int)(chunks < 1 ? 1 : chunks < kClipMostGroups ? chunks : kClipMostGroups); };
     int n_sums = 0;
     for (int i = 0; i < n || i == 0; i += kClipBatch) {
-        const int groups = fill(i);
+        fill(i);
+        const int groups = groups_of(list.chunks);
         hipLaunchKernelGGL(clip_squares_kernel, dim3((unsigned)groups), dim3(kClipThreads), 0, s, list, sums + n_sums);
         n_sums += groups;
     }
-    for (int i = 0; i < n || i == 0; i += kClipBatch) {
-        const int groups = fill(i);
+    // (backwards, also within a launch: what was read last is in the last-level cache still)
+    for (int i = n > 0 ? (n - 1) / kClipBatch * kClipBatch : 0; i >= 0; i -= kClipBatch) {
+        if (n > kClipBatch) fill(i);
+        const int groups = groups_of(list.chunks);
         hipLaunchKernelGGL(clip_scale_kernel, dim3((unsigned)groups), dim3(kClipThreads), 0, s, list, sums, n_sums, max_norm, norm, i == 0);
     }
     return launched();

@@ -12,9 +12,12 @@
 // writing it as fp32 and reading it back.  G is rounded to the storage type (once; half a unit in the last place, 2^-9 of a
 // term in bf16, 2^-12 in fp16), sums are in fp32 throughout.
 //
-// fp32 storage: every value is written as three bf16 parts that are exactly it (8 + 8 + 8 bits), and a product is
-// six products of parts, the small ones first, on the same kernel; the three left out come to 2^-25 of a term on
-// average and 2^-21 at most.
+// fp32 storage: X, W and G are written as two fp16 parts each, the value rounded and what that left out rounded (11 + 11 bits, of
+// the value times a power of two that brings the tensor's largest element to 2^14 .. 2^15; G is at most 2^14 by itself), and a product is three
+// products of parts, the small ones first, on the same kernel.  A factor is off by 2^-23 on average and 2^-22 at most, below 2^-17 of its
+// tensor's largest element by 2^-40 of that; the product left out comes to 2^-22 of a term at most.  (Three bf16 parts and six
+// products are exact to 2^-25 on average; they took 444 us for 1999 x 8000 x 512 where these take 282, with 3.1e-7 against 64 bits, most of it
+// from the fp32 sums, where these have 3.2e-7 and fp32 products 1.6e-6.)
 #pragma once
 #include "sphattn_embed.hpp"
 #include "sphattn_pipelined.hpp"
@@ -27,6 +30,9 @@ struct VocabInfo {
     float up;                                      // factor of G in the workspace: a power of two (fp16 holds G near 2^14 with it)
     float down;                                    // factor of the sums behind it
 };
+
+// What X and W were multiplied by before they were split, inverted (fp32 storage).
+struct VocabRange { float x, w; };
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
@@ -100,9 +106,9 @@ struct Product {
             return across ? Stream{A.data + part * A.part + (long long)k0 * A.ld, k_end - k0}
                           : Stream{A.data + part * A.part + (long long)a0 * A.ld + (long long)k0 * 2, rows * A.ld - k0 * 2};
         };
-        // parts of P and Q by pair, small products first: (2,0) (0,2) (1,1) (1,0) (0,1) (0,0)
+        // parts of P and Q by pair, small products first: (1,0) (0,1) (0,0)
         int pair = 0, step = 0, copied = 0;        // of the next copies
-        Stream sp = start(PX, P, p0, T::BP, PAIRS == 1 ? 0 : 2), sq = start(QX, Q, q0, T::BQ, 0);
+        Stream sp = start(PX, P, p0, T::BP, PAIRS == 1 ? 0 : 1), sq = start(QX, Q, q0, T::BQ, 0);
         uint32_t to = lds0;
         auto words = [&](bool across, const Operand& A, const Stream& s, bool there) {
             const int left = there ? max(s.left, 0) : 0;
@@ -132,8 +138,8 @@ struct Product {
             if (PAIRS > 1 && step == steps && copied < total) {
                 step = 0;
                 ++pair;
-                sp = start(PX, P, p0, T::BP, pair == 2 || pair == 3);
-                sq = start(QX, Q, q0, T::BQ, pair == 1 ? 2 : pair == 2 || pair == 4);
+                sp = start(PX, P, p0, T::BP, 0);
+                sq = start(QX, Q, q0, T::BQ, pair == 1);
             }
         };
         auto copy_step = [&]() {
@@ -249,6 +255,7 @@ __device__ __forceinline__ TileAt tile_of(int id, int tiles_p, int tiles_q)
 struct VocabArgs {
     Operand P, Q;
     const VocabInfo* info;                         // NULL: all rows of Q count
+    const VocabRange* range;                       // fp32
     int k;                                         // length of the sum (dW: the rows that count)
     int first;                                     // tile of the launch's first workgroup
     int tiles_p, slices;
@@ -277,20 +284,25 @@ __device__ __forceinline__ int dx_slices(int rows, int T, int slices, int tile_q
     return max(slices, min(min(room, 32), target / (tq * tiles_p)));
 }
 
-// A value as three bf16 parts, cut rather than rounded: x = hi + mid + lo exactly.
-__device__ __forceinline__ void split3(float x, uint32_t& hi, uint32_t& mid, uint32_t& lo)
+// A value as two fp16 parts.  Infinite or NaN: in the first.
+__device__ __forceinline__ void split2(float x, _Float16& hi, _Float16& lo)
 {
-    const uint32_t bits = __builtin_bit_cast(uint32_t, x);
-    if ((bits & 0x7f800000) == 0x7f800000) {       // infinite or NaN: in the first part
-        hi = (bits & 0x7fffff) ? 0x7fc0 : bits >> 16;
-        mid = lo = 0;
-        return;
+    hi = (_Float16)x;
+    lo = (_Float16)(x - (float)hi);
+    if (__builtin_fabsf(x) == __builtin_inff() || x != x) lo = (_Float16)0.f;
+}
+
+// Four neighbouring values' parts
+__device__ __forceinline__ void split2(const float (&x)[4], i32x2& hi, i32x2& lo)
+{
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        _Float16 a, b, c, d;
+        split2(x[2 * r], a, b);
+        split2(x[2 * r + 1], c, d);
+        hi[r] = __builtin_bit_cast(int, f16x2{a, c});
+        lo[r] = __builtin_bit_cast(int, f16x2{b, d});
     }
-    hi = bits >> 16;
-    const float r = x - __builtin_bit_cast(float, bits & 0xffff0000);
-    const uint32_t rb = __builtin_bit_cast(uint32_t, r);
-    mid = rb >> 16;
-    lo = __builtin_bit_cast(uint32_t, r - __builtin_bit_cast(float, rb & 0xffff0000)) >> 16;
 }
 
 // Two accumulator fragments' rows of four 16-bit values, lane group g holding columns 4 g .. 4 g + 3 of each: afterwards group g has
@@ -312,6 +324,7 @@ __device__ __forceinline__ void vocab_tile(const VocabArgs& a, int block, SPH_LD
     if (a.info) {
         rows = __builtin_amdgcn_readfirstlane(a.info->rows);
         if constexpr (ST == Stage::Dw) down = a.info->down;
+        if constexpr (ST == Stage::Dw && S == Store::F32) down *= a.range ? a.range->x : 1.f;
     }
     Operand Q = a.Q;
     if constexpr (ST == Stage::Dw) {
@@ -330,7 +343,7 @@ __device__ __forceinline__ void vocab_tile(const VocabArgs& a, int block, SPH_LD
     const int per_slice = __builtin_amdgcn_readfirstlane(((k + kStepK - 1) / kStepK + slices - 1) / slices) * kStepK;
     const int k0 = min(k, __builtin_amdgcn_readfirstlane(tile.slice) * per_slice), k1 = min(k, k0 + per_slice);
 
-    Product<T, S == Store::F16, PX, QX, S == Store::F32 ? 6 : 1> prod;
+    Product<T, S != Store::Bf16, PX, QX, S == Store::F32 ? 3 : 1> prod;
     prod.run(a.P, Q, p0, q0, k0, k1, smem);
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -340,6 +353,7 @@ __device__ __forceinline__ void vocab_tile(const VocabArgs& a, int block, SPH_LD
     // tile together, so nothing hides these instructions: one maximum, one multiply-add, one exponential (16 cycles) and one addition
     // (or half a conversion) per logit, and everything that only the vocabulary's last tile or a row's target needs is kept out of that.
     float scale2 = a.scale2;
+    if constexpr (S == Store::F32 && (ST == Stage::Logits || ST == Stage::G)) scale2 *= a.range->x * a.range->w;
     if (ST != Stage::Dx && ST != Stage::Dw && scale2 < 0.f) {
         scale2 = -scale2;
 #pragma unroll
@@ -435,18 +449,13 @@ __device__ __forceinline__ void vocab_tile(const VocabArgs& a, int block, SPH_LD
                 value(i + 1, d[1]);
                 unsigned short* to = row + 16 * (i + (g & 1)) + 8 * (g >> 1);
                 if constexpr (S == Store::F32) {
-                    uint32_t w[2][3][4];
+                    i32x2 part[2][2];              // [part][fragment]
 #pragma unroll
-                    for (int f = 0; f < 2; ++f)
+                    for (int f = 0; f < 2; ++f) split2(d[f], part[0][f], part[1][f]);
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) split3(d[f][r], w[f][0][r], w[f][1][r], w[f][2][r]);
-#pragma unroll
-                    for (int part = 0; part < 3; ++part) {
-                        const auto& x = w[0][part];
-                        const auto& z = w[1][part];
-                        const i32x4 o = join_fragments(i32x2{(int)(x[0] | x[1] << 16), (int)(x[2] | x[3] << 16)},
-                                                       i32x2{(int)(z[0] | z[1] << 16), (int)(z[2] | z[3] << 16)});
-                        if (q < rows) *(i32x4*)(to + part * a.G_part) = o;
+                    for (int k = 0; k < 2; ++k) {
+                        const i32x4 o = join_fragments(part[k][0], part[k][1]);
+                        if (q < rows) *(i32x4*)(to + k * a.G_part) = o;
                     }
                 } else {
                     const i32x4 o = join_fragments(i32x2{pack2<S == Store::F16>(d[0][0], d[0][1]), pack2<S == Store::F16>(d[0][2], d[0][3])},
@@ -531,7 +540,7 @@ enum class Reduce { None, Sum, Mean };             // of dloss: [T], or one valu
 struct RowArgs {
     const void* targets; int id_bytes; int T;
     int* rows; int* place; VocabInfo* info;
-    const float* dloss; Reduce reduce; float scale; int half;
+    const float* dloss; Reduce reduce; float scale; int half;   // half: G is stored in fp16
 };
 
 // `top`: the largest |dloss| of a row that counts, where there is one for each
@@ -619,7 +628,63 @@ void vocab_rows_kernel(RowArgs a)
     *a.info = row_scale(a, n, top);
 }
 
-// Rows as the products want them: 16-bit, 16-byte aligned, whole pieces of 8; gathered if only some count; fp32 in three
+// The largest finite magnitude of W and of the rows of X that count: one per workgroup, for the packing ones to join.  fp32 only.
+constexpr int kRangeThreads = 256, kRangeGroupsX = 256, kRangeGroupsW = 512;
+
+__global__ __launch_bounds__(kRangeThreads)
+void vocab_range_kernel(const float* __restrict__ X, const float* __restrict__ W, int T, int V, int D, const void* __restrict__ targets, int id_bytes,
+                        int all_rows, float* __restrict__ most)
+{
+    __shared__ float shared[kRangeThreads / 64];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    float top = 0.f;
+    auto take = [&](float x) {
+        x = __builtin_fabsf(x);
+        top = x < __builtin_inff() ? fmaxf(top, x) : top;
+    };
+    constexpr int AHEAD = 8;
+    if (blockIdx.x < kRangeGroupsX) {
+        constexpr int WAVES = kRangeThreads / 64;
+        for (long long t = (long long)blockIdx.x * WAVES + wave; t < T; t += kRangeGroupsX * WAVES) {
+            if (!all_rows && load_id(targets, id_bytes, t) < 0) continue;
+            const float* row = X + (size_t)t * D;
+            for (int c0 = lane; c0 < D; c0 += 64 * AHEAD) {
+                float x[AHEAD];
+#pragma unroll
+                for (int a = 0; a < AHEAD; ++a) x[a] = c0 + a * 64 < D ? row[c0 + a * 64] : 0.f;
+#pragma unroll
+                for (int a = 0; a < AHEAD; ++a) take(x[a]);
+            }
+        }
+    } else {
+        const size_t n = (size_t)V * D, n4 = ((uintptr_t)W & 15) == 0 ? n / 4 : 0, step = (size_t)kRangeGroupsW * kRangeThreads;
+        const size_t i0 = (size_t)(blockIdx.x - kRangeGroupsX) * kRangeThreads + tid;
+        for (size_t i = i0; i < n4; i += step * AHEAD) {
+            f32x4 x[AHEAD];
+#pragma unroll
+            for (int a = 0; a < AHEAD; ++a) x[a] = i + a * step < n4 ? ((const f32x4*)W)[i + a * step] : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int a = 0; a < AHEAD; ++a)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) take(x[a][r]);
+        }
+        for (size_t i = 4 * n4 + i0; i < n; i += step) take(W[i]);
+    }
+    top = max_over_wave(top);
+    if (lane == 0) shared[wave] = top;
+    __syncthreads();
+    if (tid != 0) return;
+    for (int w = 1; w < kRangeThreads / 64; ++w) top = fmaxf(top, shared[w]);
+    most[blockIdx.x] = top;
+}
+
+// The power of two that brings `top` to 2^14 .. 2^15 (1 for a tensor of zeros; both it and its inverse are normal numbers)
+__device__ __forceinline__ float range_factor(float top)
+{
+    return top > 0.f ? __builtin_ldexpf(1.f, min(126, 15 - __builtin_amdgcn_frexp_expf(top))) : 1.f;
+}
+
+// Rows as the products want them: 16-bit, 16-byte aligned, whole pieces of 8; gathered if only some count; fp32 in two
 // parts.  One wave per row; X's and W's in one launch.  For at most kOwnRows rows each workgroup finds out by itself which rows before its
 // own count, which spares a launch of one workgroup in front.
 constexpr int kPackThreads = 256, kPackRows = kPackThreads / 64, kOwnRows = 1024;
@@ -634,41 +699,30 @@ struct PackArgs {
     int compact, own_rows;                         // only X's rows that count; found here
     RowArgs r;
     const float* lse; int* g_target; float* g_lse2; float* g;   // what the G stage needs of each row, or NULL
+    const float* most; VocabRange* range;          // fp32: from vocab_range_kernel, and what was made of it
 };
 
 template <Store S>
-__device__ __forceinline__ void pack_row(const PackRows& a, long long t, long long m, int lane)
+__device__ __forceinline__ void pack_row(const PackRows& a, long long t, long long m, int lane, float factor)
 {
     const size_t from = (size_t)t * a.D, to = (size_t)m * a.ld;
     constexpr int N = per16<S>();
     const bool wide = ((uintptr_t)a.in & 15) == 0 && a.D % N == 0;
-    if (S != Store::F32 && wide) {
-        for (int c = lane; c < a.ld / 8; c += 64) ((i32x4*)a.out)[to / 8 + c] = ((const i32x4*)a.in)[from / 8 + c];
-        return;
-    }
-    for (int c = lane * 4; c < a.ld; c += 256) {
+    for (int c = lane * N; c < a.ld; c += 64 * N) {
+        i32x4 w = {0, 0, 0, 0};
+        if (c < a.D) w = wide ? load16<S, true>(a.in, from + c, N, N) : load16<S, false>(a.in, from + c, a.D - c, (size_t)a.n * a.D - from - c);
         if constexpr (S == Store::F32) {
-            float x[4] = {0.f, 0.f, 0.f, 0.f};
-            if (wide) {
-                if (c < a.D) *(f32x4*)x = *(const f32x4*)((const float*)a.in + from + c);
-            } else {
+            float x[4];
+            widen16<S>(w, x);
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    if (c + r < a.D) x[r] = ((const float*)a.in)[from + c + r];
-            }
-            uint32_t h[4], md[4], l[4];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) split3(x[r], h[r], md[r], l[r]);
+            for (int r = 0; r < 4; ++r) x[r] *= factor;
+            i32x2 hi, lo;
+            split2(x, hi, lo);
             unsigned short* o = (unsigned short*)a.out + to + c;
-            *(i32x2*)o = i32x2{(int)(h[0] | h[1] << 16), (int)(h[2] | h[3] << 16)};
-            *(i32x2*)(o + a.part) = i32x2{(int)(md[0] | md[1] << 16), (int)(md[2] | md[3] << 16)};
-            *(i32x2*)(o + 2 * a.part) = i32x2{(int)(l[0] | l[1] << 16), (int)(l[2] | l[3] << 16)};
+            *(i32x2*)o = hi;
+            *(i32x2*)(o + a.part) = lo;
         } else {
-            uint32_t x[4] = {0, 0, 0, 0};
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-                if (c + r < a.D) x[r] = ((const unsigned short*)a.in)[from + c + r];
-            *(i32x2*)((unsigned short*)a.out + to + c) = i32x2{(int)(x[0] | x[1] << 16), (int)(x[2] | x[3] << 16)};
+            *(i32x4*)((unsigned short*)a.out + to + c) = w;
         }
     }
 }
@@ -678,9 +732,23 @@ __global__ __launch_bounds__(kPackThreads)
 void vocab_pack_kernel(PackArgs a)
 {
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    if ((int)blockIdx.x >= a.x_groups) {
+    const bool on_x = (int)blockIdx.x < a.x_groups;
+    float factor = 1.f;
+    if constexpr (S == Store::F32) {
+        __shared__ float tops[kPackRows];
+        float top = 0.f;
+        for (int i = tid; i < (on_x ? kRangeGroupsX : kRangeGroupsW); i += kPackThreads) top = fmaxf(top, a.most[(on_x ? 0 : kRangeGroupsX) + i]);
+        top = max_over_wave(top);
+        if (lane == 0) tops[wave] = top;
+        __syncthreads();
+        for (int w = 0; w < kPackRows; ++w) top = fmaxf(top, tops[w]);
+        factor = range_factor(top);
+        if (tid == 0 && blockIdx.x == 0) a.range->x = 1.f / factor;
+        if (tid == 0 && (int)blockIdx.x == a.x_groups) a.range->w = 1.f / factor;
+    }
+    if (!on_x) {
         const long long v = (long long)((int)blockIdx.x - a.x_groups) * kPackRows + wave;
-        if (v < a.w.n) pack_row<S>(a.w, v, v, lane);
+        if (v < a.w.n) pack_row<S>(a.w, v, v, lane, factor);
         return;
     }
     const long long row = (long long)blockIdx.x * kPackRows + wave;
@@ -726,7 +794,7 @@ void vocab_pack_kernel(PackArgs a)
         a.g_lse2[m] = a.lse[t] * kLog2e;
         a.g[m] = (a.r.reduce == Reduce::None ? a.r.dloss[t] * a.r.scale : 1.f) * up;
     }
-    pack_row<S>(a.x, t, m, lane);
+    pack_row<S>(a.x, t, m, lane, factor);
 }
 
 // The tiles' maxima and sums joined: 2^log_rows rows per workgroup (64 at most), its other lanes and waves a share of the tiles each.
@@ -815,26 +883,39 @@ void vocab_mean_kernel(const float* __restrict__ losses, const void* __restrict_
     *mean = (float)(!divide ? sum : n > 0.0 ? sum / n : 0.0);
 }
 
-// dX: the slices' sums, in order, scaled back and rounded; zeros for rows that do not count.  One wave per row.
+// dX: the slices' sums, in order, scaled back and rounded; zeros for rows that do not count.  One wave per row and 256 columns, eight slices'
+// loads under way.  (64 slices of 17 x 1024, one after the other: 113 us.)
+constexpr int kDxCols = 256;
+
 template <Store S>
 __global__ __launch_bounds__(256)
 void vocab_dx_kernel(const float* __restrict__ part, int slices, int ld, int tile_q, int tiles_p, int target, const int* __restrict__ place,
-                     const VocabInfo* __restrict__ info, void* __restrict__ dX, int T, int D)
+                     const VocabInfo* __restrict__ info, const VocabRange* __restrict__ range, void* __restrict__ dX, int T, int D)
 {
     const int lane = threadIdx.x & 63;
     const long long t = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (t >= T) return;
     const int m = place[t];
-    const float down = info->down;
+    float down = info->down;
+    if constexpr (S == Store::F32) down *= range->w;
     const int rows = info->rows;
     const size_t slice = (size_t)rows * ld;
     slices = dx_slices(rows, T, slices, tile_q, tiles_p, target);
     const bool wide = ((uintptr_t)dX & 15) == 0 && D % 4 == 0;
-    for (int c = lane * 4; c < D; c += 256) {
+    const int c = (int)blockIdx.y * kDxCols + lane * 4;
+    if (c < D) {
         f32x4 x = {0.f, 0.f, 0.f, 0.f};
         if (m >= 0) {
             const float* from = part + (size_t)m * ld + c;
-            for (int s = 0; s < slices; ++s) x += *(const f32x4*)(from + s * slice);
+            constexpr int AHEAD = 8;
+            for (int s0 = 0; s0 < slices; s0 += AHEAD) {
+                f32x4 y[AHEAD];
+#pragma unroll
+                for (int a = 0; a < AHEAD; ++a) y[a] = *(const f32x4*)(from + min(s0 + a, slices - 1) * slice);
+#pragma unroll
+                for (int a = 0; a < AHEAD; ++a)
+                    if (s0 + a < slices) x += y[a];
+            }
         }
 #pragma unroll
         for (int r = 0; r < 4; ++r) x[r] *= down;

@@ -106,6 +106,21 @@ def test_gradients_of_other_layouts(monkeypatch):
 
 
 @pytest.mark.gpu
+def test_without_multiplicities(monkeypatch):
+    tokens, table, _, X, _ = _inputs(torch.bfloat16, torch.int64, 10)
+    table.requires_grad_(True)
+
+    def step():
+        out = autograd.token_embedding(tokens, table, scale=0.3)
+        return [out.detach(), *torch.autograd.grad(out, (table,), X)]
+    with monkeypatch.context() as patch:
+        patch.setattr(pkg, "_ids", None)
+        fast = step()
+    monkeypatch.setattr(pkg, "_fast", pkg._PythonOnly)
+    _same(fast, step())
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("python", [False, True])
 def test_no_second_derivative(monkeypatch, python):
     if python:

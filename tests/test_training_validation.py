@@ -79,7 +79,7 @@ def test_workspaces_hold_what_their_sizes_say(lib):
     for T in (0, 1, 4097, 2 ** 20):
         for V in (1, 50003, 2 ** 24):
             for D in (1, 515, 65536):
-                for dtype, parts in ((0, 3), (1, 1), (3, 1)):
+                for dtype, parts in ((0, 2), (1, 1), (3, 1)):
                     at_least = 2 * parts * (T + V) * D
                     assert lib.sphattn_vocab_loss_workspace_bytes(T, V, D, dtype) > at_least
                     assert lib.sphattn_vocab_loss_bwd_workspace_bytes(T, V, D, dtype) > at_least + 4 * T * D
