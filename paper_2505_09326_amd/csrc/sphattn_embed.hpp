@@ -168,13 +168,6 @@ constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64, kSortMaxIds =
 
 constexpr int sort_lds_bytes(int ids) { return (kSortWaves * ids + 2 * kSortWaves + 2) * 4; }
 
-__device__ __forceinline__ int sum_over_wave(int x)
-{
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) x += __shfl_xor(x, d);
-    return x;
-}
-
 // sum of x over the lanes below, and `total` over all
 __device__ __forceinline__ int exclusive_over_wave(int x, int lane, int& total)
 {
@@ -207,11 +200,30 @@ void embed_sort_kernel(const void* __restrict__ tokens, int id_bytes, int* __res
     // Eight times 64 positions at a time; one round per different own id among them, over all eight.  (One LDS access per id and eight batches
     // instead of one per batch: each waits for the one before it, and a token at half of 32768 positions made 32 us of them.)
     constexpr int AHEAD = 8;
-    int below = 0;
+    int below = 0, next[AHEAD];
+    // One turn before they are needed.  Every workgroup does this with every token, so instructions count: 64 tokens took 45 of them with a
+    // check and 64-bit comparisons at each load (32768 tokens 30 us).  What is no id of the table becomes -1.
+    auto fetch = [&](long long t) {
+        if (t + 64 * AHEAD > t1) {
+#pragma unroll
+            for (int a = 0; a < AHEAD; ++a) next[a] = t + a * 64 + lane < t1 ? load_id(tokens, id_bytes, t + a * 64 + lane) : -1;
+        } else if (id_bytes == 4) {
+            const int* from = (const int*)tokens + t + lane;
+#pragma unroll
+            for (int a = 0; a < AHEAD; ++a) next[a] = from[a * 64];
+        } else {
+            const int2* from = (const int2*)tokens + t + lane;
+#pragma unroll
+            for (int a = 0; a < AHEAD; ++a) {
+                const int2 x = from[a * 64];
+                next[a] = x.y == 0 ? x.x : -1;
+            }
+        }
+    };
     auto each_id = [&](const int (&v)[AHEAD], auto&& round) {
         uint64_t left[AHEAD];
 #pragma unroll
-        for (int a = 0; a < AHEAD; ++a) left[a] = __ballot(v[a] >= lo && v[a] < lo + n_ids);
+        for (int a = 0; a < AHEAD; ++a) left[a] = __ballot((unsigned)(v[a] - lo) < (unsigned)n_ids);
 #pragma unroll
         for (int a = 0; a < AHEAD; ++a) {
             while (left[a]) {
@@ -226,12 +238,14 @@ void embed_sort_kernel(const void* __restrict__ tokens, int id_bytes, int* __res
             }
         }
     };
+    fetch(t0);
     for (long long t = t0; t < t1; t += 64 * AHEAD) {
         int v[AHEAD];
 #pragma unroll
-        for (int a = 0; a < AHEAD; ++a) v[a] = t + a * 64 + lane < t1 ? load_id(tokens, id_bytes, t + a * 64 + lane) : -1;
+        for (int a = 0; a < AHEAD; ++a) v[a] = next[a];
+        fetch(t + 64 * AHEAD);
 #pragma unroll
-        for (int a = 0; a < AHEAD; ++a) below += v[a] >= 0 && v[a] < lo;
+        for (int a = 0; a < AHEAD; ++a) below += __builtin_popcountll(__ballot((unsigned)v[a] < (unsigned)lo));
         each_id(v, [&](int id, const uint64_t (&same)[AHEAD]) {
             int n = 0;
 #pragma unroll
@@ -239,7 +253,6 @@ void embed_sort_kernel(const void* __restrict__ tokens, int id_bytes, int* __res
             if (lane == 0) mine[id - lo] += n;     // (no other wave has this row of counts)
         });
     }
-    below = sum_over_wave(below);
     if (lane == 0) part[wave] = below;
     __syncthreads();
 
@@ -268,10 +281,12 @@ void embed_sort_kernel(const void* __restrict__ tokens, int id_bytes, int* __res
     }
     __syncthreads();
 
+    fetch(t0);
     for (long long t = t0; t < t1; t += 64 * AHEAD) {
         int v[AHEAD];
 #pragma unroll
-        for (int a = 0; a < AHEAD; ++a) v[a] = t + a * 64 + lane < t1 ? load_id(tokens, id_bytes, t + a * 64 + lane) : -1;
+        for (int a = 0; a < AHEAD; ++a) v[a] = next[a];
+        fetch(t + 64 * AHEAD);
         each_id(v, [&](int id, const uint64_t (&same)[AHEAD]) {
             int p = mine[id - lo];
 #pragma unroll
@@ -303,6 +318,8 @@ void embed_sort_kernel(const void* __restrict__ tokens, int id_bytes, int* __res
 // shared by as many waves as it fills pieces.  A wave adds up a piece's runs of equal tokens over 64 lanes' columns in fp32.  A
 // run that lies inside the piece is a row of the gradient; one that crosses its borders leaves a partial sum: [piece][0] if
 // it began before the piece, [piece][1] if it begins in it and goes on behind it.
+__host__ __device__ constexpr int partial_ld(int D) { return (D + 7) / 8 * 8; }   // floats per row of partial sums
+
 template <Store S, bool WIDE>
 __global__ __launch_bounds__(kEmbedThreads)
 void embed_sum_kernel(const void* __restrict__ tokens, int id_bytes, const float* __restrict__ mult, const void* __restrict__ dO,
@@ -326,10 +343,9 @@ void embed_sum_kernel(const void* __restrict__ tokens, int id_bytes, const float
         if (live) {
             if (r0 >= p0 && r1 <= p1) store16<S, WIDE>(dtable, (size_t)id * D + col, narrow16<S>(acc), D - col);
             else {
-                float* to = partial + ((size_t)piece * 2 + (r0 < p0 ? 0 : 1)) * D + col;
+                float* to = partial + ((size_t)piece * 2 + (r0 < p0 ? 0 : 1)) * partial_ld(D) + col;
 #pragma unroll
-                for (int i = 0; i < C; ++i)
-                    if (WIDE || col + i < D) to[i] = acc[i];
+                for (int i = 0; i < C; ++i) to[i] = acc[i];
             }
         }
 #pragma unroll
@@ -407,9 +423,9 @@ void embed_join_kernel(const void* __restrict__ tokens, int id_bytes, const int*
 #pragma unroll
             for (int a = 0; a < AHEAD; ++a) {
                 const long long at = min(q + a, q1 - 1);   // (loads without a condition: none waits for another)
-                const float* from = partial + ((size_t)at * 2 + (at == piece ? 1 : 0)) * D + col;
+                const float* from = partial + ((size_t)at * 2 + (at == piece ? 1 : 0)) * partial_ld(D) + col;
 #pragma unroll
-                for (int i = 0; i < C; ++i) x[a][i] = from[WIDE ? i : min(i, D - 1 - col)];
+                for (int i = 0; i < C; ++i) x[a][i] = from[i];
             }
 #pragma unroll
             for (int a = 0; a < AHEAD; ++a)

@@ -114,14 +114,15 @@ EmbedPlan embed_plan(int T, int V, int D, void* workspace)
     p.ids = (V + kCus - 1) / kCus;
     p.ids = p.ids < kSortMaxIds ? p.ids : kSortMaxIds;
     p.sort_groups = (V + p.ids - 1) / p.ids;
-    // pieces of 16 positions: a wave has 16 rows to add up, eight of them under way; no run has more than 2048 pieces
+    // pieces of 16 positions: a wave has 16 rows to add up, eight of them under way.  Longer ones once four waves per CU have work (of 512
+    // columns of two bytes each): that many reach memory's rate, and a run over many pieces has fewer partial sums to join.
     p.len = 16;
-    while (((long long)T + p.len - 1) / p.len > 2048) p.len *= 2;
+    while (((long long)T + p.len - 1) / p.len * ((D + 511) / 512) > 4 * kCus && p.len < 1 << 20) p.len *= 2;
     p.pieces = (int)(((long long)T + p.len - 1) / p.len);
     Carve c(workspace);
     p.first = c.take<int>((size_t)V + 1);
     p.sorted = c.take<int>(T);
-    p.partial = c.take<float>((size_t)p.pieces * 2 * D);
+    p.partial = c.take<float>((size_t)p.pieces * 2 * partial_ld(D));
     p.bytes = c.used();
     return p;
 }
