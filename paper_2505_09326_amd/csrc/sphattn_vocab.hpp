@@ -12,11 +12,15 @@
 // writing it as fp32 and reading it back.  G is rounded to the storage type (once; half a unit in the last place, 2^-9 of a
 // term in bf16, 2^-12 in fp16), sums are in fp32 throughout.
 //
+// Bound by the matrix pipes where the sums are long: 8192 rows, 65536 ids, width 2048 in bf16 7.0 ms, 8 T V D at 1250 TFLOP/s, what a
+// library product of 8192^3 reaches (1266).  At width 1024 a tile's end, its exponentials and stores, has no other tile's products beside it: logits and
+// G run at 0.57 busy pipes against 0.75 of dW (8192 x 32768 1.96 ms).  One row: W at 5.3 TB/s.
+//
 // fp32 storage: X, W and G are written as two fp16 parts each, the value rounded and what that left out rounded (11 + 11 bits, of
 // the value times a power of two that brings the tensor's largest element to 2^14 .. 2^15; G is at most 2^14 by itself), and a product is three
 // products of parts, the small ones first, on the same kernel.  A factor is off by 2^-23 on average and 2^-22 at most, below 2^-17 of its
 // tensor's largest element by 2^-40 of that; the product left out comes to 2^-22 of a term at most.  (Three bf16 parts and six
-// products are exact to 2^-25 on average; they took 444 us for 1999 x 8000 x 512 where these take 282, with 3.1e-7 against 64 bits, most of it
+// products are exact to 2^-25 on average; they took 444 us for 1999 x 8000 x 512 where these take 273 to 283, with 3.1e-7 against 64 bits, most of it
 // from the fp32 sums, where these have 3.2e-7 and fp32 products 1.6e-6.)
 #pragma once
 #include "sphattn_embed.hpp"
@@ -62,6 +66,8 @@ constexpr int kStepK = 32;
 // place of 16-byte piece c in row k of an operand stored across, and the piece in place c
 __device__ __forceinline__ int across_slot(int k, int c) { return c ^ (2 * ((k & 3) | (k >> 1 & 4))); }
 
+// Tiles of 256 x 256 on eight waves of 128 x 64: an operand byte in LDS feeds four or eight matrix instructions, 0.4 LDS reads per instruction (0.75
+// transposed), and 128 KB of LDS hold four steps.
 // The sum over k runs in steps of 32.  A step's part of the two operands is BP / 16 + BQ / 16 blocks of 1 KB, copied
 // straight into one of NBUF LDS buffers, NBUF - 1 steps ahead; a step's fragments are read from LDS while the matrix
 // instructions of the step before run, so that behind the one barrier per step the matrix pipe has its operands already.
@@ -275,7 +281,7 @@ enum class Stage { Logits, G, Dx, Dw };
 
 // Slices of dX's sum over the vocabulary for `rows` rows that count, where a launch for T of them has `slices`: as many more as
 // workgroups and arrays of partial sums are then free, while the chip is not full.  (8000 rows of which 1200 count, 20011 ids, width 1024:
-// dX 84 -> 21 us per half of the ids.)
+// dX 85 -> 41 us per half of the ids, and 9 more to add the slices up.)
 __device__ __forceinline__ int dx_slices(int rows, int T, int slices, int tile_q, int tiles_p, int target)
 {
     const int tq = (rows + tile_q - 1) / tile_q, tq_all = (T + tile_q - 1) / tile_q;
