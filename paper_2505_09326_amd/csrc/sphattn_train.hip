@@ -215,6 +215,16 @@ void dx_choice(long long T, long long ld, int n, bool& big, int& slices)
     }
 }
 
+// fp32 and few rows: kernels that read fp32 as it is
+bool rows_form(int T, int dtype) { return dtype == SPHATTN_F32 && T > 0 && T <= Low::BQ; }
+
+// Slices of dX's sum there: eight waves per CU of 64 columns each, of 128 ids at least
+int rows_slices(int V, int D)
+{
+    const int blocks = (D + 63) / 64, most = V / 128 < 128 ? V / 128 : 128, want = (8 * kCus + blocks - 1) / blocks;
+    return most < 1 ? 1 : want < most ? want : most;
+}
+
 Vocab vocab_fwd_plan(int T, int V, int D, int dtype, void* workspace)
 {
     Vocab p{};
@@ -246,7 +256,8 @@ Vocab vocab_bwd_plan(int T, int V, int D, int dtype, void* workspace)
     p.n_pieces = (int)((V + most - 1) / most);
     p.piece = (int)up_to((V + p.n_pieces - 1) / p.n_pieces, 256);
     p.n_pieces = (V + p.piece - 1) / p.piece;
-    dx_choice(T > 0 ? T : 1, p.ld, p.piece < V ? p.piece : V, p.dx_big, p.slices);
+    if (rows_form(T, dtype)) p.slices = rows_slices(V, D);
+    else dx_choice(T > 0 ? T : 1, p.ld, p.piece < V ? p.piece : V, p.dx_big, p.slices);
     Carve c(workspace);
     p.info = c.take<VocabInfo>(1);
     p.range = c.take<VocabRange>(1);
@@ -268,8 +279,9 @@ template <class T, Store S, Stage ST>
 int launch_tiles(VocabArgs& a, int p, int q, hipStream_t stream)
 {
     const auto kern = vocab_tile_kernel<T, S, ST>;
+    constexpr int LDS = reads_fp32<T, S, ST>() ? T::WAVES_P * T::BQ * 8 : T::LDS;   // (sums per row only)
     static std::atomic<uint64_t> done{0};
-    if (T::LDS > 65536 && !raise_lds_limit(kern, T::LDS, done)) return SPHATTN_ERR_LAUNCH;
+    if (LDS > 65536 && !raise_lds_limit(kern, LDS, done)) return SPHATTN_ERR_LAUNCH;
     a.tiles_p = (p + T::BP - 1) / T::BP;
     const long long tiles = (long long)a.tiles_p * ((q + T::BQ - 1) / T::BQ) * a.slices;
     if (tiles > INT_MAX) return SPHATTN_ERR_SHAPE;
@@ -277,7 +289,7 @@ int launch_tiles(VocabArgs& a, int p, int q, hipStream_t stream)
     constexpr long long MOST = 1 << 22;
     for (long long first = 0; first < tiles; first += MOST) {
         a.first = (int)first;
-        hipLaunchKernelGGL(kern, dim3((unsigned)(tiles - first < MOST ? tiles - first : MOST)), dim3(T::THREADS), T::LDS, stream, a);
+        hipLaunchKernelGGL(kern, dim3((unsigned)(tiles - first < MOST ? tiles - first : MOST)), dim3(T::THREADS), LDS, stream, a);
     }
     return launched();
 }
@@ -357,10 +369,16 @@ int run_vocab_fwd(const Vocab& p, const void* X, const void* W, const void* targ
     PackArgs k{};
     k.r = row_args(p, targets, id_bytes);
     k.compact = !all_rows && p.T > Low::BQ;        // (up to one tile's rows cost the same whether they count or not)
-    pack<S>(p, X, W, k.compact || !ready(X, p.D, S), all_rows, k, a.Q, a.P, stream);
+    if (S == Store::F32 && rows_form(p.T, SPHATTN_F32)) {
+        a.P = Operand{(const unsigned char*)W, 0, 0, p.V}, a.Q = Operand{(const unsigned char*)X, 0, 0, p.T};
+        a.k = p.D, a.T = p.T;
+    } else {
+        pack<S>(p, X, W, k.compact || !ready(X, p.D, S), all_rows, k, a.Q, a.P, stream);
+        a.k = p.ld;
+    }
     if (k.compact) a.info = p.info, a.rows = p.rows;
     a.range = p.range;
-    a.k = p.ld, a.slices = 1, a.V = p.V, a.scale2 = scale * kLog2e;
+    a.slices = 1, a.V = p.V, a.scale2 = scale * kLog2e;
     a.targets = targets, a.id_bytes = id_bytes;
     a.partial = p.partial, a.partial_ld = p.T, a.target_logit = p.target_logit;
     int tiles = 0;
@@ -378,6 +396,41 @@ int run_vocab_fwd(const Vocab& p, const void* X, const void* W, const void* targ
     return launched();
 }
 
+// fp32, at most 64 rows
+int run_rows_bwd(const Vocab& p, const void* X, const void* W, PackArgs k, void* dX, void* dW, float scale, hipStream_t stream)
+{
+    constexpr Store S = Store::F32;
+    // which rows count and what G needs of them (X's parts, a few rows, are not looked at)
+    k.x = PackRows{X, p.x, p.T, p.D, p.ld, (long long)p.T * p.ld};
+    k.x_groups = (p.T + kPackRows - 1) / kPackRows, k.own_rows = 1;
+    hipLaunchKernelGGL((vocab_pack_kernel<S>), dim3((unsigned)k.x_groups), dim3(kPackThreads), 0, stream, k);
+    const int blocks = (p.D + 63) / 64;
+    for (int i = 0; i < p.n_pieces; ++i) {
+        const int v0 = i * p.piece, n = p.V - v0 < p.piece ? p.V - v0 : p.piece;
+        VocabArgs a{};
+        a.P = Operand{(const unsigned char*)W + (size_t)v0 * p.D * 4, 0, 0, n}, a.Q = Operand{(const unsigned char*)X, 0, 0, p.T};
+        a.info = p.info, a.rows = p.rows, a.k = p.D, a.T = p.T, a.slices = 1, a.V = p.V, a.v0 = v0, a.scale2 = scale * kLog2e;
+        a.g_target = p.g_target, a.g_lse2 = p.g_lse2, a.g = p.g, a.G = p.G, a.G_ld = p.piece;
+        int tiles;
+        const int rc = launch_scores<S, Stage::G>(a, n, p.T, tiles, stream);
+        if (rc != SPHATTN_OK) return rc;
+        if (dX) {
+            a.slices = p.slices, a.out = p.dx, a.out_ld = p.ld, a.accumulate = i > 0;
+            const dim3 grid((unsigned)((long long)blocks * p.slices + 3) / 4);
+            if (p.T <= 16) hipLaunchKernelGGL((vocab_rows_dx_kernel<1>), grid, dim3(256), 0, stream, a);
+            else hipLaunchKernelGGL((vocab_rows_dx_kernel<4>), grid, dim3(256), 0, stream, a);
+        }
+        if (dW) {
+            a.out = (unsigned char*)dW + (size_t)v0 * p.D * 4, a.out_rows = n;
+            hipLaunchKernelGGL(vocab_rows_dw_kernel, dim3((unsigned)(((long long)(n + 63) / 64 * blocks + 3) / 4)), dim3(256), 0, stream, a);
+        }
+    }
+    if (dX)
+        hipLaunchKernelGGL((vocab_dx_kernel<S>), dim3((unsigned)(p.T + 3) / 4, (unsigned)(p.D + kDxCols - 1) / kDxCols), dim3(256), 0, stream, p.dx, p.slices,
+                           p.ld, 128, 1, 0, p.place, p.info, (const VocabRange*)nullptr, dX, p.T, p.D);
+    return launched();
+}
+
 template <Store S>
 int run_vocab_bwd(const Vocab& p, const void* X, const void* W, const void* targets, int id_bytes, const float* lse, const float* dloss,
                   void* dX, void* dW, float scale, int reduction, hipStream_t stream)
@@ -390,6 +443,8 @@ int run_vocab_bwd(const Vocab& p, const void* X, const void* W, const void* targ
     if (p.T == 0) {                                // (the info of no rows, which one workgroup writes)
         hipLaunchKernelGGL(vocab_rows_kernel, dim3(1), dim3(kRowsThreads), 0, stream, k.r);
         x = Operand{(const unsigned char*)p.x, 0, p.ld * 2, 0};
+    } else if (S == Store::F32 && rows_form(p.T, SPHATTN_F32)) {
+        return run_rows_bwd(p, X, W, k, dX, dW, scale, stream);
     } else {
         pack<S>(p, X, W, true, false, k, x, w, stream);
     }

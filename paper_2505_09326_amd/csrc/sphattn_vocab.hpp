@@ -26,6 +26,8 @@
 #include "sphattn_embed.hpp"
 #include "sphattn_pipelined.hpp"
 
+#include <type_traits>
+
 namespace sphattn {
 
 // What the host cannot know: how many rows count, and how their gradients are scaled.
@@ -265,7 +267,7 @@ struct VocabArgs {
     int k;                                         // length of the sum (dW: the rows that count)
     int first;                                     // tile of the launch's first workgroup
     int tiles_p, slices;
-    int T, target;                                 // dX: rows that the slices' arrays are made for, workgroups that the chip runs at once
+    int T, target;                                 // rows of X; dX: workgroups that the chip runs at once (0: slices are as they are)
     // logits and G: the vocabulary ids p0 .. of this launch, V of them in all
     int V, v0;
     float scale2;                                  // c log2(e)
@@ -288,6 +290,198 @@ __device__ __forceinline__ int dx_slices(int rows, int T, int slices, int tile_q
     if (rows <= 0) return slices;
     const int room = (int)min((long long)tq_all * slices / tq, (long long)T * slices / rows);
     return max(slices, min(min(room, 32), target / (tq * tiles_p)));
+}
+
+// D = A (16 x 4) B (4 x 16) + C on element ea of a's registers and eb of b's
+__device__ __forceinline__ f32x4 mfma_f32(i32x4 a, int ea, i32x4 b, int eb, f32x4 c)
+{
+    const int x = a[ea], y = b[eb];                // (a bit cast of the vector's element itself takes the vector's first)
+    return __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, x), __builtin_bit_cast(float, y), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mfma_f32(i32x4 a, i32x4 b, int e, f32x4 c) { return mfma_f32(a, e, b, e, c); }
+
+// fp32 with at most 64 rows: W decides the time, so it is read as it is, once, straight into registers, and multiplied by the fp32 matrix
+// instruction (16x16x4, a twelfth of the 16-bit rate: 64 rows of width 1024 take it as long as their W takes memory).  Lane (i, g) holds four neighbouring
+// k, 4 g .. 4 g + 3 of sixteen, of row i of both operands, and instruction r takes the r-th: any order of k will do if both have it.
+template <class T>
+struct RowsProduct {
+    f32x4 acc[T::FP][T::FQ];
+
+    __device__ __forceinline__ void run(const VocabArgs& a, int rows, int p0, int q0)
+    {
+        constexpr int CH = T::FQ > 1 ? 2 : 4;      // times sixteen k under way, and as many being multiplied
+        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n16 = lane & 15, g = lane >> 4, D = a.k;
+        const float *W = (const float*)a.P.data, *X = (const float*)a.Q.data;
+        const bool wide = (((uintptr_t)W | (uintptr_t)X) & 15) == 0 && D % 4 == 0;
+        size_t pat[T::FP], qat[T::FQ];             // (rows behind the last one take the last one's place: their results are not looked at)
+#pragma unroll
+        for (int i = 0; i < T::FP; ++i) pat[i] = (size_t)min(p0 + (wave * T::FP + i) * 16 + n16, a.P.size - 1) * D;
+#pragma unroll
+        for (int j = 0; j < T::FQ; ++j) {
+            const int q = min(q0 + j * 16 + n16, rows - 1);
+            qat[j] = (size_t)(a.rows ? a.rows[q] : q) * D;
+        }
+        auto load = [&](const float* from, size_t at, int k, size_t all) {
+            if (k >= D) return i32x4{0, 0, 0, 0};
+            return wide ? load16<Store::F32, true>(from, at + k, 4, 4) : load16<Store::F32, false>(from, at + k, D - k, all - at - k);
+        };
+        i32x4 next[CH][T::FP];
+        auto fetch = [&](int k) {
+#pragma unroll
+            for (int c = 0; c < CH; ++c)
+#pragma unroll
+                for (int i = 0; i < T::FP; ++i) next[c][i] = load(W, pat[i], k + 16 * c + 4 * g, (size_t)a.P.size * D);
+        };
+#pragma unroll
+        for (int i = 0; i < T::FP; ++i)
+#pragma unroll
+            for (int j = 0; j < T::FQ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        fetch(0);
+        for (int k = 0; k < D; k += 16 * CH) {
+            i32x4 w[CH][T::FP], x[CH][T::FQ];
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+#pragma unroll
+                for (int i = 0; i < T::FP; ++i) w[c][i] = next[c][i];
+#pragma unroll
+                for (int j = 0; j < T::FQ; ++j) x[c][j] = load(X, qat[j], k + 16 * c + 4 * g, (size_t)a.T * D);
+            }
+            fetch(k + 16 * CH);
+#pragma unroll
+            for (int c = 0; c < CH; ++c)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+#pragma unroll
+                    for (int i = 0; i < T::FP; ++i)
+#pragma unroll
+                        for (int j = 0; j < T::FQ; ++j) acc[i][j] = mfma_f32(w[c][i], x[c][j], r, acc[i][j]);
+        }
+    }
+};
+
+// dX of those: G [rows, n] in fp32 times W, a wave 64 columns and a slice of the ids.  Lane (i, g) reads four neighbouring columns 4 i of ids
+// 4 g + r, so that each of them is a fragment of its own and a row's 64 columns leave as 256 bytes.
+template <int FT>
+__global__ __launch_bounds__(256)
+void vocab_rows_dx_kernel(VocabArgs a)
+{
+    constexpr int CH = 2;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n16 = lane & 15, g = lane >> 4;
+    const int rows = a.info->rows, D = a.k, n = a.P.size, blocks = (D + 63) / 64;
+    const int unit = (int)blockIdx.x * 4 + wave, slice = unit / blocks, d = unit % blocks * 64 + 4 * n16, left = D - d;
+    if (rows == 0 || slice >= a.slices) return;
+    const int per = ((n + a.slices - 1) / a.slices + 15) / 16 * 16;
+    const int v0 = (int)min((long long)n, (long long)slice * per), v1 = min(n, v0 + per);
+    const float *W = (const float*)a.P.data, *G = (const float*)a.G;
+    const bool wide = ((uintptr_t)W & 15) == 0 && D % 4 == 0;
+    size_t gat[FT];
+#pragma unroll
+    for (int j = 0; j < FT; ++j) gat[j] = (size_t)min(j * 16 + n16, rows - 1) * a.G_ld;
+    f32x4 acc[FT][4];
+#pragma unroll
+    for (int j = 0; j < FT; ++j)
+#pragma unroll
+        for (int f = 0; f < 4; ++f) acc[j][f] = f32x4{0.f, 0.f, 0.f, 0.f};
+    i32x4 next_w[CH][4], next_g[CH][FT];
+    auto fetch = [&](int v) {
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int at = v + 16 * c + 4 * g;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const size_t from = (size_t)(at + r) * D + d;
+                next_w[c][r] = i32x4{0, 0, 0, 0};
+                if (at + r < v1 && left > 0) next_w[c][r] = wide ? load16<Store::F32, true>(W, from, 4, 4) : load16<Store::F32, false>(W, from, left, (size_t)n * D - from);
+            }
+#pragma unroll
+            for (int j = 0; j < FT; ++j) {         // (columns from n on are zeros in G, up to a tile's end)
+                next_g[c][j] = i32x4{0, 0, 0, 0};
+                if (at < v1) next_g[c][j] = *(const i32x4*)(G + gat[j] + at);
+            }
+        }
+    };
+    fetch(v0);
+    for (int v = v0; v < v1; v += 16 * CH) {
+        i32x4 w[CH][4], x[CH][FT];
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) w[c][r] = next_w[c][r];
+#pragma unroll
+            for (int j = 0; j < FT; ++j) x[c][j] = next_g[c][j];
+        }
+        fetch(v + 16 * CH);
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int j = 0; j < FT; ++j)
+#pragma unroll
+                    for (int f = 0; f < 4; ++f) acc[j][f] = mfma_f32(x[c][j], r, w[c][r], f, acc[j][f]);
+    }
+    if (left <= 0) return;
+#pragma unroll
+    for (int j = 0; j < FT; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int t = 16 * j + 4 * g + r;
+            if (t >= rows) continue;
+            f32x4* to = (f32x4*)((float*)a.out + ((size_t)slice * rows + t) * a.out_ld + d);
+            f32x4 o = {acc[j][0][r], acc[j][1][r], acc[j][2][r], acc[j][3][r]};
+            if (a.accumulate) o += *to;
+            *to = o;
+        }
+}
+
+// dW of those: a wave 64 ids x 64 columns, sums over the rows that count; bound by writing dW.  X is read in place (rows[q]).
+__global__ __launch_bounds__(256)
+void vocab_rows_dw_kernel(VocabArgs a)
+{
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n16 = lane & 15, g = lane >> 4;
+    const int rows = a.info->rows, D = a.k, n = a.out_rows, blocks = (D + 63) / 64;
+    const float down = a.info->down;
+    const long long unit = (long long)blockIdx.x * 4 + wave;
+    const int v0 = (int)(unit / blocks) * 64, d = (int)(unit % blocks) * 64 + 4 * n16, left = D - d;
+    if (v0 >= n) return;
+    const float *X = (const float*)a.Q.data, *G = (const float*)a.G;
+    const bool wide = (((uintptr_t)X | (uintptr_t)a.out) & 15) == 0 && D % 4 == 0;
+    f32x4 acc[4][4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int f = 0; f < 4; ++f) acc[e][f] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int t0 = 0; t0 < rows; t0 += 16) {
+        i32x4 y[4], x[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int t = t0 + 4 * g + r;
+            y[r] = x[r] = i32x4{0, 0, 0, 0};
+            if (t < rows) {
+                y[r] = *(const i32x4*)(G + (size_t)t * a.G_ld + v0 + 4 * n16);
+                const size_t at = (size_t)a.rows[t] * D + d;
+                if (left > 0) x[r] = wide ? load16<Store::F32, true>(X, at, 4, 4) : load16<Store::F32, false>(X, at, left, (size_t)a.T * D - at);
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int f = 0; f < 4; ++f) acc[e][f] = mfma_f32(y[r], e, x[r], f, acc[e][f]);
+    }
+    if (left <= 0) return;
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int v = v0 + 16 * g + 4 * r + e;
+            if (v >= n) continue;
+            const f32x4 o = f32x4{acc[e][0][r], acc[e][1][r], acc[e][2][r], acc[e][3][r]} * down;
+            const size_t at = (size_t)v * D + d;
+            if (wide) store16<Store::F32, true>(a.out, at, __builtin_bit_cast(i32x4, o), 4);
+            else store16<Store::F32, false>(a.out, at, __builtin_bit_cast(i32x4, o), left);
+        }
 }
 
 // A value as two fp16 parts.  Infinite or NaN: in the first.
@@ -321,6 +515,10 @@ __device__ __forceinline__ i32x4 join_fragments(i32x2 a, i32x2 b)
     return i32x4{a0, a1, b0, b1};
 }
 
+// whether logits and G are formed from fp32 as it is (RowsProduct)
+template <class T, Store S, Stage ST>
+constexpr bool reads_fp32() { return S == Store::F32 && T::BQ <= 64 && (ST == Stage::Logits || ST == Stage::G); }
+
 template <class T, Store S, Stage ST>
 __device__ __forceinline__ void vocab_tile(const VocabArgs& a, int block, SPH_LDS unsigned char* smem)
 {
@@ -349,8 +547,10 @@ __device__ __forceinline__ void vocab_tile(const VocabArgs& a, int block, SPH_LD
     const int per_slice = __builtin_amdgcn_readfirstlane(((k + kStepK - 1) / kStepK + slices - 1) / slices) * kStepK;
     const int k0 = min(k, __builtin_amdgcn_readfirstlane(tile.slice) * per_slice), k1 = min(k, k0 + per_slice);
 
-    Product<T, S != Store::Bf16, PX, QX, S == Store::F32 ? 3 : 1> prod;
-    prod.run(a.P, Q, p0, q0, k0, k1, smem);
+    constexpr bool ROWS = reads_fp32<T, S, ST>();
+    std::conditional_t<ROWS, RowsProduct<T>, Product<T, S != Store::Bf16, PX, QX, S == Store::F32 ? 3 : 1>> prod;
+    if constexpr (ROWS) prod.run(a, rows, p0, q0);
+    else prod.run(a.P, Q, p0, q0, k0, k1, smem);
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n16 = lane & 15, g = lane >> 4, wp = wave % T::WAVES_P, wq = wave / T::WAVES_P;
@@ -359,7 +559,7 @@ __device__ __forceinline__ void vocab_tile(const VocabArgs& a, int block, SPH_LD
     // tile together, so nothing hides these instructions: one maximum, one multiply-add, one exponential (16 cycles) and one addition
     // (or half a conversion) per logit, and everything that only the vocabulary's last tile or a row's target needs is kept out of that.
     float scale2 = a.scale2;
-    if constexpr (S == Store::F32 && (ST == Stage::Logits || ST == Stage::G)) scale2 *= a.range->x * a.range->w;
+    if constexpr (S == Store::F32 && !ROWS && (ST == Stage::Logits || ST == Stage::G)) scale2 *= a.range->x * a.range->w;
     if (ST != Stage::Dx && ST != Stage::Dw && scale2 < 0.f) {
         scale2 = -scale2;
 #pragma unroll
@@ -453,6 +653,12 @@ __device__ __forceinline__ void vocab_tile(const VocabArgs& a, int block, SPH_LD
                 float d[2][4];
                 value(i, d[0]);
                 value(i + 1, d[1]);
+                if constexpr (ROWS) {              // fp32 as it is
+#pragma unroll
+                    for (int f = 0; f < 2; ++f)
+                        if (q < rows) *(f32x4*)((float*)a.G + (size_t)qc * a.G_ld + pw + 16 * (i + f) + 4 * g) = f32x4{d[f][0], d[f][1], d[f][2], d[f][3]};
+                    continue;
+                }
                 unsigned short* to = row + 16 * (i + (g & 1)) + 8 * (g >> 1);
                 if constexpr (S == Store::F32) {
                     i32x2 part[2][2];              // [part][fragment]
@@ -740,7 +946,7 @@ void vocab_pack_kernel(PackArgs a)
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const bool on_x = (int)blockIdx.x < a.x_groups;
     float factor = 1.f;
-    if constexpr (S == Store::F32) {
+    if (S == Store::F32 && a.most) {
         __shared__ float tops[kPackRows];
         float top = 0.f;
         for (int i = tid; i < (on_x ? kRangeGroupsX : kRangeGroupsW); i += kPackThreads) top = fmaxf(top, a.most[(on_x ? 0 : kRangeGroupsX) + i]);
@@ -903,7 +1109,7 @@ void vocab_dx_kernel(const float* __restrict__ part, int slices, int ld, int til
     if (t >= T) return;
     const int m = place[t];
     float down = info->down;
-    if constexpr (S == Store::F32) down *= range->w;
+    if (S == Store::F32 && range) down *= range->w;
     const int rows = info->rows;
     const size_t slice = (size_t)rows * ld;
     slices = dx_slices(rows, T, slices, tile_q, tiles_p, target);

@@ -102,3 +102,13 @@ def test_zeros(pkg):
 def test_two_pieces_of_the_vocabulary(pkg):
     X, W, targets, _ = _inputs(4096, 20000, 40, 5)
     _check(pkg, X, W, targets, 1.0)
+
+
+@pytest.mark.parametrize("T,V,D,offset", [(1, 1, 1, 0), (2, 63, 3, 0), (16, 130, 20, 0), (17, 5000, 100, 0), (40, 777, 64, 1), (64, 1000, 257, 0), (64, 129, 66, 2), (33, 300_001, 5, 0)])
+def test_few_rows(pkg, T, V, D, offset):
+    """Up to 64 rows are multiplied as fp32; 300001 ids are two pieces."""
+    X, W, targets, _ = _inputs(T, V, D, 6)
+    moved = lambda t: torch.empty(t.numel() + offset, device=DEV)[offset:].copy_(t.reshape(-1)).view(t.shape)
+    _check(pkg, moved(X), moved(W), targets, 0.5)
+    targets[1:] = -1
+    _check(pkg, moved(X), moved(W), targets, -1.0)
