@@ -167,6 +167,7 @@ int run_embed_bwd(const EmbedPlan& p, const void* tokens, int id_bytes, const fl
 using Big = Tile<256, 256, 2, 4, 4>;               // eight waves of 128 x 64: one workgroup per CU
 using Mid = Tile<128, 128, 2, 2, 4>;               // four of 64 x 64: two per CU
 using Low = Tile<128, 64, 4, 1, 4>;                // up to 64 rows
+using Few = Tile<128, 32, 4, 1, 4>;                // fp32: up to 32 rows (17 x 50000 x 1024 logits 111 -> 68 us: its matrix instruction is the slow one)
 using One = Tile<128, 16, 4, 1, 6>;                // up to 16 rows
 
 constexpr size_t kPieceBytes = 256u << 20;         // of G: what the last-level cache holds
@@ -218,10 +219,11 @@ void dx_choice(long long T, long long ld, int n, bool& big, int& slices)
 // fp32 and few rows: kernels that read fp32 as it is
 bool rows_form(int T, int dtype) { return dtype == SPHATTN_F32 && T > 0 && T <= Low::BQ; }
 
-// Slices of dX's sum there: eight waves per CU of 64 columns each, of 128 ids at least
-int rows_slices(int V, int D)
+// Slices of dX's sum there, of 128 ids at least: four waves per CU of 64 columns each, eight where a wave multiplies more than it reads (64 rows,
+// 60000 x 1472: 149 us with eight, 200 with four; 17 rows, 50000 x 1024: 57 with four and 5 less for their sum)
+int rows_slices(int T, int V, int D)
 {
-    const int blocks = (D + 63) / 64, most = V / 128 < 128 ? V / 128 : 128, want = (8 * kCus + blocks - 1) / blocks;
+    const int blocks = (D + 63) / 64, most = V / 128 < 128 ? V / 128 : 128, want = ((T > 32 ? 8 : 4) * kCus + blocks - 1) / blocks;
     return most < 1 ? 1 : want < most ? want : most;
 }
 
@@ -256,7 +258,7 @@ Vocab vocab_bwd_plan(int T, int V, int D, int dtype, void* workspace)
     p.n_pieces = (int)((V + most - 1) / most);
     p.piece = (int)up_to((V + p.n_pieces - 1) / p.n_pieces, 256);
     p.n_pieces = (V + p.piece - 1) / p.piece;
-    if (rows_form(T, dtype)) p.slices = rows_slices(V, D);
+    if (rows_form(T, dtype)) p.slices = rows_slices(T, V, D);
     else dx_choice(T > 0 ? T : 1, p.ld, p.piece < V ? p.piece : V, p.dx_big, p.slices);
     Carve c(workspace);
     p.info = c.take<VocabInfo>(1);
@@ -317,6 +319,7 @@ int launch_scores(VocabArgs& a, int V, int T, int& tiles_p, hipStream_t stream)
 {
     int rc;
     if (T <= 16) rc = launch_tiles<One, S, ST>(a, V, T, stream);
+    else if (S == Store::F32 && T <= 32) rc = launch_tiles<std::conditional_t<S == Store::F32, Few, Low>, S, ST>(a, V, T, stream);
     else if (T <= 64) rc = launch_tiles<Low, S, ST>(a, V, T, stream);
     else if (big_tiles(V, T)) rc = launch_tiles<Big, S, ST>(a, V, T, stream);
     else rc = launch_tiles<Mid, S, ST>(a, V, T, stream);
@@ -418,6 +421,7 @@ int run_rows_bwd(const Vocab& p, const void* X, const void* W, PackArgs k, void*
             a.slices = p.slices, a.out = p.dx, a.out_ld = p.ld, a.accumulate = i > 0;
             const dim3 grid((unsigned)((long long)blocks * p.slices + 3) / 4);
             if (p.T <= 16) hipLaunchKernelGGL((vocab_rows_dx_kernel<1>), grid, dim3(256), 0, stream, a);
+            else if (p.T <= 32) hipLaunchKernelGGL((vocab_rows_dx_kernel<2>), grid, dim3(256), 0, stream, a);
             else hipLaunchKernelGGL((vocab_rows_dx_kernel<4>), grid, dim3(256), 0, stream, a);
         }
         if (dW) {

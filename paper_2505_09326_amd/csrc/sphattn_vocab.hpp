@@ -19,9 +19,10 @@
 // fp32 storage: X, W and G are written as two fp16 parts each, the value rounded and what that left out rounded (11 + 11 bits, of
 // the value times a power of two that brings the tensor's largest element to 2^14 .. 2^15; G is at most 2^14 by itself), and a product is three
 // products of parts, the small ones first, on the same kernel.  A factor is off by 2^-23 on average and 2^-22 at most, below 2^-17 of its
-// tensor's largest element by 2^-40 of that; the product left out comes to 2^-22 of a term at most.  (Three bf16 parts and six
+// tensor's largest element by 2^-39 of that; the product left out comes to 2^-22 of a term at most.  (Three bf16 parts and six
 // products are exact to 2^-25 on average; they took 444 us for 1999 x 8000 x 512 where these take 273 to 283, with 3.1e-7 against 64 bits, most of it
-// from the fp32 sums, where these have 3.2e-7 and fp32 products 1.6e-6.)
+// from the fp32 sums, where these have 3.2e-7 and fp32 products 1.6e-6.)  Up to 64 rows, where reading W is most of the time, use fp32 matrix
+// instructions on fp32 as it is: RowsProduct.
 #pragma once
 #include "sphattn_embed.hpp"
 #include "sphattn_pipelined.hpp"
@@ -303,6 +304,8 @@ __device__ __forceinline__ f32x4 mfma_f32(i32x4 a, i32x4 b, int e, f32x4 c) { re
 // fp32 with at most 64 rows: W decides the time, so it is read as it is, once, straight into registers, and multiplied by the fp32 matrix
 // instruction (16x16x4, a twelfth of the 16-bit rate: 64 rows of width 1024 take it as long as their W takes memory).  Lane (i, g) holds four neighbouring
 // k, 4 g .. 4 g + 3 of sixteen, of row i of both operands, and instruction r takes the r-th: any order of k will do if both have it.
+// (17 rows, 50000 x 1024: logits 68 us, W at 3.0 TB/s, dX 57, dW 62, a training step 277; with parts in memory 489.  64 rows, 60000 x 1472: 165, 149, 179,
+// and 655 against 840.  3 rows, 20000 x 512: 17.6, 11, 12.)
 template <class T>
 struct RowsProduct {
     f32x4 acc[T::FP][T::FQ];
