@@ -170,7 +170,10 @@ using Low = Tile<128, 64, 4, 1, 4>;                // up to 64 rows
 using Few = Tile<128, 32, 4, 1, 4>;                // fp32: up to 32 rows (17 x 50000 x 1024 logits 111 -> 68 us: its matrix instruction is the slow one)
 using One = Tile<128, 16, 4, 1, 6>;                // up to 16 rows
 
-constexpr size_t kPieceBytes = 256u << 20;         // of G: what the last-level cache holds
+// Of G (or, where that is more, of X): what the last-level cache holds, and half as much again where one piece is enough then.  (One piece instead of
+// two: 8000 rows, 20011 ids, 320 MB 1387 -> 1354 us, with 1200 rows that count 313 -> 287; 8192 x 23000, 377 MB 878 -> 820; but 8192 x 32768, 537 MB
+// 1978 -> 2018, and 65536 ids in three pieces instead of four 7170 -> 7330.)
+constexpr size_t kPieceBytes = 256u << 20, kOnePieceBytes = 400u << 20;
 
 bool vocab_shape(int T, int V, int D) { return T >= 0 && T <= 1 << 20 && V >= 1 && V <= 1 << 24 && D >= 1 && D <= 65536; }
 
@@ -251,7 +254,7 @@ Vocab vocab_bwd_plan(int T, int V, int D, int dtype, void* workspace)
     Vocab p{};
     p.T = T, p.V = V, p.D = D, p.parts = dtype == SPHATTN_F32 ? 2 : 1, p.ld = (int)up_to(D, 8);
     const long long row_bytes = 2ll * p.parts * (T > 0 ? T : 1);
-    size_t limit = kPieceBytes;
+    size_t limit = (size_t)row_bytes * V <= kOnePieceBytes ? kOnePieceBytes : kPieceBytes;
     if ((size_t)row_bytes * p.ld > limit) limit = (size_t)row_bytes * p.ld;
     long long most = (long long)(limit / row_bytes) / 256 * 256;
     most = most < 256 ? 256 : most > 1 << 18 ? 1 << 18 : most;
