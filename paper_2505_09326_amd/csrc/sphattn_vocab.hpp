@@ -12,9 +12,9 @@
 // writing it as fp32 and reading it back.  G is rounded to the storage type (once; half a unit in the last place, 2^-9 of a
 // term in bf16, 2^-12 in fp16), sums are in fp32 throughout.
 //
-// Bound by the matrix pipes where the sums are long: 8192 rows, 65536 ids, width 2048 in bf16 7.0 ms, 8 T V D at 1250 TFLOP/s, what a
+// Bound by the matrix pipes where the sums are long: 8192 rows, 65536 ids, width 2048 in bf16 7.0 to 7.2 ms, 8 T V D at 1226 to 1257 TFLOP/s, what a
 // library product of 8192^3 reaches (1266).  At width 1024 a tile's end, its exponentials and stores, has no other tile's products beside it: logits and
-// G run at 0.57 busy pipes against 0.75 of dW (8192 x 32768 1.96 ms).  One row: W at 5.3 TB/s.
+// G run at 0.57 busy pipes against 0.75 of dW (8192 x 32768 1.96 to 1.98 ms).  One row: W at 5.3 TB/s.
 //
 // fp32 storage: X, W and G are written as two fp16 parts each, the value rounded and what that left out rounded (11 + 11 bits, of
 // the value times a power of two that brings the tensor's largest element to 2^14 .. 2^15; G is at most 2^14 by itself), and a product is three
@@ -284,7 +284,7 @@ enum class Stage { Logits, G, Dx, Dw };
 
 // Slices of dX's sum over the vocabulary for `rows` rows that count, where a launch for T of them has `slices`: as many more as
 // workgroups and arrays of partial sums are then free, while the chip is not full.  (8000 rows of which 1200 count, 20011 ids, width 1024:
-// dX 85 -> 41 us per half of the ids, and 9 more to add the slices up.)
+// dX 169 -> 56 us, and 9 more to add the slices up.)
 __device__ __forceinline__ int dx_slices(int rows, int T, int slices, int tile_q, int tiles_p, int target)
 {
     const int tq = (rows + tile_q - 1) / tile_q, tq_all = (T + tile_q - 1) / tile_q;
