@@ -1131,9 +1131,8 @@ void vocab_dx_kernel(const float* __restrict__ part, int slices, int ld, int til
                 for (int a = 0; a < AHEAD; ++a)
                     if (s0 + a < slices) x += y[a];
             }
+            x *= down;                             // (not of rows that do not count: it may be infinite or NaN, and their gradient is 0)
         }
-#pragma unroll
-        for (int r = 0; r < 4; ++r) x[r] *= down;
         const size_t at = (size_t)t * D + c;
         if (wide) {
             if constexpr (S == Store::F32) *(f32x4*)((float*)dX + at) = x;
