@@ -77,7 +77,8 @@ int sphattn_vocab_loss_fwd(const void* X, const void* W, const void* targets, in
  *           rows that count).
  *   dX : [T,D], dW : [V,D], the dtype of X and W; either may be NULL (not wanted), not both.
  * G is formed a piece of the vocabulary at a time and rounded to the storage type (fp16: scaled by a power of two, so that
- * small gradients keep their bits; fp32: two fp16 parts, as above); sums in fp32, the results rounded once.
+ * small gradients keep their bits); sums in fp32, the results rounded once.  SPHATTN_F32: every factor keeps its 24 bits whatever
+ * the others' sizes are, terms are off by 2^-24 at most.
  */
 size_t sphattn_vocab_loss_bwd_workspace_bytes(int T, int V, int D, int dtype);
 int sphattn_vocab_loss_bwd(const void* X, const void* W, const void* targets, int id_bytes,

@@ -188,8 +188,8 @@ bool big_tiles(long long p, long long q)
 }
 
 struct Vocab {
-    int T, V, D, parts, ld;                        // ld: elements per packed row
-    int piece, n_pieces;                           // backward: vocabulary ids of a piece of G
+    int T, V, D, parts, ld;                        // parts: of X and W for the logits; ld: elements per packed row
+    int piece, n_pieces, g_parts;                  // backward: vocabulary ids of a piece of G, its 16-bit parts
     bool dx_big; int slices;                       // dX: its tile, slices of its sum over a piece
     // workspace
     VocabInfo* info;
@@ -199,6 +199,7 @@ struct Vocab {
     float *g_lse2, *g, *target_logit, *dx;
     float2* partial;
     unsigned short *x, *w, *G;
+    unsigned short *x_sum, *w_sum;                 // fp32 with parts: what G is multiplied with
     size_t bytes;
 };
 
@@ -253,7 +254,9 @@ Vocab vocab_bwd_plan(int T, int V, int D, int dtype, void* workspace)
 {
     Vocab p{};
     p.T = T, p.V = V, p.D = D, p.parts = dtype == SPHATTN_F32 ? 2 : 1, p.ld = (int)up_to(D, 8);
-    const long long row_bytes = 2ll * p.parts * (T > 0 ? T : 1);
+    const bool few = rows_form(T, dtype);
+    p.g_parts = dtype != SPHATTN_F32 ? 1 : few ? 2 : 3;            // (few rows: fp32 as it is)
+    const long long row_bytes = 2ll * p.g_parts * (T > 0 ? T : 1);
     size_t limit = (size_t)row_bytes * V <= kOnePieceBytes ? kOnePieceBytes : kPieceBytes;
     if ((size_t)row_bytes * p.ld > limit) limit = (size_t)row_bytes * p.ld;
     long long most = (long long)(limit / row_bytes) / 256 * 256;
@@ -261,7 +264,7 @@ Vocab vocab_bwd_plan(int T, int V, int D, int dtype, void* workspace)
     p.n_pieces = (int)((V + most - 1) / most);
     p.piece = (int)up_to((V + p.n_pieces - 1) / p.n_pieces, 256);
     p.n_pieces = (V + p.piece - 1) / p.piece;
-    if (rows_form(T, dtype)) p.slices = rows_slices(T, V, D);
+    if (few) p.slices = rows_slices(T, V, D);
     else dx_choice(T > 0 ? T : 1, p.ld, p.piece < V ? p.piece : V, p.dx_big, p.slices);
     Carve c(workspace);
     p.info = c.take<VocabInfo>(1);
@@ -273,9 +276,13 @@ Vocab vocab_bwd_plan(int T, int V, int D, int dtype, void* workspace)
     p.g_lse2 = c.take<float>(T);
     p.g = c.take<float>(T);
     p.x = c.take<unsigned short>((size_t)p.parts * T * p.ld);
-    p.G = c.take<unsigned short>((size_t)p.parts * T * p.piece);
+    p.G = c.take<unsigned short>((size_t)p.g_parts * T * p.piece);
     p.dx = c.take<float>((size_t)p.slices * T * p.ld);
     p.w = c.take<unsigned short>((size_t)p.parts * V * p.ld);
+    if (p.g_parts == 3 && T > 0) {
+        p.x_sum = c.take<unsigned short>((size_t)3 * T * p.ld);
+        p.w_sum = c.take<unsigned short>((size_t)3 * V * p.ld);
+    }
     p.bytes = c.used();
     return p;
 }
@@ -348,12 +355,12 @@ void pack(const Vocab& p, const void* X, const void* W, bool pack_x, bool all_ro
     w = Operand{(const unsigned char*)W, 0, p.D * 2, p.V};
     unsigned groups = 0;
     if (pack_x) {
-        k.x = PackRows{X, p.x, p.T, p.D, p.ld, (long long)p.T * p.ld};
+        k.x = PackRows{X, p.x, p.T, p.D, p.ld, (long long)p.T * p.ld, p.x_sum};
         k.x_groups = (int)(groups = (unsigned)(p.T + kPackRows - 1) / kPackRows);
         x = Operand{(const unsigned char*)p.x, k.x.part * 2, p.ld * 2, p.T};
     }
     if (!ready(W, p.D, S)) {
-        k.w = PackRows{W, p.w, p.V, p.D, p.ld, (long long)p.V * p.ld};
+        k.w = PackRows{W, p.w, p.V, p.D, p.ld, (long long)p.V * p.ld, p.w_sum};
         groups += (unsigned)(p.V + kPackRows - 1) / kPackRows;
         w = Operand{(const unsigned char*)p.w, k.w.part * 2, p.ld * 2, p.V};
     }
@@ -407,7 +414,7 @@ int run_rows_bwd(const Vocab& p, const void* X, const void* W, PackArgs k, void*
 {
     constexpr Store S = Store::F32;
     // which rows count and what G needs of them (X's parts, a few rows, are not looked at)
-    k.x = PackRows{X, p.x, p.T, p.D, p.ld, (long long)p.T * p.ld};
+    k.x = PackRows{X, p.x, p.T, p.D, p.ld, (long long)p.T * p.ld, nullptr};
     k.x_groups = (p.T + kPackRows - 1) / kPackRows, k.own_rows = 1;
     hipLaunchKernelGGL((vocab_pack_kernel<S>), dim3((unsigned)k.x_groups), dim3(kPackThreads), 0, stream, k);
     const int blocks = (p.D + 63) / 64;
@@ -434,7 +441,7 @@ int run_rows_bwd(const Vocab& p, const void* X, const void* W, PackArgs k, void*
     }
     if (dX)
         hipLaunchKernelGGL((vocab_dx_kernel<S>), dim3((unsigned)(p.T + 3) / 4, (unsigned)(p.D + kDxCols - 1) / kDxCols), dim3(256), 0, stream, p.dx, p.slices,
-                           p.ld, 128, 1, 0, p.place, p.info, (const VocabRange*)nullptr, dX, p.T, p.D);
+                           p.ld, 128, 1, 0, p.place, p.info, dX, p.T, p.D);
     return launched();
 }
 
@@ -444,7 +451,7 @@ int run_vocab_bwd(const Vocab& p, const void* X, const void* W, const void* targ
 {
     PackArgs k{};
     k.r = row_args(p, targets, id_bytes);
-    k.r.dloss = dloss, k.r.reduce = (Reduce)reduction, k.r.scale = scale, k.r.half = S != Store::Bf16;
+    k.r.dloss = dloss, k.r.reduce = (Reduce)reduction, k.r.scale = scale, k.r.half = S == Store::F16;
     k.compact = 1, k.lse = lse, k.g_target = p.g_target, k.g_lse2 = p.g_lse2, k.g = p.g;
     Operand x{}, w{};
     if (p.T == 0) {                                // (the info of no rows, which one workgroup writes)
@@ -460,6 +467,10 @@ int run_vocab_bwd(const Vocab& p, const void* X, const void* W, const void* targ
     for (int i = 0; i < p.n_pieces && rc == SPHATTN_OK; ++i) {
         const int v0 = i * p.piece, n = p.V - v0 < p.piece ? p.V - v0 : p.piece;
         const Operand wi{p.T ? w.data + (size_t)v0 * w.ld : nullptr, w.part, w.ld, n};
+        // what G is multiplied with: fp32 in parts of its own
+        const bool sum_parts = p.x_sum != nullptr;
+        const Operand ws = sum_parts ? Operand{(const unsigned char*)(p.w_sum + (size_t)v0 * p.ld), (long long)p.V * p.ld * 2, p.ld * 2, p.ld} : Operand{wi.data, wi.part, wi.ld, p.ld};
+        const Operand xs = sum_parts ? Operand{(const unsigned char*)p.x_sum, (long long)p.T * p.ld * 2, p.ld * 2, p.ld} : Operand{x.data, x.part, x.ld, p.ld};
         const Operand G{(const unsigned char*)p.G, (long long)p.T * p.piece * 2, p.piece * 2, 0};
         VocabArgs a{};
         a.range = p.range;
@@ -470,13 +481,12 @@ int run_vocab_bwd(const Vocab& p, const void* X, const void* W, const void* targ
         if (p.T > 0) rc = launch_scores<S, Stage::G>(a, n, p.T, tiles, stream);
         if (rc != SPHATTN_OK) break;
         VocabArgs bx{}, bw{};
-        bx.range = bw.range = p.T ? p.range : nullptr;
         const bool with_dx = dX && p.T > 0, with_dw = dW != nullptr;
-        bx.P = Operand{wi.data, wi.part, wi.ld, p.ld};
+        bx.P = ws;
         bx.Q = G, bx.Q.size = p.T, bx.info = p.info, bx.k = n, bx.slices = p.slices;
         bx.T = p.T, bx.target = dx_at_once;
         bx.out = p.dx, bx.out_ld = p.ld, bx.out_cols = p.ld, bx.accumulate = i > 0;
-        bw.P = Operand{x.data, x.part, x.ld, p.ld};
+        bw.P = xs;
         bw.Q = G, bw.Q.size = (int)up_to(n, 8), bw.info = p.info, bw.slices = 1;
         bw.out = dW ? (unsigned char*)dW + (size_t)v0 * p.D * store_bytes<S>() : nullptr, bw.out_ld = p.D, bw.out_cols = p.D, bw.out_rows = n;
         const bool dw_big = big_tiles(p.ld, n);
@@ -490,7 +500,7 @@ int run_vocab_bwd(const Vocab& p, const void* X, const void* W, const void* targ
     }
     if (rc == SPHATTN_OK && dX && p.T > 0)
         hipLaunchKernelGGL((vocab_dx_kernel<S>), dim3((unsigned)(p.T + 3) / 4, (unsigned)(p.D + kDxCols - 1) / kDxCols), dim3(256), 0, stream, p.dx, p.slices, p.ld,
-                           dx_tile, (p.ld + dx_tile - 1) / dx_tile, dx_at_once, p.place, p.info, p.range, dX, p.T, p.D);
+                           dx_tile, (p.ld + dx_tile - 1) / dx_tile, dx_at_once, p.place, p.info, dX, p.T, p.D);
     return rc == SPHATTN_OK ? launched() : rc;
 }
 

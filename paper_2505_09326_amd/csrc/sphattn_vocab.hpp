@@ -16,13 +16,14 @@
 // library product of 8192^3 reaches (1266).  At width 1024 a tile's end, its exponentials and stores, has no other tile's products beside it: logits and
 // G run at 0.57 busy pipes against 0.75 of dW (8192 x 32768 1.96 to 1.98 ms).  One row: W at 5.3 TB/s.
 //
-// fp32 storage: X, W and G are written as two fp16 parts each, the value rounded and what that left out rounded (11 + 11 bits, of
-// the value times a power of two that brings the tensor's largest element to 2^14 .. 2^15; G is at most 2^14 by itself), and a product is three
+// fp32 storage, logits: X and W are written as two fp16 parts each, the value rounded and what that left out rounded (11 + 11 bits, of
+// the value times a power of two that brings the tensor's largest element to 2^14 .. 2^15), and a product is three
 // products of parts, the small ones first, on the same kernel.  A factor is off by 2^-23 on average and 2^-22 at most, below 2^-17 of its
-// tensor's largest element by 2^-39 of that; the product left out comes to 2^-22 of a term at most.  (Three bf16 parts and six
-// products are exact to 2^-25 on average; they took 444 us for 1999 x 8000 x 512 where these take 273 to 283, with 3.1e-7 against 64 bits, most of it
-// from the fp32 sums, where these have 3.2e-7 and fp32 products 1.6e-6.)  Up to 64 rows, where reading W is most of the time, use fp32 matrix
-// instructions on fp32 as it is: RowsProduct.
+// tensor's largest element by 2^-39 of that; the product left out comes to 2^-22 of a term at most.
+// Gradients: G, X and W as three bf16 parts each, which are the value over the whole range of fp32, and six products; what is left out comes to 2^-24 of
+// a term.  (Two fp16 parts and three products took 273 us for 1999 x 8000 x 512 where this takes 415, but hold nothing below 2^-39 of the
+// largest: a row of dX whose gradient is 1e-8 of another's lost 2 % of itself, ids that no row gives a weight above 1e-12 their whole row of dW.)
+// Up to 64 rows, where reading W is most of the time, use fp32 matrix instructions on fp32 as it is: RowsProduct.
 #pragma once
 #include "sphattn_embed.hpp"
 #include "sphattn_pipelined.hpp"
@@ -115,9 +116,12 @@ struct Product {
             return across ? Stream{A.data + part * A.part + (long long)k0 * A.ld, k_end - k0}
                           : Stream{A.data + part * A.part + (long long)a0 * A.ld + (long long)k0 * 2, rows * A.ld - k0 * 2};
         };
-        // parts of P and Q by pair, small products first: (1,0) (0,1) (0,0)
+        // parts of P and Q by pair, small products first: (1,0) (0,1) (0,0), or of three parts (2,0) (0,2) (1,1) (1,0) (0,1) (0,0)
+        static_assert(PAIRS == 1 || PAIRS == 3 || PAIRS == 6, "");
         int pair = 0, step = 0, copied = 0;        // of the next copies
-        Stream sp = start(PX, P, p0, T::BP, PAIRS == 1 ? 0 : 1), sq = start(QX, Q, q0, T::BQ, 0);
+        auto part_p = [&]() { return PAIRS == 3 ? pair == 0 : PAIRS == 6 ? (pair == 0 ? 2 : pair == 2 || pair == 3) : 0; };
+        auto part_q = [&]() { return PAIRS == 3 ? pair == 1 : PAIRS == 6 ? (pair == 1 ? 2 : pair == 2 || pair == 4) : 0; };
+        Stream sp = start(PX, P, p0, T::BP, part_p()), sq = start(QX, Q, q0, T::BQ, part_q());
         uint32_t to = lds0;
         auto words = [&](bool across, const Operand& A, const Stream& s, bool there) {
             const int left = there ? max(s.left, 0) : 0;
@@ -147,8 +151,8 @@ struct Product {
             if (PAIRS > 1 && step == steps && copied < total) {
                 step = 0;
                 ++pair;
-                sp = start(PX, P, p0, T::BP, 0);
-                sq = start(QX, Q, q0, T::BQ, pair == 1);
+                sp = start(PX, P, p0, T::BP, part_p());
+                sq = start(QX, Q, q0, T::BQ, part_q());
             }
         };
         auto copy_step = [&]() {
@@ -508,6 +512,29 @@ __device__ __forceinline__ void split2(const float (&x)[4], i32x2& hi, i32x2& lo
     }
 }
 
+// Four neighbouring values as three bf16 parts that are them (8 + 8 + 8 bits), over the whole range of fp32.  Infinite or NaN: in the first.
+__device__ __forceinline__ void split3(const float (&x)[4], i32x2 (&part)[3])
+{
+    constexpr float MOST = 0x1.fep127f;            // (a finite value is not to be rounded to an infinite one)
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        float left[2];
+        bool finite[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            left[i] = x[2 * r + i];
+            finite[i] = __builtin_fabsf(left[i]) < __builtin_inff();
+        }
+        const int hi = pack2<false>(finite[0] ? fminf(fmaxf(left[0], -MOST), MOST) : left[0], finite[1] ? fminf(fmaxf(left[1], -MOST), MOST) : left[1]);
+        left[0] = finite[0] ? left[0] - __builtin_bit_cast(float, hi << 16) : 0.f;
+        left[1] = finite[1] ? left[1] - __builtin_bit_cast(float, hi & (int)0xffff0000) : 0.f;
+        const int mid = pack2<false>(left[0], left[1]);
+        part[0][r] = hi;
+        part[1][r] = mid;
+        part[2][r] = pack2<false>(left[0] - __builtin_bit_cast(float, mid << 16), left[1] - __builtin_bit_cast(float, mid & (int)0xffff0000));
+    }
+}
+
 // Two accumulator fragments' rows of four 16-bit values, lane group g holding columns 4 g .. 4 g + 3 of each: afterwards group g has
 // columns 8 (g / 2) .. + 7 of fragment g % 2.
 __device__ __forceinline__ i32x4 join_fragments(i32x2 a, i32x2 b)
@@ -531,7 +558,6 @@ __device__ __forceinline__ void vocab_tile(const VocabArgs& a, int block, SPH_LD
     if (a.info) {
         rows = __builtin_amdgcn_readfirstlane(a.info->rows);
         if constexpr (ST == Stage::Dw) down = a.info->down;
-        if constexpr (ST == Stage::Dw && S == Store::F32) down *= a.range ? a.range->x : 1.f;
     }
     Operand Q = a.Q;
     if constexpr (ST == Stage::Dw) {
@@ -551,7 +577,8 @@ __device__ __forceinline__ void vocab_tile(const VocabArgs& a, int block, SPH_LD
     const int k0 = min(k, __builtin_amdgcn_readfirstlane(tile.slice) * per_slice), k1 = min(k, k0 + per_slice);
 
     constexpr bool ROWS = reads_fp32<T, S, ST>();
-    std::conditional_t<ROWS, RowsProduct<T>, Product<T, S != Store::Bf16, PX, QX, S == Store::F32 ? 3 : 1>> prod;
+    constexpr bool SUMS = ST == Stage::Dx || ST == Stage::Dw, F32 = S == Store::F32;
+    std::conditional_t<ROWS, RowsProduct<T>, Product<T, S == Store::F16 || (F32 && !SUMS), PX, QX, !F32 ? 1 : SUMS ? 6 : 3>> prod;
     if constexpr (ROWS) prod.run(a, rows, p0, q0);
     else prod.run(a.P, Q, p0, q0, k0, k1, smem);
 
@@ -664,12 +691,12 @@ __device__ __forceinline__ void vocab_tile(const VocabArgs& a, int block, SPH_LD
                 }
                 unsigned short* to = row + 16 * (i + (g & 1)) + 8 * (g >> 1);
                 if constexpr (S == Store::F32) {
-                    i32x2 part[2][2];              // [part][fragment]
+                    i32x2 part[2][3];              // [fragment][part]
 #pragma unroll
-                    for (int f = 0; f < 2; ++f) split2(d[f], part[0][f], part[1][f]);
+                    for (int f = 0; f < 2; ++f) split3(d[f], part[f]);
 #pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        const i32x4 o = join_fragments(part[k][0], part[k][1]);
+                    for (int k = 0; k < 3; ++k) {
+                        const i32x4 o = join_fragments(part[0][k], part[1][k]);
                         if (q < rows) *(i32x4*)(to + k * a.G_part) = o;
                     }
                 } else {
@@ -907,6 +934,7 @@ constexpr int kPackThreads = 256, kPackRows = kPackThreads / 64, kOwnRows = 1024
 struct PackRows {
     const void* in; void* out; int n, D, ld;       // (ld: elements per row of out, a multiple of 8)
     long long part;                                // elements from part to part
+    void* sum_out;                                 // fp32: the three parts that the products with G take, or NULL
 };
 struct PackArgs {
     PackRows x, w;
@@ -929,9 +957,15 @@ __device__ __forceinline__ void pack_row(const PackRows& a, long long t, long lo
         if constexpr (S == Store::F32) {
             float x[4];
             widen16<S>(w, x);
+            i32x2 hi, lo;
+            if (a.sum_out) {
+                i32x2 part[3];
+                split3(x, part);
+#pragma unroll
+                for (int k = 0; k < 3; ++k) *(i32x2*)((unsigned short*)a.sum_out + to + c + k * a.part) = part[k];
+            }
 #pragma unroll
             for (int r = 0; r < 4; ++r) x[r] *= factor;
-            i32x2 hi, lo;
             split2(x, hi, lo);
             unsigned short* o = (unsigned short*)a.out + to + c;
             *(i32x2*)o = hi;
@@ -1105,14 +1139,13 @@ constexpr int kDxCols = 256;
 template <Store S>
 __global__ __launch_bounds__(256)
 void vocab_dx_kernel(const float* __restrict__ part, int slices, int ld, int tile_q, int tiles_p, int target, const int* __restrict__ place,
-                     const VocabInfo* __restrict__ info, const VocabRange* __restrict__ range, void* __restrict__ dX, int T, int D)
+                     const VocabInfo* __restrict__ info, void* __restrict__ dX, int T, int D)
 {
     const int lane = threadIdx.x & 63;
     const long long t = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (t >= T) return;
     const int m = place[t];
-    float down = info->down;
-    if (S == Store::F32 && range) down *= range->w;
+    const float down = info->down;
     const int rows = info->rows;
     const size_t slice = (size_t)rows * ld;
     slices = dx_slices(rows, T, slices, tile_q, tiles_p, target);

@@ -1,0 +1,107 @@
+"""Cross entropy over a vocabulary, row by row and id by id: what one row or one id holds takes nothing away from the others.
+
+Tolerances (u = 2^-24, e = eps / 2 of the storage type; everything else of fp32 with more than 64 rows: a term of a logit off by 3 2^-22, and elements of X
+and W to 2^-51 of their row's largest):
+  logit    a = (3 2^-22 + (D + 4) u) sum_k |x_k w_k| + 2^-50 (max |x| sum |w| + max |w| sum |x|); in 16-bit storage (D + 4) u sum_k |x_k w_k|
+  lse      the mean of that over its terms, 8 u |lse| and u (V / 64 + 100) for the sum
+  G        of its own size: p (a + lse's + 16 u), 16 u more for a row's target, and the rounding to the storage type, e |G|; fp16: 2^-24 of a value that the
+           row's own gradient brings to 2^13 and more, so 2^-37 of |g|
+  dX, dW   the sum of those, (n + 4) u of the terms' sizes for adding n of them (fp32: 2^-21 more for the products of parts that are left out), e of the result"""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+U = 2.0 ** -24
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+
+
+@pytest.fixture(scope="module")
+def pkg():
+    import paper_2505_09326_amd as p
+    p.load_library()
+    return p
+
+
+def _inputs(T, V, D, dtype, seed, spread=2.0, share=0.8):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    X = torch.randn(T, D, generator=g, device=DEV).to(TYPES[dtype])
+    W = (torch.randn(V, D, generator=g, device=DEV) * spread * D ** -0.5).to(TYPES[dtype])
+    targets = torch.randint(V, (T,), generator=g, device=DEV)
+    targets[torch.rand(T, generator=g, device=DEV) >= share] = -1
+    return X, W, targets, g
+
+
+def _exact(X, W, targets, g):
+    """(lse, losses, dX, dW) in 64 bits for gradients g of the rows, each with what it may be off by."""
+    f32 = X.dtype == torch.float32
+    e, tiny = torch.finfo(X.dtype).eps / 2, torch.finfo(X.dtype).tiny * torch.finfo(X.dtype).eps
+    x, w, (V, D) = X.double(), W.double(), W.shape
+    wt = w.t().contiguous()
+    logits = x @ wt
+    a = (D + 4) * U * (x.abs() @ wt.abs())
+    if f32:
+        a = a * (1 + 3 * 2.0 ** -22 / ((D + 4) * U))
+        a += 2.0 ** -50 * (x.abs().amax(1)[:, None] * wt.abs().sum(0)[None] + wt.abs().amax(0)[None] * x.abs().sum(1)[:, None])
+    lse = torch.logsumexp(logits, 1)
+    p = (logits - lse[:, None]).exp()
+    part = lambda t: torch.where(p > 0, p * t, 0.0)            # (what has no weight may be off by anything)
+    lse_tol = part(a).sum(1) + U * (V / 64 + 100) + 8 * U * lse.abs()
+    counted, at = targets >= 0, targets.clamp_min(0)[:, None]
+    mine, mine_tol = logits.gather(1, at)[:, 0], a.gather(1, at)[:, 0]
+    losses, loss_tol = (torch.where(counted, t, 0.0) for t in (lse - mine, lse_tol + mine_tol + 8 * U * mine.abs()))
+    G, off = p.clone(), part(a + lse_tol[:, None] + 16 * U)
+    G.scatter_add_(1, at, torch.full_like(lse[:, None], -1.0))
+    off.scatter_add_(1, at, torch.full_like(lse[:, None], 16 * U))
+    off += e * G.abs() + (2.0 ** -37 if X.dtype == torch.float16 else 0.0)
+    g = torch.where(counted, g.double(), 0.0)[:, None]
+    G, off = G * g, off * g.abs()
+    more = 2.0 ** -21 if f32 else 0.0
+    dX, dW = G @ w, G.t().contiguous() @ x
+    dX_tol = off @ w.abs() + ((V + 4) * U + more) * (G.abs() @ w.abs()) + e * dX.abs() + tiny
+    dW_tol = off.t().contiguous() @ x.abs() + ((X.shape[0] + 4) * U + more) * (G.abs().t().contiguous() @ x.abs()) + e * dW.abs() + tiny
+    return (lse, lse_tol), (losses, loss_tol), (dX, dX_tol), (dW, dW_tol)
+
+
+def _near(got, want, what):
+    want, tol = want
+    assert int((~got.isfinite()).sum()) == 0, what
+    far = (got.double() - want).abs()
+    far = torch.where(far > tol, far / tol, 0.0)               # (losses of rows that do not count are to be exactly 0)
+    assert float(far.max()) == 0, (what, float(far.max()), divmod(int(far.argmax()), got.shape[-1]))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [40, 200, 1500])
+def test_gradients_of_rows_over_many_powers_of_ten(pkg, T, dtype):
+    """Each row's dX to its own size, whatever the other rows' gradients are; dW to its terms'."""
+    X, W, targets, r = _inputs(T, 777, 72, dtype, 2, spread=8.0)
+    decades = torch.randint(-12, 1, (T,), generator=r, device=DEV) if dtype != "f16" else torch.randint(-5, 5, (T,), generator=r, device=DEV)
+    g = torch.randn(T, generator=r, device=DEV).clamp(-3, 3) * 10.0 ** decades
+    lse, losses, dX, _ = _exact(X, W, targets, g)
+    got_losses, got_lse = pkg.sphattn_vocab_loss_fwd(X, W, targets)
+    _near(got_lse, lse, "lse")
+    _near(got_losses, losses, "losses")
+    gX, gW = pkg.sphattn_vocab_loss_bwd(X, W, targets, got_lse, g)
+    _near(gX, dX, "dX")
+    # dW: sums over all rows, the largest of which may take the small ones' bits (fp16: 2^-37 of the largest gradient)
+    _, _, _, (dW, dW_tol) = _exact(X, W, targets, g)
+    if dtype == "f16":
+        dW_tol = dW_tol + 2.0 ** -37 * float(g[targets >= 0].abs().max()) * X[targets >= 0].double().abs().sum(0)[None]
+    _near(gW, (dW, dW_tol), "dW")
+    assert torch.equal(pkg.sphattn_vocab_loss_bwd(X, W, targets, got_lse, g, want_dW=False)[0], gX)
+    assert torch.equal(pkg.sphattn_vocab_loss_bwd(X, W, targets, got_lse, g, want_dX=False)[1], gW)
+
+
+@pytest.mark.parametrize("T", [40, 65, 300, 1500])
+def test_gradients_of_rare_ids(pkg, T):
+    """fp32: an id that no row gives a weight above 1e-12, or 1e-30, has its row of dW to that row's own size."""
+    X, W, targets, r = _inputs(T, 900, 40, "f32", 3)
+    targets = targets.fmod(200)                    # (most ids are no row's target)
+    X[:, 0], W[:, 0] = 1.0, -torch.rand(900, generator=r, device=DEV) * 75
+    lse, _, dX, dW = _exact(X, W, targets, torch.ones(T, device=DEV))
+    sizes = dW[0].abs().amax(1)
+    assert float(sizes.min()) < 1e-28 < float(sizes.median()) < 1e-3
+    gX, gW = pkg.sphattn_vocab_loss_bwd(X, W, targets, pkg.sphattn_vocab_loss_fwd(X, W, targets)[1], torch.ones((), device=DEV), reduction="sum")
+    _near(gX, dX, "dX")
+    _near(gW, dW, "dW")
