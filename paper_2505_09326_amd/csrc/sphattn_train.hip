@@ -193,8 +193,7 @@ struct Vocab {
     bool dx_big; int slices;                       // dX: its tile, slices of its sum over a piece
     // workspace
     VocabInfo* info;
-    VocabRange* range;                             // fp32
-    float* most;
+    int *x_exp, *w_exp;                            // fp32 in parts
     int *rows, *place, *g_target;
     float *g_lse2, *g, *target_logit, *dx;
     float2* partial;
@@ -237,8 +236,8 @@ Vocab vocab_fwd_plan(int T, int V, int D, int dtype, void* workspace)
     p.T = T, p.V = V, p.D = D, p.parts = dtype == SPHATTN_F32 ? 2 : 1, p.ld = (int)up_to(D, 8);
     Carve c(workspace);
     p.info = c.take<VocabInfo>(1);
-    p.range = c.take<VocabRange>(1);
-    p.most = c.take<float>(p.parts > 1 ? kRangeGroupsX + kRangeGroupsW : 0);
+    p.x_exp = c.take<int>(p.parts > 1 ? T : 0);
+    p.w_exp = c.take<int>(p.parts > 1 ? up_to(V, 256) : 0);
     p.rows = c.take<int>(T);
     p.place = c.take<int>(T);
     p.target_logit = c.take<float>(T);
@@ -268,8 +267,8 @@ Vocab vocab_bwd_plan(int T, int V, int D, int dtype, void* workspace)
     else dx_choice(T > 0 ? T : 1, p.ld, p.piece < V ? p.piece : V, p.dx_big, p.slices);
     Carve c(workspace);
     p.info = c.take<VocabInfo>(1);
-    p.range = c.take<VocabRange>(1);
-    p.most = c.take<float>(p.parts > 1 ? kRangeGroupsX + kRangeGroupsW : 0);
+    p.x_exp = c.take<int>(p.parts > 1 ? T : 0);
+    p.w_exp = c.take<int>(p.parts > 1 ? up_to(V, 256) : 0);
     p.rows = c.take<int>(T);
     p.place = c.take<int>(T);
     p.g_target = c.take<int>(T);
@@ -349,27 +348,22 @@ RowArgs row_args(const Vocab& p, const void* targets, int id_bytes)
 
 // X and W as the products want them; what can be read as it is stays where it is
 template <Store S>
-void pack(const Vocab& p, const void* X, const void* W, bool pack_x, bool all_rows, PackArgs k, Operand& x, Operand& w, hipStream_t stream)
+void pack(const Vocab& p, const void* X, const void* W, bool pack_x, PackArgs k, Operand& x, Operand& w, hipStream_t stream)
 {
     x = Operand{(const unsigned char*)X, 0, p.D * 2, p.T};
     w = Operand{(const unsigned char*)W, 0, p.D * 2, p.V};
     unsigned groups = 0;
     if (pack_x) {
-        k.x = PackRows{X, p.x, p.T, p.D, p.ld, (long long)p.T * p.ld, p.x_sum};
+        k.x = PackRows{X, p.x, p.T, p.D, p.ld, (long long)p.T * p.ld, p.x_sum, p.x_exp};
         k.x_groups = (int)(groups = (unsigned)(p.T + kPackRows - 1) / kPackRows);
         x = Operand{(const unsigned char*)p.x, k.x.part * 2, p.ld * 2, p.T};
     }
     if (!ready(W, p.D, S)) {
-        k.w = PackRows{W, p.w, p.V, p.D, p.ld, (long long)p.V * p.ld, p.w_sum};
+        k.w = PackRows{W, p.w, p.V, p.D, p.ld, (long long)p.V * p.ld, p.w_sum, p.w_exp};
         groups += (unsigned)(p.V + kPackRows - 1) / kPackRows;
         w = Operand{(const unsigned char*)p.w, k.w.part * 2, p.ld * 2, p.V};
     }
     k.own_rows = p.T <= kOwnRows;
-    if (S == Store::F32) {
-        hipLaunchKernelGGL(vocab_range_kernel, dim3(kRangeGroupsX + kRangeGroupsW), dim3(kRangeThreads), 0, stream, (const float*)X, (const float*)W, p.T, p.V, p.D,
-                           k.r.targets, k.r.id_bytes, (int)all_rows, p.most);
-        k.most = p.most, k.range = p.range;
-    }
     if (k.compact && !k.own_rows) hipLaunchKernelGGL(vocab_rows_kernel, dim3(1), dim3(kRowsThreads), 0, stream, k.r);
     if (groups) hipLaunchKernelGGL((vocab_pack_kernel<S>), dim3(groups), dim3(kPackThreads), 0, stream, k);
 }
@@ -386,11 +380,11 @@ int run_vocab_fwd(const Vocab& p, const void* X, const void* W, const void* targ
         a.P = Operand{(const unsigned char*)W, 0, 0, p.V}, a.Q = Operand{(const unsigned char*)X, 0, 0, p.T};
         a.k = p.D, a.T = p.T;
     } else {
-        pack<S>(p, X, W, k.compact || !ready(X, p.D, S), all_rows, k, a.Q, a.P, stream);
+        pack<S>(p, X, W, k.compact || !ready(X, p.D, S), k, a.Q, a.P, stream);
         a.k = p.ld;
+        if (S == Store::F32) a.p_exp = p.w_exp, a.q_exp = p.x_exp;
     }
     if (k.compact) a.info = p.info, a.rows = p.rows;
-    a.range = p.range;
     a.slices = 1, a.V = p.V, a.scale2 = scale * kLog2e;
     a.targets = targets, a.id_bytes = id_bytes;
     a.partial = p.partial, a.partial_ld = p.T, a.target_logit = p.target_logit;
@@ -413,8 +407,8 @@ int run_vocab_fwd(const Vocab& p, const void* X, const void* W, const void* targ
 int run_rows_bwd(const Vocab& p, const void* X, const void* W, PackArgs k, void* dX, void* dW, float scale, hipStream_t stream)
 {
     constexpr Store S = Store::F32;
-    // which rows count and what G needs of them (X's parts, a few rows, are not looked at)
-    k.x = PackRows{X, p.x, p.T, p.D, p.ld, (long long)p.T * p.ld, nullptr};
+    // which rows count and what G needs of them; no parts are made
+    k.x = PackRows{X, nullptr, p.T, p.D, p.ld, 0, nullptr, nullptr};
     k.x_groups = (p.T + kPackRows - 1) / kPackRows, k.own_rows = 1;
     hipLaunchKernelGGL((vocab_pack_kernel<S>), dim3((unsigned)k.x_groups), dim3(kPackThreads), 0, stream, k);
     const int blocks = (p.D + 63) / 64;
@@ -460,7 +454,7 @@ int run_vocab_bwd(const Vocab& p, const void* X, const void* W, const void* targ
     } else if (S == Store::F32 && rows_form(p.T, SPHATTN_F32)) {
         return run_rows_bwd(p, X, W, k, dX, dW, scale, stream);
     } else {
-        pack<S>(p, X, W, true, false, k, x, w, stream);
+        pack<S>(p, X, W, true, k, x, w, stream);
     }
     int rc = SPHATTN_OK;
     const int dx_tile = p.dx_big ? 256 : 128, dx_at_once = p.dx_big ? kCus : 2 * kCus;
@@ -473,7 +467,7 @@ int run_vocab_bwd(const Vocab& p, const void* X, const void* W, const void* targ
         const Operand xs = sum_parts ? Operand{(const unsigned char*)p.x_sum, (long long)p.T * p.ld * 2, p.ld * 2, p.ld} : Operand{x.data, x.part, x.ld, p.ld};
         const Operand G{(const unsigned char*)p.G, (long long)p.T * p.piece * 2, p.piece * 2, 0};
         VocabArgs a{};
-        a.range = p.range;
+        if (S == Store::F32) a.p_exp = p.w_exp + v0, a.q_exp = p.x_exp;
         a.P = wi, a.Q = x, a.info = p.info, a.k = p.ld, a.slices = 1, a.V = p.V, a.v0 = v0, a.scale2 = scale * kLog2e;
         a.g_target = p.g_target, a.g_lse2 = p.g_lse2, a.g = p.g;
         a.G = p.G, a.G_part = (long long)p.T * p.piece, a.G_ld = p.piece;

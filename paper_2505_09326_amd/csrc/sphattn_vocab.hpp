@@ -16,10 +16,11 @@
 // library product of 8192^3 reaches (1266).  At width 1024 a tile's end, its exponentials and stores, has no other tile's products beside it: logits and
 // G run at 0.57 busy pipes against 0.75 of dW (8192 x 32768 1.96 to 1.98 ms).  One row: W at 5.3 TB/s.
 //
-// fp32 storage, logits: X and W are written as two fp16 parts each, the value rounded and what that left out rounded (11 + 11 bits, of
-// the value times a power of two that brings the tensor's largest element to 2^14 .. 2^15), and a product is three
-// products of parts, the small ones first, on the same kernel.  A factor is off by 2^-23 on average and 2^-22 at most, below 2^-17 of its
-// tensor's largest element by 2^-39 of that; the product left out comes to 2^-22 of a term at most.
+// fp32 storage, logits: X and W are written as two fp16 parts each, the value rounded and 2^12 times what that left out rounded (11 + 11 bits, of
+// the value times a power of two that brings its row's largest element to 2^14 .. 2^15), and a product is three
+// products of parts, the small ones first, on the same kernel.  A factor is off by 2^-23 on average and 2^-22 at most, below 2^-29 of its
+// row's largest element by 2^-51 of that; the product left out comes to 2^-22 of a term at most.  The powers of two come back to the logits in a tile's end,
+// so no row takes bits from another (one for all of W lost every id beside a bias of -1e9).
 // Gradients: G, X and W as three bf16 parts each, which are the value over the whole range of fp32, and six products; what is left out comes to 2^-24 of
 // a term.  (Two fp16 parts and three products took 273 us for 1999 x 8000 x 512 where this takes 415, but hold nothing below 2^-39 of the
 // largest: a row of dX whose gradient is 1e-8 of another's lost 2 % of itself, ids that no row gives a weight above 1e-12 their whole row of dW.)
@@ -39,8 +40,7 @@ struct VocabInfo {
     float down;                                    // factor of the sums behind it
 };
 
-// What X and W were multiplied by before they were split, inverted (fp32 storage).
-struct VocabRange { float x, w; };
+constexpr float kLowPart = 4096.f;                 // what the second fp16 part is multiplied by: below 2^-14 that type has fewer bits
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
@@ -209,6 +209,13 @@ struct Product {
 #pragma unroll
         for (int i = 0; i < T::FP - 1; ++i) read_p(from, i);
         for (int s = 0; s < total; s += 2) {
+            // of three products the first two have a second part, 2^12 times as large as it is: an even number of steps, after which the sums are brought back
+            if (PAIRS == 3 && s == 2 * steps) {
+#pragma unroll
+                for (int i = 0; i < T::FP; ++i)
+#pragma unroll
+                    for (int j = 0; j < T::FQ; ++j) acc[i][j] *= 1.f / kLowPart;
+            }
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 arrive();                          // step s + u + 1 is there; the fragments of step s + u - 1 are used up
@@ -268,7 +275,7 @@ __device__ __forceinline__ TileAt tile_of(int id, int tiles_p, int tiles_q)
 struct VocabArgs {
     Operand P, Q;
     const VocabInfo* info;                         // NULL: all rows of Q count
-    const VocabRange* range;                       // fp32
+    const int *p_exp, *q_exp;                      // fp32 in parts: the powers of two that each row was divided by
     int k;                                         // length of the sum (dW: the rows that count)
     int first;                                     // tile of the launch's first workgroup
     int tiles_p, slices;
@@ -491,11 +498,11 @@ void vocab_rows_dw_kernel(VocabArgs a)
         }
 }
 
-// A value as two fp16 parts.  Infinite or NaN: in the first.
+// A value (2^15 at most) as two fp16 parts.  Infinite or NaN: in the first.
 __device__ __forceinline__ void split2(float x, _Float16& hi, _Float16& lo)
 {
     hi = (_Float16)x;
-    lo = (_Float16)(x - (float)hi);
+    lo = (_Float16)((x - (float)hi) * kLowPart);
     if (__builtin_fabsf(x) == __builtin_inff() || x != x) lo = (_Float16)0.f;
 }
 
@@ -585,11 +592,23 @@ __device__ __forceinline__ void vocab_tile(const VocabArgs& a, int block, SPH_LD
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n16 = lane & 15, g = lane >> 4, wp = wave % T::WAVES_P, wq = wave / T::WAVES_P;
     const int pw = p0 + wp * T::FP * 16, qw = q0 + wq * T::FQ * 16;     // this wave's corner
+    if constexpr (F32 && !ROWS && !SUMS) {         // the rows' powers of two
+        int qe[T::FQ];
+#pragma unroll
+        for (int j = 0; j < T::FQ; ++j) qe[j] = a.q_exp[min(qw + 16 * j + n16, rows - 1)];
+#pragma unroll
+        for (int i = 0; i < T::FP; ++i) {          // (the array goes on to a tile's end; what stands there changes nothing: the products are 0)
+            const i32x4 pe = *(const i32x4*)(a.p_exp + pw + 16 * i + 4 * g);
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int j = 0; j < T::FQ; ++j) prod.acc[i][j][r] = __builtin_ldexpf(prod.acc[i][j][r], pe[r] + qe[j]);
+        }
+    }
     // Exponentials are in base 2, the scale and log2(e) in one factor that is not negative.  Eight waves reach the end of a
     // tile together, so nothing hides these instructions: one maximum, one multiply-add, one exponential (16 cycles) and one addition
     // (or half a conversion) per logit, and everything that only the vocabulary's last tile or a row's target needs is kept out of that.
     float scale2 = a.scale2;
-    if constexpr (S == Store::F32 && !ROWS && (ST == Stage::Logits || ST == Stage::G)) scale2 *= a.range->x * a.range->w;
     if (ST != Stage::Dx && ST != Stage::Dw && scale2 < 0.f) {
         scale2 = -scale2;
 #pragma unroll
@@ -870,62 +889,6 @@ void vocab_rows_kernel(RowArgs a)
     *a.info = row_scale(a, n, top);
 }
 
-// The largest finite magnitude of W and of the rows of X that count: one per workgroup, for the packing ones to join.  fp32 only.
-constexpr int kRangeThreads = 256, kRangeGroupsX = 256, kRangeGroupsW = 512;
-
-__global__ __launch_bounds__(kRangeThreads)
-void vocab_range_kernel(const float* __restrict__ X, const float* __restrict__ W, int T, int V, int D, const void* __restrict__ targets, int id_bytes,
-                        int all_rows, float* __restrict__ most)
-{
-    __shared__ float shared[kRangeThreads / 64];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    float top = 0.f;
-    auto take = [&](float x) {
-        x = __builtin_fabsf(x);
-        top = x < __builtin_inff() ? fmaxf(top, x) : top;
-    };
-    constexpr int AHEAD = 8;
-    if (blockIdx.x < kRangeGroupsX) {
-        constexpr int WAVES = kRangeThreads / 64;
-        for (long long t = (long long)blockIdx.x * WAVES + wave; t < T; t += kRangeGroupsX * WAVES) {
-            if (!all_rows && load_id(targets, id_bytes, t) < 0) continue;
-            const float* row = X + (size_t)t * D;
-            for (int c0 = lane; c0 < D; c0 += 64 * AHEAD) {
-                float x[AHEAD];
-#pragma unroll
-                for (int a = 0; a < AHEAD; ++a) x[a] = c0 + a * 64 < D ? row[c0 + a * 64] : 0.f;
-#pragma unroll
-                for (int a = 0; a < AHEAD; ++a) take(x[a]);
-            }
-        }
-    } else {
-        const size_t n = (size_t)V * D, n4 = ((uintptr_t)W & 15) == 0 ? n / 4 : 0, step = (size_t)kRangeGroupsW * kRangeThreads;
-        const size_t i0 = (size_t)(blockIdx.x - kRangeGroupsX) * kRangeThreads + tid;
-        for (size_t i = i0; i < n4; i += step * AHEAD) {
-            f32x4 x[AHEAD];
-#pragma unroll
-            for (int a = 0; a < AHEAD; ++a) x[a] = i + a * step < n4 ? ((const f32x4*)W)[i + a * step] : f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int a = 0; a < AHEAD; ++a)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) take(x[a][r]);
-        }
-        for (size_t i = 4 * n4 + i0; i < n; i += step) take(W[i]);
-    }
-    top = max_over_wave(top);
-    if (lane == 0) shared[wave] = top;
-    __syncthreads();
-    if (tid != 0) return;
-    for (int w = 1; w < kRangeThreads / 64; ++w) top = fmaxf(top, shared[w]);
-    most[blockIdx.x] = top;
-}
-
-// The power of two that brings `top` to 2^14 .. 2^15 (1 for a tensor of zeros; both it and its inverse are normal numbers)
-__device__ __forceinline__ float range_factor(float top)
-{
-    return top > 0.f ? __builtin_ldexpf(1.f, min(126, 15 - __builtin_amdgcn_frexp_expf(top))) : 1.f;
-}
-
 // Rows as the products want them: 16-bit, 16-byte aligned, whole pieces of 8; gathered if only some count; fp32 in two
 // parts.  One wave per row; X's and W's in one launch.  For at most kOwnRows rows each workgroup finds out by itself which rows before its
 // own count, which spares a launch of one workgroup in front.
@@ -935,6 +898,7 @@ struct PackRows {
     const void* in; void* out; int n, D, ld;       // (ld: elements per row of out, a multiple of 8)
     long long part;                                // elements from part to part
     void* sum_out;                                 // fp32: the three parts that the products with G take, or NULL
+    int* exp;                                      // fp32: for the logits, the power of two that the row was divided by
 };
 struct PackArgs {
     PackRows x, w;
@@ -942,18 +906,35 @@ struct PackArgs {
     int compact, own_rows;                         // only X's rows that count; found here
     RowArgs r;
     const float* lse; int* g_target; float* g_lse2; float* g;   // what the G stage needs of each row, or NULL
-    const float* most; VocabRange* range;          // fp32: from vocab_range_kernel, and what was made of it
 };
 
 template <Store S>
-__device__ __forceinline__ void pack_row(const PackRows& a, long long t, long long m, int lane, float factor)
+__device__ __forceinline__ void pack_row(const PackRows& a, long long t, long long m, int lane)
 {
+    if (!a.out) return;                            // (few rows of fp32 are read where they are)
     const size_t from = (size_t)t * a.D, to = (size_t)m * a.ld;
     constexpr int N = per16<S>();
     const bool wide = ((uintptr_t)a.in & 15) == 0 && a.D % N == 0;
+    auto load = [&](int c) { return wide ? load16<S, true>(a.in, from + c, N, N) : load16<S, false>(a.in, from + c, a.D - c, (size_t)a.n * a.D - from - c); };
+    int up = 0;
+    if constexpr (S == Store::F32) {               // the row's largest finite element goes to 2^14 .. 2^15
+        float top = 0.f;
+        for (int c = lane * N; c < a.D; c += 64 * N) {
+            float x[N];
+            widen16<S>(load(c), x);
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float size = __builtin_fabsf(x[i]);
+                top = size < __builtin_inff() ? fmaxf(top, size) : top;
+            }
+        }
+        top = max_over_wave(top);
+        up = top > 0.f ? 15 - __builtin_amdgcn_frexp_expf(top) : 0;
+        if (lane == 0) a.exp[m] = -up;
+    }
     for (int c = lane * N; c < a.ld; c += 64 * N) {
         i32x4 w = {0, 0, 0, 0};
-        if (c < a.D) w = wide ? load16<S, true>(a.in, from + c, N, N) : load16<S, false>(a.in, from + c, a.D - c, (size_t)a.n * a.D - from - c);
+        if (c < a.D) w = load(c);
         if constexpr (S == Store::F32) {
             float x[4];
             widen16<S>(w, x);
@@ -965,7 +946,7 @@ __device__ __forceinline__ void pack_row(const PackRows& a, long long t, long lo
                 for (int k = 0; k < 3; ++k) *(i32x2*)((unsigned short*)a.sum_out + to + c + k * a.part) = part[k];
             }
 #pragma unroll
-            for (int r = 0; r < 4; ++r) x[r] *= factor;
+            for (int r = 0; r < 4; ++r) x[r] = __builtin_ldexpf(x[r], up);
             split2(x, hi, lo);
             unsigned short* o = (unsigned short*)a.out + to + c;
             *(i32x2*)o = hi;
@@ -982,22 +963,9 @@ void vocab_pack_kernel(PackArgs a)
 {
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const bool on_x = (int)blockIdx.x < a.x_groups;
-    float factor = 1.f;
-    if (S == Store::F32 && a.most) {
-        __shared__ float tops[kPackRows];
-        float top = 0.f;
-        for (int i = tid; i < (on_x ? kRangeGroupsX : kRangeGroupsW); i += kPackThreads) top = fmaxf(top, a.most[(on_x ? 0 : kRangeGroupsX) + i]);
-        top = max_over_wave(top);
-        if (lane == 0) tops[wave] = top;
-        __syncthreads();
-        for (int w = 0; w < kPackRows; ++w) top = fmaxf(top, tops[w]);
-        factor = range_factor(top);
-        if (tid == 0 && blockIdx.x == 0) a.range->x = 1.f / factor;
-        if (tid == 0 && (int)blockIdx.x == a.x_groups) a.range->w = 1.f / factor;
-    }
     if (!on_x) {
         const long long v = (long long)((int)blockIdx.x - a.x_groups) * kPackRows + wave;
-        if (v < a.w.n) pack_row<S>(a.w, v, v, lane, factor);
+        if (v < a.w.n) pack_row<S>(a.w, v, v, lane);
         return;
     }
     const long long row = (long long)blockIdx.x * kPackRows + wave;
@@ -1043,7 +1011,7 @@ void vocab_pack_kernel(PackArgs a)
         a.g_lse2[m] = a.lse[t] * kLog2e;
         a.g[m] = (a.r.reduce == Reduce::None ? a.r.dloss[t] * a.r.scale : 1.f) * up;
     }
-    pack_row<S>(a.x, t, m, lane, factor);
+    pack_row<S>(a.x, t, m, lane);
 }
 
 // The tiles' maxima and sums joined: 2^log_rows rows per workgroup (64 at most), its other lanes and waves a share of the tiles each.

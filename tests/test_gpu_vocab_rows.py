@@ -105,3 +105,54 @@ def test_gradients_of_rare_ids(pkg, T):
     gX, gW = pkg.sphattn_vocab_loss_bwd(X, W, targets, pkg.sphattn_vocab_loss_fwd(X, W, targets)[1], torch.ones((), device=DEV), reduction="sum")
     _near(gX, dX, "dX")
     _near(gW, dW, "dW")
+
+
+@pytest.mark.parametrize("T", [40, 65, 300, 1500])
+@pytest.mark.parametrize("masked", [-1e4, -1e9, torch.finfo(torch.float32).min])
+def test_ids_masked_by_a_bias(pkg, T, masked):
+    """fp32: a column of ones in X makes a column of W a bias, and some ids' bias takes them out.  The others lose nothing."""
+    X, W, targets, r = _inputs(T, 700, 64, "f32", 4)
+    X[:, 9] = 1.0
+    out = torch.rand(700, generator=r, device=DEV) < 0.3
+    out[targets.clamp_min(0)] = False
+    W[out, 9] = masked
+    ones = torch.ones(T, device=DEV)
+    lse, losses, (dX, dX_tol), dW = _exact(X, W, targets, ones)
+    got_losses, got_lse = pkg.sphattn_vocab_loss_fwd(X, W, targets)
+    _near(got_lse, lse, "lse")
+    _near(got_losses, losses, "losses")
+    gX, gW = pkg.sphattn_vocab_loss_bwd(X, W, targets, got_lse, torch.ones((), device=DEV), reduction="sum")
+    _near(gX, (dX, dX_tol), "dX")
+    _near(gW, dW, "dW")
+    assert bool((gW[out] == 0).all())
+
+
+@pytest.mark.parametrize("T", [40, 65, 300, 1500])
+def test_rows_of_far_different_sizes(pkg, T):
+    """fp32: a row of X or of W is split by its own largest element, not by its tensor's."""
+    X, W, targets, r = _inputs(T, 700, 64, "f32", 5)
+    X *= 10.0 ** -torch.randint(0, 16, (T, 1), generator=r, device=DEV).float()
+    W *= 10.0 ** torch.randint(0, 4, (700, 1), generator=r, device=DEV).float()
+    W[5] *= 1e12                                   # one row of W that hides its tensor's others
+    X[:, :32], W[5, 32:] = 0, 0                    # and that no row of X meets
+    lse, losses, dX, dW = _exact(X, W, targets, torch.ones(T, device=DEV))
+    got_losses, got_lse = pkg.sphattn_vocab_loss_fwd(X, W, targets)
+    _near(got_lse, lse, "lse")
+    _near(got_losses, losses, "losses")
+    gX, gW = pkg.sphattn_vocab_loss_bwd(X, W, targets, got_lse, torch.ones((), device=DEV), reduction="sum")
+    _near(gX, dX, "dX")
+    _near(gW, dW, "dW")
+
+
+@pytest.mark.parametrize("T", [40, 65, 300])
+@pytest.mark.parametrize("scale", [1.0, -0.5])
+def test_factors_that_would_leave_the_range_together(pkg, T, scale):
+    """fp32: largest elements of 2^100 in X and in W that never meet."""
+    X, W, targets, _ = _inputs(T, 300, 48, "f32", 6)
+    X[3], X[3, 0], W[:, 0] = 0, 2.0 ** 100, 0
+    W[7], W[7, 1], X[:, 1] = 0, 2.0 ** 100, 0
+    targets[3], targets[4] = 7, 9
+    (lse, lse_tol), (losses, loss_tol), _, _ = _exact(X, W * scale, targets, torch.ones(T, device=DEV))
+    got_losses, got_lse = pkg.sphattn_vocab_loss_fwd(X, W, targets, scale)
+    _near(got_lse, (lse, lse_tol), "lse")
+    _near(got_losses, (losses, loss_tol), "losses")
