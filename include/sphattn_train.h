@@ -57,7 +57,8 @@ int sphattn_embed_bwd(const void* tokens, int id_bytes, const float* mult, const
  *          count (SPHATTN_LOSS_MEAN; 0 if none does).  Not looked at with SPHATTN_LOSS_NONE.
  *   all_rows : 1: lse also of rows that do not count; 0: those rows cost nothing and get lse 0.
  * fp32 sums of exact products (SPHATTN_F32 with more than 64 rows: the factors to 2^-23 on average and 2^-22 at most, those
- * below 2^-29 of their row's largest element to 2^-51 of that; terms off by 3/4 2^-20 at most).  T <= 2^20, 1 <= V <= 2^24, 1 <= D <= 65536
+ * below 2^-29 of their row's largest element to 2^-51 of that; terms off by 3/4 2^-20 at most).  Infinite and NaN elements give
+ * the logits that the sum gives.  T <= 2^20, 1 <= V <= 2^24, 1 <= D <= 65536
  * (SPHATTN_ERR_SHAPE); scale finite, reduction a sphattn_reduction (SPHATTN_ERR_VALUE).
  * Workspace sizes are 0 for sizes that the call would reject.
  */

@@ -382,7 +382,7 @@ int run_vocab_fwd(const Vocab& p, const void* X, const void* W, const void* targ
     } else {
         pack<S>(p, X, W, k.compact || !ready(X, p.D, S), k, a.Q, a.P, stream);
         a.k = p.ld;
-        if (S == Store::F32) a.p_exp = p.w_exp, a.q_exp = p.x_exp;
+        if (S == Store::F32) a.p_exp = p.w_exp, a.q_exp = p.x_exp, a.p_whole = (const float*)W, a.q_whole = (const float*)X, a.D = p.D;
     }
     if (k.compact) a.info = p.info, a.rows = p.rows;
     a.slices = 1, a.V = p.V, a.scale2 = scale * kLog2e;
@@ -467,7 +467,7 @@ int run_vocab_bwd(const Vocab& p, const void* X, const void* W, const void* targ
         const Operand xs = sum_parts ? Operand{(const unsigned char*)p.x_sum, (long long)p.T * p.ld * 2, p.ld * 2, p.ld} : Operand{x.data, x.part, x.ld, p.ld};
         const Operand G{(const unsigned char*)p.G, (long long)p.T * p.piece * 2, p.piece * 2, 0};
         VocabArgs a{};
-        if (S == Store::F32) a.p_exp = p.w_exp + v0, a.q_exp = p.x_exp;
+        if (S == Store::F32) a.p_exp = p.w_exp + v0, a.q_exp = p.x_exp, a.p_whole = (const float*)W + (size_t)v0 * p.D, a.q_whole = (const float*)X, a.D = p.D, a.rows = p.rows;
         a.P = wi, a.Q = x, a.info = p.info, a.k = p.ld, a.slices = 1, a.V = p.V, a.v0 = v0, a.scale2 = scale * kLog2e;
         a.g_target = p.g_target, a.g_lse2 = p.g_lse2, a.g = p.g;
         a.G = p.G, a.G_part = (long long)p.T * p.piece, a.G_ld = p.piece;

@@ -20,7 +20,8 @@
 // the value times a power of two that brings its row's largest element to 2^14 .. 2^15), and a product is three
 // products of parts, the small ones first, on the same kernel.  A factor is off by 2^-23 on average and 2^-22 at most, below 2^-29 of its
 // row's largest element by 2^-51 of that; the product left out comes to 2^-22 of a term at most.  The powers of two come back to the logits in a tile's end,
-// so no row takes bits from another (one for all of W lost every id beside a bias of -1e9).
+// so no row takes bits from another (one for all of W lost every id beside a bias of -1e9).  Rows with an infinite element, which a product of parts makes
+// NaN of where the other part is zero, take fp32 products there instead.
 // Gradients: G, X and W as three bf16 parts each, which are the value over the whole range of fp32, and six products; what is left out comes to 2^-24 of
 // a term.  (Two fp16 parts and three products took 273 us for 1999 x 8000 x 512 where this takes 415, but hold nothing below 2^-39 of the
 // largest: a row of dX whose gradient is 1e-8 of another's lost 2 % of itself, ids that no row gives a weight above 1e-12 their whole row of dW.)
@@ -41,6 +42,7 @@ struct VocabInfo {
 };
 
 constexpr float kLowPart = 4096.f;                 // what the second fp16 part is multiplied by: below 2^-14 that type has fewer bits
+constexpr int kEndless = 1 << 20;                  // in place of the power of two of a row with an infinite element
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
@@ -275,7 +277,8 @@ __device__ __forceinline__ TileAt tile_of(int id, int tiles_p, int tiles_q)
 struct VocabArgs {
     Operand P, Q;
     const VocabInfo* info;                         // NULL: all rows of Q count
-    const int *p_exp, *q_exp;                      // fp32 in parts: the powers of two that each row was divided by
+    // fp32 in parts: the powers of two that each row was divided by (or kEndless), and the rows as they are
+    const int *p_exp, *q_exp; const float *p_whole, *q_whole; int D;
     int k;                                         // length of the sum (dW: the rows that count)
     int first;                                     // tile of the launch's first workgroup
     int tiles_p, slices;
@@ -498,7 +501,7 @@ void vocab_rows_dw_kernel(VocabArgs a)
         }
 }
 
-// A value (2^15 at most) as two fp16 parts.  Infinite or NaN: in the first.
+// A value (2^15 at most) as two fp16 parts.  NaN: in the first.
 __device__ __forceinline__ void split2(float x, _Float16& hi, _Float16& lo)
 {
     hi = (_Float16)x;
@@ -556,6 +559,36 @@ __device__ __forceinline__ i32x4 join_fragments(i32x2 a, i32x2 b)
 template <class T, Store S, Stage ST>
 constexpr bool reads_fp32() { return S == Store::F32 && T::BQ <= 64 && (ST == Stage::Logits || ST == Stage::G); }
 
+// The logits of a wave's corner from rows of fp32 as they are, four k at a time: for the rare tile that meets a row with an infinite element, where only
+// the formula itself says which infinity it is or that it is none.  Waits for nothing but its own loads.
+template <class T>
+__device__ __forceinline__ void whole_logits(f32x4 (&acc)[T::FP][T::FQ], const VocabArgs& a, int rows, int pw, int qw)
+{
+    const int lane = threadIdx.x & 63, n16 = lane & 15, g = lane >> 4;
+    const float *pat[T::FP], *qat[T::FQ];          // (rows behind the last one: see RowsProduct)
+#pragma unroll
+    for (int i = 0; i < T::FP; ++i) pat[i] = a.p_whole + (size_t)min(pw + 16 * i + n16, a.P.size - 1) * a.D;
+#pragma unroll
+    for (int j = 0; j < T::FQ; ++j) {
+        const int q = min(qw + 16 * j + n16, rows - 1);
+        qat[j] = a.q_whole + (size_t)(a.rows ? a.rows[q] : q) * a.D;
+#pragma unroll
+        for (int i = 0; i < T::FP; ++i) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+#pragma unroll 1
+    for (int k = g; k < a.D + g; k += 4) {
+        float w[T::FP], x[T::FQ];
+#pragma unroll
+        for (int i = 0; i < T::FP; ++i) w[i] = k < a.D ? pat[i][k] : 0.f;
+#pragma unroll
+        for (int j = 0; j < T::FQ; ++j) x[j] = k < a.D ? qat[j][k] : 0.f;
+#pragma unroll
+        for (int i = 0; i < T::FP; ++i)
+#pragma unroll
+            for (int j = 0; j < T::FQ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(w[i], x[j], acc[i][j], 0, 0, 0);
+    }
+}
+
 template <class T, Store S, Stage ST>
 __device__ __forceinline__ void vocab_tile(const VocabArgs& a, int block, SPH_LDS unsigned char* smem)
 {
@@ -594,16 +627,20 @@ __device__ __forceinline__ void vocab_tile(const VocabArgs& a, int block, SPH_LD
     const int pw = p0 + wp * T::FP * 16, qw = q0 + wq * T::FQ * 16;     // this wave's corner
     if constexpr (F32 && !ROWS && !SUMS) {         // the rows' powers of two
         int qe[T::FQ];
+        bool endless = false;
 #pragma unroll
-        for (int j = 0; j < T::FQ; ++j) qe[j] = a.q_exp[min(qw + 16 * j + n16, rows - 1)];
+        for (int j = 0; j < T::FQ; ++j) endless |= (qe[j] = a.q_exp[min(qw + 16 * j + n16, rows - 1)]) == kEndless;
 #pragma unroll
         for (int i = 0; i < T::FP; ++i) {          // (the array goes on to a tile's end; what stands there changes nothing: the products are 0)
             const i32x4 pe = *(const i32x4*)(a.p_exp + pw + 16 * i + 4 * g);
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
+            for (int r = 0; r < 4; ++r) {
+                endless |= pe[r] == kEndless && pw + 16 * i + 4 * g + r < a.P.size;
 #pragma unroll
                 for (int j = 0; j < T::FQ; ++j) prod.acc[i][j][r] = __builtin_ldexpf(prod.acc[i][j][r], pe[r] + qe[j]);
+            }
         }
+        if (__ballot(endless)) whole_logits<T>(prod.acc, a, rows, pw, qw);
     }
     // Exponentials are in base 2, the scale and log2(e) in one factor that is not negative.  Eight waves reach the end of a
     // tile together, so nothing hides these instructions: one maximum, one multiply-add, one exponential (16 cycles) and one addition
@@ -919,6 +956,7 @@ __device__ __forceinline__ void pack_row(const PackRows& a, long long t, long lo
     int up = 0;
     if constexpr (S == Store::F32) {               // the row's largest finite element goes to 2^14 .. 2^15
         float top = 0.f;
+        bool endless = false;
         for (int c = lane * N; c < a.D; c += 64 * N) {
             float x[N];
             widen16<S>(load(c), x);
@@ -926,11 +964,13 @@ __device__ __forceinline__ void pack_row(const PackRows& a, long long t, long lo
             for (int i = 0; i < N; ++i) {
                 const float size = __builtin_fabsf(x[i]);
                 top = size < __builtin_inff() ? fmaxf(top, size) : top;
+                endless |= size == __builtin_inff();
             }
         }
         top = max_over_wave(top);
         up = top > 0.f ? 15 - __builtin_amdgcn_frexp_expf(top) : 0;
-        if (lane == 0) a.exp[m] = -up;
+        if (__ballot(endless) && lane == 0) a.exp[m] = kEndless;
+        else if (lane == 0) a.exp[m] = -up;
     }
     for (int c = lane * N; c < a.ld; c += 64 * N) {
         i32x4 w = {0, 0, 0, 0};

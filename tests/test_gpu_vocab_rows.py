@@ -156,3 +156,34 @@ def test_factors_that_would_leave_the_range_together(pkg, T, scale):
     got_losses, got_lse = pkg.sphattn_vocab_loss_fwd(X, W, targets, scale)
     _near(got_lse, (lse, lse_tol), "lse")
     _near(got_losses, (losses, loss_tol), "losses")
+
+
+@pytest.mark.parametrize("T", [40, 65, 300, 1500])
+def test_infinite_elements(pkg, T):
+    """fp32: logits of plus and minus infinity and NaN where the formula has them, and nowhere else."""
+    X, W, targets, r = _inputs(T, 700, 64, "f32", 7, share=1.0)
+    X[:, 9] = X[:, 9].abs() + 0.1
+    targets = targets % 600
+    clean = _exact(X, W[:600], targets, torch.ones(T, device=DEV))
+    W[600:] = 0
+    W[600:, 9] = float("-inf")                     # (its zeros meet finite values only)
+    losses, lse = pkg.sphattn_vocab_loss_fwd(X, W, targets)
+    _near(lse, clean[0], "lse")
+    _near(losses, clean[1], "losses")
+    ones = torch.ones((), device=DEV)
+    dX, dW = pkg.sphattn_vocab_loss_bwd(X, W, targets, lse, ones, reduction="sum")
+    assert bool((dW[600:] == 0).all()) and bool(dX[:, 9].isnan().all())       # 0 times infinity, in that column alone
+    other = torch.arange(64, device=DEV) != 9
+    _near(dX[:, other], [t[:, other] for t in clean[2]], "dX")
+    _near(dW[:600], clean[3], "dW")
+    # anything that is not finite, by what the formula makes of it
+    W[600:] = 0
+    W[601], W[650, 3], W[650, 4] = float("-inf"), float("inf"), float("-inf")
+    X[5, 7], X[7, 2], X[min(T - 1, 64)] = float("inf"), float("nan"), float("inf")
+    x, w = X.double(), W.double()
+    logits = torch.stack([(row[None] * w).sum(1) for row in x])
+    want_lse = torch.logsumexp(logits, 1)
+    want = want_lse - logits.gather(1, targets[:, None])[:, 0]
+    for got, exact in zip(pkg.sphattn_vocab_loss_fwd(X, W, targets), (want, want_lse)):
+        assert torch.equal(got.isnan(), exact.isnan())
+        assert torch.equal(got == float("inf"), exact == float("inf")) and torch.equal(got == float("-inf"), exact == float("-inf"))
