@@ -77,8 +77,10 @@ int sphattn_vocab_loss_fwd(const void* X, const void* W, const void* targets, in
  *   dloss : SPHATTN_LOSS_NONE: [T] fp32, g = dloss;  SUM: one fp32, g[t] = dloss;  MEAN: one fp32, g[t] = dloss / (number of
  *           rows that count).
  *   dX : [T,D], dW : [V,D], the dtype of X and W; either may be NULL (not wanted), not both.
- * G is formed a piece of the vocabulary at a time and rounded to the storage type (fp16: scaled by a power of two, so that
- * small gradients keep their bits); sums in fp32, the results rounded once.  SPHATTN_F32: every factor keeps its 24 bits whatever
+ * G is formed a piece of the vocabulary at a time and rounded to the storage type; sums in fp32, the results rounded once.  fp16: G is
+ * scaled by powers of two, so that it keeps the type's bits down to 2^-28 of a row's gradient and 2^-38 of that at the least; with
+ * SPHATTN_LOSS_NONE in dW of the largest gradient of a row that counts.  (Where the rows' gradients differ by more than 2^4 it is formed
+ * once for dX and once for dW.)  SPHATTN_F32: every factor keeps its 24 bits whatever
  * the others' sizes are, terms are off by 2^-24 at most.
  */
 size_t sphattn_vocab_loss_bwd_workspace_bytes(int T, int V, int D, int dtype);

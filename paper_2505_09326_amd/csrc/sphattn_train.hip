@@ -196,6 +196,7 @@ struct Vocab {
     int *x_exp, *w_exp;                            // fp32 in parts
     int *rows, *place, *g_target;
     float *g_lse2, *g, *target_logit, *dx;
+    float *g_own, *own_down;                       // fp16
     float2* partial;
     unsigned short *x, *w, *G;
     unsigned short *x_sum, *w_sum;                 // fp32 with parts: what G is multiplied with
@@ -274,6 +275,8 @@ Vocab vocab_bwd_plan(int T, int V, int D, int dtype, void* workspace)
     p.g_target = c.take<int>(T);
     p.g_lse2 = c.take<float>(T);
     p.g = c.take<float>(T);
+    p.g_own = c.take<float>(dtype == SPHATTN_F16 ? T : 0);
+    p.own_down = c.take<float>(dtype == SPHATTN_F16 ? T : 0);
     p.x = c.take<unsigned short>((size_t)p.parts * T * p.ld);
     p.G = c.take<unsigned short>((size_t)p.g_parts * T * p.piece);
     p.dx = c.take<float>((size_t)p.slices * T * p.ld);
@@ -435,7 +438,7 @@ int run_rows_bwd(const Vocab& p, const void* X, const void* W, PackArgs k, void*
     }
     if (dX)
         hipLaunchKernelGGL((vocab_dx_kernel<S>), dim3((unsigned)(p.T + 3) / 4, (unsigned)(p.D + kDxCols - 1) / kDxCols), dim3(256), 0, stream, p.dx, p.slices,
-                           p.ld, 128, 1, 0, p.place, p.info, dX, p.T, p.D);
+                           p.ld, 128, 1, 0, p.place, p.info, (const float*)nullptr, dX, p.T, p.D);
     return launched();
 }
 
@@ -447,6 +450,9 @@ int run_vocab_bwd(const Vocab& p, const void* X, const void* W, const void* targ
     k.r = row_args(p, targets, id_bytes);
     k.r.dloss = dloss, k.r.reduce = (Reduce)reduction, k.r.scale = scale, k.r.half = S == Store::F16;
     k.compact = 1, k.lse = lse, k.g_target = p.g_target, k.g_lse2 = p.g_lse2, k.g = p.g;
+    // fp16 and one gradient per row: dX's G is scaled row by row, dW's by the largest gradient
+    const bool own = S == Store::F16 && reduction == SPHATTN_LOSS_NONE && dX, twice = own && dW;
+    if (own) k.g_own = p.g_own, k.own_down = p.own_down;
     Operand x{}, w{};
     if (p.T == 0) {                                // (the info of no rows, which one workgroup writes)
         hipLaunchKernelGGL(vocab_rows_kernel, dim3(1), dim3(kRowsThreads), 0, stream, k.r);
@@ -469,7 +475,7 @@ int run_vocab_bwd(const Vocab& p, const void* X, const void* W, const void* targ
         VocabArgs a{};
         if (S == Store::F32) a.p_exp = p.w_exp + v0, a.q_exp = p.x_exp, a.p_whole = (const float*)W + (size_t)v0 * p.D, a.q_whole = (const float*)X, a.D = p.D, a.rows = p.rows;
         a.P = wi, a.Q = x, a.info = p.info, a.k = p.ld, a.slices = 1, a.V = p.V, a.v0 = v0, a.scale2 = scale * kLog2e;
-        a.g_target = p.g_target, a.g_lse2 = p.g_lse2, a.g = p.g;
+        a.g_target = p.g_target, a.g_lse2 = p.g_lse2, a.g = own && !twice ? p.g_own : p.g;
         a.G = p.G, a.G_part = (long long)p.T * p.piece, a.G_ld = p.piece;
         int tiles;
         if (p.T > 0) rc = launch_scores<S, Stage::G>(a, n, p.T, tiles, stream);
@@ -484,6 +490,13 @@ int run_vocab_bwd(const Vocab& p, const void* X, const void* W, const void* targ
         bw.Q = G, bw.Q.size = (int)up_to(n, 8), bw.info = p.info, bw.slices = 1;
         bw.out = dW ? (unsigned char*)dW + (size_t)v0 * p.D * store_bytes<S>() : nullptr, bw.out_ld = p.D, bw.out_cols = p.D, bw.out_rows = n;
         const bool dw_big = big_tiles(p.ld, n);
+        if (twice && p.T > 0) {
+            rc = dw_big ? launch_tiles<Big, S, Stage::Dw>(bw, p.ld, n, stream) : launch_tiles<Mid, S, Stage::Dw>(bw, p.ld, n, stream);
+            a.g = p.g_own, a.unless_even = 1;
+            if (rc == SPHATTN_OK) rc = launch_scores<S, Stage::G>(a, n, p.T, tiles, stream);
+            if (rc == SPHATTN_OK) rc = p.dx_big ? launch_tiles<Big, S, Stage::Dx>(bx, p.ld, p.T, stream) : launch_tiles<Mid, S, Stage::Dx>(bx, p.ld, p.T, stream);
+            continue;
+        }
         if (with_dx && with_dw && !p.dx_big && !dw_big) {
             rc = launch_gradients<Mid, S>(bx, bw, p.ld, p.T, n, stream);
             continue;
@@ -494,7 +507,7 @@ int run_vocab_bwd(const Vocab& p, const void* X, const void* W, const void* targ
     }
     if (rc == SPHATTN_OK && dX && p.T > 0)
         hipLaunchKernelGGL((vocab_dx_kernel<S>), dim3((unsigned)(p.T + 3) / 4, (unsigned)(p.D + kDxCols - 1) / kDxCols), dim3(256), 0, stream, p.dx, p.slices, p.ld,
-                           dx_tile, (p.ld + dx_tile - 1) / dx_tile, dx_at_once, p.place, p.info, dX, p.T, p.D);
+                           dx_tile, (p.ld + dx_tile - 1) / dx_tile, dx_at_once, p.place, p.info, own ? p.own_down : (const float*)nullptr, dX, p.T, p.D);
     return rc == SPHATTN_OK ? launched() : rc;
 }
 

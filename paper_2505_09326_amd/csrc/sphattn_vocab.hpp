@@ -39,6 +39,7 @@ struct VocabInfo {
     int rows;                                      // rows with a target
     float up;                                      // factor of G in the workspace: a power of two (fp16 holds G near 2^14 with it)
     float down;                                    // factor of the sums behind it
+    int even;                                      // one gradient per row, fp16: all of them within 2^4 of the largest, so that one `up` serves every row
 };
 
 constexpr float kLowPart = 4096.f;                 // what the second fp16 part is multiplied by: below 2^-14 that type has fewer bits
@@ -289,6 +290,7 @@ struct VocabArgs {
     const void* targets; int id_bytes; const int* rows;   // targets[rows[q]], or targets[q] without rows
     float2* partial; int partial_ld; float* target_logit; // logits
     const int* g_target; const float* g_lse2; const float* g;   // G, by row that counts
+    int unless_even;                               // G: already there if the rows' gradients are even
     void* G; long long G_part; int G_ld;           // (elements)
     // dX, dW
     void* out; int out_ld; int out_cols, out_rows; int accumulate;   // (dX: slice after slice, `rows` rows each)
@@ -597,6 +599,8 @@ __device__ __forceinline__ void vocab_tile(const VocabArgs& a, int block, SPH_LD
     float down = 1.f;
     if (a.info) {
         rows = __builtin_amdgcn_readfirstlane(a.info->rows);
+        if constexpr (ST == Stage::G && S == Store::F16)
+            if (a.unless_even && __builtin_amdgcn_readfirstlane(a.info->even)) return;
         if constexpr (ST == Stage::Dw) down = a.info->down;
     }
     Operand Q = a.Q;
@@ -841,10 +845,17 @@ struct RowArgs {
     const float* dloss; Reduce reduce; float scale; int half;   // half: G is stored in fp16
 };
 
-// `top`: the largest |dloss| of a row that counts, where there is one for each
-__device__ __forceinline__ VocabInfo row_scale(const RowArgs& a, int n, float top)
+// The power of two that brings |x| to 2^13 .. 2^14
+__device__ __forceinline__ float gradient_factor(float x)
 {
-    VocabInfo out{n, 1.f, 1.f};
+    x = __builtin_fabsf(x);
+    return x > 0.f && x < __builtin_inff() ? __builtin_ldexpf(1.f, max(-126, min(126, 13 - (__builtin_amdgcn_frexp_expf(x) - 1)))) : 1.f;
+}
+
+// `top`, `least`: the largest |dloss| of a row that counts and the smallest that is not 0, where there is one for each
+__device__ __forceinline__ VocabInfo row_scale(const RowArgs& a, int n, float top, float least)
+{
+    VocabInfo out{n, 1.f, 1.f, 1};
     if (a.dloss && a.reduce != Reduce::None) {
         // One gradient for all rows comes behind the sums: G is then p - [v = y], and the -1 of a target, which is most of a row's
         // gradient and of a rare id's, has no rounding (with g in front, g (p - 1) is rounded to the type: 2.6e-3 from 64 bits in bf16 where
@@ -853,13 +864,11 @@ __device__ __forceinline__ VocabInfo row_scale(const RowArgs& a, int n, float to
         out.up = a.half ? 16384.f : 1.f;
         out.down = g * a.scale / out.up;
     } else if (a.dloss && a.half) {
-        // the largest |c g| goes to 2^13 .. 2^14
-        const float x = __builtin_fabsf(top * a.scale);
-        if (x > 0.f && x < __builtin_inff()) {
-            const int e = max(-126, min(126, 13 - (__builtin_amdgcn_frexp_expf(x) - 1)));
-            out.up = __builtin_ldexpf(1.f, e);
-            out.down = __builtin_ldexpf(1.f, -e);
-        }
+        // By the largest |c g|.  That keeps dW's sums over the rows to 2^-38 of it; a row of dX has to keep its own gradient's bits, so where the
+        // rows' gradients differ dX takes a G of its own, each row brought up by itself.
+        out.up = gradient_factor(top * a.scale);
+        out.down = 1.f / out.up;
+        out.even = top < __builtin_inff() && least >= top * 0.0625f;
     }
     return out;
 }
@@ -869,6 +878,13 @@ __device__ __forceinline__ float max_over_wave(float x)
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) x = fmaxf(x, __shfl_xor(x, d));
     return x;
+}
+
+// |x| among those that `least` is the smallest of
+__device__ __forceinline__ float smaller(float least, float x)
+{
+    x = __builtin_fabsf(x);
+    return x > 0.f ? fminf(least, x) : least;
 }
 
 __device__ __forceinline__ int lanes_below(uint64_t mask)
@@ -884,10 +900,10 @@ void vocab_rows_kernel(RowArgs a)
 {
     constexpr int WAVES = kRowsThreads / 64, EACH = 8;      // a wave takes EACH times 64 neighbouring rows at a time
     __shared__ int part[2][WAVES];
-    __shared__ float most[WAVES];
+    __shared__ float most[WAVES], fewest[WAVES];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     int n = 0, turn = 0;
-    float top = 0.f;
+    float top = 0.f, least = __builtin_inff();
     for (long long t0 = 0; t0 < a.T; t0 += kRowsThreads * EACH, turn ^= 1) {
         const long long t = t0 + wave * (64 * EACH) + lane;
         int id[EACH];
@@ -913,17 +929,22 @@ void vocab_rows_kernel(RowArgs a)
             if (t + i * 64 < a.T) a.place[t + i * 64] = id[i] >= 0 ? m : -1;
             if (id[i] >= 0) {
                 a.rows[m] = (int)(t + i * 64);
-                if (a.dloss && a.reduce == Reduce::None) top = fmaxf(top, __builtin_fabsf(a.dloss[t + i * 64]));
+                if (a.dloss && a.reduce == Reduce::None) {
+                    const float g = a.dloss[t + i * 64];
+                    top = fmaxf(top, __builtin_fabsf(g));
+                    least = smaller(least, g);
+                }
             }
             at += __builtin_popcountll(counts[i]);
         }
     }
     top = max_over_wave(top);
-    if (lane == 0) most[wave] = top;
+    least = -max_over_wave(-least);
+    if (lane == 0) most[wave] = top, fewest[wave] = least;
     __syncthreads();
     if (tid != 0) return;
-    for (int w = 1; w < WAVES; ++w) top = fmaxf(top, most[w]);
-    *a.info = row_scale(a, n, top);
+    for (int w = 1; w < WAVES; ++w) top = fmaxf(top, most[w]), least = fminf(least, fewest[w]);
+    *a.info = row_scale(a, n, top, least);
 }
 
 // Rows as the products want them: 16-bit, 16-byte aligned, whole pieces of 8; gathered if only some count; fp32 in two
@@ -943,6 +964,7 @@ struct PackArgs {
     int compact, own_rows;                         // only X's rows that count; found here
     RowArgs r;
     const float* lse; int* g_target; float* g_lse2; float* g;   // what the G stage needs of each row, or NULL
+    float *g_own, *own_down;                       // fp16, one gradient per row: g of dX's own G and the factor of dX's rows, or NULL
 };
 
 template <Store S>
@@ -1011,25 +1033,31 @@ void vocab_pack_kernel(PackArgs a)
     const long long row = (long long)blockIdx.x * kPackRows + wave;
     long long t = row, m = row;
     float up = 1.f;
+    int even = 1;
     if (a.compact && a.own_rows) {
         __shared__ int before[kPackRows], all[kPackRows];
-        __shared__ float most[kPackRows];
+        __shared__ float most[kPackRows], fewest[kPackRows];
         const int t0 = (int)blockIdx.x * kPackRows;
         int b = 0, n = 0;
-        float top = 0.f;
+        float top = 0.f, least = __builtin_inff();
         for (int i0 = 0; i0 < a.r.T; i0 += kPackThreads) {
             const int i = i0 + tid;
             const bool counts = i < a.r.T && load_id(a.r.targets, a.r.id_bytes, i) >= 0;
             n += __builtin_popcountll(__ballot(counts));
             b += __builtin_popcountll(__ballot(counts && i < t0));
-            if (counts && a.r.dloss && a.r.reduce == Reduce::None) top = fmaxf(top, __builtin_fabsf(a.r.dloss[i]));
+            if (counts && a.r.dloss && a.r.reduce == Reduce::None) {
+                const float g = a.r.dloss[i];
+                top = fmaxf(top, __builtin_fabsf(g));
+                least = smaller(least, g);
+            }
         }
         top = max_over_wave(top);
-        if (lane == 0) before[wave] = b, all[wave] = n, most[wave] = top;
+        least = -max_over_wave(-least);
+        if (lane == 0) before[wave] = b, all[wave] = n, most[wave] = top, fewest[wave] = least;
         __syncthreads();
         b = n = 0;
-        for (int w = 0; w < kPackRows; ++w) b += before[w], n += all[w], top = fmaxf(top, most[w]);
-        const VocabInfo info = row_scale(a.r, n, top);
+        for (int w = 0; w < kPackRows; ++w) b += before[w], n += all[w], top = fmaxf(top, most[w]), least = fminf(least, fewest[w]);
+        const VocabInfo info = row_scale(a.r, n, top, least);
         if (blockIdx.x == 0 && tid == 0) *a.r.info = info;
         if (row >= a.r.T) return;
         const bool counts = load_id(a.r.targets, a.r.id_bytes, row) >= 0;
@@ -1039,17 +1067,25 @@ void vocab_pack_kernel(PackArgs a)
         if (!counts) return;
         if (lane == 0) a.r.rows[m] = (int)row;
         up = info.up;
+        even = info.even;
     } else if (a.compact) {
         if (m >= a.r.info->rows) return;
         t = a.r.rows[m];
         up = a.r.info->up;
+        even = a.r.info->even;
     } else if (m >= a.x.n) {
         return;
     }
     if (a.g_target && lane == 0) {
         a.g_target[m] = load_id(a.r.targets, a.r.id_bytes, t);
         a.g_lse2[m] = a.lse[t] * kLog2e;
-        a.g[m] = (a.r.reduce == Reduce::None ? a.r.dloss[t] * a.r.scale : 1.f) * up;
+        const float g = a.r.reduce == Reduce::None ? a.r.dloss[t] * a.r.scale : 1.f;
+        a.g[m] = g * up;
+        if (a.g_own) {
+            const float own = even ? up : gradient_factor(g);
+            a.g_own[m] = g * own;
+            a.own_down[m] = 1.f / own;
+        }
     }
     pack_row<S>(a.x, t, m, lane);
 }
@@ -1147,13 +1183,12 @@ constexpr int kDxCols = 256;
 template <Store S>
 __global__ __launch_bounds__(256)
 void vocab_dx_kernel(const float* __restrict__ part, int slices, int ld, int tile_q, int tiles_p, int target, const int* __restrict__ place,
-                     const VocabInfo* __restrict__ info, void* __restrict__ dX, int T, int D)
+                     const VocabInfo* __restrict__ info, const float* __restrict__ own_down, void* __restrict__ dX, int T, int D)
 {
     const int lane = threadIdx.x & 63;
     const long long t = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (t >= T) return;
     const int m = place[t];
-    const float down = info->down;
     const int rows = info->rows;
     const size_t slice = (size_t)rows * ld;
     slices = dx_slices(rows, T, slices, tile_q, tiles_p, target);
@@ -1172,7 +1207,7 @@ void vocab_dx_kernel(const float* __restrict__ part, int slices, int ld, int til
                 for (int a = 0; a < AHEAD; ++a)
                     if (s0 + a < slices) x += y[a];
             }
-            x *= down;                             // (not of rows that do not count: it may be infinite or NaN, and their gradient is 0)
+            x *= own_down ? own_down[m] : info->down;   // (not of rows that do not count: it may be infinite or NaN, and their gradient is 0)
         }
         const size_t at = (size_t)t * D + c;
         if (wide) {

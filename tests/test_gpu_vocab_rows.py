@@ -71,12 +71,12 @@ def _near(got, want, what):
     assert float(far.max()) == 0, (what, float(far.max()), divmod(int(far.argmax()), got.shape[-1]))
 
 
-@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("T", [40, 200, 1500])
 def test_gradients_of_rows_over_many_powers_of_ten(pkg, T, dtype):
     """Each row's dX to its own size, whatever the other rows' gradients are; dW to its terms'."""
     X, W, targets, r = _inputs(T, 777, 72, dtype, 2, spread=8.0)
-    decades = torch.randint(-12, 1, (T,), generator=r, device=DEV) if dtype != "f16" else torch.randint(-5, 5, (T,), generator=r, device=DEV)
+    decades = torch.randint(-12, 1, (T,), generator=r, device=DEV) if dtype != "f16" else torch.randint(-5, 4, (T,), generator=r, device=DEV)
     g = torch.randn(T, generator=r, device=DEV).clamp(-3, 3) * 10.0 ** decades
     lse, losses, dX, _ = _exact(X, W, targets, g)
     got_losses, got_lse = pkg.sphattn_vocab_loss_fwd(X, W, targets)
