@@ -961,7 +961,7 @@ def sphattn_clip_grads_workspace_bytes(n) -> int:
 def sphattn_clip_grads(grads, max_norm, out=None, norm=None, workspace=None, stream=None):
     """Scale gradients down so that their common 2-norm is at most max_norm: out[i] = grads[i] * min(1, max_norm / (norm + 1e-6)),
     in place unless `out` (a tensor like each of `grads`) is given.  Tensors of fp32, bf16 and fp16, in any mixture, of any
-    shape, dense in memory.  Returns the norm (before clipping) as an fp32 scalar on the device; nothing waits for it."""
+    shape, dense in memory; what is written has its version raised, as by torch's operations in place.  Returns the norm (before clipping) as an fp32 scalar on the device; nothing waits for it."""
     import torch
     lib = load_library()
     grads = list(grads)
@@ -996,4 +996,7 @@ def sphattn_clip_grads(grads, max_norm, out=None, norm=None, workspace=None, str
     _raise_on(lib.sphattn_clip_grads(pointers(*[g.data_ptr() for g in grads]), pointers(*[o.data_ptr() for o in outs]),
                                      sizes(*[g.numel() for g in grads]), types(*[codes[g.dtype] for g in grads]), n, max_norm,
                                      norm.data_ptr(), ws.data_ptr(), ws_bytes, _stream_of(norm, stream)))
+    for o in outs:                                 # autograd is told, as by torch's own operations in place
+        if not o.is_inference():
+            torch.autograd.graph.increment_version(o)
     return norm

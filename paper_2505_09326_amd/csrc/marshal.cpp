@@ -573,6 +573,7 @@ PyObject* clip(PyObject*, PyObject* const* args, Py_ssize_t n)
         std::vector<void*> out(count);
         std::vector<long long> size(count);
         std::vector<int> type(count);
+        std::vector<const at::Tensor*> written(count);
         const at::Tensor* first = nullptr;
         for (Py_ssize_t i = 0; i < count; ++i) {
             const at::Tensor *g = tensor(PyList_GET_ITEM(args[0], i)), *o = tensor(PyList_GET_ITEM(args[1], i));
@@ -581,6 +582,7 @@ PyObject* clip(PyObject*, PyObject* const* args, Py_ssize_t n)
             if (g->device() != first->device() || (o != g && (o->scalar_type() != g->scalar_type() || o->device() != g->device() || o->layout() != at::kStrided ||
                                                               o->sizes() != g->sizes() || o->strides() != g->strides())))
                 Py_RETURN_NONE;
+            written[i] = o;
             in[i] = data(*g), out[i] = data(*o), size[i] = g->numel(), type[i] = code_of(*g);
         }
         const Unlocked unlocked;
@@ -588,6 +590,10 @@ PyObject* clip(PyObject*, PyObject* const* args, Py_ssize_t n)
         const size_t bytes = entry.clip_bytes((int)count);
         const at::Tensor ws = bytes_of(bytes, *first);
         rc = entry.clip(in.data(), out.data(), size.data(), type.data(), (int)count, (float)max_norm, (float*)data(norm), data(ws), bytes, stream_of(*first));
+        // autograd is told, as by torch's own operations in place: what it has saved of these tensors is no longer there
+        if (rc == 0)
+            for (const at::Tensor* o : written)
+                if (!o->is_inference()) o->unsafeGetTensorImpl()->bump_version();
     } catch (...) {
         PyErr_Clear();
         Py_RETURN_NONE;
