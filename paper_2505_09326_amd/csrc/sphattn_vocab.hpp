@@ -9,8 +9,9 @@
 //   G        the same tiles again for a piece of the vocabulary, each turned into 16-bit values of G in a workspace
 //   dX, dW   products of that piece with W and X, the operand whose rows run along the sum read from LDS transposed
 // The logits are formed twice (8 T V D operations for a training step instead of 6): a tile costs less than
-// writing it as fp32 and reading it back.  G is rounded to the storage type (once; half a unit in the last place, 2^-9 of a
-// term in bf16, 2^-12 in fp16), sums are in fp32 throughout.
+// writing it as fp32 and reading it back.  G is rounded to the storage type, which is what the matrix instructions take (once, by 2^-8 of a term in bf16 and 2^-11
+// in fp16 at most; that is a tenth of the whole error against 64 bits, most of which is the rounding of the results: 1.8e-3 against 1.7e-3 with G in fp32),
+// sums are in fp32 throughout.
 //
 // Bound by the matrix pipes where the sums are long: 8192 rows, 65536 ids, width 2048 in bf16 7.0 to 7.2 ms, 8 T V D at 1226 to 1257 TFLOP/s, what a
 // library product of 8192^3 reaches (1266).  At width 1024 a tile's end, its exponentials and stores, has no other tile's products beside it: logits and
@@ -23,7 +24,7 @@
 // so no row takes bits from another (one for all of W lost every id beside a bias of -1e9).  Rows with an infinite element, which a product of parts makes
 // NaN of where the other part is zero, take fp32 products there instead.
 // Gradients: G, X and W as three bf16 parts each, which are the value over the whole range of fp32, and six products; what is left out comes to 2^-24 of
-// a term.  (Two fp16 parts and three products took 273 us for 1999 x 8000 x 512 where this takes 415, but hold nothing below 2^-39 of the
+// a term.  (Two fp16 parts and three products took 273 us for 1999 x 8000 x 512 where this takes 395 to 400, but hold nothing below 2^-39 of the
 // largest: a row of dX whose gradient is 1e-8 of another's lost 2 % of itself, ids that no row gives a weight above 1e-12 their whole row of dW.)
 // Up to 64 rows, where reading W is most of the time, use fp32 matrix instructions on fp32 as it is: RowsProduct.
 #pragma once
@@ -300,7 +301,7 @@ enum class Stage { Logits, G, Dx, Dw };
 
 // Slices of dX's sum over the vocabulary for `rows` rows that count, where a launch for T of them has `slices`: as many more as
 // workgroups and arrays of partial sums are then free, while the chip is not full.  (8000 rows of which 1200 count, 20011 ids, width 1024:
-// dX 169 -> 56 us, and 9 more to add the slices up.)
+// dX 169 -> 56 us, and 15 to add the slices up where it was 6.)
 __device__ __forceinline__ int dx_slices(int rows, int T, int slices, int tile_q, int tiles_p, int target)
 {
     const int tq = (rows + tile_q - 1) / tile_q, tq_all = (T + tile_q - 1) / tile_q;
@@ -321,7 +322,8 @@ __device__ __forceinline__ f32x4 mfma_f32(i32x4 a, i32x4 b, int e, f32x4 c) { re
 // instruction (16x16x4, a twelfth of the 16-bit rate: 64 rows of width 1024 take it as long as their W takes memory).  Lane (i, g) holds four neighbouring
 // k, 4 g .. 4 g + 3 of sixteen, of row i of both operands, and instruction r takes the r-th: any order of k will do if both have it.
 // (17 rows, 50000 x 1024: logits 68 us, W at 3.0 TB/s, dX 57, dW 62, a training step 277; with parts in memory 489.  64 rows, 60000 x 1472: 165, 149, 179,
-// and 655 against 840.  3 rows, 20000 x 512: 17.6, 11, 12.)
+// and 655 against 840, which the instruction's rate is less than half of: X's fragments are loaded in the step that multiplies them.  3 rows, 20000 x
+// 512: 17.6, 11, 12.)
 template <class T>
 struct RowsProduct {
     f32x4 acc[T::FP][T::FQ];
@@ -453,7 +455,8 @@ void vocab_rows_dx_kernel(VocabArgs a)
         }
 }
 
-// dW of those: a wave 64 ids x 64 columns, sums over the rows that count; bound by writing dW.  X is read in place (rows[q]).
+// dW of those: a wave 64 ids x 64 columns, sums over the rows that count.  X is read in place (rows[q]) and nothing
+// ahead, so dW leaves at less than memory's rate: 17 rows, 50000 x 1024 at 3.3 TB/s, 64 rows, 60000 x 1472 at 2.0.
 __global__ __launch_bounds__(256)
 void vocab_rows_dw_kernel(VocabArgs a)
 {
@@ -843,6 +846,7 @@ struct RowArgs {
     const void* targets; int id_bytes; int T;
     int* rows; int* place; VocabInfo* info;
     const float* dloss; Reduce reduce; float scale; int half;   // half: G is stored in fp16
+    __device__ __forceinline__ bool by_row() const { return dloss && half && reduce == Reduce::None; }
 };
 
 // The power of two that brings |x| to 2^13 .. 2^14
@@ -863,7 +867,7 @@ __device__ __forceinline__ VocabInfo row_scale(const RowArgs& a, int n, float to
         const float g = n ? (a.reduce == Reduce::Mean ? *a.dloss / (float)n : *a.dloss) : 0.f;
         out.up = a.half ? 16384.f : 1.f;
         out.down = g * a.scale / out.up;
-    } else if (a.dloss && a.half) {
+    } else if (a.by_row()) {
         // By the largest |c g|.  That keeps dW's sums over the rows to 2^-38 of it; a row of dX has to keep its own gradient's bits, so where the
         // rows' gradients differ dX takes a G of its own, each row brought up by itself.
         out.up = gradient_factor(top * a.scale);
@@ -929,7 +933,7 @@ void vocab_rows_kernel(RowArgs a)
             if (t + i * 64 < a.T) a.place[t + i * 64] = id[i] >= 0 ? m : -1;
             if (id[i] >= 0) {
                 a.rows[m] = (int)(t + i * 64);
-                if (a.dloss && a.reduce == Reduce::None) {
+                if (a.by_row()) {
                     const float g = a.dloss[t + i * 64];
                     top = fmaxf(top, __builtin_fabsf(g));
                     least = smaller(least, g);
@@ -1045,14 +1049,16 @@ void vocab_pack_kernel(PackArgs a)
             const bool counts = i < a.r.T && load_id(a.r.targets, a.r.id_bytes, i) >= 0;
             n += __builtin_popcountll(__ballot(counts));
             b += __builtin_popcountll(__ballot(counts && i < t0));
-            if (counts && a.r.dloss && a.r.reduce == Reduce::None) {
+            if (counts && a.r.by_row()) {
                 const float g = a.r.dloss[i];
                 top = fmaxf(top, __builtin_fabsf(g));
                 least = smaller(least, g);
             }
         }
-        top = max_over_wave(top);
-        least = -max_over_wave(-least);
+        if (a.r.by_row()) {
+            top = max_over_wave(top);
+            least = -max_over_wave(-least);
+        }
         if (lane == 0) before[wave] = b, all[wave] = n, most[wave] = top, fewest[wave] = least;
         __syncthreads();
         b = n = 0;
