@@ -24,7 +24,7 @@
 // so no row takes bits from another (one for all of W lost every id beside a bias of -1e9).  Rows with an infinite element, which a product of parts makes
 // NaN of where the other part is zero, take fp32 products there instead.
 // Gradients: G, X and W as three bf16 parts each, which are the value over the whole range of fp32, and six products; what is left out comes to 2^-24 of
-// a term.  (Two fp16 parts and three products took 273 us for 1999 x 8000 x 512 where this takes 395 to 400, but hold nothing below 2^-39 of the
+// a term.  (Two fp16 parts and three products took 273 us for 1999 x 8000 x 512 where this takes 394 to 412, but hold nothing below 2^-39 of the
 // largest: a row of dX whose gradient is 1e-8 of another's lost 2 % of itself, ids that no row gives a weight above 1e-12 their whole row of dW.)
 // Up to 64 rows, where reading W is most of the time, use fp32 matrix instructions on fp32 as it is: RowsProduct.
 #pragma once
