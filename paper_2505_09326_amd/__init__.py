@@ -52,6 +52,7 @@ EXPORTED_SYMBOLS = ("sphattn_fwd", "sphattn_fwd_z", "sphattn_fwd_tile_rows", "sp
                     "sphattn_vocab_loss_workspace_bytes", "sphattn_vocab_loss_fwd",
                     "sphattn_vocab_loss_bwd_workspace_bytes", "sphattn_vocab_loss_bwd",
                     "sphattn_clip_grads_workspace_bytes", "sphattn_clip_grads",
+                    "sphattn_head_norm_rotary_fwd", "sphattn_head_norm_rotary_bwd_workspace_bytes", "sphattn_head_norm_rotary_bwd",
                     "sphattn_strerror", "sphattn_version")
 
 NORMALIZERS = {"l2": 0, "softmax": 1, "l1": 2, "sqrelu": 3}
@@ -149,6 +150,12 @@ def load_library() -> ctypes.CDLL:
         lib.sphattn_clip_grads_workspace_bytes.argtypes = [ip]
         lib.sphattn_clip_grads.restype = ip
         lib.sphattn_clip_grads.argtypes = [vp, vp, vp, vp, ip, fl, vp, vp, sz, vp]
+        lib.sphattn_head_norm_rotary_fwd.restype = ip
+        lib.sphattn_head_norm_rotary_fwd.argtypes = [vp] * 7 + [ip] * 6 + [fl, ip, vp]
+        lib.sphattn_head_norm_rotary_bwd_workspace_bytes.restype = sz
+        lib.sphattn_head_norm_rotary_bwd_workspace_bytes.argtypes = [ip]
+        lib.sphattn_head_norm_rotary_bwd.restype = ip
+        lib.sphattn_head_norm_rotary_bwd.argtypes = [vp] * 11 + [ip] * 6 + [fl, ip, vp, sz, vp]
         lib.sphattn_strerror.restype = ctypes.c_char_p
         lib.sphattn_strerror.argtypes = [ip]
         lib.sphattn_version.restype = ip
@@ -1000,3 +1007,162 @@ def sphattn_clip_grads(grads, max_norm, out=None, norm=None, workspace=None, str
         if not o.is_inference():
             torch.autograd.graph.increment_version(o)
     return norm
+
+
+# ---- what a layer has around the attention (include/sphattn_layer.h) ---------------------------------------
+
+class _Heads(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("batch", ctypes.c_longlong), ("token", ctypes.c_longlong), ("head", ctypes.c_longlong)]
+
+
+class _Rotary(ctypes.Structure):
+    _fields_ = [("positions", ctypes.c_void_p), ("id_bytes", ctypes.c_int), ("axis", ctypes.c_longlong), ("batch", ctypes.c_longlong),
+                ("inv_freq", ctypes.c_void_p), ("axes", ctypes.c_int), ("sections", ctypes.c_int * 3), ("interleaved", ctypes.c_int)]
+
+
+def _heads_of(t, by_token):
+    """t [B,N,H,d] (by_token) or [B,H,N,d] by its strides, as sphattn_heads; None: NULL."""
+    if t is None:
+        return None
+    stride = t.stride()
+    return ctypes.byref(_Heads(t.data_ptr(), stride[0], *((stride[1], stride[2]) if by_token else (stride[2], stride[1]))))
+
+
+def _need_heads(name, t, shape, dtype, optional=False):
+    """Rows of d neighbouring elements, anywhere."""
+    if t is None and optional:
+        return
+    if t is None:
+        raise ValueError(f"{name} is required")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must have dtype {dtype}, got {t.dtype}")
+    if t.stride(3) != 1 and t.shape[3] != 1:
+        raise ValueError(f"{name}'s last dimension must be contiguous")
+
+
+def _rotary_of(positions, inv_freq, sections, interleaved, B, N, d):
+    """sphattn_rotary from positions [N], [B,N] or [axes,B,N] (B 1: the same for every sequence); None without positions."""
+    import torch
+    if positions is None:
+        if inv_freq is not None or sections is not None:
+            raise ValueError("positions is required with inv_freq or sections")
+        return None
+    if positions.dtype not in _id_types():
+        raise ValueError(f"positions must have dtype torch.int32 or torch.int64, got {positions.dtype}")
+    if positions.dim() not in (1, 2, 3) or positions.shape[-1] != N or (positions.dim() > 1 and positions.shape[-2] not in (1, B)) or \
+            (positions.dim() == 3 and not 1 <= positions.shape[0] <= 3):
+        raise ValueError(f"positions must have shape ({N},), ({B}, {N}) or (axes, {B}, {N}) with 1 to 3 axes, got {tuple(positions.shape)}")
+    if N > 1 and positions.stride(-1) != 1:
+        raise ValueError("positions' last dimension must be contiguous")
+    axes = positions.shape[0] if positions.dim() == 3 else 1
+    sections = ([d // 2] if axes == 1 else None) if sections is None else [int(x) for x in sections]
+    if sections is None or len(sections) != axes or min(sections) < 0 or sum(sections) != d // 2:
+        raise ValueError(f"sections must say how many of the {d // 2} frequencies go by each of the {axes} axes, got {sections}")
+    _need("inv_freq", inv_freq, (d // 2,), (torch.float32,))
+    batch = positions.stride(-2) if positions.dim() > 1 and positions.shape[-2] > 1 else 0
+    return _Rotary(positions.data_ptr(), _id_types()[positions.dtype], positions.stride(0) if positions.dim() == 3 else 0, batch, inv_freq.data_ptr(), axes,
+                   (ctypes.c_int * 3)(*(sections + [0] * (3 - axes))), int(bool(interleaved)))
+
+
+def _projection(Xq, Xk, wq, wk):
+    """(B, N, Hq, Hk, d, code) of queries [B,N,Hq,d] and keys [B,N,Hk,d] or None."""
+    if Xq is None or Xq.dim() != 4:
+        raise ValueError("Xq must be a [B,N,H,d] tensor")
+    B, N, Hq, d = (int(x) for x in Xq.shape)
+    code = _code_of("Xq", Xq)
+    if Xk is not None and Xk.dim() != 4:
+        raise ValueError("Xk must be a [B,N,H,d] tensor")
+    Hk = 0 if Xk is None else int(Xk.shape[2])
+    if Xk is not None and Hk < 1:
+        raise ValueError("Xk has no heads")
+    if Xk is None and wk is not None:
+        raise ValueError("wk without Xk")
+    _need_heads("Xq", Xq, (B, N, Hq, d), Xq.dtype)
+    _need_heads("Xk", Xk, (B, N, Hk, d), Xq.dtype, optional=True)
+    _need("wq", wq, (d,), (Xq.dtype,), optional=True)
+    _need("wk", wk, (d,), (Xq.dtype,), optional=True)
+    return B, N, Hq, Hk, d, code
+
+
+def _eps(eps):
+    eps = _finite("eps", eps)
+    if eps < 0:
+        raise ValueError(f"eps must not be negative, got {eps}")
+    return eps
+
+
+def sphattn_head_norm_rotary_fwd(Xq, Xk=None, wq=None, wk=None, positions=None, inv_freq=None, sections=None, interleaved=False, norm=True,
+                                 eps=1e-6, Q=None, K=None, stream=None):
+    """Queries Xq [B,N,Hq,d] and keys Xk [B,N,Hk,d] (or None) of a projection, of any strides with rows of d neighbouring elements, for the
+    attention: each row x / sqrt(mean(x^2) + eps) (norm=False: x as it is) times wq or wk [d], rotated by its token's position.  positions [N], [B,N] or, for
+    several axes, [axes,B,N] (int32 or int64), inv_freq [d/2] fp32 (radians per position), sections: how many of the frequencies go by each axis;
+    interleaved: neighbouring dimensions turn together instead of i and i + d/2.  Returns (Q [B,Hq,N,d], K [B,Hk,N,d] or None), or writes into
+    those given, which may have any strides that leave each row a place of its own (a slice of a cache)."""
+    import torch
+    lib = load_library()
+    B, N, Hq, Hk, d, code = _projection(Xq, Xk, wq, wk)
+    eps = _eps(eps)
+    rotary = _rotary_of(positions, inv_freq, sections, interleaved, B, N, d)
+    _brought(stream, Q=Q, **({"K": K} if Hk else {}))
+    if K is not None and not Hk:
+        raise ValueError("K without Xk")
+    _need_heads("Q", Q, (B, Hq, N, d), Xq.dtype, optional=True)
+    _need_heads("K", K, (B, Hk, N, d), Xq.dtype, optional=True)
+    _on_device(Xq=Xq, Xk=Xk, wq=wq, wk=wk, positions=positions, inv_freq=inv_freq, Q=Q, K=K)
+    given = [t for t in (Q, K) if t is not None]
+    if Q is None:
+        Q = torch.empty((B, Hq, N, d), dtype=Xq.dtype, device=Xq.device)
+    if K is None and Hk:
+        K = torch.empty((B, Hk, N, d), dtype=Xq.dtype, device=Xq.device)
+    _raise_on(lib.sphattn_head_norm_rotary_fwd(_heads_of(Xq, True), _heads_of(Xk, True), _ptr(wq), _ptr(wk), _heads_of(Q, False), _heads_of(K, False),
+                                               None if rotary is None else ctypes.byref(rotary), B, N, Hq, Hk, d, int(bool(norm)), eps, code,
+                                               _stream_of(Xq, stream)))
+    for t in given:                                # autograd is told, as by torch's own operations in place
+        if not t.is_inference():
+            torch.autograd.graph.increment_version(t)
+    return Q, K
+
+
+def sphattn_head_norm_rotary_bwd_workspace_bytes(d) -> int:
+    return int(load_library().sphattn_head_norm_rotary_bwd_workspace_bytes(d))
+
+
+def sphattn_head_norm_rotary_bwd(Xq, Xk, wq, wk, dQ, dK, positions=None, inv_freq=None, sections=None, interleaved=False, norm=True, eps=1e-6,
+                                 dXq=None, dXk=None, dwq=None, dwk=None, want_dX=(True, True), want_dw=(True, True), workspace=None, stream=None):
+    """Gradients (dXq, dXk, dwq, dwk) of sphattn_head_norm_rotary_fwd for dQ [B,Hq,N,d] and dK [B,Hk,N,d], of any strides with rows of d neighbouring
+    elements.  dXq [B,N,Hq,d] and dXk [B,N,Hk,d] are contiguous, or written into those given, of any strides that leave each row a place of its
+    own.  None in the place of what is not wanted or not there (want_dX, want_dw: of queries, of keys; at least one)."""
+    import torch
+    lib = load_library()
+    B, N, Hq, Hk, d, code = _projection(Xq, Xk, wq, wk)
+    eps = _eps(eps)
+    rotary = _rotary_of(positions, inv_freq, sections, interleaved, B, N, d)
+    wants = [bool(want_dX[0]), bool(want_dX[1]) and Hk > 0, bool(want_dw[0]) and wq is not None, bool(want_dw[1]) and wk is not None]
+    if not any(wants):
+        raise ValueError("no gradient is wanted")
+    if Xk is None and dK is not None:
+        raise ValueError("dK without Xk")
+    _need_heads("dQ", dQ, (B, Hq, N, d), Xq.dtype)
+    _need_heads("dK", dK, (B, Hk, N, d), Xq.dtype, optional=not Hk)
+    shapes = [(B, N, Hq, d), (B, N, Hk, d), (d,), (d,)]
+    out = [t if w else None for t, w in zip((dXq, dXk, dwq, dwk), wants)]
+    _brought(stream, **{n: t for n, t, w in zip(("dXq", "dXk", "dwq", "dwk"), out, wants) if w}, **({"workspace": workspace} if wants[2] or wants[3] else {}))
+    _need_heads("dXq", out[0], shapes[0], Xq.dtype, optional=True)
+    _need_heads("dXk", out[1], shapes[1], Xq.dtype, optional=True)
+    _need("dwq", out[2], (d,), (Xq.dtype,), optional=True)
+    _need("dwk", out[3], (d,), (Xq.dtype,), optional=True)
+    _on_device(Xq=Xq, Xk=Xk, wq=wq, wk=wk, dQ=dQ, dK=dK, positions=positions, inv_freq=inv_freq, dXq=out[0], dXk=out[1], dwq=out[2], dwk=out[3],
+               workspace=workspace)
+    given = [t for t in out if t is not None]
+    out = [torch.empty(s, dtype=Xq.dtype, device=Xq.device) if w and t is None else t for t, s, w in zip(out, shapes, wants)]
+    ws, ws_bytes = _scratch(workspace, sphattn_head_norm_rotary_bwd_workspace_bytes(d), Xq) if wants[2] or wants[3] else (None, 0)
+    _raise_on(lib.sphattn_head_norm_rotary_bwd(_heads_of(Xq, True), _heads_of(Xk, True), _ptr(wq), _ptr(wk), _heads_of(dQ, False), _heads_of(dK, False),
+                                               _heads_of(out[0], True), _heads_of(out[1], True), _ptr(out[2]), _ptr(out[3]),
+                                               None if rotary is None else ctypes.byref(rotary), B, N, Hq, Hk, d, int(bool(norm)), eps, code, _ptr(ws),
+                                               ws_bytes, _stream_of(Xq, stream)))
+    for t in given:
+        if not t.is_inference():
+            torch.autograd.graph.increment_version(t)
+    return tuple(out)

@@ -5,6 +5,7 @@
     O.sum().backward()                        # dQ, dK, dV from sphattn_bwd / sphattn_grn_bwd
 
     X = token_embedding(tokens, table, mult, scale)      # rows of a table, scaled
+    Q, K = head_norm_rotary(Xq, Xk, wq, wk, positions, inv_freq)      # norms of heads, rotated by positions, as the attention reads them
     loss = vocab_cross_entropy(X, W, targets)            # -log softmax(X W^T)[targets], no logits in memory
 
 Forward = sphattn_fwd_z (O and the row aggregates z, which the backward needs), or
@@ -17,7 +18,7 @@ import torch
 from torch.autograd.function import once_differentiable
 
 from . import (REDUCTIONS, _cross_fwd_z, _fast_calls, sphattn_bwd, sphattn_embed_bwd, sphattn_embed_fwd, sphattn_fwd_z, sphattn_grn_bwd,
-               sphattn_vocab_loss_bwd, sphattn_vocab_loss_fwd)
+               sphattn_head_norm_rotary_bwd, sphattn_head_norm_rotary_fwd, sphattn_vocab_loss_bwd, sphattn_vocab_loss_fwd)
 
 _DTYPES = {torch.bfloat16: "bf16", torch.float16: "f16"}
 
@@ -116,3 +117,32 @@ def vocab_cross_entropy(X, W, targets, scale=1.0, reduction="mean"):
         if done is not None:
             return done
     return _VocabCrossEntropy.apply(X, W, targets, scale, reduction)
+
+
+class _HeadNormRotary(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, Xq, Xk, wq, wk, positions, inv_freq, sections, interleaved, norm, eps):
+        rows = lambda t: t if t is None or t.stride(-1) == 1 else t.contiguous()
+        Xq, Xk, wq, wk = rows(Xq), rows(Xk), *(None if w is None else w.contiguous() for w in (wq, wk))
+        ctx.rotary = (positions, inv_freq, sections, interleaved, norm, eps)
+        Q, K = sphattn_head_norm_rotary_fwd(Xq, Xk, wq, wk, *ctx.rotary)
+        ctx.save_for_backward(Xq, Xk, wq, wk, positions, inv_freq)
+        ctx.rotary = (sections, interleaved, norm, eps)
+        return Q, K
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dQ, dK):
+        Xq, Xk, wq, wk, positions, inv_freq = ctx.saved_tensors
+        rows = lambda t: t if t is None or t.stride(-1) == 1 else t.contiguous()
+        need = ctx.needs_input_grad
+        grads = sphattn_head_norm_rotary_bwd(Xq, Xk, wq, wk, rows(dQ), rows(dK) if Xk is not None else None, positions, inv_freq, *ctx.rotary,
+                                             want_dX=need[:2], want_dw=need[2:4])
+        return *grads, None, None, None, None, None, None
+
+
+def head_norm_rotary(Xq, Xk=None, wq=None, wk=None, positions=None, inv_freq=None, sections=None, interleaved=False, norm=True, eps=1e-6):
+    """Differentiable norms of queries Xq [B,N,Hq,d] and keys Xk [B,N,Hk,d] (or None) for each head, times wq and wk [d], rotated by their
+    positions, laid out for spherical_attention: (Q [B,Hq,N,d], K [B,Hk,N,d] or None).  Xq and Xk may be slices of one projection's
+    output.  Arguments as sphattn_head_norm_rotary_fwd; no gradients of positions and inv_freq."""
+    return _HeadNormRotary.apply(Xq, Xk, wq, wk, positions, inv_freq, sections, interleaved, norm, eps)

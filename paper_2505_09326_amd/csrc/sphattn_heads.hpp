@@ -1,0 +1,316 @@
+// Norms of queries and keys for each head and the rotation by their positions, in one pass, for gfx950.
+//
+//   r = 1 / sqrt(mean(x^2) + eps)      y = x r w      o = R y      R turns each pair of dimensions by position times frequency
+//   dy = R^T do      dw = sum dy x r      dx = r (dy w - x r mean(dy w x r))
+//
+// Bound by memory: every row is read and written once (backward: two read, one written).  A row is d elements on d / 8 lanes, a lane
+// holding four neighbouring dimensions of each half, so that both kinds of pairs lie in one lane and a rotation exchanges nothing between lanes.
+// cos and sin are formed once per token and lane, for all heads that the lane's group of lanes takes of that token.
+#pragma once
+#include "sphattn_store.hpp"
+
+namespace sphattn {
+
+struct HeadRows { unsigned char* data; long long batch, token, head; };   // strides in bytes
+
+struct HeadSide {
+    HeadRows x, o, dx;                             // backward: o is the gradient that comes in
+    const void* w;
+    int heads;
+};
+
+struct HeadsArgs {
+    HeadSide side[2];                              // queries, keys
+    const void* positions; int id_bytes; long long pos_axis, pos_batch;
+    const float* inv_freq; int until[2];           // frequencies below until[0] go by the first axis, below until[1] by the second, the rest by the third
+    int interleaved, norm;
+    float eps;
+    int B, N, share;                               // groups of lanes that share a token's heads
+    float* partial;                                // backward: [workgroups][2][d] sums of dw, or NULL
+};
+
+constexpr int kHeadsThreads = 256;
+constexpr int kHeadsMostGroups = 1024;             // backward: workgroups, each with a sum of dw for the joining kernel
+
+// The sum over D / 8 neighbouring lanes, in each of them: exchanges within a row of sixteen lanes, no LDS
+template <int D>
+__device__ __forceinline__ float sum_over_row(float x)
+{
+    auto add = [&](auto ctrl) { x += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctrl)::value, 0xf, 0xf, true)); };
+    add(std::integral_constant<int, 0xB1>{});      // lane ^ 1
+    add(std::integral_constant<int, 0x4E>{});      // lane ^ 2
+    add(std::integral_constant<int, 0x141>{});     // the other four of eight
+    if constexpr (D == 128) add(std::integral_constant<int, 0x140>{});    // the other eight of sixteen
+    return x;
+}
+
+// Four neighbouring elements.  (aligned to an element: the memory pipe takes them in one access all the same)
+template <Store S> struct Four { int w[S == Store::F32 ? 4 : 2]; };
+
+template <Store S> __device__ __forceinline__ Four<S> load4(const unsigned char* p)
+{
+    Four<S> f;
+    __builtin_memcpy(&f, p, sizeof(f));
+    return f;
+}
+template <Store S> __device__ __forceinline__ void widen4(const Four<S>& f, float* x)
+{
+    if constexpr (S == Store::F32) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = __builtin_bit_cast(float, f.w[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            if constexpr (S == Store::Bf16) {
+                x[2 * i] = __builtin_bit_cast(float, f.w[i] << 16);
+                x[2 * i + 1] = __builtin_bit_cast(float, f.w[i] & (int)0xffff0000);
+            } else {
+                const f16x2 h = __builtin_bit_cast(f16x2, f.w[i]);
+                x[2 * i] = (float)h[0];
+                x[2 * i + 1] = (float)h[1];
+            }
+        }
+    }
+}
+template <Store S> __device__ __forceinline__ void store4(unsigned char* p, const float* x)
+{
+    Four<S> f;
+#pragma unroll
+    for (int i = 0; i < (S == Store::F32 ? 4 : 2); ++i) {
+        if constexpr (S == Store::F32) f.w[i] = __builtin_bit_cast(int, x[i]);
+        else f.w[i] = pack2<S == Store::F16>(x[2 * i], x[2 * i + 1]);
+    }
+    __builtin_memcpy(p, &f, sizeof(f));
+}
+
+// A row's eight dimensions of this lane: 0..3 of the first half, 4..7 of the second
+template <Store S, int D> struct HeadRow { Four<S> lo, hi; };
+template <Store S, int D> __device__ __forceinline__ HeadRow<S, D> load_row(const unsigned char* p, int l)
+{
+    constexpr int E = store_bytes<S>();
+    return HeadRow<S, D>{load4<S>(p + 4 * l * E), load4<S>(p + (D / 2 + 4 * l) * E)};
+}
+template <Store S, int D> __device__ __forceinline__ void widen_row(const HeadRow<S, D>& r, float (&x)[8])
+{
+    widen4<S>(r.lo, x);
+    widen4<S>(r.hi, x + 4);
+}
+template <Store S, int D> __device__ __forceinline__ void store_row(unsigned char* p, int l, const float (&x)[8])
+{
+    constexpr int E = store_bytes<S>();
+    store4<S>(p + 4 * l * E, x);
+    store4<S>(p + (D / 2 + 4 * l) * E, x + 4);
+}
+
+// Pairs of a lane's eight dimensions: (i, 4 + i), or neighbours.  `back`: turned the other way.
+__device__ __forceinline__ void rotate(float (&x)[8], const float (&cos)[4], const float (&sin)[4], bool interleaved, float back)
+{
+    float y[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int a0 = i, b0 = 4 + i, a1 = 2 * i, b1 = 2 * i + 1;
+        const float a = interleaved ? x[a1] : x[a0], b = interleaved ? x[b1] : x[b0], s = sin[i] * back;
+        const float ta = __builtin_fmaf(a, cos[i], -b * s), tb = __builtin_fmaf(b, cos[i], a * s);
+        y[i] = ta;
+        y[4 + i] = tb;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[i] = interleaved ? (i & 1 ? y[4 + i / 2] : y[i / 2]) : y[i];
+        x[4 + i] = interleaved ? (i & 1 ? y[4 + 2 + i / 2] : y[2 + i / 2]) : y[4 + i];
+    }
+}
+
+// What a lane keeps for all rows: frequencies in turns per position, axes, weights
+template <Store S, int D>
+struct HeadsLane {
+    double turns[4];
+    int axis[4];
+    float w[2][8];
+
+    __device__ __forceinline__ void begin(const HeadsArgs& a, int l)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int f = !a.interleaved ? 4 * l + i : i < 2 ? 2 * l + i : D / 4 + 2 * l + i - 2;
+            turns[i] = a.positions ? (double)a.inv_freq[f] * 0.15915494309189533577 : 0.0;
+            axis[i] = f < a.until[0] ? 0 : f < a.until[1] ? 1 : 2;
+        }
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            if (a.side[s].w) {
+                const HeadRow<S, D> r = load_row<S, D>((const unsigned char*)a.side[s].w, l);
+                widen_row<S, D>(r, w[s]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) w[s][i] = 1.f;
+            }
+        }
+    }
+    // The fraction of a turn is taken in fp64: position times frequency is exact there up to 2^29, and what fp32 would leave of
+    // an angle of a far position is no angle any more.
+    __device__ __forceinline__ void angles(const HeadsArgs& a, long long b, long long n, float (&cos)[4], float (&sin)[4]) const
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const long long at = axis[i] * a.pos_axis + b * a.pos_batch + n;
+            const double p = a.id_bytes == 4 ? (double)((const int*)a.positions)[at] : (double)((const long long*)a.positions)[at];
+            const double t = p * turns[i];
+            sincospif(2.f * (float)(t - __builtin_rint(t)), &sin[i], &cos[i]);
+        }
+    }
+};
+
+// Groups of d / 8 lanes take tokens, or (share > 1, where tokens are few) every share-th head of one.
+template <Store S, int D, bool ROTATE>
+__global__ __launch_bounds__(kHeadsThreads)
+void heads_fwd_kernel(HeadsArgs a)
+{
+    constexpr int LANES = D / 8, AHEAD = 4;
+    const int l = threadIdx.x % LANES;
+    HeadsLane<S, D> lane;
+    lane.begin(a, l);
+    const long long units = (long long)a.B * a.N * a.share, step = (long long)gridDim.x * (kHeadsThreads / LANES);
+    for (long long u = (long long)blockIdx.x * (kHeadsThreads / LANES) + threadIdx.x / LANES; u < units; u += step) {
+        const long long token = u / a.share, b = token / a.N, n = token - b * a.N;
+        const int first = (int)(u - token * a.share);
+        float cos[4], sin[4];
+        if constexpr (ROTATE) lane.angles(a, b, n, cos, sin);
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const HeadSide& side = a.side[s];
+            const unsigned char* from = side.x.data + b * side.x.batch + n * side.x.token;
+            unsigned char* to = side.o.data + b * side.o.batch + n * side.o.token;
+            for (int h0 = first; h0 < side.heads; h0 += AHEAD * a.share) {
+                HeadRow<S, D> rows[AHEAD];
+#pragma unroll
+                for (int i = 0; i < AHEAD; ++i) rows[i] = load_row<S, D>(from + min(h0 + i * a.share, side.heads - 1) * side.x.head, l);
+#pragma unroll
+                for (int i = 0; i < AHEAD; ++i) {
+                    const int h = h0 + i * a.share;
+                    float x[8];
+                    widen_row<S, D>(rows[i], x);
+                    float r = 1.f;
+                    if (a.norm) {
+                        float ss = 0.f;
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) ss = __builtin_fmaf(x[k], x[k], ss);
+                        r = 1.f / __builtin_sqrtf(__builtin_fmaf(sum_over_row<D>(ss), 1.f / D, a.eps));
+                    }
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) x[k] = x[k] * r * lane.w[s][k];
+                    if constexpr (ROTATE) rotate(x, cos, sin, a.interleaved, 1.f);
+                    if (h < side.heads) store_row<S, D>(to + h * side.o.head, l, x);
+                }
+            }
+        }
+    }
+}
+
+template <Store S, int D, bool ROTATE>
+__global__ __launch_bounds__(kHeadsThreads)
+void heads_bwd_kernel(HeadsArgs a)
+{
+    constexpr int LANES = D / 8, AHEAD = 2;
+    const int l = threadIdx.x % LANES;
+    HeadsLane<S, D> lane;
+    lane.begin(a, l);
+    float dw[2][8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) dw[0][k] = dw[1][k] = 0.f;
+    const long long units = (long long)a.B * a.N * a.share, step = (long long)gridDim.x * (kHeadsThreads / LANES);
+    for (long long u = (long long)blockIdx.x * (kHeadsThreads / LANES) + threadIdx.x / LANES; u < units; u += step) {
+        const long long token = u / a.share, b = token / a.N, n = token - b * a.N;
+        const int first = (int)(u - token * a.share);
+        float cos[4], sin[4];
+        if constexpr (ROTATE) lane.angles(a, b, n, cos, sin);
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const HeadSide& side = a.side[s];
+            const unsigned char* from = side.x.data + b * side.x.batch + n * side.x.token;
+            const unsigned char* grad = side.o.data + b * side.o.batch + n * side.o.token;
+            unsigned char* to = side.dx.data ? side.dx.data + b * side.dx.batch + n * side.dx.token : nullptr;
+            for (int h0 = first; h0 < side.heads; h0 += AHEAD * a.share) {
+                HeadRow<S, D> rows[AHEAD], grads[AHEAD];
+#pragma unroll
+                for (int i = 0; i < AHEAD; ++i) {
+                    const int h = min(h0 + i * a.share, side.heads - 1);
+                    rows[i] = load_row<S, D>(from + h * side.x.head, l);
+                    grads[i] = load_row<S, D>(grad + h * side.o.head, l);
+                }
+#pragma unroll
+                for (int i = 0; i < AHEAD; ++i) {
+                    const int h = h0 + i * a.share;
+                    float x[8], dy[8];
+                    widen_row<S, D>(rows[i], x);
+                    widen_row<S, D>(grads[i], dy);
+                    if constexpr (ROTATE) rotate(dy, cos, sin, a.interleaved, -1.f);
+                    float r = 1.f, along = 0.f;
+                    if (a.norm) {
+                        float ss = 0.f;
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) ss = __builtin_fmaf(x[k], x[k], ss);
+                        r = 1.f / __builtin_sqrtf(__builtin_fmaf(sum_over_row<D>(ss), 1.f / D, a.eps));
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            x[k] *= r;
+                            along = __builtin_fmaf(dy[k] * lane.w[s][k], x[k], along);
+                        }
+                        along = sum_over_row<D>(along) * (1.f / D);
+                    }
+                    if (h >= side.heads) continue;
+                    float dx[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        dw[s][k] = __builtin_fmaf(dy[k], x[k], dw[s][k]);
+                        const float dn = dy[k] * lane.w[s][k];
+                        dx[k] = a.norm ? r * __builtin_fmaf(-x[k], along, dn) : dn;
+                    }
+                    if (to) store_row<S, D>(to + h * side.dx.head, l, dx);
+                }
+            }
+        }
+    }
+    if (!a.partial) return;
+    // the workgroup's sums: over the groups of lanes of a wave, then over the waves
+    constexpr int WAVES = kHeadsThreads / 64;
+    __shared__ float sums[WAVES][2][D];
+    const int wave = threadIdx.x >> 6, in = threadIdx.x & 63;
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            float x = dw[s][k];
+#pragma unroll
+            for (int m = LANES; m < 64; m <<= 1) x += __shfl_xor(x, m);
+            if (in < LANES) sums[wave][s][(k < 4 ? 0 : D / 2) + 4 * l + (k & 3)] = x;
+        }
+    __syncthreads();
+    if ((int)threadIdx.x < 2 * D) {
+        const float* at = &sums[0][0][0] + threadIdx.x;
+        float x = 0.f;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) x += at[w * 2 * D];
+        a.partial[(size_t)blockIdx.x * 2 * D + threadIdx.x] = x;
+    }
+}
+
+// dw from the workgroups' sums: a workgroup takes sixteen columns, 16 lanes' worth of rows at a time
+template <Store S>
+__global__ __launch_bounds__(1024)
+void heads_dw_kernel(const float* __restrict__ partial, int groups, int D, void* __restrict__ dwq, void* __restrict__ dwk)
+{
+    __shared__ float shared[64][16];
+    const int col = (int)blockIdx.x * 16 + (threadIdx.x & 15), row = threadIdx.x >> 4;
+    float x = 0.f;
+    for (int g = row; g < groups; g += 64) x += partial[(size_t)g * 2 * D + col];
+    shared[row][threadIdx.x & 15] = x;
+    __syncthreads();
+    if (threadIdx.x >= 16) return;
+    x = 0.f;
+    for (int r = 0; r < 64; ++r) x += shared[r][threadIdx.x];
+    void* out = col < D ? dwq : dwk;
+    if (out) store_el<S>(out, col < D ? col : col - D, x);
+}
+
+}  // namespace sphattn

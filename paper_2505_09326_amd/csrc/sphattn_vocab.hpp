@@ -29,7 +29,7 @@
 // Up to 64 rows, where reading W is most of the time, use fp32 matrix instructions on fp32 as it is: RowsProduct.
 #pragma once
 #include "sphattn_embed.hpp"
-#include "sphattn_pipelined.hpp"
+#include "sphattn_tiles.hpp"
 
 #include <type_traits>
 
@@ -43,238 +43,9 @@ struct VocabInfo {
     int even;                                      // one gradient per row, fp16: all of them within 2^4 of the largest, so that one `up` serves every row
 };
 
-constexpr float kLowPart = 4096.f;                 // what the second fp16 part is multiplied by: below 2^-14 that type has fewer bits
 constexpr int kEndless = 1 << 20;                  // in place of the power of two of a row with an infinite element
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
-
-// ---- tile products -------------------------------------------------------------------------------------
-
-// out[q][p] = sum_k P[p][k] Q[q][k].  An operand is stored with rows along k ("across": row k holds all p) or with
-// rows of k.  P's index lies along a lane's registers, Q's along the lanes.
-struct Operand {
-    const unsigned char* data;                     // 16-byte aligned
-    long long part;                                // bytes from one part to the next (fp32)
-    int ld;                                        // bytes per row, a multiple of 16
-    int size;                                      // valid p or q (across: columns, a multiple of 8)
-};
-
-template <int BP_, int BQ_, int WAVES_P_, int WAVES_Q_, int NBUF_>
-struct Tile {
-    static constexpr int BP = BP_, BQ = BQ_, WAVES_P = WAVES_P_, WAVES_Q = WAVES_Q_, NBUF = NBUF_;
-    static constexpr int WAVES = WAVES_P * WAVES_Q, THREADS = 64 * WAVES;
-    static constexpr int FP = BP / WAVES_P / 16, FQ = BQ / WAVES_Q / 16;      // fragments of a wave
-    // 1 KB copies per wave and step; where there are fewer blocks than waves several copy the same one (the same bytes)
-    static constexpr int CP = BP / 16 / WAVES, CQ = (BQ / 16 + WAVES - 1) / WAVES, COPIES = CP + CQ;
-    static constexpr int BUF = (BP + BQ) * 64, LDS = NBUF * BUF;
-    static_assert(CP * WAVES * 16 == BP && (CQ * WAVES * 16 == BQ || CQ == 1), "");
-};
-constexpr int kStepK = 32;
-
-// place of 16-byte piece c in row k of an operand stored across, and the piece in place c
-__device__ __forceinline__ int across_slot(int k, int c) { return c ^ (2 * ((k & 3) | (k >> 1 & 4))); }
-
-// Tiles of 256 x 256 on eight waves of 128 x 64: an operand byte in LDS feeds four or eight matrix instructions, 0.4 LDS reads per instruction (0.75
-// transposed), and 128 KB of LDS hold four steps.
-// The sum over k runs in steps of 32.  A step's part of the two operands is BP / 16 + BQ / 16 blocks of 1 KB, copied
-// straight into one of NBUF LDS buffers, NBUF - 1 steps ahead; a step's fragments are read from LDS while the matrix
-// instructions of the step before run, so that behind the one barrier per step the matrix pipe has its operands already.
-template <class T, bool HALF, bool PX, bool QX, int PAIRS>
-struct Product {
-    f32x4 acc[T::FP][T::FQ];
-
-    __device__ __forceinline__ void run(const Operand& P, const Operand& Q, int p0, int q0, int k0, int k_end,
-                                        SPH_LDS unsigned char* smem)
-    {
-        const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-        const int n16 = lane & 15, g = lane >> 4;
-        const int wp = wave % T::WAVES_P, wq = wave / T::WAVES_P;
-        const uint32_t lds0 = (uint32_t)(uintptr_t)smem;
-        const int steps = (k_end - k0 + kStepK - 1) / kStepK;
-        const int total = steps * PAIRS;
-
-        // A copy's lane: rows of k lie in blocks of 16 x 64 bytes, lane l on row l / 4 with the piece of its slot.  Across, the buffer
-        // holds 32 whole rows of the tile, so that a copy fetches whole lines of memory, their 16-byte pieces exchanged by
-        // row (across_slot) so that the transposing reads of eight rows fall on different banks.
-        const int row = lane >> 2, piece = block_piece_in_slot(lane);
-        int voff[T::COPIES];
-        uint32_t at[T::COPIES];                    // place in a buffer
-        auto place = [&](bool across, const Operand& A, int a0, int size, int b, int& v) {
-            if (!across) v = (b * 16 + row) * A.ld + piece * 16;
-            else {
-                const int slots = size / 8, k = (b * 64 + lane) / slots, col = a0 + across_slot(k, lane % slots) * 8;
-                v = col < A.size ? k * A.ld + col * 2 : 0x7fffffff;
-            }
-        };
-#pragma unroll
-        for (int i = 0; i < T::COPIES; ++i) {
-            const int b = i < T::CP ? wave * T::CP + i : (wave * T::CQ + (i - T::CP)) % (T::BQ / 16);
-            place(i < T::CP ? PX : QX, i < T::CP ? P : Q, i < T::CP ? p0 : q0, i < T::CP ? T::BP : T::BQ, b, voff[i]);
-            at[i] = (i < T::CP ? 0 : T::BP * 64) + b * 1024;
-        }
-        // where the next step's part begins, and (rows of k) how many bytes or (across) how many rows are left.  All of it in
-        // scalar registers, which have no 64-bit comparisons.
-        struct Stream { const unsigned char* base; int left; };
-        auto start = [&](bool across, const Operand& A, int a0, int size, int part) {
-            const int rows = min(size, A.size - a0);
-            return across ? Stream{A.data + part * A.part + (long long)k0 * A.ld, k_end - k0}
-                          : Stream{A.data + part * A.part + (long long)a0 * A.ld + (long long)k0 * 2, rows * A.ld - k0 * 2};
-        };
-        // parts of P and Q by pair, small products first: (1,0) (0,1) (0,0), or of three parts (2,0) (0,2) (1,1) (1,0) (0,1) (0,0)
-        static_assert(PAIRS == 1 || PAIRS == 3 || PAIRS == 6, "");
-        int pair = 0, step = 0, copied = 0;        // of the next copies
-        auto part_p = [&]() { return PAIRS == 3 ? pair == 0 : PAIRS == 6 ? (pair == 0 ? 2 : pair == 2 || pair == 3) : 0; };
-        auto part_q = [&]() { return PAIRS == 3 ? pair == 1 : PAIRS == 6 ? (pair == 1 ? 2 : pair == 2 || pair == 4) : 0; };
-        Stream sp = start(PX, P, p0, T::BP, part_p()), sq = start(QX, Q, q0, T::BQ, part_q());
-        uint32_t to = lds0;
-        auto words = [&](bool across, const Operand& A, const Stream& s, bool there) {
-            const int left = there ? max(s.left, 0) : 0;
-            return rsrc_words(s.base, (uint32_t)__builtin_amdgcn_readfirstlane(across ? min(left, kStepK) * A.ld : left));
-        };
-        // of the step that is copied next
-        i32x4 rp, rq;
-        bool past = false;
-        auto copy_begin = [&]() {
-            const bool there = copied < total;
-            rp = words(PX, P, sp, there);
-            rq = words(QX, Q, sq, there);
-            past = k0 * 2 + step * 64 + piece * 16 >= k_end * 2;   // pieces behind the end of the sum are zeros
-        };
-        auto copy_one = [&](int i) {
-            const bool across = i < T::CP ? PX : QX;
-            copy_to_lds(i < T::CP ? rp : rq, to + at[i], !across && past ? 0x7fffffff : voff[i], 0);
-        };
-        auto copy_end = [&]() {
-            ++copied;
-            ++step;
-            to = to == lds0 + (T::NBUF - 1) * T::BUF ? lds0 : to + T::BUF;
-            sp.base += PX ? (long long)kStepK * P.ld : 64;
-            sp.left -= PX ? kStepK : 64;
-            sq.base += QX ? (long long)kStepK * Q.ld : 64;
-            sq.left -= QX ? kStepK : 64;
-            if (PAIRS > 1 && step == steps && copied < total) {
-                step = 0;
-                ++pair;
-                sp = start(PX, P, p0, T::BP, part_p());
-                sq = start(QX, Q, q0, T::BQ, part_q());
-            }
-        };
-        auto copy_step = [&]() {
-            copy_begin();
-#pragma unroll
-            for (int i = 0; i < T::COPIES; ++i) copy_one(i);
-            copy_end();
-        };
-
-        i32x4 pf[T::FP], qf[2][T::FQ];
-        auto fragment = [&](bool across, const SPH_LDS unsigned char* block0, int size, int i) -> i32x4 {
-            if (!across) return lds_read_b128(block0 + i * 1024 + block_piece_offset(n16, g));
-            // lane (i, g): rows 8 g + i / 4 and 4 more, columns 4 (i % 4) .. + 3 of the sixteen
-            const int k = 8 * g + (n16 >> 2), at = across_slot(k, 2 * i + ((lane >> 1) & 1)) * 16 + (lane & 1) * 8;
-            const SPH_LDS unsigned char* b = block0 + k * size * 2 + at;
-            const i32x2 lo = lds_read_tr64(b), hi = lds_read_tr64(b + 4 * size * 2);   // (rows k and k + 4 exchange alike)
-            return i32x4{lo[0], lo[1], hi[0], hi[1]};
-        };
-        auto read_p = [&](uint32_t from, int i) {
-            pf[i] = fragment(PX, smem + from + (PX ? 0 : wp * T::FP * 1024), T::BP, PX ? wp * T::FP + i : i);
-        };
-        auto read_q = [&](uint32_t from, int set, int j) {
-            qf[set][j] = fragment(QX, smem + from + T::BP * 64 + (QX ? 0 : wq * T::FQ * 1024), T::BQ, QX ? wq * T::FQ + j : j);
-        };
-        auto behind = [](uint32_t from) { return from == (T::NBUF - 1) * T::BUF ? 0u : from + T::BUF; };
-        constexpr int VM = (T::NBUF - 3) * T::COPIES;   // copies that may still be under way when the next step's have to be there
-        static_assert(T::NBUF >= 3 && VM < 64, "");
-        auto arrive = [&]() {
-            asm volatile("" ::: "memory");
-            __builtin_amdgcn_s_waitcnt(0x0F70 | (VM & 15) | ((VM >> 4) << 14));
-            __builtin_amdgcn_s_barrier();
-            asm volatile("" ::: "memory");
-        };
-
-#pragma unroll
-        for (int i = 0; i < T::FP; ++i)
-#pragma unroll
-            for (int j = 0; j < T::FQ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-        // (every step is copied, those past the last one as zeros, which add nothing: the loop takes two at a time)
-#pragma unroll
-        for (int s = 0; s < T::NBUF - 2; ++s) copy_step();
-        copy_step();
-        {
-            constexpr int VM0 = (T::NBUF - 2) * T::COPIES;
-            static_assert(VM0 < 64, "");
-            asm volatile("" ::: "memory");
-            __builtin_amdgcn_s_waitcnt(0x0F70 | (VM0 & 15) | ((VM0 >> 4) << 14));
-            __builtin_amdgcn_s_barrier();
-            asm volatile("" ::: "memory");
-        }
-        uint32_t from = 0;                         // buffer of step s
-#pragma unroll
-        for (int j = 0; j < T::FQ; ++j) read_q(from, 0, j);
-#pragma unroll
-        for (int i = 0; i < T::FP - 1; ++i) read_p(from, i);
-        for (int s = 0; s < total; s += 2) {
-            // of three products the first two have a second part, 2^12 times as large as it is: an even number of steps, after which the sums are brought back
-            if (PAIRS == 3 && s == 2 * steps) {
-#pragma unroll
-                for (int i = 0; i < T::FP; ++i)
-#pragma unroll
-                    for (int j = 0; j < T::FQ; ++j) acc[i][j] *= 1.f / kLowPart;
-            }
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                arrive();                          // step s + u + 1 is there; the fragments of step s + u - 1 are used up
-                copy_begin();                      // into that one's buffer
-                const uint32_t next = behind(from);
-                // One P fragment with all of Q at a time, and beside these products a share of the step's copies and of the reads for the
-                // next one.  All copies behind the barrier would queue at the memory pipe, eight waves' at once, and the products
-                // behind them in the program with them; left to itself the compiler also puts a read right before the product that
-                // needs it.  A P fragment is used up when its products are done and makes place for the next step's (the last
-                // one's place is taken a step later); Q's are needed to the end and have two sets.
-#pragma unroll
-                for (int i = 0; i < T::FP; ++i) {
-#pragma unroll
-                    for (int c = i * T::COPIES / T::FP; c < (i + 1) * T::COPIES / T::FP; ++c) copy_one(c);
-                    if (i == 0) read_p(from, T::FP - 1);
-                    else read_p(next, i - 1);
-                    const int q0f = i * T::FQ / T::FP, q1f = (i + 1) * T::FQ / T::FP;
-#pragma unroll
-                    for (int j = q0f; j < q1f; ++j) read_q(next, u ^ 1, j);
-#pragma unroll
-                    for (int j = 0; j < T::FQ; ++j) {   // to and fro: one operand changes at a time
-                        const int jj = i & 1 ? T::FQ - 1 - j : j;
-                        acc[i][jj] = mfma16x16<HALF>(pf[i], qf[u][jj], acc[i][jj]);
-                    }
-                    const int reads = (PX ? 2 : 1) + (q1f - q0f) * (QX ? 2 : 1);
-#pragma unroll
-                    for (int j = 0; j < T::FQ; ++j) {
-                        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-                        if (j < reads) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-                    }
-                    __builtin_amdgcn_sched_barrier(0);
-                }
-                copy_end();
-                from = next;
-            }
-        }
-        asm volatile("" ::: "memory");
-        __builtin_amdgcn_s_waitcnt(0x0070);        // vmcnt(0), lgkmcnt(0): nothing of this lands in what follows
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-    }
-};
-
-// Workgroup -> tile.  Each XCD takes a contiguous range; within it, groups of eight q tiles are walked p by p, so that the
-// workgroups that run together share operand panels in the XCD's L2.
-struct TileAt { int p, q, slice; };
-__device__ __forceinline__ TileAt tile_of(int id, int tiles_p, int tiles_q)
-{
-    constexpr int GROUP = 8;
-    const int per_slice = tiles_p * tiles_q, slice = id / per_slice;
-    id -= slice * per_slice;
-    const int per_group = GROUP * tiles_p, group = id / per_group, in = id - group * per_group;
-    const int rows = min(GROUP, tiles_q - group * GROUP);
-    return TileAt{in / rows, group * GROUP + in % rows, slice};
-}
 
 struct VocabArgs {
     Operand P, Q;
@@ -504,60 +275,6 @@ void vocab_rows_dw_kernel(VocabArgs a)
             if (wide) store16<Store::F32, true>(a.out, at, __builtin_bit_cast(i32x4, o), 4);
             else store16<Store::F32, false>(a.out, at, __builtin_bit_cast(i32x4, o), left);
         }
-}
-
-// A value (2^15 at most) as two fp16 parts.  NaN: in the first.
-__device__ __forceinline__ void split2(float x, _Float16& hi, _Float16& lo)
-{
-    hi = (_Float16)x;
-    lo = (_Float16)((x - (float)hi) * kLowPart);
-    if (__builtin_fabsf(x) == __builtin_inff() || x != x) lo = (_Float16)0.f;
-}
-
-// Four neighbouring values' parts
-__device__ __forceinline__ void split2(const float (&x)[4], i32x2& hi, i32x2& lo)
-{
-#pragma unroll
-    for (int r = 0; r < 2; ++r) {
-        _Float16 a, b, c, d;
-        split2(x[2 * r], a, b);
-        split2(x[2 * r + 1], c, d);
-        hi[r] = __builtin_bit_cast(int, f16x2{a, c});
-        lo[r] = __builtin_bit_cast(int, f16x2{b, d});
-    }
-}
-
-// Four neighbouring values as three bf16 parts that are them (8 + 8 + 8 bits), over the whole range of fp32.  Infinite or NaN: in the first.
-__device__ __forceinline__ void split3(const float (&x)[4], i32x2 (&part)[3])
-{
-    constexpr float MOST = 0x1.fep127f;            // (a finite value is not to be rounded to an infinite one)
-#pragma unroll
-    for (int r = 0; r < 2; ++r) {
-        float left[2];
-        bool finite[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            left[i] = x[2 * r + i];
-            finite[i] = __builtin_fabsf(left[i]) < __builtin_inff();
-        }
-        const int hi = pack2<false>(finite[0] ? fminf(fmaxf(left[0], -MOST), MOST) : left[0], finite[1] ? fminf(fmaxf(left[1], -MOST), MOST) : left[1]);
-        left[0] = finite[0] ? left[0] - __builtin_bit_cast(float, hi << 16) : 0.f;
-        left[1] = finite[1] ? left[1] - __builtin_bit_cast(float, hi & (int)0xffff0000) : 0.f;
-        const int mid = pack2<false>(left[0], left[1]);
-        part[0][r] = hi;
-        part[1][r] = mid;
-        part[2][r] = pack2<false>(left[0] - __builtin_bit_cast(float, mid << 16), left[1] - __builtin_bit_cast(float, mid & (int)0xffff0000));
-    }
-}
-
-// Two accumulator fragments' rows of four 16-bit values, lane group g holding columns 4 g .. 4 g + 3 of each: afterwards group g has
-// columns 8 (g / 2) .. + 7 of fragment g % 2.
-__device__ __forceinline__ i32x4 join_fragments(i32x2 a, i32x2 b)
-{
-    int a0 = a[0], a1 = a[1], b0 = b[0], b1 = b[1];
-    // (odd rows of sixteen lanes of the first operand and even rows of the second change places)
-    asm volatile("s_nop 1\n\tv_permlane16_swap_b32 %0, %2\n\tv_permlane16_swap_b32 %1, %3\n\ts_nop 1" : "+v"(a0), "+v"(a1), "+v"(b0), "+v"(b1));
-    return i32x4{a0, a1, b0, b1};
 }
 
 // whether logits and G are formed from fp32 as it is (RowsProduct)
