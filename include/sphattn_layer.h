@@ -60,6 +60,35 @@ int sphattn_head_norm_rotary_bwd(const sphattn_heads* Xq, const sphattn_heads* X
                                  const sphattn_heads* dXq, const sphattn_heads* dXk, void* dwq, void* dwk, const sphattn_rotary* rotary,
                                  int B, int N, int Hq, int Hk, int d, int norm, float eps, int dtype, void* workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * The gated feed-forward product of a layer:  H = act(X Wg^T) * (X Wu^T)
+ *   X : [T,D], Wg, Wu : [F,D], H : [T,F], contiguous, of one type.  Sums and act in fp32, rounded once.
+ *   act: silu a / (1 + e^-a), gelu a Phi(a) (with the normal distribution's Phi), relu max(a, 0).
+ * SPHATTN_F32 with more than 64 rows: the factors to 2^-23 on average and 2^-22 at most, those below 2^-29 of their row's largest element to 2^-51 of
+ * that; terms off by 3/4 2^-20 at most.  T <= 2^20 (0: nothing is done), 1 <= D <= 65536, 1 <= F <= 2^18, T F <= 2^36 (SPHATTN_ERR_SHAPE); gate a sphattn_gate
+ * (SPHATTN_ERR_VALUE).  Outputs overlap neither each other nor inputs nor the workspace (SPHATTN_ERR_ALIAS).
+ *   workspace : at least sphattn_gated_ffn_workspace_bytes(T, D, F, dtype) bytes (0 for sizes that the call would reject, and where it needs
+ *               none: it may be NULL then).
+ */
+typedef enum { SPHATTN_GATE_SILU = 0, SPHATTN_GATE_GELU = 1, SPHATTN_GATE_RELU = 2 } sphattn_gate;
+
+size_t sphattn_gated_ffn_workspace_bytes(int T, int D, int F, int dtype);
+int sphattn_gated_ffn_fwd(const void* X, const void* Wg, const void* Wu, void* H, int T, int D, int F, int gate, int dtype,
+                          void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Gradients of that, from its inputs alone (A = X Wg^T and U = X Wu^T are formed again):
+ *   dA = dH U act'(A)    dB = dH act(A)    dX = dA Wg + dB Wu    dWg = dA^T X    dWu = dB^T X        (relu: act'(0) = 0)
+ *   dH : [T,F].  dX : [T,D], dWg, dWu : [F,D]; each may be NULL (not wanted), not all (SPHATTN_ERR_NULL).  T = 0: dWg and dWu are zeros.
+ * dA and dB are rounded once to the storage type (SPHATTN_F32: none; every factor of the sums keeps its 24 bits, terms are off by 2^-24 at
+ * most), sums in fp32, the results rounded once.  fp16: dA and dB are scaled by powers of two, for dX by row and for dW by the largest row, from what
+ * the norms of X's and W's rows and a row's largest dH allow at most: values down to 2^-27 of that keep the type's bits.
+ * SPHATTN_F32: an infinite element of dA, dB, X or W makes NaN of the sums that it is in.
+ */
+size_t sphattn_gated_ffn_bwd_workspace_bytes(int T, int D, int F, int dtype);
+int sphattn_gated_ffn_bwd(const void* X, const void* Wg, const void* Wu, const void* dH, void* dX, void* dWg, void* dWu, int T, int D, int F,
+                          int gate, int dtype, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

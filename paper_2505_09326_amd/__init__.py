@@ -53,6 +53,7 @@ EXPORTED_SYMBOLS = ("sphattn_fwd", "sphattn_fwd_z", "sphattn_fwd_tile_rows", "sp
                     "sphattn_vocab_loss_bwd_workspace_bytes", "sphattn_vocab_loss_bwd",
                     "sphattn_clip_grads_workspace_bytes", "sphattn_clip_grads",
                     "sphattn_head_norm_rotary_fwd", "sphattn_head_norm_rotary_bwd_workspace_bytes", "sphattn_head_norm_rotary_bwd",
+                    "sphattn_gated_ffn_workspace_bytes", "sphattn_gated_ffn_fwd", "sphattn_gated_ffn_bwd_workspace_bytes", "sphattn_gated_ffn_bwd",
                     "sphattn_strerror", "sphattn_version")
 
 NORMALIZERS = {"l2": 0, "softmax": 1, "l1": 2, "sqrelu": 3}
@@ -156,6 +157,14 @@ def load_library() -> ctypes.CDLL:
         lib.sphattn_head_norm_rotary_bwd_workspace_bytes.argtypes = [ip]
         lib.sphattn_head_norm_rotary_bwd.restype = ip
         lib.sphattn_head_norm_rotary_bwd.argtypes = [vp] * 11 + [ip] * 6 + [fl, ip, vp, sz, vp]
+        for name in ("sphattn_gated_ffn_workspace_bytes", "sphattn_gated_ffn_bwd_workspace_bytes"):
+            fn = getattr(lib, name)
+            fn.restype = sz
+            fn.argtypes = [ip] * 4
+        lib.sphattn_gated_ffn_fwd.restype = ip
+        lib.sphattn_gated_ffn_fwd.argtypes = [vp] * 4 + [ip] * 5 + [vp, sz, vp]
+        lib.sphattn_gated_ffn_bwd.restype = ip
+        lib.sphattn_gated_ffn_bwd.argtypes = [vp] * 7 + [ip] * 5 + [vp, sz, vp]
         lib.sphattn_strerror.restype = ctypes.c_char_p
         lib.sphattn_strerror.argtypes = [ip]
         lib.sphattn_version.restype = ip
@@ -1165,4 +1174,67 @@ def sphattn_head_norm_rotary_bwd(Xq, Xk, wq, wk, dQ, dK, positions=None, inv_fre
     for t in given:
         if not t.is_inference():
             torch.autograd.graph.increment_version(t)
+    return tuple(out)
+
+
+GATES = {"silu": 0, "gelu": 1, "relu": 2}
+
+
+def _gated(X, Wg, Wu):
+    T, D = _matrix("X", X)
+    F, _ = _matrix("Wg", Wg)
+    code = _code_of("X", X)
+    _need("X", X, (T, D), (X.dtype,))
+    _need("Wg", Wg, (F, D), (X.dtype,))
+    _need("Wu", Wu, (F, D), (X.dtype,))
+    return T, D, F, code
+
+
+def sphattn_gated_ffn_workspace_bytes(T, D, F, dtype="bf16") -> int:
+    return int(load_library().sphattn_gated_ffn_workspace_bytes(T, D, F, _dtype_code(dtype)))
+
+
+def sphattn_gated_ffn_bwd_workspace_bytes(T, D, F, dtype="bf16") -> int:
+    return int(load_library().sphattn_gated_ffn_bwd_workspace_bytes(T, D, F, _dtype_code(dtype)))
+
+
+def sphattn_gated_ffn_fwd(X, Wg, Wu, activation="silu", H=None, workspace=None, stream=None):
+    """H = act(X Wg^T) * (X Wu^T): X [T,D], Wg and Wu [F,D] (fp32, bf16 or fp16), activation "silu", "gelu" or "relu"; returns H [T,F].  `workspace` is a
+    device byte tensor of at least sphattn_gated_ffn_workspace_bytes(T, D, F, dtype)."""
+    import torch
+    lib = load_library()
+    gate = GATES[activation]
+    T, D, F, code = _gated(X, Wg, Wu)
+    need = lib.sphattn_gated_ffn_workspace_bytes(T, D, F, code)
+    _brought(stream, H=H, **({"workspace": workspace} if need else {}))
+    _on_device(X=X, Wg=Wg, Wu=Wu, H=H, workspace=workspace)
+    if H is None:
+        H = torch.empty((T, F), dtype=X.dtype, device=X.device)
+    _need("H", H, (T, F), (X.dtype,))
+    ws, ws_bytes = _scratch(workspace, need, X) if need else (None, 0)
+    _raise_on(lib.sphattn_gated_ffn_fwd(X.data_ptr(), Wg.data_ptr(), Wu.data_ptr(), H.data_ptr(), T, D, F, gate, code, _ptr(ws), ws_bytes, _stream_of(X, stream)))
+    return H
+
+
+def sphattn_gated_ffn_bwd(X, Wg, Wu, dH, activation="silu", dX=None, dWg=None, dWu=None, want_dX=True, want_dWg=True, want_dWu=True, workspace=None,
+                          stream=None):
+    """Gradients (dX [T,D], dWg [F,D], dWu [F,D]) of sphattn_gated_ffn_fwd for dH [T,F], from its inputs alone; None in the place of what is not wanted
+    (at least one is)."""
+    import torch
+    lib = load_library()
+    gate = GATES[activation]
+    T, D, F, code = _gated(X, Wg, Wu)
+    _need("dH", dH, (T, F), (X.dtype,))
+    wants = (bool(want_dX), bool(want_dWg), bool(want_dWu))
+    if not any(wants):
+        raise ValueError("no gradient is wanted")
+    out = [t if w else None for t, w in zip((dX, dWg, dWu), wants)]
+    _brought(stream, workspace=workspace, **{n: t for n, t, w in zip(("dX", "dWg", "dWu"), out, wants) if w})
+    _on_device(X=X, Wg=Wg, Wu=Wu, dH=dH, dX=out[0], dWg=out[1], dWu=out[2], workspace=workspace)
+    out = [torch.empty_like(x) if w and t is None else t for t, x, w in zip(out, (X, Wg, Wu), wants)]
+    for name, t, shape in zip(("dX", "dWg", "dWu"), out, ((T, D), (F, D), (F, D))):
+        _need(name, t, shape, (X.dtype,), optional=True)
+    ws, ws_bytes = _scratch(workspace, lib.sphattn_gated_ffn_bwd_workspace_bytes(T, D, F, code), X)
+    _raise_on(lib.sphattn_gated_ffn_bwd(X.data_ptr(), Wg.data_ptr(), Wu.data_ptr(), dH.data_ptr(), *(_ptr(t) for t in out), T, D, F, gate, code, ws.data_ptr(),
+                                        ws_bytes, _stream_of(X, stream)))
     return tuple(out)

@@ -6,6 +6,7 @@
 
     X = token_embedding(tokens, table, mult, scale)      # rows of a table, scaled
     Q, K = head_norm_rotary(Xq, Xk, wq, wk, positions, inv_freq)      # norms of heads, rotated by positions, as the attention reads them
+    H = gated_feed_forward(X, Wg, Wu)                    # silu(X Wg^T) * (X Wu^T)
     loss = vocab_cross_entropy(X, W, targets)            # -log softmax(X W^T)[targets], no logits in memory
 
 Forward = sphattn_fwd_z (O and the row aggregates z, which the backward needs), or
@@ -17,8 +18,8 @@ import math
 import torch
 from torch.autograd.function import once_differentiable
 
-from . import (REDUCTIONS, _cross_fwd_z, _fast_calls, sphattn_bwd, sphattn_embed_bwd, sphattn_embed_fwd, sphattn_fwd_z, sphattn_grn_bwd,
-               sphattn_head_norm_rotary_bwd, sphattn_head_norm_rotary_fwd, sphattn_vocab_loss_bwd, sphattn_vocab_loss_fwd)
+from . import (REDUCTIONS, _cross_fwd_z, _fast_calls, sphattn_bwd, sphattn_embed_bwd, sphattn_embed_fwd, sphattn_fwd_z, sphattn_gated_ffn_bwd,
+               sphattn_gated_ffn_fwd, sphattn_grn_bwd, sphattn_head_norm_rotary_bwd, sphattn_head_norm_rotary_fwd, sphattn_vocab_loss_bwd, sphattn_vocab_loss_fwd)
 
 _DTYPES = {torch.bfloat16: "bf16", torch.float16: "f16"}
 
@@ -146,3 +147,29 @@ def head_norm_rotary(Xq, Xk=None, wq=None, wk=None, positions=None, inv_freq=Non
     positions, laid out for spherical_attention: (Q [B,Hq,N,d], K [B,Hk,N,d] or None).  Xq and Xk may be slices of one projection's
     output.  Arguments as sphattn_head_norm_rotary_fwd; no gradients of positions and inv_freq."""
     return _HeadNormRotary.apply(Xq, Xk, wq, wk, positions, inv_freq, sections, interleaved, norm, eps)
+
+
+class _GatedFeedForward(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, X, Wg, Wu, activation):
+        if X.dtype != Wg.dtype or X.dtype != Wu.dtype:
+            raise TypeError(f"X, Wg and Wu must have one dtype, got {X.dtype}, {Wg.dtype} and {Wu.dtype}")
+        ctx.shape, ctx.activation = X.shape, activation
+        X, Wg, Wu = X.reshape(-1, X.shape[-1]).contiguous(), Wg.contiguous(), Wu.contiguous()
+        ctx.save_for_backward(X, Wg, Wu)
+        return sphattn_gated_ffn_fwd(X, Wg, Wu, activation).view(*ctx.shape[:-1], Wg.shape[0])
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dH):
+        X, Wg, Wu = ctx.saved_tensors
+        need = ctx.needs_input_grad
+        dX, dWg, dWu = sphattn_gated_ffn_bwd(X, Wg, Wu, dH.reshape(-1, dH.shape[-1]).contiguous(), ctx.activation, want_dX=need[0], want_dWg=need[1],
+                                             want_dWu=need[2])
+        return None if dX is None else dX.view(ctx.shape), dWg, dWu, None
+
+
+def gated_feed_forward(X, Wg, Wu, activation="silu"):
+    """Differentiable act(X Wg^T) * (X Wu^T): X [..., D], Wg and Wu [F,D] of one type (fp32, bf16 or fp16), activation "silu", "gelu" or "relu".  Nothing but
+    the inputs is kept for the gradients."""
+    return _GatedFeedForward.apply(X, Wg, Wu, activation)

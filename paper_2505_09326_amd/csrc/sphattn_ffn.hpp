@@ -1,0 +1,537 @@
+// The gated feed-forward product of a layer and its gradients, for gfx950.
+//
+//   A = X Wg^T      U = X Wu^T      H = act(A) U
+//   dA = dH U act'(A)      dB = dH act(A)      dX = dA Wg + dB Wu      dWg = dA^T X      dWu = dB^T X
+//
+// Both projections run in one tile (Form::Two of the tile products): a lane holds the same element of A and of U, so the product of the two needs no
+// memory.  The gradients form A and U once more, into dA and dB, instead of reading back what a forward call would have to keep: 4 T F D operations
+// against writing and reading 16 T F bytes (fp32: what 16 bits of A and U leave of dA and dB would be most of the error), and nothing has to be
+// kept between the two calls.  dX is one sum over 2 F (Form::Sum), dWg and dWu are two over T.
+//
+// dA and dB are rounded once to the storage type, which is what the matrix instructions take; sums are in fp32 throughout.  fp16: they are scaled by powers
+// of two that keep them in the type's range whatever the gradients' size, by each row for dX and by the largest row for dW.
+// fp32: A and U as three products of two fp16 parts with a power of two per row, the gradients as six of three bf16 parts, as the vocabulary loss has them.
+#pragma once
+#include "sphattn_tiles.hpp"
+
+namespace sphattn {
+
+enum class Gate { Silu, Gelu, Relu };
+
+// act(a) and its slope.  The exponential's argument is rounded to fp32: |a| 2^-24 of the exponential, which EXACT (fp32 storage) makes up for.
+template <Gate G, bool EXACT>
+__device__ __forceinline__ void gate(float a, float& act, float& slope)
+{
+    auto exp_of = [](float x) {                    // e^x, x <= 87
+        const float y = x * kLog2e;
+        float e = __builtin_amdgcn_exp2f(y);
+        if constexpr (EXACT) e = __builtin_fmaf(e, kLn2 * (__builtin_fmaf(x, kLog2e, -y) + x * 1.925963033e-8f), e);   // (log2(e) and what fp32 leaves of it)
+        return e;
+    };
+    if constexpr (G == Gate::Relu) {
+        act = a <= 0.f ? 0.f : a;
+        slope = a > 0.f ? 1.f : 0.f;
+    } else if constexpr (G == Gate::Silu) {
+        const float e = exp_of(fminf(-a, 87.f));   // (where it ends, a / (1 + e) is below 1e-35)
+        float s;
+        if constexpr (EXACT) s = 1.f / (1.f + e);
+        else s = __builtin_amdgcn_rcpf(1.f + e);
+        act = a * s;
+        slope = s * __builtin_fmaf(a, e * s, 1.f);
+        if (a != a) act = slope = a;               // (the minimum has lost it)
+    } else {
+        const float half = exp_of(fmaxf(-0.5f * a * a, -87.f));
+        float below;                               // the normal distribution's share below a
+        if constexpr (EXACT) below = 0.5f * erfcf(a * -0.70710678118654752f);
+        else {
+            // Abramowitz and Stegun 7.1.26: 1.5e-7 at most, a twentieth of half a step of fp16 at 1
+            const float x = __builtin_fabsf(a) * 0.70710678118654752f, t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3275911f, x, 1.f));
+            float p = 1.061405429f;
+            p = __builtin_fmaf(p, t, -1.453152027f);
+            p = __builtin_fmaf(p, t, 1.421413741f);
+            p = __builtin_fmaf(p, t, -0.284496736f);
+            p = __builtin_fmaf(p, t, 0.254829592f);
+            const float tail = 0.5f * p * t * half;
+            below = a < 0.f ? tail : 1.f - tail;
+        }
+        act = a * below;
+        slope = __builtin_fmaf(a * 0.39894228040143268f, half, below);
+        if (a != a) act = slope = a;
+    }
+}
+
+struct FfnArgs {
+    Operand G, U, X;                               // Wg, Wu, X as the products take them
+    const int *g_exp, *u_exp, *x_exp;              // fp32: the powers of two that each row was divided by (or kEndless) ...
+    const float *g_whole, *u_whole, *x_whole; int D;   // ... and the rows as they are
+    int k, tiles_p, T, F;
+    void* H;                                       // forward: [T,F]
+    const void* dH;                                // backward: [T,F]
+    unsigned short *dA, *dB; long long part; int ld;   // [T,ld], in parts (fp32)
+    const float *row_up, *all_up; unsigned short *dA_all, *dB_all;   // fp16: factors of dA and dB, and the second pair
+};
+
+// Eight (fp32: four) neighbouring elements of a row of F: what of it is in the row
+template <Store S>
+__device__ __forceinline__ void store_piece(void* out, size_t at, i32x4 w, int left, bool wide)
+{
+    if (left <= 0) return;
+    if (wide) store16<S, true>(out, at, w, per16<S>());
+    else store16<S, false>(out, at, w, left);
+}
+
+// the corner of A and U of this wave from rows of fp32 as they are, for the rare tile that meets a row with an infinite element (see whole_logits)
+template <class T>
+__device__ __forceinline__ void whole_projections(f32x4 (&acc)[T::FP][T::FQ], const FfnArgs& a, int fw, int qw)
+{
+    const int lane = threadIdx.x & 63, n16 = lane & 15, g = lane >> 4;
+    const float *pat[T::FP], *qat[T::FQ];          // (rows behind the last one take the last one's place: their results are not looked at)
+#pragma unroll
+    for (int i = 0; i < T::FP; ++i) pat[i] = (i & 1 ? a.u_whole : a.g_whole) + (size_t)min(fw + i / 2 * 16 + n16, a.F - 1) * a.D;
+#pragma unroll
+    for (int j = 0; j < T::FQ; ++j) {
+        qat[j] = a.x_whole + (size_t)min(qw + 16 * j + n16, a.T - 1) * a.D;
+#pragma unroll
+        for (int i = 0; i < T::FP; ++i) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+#pragma unroll 1
+    for (int k = g; k < a.D + g; k += 4) {
+        float w[T::FP], x[T::FQ];
+#pragma unroll
+        for (int i = 0; i < T::FP; ++i) w[i] = k < a.D ? pat[i][k] : 0.f;
+#pragma unroll
+        for (int j = 0; j < T::FQ; ++j) x[j] = k < a.D ? qat[j][k] : 0.f;
+#pragma unroll
+        for (int i = 0; i < T::FP; ++i)
+#pragma unroll
+            for (int j = 0; j < T::FQ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(w[i], x[j], acc[i][j], 0, 0, 0);
+    }
+}
+
+// A tile of BP / 2 columns of F and BQ rows: H, or dA and dB
+template <class T, Store S, bool BACK>
+__global__ __launch_bounds__(T::THREADS, T::FP * T::FQ > 32 ? 1 : 2)
+void ffn_gate_kernel(FfnArgs a, int act)
+{
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem_raw[];
+    SPH_LDS unsigned char* const smem = (SPH_LDS unsigned char*)smem_raw;
+    constexpr bool F32 = S == Store::F32, HALF = S == Store::F16;
+    const int tiles_q = (a.T + T::BQ - 1) / T::BQ;
+    const TileAt tile = tile_of(xcd_contiguous_id(blockIdx.x, a.tiles_p * tiles_q), a.tiles_p, tiles_q);
+    const int f0 = __builtin_amdgcn_readfirstlane(tile.p) * (T::BP / 2), q0 = __builtin_amdgcn_readfirstlane(tile.q) * T::BQ;
+    Product<T, HALF || F32, false, false, F32 ? 3 : 1, Form::Two> prod;
+    prod.run(a.G, a.X, f0, q0, 0, a.k, smem, a.U);
+
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n16 = lane & 15, g = lane >> 4;
+    const int fw = f0 + wave % T::WAVES_P * (T::FP / 2) * 16, qw = q0 + wave / T::WAVES_P * T::FQ * 16;   // this wave's corner
+    if constexpr (F32) {
+        int qe[T::FQ];
+        bool endless = false;
+#pragma unroll
+        for (int j = 0; j < T::FQ; ++j) endless |= (qe[j] = a.x_exp[min(qw + 16 * j + n16, a.T - 1)]) == kEndless;
+#pragma unroll
+        for (int i = 0; i < T::FP; ++i) {          // (the arrays go on to a tile's end; what stands there changes nothing: the products are 0)
+            const int f = fw + i / 2 * 16 + 4 * g;
+            const i32x4 pe = *(const i32x4*)((i & 1 ? a.u_exp : a.g_exp) + f);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                endless |= pe[r] == kEndless && f + r < a.F;
+#pragma unroll
+                for (int j = 0; j < T::FQ; ++j) prod.acc[i][j][r] = __builtin_ldexpf(prod.acc[i][j][r], pe[r] + qe[j]);
+            }
+        }
+        if (__ballot(endless)) whole_projections<T>(prod.acc, a, fw, qw);
+    }
+    static_assert(T::FP % 4 == 0, "");
+    constexpr int E = store_bytes<S>();
+    const void* const rows = BACK ? a.dH : a.H;
+    const bool wide = (((uintptr_t)rows | (uintptr_t)((size_t)a.F * E)) & 15) == 0;
+    // 16-bit: two fragments at a time, whose lanes exchange halves, so that each has eight neighbouring columns of one and 16 bytes to load or store
+    auto corner = [&](auto gate_of) {
+        constexpr Gate G = decltype(gate_of)::value;
+#pragma unroll
+        for (int j = 0; j < T::FQ; ++j) {
+            const int q = qw + 16 * j + n16;
+            const size_t row = (size_t)min(q, a.T - 1) * a.F;
+            float up = 1.f, up_all = 1.f;
+            if constexpr (BACK && HALF) up = a.row_up[min(q, a.T - 1)], up_all = *a.all_up;
+#pragma unroll
+            for (int i = 0; i < T::FP / 2; i += 2) {
+                // where this lane's piece of the two fragments stands (fp32: a piece of each)
+                const int f = F32 ? fw + 16 * i + 4 * g : fw + 16 * (i + (g & 1)) + 8 * (g >> 1);
+                float d[2][4];
+                if constexpr (BACK) {
+                    auto load = [&](int at) {
+                        if (at >= a.F) return i32x4{0, 0, 0, 0};
+                        return wide ? load16<S, true>(a.dH, row + at, per16<S>(), per16<S>()) : load16<S, false>(a.dH, row + at, a.F - at, (size_t)a.T * a.F - row - at);
+                    };
+                    if constexpr (F32) {
+                        widen16<S>(load(f), d[0]);
+                        widen16<S>(load(f + 16), d[1]);
+                    } else {
+                        const i32x4 w = load(f), h = join_fragments(i32x2{w[0], w[1]}, i32x2{w[2], w[3]});   // (the exchange is its own inverse)
+                        float x[8];
+                        widen16<S>(h, x);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) d[0][r] = x[r], d[1][r] = x[4 + r];
+                    }
+                }
+                float y[2][4], z[2][4];
+#pragma unroll
+                for (int s = 0; s < 2; ++s)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const float u = prod.acc[2 * (i + s) + 1][j][r];
+                        float value, slope;
+                        gate<G, F32>(prod.acc[2 * (i + s)][j][r], value, slope);
+                        if constexpr (BACK) {
+                            y[s][r] = d[s][r] * u * slope;
+                            z[s][r] = d[s][r] * value;
+                        } else {
+                            y[s][r] = value * u;
+                        }
+                    }
+                auto pack = [&](const float (&v)[2][4], float by) {
+                    return join_fragments(i32x2{pack2<HALF>(v[0][0] * by, v[0][1] * by), pack2<HALF>(v[0][2] * by, v[0][3] * by)},
+                                          i32x2{pack2<HALF>(v[1][0] * by, v[1][1] * by), pack2<HALF>(v[1][2] * by, v[1][3] * by)});
+                };
+                if constexpr (!BACK) {
+                    if constexpr (F32) {
+#pragma unroll
+                        for (int s = 0; s < 2; ++s)
+                            if (q < a.T) store_piece<S>(a.H, row + f + 16 * s, narrow16<S>(y[s]), a.F - f - 16 * s, wide);
+                    } else {
+                        const i32x4 w = pack(y, 1.f);
+                        if (q < a.T) store_piece<S>(a.H, row + f, w, a.F - f, wide);
+                    }
+                } else {
+                    const size_t at = (size_t)q * a.ld + (F32 ? fw + 16 * (i + (g & 1)) + 8 * (g >> 1) : f);
+                    const bool in = q < a.T && (F32 ? fw + 16 * (i + (g & 1)) + 8 * (g >> 1) : f) < a.ld;
+                    if constexpr (F32) {
+#pragma unroll
+                        for (int m = 0; m < 2; ++m) {
+                            i32x2 part[2][3];      // [fragment][part]
+#pragma unroll
+                            for (int s = 0; s < 2; ++s) split3(m ? z[s] : y[s], part[s]);
+#pragma unroll
+                            for (int p = 0; p < 3; ++p) {
+                                const i32x4 w = join_fragments(part[0][p], part[1][p]);
+                                if (in) *(i32x4*)((m ? a.dB : a.dA) + p * a.part + at) = w;
+                            }
+                        }
+                    } else {
+                        const i32x4 wa = pack(y, up), wb = pack(z, up);
+                        if (in) {
+                            *(i32x4*)(a.dA + at) = wa;
+                            *(i32x4*)(a.dB + at) = wb;
+                        }
+                        if constexpr (HALF) {
+                            if (a.dA_all) {
+                                const i32x4 va = pack(y, up_all), vb = pack(z, up_all);
+                                if (in) {
+                                    *(i32x4*)(a.dA_all + at) = va;
+                                    *(i32x4*)(a.dB_all + at) = vb;
+                                }
+                            }
+                        }
+                    }
+                }
+            }
+        }
+    };
+    if (act == (int)Gate::Silu) corner(std::integral_constant<Gate, Gate::Silu>{});
+    else if (act == (int)Gate::Gelu) corner(std::integral_constant<Gate, Gate::Gelu>{});
+    else corner(std::integral_constant<Gate, Gate::Relu>{});
+}
+
+// ---- few rows -----------------------------------------------------------------------------------------------
+
+// H for at most 64 rows, where reading the weights is most of the time: they go from memory straight into registers, once.  A workgroup takes sixteen
+// columns of F, its waves a share of D each, in runs of 256 bytes of a row; lane (i, g) holds 16 bytes of row i of each operand (any order of k
+// will do if both have it).  fp32 on the fp32 matrix instruction, as it is.
+template <int FQ> constexpr int ffn_row_waves() { return FQ == 4 ? 4 : 8; }
+
+template <Store S, int FQ, bool WIDE>
+__global__ __launch_bounds__(64 * ffn_row_waves<FQ>())
+void ffn_rows_kernel(const void* __restrict__ X, const void* __restrict__ Wg, const void* __restrict__ Wu, void* __restrict__ H, int T, int D, int F, int act)
+{
+    constexpr int WAVES = ffn_row_waves<FQ>(), N = per16<S>(), STEP = 4 * N, RUN = 4;   // STEP: k of one 16-byte load of all lanes; RUN of them neighbours
+    __shared__ f32x4 sums[WAVES][2][FQ][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n16 = lane & 15, g = lane >> 4;
+    const int f0 = (int)blockIdx.x * 16;
+    const size_t pat = (size_t)min(f0 + n16, F - 1) * D, all = (size_t)F * D, all_x = (size_t)T * D;
+    size_t qat[FQ];
+#pragma unroll
+    for (int j = 0; j < FQ; ++j) qat[j] = (size_t)min(16 * j + n16, T - 1) * D;
+    f32x4 acc[2][FQ];
+#pragma unroll
+    for (int j = 0; j < FQ; ++j) acc[0][j] = acc[1][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    auto load = [&](const void* from, size_t at, int k, size_t end) {
+        if (k >= D) return i32x4{0, 0, 0, 0};
+        return load16<S, WIDE>(from, at + k, D - k, end - at - k);
+    };
+    i32x4 next[2][RUN];
+    auto fetch = [&](int k) {
+#pragma unroll
+        for (int c = 0; c < RUN; ++c) {
+            next[0][c] = load(Wg, pat, k + c * STEP + g * N, all);
+            next[1][c] = load(Wu, pat, k + c * STEP + g * N, all);
+        }
+    };
+    const int first = wave * RUN * STEP;
+    fetch(first);
+    for (int k = first; k < D; k += WAVES * RUN * STEP) {
+        i32x4 w[2][RUN], x[RUN][FQ];
+#pragma unroll
+        for (int c = 0; c < RUN; ++c) {
+            w[0][c] = next[0][c], w[1][c] = next[1][c];
+#pragma unroll
+            for (int j = 0; j < FQ; ++j) x[c][j] = load(X, qat[j], k + c * STEP + g * N, all_x);
+        }
+        fetch(k + WAVES * RUN * STEP);
+#pragma unroll
+        for (int c = 0; c < RUN; ++c)
+#pragma unroll
+            for (int m = 0; m < 2; ++m)
+#pragma unroll
+                for (int j = 0; j < FQ; ++j) {
+                    if constexpr (S == Store::F32) {
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) acc[m][j] = mfma_f32(w[m][c], x[c][j], r, acc[m][j]);
+                    } else {
+                        acc[m][j] = mfma16x16<S == Store::F16>(w[m][c], x[c][j], acc[m][j]);
+                    }
+                }
+    }
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int j = 0; j < FQ; ++j) sums[wave][m][j][lane] = acc[m][j];
+    __syncthreads();
+    // lane (t, g) of wave j: columns 4 g .. + 3 of row 16 j + t
+    if (wave >= FQ) return;
+    f32x4 A = sums[0][0][wave][lane], U = sums[0][1][wave][lane];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) A += sums[w][0][wave][lane], U += sums[w][1][wave][lane];
+    const int t = 16 * wave + n16;
+    if (t >= T) return;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const int f = f0 + 4 * g + r;
+        if (f >= F) return;
+        float value, slope;
+        if (act == (int)Gate::Silu) gate<Gate::Silu, S == Store::F32>(A[r], value, slope);
+        else if (act == (int)Gate::Gelu) gate<Gate::Gelu, S == Store::F32>(A[r], value, slope);
+        else gate<Gate::Relu, S == Store::F32>(A[r], value, slope);
+        store_el<S>(H, (size_t)t * F + f, value * U[r]);
+    }
+}
+
+// ---- sums of the gradients ------------------------------------------------------------------------------------
+
+struct FfnSum {
+    Operand P, P2, Q, Q2;
+    int k, tiles_p, slices;
+    void* out; int out_ld, out_cols, out_rows;     // in the storage type, where there is one slice
+    float* part; int part_ld;                      // else [slices][out_rows][part_ld]
+    const float *row_down, *down;                  // fp16: by row, or one
+};
+
+// dX [T,D] = dA Wg + dB Wu
+template <class T, Store S, bool DX>
+__device__ __forceinline__ void ffn_sum_tile(const FfnSum& a, int id, SPH_LDS unsigned char* smem)
+{
+    constexpr bool F32 = S == Store::F32;
+    const int tiles_q = (a.out_rows + T::BQ - 1) / T::BQ;
+    const TileAt tile = tile_of(xcd_contiguous_id(id, a.tiles_p * tiles_q * a.slices), a.tiles_p, tiles_q);
+    const int p0 = __builtin_amdgcn_readfirstlane(tile.p) * T::BP, q0 = __builtin_amdgcn_readfirstlane(tile.q) * T::BQ;
+    const int per_slice = __builtin_amdgcn_readfirstlane(((a.k + kStepK - 1) / kStepK + a.slices - 1) / a.slices) * kStepK;
+    const int slice = __builtin_amdgcn_readfirstlane(tile.slice);
+    const int k0 = min(a.k, slice * per_slice), k1 = min(a.k, k0 + per_slice);
+    Product<T, S == Store::F16, true, !DX, F32 ? 6 : 1, DX ? Form::Sum : Form::One> prod;
+    prod.run(a.P, a.Q, p0, q0, k0, k1, smem, a.P2, a.Q2);
+
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n16 = lane & 15, g = lane >> 4;
+    const int pw = p0 + wave % T::WAVES_P * T::FP * 16, qw = q0 + wave / T::WAVES_P * T::FQ * 16;
+    const bool wide = (((uintptr_t)a.out | (uintptr_t)((size_t)a.out_ld * store_bytes<S>())) & 15) == 0;
+#pragma unroll
+    for (int j = 0; j < T::FQ; ++j) {
+        const int q = qw + 16 * j + n16;
+        const bool in = q < a.out_rows;
+        if (a.slices > 1) {
+#pragma unroll
+            for (int i = 0; i < T::FP; ++i) {
+                const int p = pw + 16 * i + 4 * g;
+                if (in && p < a.part_ld) *(f32x4*)(a.part + ((size_t)slice * a.out_rows + q) * a.part_ld + p) = prod.acc[i][j];
+            }
+            continue;
+        }
+        float by = 1.f;
+        if constexpr (S == Store::F16) by = a.row_down ? a.row_down[min(q, a.out_rows - 1)] : a.down ? *a.down : 1.f;
+        const size_t row = (size_t)q * a.out_ld;
+#pragma unroll
+        for (int i = 0; i < T::FP; i += 2) {
+            const f32x4 x = prod.acc[i][j] * by, z = prod.acc[i + 1][j] * by;
+            if constexpr (F32) {
+                const int p = pw + 16 * i + 4 * g;
+                if (in) store_piece<S>(a.out, row + p, __builtin_bit_cast(i32x4, x), a.out_cols - p, wide);
+                if (in) store_piece<S>(a.out, row + p + 16, __builtin_bit_cast(i32x4, z), a.out_cols - p - 16, wide);
+            } else {
+                const i32x4 o = join_fragments(i32x2{pack2<S == Store::F16>(x[0], x[1]), pack2<S == Store::F16>(x[2], x[3])},
+                                               i32x2{pack2<S == Store::F16>(z[0], z[1]), pack2<S == Store::F16>(z[2], z[3])});
+                const int p = pw + 16 * (i + (g & 1)) + 8 * (g >> 1);
+                if (in) store_piece<S>(a.out, row + p, o, a.out_cols - p, wide);
+            }
+        }
+    }
+}
+
+template <class T, Store S>
+__global__ __launch_bounds__(T::THREADS, T::FP * T::FQ > 32 ? 1 : 2)
+void ffn_dx_kernel(FfnSum a)
+{
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem_raw[];
+    ffn_sum_tile<T, S, true>(a, blockIdx.x, (SPH_LDS unsigned char*)smem_raw);
+}
+
+// dWg and dWu: `each` workgroups for the first, the rest for the second
+template <class T, Store S>
+__global__ __launch_bounds__(T::THREADS, T::FP * T::FQ > 32 ? 1 : 2)
+void ffn_dw_kernel(FfnSum a, FfnSum b, int each)
+{
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem_raw[];
+    const bool second = (int)blockIdx.x >= each;
+    ffn_sum_tile<T, S, false>(second ? b : a, (int)blockIdx.x - (second ? each : 0), (SPH_LDS unsigned char*)smem_raw);
+}
+
+// Slices added up in order, scaled and rounded: a wave 256 columns of a row, eight slices' loads under way
+template <Store S>
+__global__ __launch_bounds__(256)
+void ffn_join_kernel(FfnSum a, int columns)
+{
+    const int lane = threadIdx.x & 63;
+    const long long unit = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = unit / columns;
+    if (q >= a.out_rows) return;
+    const int c = (int)(unit - q * columns) * 256 + lane * 4;
+    if (c >= a.out_cols) return;
+    const size_t slice = (size_t)a.out_rows * a.part_ld;
+    const float* from = a.part + (size_t)q * a.part_ld + c;
+    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+    constexpr int AHEAD = 8;
+    for (int s0 = 0; s0 < a.slices; s0 += AHEAD) {
+        f32x4 y[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) y[i] = *(const f32x4*)(from + min(s0 + i, a.slices - 1) * slice);
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i)
+            if (s0 + i < a.slices) x += y[i];
+    }
+    if constexpr (S == Store::F16) x *= a.row_down ? a.row_down[q] : a.down ? *a.down : 1.f;
+    const size_t at = (size_t)q * a.out_ld + c;
+    const int left = a.out_cols - c;
+    if (left >= 4) {
+        if constexpr (S == Store::F32) __builtin_memcpy((float*)a.out + at, &x, 16);
+        else {
+            const i32x2 w = {pack2<S == Store::F16>(x[0], x[1]), pack2<S == Store::F16>(x[2], x[3])};
+            __builtin_memcpy((unsigned short*)a.out + at, &w, 8);
+        }
+    } else {
+#pragma unroll
+        for (int r = 0; r < 3; ++r)
+            if (r < left) store_el<S>(a.out, at + r, x[r]);
+    }
+}
+
+// ---- around the products ------------------------------------------------------------------------------------
+
+// X, Wg and Wu as the products take them (those with an `out`): a wave per row
+struct FfnPack { PackRows m[3]; int until[2]; };   // workgroups below until[0] on the first, below until[1] on the second
+constexpr int kFfnPackThreads = 256, kFfnPackRows = kFfnPackThreads / 64;
+
+template <Store S>
+__global__ __launch_bounds__(kFfnPackThreads)
+void ffn_pack_kernel(FfnPack a)
+{
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), block = blockIdx.x;
+    const int m = block < a.until[0] ? 0 : block < a.until[1] ? 1 : 2;
+    const PackRows& rows = a.m[m];
+    const long long row = (long long)(block - (m == 0 ? 0 : a.until[m - 1])) * kFfnPackRows + wave;
+    if (row < rows.n) pack_row<S>(rows, row, row, lane);
+}
+
+// fp16.  dA and dB are at most |dH| |x| |w| 1.13 for the rows' norms (act's slope is 1.13 at most), which a power of two brings to 2^13 .. 2^14: by each
+// row t for dX, by the largest row for dW.  A dot product of D terms is about sqrt(D) below the product of the norms; from there down the type has
+// 2^-14 for normal numbers, so with D = 2048 a row's values keep their bits to 2^-22 of their usual size.
+// Norms of X's rows with the largest |dH| of each, and of Wg's and Wu's: a wave per row.
+template <bool WIDE>
+__global__ __launch_bounds__(256)
+void ffn_norms_kernel(const void* __restrict__ X, const void* __restrict__ dH, const void* __restrict__ Wg, const void* __restrict__ Wu, int T, int D, int F,
+                      float* __restrict__ x_bound, float* __restrict__ w_norm)
+{
+    constexpr Store S = Store::F16;
+    const int lane = threadIdx.x & 63;
+    const long long unit = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (unit >= (long long)T + 2 * F) return;
+    const bool on_x = unit < T;
+    const long long f = unit - T;
+    const void* from = on_x ? X : f < F ? Wg : Wu;
+    const size_t row = (size_t)(on_x ? unit : f < F ? f : f - F) * D, end = (size_t)(on_x ? T : F) * D;
+    float sum = 0.f, top = 1.f;
+    for (int c = lane * 8; c < D; c += 512) {
+        float x[8];
+        widen16<S>(load16<S, WIDE>(from, row + c, D - c, end - row - c), x);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum = __builtin_fmaf(x[i], x[i], sum);
+    }
+    if (on_x) {
+        const size_t at = (size_t)unit * F;
+        top = 0.f;
+        for (int c = lane * 8; c < F; c += 512) {
+            float x[8];
+            widen16<S>(load16<S, false>(dH, at + c, F - c, (size_t)T * F - at - c), x);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) top = fmaxf(top, __builtin_fabsf(x[i]));
+        }
+        top = max_over_wave(top);
+    }
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+    if (lane == 0) (on_x ? x_bound[unit] : w_norm[f]) = __builtin_sqrtf(sum) * top;
+}
+
+// The rows' factors and the one for all; one workgroup.  A row whose bound is infinite or 0 keeps its values as they are.
+__global__ __launch_bounds__(1024)
+void ffn_factors_kernel(const float* __restrict__ x_bound, const float* __restrict__ w_norm, int T, int F, float* __restrict__ row_up, float* __restrict__ row_down,
+                        float* __restrict__ all)       // all: up, down
+{
+    __shared__ float shared[16];
+    const int tid = threadIdx.x;
+    auto over_all = [&](float x) {
+        x = max_over_wave(x);
+        __syncthreads();
+        if ((tid & 63) == 0) shared[tid >> 6] = x;
+        __syncthreads();
+        for (int w = 0; w < 16; ++w) x = fmaxf(x, shared[w]);
+        return x;
+    };
+    float w = 0.f;
+    for (int f = tid; f < 2 * F; f += 1024) w = w_norm[f] < __builtin_inff() ? fmaxf(w, w_norm[f]) : w;
+    w = over_all(w);
+    auto factor = [](float x) {
+        return x > 0.f && x < __builtin_inff() ? __builtin_ldexpf(1.f, max(-100, min(100, 13 - (__builtin_amdgcn_frexp_expf(x) - 1)))) : 1.f;
+    };
+    float top = 0.f;
+    for (int t = tid; t < T; t += 1024) {
+        const float b = x_bound[t] * w * 1.13f, up = factor(b);
+        top = b < __builtin_inff() ? fmaxf(top, b) : top;
+        row_up[t] = up;
+        row_down[t] = 1.f / up;
+    }
+    top = over_all(top);
+    if (tid == 0) {
+        all[0] = factor(top);
+        all[1] = 1.f / all[0];
+    }
+}
+
+}  // namespace sphattn

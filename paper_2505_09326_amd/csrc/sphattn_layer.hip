@@ -1,7 +1,8 @@
 // Host side of the C ABI declared in include/sphattn_layer.h: argument checks, choice of launches on the caller's
 // stream.  Allocates nothing and never synchronises.
+#include "sphattn_ffn.hpp"
 #include "sphattn_heads.hpp"
-#include "sphattn_host.hpp"
+#include "sphattn_tile_choice.hpp"
 #include "../../include/sphattn_layer.h"
 
 #include <climits>
@@ -144,6 +145,247 @@ long long heads_groups(const HeadsArgs& a, int d)
     return ((long long)a.B * a.N * a.share + per - 1) / per;
 }
 
+// ---- gated feed-forward ------------------------------------------------------------------------------------
+
+constexpr int kFfnRows = 64;                       // up to here the weights go from memory straight into registers
+
+bool ffn_shape(int T, int D, int F)
+{
+    return T >= 0 && T <= 1 << 20 && D >= 1 && D <= 65536 && F >= 1 && F <= 1 << 18 && (long long)T * F <= 1ll << 36;   // (a launch has less than 2^32 threads)
+}
+
+// The tile and slices of a sum over k for `count` results of rows x cols, by the time that its rounds take: in a round of 256 Big tiles each takes 27 ns
+// per k, in one of 512 Mid tiles 20, and every slice is written and read again as fp32.
+struct SumChoice { bool big; int slices; };
+SumChoice sum_choice(long long rows, long long cols, long long k, int count, int products)
+{
+    SumChoice c{false, 1};
+    double best = 0.0;
+    for (int b = 1; b >= 0; --b) {
+        const int tile = b ? 256 : 128, at_once = b ? kCus : 2 * kCus;
+        const long long tiles = count * ((rows + tile - 1) / tile) * ((cols + tile - 1) / tile);
+        for (int s = 1; s <= 64 && (s == 1 || (k / s >= 256 && (double)s * count * rows * cols <= 2.5e8)); s *= 2) {
+            const double rounds = (double)((tiles * s + at_once - 1) / at_once);
+            const double us = rounds * (double)(k / s) * products * (b ? 0.027 : 0.020) + (s > 1 ? 4.0 + s * (double)(count * rows * cols) * 8.0 / 4.5e6 : 0.0);
+            if (best == 0.0 || us < best) best = us, c = SumChoice{b != 0, s};
+        }
+    }
+    return c;
+}
+
+struct Ffn {
+    int T, D, F, ld, ldf, parts, g_parts;          // ld, ldf: elements per packed row of D, of F; parts: of X and W, of dA and dB
+    SumChoice dx, dw;
+    int *x_exp, *g_exp, *u_exp;                    // fp32
+    unsigned short *x, *g, *u, *x_sum, *g_sum, *u_sum;
+    unsigned short *dA, *dB, *dA_all, *dB_all;
+    float *x_bound, *w_norm, *row_up, *row_down, *all_up;   // fp16
+    float* part;                                   // of dX, then of dW
+    size_t bytes;
+};
+
+Ffn ffn_plan(int T, int D, int F, int dtype, bool back, void* workspace)
+{
+    Ffn p{};
+    p.T = T, p.D = D, p.F = F, p.ld = (int)up_to(D, 8), p.ldf = (int)up_to(F, 8);
+    p.parts = dtype == SPHATTN_F32 ? 2 : 1, p.g_parts = dtype == SPHATTN_F32 ? 3 : 1;
+    if (!back && T <= kFfnRows) return p;
+    const bool f32 = dtype == SPHATTN_F32, f16 = dtype == SPHATTN_F16;
+    Carve c(workspace);
+    p.x_exp = c.take<int>(f32 ? T : 0);
+    p.g_exp = c.take<int>(f32 ? up_to(F, 256) : 0);
+    p.u_exp = c.take<int>(f32 ? up_to(F, 256) : 0);
+    // (rows that the products can read as they are need no copy, but who asks for the size knows no addresses)
+    p.x = c.take<unsigned short>((size_t)p.parts * T * p.ld);
+    p.g = c.take<unsigned short>((size_t)p.parts * F * p.ld);
+    p.u = c.take<unsigned short>((size_t)p.parts * F * p.ld);
+    if (back) {
+        p.x_sum = c.take<unsigned short>(f32 ? (size_t)3 * T * p.ld : 0);
+        p.g_sum = c.take<unsigned short>(f32 ? (size_t)3 * F * p.ld : 0);
+        p.u_sum = c.take<unsigned short>(f32 ? (size_t)3 * F * p.ld : 0);
+        const size_t n = (size_t)p.g_parts * T * p.ldf;
+        p.dA = c.take<unsigned short>(n);
+        p.dB = c.take<unsigned short>(n);
+        p.dA_all = c.take<unsigned short>(f16 ? n : 0);
+        p.dB_all = c.take<unsigned short>(f16 ? n : 0);
+        p.x_bound = c.take<float>(f16 ? T : 0);
+        p.w_norm = c.take<float>(f16 ? (size_t)2 * F : 0);
+        p.row_up = c.take<float>(f16 ? T : 0);
+        p.row_down = c.take<float>(f16 ? T : 0);
+        p.all_up = c.take<float>(f16 ? 2 : 0);
+        const int products = f32 ? 6 : 1;
+        p.dx = sum_choice(T > 0 ? T : 1, p.ld, 2ll * F, 1, products);
+        p.dw = T > 0 ? sum_choice(F, p.ld, T, 2, products) : SumChoice{false, 1};
+        const size_t of_dx = p.dx.slices > 1 ? (size_t)p.dx.slices * T * p.ld : 0, of_dw = p.dw.slices > 1 ? (size_t)p.dw.slices * 2 * F * p.ld : 0;
+        p.part = c.take<float>(of_dx > of_dw ? of_dx : of_dw);
+    }
+    p.bytes = c.used();
+    return p;
+}
+
+template <class T, Store S, bool BACK>
+int launch_gate(FfnArgs& a, int act, hipStream_t stream)
+{
+    const auto kern = ffn_gate_kernel<T, S, BACK>;
+    static std::atomic<uint64_t> done{0};
+    if (T::LDS > 65536 && !raise_lds_limit(kern, T::LDS, done)) return SPHATTN_ERR_LAUNCH;
+    a.tiles_p = (a.F + T::BP / 2 - 1) / (T::BP / 2);
+    const long long tiles = (long long)a.tiles_p * ((a.T + T::BQ - 1) / T::BQ);
+    if (tiles > 1 << 22) return SPHATTN_ERR_SHAPE;                    // (a launch has less than 2^32 threads)
+    hipLaunchKernelGGL(kern, dim3((unsigned)tiles), dim3(T::THREADS), T::LDS, stream, a, act);
+    return launched();
+}
+
+template <Store S, bool BACK>
+int run_gate(FfnArgs& a, int act, hipStream_t stream)
+{
+    return big_tiles(2ll * a.F, a.T) ? launch_gate<Big, S, BACK>(a, act, stream) : launch_gate<Mid, S, BACK>(a, act, stream);
+}
+
+// X, Wg and Wu as the products take them; what can be read as it is stays where it is
+template <Store S>
+FfnArgs ffn_pack(const Ffn& p, const void* X, const void* Wg, const void* Wu, hipStream_t stream)
+{
+    FfnArgs a{};
+    FfnPack k{};
+    int groups = 0;
+    auto take = [&](int m, const void* in, int n, unsigned short* out, unsigned short* sum_out, int* exp) {
+        Operand o{(const unsigned char*)in, 0, p.D * 2, n};
+        if (!ready(in, p.D, S)) {
+            k.m[m] = PackRows{in, out, n, p.D, p.ld, (long long)n * p.ld, sum_out, exp};
+            groups += (n + kFfnPackRows - 1) / kFfnPackRows;
+            o = Operand{(const unsigned char*)out, k.m[m].part * 2, p.ld * 2, n};
+        }
+        if (m < 2) k.until[m] = groups;
+        return o;
+    };
+    a.X = take(0, X, p.T, p.x, p.x_sum, p.x_exp);
+    a.G = take(1, Wg, p.F, p.g, p.g_sum, p.g_exp);
+    a.U = take(2, Wu, p.F, p.u, p.u_sum, p.u_exp);
+    if (groups) hipLaunchKernelGGL((ffn_pack_kernel<S>), dim3((unsigned)groups), dim3(kFfnPackThreads), 0, stream, k);
+    a.g_exp = p.g_exp, a.u_exp = p.u_exp, a.x_exp = p.x_exp;
+    a.g_whole = (const float*)Wg, a.u_whole = (const float*)Wu, a.x_whole = (const float*)X, a.D = p.D;
+    a.k = p.ld, a.T = p.T, a.F = p.F;
+    return a;
+}
+
+template <Store S, int FQ>
+int launch_rows(const void* X, const void* Wg, const void* Wu, void* H, int T, int D, int F, int act, hipStream_t stream)
+{
+    const dim3 grid((unsigned)(F + 15) / 16), block(64 * ffn_row_waves<FQ>());
+    const bool wide = !off(X, 16) && !off(Wg, 16) && !off(Wu, 16) && D % per16<S>() == 0;
+    if (wide) hipLaunchKernelGGL((ffn_rows_kernel<S, FQ, true>), grid, block, 0, stream, X, Wg, Wu, H, T, D, F, act);
+    else hipLaunchKernelGGL((ffn_rows_kernel<S, FQ, false>), grid, block, 0, stream, X, Wg, Wu, H, T, D, F, act);
+    return launched();
+}
+
+template <Store S>
+int run_ffn_fwd(const Ffn& p, const void* X, const void* Wg, const void* Wu, void* H, int act, hipStream_t stream)
+{
+    if (p.T <= 16) return launch_rows<S, 1>(X, Wg, Wu, H, p.T, p.D, p.F, act, stream);
+    if (p.T <= 32) return launch_rows<S, 2>(X, Wg, Wu, H, p.T, p.D, p.F, act, stream);
+    if (p.T <= kFfnRows) return launch_rows<S, 4>(X, Wg, Wu, H, p.T, p.D, p.F, act, stream);
+    FfnArgs a = ffn_pack<S>(p, X, Wg, Wu, stream);
+    a.H = H;
+    return run_gate<S, false>(a, act, stream);
+}
+
+template <class T, Store S, bool DX>
+int launch_sum(FfnSum& a, FfnSum* b, hipStream_t stream)
+{
+    a.tiles_p = (a.P.size + T::BP - 1) / T::BP;
+    const long long each = (long long)a.tiles_p * ((a.out_rows + T::BQ - 1) / T::BQ) * a.slices;
+    if (each > 1 << 21) return SPHATTN_ERR_SHAPE;                     // (a launch has less than 2^32 threads)
+    static std::atomic<uint64_t> done{0};
+    if constexpr (DX) {
+        const auto kern = ffn_dx_kernel<T, S>;
+        if (T::LDS > 65536 && !raise_lds_limit(kern, T::LDS, done)) return SPHATTN_ERR_LAUNCH;
+        hipLaunchKernelGGL(kern, dim3((unsigned)each), dim3(T::THREADS), T::LDS, stream, a);
+    } else {
+        const auto kern = ffn_dw_kernel<T, S>;
+        if (T::LDS > 65536 && !raise_lds_limit(kern, T::LDS, done)) return SPHATTN_ERR_LAUNCH;
+        if (b) b->tiles_p = a.tiles_p;
+        hipLaunchKernelGGL(kern, dim3((unsigned)(b ? 2 * each : each)), dim3(T::THREADS), T::LDS, stream, a, b ? *b : a, (int)each);
+    }
+    return launched();
+}
+
+template <Store S>
+int join_slices(const FfnSum& a, hipStream_t stream)
+{
+    const int columns = (a.out_cols + 255) / 256;
+    const long long waves = (long long)a.out_rows * columns;
+    hipLaunchKernelGGL((ffn_join_kernel<S>), dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, stream, a, columns);
+    return launched();
+}
+
+template <Store S>
+int run_ffn_bwd(const Ffn& p, const void* X, const void* Wg, const void* Wu, const void* dH, void* dX, void* dWg, void* dWu, int act, hipStream_t stream)
+{
+    constexpr bool F32 = S == Store::F32, F16 = S == Store::F16;
+    const bool dw = dWg || dWu;
+    FfnArgs a{};
+    a.X = Operand{nullptr, 0, p.ld * 2, 0};
+    int rc = SPHATTN_OK;
+    if (p.T > 0) {
+        a = ffn_pack<S>(p, X, Wg, Wu, stream);
+        a.dH = dH, a.dA = p.dA, a.dB = p.dB, a.part = (long long)p.T * p.ldf, a.ld = p.ldf;
+        if (F16) {
+            const dim3 grid((unsigned)(((long long)p.T + 2 * p.F + 3) / 4));
+            if (!off(X, 16) && !off(Wg, 16) && !off(Wu, 16) && p.D % 8 == 0)
+                hipLaunchKernelGGL((ffn_norms_kernel<true>), grid, dim3(256), 0, stream, X, dH, Wg, Wu, p.T, p.D, p.F, p.x_bound, p.w_norm);
+            else hipLaunchKernelGGL((ffn_norms_kernel<false>), grid, dim3(256), 0, stream, X, dH, Wg, Wu, p.T, p.D, p.F, p.x_bound, p.w_norm);
+            hipLaunchKernelGGL(ffn_factors_kernel, dim3(1), dim3(1024), 0, stream, p.x_bound, p.w_norm, p.T, p.F, p.row_up, p.row_down, p.all_up);
+            a.row_up = p.row_up, a.all_up = p.all_up, a.dA_all = dw ? p.dA_all : nullptr, a.dB_all = p.dB_all;
+        }
+        rc = run_gate<S, true>(a, act, stream);
+    }
+    const long long part = F32 ? (long long)p.T * p.ldf * 2 : 0;
+    // (fp32: what dA and dB are multiplied with are parts of their own)
+    auto columns = [&](const Operand& o, const unsigned short* sum, int rows) {
+        return F32 ? Operand{(const unsigned char*)sum, (long long)rows * p.ld * 2, p.ld * 2, p.ld} : Operand{o.data, 0, o.ld, p.ld};
+    };
+    if (rc == SPHATTN_OK && dX && p.T > 0) {
+        FfnSum s{};
+        s.P = columns(a.G, p.g_sum, p.F), s.P2 = columns(a.U, p.u_sum, p.F);
+        s.Q = Operand{(const unsigned char*)p.dA, part, p.ldf * 2, p.T}, s.Q2 = Operand{(const unsigned char*)p.dB, part, p.ldf * 2, p.T};
+        s.k = p.F, s.slices = p.dx.slices, s.out = dX, s.out_ld = s.out_cols = p.D, s.out_rows = p.T, s.part = p.part, s.part_ld = p.ld;
+        if (F16) s.row_down = p.row_down;
+        rc = p.dx.big ? launch_sum<Big, S, true>(s, nullptr, stream) : launch_sum<Mid, S, true>(s, nullptr, stream);
+        if (rc == SPHATTN_OK && s.slices > 1) rc = join_slices<S>(s, stream);
+    }
+    if (rc == SPHATTN_OK && dw) {
+        FfnSum s[2]{};
+        int n = 0;
+        for (int m = 0; m < 2; ++m) {
+            void* out = m ? dWu : dWg;
+            if (!out) continue;
+            const unsigned short* q = m ? (F16 ? p.dB_all : p.dB) : (F16 ? p.dA_all : p.dA);
+            s[n].P = columns(a.X, p.x_sum, p.T);
+            s[n].Q = Operand{(const unsigned char*)q, part, p.ldf * 2, p.ldf};
+            s[n].k = p.T, s[n].slices = p.dw.slices, s[n].out = out, s[n].out_ld = s[n].out_cols = p.D, s[n].out_rows = p.F;
+            s[n].part = p.part ? p.part + (size_t)n * p.dw.slices * p.F * p.ld : nullptr, s[n].part_ld = p.ld;
+            if (F16 && p.T > 0) s[n].down = p.all_up + 1;
+            ++n;
+        }
+        FfnSum* second = n == 2 ? &s[1] : nullptr;
+        rc = p.dw.big ? launch_sum<Big, S, false>(s[0], second, stream) : launch_sum<Mid, S, false>(s[0], second, stream);
+        for (int m = 0; m < n && rc == SPHATTN_OK && s[m].slices > 1; ++m) rc = join_slices<S>(s[m], stream);
+    }
+    return rc;
+}
+
+int ffn_check(const void* X, const void* Wg, const void* Wu, int T, int D, int F, int gate, int dtype)
+{
+    if (!ffn_shape(T, D, F)) return SPHATTN_ERR_SHAPE;
+    const size_t e = (size_t)element_bytes(dtype);
+    if (!e) return SPHATTN_ERR_DTYPE;
+    if (!Wg || !Wu || (T > 0 && !X)) return SPHATTN_ERR_NULL;
+    if (off(X, e) || off(Wg, e) || off(Wu, e)) return SPHATTN_ERR_ALIGN;
+    if (gate < SPHATTN_GATE_SILU || gate > SPHATTN_GATE_RELU) return SPHATTN_ERR_VALUE;
+    return SPHATTN_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -229,6 +471,60 @@ int sphattn_head_norm_rotary_bwd(const sphattn_heads* Xq, const sphattn_heads* X
         }
     }
     return launched();
+}
+
+size_t sphattn_gated_ffn_workspace_bytes(int T, int D, int F, int dtype)
+{
+    return ffn_shape(T, D, F) && element_bytes(dtype) ? ffn_plan(T, D, F, dtype, false, nullptr).bytes : 0;
+}
+
+int sphattn_gated_ffn_fwd(const void* X, const void* Wg, const void* Wu, void* H, int T, int D, int F, int gate, int dtype,
+                          void* workspace, size_t workspace_bytes, void* stream)
+{
+    const int rc = ffn_check(X, Wg, Wu, T, D, F, gate, dtype);
+    if (rc != SPHATTN_OK) return rc;
+    if (T > 0 && !H) return SPHATTN_ERR_NULL;
+    const size_t e = (size_t)element_bytes(dtype);
+    if (off(H, e)) return SPHATTN_ERR_ALIGN;
+    const Ffn p = ffn_plan(T, D, F, dtype, false, workspace);
+    if (p.bytes && (!workspace || off(workspace, 16) || workspace_bytes < p.bytes)) return SPHATTN_ERR_WORKSPACE;
+    const Range written[] = {{H, (size_t)T * F * e}, {workspace, p.bytes}};
+    const Range read[] = {{X, (size_t)T * D * e}, {Wg, (size_t)F * D * e}, {Wu, (size_t)F * D * e}};
+    if (any_meet(written, read)) return SPHATTN_ERR_ALIAS;
+    if (T == 0) return SPHATTN_OK;
+    const hipStream_t s = (hipStream_t)stream;
+    switch (dtype) {
+    case SPHATTN_F32: return run_ffn_fwd<Store::F32>(p, X, Wg, Wu, H, gate, s);
+    case SPHATTN_BF16: return run_ffn_fwd<Store::Bf16>(p, X, Wg, Wu, H, gate, s);
+    default: return run_ffn_fwd<Store::F16>(p, X, Wg, Wu, H, gate, s);
+    }
+}
+
+size_t sphattn_gated_ffn_bwd_workspace_bytes(int T, int D, int F, int dtype)
+{
+    return ffn_shape(T, D, F) && element_bytes(dtype) ? ffn_plan(T, D, F, dtype, true, nullptr).bytes : 0;
+}
+
+int sphattn_gated_ffn_bwd(const void* X, const void* Wg, const void* Wu, const void* dH, void* dX, void* dWg, void* dWu, int T, int D, int F,
+                          int gate, int dtype, void* workspace, size_t workspace_bytes, void* stream)
+{
+    const int rc = ffn_check(X, Wg, Wu, T, D, F, gate, dtype);
+    if (rc != SPHATTN_OK) return rc;
+    if ((T > 0 && !dH) || (!dX && !dWg && !dWu)) return SPHATTN_ERR_NULL;
+    const size_t e = (size_t)element_bytes(dtype);
+    if (off(dH, e) || off(dX, e) || off(dWg, e) || off(dWu, e)) return SPHATTN_ERR_ALIGN;
+    const Ffn p = ffn_plan(T, D, F, dtype, true, workspace);
+    if (!workspace || off(workspace, 16) || workspace_bytes < p.bytes) return SPHATTN_ERR_WORKSPACE;
+    const size_t x = (size_t)T * D * e, w = (size_t)F * D * e;
+    const Range written[] = {{dX, x}, {dWg, w}, {dWu, w}, {workspace, p.bytes}};
+    const Range read[] = {{X, x}, {Wg, w}, {Wu, w}, {dH, (size_t)T * F * e}};
+    if (any_meet(written, read)) return SPHATTN_ERR_ALIAS;
+    const hipStream_t s = (hipStream_t)stream;
+    switch (dtype) {
+    case SPHATTN_F32: return run_ffn_bwd<Store::F32>(p, X, Wg, Wu, dH, dX, dWg, dWu, gate, s);
+    case SPHATTN_BF16: return run_ffn_bwd<Store::Bf16>(p, X, Wg, Wu, dH, dX, dWg, dWu, gate, s);
+    default: return run_ffn_bwd<Store::F16>(p, X, Wg, Wu, dH, dX, dWg, dWu, gate, s);
+    }
 }
 
 }  // extern "C"

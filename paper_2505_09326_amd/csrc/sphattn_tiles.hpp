@@ -5,7 +5,10 @@
 
 namespace sphattn {
 
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+
 constexpr float kLowPart = 4096.f;                 // what the second fp16 part is multiplied by: below 2^-14 that type has fewer bits
+constexpr int kEndless = 1 << 20;                  // in place of the power of two of a row with an infinite element
 
 // ---- tile products -------------------------------------------------------------------------------------
 
@@ -38,19 +41,26 @@ __device__ __forceinline__ int across_slot(int k, int c) { return c ^ (2 * ((k &
 // The sum over k runs in steps of 32.  A step's part of the two operands is BP / 16 + BQ / 16 blocks of 1 KB, copied
 // straight into one of NBUF LDS buffers, NBUF - 1 steps ahead; a step's fragments are read from LDS while the matrix
 // instructions of the step before run, so that behind the one barrier per step the matrix pipe has its operands already.
-template <class T, bool HALF, bool PX, bool QX, int PAIRS>
+//
+// Beside one product there are two at once, P's and P2's rows with Q (Form::Two: a tile has BP / 2 of each, sixteen by sixteen in turn, so that fragments
+// 2 i and 2 i + 1 of a wave are the same p of either), and the sum of two, P Q and P2 Q2 one after the other (Form::Sum).  P2 and Q2 are of P's and Q's sizes.
+enum class Form { One, Two, Sum };
+
+template <class T, bool HALF, bool PX, bool QX, int PAIRS, Form FORM = Form::One>
 struct Product {
     f32x4 acc[T::FP][T::FQ];
 
     __device__ __forceinline__ void run(const Operand& P, const Operand& Q, int p0, int q0, int k0, int k_end,
-                                        SPH_LDS unsigned char* smem)
+                                        SPH_LDS unsigned char* smem, const Operand& P2 = Operand{}, const Operand& Q2 = Operand{})
     {
+        static_assert(FORM != Form::Two || (!PX && T::CP % 2 == 0), "");
+        static_assert(FORM != Form::Sum || PAIRS != 3, "");
         const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
         const int n16 = lane & 15, g = lane >> 4;
         const int wp = wave % T::WAVES_P, wq = wave / T::WAVES_P;
         const uint32_t lds0 = (uint32_t)(uintptr_t)smem;
         const int steps = (k_end - k0 + kStepK - 1) / kStepK;
-        const int total = steps * PAIRS;
+        const int total = steps * PAIRS * (FORM == Form::Sum ? 2 : 1);
 
         // A copy's lane: rows of k lie in blocks of 16 x 64 bytes, lane l on row l / 4 with the piece of its slot.  Across, the buffer
         // holds 32 whole rows of the tile, so that a copy fetches whole lines of memory, their 16-byte pieces exchanged by
@@ -68,7 +78,7 @@ struct Product {
 #pragma unroll
         for (int i = 0; i < T::COPIES; ++i) {
             const int b = i < T::CP ? wave * T::CP + i : (wave * T::CQ + (i - T::CP)) % (T::BQ / 16);
-            place(i < T::CP ? PX : QX, i < T::CP ? P : Q, i < T::CP ? p0 : q0, i < T::CP ? T::BP : T::BQ, b, voff[i]);
+            place(i < T::CP ? PX : QX, i < T::CP ? P : Q, i < T::CP ? p0 : q0, i < T::CP ? T::BP : T::BQ, FORM == Form::Two && i < T::CP ? b / 2 : b, voff[i]);
             at[i] = (i < T::CP ? 0 : T::BP * 64) + b * 1024;
         }
         // where the next step's part begins, and (rows of k) how many bytes or (across) how many rows are left.  All of it in
@@ -84,24 +94,28 @@ struct Product {
         int pair = 0, step = 0, copied = 0;        // of the next copies
         auto part_p = [&]() { return PAIRS == 3 ? pair == 0 : PAIRS == 6 ? (pair == 0 ? 2 : pair == 2 || pair == 3) : 0; };
         auto part_q = [&]() { return PAIRS == 3 ? pair == 1 : PAIRS == 6 ? (pair == 1 ? 2 : pair == 2 || pair == 4) : 0; };
-        Stream sp = start(PX, P, p0, T::BP, part_p()), sq = start(QX, Q, q0, T::BQ, part_q());
+        constexpr int ROWS_P = FORM == Form::Two ? T::BP / 2 : T::BP;
+        Stream sp = start(PX, P, p0, ROWS_P, part_p()), sq = start(QX, Q, q0, T::BQ, part_q());
+        Stream sp2 = FORM == Form::Two ? start(PX, P2, p0, ROWS_P, part_p()) : sp;
+        bool second = false;                       // Form::Sum: of the second product
         uint32_t to = lds0;
         auto words = [&](bool across, const Operand& A, const Stream& s, bool there) {
             const int left = there ? max(s.left, 0) : 0;
             return rsrc_words(s.base, (uint32_t)__builtin_amdgcn_readfirstlane(across ? min(left, kStepK) * A.ld : left));
         };
         // of the step that is copied next
-        i32x4 rp, rq;
+        i32x4 rp, rq, rp2;
         bool past = false;
         auto copy_begin = [&]() {
             const bool there = copied < total;
             rp = words(PX, P, sp, there);
+            if constexpr (FORM == Form::Two) rp2 = words(PX, P2, sp2, there);
             rq = words(QX, Q, sq, there);
             past = k0 * 2 + step * 64 + piece * 16 >= k_end * 2;   // pieces behind the end of the sum are zeros
         };
         auto copy_one = [&](int i) {
             const bool across = i < T::CP ? PX : QX;
-            copy_to_lds(i < T::CP ? rp : rq, to + at[i], !across && past ? 0x7fffffff : voff[i], 0);
+            copy_to_lds(i >= T::CP ? rq : FORM == Form::Two && i % 2 ? rp2 : rp, to + at[i], !across && past ? 0x7fffffff : voff[i], 0);
         };
         auto copy_end = [&]() {
             ++copied;
@@ -111,11 +125,17 @@ struct Product {
             sp.left -= PX ? kStepK : 64;
             sq.base += QX ? (long long)kStepK * Q.ld : 64;
             sq.left -= QX ? kStepK : 64;
-            if (PAIRS > 1 && step == steps && copied < total) {
+            if constexpr (FORM == Form::Two) {
+                sp2.base += 64;
+                sp2.left -= 64;
+            }
+            if ((PAIRS > 1 || FORM == Form::Sum) && step == steps && copied < total) {
                 step = 0;
                 ++pair;
-                sp = start(PX, P, p0, T::BP, part_p());
-                sq = start(QX, Q, q0, T::BQ, part_q());
+                if (FORM == Form::Sum && pair == PAIRS) second = true, pair = 0;
+                sp = start(PX, FORM == Form::Sum && second ? P2 : P, p0, ROWS_P, part_p());
+                sq = start(QX, FORM == Form::Sum && second ? Q2 : Q, q0, T::BQ, part_q());
+                if constexpr (FORM == Form::Two) sp2 = start(PX, P2, p0, ROWS_P, part_p());
             }
         };
         auto copy_step = [&]() {
@@ -289,6 +309,80 @@ __device__ __forceinline__ i32x4 join_fragments(i32x2 a, i32x2 b)
     // (odd rows of sixteen lanes of the first operand and even rows of the second change places)
     asm volatile("s_nop 1\n\tv_permlane16_swap_b32 %0, %2\n\tv_permlane16_swap_b32 %1, %3\n\ts_nop 1" : "+v"(a0), "+v"(a1), "+v"(b0), "+v"(b1));
     return i32x4{a0, a1, b0, b1};
+}
+
+// D = A (16 x 4) B (4 x 16) + C on element ea of a's registers and eb of b's
+__device__ __forceinline__ f32x4 mfma_f32(i32x4 a, int ea, i32x4 b, int eb, f32x4 c)
+{
+    const int x = a[ea], y = b[eb];                // (a bit cast of the vector's element itself takes the vector's first)
+    return __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, x), __builtin_bit_cast(float, y), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mfma_f32(i32x4 a, i32x4 b, int e, f32x4 c) { return mfma_f32(a, e, b, e, c); }
+
+__device__ __forceinline__ float max_over_wave(float x)
+{
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) x = fmaxf(x, __shfl_xor(x, d));
+    return x;
+}
+
+// Rows as the products want them: 16-bit, 16-byte aligned, whole pieces of 8; fp32 in parts.  One wave per row.
+struct PackRows {
+    const void* in; void* out; int n, D, ld;       // (ld: elements per row of out, a multiple of 8)
+    long long part;                                // elements from part to part
+    void* sum_out;                                 // fp32: the three parts that the products with G take, or NULL
+    int* exp;                                      // fp32: for the logits, the power of two that the row was divided by
+};
+template <Store S>
+__device__ __forceinline__ void pack_row(const PackRows& a, long long t, long long m, int lane)
+{
+    if (!a.out) return;                            // (few rows of fp32 are read where they are)
+    const size_t from = (size_t)t * a.D, to = (size_t)m * a.ld;
+    constexpr int N = per16<S>();
+    const bool wide = ((uintptr_t)a.in & 15) == 0 && a.D % N == 0;
+    auto load = [&](int c) { return wide ? load16<S, true>(a.in, from + c, N, N) : load16<S, false>(a.in, from + c, a.D - c, (size_t)a.n * a.D - from - c); };
+    int up = 0;
+    if constexpr (S == Store::F32) {               // the row's largest finite element goes to 2^14 .. 2^15
+        float top = 0.f;
+        bool endless = false;
+        for (int c = lane * N; c < a.D; c += 64 * N) {
+            float x[N];
+            widen16<S>(load(c), x);
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float size = __builtin_fabsf(x[i]);
+                top = size < __builtin_inff() ? fmaxf(top, size) : top;
+                endless |= size == __builtin_inff();
+            }
+        }
+        top = max_over_wave(top);
+        up = top > 0.f ? 15 - __builtin_amdgcn_frexp_expf(top) : 0;
+        if (__ballot(endless) && lane == 0) a.exp[m] = kEndless;
+        else if (lane == 0) a.exp[m] = -up;
+    }
+    for (int c = lane * N; c < a.ld; c += 64 * N) {
+        i32x4 w = {0, 0, 0, 0};
+        if (c < a.D) w = load(c);
+        if constexpr (S == Store::F32) {
+            float x[4];
+            widen16<S>(w, x);
+            i32x2 hi, lo;
+            if (a.sum_out) {
+                i32x2 part[3];
+                split3(x, part);
+#pragma unroll
+                for (int k = 0; k < 3; ++k) *(i32x2*)((unsigned short*)a.sum_out + to + c + k * a.part) = part[k];
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x[r] = __builtin_ldexpf(x[r], up);
+            split2(x, hi, lo);
+            unsigned short* o = (unsigned short*)a.out + to + c;
+            *(i32x2*)o = hi;
+            *(i32x2*)(o + a.part) = lo;
+        } else {
+            *(i32x4*)((unsigned short*)a.out + to + c) = w;
+        }
+    }
 }
 
 }  // namespace sphattn

@@ -3,7 +3,7 @@
 #include "sphattn_embed.hpp"
 #include "sphattn_vocab.hpp"
 #include "sphattn_clip.hpp"
-#include "sphattn_host.hpp"
+#include "sphattn_tile_choice.hpp"
 #include "../../include/sphattn_train.h"
 
 #include <climits>
@@ -95,8 +95,6 @@ int run_embed_bwd(const EmbedPlan& p, const void* tokens, int id_bytes, const fl
 
 // ---- vocabulary loss ---------------------------------------------------------------------------------
 
-using Big = Tile<256, 256, 2, 4, 4>;               // eight waves of 128 x 64: one workgroup per CU
-using Mid = Tile<128, 128, 2, 2, 4>;               // four of 64 x 64: two per CU
 using Low = Tile<128, 64, 4, 1, 4>;                // up to 64 rows
 using Few = Tile<128, 32, 4, 1, 4>;                // fp32: up to 32 rows (17 x 50000 x 1024 logits 111 -> 68 us: its matrix instruction is the slow one)
 using One = Tile<128, 16, 4, 1, 6>;                // up to 16 rows
@@ -107,16 +105,6 @@ using One = Tile<128, 16, 4, 1, 6>;                // up to 16 rows
 constexpr size_t kPieceBytes = 256u << 20, kOnePieceBytes = 400u << 20;
 
 bool vocab_shape(int T, int V, int D) { return T >= 0 && T <= 1 << 20 && V >= 1 && V <= 1 << 24 && D >= 1 && D <= 65536; }
-
-long long up_to(long long x, long long m) { return (x + m - 1) / m * m; }
-
-// The tile of fewest rounds of the CUs' time: a Mid tile takes 0.36 of a Big one's in a CU that runs two of them
-bool big_tiles(long long p, long long q)
-{
-    const long long big = ((p + 255) / 256) * ((q + 255) / 256), mid = ((p + 127) / 128) * ((q + 127) / 128);
-    const double big_time = (double)((big + kCus - 1) / kCus), mid_time = 0.72 * (double)((mid + 2 * kCus - 1) / (2 * kCus));
-    return big_time <= mid_time;
-}
 
 struct Vocab {
     int T, V, D, parts, ld;                        // parts: of X and W for the logits; ld: elements per packed row
@@ -269,9 +257,6 @@ int launch_scores(VocabArgs& a, int V, int T, int& tiles_p, hipStream_t stream)
     tiles_p = a.tiles_p;
     return rc;
 }
-
-// whether the products can read rows of D elements at p as they are
-bool ready(const void* p, int D, Store S) { return S != Store::F32 && !off(p, 16) && D % 8 == 0; }
 
 RowArgs row_args(const Vocab& p, const void* targets, int id_bytes)
 {

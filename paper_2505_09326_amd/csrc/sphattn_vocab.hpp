@@ -43,10 +43,6 @@ struct VocabInfo {
     int even;                                      // one gradient per row, fp16: all of them within 2^4 of the largest, so that one `up` serves every row
 };
 
-constexpr int kEndless = 1 << 20;                  // in place of the power of two of a row with an infinite element
-
-constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
-
 struct VocabArgs {
     Operand P, Q;
     const VocabInfo* info;                         // NULL: all rows of Q count
@@ -80,14 +76,6 @@ __device__ __forceinline__ int dx_slices(int rows, int T, int slices, int tile_q
     const int room = (int)min((long long)tq_all * slices / tq, (long long)T * slices / rows);
     return max(slices, min(min(room, 32), target / (tq * tiles_p)));
 }
-
-// D = A (16 x 4) B (4 x 16) + C on element ea of a's registers and eb of b's
-__device__ __forceinline__ f32x4 mfma_f32(i32x4 a, int ea, i32x4 b, int eb, f32x4 c)
-{
-    const int x = a[ea], y = b[eb];                // (a bit cast of the vector's element itself takes the vector's first)
-    return __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, x), __builtin_bit_cast(float, y), c, 0, 0, 0);
-}
-__device__ __forceinline__ f32x4 mfma_f32(i32x4 a, i32x4 b, int e, f32x4 c) { return mfma_f32(a, e, b, e, c); }
 
 // fp32 with at most 64 rows: W decides the time, so it is read as it is, once, straight into registers, and multiplied by the fp32 matrix
 // instruction (16x16x4, a twelfth of the 16-bit rate: 64 rows of width 1024 take it as long as their W takes memory).  Lane (i, g) holds four neighbouring
@@ -594,13 +582,6 @@ __device__ __forceinline__ VocabInfo row_scale(const RowArgs& a, int n, float to
     return out;
 }
 
-__device__ __forceinline__ float max_over_wave(float x)
-{
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) x = fmaxf(x, __shfl_xor(x, d));
-    return x;
-}
-
 // |x| among those that `least` is the smallest of
 __device__ __forceinline__ float smaller(float least, float x)
 {
@@ -673,12 +654,6 @@ void vocab_rows_kernel(RowArgs a)
 // own count, which spares a launch of one workgroup in front.
 constexpr int kPackThreads = 256, kPackRows = kPackThreads / 64, kOwnRows = 1024;
 
-struct PackRows {
-    const void* in; void* out; int n, D, ld;       // (ld: elements per row of out, a multiple of 8)
-    long long part;                                // elements from part to part
-    void* sum_out;                                 // fp32: the three parts that the products with G take, or NULL
-    int* exp;                                      // fp32: for the logits, the power of two that the row was divided by
-};
 struct PackArgs {
     PackRows x, w;
     int x_groups;                                  // workgroups on X, the rest on W
@@ -687,58 +662,6 @@ struct PackArgs {
     const float* lse; int* g_target; float* g_lse2; float* g;   // what the G stage needs of each row, or NULL
     float *g_own, *own_down;                       // fp16, one gradient per row: g of dX's own G and the factor of dX's rows, or NULL
 };
-
-template <Store S>
-__device__ __forceinline__ void pack_row(const PackRows& a, long long t, long long m, int lane)
-{
-    if (!a.out) return;                            // (few rows of fp32 are read where they are)
-    const size_t from = (size_t)t * a.D, to = (size_t)m * a.ld;
-    constexpr int N = per16<S>();
-    const bool wide = ((uintptr_t)a.in & 15) == 0 && a.D % N == 0;
-    auto load = [&](int c) { return wide ? load16<S, true>(a.in, from + c, N, N) : load16<S, false>(a.in, from + c, a.D - c, (size_t)a.n * a.D - from - c); };
-    int up = 0;
-    if constexpr (S == Store::F32) {               // the row's largest finite element goes to 2^14 .. 2^15
-        float top = 0.f;
-        bool endless = false;
-        for (int c = lane * N; c < a.D; c += 64 * N) {
-            float x[N];
-            widen16<S>(load(c), x);
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const float size = __builtin_fabsf(x[i]);
-                top = size < __builtin_inff() ? fmaxf(top, size) : top;
-                endless |= size == __builtin_inff();
-            }
-        }
-        top = max_over_wave(top);
-        up = top > 0.f ? 15 - __builtin_amdgcn_frexp_expf(top) : 0;
-        if (__ballot(endless) && lane == 0) a.exp[m] = kEndless;
-        else if (lane == 0) a.exp[m] = -up;
-    }
-    for (int c = lane * N; c < a.ld; c += 64 * N) {
-        i32x4 w = {0, 0, 0, 0};
-        if (c < a.D) w = load(c);
-        if constexpr (S == Store::F32) {
-            float x[4];
-            widen16<S>(w, x);
-            i32x2 hi, lo;
-            if (a.sum_out) {
-                i32x2 part[3];
-                split3(x, part);
-#pragma unroll
-                for (int k = 0; k < 3; ++k) *(i32x2*)((unsigned short*)a.sum_out + to + c + k * a.part) = part[k];
-            }
-#pragma unroll
-            for (int r = 0; r < 4; ++r) x[r] = __builtin_ldexpf(x[r], up);
-            split2(x, hi, lo);
-            unsigned short* o = (unsigned short*)a.out + to + c;
-            *(i32x2*)o = hi;
-            *(i32x2*)(o + a.part) = lo;
-        } else {
-            *(i32x4*)((unsigned short*)a.out + to + c) = w;
-        }
-    }
-}
 
 template <Store S>
 __global__ __launch_bounds__(kPackThreads)
