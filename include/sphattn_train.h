@@ -90,6 +90,34 @@ int sphattn_vocab_loss_bwd(const void* X, const void* W, const void* targets, in
                            void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * Divergence of that head's softmax from a teacher's K best logits, at a temperature tau:
+ *   l[t,v] = (scale / tau) X[t,:] . W[v,:]     lse[t] = log(sum over v of exp l[t,v])     p[t,:] = softmax(teacher[t,:] / tau) over the row's entries
+ *   losses[t] = tau^2 sum over k of p[t,k] (log p[t,k] - l[t,ids[t,k]] + lse[t])          (entries of p 0 add nothing)
+ *   ids, teacher : [T,K], in any order.  A negative id is no entry, whatever its logit; a logit of minus infinity has p 0.  A row in which nothing else
+ *   is left does not count: its loss and lse are 0 and its gradients are zeros.  An id that is there twice has both p.  An id >= V is a mistake that
+ *   only the device can see: the row's loss and lse are NaN, and so are the gradients that it takes part in.
+ *   losses, lse : [T] fp32.  kept : [T,K] fp32 or NULL (no gradients are wanted): what the backward call takes, entries in an order of the library's.
+ *   mean, reduction, dtypes, sizes, precision and workspaces as for sphattn_vocab_loss_fwd (the logits have its errors), all_rows 0.
+ * 1 <= K <= 1024 (SPHATTN_ERR_SHAPE); 2^-20 <= tau <= 2^20 and scale / tau finite (SPHATTN_ERR_VALUE).
+ */
+size_t sphattn_vocab_distill_workspace_bytes(int T, int V, int D, int K, int dtype);
+int sphattn_vocab_distill_fwd(const void* X, const void* W, const void* ids, int id_bytes, const float* teacher,
+                              float* losses, float* lse, float* kept, float* mean,
+                              int T, int V, int D, int K, float scale, float temperature, int reduction, int dtype,
+                              void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Gradients of that:  G[t,v] = g[t] tau^2 (exp(l[t,v] - lse[t]) - sum of p[t,k] over the entries with ids[t,k] == v) for rows that count, 0 for others
+ *                     dX = (scale / tau) G W      dW = (scale / tau) G^T X
+ *   lse, kept : from the forward call.  The rest as for sphattn_vocab_loss_bwd.
+ */
+size_t sphattn_vocab_distill_bwd_workspace_bytes(int T, int V, int D, int K, int dtype);
+int sphattn_vocab_distill_bwd(const void* X, const void* W, const void* ids, int id_bytes, const float* teacher,
+                              const float* lse, const float* kept, const float* dloss, void* dX, void* dW,
+                              int T, int V, int D, int K, float scale, float temperature, int reduction, int dtype,
+                              void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Clipping of gradients by their common 2-norm:
  *   norm = sqrt(sum over all elements of all tensors of in^2)      out[i] = in[i] * min(1, max_norm / (norm + 1e-6))
  *   in, out : host arrays of n device pointers; out[i] may be in[i] (then it is not written where the factor

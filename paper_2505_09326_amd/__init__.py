@@ -51,6 +51,8 @@ EXPORTED_SYMBOLS = ("sphattn_fwd", "sphattn_fwd_z", "sphattn_fwd_tile_rows", "sp
                     "sphattn_embed_fwd", "sphattn_embed_bwd_workspace_bytes", "sphattn_embed_bwd",
                     "sphattn_vocab_loss_workspace_bytes", "sphattn_vocab_loss_fwd",
                     "sphattn_vocab_loss_bwd_workspace_bytes", "sphattn_vocab_loss_bwd",
+                    "sphattn_vocab_distill_workspace_bytes", "sphattn_vocab_distill_fwd",
+                    "sphattn_vocab_distill_bwd_workspace_bytes", "sphattn_vocab_distill_bwd",
                     "sphattn_clip_grads_workspace_bytes", "sphattn_clip_grads",
                     "sphattn_head_norm_rotary_fwd", "sphattn_head_norm_rotary_bwd_workspace_bytes", "sphattn_head_norm_rotary_bwd",
                     "sphattn_gated_ffn_workspace_bytes", "sphattn_gated_ffn_fwd", "sphattn_gated_ffn_bwd_workspace_bytes", "sphattn_gated_ffn_bwd",
@@ -147,6 +149,14 @@ def load_library() -> ctypes.CDLL:
         lib.sphattn_vocab_loss_fwd.argtypes = [vp, vp, vp, ip, vp, vp, vp, ip, ip, ip, fl, ip, ip, ip, vp, sz, vp]
         lib.sphattn_vocab_loss_bwd.restype = ip
         lib.sphattn_vocab_loss_bwd.argtypes = [vp, vp, vp, ip, vp, vp, vp, vp, ip, ip, ip, fl, ip, ip, vp, sz, vp]
+        for name in ("sphattn_vocab_distill_workspace_bytes", "sphattn_vocab_distill_bwd_workspace_bytes"):
+            fn = getattr(lib, name)
+            fn.restype = sz
+            fn.argtypes = [ip] * 5
+        lib.sphattn_vocab_distill_fwd.restype = ip
+        lib.sphattn_vocab_distill_fwd.argtypes = [vp, vp, vp, ip, vp, vp, vp, vp, vp, ip, ip, ip, ip, fl, fl, ip, ip, vp, sz, vp]
+        lib.sphattn_vocab_distill_bwd.restype = ip
+        lib.sphattn_vocab_distill_bwd.argtypes = [vp, vp, vp, ip, vp, vp, vp, vp, vp, vp, ip, ip, ip, ip, fl, fl, ip, ip, vp, sz, vp]
         lib.sphattn_clip_grads_workspace_bytes.restype = sz
         lib.sphattn_clip_grads_workspace_bytes.argtypes = [ip]
         lib.sphattn_clip_grads.restype = ip
@@ -953,6 +963,95 @@ def sphattn_vocab_loss_bwd(X, W, targets, lse, dloss, scale=1.0, reduction="none
     ws, ws_bytes = _scratch(workspace, lib.sphattn_vocab_loss_bwd_workspace_bytes(T, V, D, code), X)
     _raise_on(lib.sphattn_vocab_loss_bwd(X.data_ptr(), W.data_ptr(), targets.data_ptr(), id_bytes, lse.data_ptr(), dloss.data_ptr(),
                                          _ptr(dX), _ptr(dW), T, V, D, scale, red, code, ws.data_ptr(), ws_bytes, _stream_of(X, stream)))
+    return dX, dW
+
+
+# ---- divergence from a teacher's logits over the vocabulary ---------------------------------------------
+
+def _taught(X, W, ids, teacher):
+    T, D = _matrix("X", X)
+    V, _ = _matrix("W", W)
+    code = _code_of("X", X)
+    _, K = _matrix("ids", ids)
+    _need("ids", ids, (T, K), tuple(_id_types()))
+    _need("X", X, (T, D), (X.dtype,))
+    _need("W", W, (V, D), (X.dtype,))
+    _f32("teacher", teacher, (T, K), optional=False)
+    return T, V, D, K, code, _id_types()[ids.dtype]
+
+
+def _temperature(x):
+    x = float(x)
+    if not 2.0 ** -20 <= x <= 2.0 ** 20:
+        raise ValueError(f"temperature must be from 2^-20 to 2^20, got {x}")
+    return x
+
+
+def sphattn_vocab_distill_workspace_bytes(T, V, D, K, dtype="bf16") -> int:
+    return int(load_library().sphattn_vocab_distill_workspace_bytes(T, V, D, K, _dtype_code(dtype)))
+
+
+def sphattn_vocab_distill_bwd_workspace_bytes(T, V, D, K, dtype="bf16") -> int:
+    return int(load_library().sphattn_vocab_distill_bwd_workspace_bytes(T, V, D, K, _dtype_code(dtype)))
+
+
+def sphattn_vocab_distill_fwd(X, W, ids, teacher, scale=1.0, temperature=1.0, reduction="none", keep=False, losses=None, lse=None, kept=None, mean=None,
+                              workspace=None, stream=None):
+    """Divergence of softmax(scale / temperature X W^T) from a teacher's best logits: X [T,D], W [V,D] (fp32, bf16 or fp16), ids [T,K] int32 or
+    int64 (negative: no entry; not below V: NaN), teacher [T,K] fp32, its logits of those ids, whose softmax at the temperature is what the row is
+    compared with; times temperature^2.  Rows without an entry do not count.  Returns (losses [T], lse [T]) in fp32, with keep=True then kept [T,K] for the
+    gradients, and with reduction "sum" or "mean" last that of the rows that count."""
+    import torch
+    lib = load_library()
+    red = REDUCTIONS[reduction]
+    scale, temperature = _finite("scale", scale), _temperature(temperature)
+    T, V, D, K, code, id_bytes = _taught(X, W, ids, teacher)
+    keep = bool(keep) or kept is not None
+    _brought(stream, losses=losses, lse=lse, workspace=workspace, **({"mean": mean} if red else {}), **({"kept": kept} if keep else {}))
+    _on_device(X=X, W=W, ids=ids, teacher=teacher, losses=losses, lse=lse, kept=kept, mean=mean, workspace=workspace)
+    losses = torch.empty(T, dtype=torch.float32, device=X.device) if losses is None else losses
+    lse = torch.empty(T, dtype=torch.float32, device=X.device) if lse is None else lse
+    if keep and kept is None:
+        kept = torch.empty((T, K), dtype=torch.float32, device=X.device)
+    if red and mean is None:
+        mean = torch.empty((), dtype=torch.float32, device=X.device)
+    _f32("losses", losses, (T,))
+    _f32("lse", lse, (T,))
+    _f32("kept", kept, (T, K))
+    _f32("mean", mean, ())
+    ws, ws_bytes = _scratch(workspace, lib.sphattn_vocab_distill_workspace_bytes(T, V, D, K, code), X)
+    _raise_on(lib.sphattn_vocab_distill_fwd(X.data_ptr(), W.data_ptr(), ids.data_ptr(), id_bytes, teacher.data_ptr(), losses.data_ptr(), lse.data_ptr(),
+                                            _ptr(kept), _ptr(mean), T, V, D, K, scale, temperature, red, code, ws.data_ptr(), ws_bytes, _stream_of(X, stream)))
+    return (losses, lse) + ((kept,) if keep else ()) + ((mean,) if red else ())
+
+
+def sphattn_vocab_distill_bwd(X, W, ids, teacher, lse, kept, dloss, scale=1.0, temperature=1.0, reduction="none", dX=None, dW=None, want_dX=True, want_dW=True,
+                              workspace=None, stream=None):
+    """Gradients (dX, dW) of the losses of sphattn_vocab_distill_fwd: lse [T] and kept [T,K] from it; dloss fp32, [T] with reduction "none" and one
+    value with "sum" and "mean".  One of the two may be not wanted (None in its place).  None of the teacher's logits."""
+    import torch
+    lib = load_library()
+    red = REDUCTIONS[reduction]
+    scale, temperature = _finite("scale", scale), _temperature(temperature)
+    if not want_dX and not want_dW:
+        raise ValueError("neither dX nor dW is wanted")
+    T, V, D, K, code, id_bytes = _taught(X, W, ids, teacher)
+    _f32("lse", lse, (T,), optional=False)
+    _f32("kept", kept, (T, K), optional=False)
+    _f32("dloss", dloss, () if red else (T,), optional=False)
+    _brought(stream, workspace=workspace, **({"dX": dX} if want_dX else {}), **({"dW": dW} if want_dW else {}))
+    _on_device(X=X, W=W, ids=ids, teacher=teacher, lse=lse, kept=kept, dloss=dloss, dX=dX, dW=dW, workspace=workspace)
+    if want_dX and dX is None:
+        dX = torch.empty_like(X)
+    if want_dW and dW is None:
+        dW = torch.empty_like(W)
+    dX, dW = dX if want_dX else None, dW if want_dW else None
+    _need("dX", dX, (T, D), (X.dtype,), optional=True)
+    _need("dW", dW, (V, D), (X.dtype,), optional=True)
+    ws, ws_bytes = _scratch(workspace, lib.sphattn_vocab_distill_bwd_workspace_bytes(T, V, D, K, code), X)
+    _raise_on(lib.sphattn_vocab_distill_bwd(X.data_ptr(), W.data_ptr(), ids.data_ptr(), id_bytes, teacher.data_ptr(), lse.data_ptr(), kept.data_ptr(),
+                                            dloss.data_ptr(), _ptr(dX), _ptr(dW), T, V, D, K, scale, temperature, red, code, ws.data_ptr(), ws_bytes,
+                                            _stream_of(X, stream)))
     return dX, dW
 
 

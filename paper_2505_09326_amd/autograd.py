@@ -8,6 +8,7 @@
     Q, K = head_norm_rotary(Xq, Xk, wq, wk, positions, inv_freq)      # norms of heads, rotated by positions, as the attention reads them
     H = gated_feed_forward(X, Wg, Wu)                    # silu(X Wg^T) * (X Wu^T)
     loss = vocab_cross_entropy(X, W, targets)            # -log softmax(X W^T)[targets], no logits in memory
+    loss = vocab_distillation(X, W, ids, teacher)        # softmax(X W^T) against a teacher's best logits
 
 Forward = sphattn_fwd_z (O and the row aggregates z, which the backward needs), or
 sphattn_cross_fwd when multiplicities or shared K/V heads are given; backward = the library's
@@ -19,7 +20,8 @@ import torch
 from torch.autograd.function import once_differentiable
 
 from . import (REDUCTIONS, _cross_fwd_z, _fast_calls, sphattn_bwd, sphattn_embed_bwd, sphattn_embed_fwd, sphattn_fwd_z, sphattn_gated_ffn_bwd,
-               sphattn_gated_ffn_fwd, sphattn_grn_bwd, sphattn_head_norm_rotary_bwd, sphattn_head_norm_rotary_fwd, sphattn_vocab_loss_bwd, sphattn_vocab_loss_fwd)
+               sphattn_gated_ffn_fwd, sphattn_grn_bwd, sphattn_head_norm_rotary_bwd, sphattn_head_norm_rotary_fwd, sphattn_vocab_distill_bwd,
+               sphattn_vocab_distill_fwd, sphattn_vocab_loss_bwd, sphattn_vocab_loss_fwd)
 
 _DTYPES = {torch.bfloat16: "bf16", torch.float16: "f16"}
 
@@ -173,3 +175,35 @@ def gated_feed_forward(X, Wg, Wu, activation="silu"):
     """Differentiable act(X Wg^T) * (X Wu^T): X [..., D], Wg and Wu [F,D] of one type (fp32, bf16 or fp16), activation "silu", "gelu" or "relu".  Nothing but
     the inputs is kept for the gradients."""
     return _GatedFeedForward.apply(X, Wg, Wu, activation)
+
+
+class _VocabDistillation(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, X, W, ids, teacher, scale, temperature, reduction):
+        if X.dtype != W.dtype:
+            raise TypeError(f"X and W must have one dtype, got {X.dtype} and {W.dtype}")
+        if ids.dim() < 1 or X.shape[:-1] != ids.shape[:-1] or teacher.shape != ids.shape:
+            raise ValueError(f"ids and teacher must be [..., K] with X's rows {tuple(X.shape[:-1])}, got {tuple(ids.shape)} and {tuple(teacher.shape)}")
+        ctx.shape, ctx.how = X.shape, (scale, temperature, reduction)
+        X, W = X.reshape(-1, X.shape[-1]).contiguous(), W.contiguous()
+        ids, teacher = (t.reshape(-1, t.shape[-1]).contiguous() for t in (ids, teacher))
+        losses, lse, kept, *mean = sphattn_vocab_distill_fwd(X, W, ids, teacher, *ctx.how, keep=True)
+        ctx.save_for_backward(X, W, ids, teacher, lse, kept)
+        return mean[0] if mean else losses.view(ctx.shape[:-1])
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dloss):
+        X, W, ids, teacher, lse, kept = ctx.saved_tensors
+        if ctx.how[2] == "none":
+            dloss = dloss.reshape(-1)
+        dX, dW = sphattn_vocab_distill_bwd(X, W, ids, teacher, lse, kept, dloss.contiguous(), *ctx.how, want_dX=ctx.needs_input_grad[0],
+                                           want_dW=ctx.needs_input_grad[1])
+        return None if dX is None else dX.view(ctx.shape), dW, None, None, None, None, None
+
+
+def vocab_distillation(X, W, ids, teacher, scale=1.0, temperature=1.0, reduction="mean"):
+    """Differentiable divergence of softmax(scale / temperature X W^T) over a vocabulary from a teacher's best logits, times temperature^2, in fp32: X [..., D]
+    and W [V,D] of one type (fp32, bf16 or fp16), ids [..., K] (int32 or int64; negative: no entry), teacher [..., K] (fp32, its logits of those ids, no
+    gradient).  reduction "mean" (over the rows with an entry; 0 if there is none), "sum" or "none"."""
+    return _VocabDistillation.apply(X, W, ids, teacher, scale, temperature, reduction)

@@ -208,6 +208,44 @@ Vocab vocab_bwd_plan(int T, int V, int D, int dtype, void* workspace)
     return p;
 }
 
+// A teacher's part of a call
+struct Teacher {
+    int K, padded, shift, blocks;
+    float tau;
+    int *targets, *sorted;
+    float *weights, *logits;                       // (logits: the caller's)
+    unsigned short* starts;
+    size_t bytes;
+};
+
+bool teacher_shape(int T, int V, int D, int K) { return vocab_shape(T, V, D) && K >= 1 && K <= kTaughtMost; }
+
+// Its workspace lies behind the loss's own.  Blocks of 128 ids, half of a Big tile's, as long as where they begin in each row takes no more than 256 MB.
+Teacher teacher_plan(int T, int V, int K, bool back, bool keep, size_t behind, void* workspace)
+{
+    Teacher p{};
+    p.K = K, p.padded = 2;
+    while (p.padded < K) p.padded *= 2;
+    auto blocks = [&] { return (V + (128 << p.shift) - 1) / (128 << p.shift); };
+    while (p.shift < 17 && (size_t)T * (blocks() + 1) * 2 > 256u << 20) ++p.shift;
+    p.blocks = blocks();
+    Carve c(workspace ? (unsigned char*)workspace + behind : nullptr);
+    p.targets = c.take<int>(T);
+    p.sorted = c.take<int>((size_t)T * K);
+    p.weights = c.take<float>((size_t)T * K);
+    if (!back) p.starts = c.take<unsigned short>((size_t)T * (p.blocks + 1));
+    if (keep) p.logits = c.take<float>((size_t)T * K);
+    p.bytes = behind + c.used();
+    return p;
+}
+
+int launch_teacher(const Teacher& p, const void* ids, int id_bytes, const float* teacher, int T, int V, hipStream_t stream)
+{
+    hipLaunchKernelGGL(taught_kernel, dim3((unsigned)(T + kTaughtWaves - 1) / kTaughtWaves), dim3(kTaughtThreads), (size_t)taught_lds_bytes(p.padded), stream,
+                       ids, id_bytes, teacher, T, V, p.K, p.padded, 1.f / p.tau, p.targets, p.sorted, p.weights, p.starts, p.shift, p.blocks);
+    return launched();
+}
+
 template <class T, Store S, Stage ST>
 int launch_tiles(VocabArgs& a, int p, int q, hipStream_t stream)
 {
@@ -289,7 +327,7 @@ void pack(const Vocab& p, const void* X, const void* W, bool pack_x, PackArgs k,
 
 template <Store S>
 int run_vocab_fwd(const Vocab& p, const void* X, const void* W, const void* targets, int id_bytes, float* losses, float* lse, float* mean,
-                  float scale, int reduction, int all_rows, hipStream_t stream)
+                  float scale, int reduction, int all_rows, hipStream_t stream, const Teacher* teacher = nullptr)
 {
     VocabArgs a{};
     PackArgs k{};
@@ -307,23 +345,36 @@ int run_vocab_fwd(const Vocab& p, const void* X, const void* W, const void* targ
     a.slices = 1, a.V = p.V, a.scale2 = scale * kLog2e;
     a.targets = targets, a.id_bytes = id_bytes;
     a.partial = p.partial, a.partial_ld = p.T, a.target_logit = p.target_logit;
+    if (teacher) a.taught = Taught{teacher->sorted, teacher->starts, teacher->logits, teacher->K, teacher->shift, teacher->blocks};
     int tiles = 0;
-    const int rc = launch_scores<S, Stage::Logits>(a, p.V, p.T, tiles, stream);
+    const int rc = teacher ? launch_scores<S, Stage::Taught>(a, p.V, p.T, tiles, stream) : launch_scores<S, Stage::Logits>(a, p.V, p.T, tiles, stream);
     if (rc != SPHATTN_OK) return rc;
     if (reduction == SPHATTN_LOSS_NONE) mean = nullptr;
-    const bool at_once = mean && p.T <= 64 && (long long)tiles * p.T <= 16 * kJoinLossThreads;   // one workgroup, 16 sums per lane at most
+    const bool at_once = mean && !teacher && p.T <= 64 && (long long)tiles * p.T <= 16 * kJoinLossThreads;   // one workgroup, 16 sums per lane at most
     int log_rows = 0;                              // rows of a joining workgroup: half a round of the CUs where they are few
     while (log_rows < 6 && (p.T >> log_rows) > (at_once ? 0 : kCus / 2)) ++log_rows;
     hipLaunchKernelGGL(vocab_join_kernel, dim3((unsigned)(p.T + (1 << log_rows) - 1) >> log_rows), dim3(kJoinLossThreads), 0, stream, p.partial, p.T, tiles,
-                       log_rows, p.target_logit, targets, id_bytes, k.compact ? p.place : (const int*)nullptr, all_rows, losses, lse,
+                       log_rows, teacher ? (const float*)nullptr : p.target_logit, targets, id_bytes, k.compact ? p.place : (const int*)nullptr, all_rows, losses, lse,
                        at_once ? mean : (float*)nullptr, reduction == SPHATTN_LOSS_MEAN, p.T, p.V);
+    if (teacher)
+        hipLaunchKernelGGL(taught_loss_kernel, dim3((unsigned)(p.T + 3) / 4), dim3(256), 0, stream, teacher->targets, teacher->sorted, teacher->weights, teacher->logits,
+                           lse, p.T, teacher->K, teacher->tau * teacher->tau, losses);
     if (mean && !at_once)
         hipLaunchKernelGGL(vocab_mean_kernel, dim3(1), dim3(1024), 0, stream, losses, targets, id_bytes, p.T, mean, reduction == SPHATTN_LOSS_MEAN);
     return launched();
 }
 
+// The teacher's weights taken off a piece of G
+template <Store S, bool WHOLE>
+int launch_taught_g(const Teacher& p, const VocabArgs& a, const int* rows, int n, hipStream_t stream)
+{
+    hipLaunchKernelGGL((taught_g_kernel<S, WHOLE>), dim3((unsigned)(a.Q.size + 3) / 4), dim3(256), 0, stream, a.info, rows, p.sorted, p.weights, p.logits, a.g_lse2, a.g,
+                       a.unless_even, p.K, a.v0, n, a.G, a.G_part, a.G_ld);
+    return launched();
+}
+
 // fp32, at most 64 rows
-int run_rows_bwd(const Vocab& p, const void* X, const void* W, PackArgs k, void* dX, void* dW, float scale, hipStream_t stream)
+int run_rows_bwd(const Vocab& p, const void* X, const void* W, PackArgs k, void* dX, void* dW, float scale, hipStream_t stream, const Teacher* teacher)
 {
     constexpr Store S = Store::F32;
     // which rows count and what G needs of them; no parts are made
@@ -338,7 +389,8 @@ int run_rows_bwd(const Vocab& p, const void* X, const void* W, PackArgs k, void*
         a.info = p.info, a.rows = p.rows, a.k = p.D, a.T = p.T, a.slices = 1, a.V = p.V, a.v0 = v0, a.scale2 = scale * kLog2e;
         a.g_target = p.g_target, a.g_lse2 = p.g_lse2, a.g = p.g, a.G = p.G, a.G_ld = p.piece;
         int tiles;
-        const int rc = launch_scores<S, Stage::G>(a, n, p.T, tiles, stream);
+        int rc = launch_scores<S, Stage::G>(a, n, p.T, tiles, stream);
+        if (rc == SPHATTN_OK && teacher) rc = launch_taught_g<S, true>(*teacher, a, p.rows, n, stream);
         if (rc != SPHATTN_OK) return rc;
         if (dX) {
             a.slices = p.slices, a.out = p.dx, a.out_ld = p.ld, a.accumulate = i > 0;
@@ -360,11 +412,12 @@ int run_rows_bwd(const Vocab& p, const void* X, const void* W, PackArgs k, void*
 
 template <Store S>
 int run_vocab_bwd(const Vocab& p, const void* X, const void* W, const void* targets, int id_bytes, const float* lse, const float* dloss,
-                  void* dX, void* dW, float scale, int reduction, hipStream_t stream)
+                  void* dX, void* dW, float scale, int reduction, hipStream_t stream, const Teacher* teacher = nullptr)
 {
     PackArgs k{};
     k.r = row_args(p, targets, id_bytes);
-    k.r.dloss = dloss, k.r.reduce = (Reduce)reduction, k.r.scale = scale, k.r.half = S == Store::F16;
+    k.r.dloss = dloss, k.r.reduce = (Reduce)reduction, k.r.scale = teacher ? scale * teacher->tau * teacher->tau : scale, k.r.half = S == Store::F16;
+    k.no_target = teacher != nullptr;
     k.compact = 1, k.lse = lse, k.g_target = p.g_target, k.g_lse2 = p.g_lse2, k.g = p.g;
     // fp16 and one gradient per row: dX's G is scaled row by row, dW's by the largest gradient
     const bool own = S == Store::F16 && reduction == SPHATTN_LOSS_NONE && dX, twice = own && dW;
@@ -374,7 +427,7 @@ int run_vocab_bwd(const Vocab& p, const void* X, const void* W, const void* targ
         hipLaunchKernelGGL(vocab_rows_kernel, dim3(1), dim3(kRowsThreads), 0, stream, k.r);
         x = Operand{(const unsigned char*)p.x, 0, p.ld * 2, 0};
     } else if (S == Store::F32 && rows_form(p.T, SPHATTN_F32)) {
-        return run_rows_bwd(p, X, W, k, dX, dW, scale, stream);
+        return run_rows_bwd(p, X, W, k, dX, dW, scale, stream, teacher);
     } else {
         pack<S>(p, X, W, true, k, x, w, stream);
     }
@@ -395,6 +448,7 @@ int run_vocab_bwd(const Vocab& p, const void* X, const void* W, const void* targ
         a.G = p.G, a.G_part = (long long)p.T * p.piece, a.G_ld = p.piece;
         int tiles;
         if (p.T > 0) rc = launch_scores<S, Stage::G>(a, n, p.T, tiles, stream);
+        if (rc == SPHATTN_OK && teacher && p.T > 0) rc = launch_taught_g<S, false>(*teacher, a, p.rows, n, stream);
         if (rc != SPHATTN_OK) break;
         VocabArgs bx{}, bw{};
         const bool with_dx = dX && p.T > 0, with_dw = dW != nullptr;
@@ -410,6 +464,7 @@ int run_vocab_bwd(const Vocab& p, const void* X, const void* W, const void* targ
             rc = dw_big ? launch_tiles<Big, S, Stage::Dw>(bw, p.ld, n, stream) : launch_tiles<Mid, S, Stage::Dw>(bw, p.ld, n, stream);
             a.g = p.g_own, a.unless_even = 1;
             if (rc == SPHATTN_OK) rc = launch_scores<S, Stage::G>(a, n, p.T, tiles, stream);
+            if (rc == SPHATTN_OK && teacher) rc = launch_taught_g<S, false>(*teacher, a, p.rows, n, stream);
             if (rc == SPHATTN_OK) rc = p.dx_big ? launch_tiles<Big, S, Stage::Dx>(bx, p.ld, p.T, stream) : launch_tiles<Mid, S, Stage::Dx>(bx, p.ld, p.T, stream);
             continue;
         }
@@ -434,6 +489,19 @@ int vocab_check(const void* X, const void* W, const void* targets, int id_bytes,
     if (!W || (T > 0 && (!X || !targets))) return SPHATTN_ERR_NULL;
     if (off(X, element_bytes(dtype)) || off(W, element_bytes(dtype)) || off(targets, id_bytes)) return SPHATTN_ERR_ALIGN;
     if (!std::isfinite(scale) || reduction < SPHATTN_LOSS_NONE || reduction > SPHATTN_LOSS_MEAN) return SPHATTN_ERR_VALUE;
+    return SPHATTN_OK;
+}
+
+int distill_check(const void* X, const void* W, const void* ids, int id_bytes, const float* teacher, int T, int V, int D, int K, float scale, float temperature,
+                  int reduction, int dtype)
+{
+    if (!teacher_shape(T, V, D, K)) return SPHATTN_ERR_SHAPE;
+    const int rc = vocab_check(X, W, ids, id_bytes, T, V, D, scale, reduction, dtype);
+    if (rc != SPHATTN_OK) return rc;
+    if (T > 0 && !teacher) return SPHATTN_ERR_NULL;
+    if (off(teacher, 4)) return SPHATTN_ERR_ALIGN;
+    // (the losses have its square as a factor, the logits its inverse)
+    if (!(temperature >= 0x1p-20f && temperature <= 0x1p20f) || !std::isfinite(scale / temperature)) return SPHATTN_ERR_VALUE;
     return SPHATTN_OK;
 }
 
@@ -547,6 +615,82 @@ int sphattn_vocab_loss_bwd(const void* X, const void* W, const void* targets, in
     case SPHATTN_F32: return run_vocab_bwd<Store::F32>(p, X, W, targets, id_bytes, lse, dloss, dX, dW, scale, reduction, s);
     case SPHATTN_BF16: return run_vocab_bwd<Store::Bf16>(p, X, W, targets, id_bytes, lse, dloss, dX, dW, scale, reduction, s);
     default: return run_vocab_bwd<Store::F16>(p, X, W, targets, id_bytes, lse, dloss, dX, dW, scale, reduction, s);
+    }
+}
+
+size_t sphattn_vocab_distill_workspace_bytes(int T, int V, int D, int K, int dtype)
+{
+    return teacher_shape(T, V, D, K) && element_bytes(dtype) ? teacher_plan(T, V, K, false, true, vocab_fwd_plan(T, V, D, dtype, nullptr).bytes, nullptr).bytes : 0;
+}
+
+int sphattn_vocab_distill_fwd(const void* X, const void* W, const void* ids, int id_bytes, const float* teacher,
+                              float* losses, float* lse, float* kept, float* mean,
+                              int T, int V, int D, int K, float scale, float temperature, int reduction, int dtype,
+                              void* workspace, size_t workspace_bytes, void* stream)
+{
+    const int rc = distill_check(X, W, ids, id_bytes, teacher, T, V, D, K, scale, temperature, reduction, dtype);
+    if (rc != SPHATTN_OK) return rc;
+    if (T > 0 && (!losses || !lse)) return SPHATTN_ERR_NULL;
+    if (off(losses, 4) || off(lse, 4) || off(kept, 4) || off(mean, 4)) return SPHATTN_ERR_ALIGN;
+    const size_t e = (size_t)element_bytes(dtype), entries = (size_t)T * K;
+    const Vocab p = vocab_fwd_plan(T, V, D, dtype, workspace);
+    Teacher k = teacher_plan(T, V, K, false, true, p.bytes, workspace);
+    if (!workspace || off(workspace, 16) || workspace_bytes < k.bytes) return SPHATTN_ERR_WORKSPACE;
+    const Range written[] = {{losses, (size_t)T * 4}, {lse, (size_t)T * 4}, {kept, kept ? entries * 4 : 0}, {mean, mean ? (size_t)4 : 0}, {workspace, k.bytes}};
+    const Range read[] = {{X, (size_t)T * D * e}, {W, (size_t)V * D * e}, {ids, entries * id_bytes}, {teacher, entries * 4}};
+    if (any_meet(written, read)) return SPHATTN_ERR_ALIAS;
+    const hipStream_t s = (hipStream_t)stream;
+    if (T == 0) {
+        if (mean && reduction != SPHATTN_LOSS_NONE)
+            hipLaunchKernelGGL(vocab_mean_kernel, dim3(1), dim3(1024), 0, s, losses, ids, 4, 0, mean, 0);
+        return launched();
+    }
+    k.tau = temperature;
+    if (kept) k.logits = kept;
+    const int sorted = launch_teacher(k, ids, id_bytes, teacher, T, V, s);
+    if (sorted != SPHATTN_OK) return sorted;
+    scale /= temperature;
+    switch (dtype) {
+    case SPHATTN_F32: return run_vocab_fwd<Store::F32>(p, X, W, k.targets, 4, losses, lse, mean, scale, reduction, 0, s, &k);
+    case SPHATTN_BF16: return run_vocab_fwd<Store::Bf16>(p, X, W, k.targets, 4, losses, lse, mean, scale, reduction, 0, s, &k);
+    default: return run_vocab_fwd<Store::F16>(p, X, W, k.targets, 4, losses, lse, mean, scale, reduction, 0, s, &k);
+    }
+}
+
+size_t sphattn_vocab_distill_bwd_workspace_bytes(int T, int V, int D, int K, int dtype)
+{
+    return teacher_shape(T, V, D, K) && element_bytes(dtype) ? teacher_plan(T, V, K, true, false, vocab_bwd_plan(T, V, D, dtype, nullptr).bytes, nullptr).bytes : 0;
+}
+
+int sphattn_vocab_distill_bwd(const void* X, const void* W, const void* ids, int id_bytes, const float* teacher,
+                              const float* lse, const float* kept, const float* dloss, void* dX, void* dW,
+                              int T, int V, int D, int K, float scale, float temperature, int reduction, int dtype,
+                              void* workspace, size_t workspace_bytes, void* stream)
+{
+    const int rc = distill_check(X, W, ids, id_bytes, teacher, T, V, D, K, scale, temperature, reduction, dtype);
+    if (rc != SPHATTN_OK) return rc;
+    if ((T > 0 && (!lse || !kept || !dloss)) || (!dX && !dW)) return SPHATTN_ERR_NULL;
+    const size_t e = (size_t)element_bytes(dtype), entries = (size_t)T * K;
+    if (off(lse, 4) || off(kept, 4) || off(dloss, 4) || off(dX, e) || off(dW, e)) return SPHATTN_ERR_ALIGN;
+    const Vocab p = vocab_bwd_plan(T, V, D, dtype, workspace);
+    Teacher k = teacher_plan(T, V, K, true, false, p.bytes, workspace);
+    if (!workspace || off(workspace, 16) || workspace_bytes < k.bytes) return SPHATTN_ERR_WORKSPACE;
+    const Range written[] = {{dX, (size_t)T * D * e}, {dW, (size_t)V * D * e}, {workspace, k.bytes}};
+    const Range read[] = {{X, (size_t)T * D * e}, {W, (size_t)V * D * e}, {ids, entries * id_bytes}, {teacher, entries * 4}, {lse, (size_t)T * 4}, {kept, entries * 4},
+                          {dloss, reduction == SPHATTN_LOSS_NONE ? (size_t)T * 4 : 4}};
+    if (any_meet(written, read)) return SPHATTN_ERR_ALIAS;
+    const hipStream_t s = (hipStream_t)stream;
+    k.tau = temperature;
+    k.logits = const_cast<float*>(kept);
+    if (T > 0) {
+        const int sorted = launch_teacher(k, ids, id_bytes, teacher, T, V, s);
+        if (sorted != SPHATTN_OK) return sorted;
+    }
+    scale /= temperature;
+    switch (dtype) {
+    case SPHATTN_F32: return run_vocab_bwd<Store::F32>(p, X, W, k.targets, 4, lse, dloss, dX, dW, scale, reduction, s, &k);
+    case SPHATTN_BF16: return run_vocab_bwd<Store::Bf16>(p, X, W, k.targets, 4, lse, dloss, dX, dW, scale, reduction, s, &k);
+    default: return run_vocab_bwd<Store::F16>(p, X, W, k.targets, 4, lse, dloss, dX, dW, scale, reduction, s, &k);
     }
 }
 

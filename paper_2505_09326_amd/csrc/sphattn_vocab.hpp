@@ -43,6 +43,13 @@ struct VocabInfo {
     int even;                                      // one gradient per row, fp16: all of them within 2^4 of the largest, so that one `up` serves every row
 };
 
+// A teacher's ids of each row in order (those that are none behind them, as INT_MAX), where the ids of each 128 << shift begin among them, and the
+// student's logits of them in base 2.  By row of X, K of each.
+struct Taught {
+    const int* ids; const unsigned short* starts; float* logits;
+    int K, shift, blocks;                          // starts: [T][blocks + 1]
+};
+
 struct VocabArgs {
     Operand P, Q;
     const VocabInfo* info;                         // NULL: all rows of Q count
@@ -59,12 +66,14 @@ struct VocabArgs {
     float2* partial; int partial_ld; float* target_logit; // logits
     const int* g_target; const float* g_lse2; const float* g;   // G, by row that counts
     int unless_even;                               // G: already there if the rows' gradients are even
+    Taught taught;                                 // logits with a teacher's ids
     void* G; long long G_part; int G_ld;           // (elements)
     // dX, dW
     void* out; int out_ld; int out_cols, out_rows; int accumulate;   // (dX: slice after slice, `rows` rows each)
 };
 
-enum class Stage { Logits, G, Dx, Dw };
+enum class Stage { Logits, Taught, G, Dx, Dw };      // Taught: logits, and those of a teacher's ids kept instead of a target's
+constexpr bool is_logits(Stage s) { return s == Stage::Logits || s == Stage::Taught; }
 
 // Slices of dX's sum over the vocabulary for `rows` rows that count, where a launch for T of them has `slices`: as many more as
 // workgroups and arrays of partial sums are then free, while the chip is not full.  (8000 rows of which 1200 count, 20011 ids, width 1024:
@@ -267,7 +276,7 @@ void vocab_rows_dw_kernel(VocabArgs a)
 
 // whether logits and G are formed from fp32 as it is (RowsProduct)
 template <class T, Store S, Stage ST>
-constexpr bool reads_fp32() { return S == Store::F32 && T::BQ <= 64 && (ST == Stage::Logits || ST == Stage::G); }
+constexpr bool reads_fp32() { return S == Store::F32 && T::BQ <= 64 && (is_logits(ST) || ST == Stage::G); }
 
 // The logits of a wave's corner from rows of fp32 as they are, four k at a time: for the rare tile that meets a row with an infinite element, where only
 // the formula itself says which infinity it is or that it is none.  Waits for nothing but its own loads.
@@ -296,6 +305,48 @@ __device__ __forceinline__ void whole_logits(f32x4 (&acc)[T::FP][T::FQ], const V
         for (int i = 0; i < T::FP; ++i)
 #pragma unroll
             for (int j = 0; j < T::FQ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(w[i], x[j], acc[i][j], 0, 0, 0);
+    }
+}
+
+// Of this wave's corner the logits that the teacher's ids ask for.  A row has few of them in a tile (64 of 32768 ids: one in four rows in 128 columns): all
+// rows' next one at a time, and a lane finds its value among its registers by the five bits of its place.
+template <class T>
+__device__ __forceinline__ void keep_taught(const f32x4 (&acc)[T::FP][T::FQ], const VocabArgs& a, int rows, int pw, int qw, float scale2)
+{
+    const int lane = threadIdx.x & 63, n16 = lane & 15, g = lane >> 4;
+    const Taught& k = a.taught;
+    const int b0 = min(pw >> (7 + k.shift), k.blocks), b1 = min(((pw + T::FP * 16 - 1) >> (7 + k.shift)) + 1, k.blocks);
+    size_t at[T::FQ];
+    int left[T::FQ], most = 0;
+#pragma unroll
+    for (int j = 0; j < T::FQ; ++j) {
+        const int q = qw + 16 * j + n16, t = q < rows ? (a.rows ? a.rows[q] : q) : 0;
+        const unsigned short* starts = k.starts + (size_t)t * (k.blocks + 1);
+        const int e0 = starts[b0], e1 = starts[b1];
+        at[j] = (size_t)t * k.K + e0;
+        left[j] = q < rows ? e1 - e0 : 0;
+        most = max(most, left[j]);
+    }
+    for (int e = 0; __ballot(e < most); ++e) {
+        int y[T::FQ];
+#pragma unroll
+        for (int j = 0; j < T::FQ; ++j) y[j] = e < left[j] ? k.ids[at[j] + e] - pw : -1;
+#pragma unroll
+        for (int j = 0; j < T::FQ; ++j) {
+            const bool mine = y[j] >= 0 && y[j] < T::FP * 16 && ((y[j] >> 2) & 3) == g;
+            if (!__ballot(mine)) continue;
+            float x[T::FP * 4];
+#pragma unroll
+            for (int i = 0; i < T::FP * 4; ++i) x[i] = acc[i / 4][j][i & 3];
+            const int place = (y[j] & 3) | (y[j] >> 4) << 2;
+#pragma unroll
+            for (int n = 1; n < T::FP * 4; n *= 2) {
+                const bool odd = place & n;
+#pragma unroll
+                for (int i = 0; i < T::FP * 4; i += 2 * n) x[i] = odd ? x[i + n] : x[i];
+            }
+            if (mine) k.logits[at[j] + e] = x[0] * scale2;
+        }
     }
 }
 
@@ -375,8 +426,9 @@ __device__ __forceinline__ void vocab_tile(const VocabArgs& a, int block, SPH_LD
             for (int r = 0; r < 4; ++r) x = y == 16 * i + 4 * g + r ? prod.acc[i][j][r] : x;
         return x;
     };
-    if constexpr (ST == Stage::Logits) {
+    if constexpr (is_logits(ST)) {
         SPH_LDS float* shared = (SPH_LDS float*)smem;                     // [WAVES_P][BQ][2]
+        if constexpr (ST == Stage::Taught) keep_taught<T>(prod.acc, a, rows, pw, qw, scale2);
         if (!whole) {
 #pragma unroll
             for (int i = 0; i < T::FP; ++i)
@@ -407,7 +459,7 @@ __device__ __forceinline__ void vocab_tile(const VocabArgs& a, int block, SPH_LD
                 shared[(wp * T::BQ + q - q0) * 2] = m;
                 shared[(wp * T::BQ + q - q0) * 2 + 1] = all;
             }
-            if (q < rows) {
+            if (ST == Stage::Logits && q < rows) {
                 const int y = load_id(a.targets, a.id_bytes, a.rows ? a.rows[q] : q) - pw;
                 if (y >= 0 && y < T::FP * 16 && pw + y < a.V && ((y >> 2) & 3) == g) a.target_logit[q] = pick(j, y) * scale2;
             }
@@ -661,6 +713,7 @@ struct PackArgs {
     RowArgs r;
     const float* lse; int* g_target; float* g_lse2; float* g;   // what the G stage needs of each row, or NULL
     float *g_own, *own_down;                       // fp16, one gradient per row: g of dX's own G and the factor of dX's rows, or NULL
+    int no_target;                                 // G has a teacher's weights instead, which taught_g_kernel takes off
 };
 
 template <Store S>
@@ -723,7 +776,7 @@ void vocab_pack_kernel(PackArgs a)
         return;
     }
     if (a.g_target && lane == 0) {
-        a.g_target[m] = load_id(a.r.targets, a.r.id_bytes, t);
+        a.g_target[m] = a.no_target ? -(1 << 30) : load_id(a.r.targets, a.r.id_bytes, t);
         a.g_lse2[m] = a.lse[t] * kLog2e;
         const float g = a.r.reduce == Reduce::None ? a.r.dloss[t] * a.r.scale : 1.f;
         a.g[m] = g * up;
@@ -780,7 +833,7 @@ void vocab_join_kernel(const float2* __restrict__ partial, int partial_ld, int t
             for (int w = 1; w < W; ++w) s = join_sums(s, shared[w][row]);
             const float l2 = (__builtin_fabsf(s.top) < __builtin_inff() ? s.top : 0.f) + __builtin_amdgcn_logf(s.sum);
             l = y >= V ? __builtin_nanf("") : l2 * kLn2;
-            if (y >= 0) of_row = y >= V ? __builtin_nanf("") : (l2 - target_logit[m]) * kLn2;
+            if (y >= 0 && target_logit) of_row = y >= V ? __builtin_nanf("") : (l2 - target_logit[m]) * kLn2;
         }
         if (lse) lse[t] = l;
         losses[t] = of_row;
@@ -863,6 +916,134 @@ void vocab_dx_kernel(const float* __restrict__ part, int slices, int ld, int til
 #pragma unroll
             for (int r = 0; r < 4; ++r)
                 if (c + r < D) store_el<S>(dX, at + r, x[r]);
+        }
+    }
+}
+
+// ---- a teacher's logits ------------------------------------------------------------------------------------------
+//
+//   p = softmax over a row's entries of teacher / tau      loss = tau^2 sum_k p_k (log p_k - l_{id_k} + lse)
+//   G = g tau^2 (exp(l - lse) - sum of p_k over the entries of that id)      l = (c / tau) x . w
+//
+// The products are those of the cross entropy, with the logits of K ids kept per row where that keeps one, and with K weights taken off G where that
+// takes off one: behind the tiles, in fp32 from the kept logits, so that a value of G is rounded once.  What a row counts for is given on
+// as a target: -1 for a row without an entry, 0 for others, INT_MAX for one with an id that is none.
+
+// Entries in order of their ids, equal ids in theirs (a sort of K keys in LDS, as a network of exchanges), the softmax of their logits, and
+// where each block of ids begins.  A wave per row.
+constexpr int kTaughtThreads = 256, kTaughtWaves = kTaughtThreads / 64, kTaughtMost = 1024;
+inline int taught_lds_bytes(int padded) { return kTaughtWaves * padded * 12; }
+
+__global__ __launch_bounds__(kTaughtThreads)
+void taught_kernel(const void* __restrict__ ids, int id_bytes, const float* __restrict__ teacher, int T, int V, int K, int padded, float over_tau,
+                   int* __restrict__ targets, int* __restrict__ sorted, float* __restrict__ weights, unsigned short* __restrict__ starts, int shift, int blocks)
+{
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem_raw[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    uint64_t* const keys = (uint64_t*)smem_raw + (size_t)wave * padded;
+    float* const p = (float*)((uint64_t*)smem_raw + (size_t)kTaughtWaves * padded) + (size_t)wave * padded;
+    const long long t = (long long)blockIdx.x * kTaughtWaves + wave;
+    const size_t row = (size_t)t * K;
+    float top = -__builtin_inff(), sum = 0.f;
+    bool bad = false, none = false;                // an id past the vocabulary; a logit that is no number
+    for (int k = lane; k < padded; k += 64) {
+        const int id = t < T && k < K ? load_id(ids, id_bytes, row + k) : -1;
+        const float x = id >= 0 ? teacher[row + k] * over_tau : -__builtin_inff();
+        bad |= id >= V;
+        none |= x != x;
+        top = fmaxf(top, x);
+        p[k] = x;
+        keys[k] = (uint64_t)(uint32_t)(id >= 0 && id < V ? id : 0x7fffffff) << 32 | (uint32_t)k;
+    }
+    top = max_over_wave(top);
+    none = __ballot(none) != 0;
+    bad = __ballot(bad) != 0;
+    for (int k = lane; k < padded; k += 64) {      // (an infinite top: its difference to itself is no number, as in the formula)
+        const float e = p[k] == -__builtin_inff() ? 0.f : expf(p[k] - top);
+        p[k] = e;
+        sum += e;
+    }
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+    const bool counts = none || top > -__builtin_inff();
+    for (int size = 2; size <= padded; size *= 2)
+        for (int step = size / 2; step > 0; step /= 2) {
+            __syncthreads();
+            for (int i = lane; i < padded / 2; i += 64) {
+                const int lo = i / step * step * 2 + i % step, hi = lo + step;
+                const uint64_t a = keys[lo], b = keys[hi];
+                if ((a > b) == ((lo & size) == 0)) keys[lo] = b, keys[hi] = a;
+            }
+        }
+    __syncthreads();
+    if (t >= T) return;
+    for (int k = lane; k < K; k += 64) {
+        const uint64_t key = keys[k];
+        sorted[row + k] = counts ? (int)(key >> 32) : 0x7fffffff;
+        weights[row + k] = p[(uint32_t)key] / sum;
+    }
+    if (lane == 0) targets[t] = !counts ? -1 : bad ? 0x7fffffff : 0;
+    if (!starts) return;
+    for (int b = lane; b <= blocks; b += 64) {     // entries below the block's first id
+        const uint64_t from = (uint64_t)min((long long)b << (7 + shift), (long long)V) << 32;
+        int n = 0;
+        for (int step = padded; step > 0; step /= 2)
+            if (n + step <= padded && keys[n + step - 1] < from) n += step;
+        starts[(size_t)t * (blocks + 1) + b] = (unsigned short)(counts ? n : 0);
+    }
+}
+
+// The rows' losses from the kept logits: a wave per row
+__global__ __launch_bounds__(256)
+void taught_loss_kernel(const int* __restrict__ targets, const int* __restrict__ sorted, const float* __restrict__ weights, const float* __restrict__ logits,
+                        const float* __restrict__ lse, int T, int K, float tau2, float* __restrict__ losses)
+{
+    const int lane = threadIdx.x & 63;
+    const long long t = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (t >= T) return;
+    float sum = 0.f;
+    const int y = targets[t];
+    if (y >= 0) {
+        const float lse2 = lse[t] * kLog2e;
+        for (int k = lane; k < K; k += 64) {
+            const size_t at = (size_t)t * K + k;
+            const float w = weights[at];
+            // (below the normal numbers the logarithm's instruction takes 0 for it, and the term is nothing)
+            if (sorted[at] != 0x7fffffff && !(w < 0x1p-126f)) sum = __builtin_fmaf(w, __builtin_amdgcn_logf(w) + (lse2 - logits[at]), sum);
+        }
+#pragma unroll
+        for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+    }
+    if (lane == 0) losses[t] = y == 0x7fffffff ? __builtin_nanf("") : sum * kLn2 * tau2;
+}
+
+// G of a piece of the vocabulary at the teacher's ids: a wave per row that counts.  Equal ids are one value, the first's to write.
+template <Store S, bool WHOLE>                     // WHOLE: fp32 as it is, not in parts
+__global__ __launch_bounds__(256)
+void taught_g_kernel(const VocabInfo* __restrict__ info, const int* __restrict__ rows, const int* __restrict__ sorted, const float* __restrict__ weights,
+                     const float* __restrict__ logits, const float* __restrict__ g_lse2, const float* __restrict__ g, int unless_even, int K, int v0, int n,
+                     void* __restrict__ G, long long part, int ld)
+{
+    const int lane = threadIdx.x & 63;
+    const long long m = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (m >= info->rows || (unless_even && info->even)) return;
+    const size_t row = (size_t)rows[m] * K;
+    const float lse2 = g_lse2[m], gm = g[m];
+    for (int k = lane; k < K; k += 64) {
+        const int id = sorted[row + k];
+        if (id < v0 || id - v0 >= n || (k > 0 && sorted[row + k - 1] == id)) continue;
+        float w = weights[row + k];
+        for (int i = k + 1; i < K && sorted[row + i] == id; ++i) w += weights[row + i];
+        const float d = (__builtin_amdgcn_exp2f(logits[row + k] - lse2) - w) * gm;
+        const size_t at = (size_t)m * ld + (id - v0);
+        if constexpr (S == Store::F32 && !WHOLE) {
+            const float x[4] = {d, 0.f, 0.f, 0.f};
+            i32x2 parts[3];
+            split3(x, parts);
+#pragma unroll
+            for (int i = 0; i < 3; ++i) ((unsigned short*)G)[at + i * part] = (unsigned short)parts[i][0];
+        } else {
+            store_el<S>(G, at, d);
         }
     }
 }

@@ -1,0 +1,287 @@
+"""The divergence from a teacher's logits over a vocabulary and its gradients, against the formulas in 64 bits.
+
+Tolerances (u = 2^-24, e = eps / 2 of the storage type; fp32 with more than 64 rows: a term of a logit off by 3 2^-22, and elements of X and W to 2^-51 of their
+row's largest):
+  logit    a = (D + 6) u sum_k |x_k w_k| (and fp32's) times scale / tau
+  lse      the mean of that over its terms, 8 u |lse| and u (V / 64 + 100) for the sum
+  p        its exponent's rounding 4 u (1 + largest |teacher / tau|), (K / 64 + 20) u for the sum
+  losses   tau^2 sum p (2 u |log p| + 6 u (|l| + |lse|) + p's (1 + |log p - l + lse|) + l's + lse's + (K / 64 + 12) u of the term)
+  G        exp(l - lse) (a + lse's + 16 u (1 + |l|)) + p's + 2 u (exp + p), the rounding e |G|; fp16: 2^-24 of a value that the row's own gradient brings to 2^13 and
+           more, so 2^-37 of |g| (in dW of the largest |g|)
+  dX, dW   the sum of those, (n + 4) u of the terms' sizes for adding n of them (fp32: 2^-21 more for the products of parts that are left out), e of the result"""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+U = 2.0 ** -24
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+
+
+@pytest.fixture(scope="module")
+def pkg():
+    import paper_2505_09326_amd as p
+    p.load_library()
+    return p
+
+
+def _inputs(T, V, D, K, dtype, seed, share=0.8, ids_type=torch.int64):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    X = torch.randn(T, D, generator=g, device=DEV).to(TYPES[dtype])
+    W = (torch.randn(V, D, generator=g, device=DEV) * 2 * D ** -0.5).to(TYPES[dtype])
+    # (few ids near each other among many far apart; the same one several times where K is more than V allows or chance has it)
+    ids = torch.randint(V, (T, K), generator=g, device=DEV)
+    near = torch.rand((T, K), generator=g, device=DEV) < 0.3
+    ids = torch.where(near, (ids[:, :1] + torch.arange(K, device=DEV)) % V, ids)
+    teacher = 3 * torch.randn(T, K, generator=g, device=DEV)
+    hole = torch.rand((T, K), generator=g, device=DEV) < 0.2
+    ids[hole] = -1
+    teacher[hole] = float("nan")                               # what stands beside no entry is not looked at
+    teacher[torch.rand((T, K), generator=g, device=DEV) < 0.05] = float("-inf")
+    ids[torch.rand(T, generator=g, device=DEV) >= share] = -7
+    return X, W, ids.to(ids_type), teacher, g
+
+
+def _exact(X, W, ids, teacher, scale, tau, g=None):
+    """(losses, lse) with tolerances, and for gradients g of the rows (dX, dW) with theirs."""
+    f32, (T, D), (V, K) = X.dtype == torch.float32, X.shape, (W.shape[0], ids.shape[1])
+    e = torch.finfo(X.dtype).eps / 2
+    x, w, c = X.double(), W.double(), scale / tau
+    wt = w.t().contiguous()
+    logits, a = c * (x @ wt), (D + 6) * U * (x.abs() @ wt.abs())
+    if f32 and T > 64:
+        a = a * (1 + 3 * 2.0 ** -22 / ((D + 6) * U))
+        a += 2.0 ** -50 * (x.abs().amax(1)[:, None] * wt.abs().sum(0)[None] + wt.abs().amax(0)[None] * x.abs().sum(1)[:, None])
+    a *= abs(c)
+    lse = torch.logsumexp(logits, 1)
+    soft = (logits - lse[:, None]).exp()
+    part = lambda t: torch.where(soft > 0, soft * t, 0.0)
+    lse_tol = part(a).sum(1) + U * (V / 64 + 100) + 8 * U * lse.abs()
+    there, at = ids >= 0, ids.clamp_min(0).long()
+    best = torch.where(there, teacher.double() / tau, -math.inf)
+    counted = (best > -math.inf).any(1)
+    p = torch.softmax(torch.where(counted[:, None], best, 0.0), 1) * (there & counted[:, None])
+    far = torch.where(best > -math.inf, best.abs(), 0.0).amax(1, keepdim=True)
+    p_rel = 4 * U * (1 + 2 * far) + (K / 64 + 20) * U
+    logp = torch.where(p > 0, p.clamp_min(1e-300).log(), 0.0)
+    mine, mine_tol = logits.gather(1, at), a.gather(1, at)
+    term = logp - mine + lse[:, None]
+    losses = tau ** 2 * (p * term).sum(1)
+    loss_tol = tau ** 2 * (p * (2 * U * logp.abs() + 6 * U * (mine.abs() + lse[:, None].abs()) + p_rel * (1 + term.abs()) + mine_tol + lse_tol[:, None]
+                                + (K / 64 + 12) * U * term.abs())).sum(1)
+    zero = lambda t: torch.where(counted, t, 0.0)
+    if g is None:
+        return (zero(losses), loss_tol), (zero(lse), zero(lse_tol))
+    spread = torch.zeros_like(soft).scatter_add_(1, at, p)
+    G, off = soft - spread, part(a + lse_tol[:, None] + 16 * U * (1 + logits.abs())) + spread * p_rel + 2 * U * (soft + spread)
+    if f32:
+        off += U * G.abs()
+    g = zero(g.double())[:, None] * tau ** 2
+    half = X.dtype == torch.float16
+    off = (off + e * (G.abs() + off) * (not f32)) * g.abs()
+    G = G * g
+    more = 2.0 ** -21 if f32 else 0.0
+    tiny, tiny_all = (2.0 ** -37 * g.abs(), 2.0 ** -37 * g.abs().max()) if half else (0.0, 0.0)
+    Gt, ot = G.t().contiguous(), (off + tiny_all).t().contiguous()
+    dX, tX = G @ w, (off + tiny) @ w.abs() + ((V + 40) * U + more) * (G.abs() @ w.abs())
+    dW, tW = Gt @ x, ot @ x.abs() + ((T + 40) * U + more) * (Gt.abs() @ x.abs())
+    return (dX * c, tX * abs(c)), (dW * c, tW * abs(c))
+
+
+def _near(got, want, tol, what):
+    fi = torch.finfo(got.dtype)
+    allowed = tol * (1 + fi.eps) + fi.eps / 2 * want.abs() * (1 + 2.0 ** -10) + fi.tiny * fi.eps
+    off = (got.double() - want).abs()
+    bad = ~(off <= allowed)
+    assert not bad.any(), f"{what}: {int(bad.sum())} of {bad.numel()}, worst {float((off / allowed.clamp_min(1e-300)).max()):.2f} of its tolerance"
+
+
+CASES = [  # T, V, D, K, tau, reduction, share
+    (1, 1, 8, 1, 1.0, "mean", 1.0), (1, 3000, 256, 64, 1.0, "none", 1.0), (5, 300, 40, 1, 2.0, "sum", 0.8), (16, 257, 515, 7, 0.5, "mean", 0.8),
+    (17, 130, 64, 130, 1.0, "none", 0.8), (48, 5000, 128, 33, 4.0, "mean", 1.0), (64, 128, 96, 1000, 1.0, "sum", 0.8), (65, 129, 64, 2, 1.0, "mean", 0.8),
+    (200, 1111, 131, 20, 2.0, "none", 0.5), (700, 4099, 64, 64, 1.0, "mean", 0.8), (1300, 600, 72, 5, 1.5, "none", 0.1), (2100, 8200, 200, 50, 1.0, "mean", 0.9)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("T,V,D,K,tau,reduction,share", CASES)
+def test_against_the_formulas(pkg, T, V, D, K, tau, reduction, share, dtype):
+    X, W, ids, teacher, gen = _inputs(T, V, D, K, dtype, T + 3 * V + 5 * D + K, share, torch.int32 if K % 2 else torch.int64)
+    scale = -0.7 if T == 200 else 1.3
+    losses, lse, kept, *mean = pkg.sphattn_vocab_distill_fwd(X, W, ids, teacher, scale, tau, reduction, keep=True)
+    (want, tol), (want_lse, tol_lse) = _exact(X, W, ids, teacher, scale, tau)
+    _near(losses, want, tol, "losses")
+    _near(lse, want_lse, tol_lse, "lse")
+    counted = ((ids >= 0) & (teacher > -math.inf)).any(1)
+    n = max(1, int(counted.sum()))
+    assert (losses[~counted] == 0).all() and (lse[~counted] == 0).all()
+    if reduction != "none":
+        by = n if reduction == "mean" else 1
+        _near(mean[0][None], want.sum()[None] / by, tol.sum()[None] / by, reduction)
+    plain = pkg.sphattn_vocab_distill_fwd(X, W, ids, teacher, scale, tau)
+    assert torch.equal(plain[0], losses) and torch.equal(plain[1], lse)
+    if reduction == "none":
+        dloss = torch.randn(T, generator=gen, device=DEV) * torch.pow(10.0, -4.0 * torch.rand(T, generator=gen, device=DEV))
+        g = dloss
+        dloss = torch.where(counted, dloss, float("nan"))      # (what comes back of rows that do not count is not looked at)
+    else:
+        dloss = torch.tensor(-3.0, device=DEV)
+        g = dloss.expand(T) / (n if reduction == "mean" else 1)
+    got = pkg.sphattn_vocab_distill_bwd(X, W, ids, teacher, lse, kept, dloss, scale, tau, reduction)
+    for name, a, (w, t) in zip(("dX", "dW"), got, _exact(X, W, ids, teacher, scale, tau, g)):
+        _near(a, w, t, name)
+    assert (got[0][~counted] == 0).all()
+    for a, b in zip(got, pkg.sphattn_vocab_distill_bwd(X, W, ids, teacher, lse, kept, dloss, scale, tau, reduction)):
+        assert torch.equal(a, b)
+
+
+def test_a_vocabulary_in_pieces(pkg):
+    """G of 6000 rows and 50000 ids does not fit one piece."""
+    T, V, D, K = 6000, 50000, 64, 40
+    X, W, ids, teacher, _ = _inputs(T, V, D, K, "bf16", 5, 1.0)
+    losses, lse, kept = pkg.sphattn_vocab_distill_fwd(X, W, ids, teacher, keep=True)
+    some = torch.arange(0, T, 37, device=DEV)
+    (want, tol), _ = _exact(X[some], W, ids[some], teacher[some], 1.0, 1.0)
+    _near(losses[some], want, tol, "losses")
+    g = torch.zeros(T, device=DEV)
+    g[some] = 1.0                                              # (rows of no weight have gradients of 0: dW is that of the others)
+    dX, dW = pkg.sphattn_vocab_distill_bwd(X, W, ids, teacher, lse, kept, g)
+    (wx, tx), (ww, tw) = _exact(X[some], W, ids[some], teacher[some], 1.0, 1.0, g[some])
+    _near(dX[some], wx, tx, "dX")
+    _near(dW, ww, tw + T * U * ww.abs(), "dW")
+
+
+@pytest.mark.parametrize("T", [3, 100])
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_entries_that_are_none_equal_ones_and_mistakes(pkg, T, dtype):
+    V, D, K = 500, 64, 6
+    X, W, _, _, _ = _inputs(T, V, D, K, dtype, 9)
+    ids = torch.arange(K, device=DEV).expand(T, K) * 77 + torch.arange(T, device=DEV)[:, None]
+    teacher = torch.randn(T, K, device=DEV)
+    base = pkg.sphattn_vocab_distill_fwd(X, W, ids, teacher, keep=True)
+    dl = torch.ones(T, device=DEV)
+    grads = pkg.sphattn_vocab_distill_bwd(X, W, ids, teacher, base[1], base[2], dl)
+    # an entry split in two of half its weight, in another order: the same divergence but for log 2 of that weight
+    twice, both = torch.cat([ids[:, 2:3], ids], 1), torch.cat([teacher[:, 2:3], teacher], 1)
+    both[:, [0, 3]] -= math.log(2.0)
+    got = pkg.sphattn_vocab_distill_fwd(X, W, twice, both, keep=True)
+    p = torch.softmax(teacher.double(), 1)
+    _near(got[0], base[0].double() - math.log(2.0) * p[:, 2], 60 * U * (base[0].double().abs() + 30), "split")
+    again = pkg.sphattn_vocab_distill_bwd(X, W, twice, both, got[1], got[2], dl)
+    for a, b in zip(again, grads):
+        fi = torch.finfo(a.dtype)
+        assert (a.double() - b.double()).abs().max() <= (2 * fi.eps + 200 * U) * float(b.abs().max()) + 1e-6
+    # rows of nothing
+    ids[1], teacher[2] = -1, float("-inf")
+    got = pkg.sphattn_vocab_distill_fwd(X, W, ids, teacher, keep=True)
+    assert (got[0][1:3] == 0).all() and (got[1][1:3] == 0).all() and torch.equal(got[0][0], base[0][0])
+    dX, dW = pkg.sphattn_vocab_distill_bwd(X, W, ids, teacher, got[1], got[2], dl)
+    assert (dX[1:3] == 0).all() and dW.isfinite().all()
+    none = torch.full_like(ids, -1)
+    got = pkg.sphattn_vocab_distill_fwd(X, W, none, teacher, reduction="mean", keep=True)
+    assert got[3] == 0 and (got[0] == 0).all()
+    dX, dW = pkg.sphattn_vocab_distill_bwd(X, W, none, teacher, got[1], got[2], torch.ones((), device=DEV), reduction="mean")
+    assert (dX == 0).all() and (dW == 0).all()
+    # an id past the vocabulary, and logits that are no numbers: that row, and what it takes part in
+    ids[0, 3], teacher[T - 1, 1] = V, float("nan")
+    got = pkg.sphattn_vocab_distill_fwd(X, W, ids, teacher, keep=True)
+    assert got[0][0].isnan() and got[1][0].isnan() and got[0][T - 1].isnan()
+    dX, dW = pkg.sphattn_vocab_distill_bwd(X, W, ids, teacher, got[1], got[2], dl)
+    assert dX[0].isnan().all() and dX[3:T - 1].isfinite().all() and dW.isnan().all()
+
+
+def test_sharp_and_flat_teachers(pkg):
+    """Weights below fp32's normal numbers, a teacher sure of one id (a plain cross entropy), the student's own logits (no divergence)."""
+    T, V, D, K = 80, 900, 64, 16
+    X, W, *_ = _inputs(T, V, D, K, "f32", 13)
+    logits = X.double() @ W.double().t().contiguous()
+    top = logits.topk(K, 1)
+    teacher = torch.full((T, K), -95.0, device=DEV)
+    teacher[:, 3] = 0.0
+    got = pkg.sphattn_vocab_distill_fwd(X, W, top.indices, teacher)[0]
+    want = torch.logsumexp(logits, 1) - logits.gather(1, top.indices[:, 3:4])[:, 0]
+    _near(got, want, 200 * U * (1 + want.abs()), "one-hot")
+    teacher[:, 0] = 400.0
+    _near(pkg.sphattn_vocab_distill_fwd(X, W, top.indices, teacher)[0], torch.logsumexp(logits, 1) - top.values[:, 0], 400 * U * (1 + want.abs()), "sharper")
+    same = W[:K].contiguous()                                  # all of a small vocabulary
+    own = X.double() @ same.double().t().contiguous()
+    losses, lse, kept = pkg.sphattn_vocab_distill_fwd(X, same, torch.arange(K, device=DEV).flip(0).expand(T, K).contiguous(), own.flip(1).float(), keep=True)
+    assert losses.abs().max() < 100 * U * 10
+
+
+def test_no_rows_and_alignment(pkg):
+    for dtype in TYPES:
+        X, W, ids, teacher, _ = _inputs(90, 300, 33, 9, dtype, 17)
+        empty = pkg.sphattn_vocab_distill_fwd(X[:0], W, ids[:0], teacher[:0], reduction="mean", keep=True)
+        assert empty[0].shape == (0,) and empty[3] == 0
+        dX, dW = pkg.sphattn_vocab_distill_bwd(X[:0], W, ids[:0], teacher[:0], empty[1], empty[2], torch.ones((), device=DEV), reduction="mean")
+        assert dX.shape == (0, 33) and (dW == 0).all()
+        want = pkg.sphattn_vocab_distill_fwd(X, W, ids, teacher, keep=True)
+        move = lambda t: torch.cat([t.new_zeros(3), t.flatten()])[3:].view(t.shape)
+        got = pkg.sphattn_vocab_distill_fwd(move(X), move(W), move(ids), move(teacher), keep=True)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+        dl = torch.ones(90, device=DEV)
+        for a, b in zip(pkg.sphattn_vocab_distill_bwd(move(X), move(W), move(ids), move(teacher), move(got[1]), move(got[2]), move(dl)),
+                        pkg.sphattn_vocab_distill_bwd(X, W, ids, teacher, want[1], want[2], dl)):
+            assert torch.equal(a, b)
+
+
+def test_autograd(pkg):
+    from paper_2505_09326_amd import autograd
+    X, W, ids, teacher, _ = _inputs(60, 400, 48, 12, "bf16", 21)
+    x, w = X.view(4, 15, 48).clone().requires_grad_(True), W.clone().requires_grad_(True)
+    for reduction in ("mean", "sum", "none"):
+        loss = autograd.vocab_distillation(x, w, ids.view(4, 15, 12), teacher.view(4, 15, 12), 1.5, 2.0, reduction)
+        assert loss.shape == ((4, 15) if reduction == "none" else ())
+        dl = torch.full_like(loss, 0.5)
+        grads = torch.autograd.grad(loss, (x, w), dl)
+        fwd = pkg.sphattn_vocab_distill_fwd(X, W, ids, teacher, 1.5, 2.0, reduction, keep=True)
+        want = pkg.sphattn_vocab_distill_bwd(X, W, ids, teacher, fwd[1], fwd[2], dl.reshape(-1) if reduction == "none" else dl, 1.5, 2.0, reduction)
+        assert torch.equal(grads[0].view(60, 48), want[0]) and torch.equal(grads[1], want[1])
+    only, = torch.autograd.grad(autograd.vocab_distillation(x, W, ids.view(4, 15, 12), teacher.view(4, 15, 12)), (x,))
+    assert only.shape == x.shape
+    with pytest.raises(ValueError):
+        autograd.vocab_distillation(x, w, ids, teacher)
+    with pytest.raises(RuntimeError):
+        first, = torch.autograd.grad(autograd.vocab_distillation(x, w, ids.view(4, 15, 12), teacher.view(4, 15, 12)), (x,), create_graph=True)
+        first.sum().backward()
+
+
+def test_gradients_against_differences(pkg):
+    """Central differences of the formula in 64 bits (a step of 2^-9 of the norm 1: third derivatives below 2^-14 of the largest gradient)."""
+    T, V, D, K = 70, 300, 40, 9
+    X, W, ids, teacher, gen = _inputs(T, V, D, K, "f32", 23)
+    _, lse, kept = pkg.sphattn_vocab_distill_fwd(X, W, ids, teacher, 1.0, 2.0, keep=True)
+    g = torch.randn(T, generator=gen, device=DEV)
+    grads = pkg.sphattn_vocab_distill_bwd(X, W, ids, teacher, lse, kept, g, 1.0, 2.0)
+    at = [X.double(), W.double()]
+    for i in range(2):
+        step = torch.randn(at[i].shape, generator=gen, device=DEV, dtype=torch.float64)
+        step *= 2.0 ** -9 / step.norm()
+        up, down = (float((_exact(*[t + s * step if j == i else t for j, t in enumerate(at)], ids, teacher, 1.0, 2.0)[0][0] * g.double()).sum()) for s in (1, -1))
+        assert abs((up - down) / 2 - float((grads[i].double() * step).sum())) <= 2.0 ** -14 * float(grads[i].norm()) * 2.0 ** -9
+
+
+@pytest.mark.parametrize("dtype,T", [("bf16", 10), ("f16", 300), ("f32", 300)])
+def test_graph_replays(pkg, dtype, T):
+    X, W, ids, teacher, _ = _inputs(T, 1000, 64, 24, dtype, 27)
+    dl = torch.ones(T, device=DEV)
+
+    def call():
+        losses, lse, kept = pkg.sphattn_vocab_distill_fwd(X, W, ids, teacher, keep=True)
+        return losses, lse, *pkg.sphattn_vocab_distill_bwd(X, W, ids, teacher, lse, kept, dl)
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = call()
+    for i in range(3):
+        X.mul_(1.03125)
+        teacher.add_(0.125)
+        ids.add_(ids >= 0).clamp_(max=999)
+        dl.mul_(0.75)
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(out, call()):
+            assert torch.equal(a, b), i
