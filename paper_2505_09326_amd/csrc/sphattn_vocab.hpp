@@ -308,47 +308,72 @@ __device__ __forceinline__ void whole_logits(f32x4 (&acc)[T::FP][T::FQ], const V
     }
 }
 
-// Of this wave's corner the logits that the teacher's ids ask for.  A row has few of them in a tile (64 of 32768 ids: one in four rows in 128 columns): all
-// rows' next one at a time, and a lane finds its value among its registers by the five bits of its place.
+// The teacher's ids of this wave's corner.  A row has few of them in a tile (64 of 32768 ids: one in four rows in 128 columns), and where they are
+// takes three loads, each behind the one before: so they are looked up before the products, four of a row's by the four lanes that have its logits.
 template <class T>
-__device__ __forceinline__ void keep_taught(const f32x4 (&acc)[T::FP][T::FQ], const VocabArgs& a, int rows, int pw, int qw, float scale2)
-{
-    const int lane = threadIdx.x & 63, n16 = lane & 15, g = lane >> 4;
-    const Taught& k = a.taught;
-    const int b0 = min(pw >> (7 + k.shift), k.blocks), b1 = min(((pw + T::FP * 16 - 1) >> (7 + k.shift)) + 1, k.blocks);
-    size_t at[T::FQ];
-    int left[T::FQ], most = 0;
-#pragma unroll
-    for (int j = 0; j < T::FQ; ++j) {
-        const int q = qw + 16 * j + n16, t = q < rows ? (a.rows ? a.rows[q] : q) : 0;
-        const unsigned short* starts = k.starts + (size_t)t * (k.blocks + 1);
-        const int e0 = starts[b0], e1 = starts[b1];
-        at[j] = (size_t)t * k.K + e0;
-        left[j] = q < rows ? e1 - e0 : 0;
-        most = max(most, left[j]);
+struct TaughtIds {
+    int t[T::FQ], first[T::FQ], left[T::FQ], id[T::FQ];   // row of X; its entries here; one of the next four
+
+    __device__ __forceinline__ int load(const VocabArgs& a, int j, int e, int g) const
+    {
+        return e + g < left[j] ? a.taught.ids[(size_t)t[j] * a.taught.K + first[j] + e + g] : -1;
     }
-    for (int e = 0; __ballot(e < most); ++e) {
-        int y[T::FQ];
-#pragma unroll
-        for (int j = 0; j < T::FQ; ++j) y[j] = e < left[j] ? k.ids[at[j] + e] - pw : -1;
+    __device__ __forceinline__ void begin(const VocabArgs& a, int rows, int pw, int qw)
+    {
+        const int lane = threadIdx.x & 63, n16 = lane & 15, g = lane >> 4;
+        const Taught& k = a.taught;
+        const int b0 = min(pw >> (7 + k.shift), k.blocks), b1 = min(((pw + T::FP * 16 - 1) >> (7 + k.shift)) + 1, k.blocks);
 #pragma unroll
         for (int j = 0; j < T::FQ; ++j) {
-            const bool mine = y[j] >= 0 && y[j] < T::FP * 16 && ((y[j] >> 2) & 3) == g;
-            if (!__ballot(mine)) continue;
-            float x[T::FP * 4];
+            const int q = qw + 16 * j + n16;
+            t[j] = q < rows ? (a.rows ? a.rows[q] : q) : 0;
+        }
 #pragma unroll
-            for (int i = 0; i < T::FP * 4; ++i) x[i] = acc[i / 4][j][i & 3];
-            const int place = (y[j] & 3) | (y[j] >> 4) << 2;
+        for (int j = 0; j < T::FQ; ++j) {
+            const unsigned short* starts = k.starts + (size_t)t[j] * (k.blocks + 1);
+            first[j] = starts[b0];
+            left[j] = qw + 16 * j + n16 < rows ? starts[b1] - first[j] : 0;
+        }
 #pragma unroll
-            for (int n = 1; n < T::FP * 4; n *= 2) {
-                const bool odd = place & n;
+        for (int j = 0; j < T::FQ; ++j) id[j] = load(a, j, 0, g);
+    }
+    // A lane finds its value among its registers by the bits of its place
+    __device__ __forceinline__ void keep(const f32x4 (&acc)[T::FP][T::FQ], const VocabArgs& a, int pw, float scale2)
+    {
+        const int lane = threadIdx.x & 63, n16 = lane & 15, g = lane >> 4;
+        int most = 0;
 #pragma unroll
-                for (int i = 0; i < T::FP * 4; i += 2 * n) x[i] = odd ? x[i + n] : x[i];
-            }
-            if (mine) k.logits[at[j] + e] = x[0] * scale2;
+        for (int j = 0; j < T::FQ; ++j) most = max(most, left[j]);
+        for (int e0 = 0; __ballot(e0 < most); e0 += 4) {
+            int next[T::FQ];
+#pragma unroll
+            for (int j = 0; j < T::FQ; ++j) next[j] = load(a, j, e0 + 4, g);
+#pragma unroll
+            for (int j = 0; j < T::FQ; ++j)
+                for (int e = 0; e < 4 && __ballot(e0 + e < left[j]); ++e) {
+                    const int y = __shfl(id[j], n16 + 16 * e) - pw;
+                    const bool mine = e0 + e < left[j] && y >= 0 && y < T::FP * 16 && ((y >> 2) & 3) == g;
+                    int x[T::FP * 4];
+#pragma unroll
+                    for (int i = 0; i < T::FP * 4; ++i) {
+                        const float value = acc[i / 4][j][i & 3];
+                        x[i] = __builtin_bit_cast(int, value);
+                    }
+                    const int place = (y & 3) | (y >> 4) << 2;
+#pragma unroll
+                    for (int n = 1; n < T::FP * 4; n *= 2) {
+                        int other = (place & n) ? -1 : 0;
+                        asm("" : "+v"(other));     // (seen through, the selections become one comparison and one of them for every pair of places)
+#pragma unroll
+                        for (int i = 0; i < T::FP * 4; i += 2 * n) x[i] = (x[i + n] & other) | (x[i] & ~other);
+                    }
+                    if (mine) a.taught.logits[(size_t)t[j] * a.taught.K + first[j] + e0 + e] = __builtin_bit_cast(float, x[0]) * scale2;
+                }
+#pragma unroll
+            for (int j = 0; j < T::FQ; ++j) id[j] = next[j];
         }
     }
-}
+};
 
 template <class T, Store S, Stage ST>
 __device__ __forceinline__ void vocab_tile(const VocabArgs& a, int block, SPH_LDS unsigned char* smem)
@@ -382,12 +407,13 @@ __device__ __forceinline__ void vocab_tile(const VocabArgs& a, int block, SPH_LD
     constexpr bool ROWS = reads_fp32<T, S, ST>();
     constexpr bool SUMS = ST == Stage::Dx || ST == Stage::Dw, F32 = S == Store::F32;
     std::conditional_t<ROWS, RowsProduct<T>, Product<T, S == Store::F16 || (F32 && !SUMS), PX, QX, !F32 ? 1 : SUMS ? 6 : 3>> prod;
-    if constexpr (ROWS) prod.run(a, rows, p0, q0);
-    else prod.run(a.P, Q, p0, q0, k0, k1, smem);
-
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n16 = lane & 15, g = lane >> 4, wp = wave % T::WAVES_P, wq = wave / T::WAVES_P;
     const int pw = p0 + wp * T::FP * 16, qw = q0 + wq * T::FQ * 16;     // this wave's corner
+    TaughtIds<T> taught;
+    if constexpr (ST == Stage::Taught) taught.begin(a, rows, pw, qw);
+    if constexpr (ROWS) prod.run(a, rows, p0, q0);
+    else prod.run(a.P, Q, p0, q0, k0, k1, smem);
     if constexpr (F32 && !ROWS && !SUMS) {         // the rows' powers of two
         int qe[T::FQ];
         bool endless = false;
@@ -428,7 +454,7 @@ __device__ __forceinline__ void vocab_tile(const VocabArgs& a, int block, SPH_LD
     };
     if constexpr (is_logits(ST)) {
         SPH_LDS float* shared = (SPH_LDS float*)smem;                     // [WAVES_P][BQ][2]
-        if constexpr (ST == Stage::Taught) keep_taught<T>(prod.acc, a, rows, pw, qw, scale2);
+        if constexpr (ST == Stage::Taught) taught.keep(prod.acc, a, pw, scale2);
         if (!whole) {
 #pragma unroll
             for (int i = 0; i < T::FP; ++i)
