@@ -69,7 +69,7 @@ class _PythonOnly:
     @staticmethod
     def forward(*args):
         return None
-    backward = fp8_forward = embed_forward = embed_backward = loss_forward = loss_backward = clip = forward
+    backward = fp8_forward = embed_forward = embed_backward = loss_forward = loss_backward = clip = distill_forward = heads_forward = ffn_forward = forward
 
 
 class SphattnError(RuntimeError):
@@ -205,6 +205,9 @@ def _bound_marshal(lib):
              "sphattn_grn_bwd_split", "sphattn_bwd_workspace_bytes", "sphattn_fp8_grn_fwd", "sphattn_embed_fwd",
              "sphattn_embed_bwd_workspace_bytes", "sphattn_embed_bwd", "sphattn_vocab_loss_workspace_bytes", "sphattn_vocab_loss_fwd",
              "sphattn_vocab_loss_bwd_workspace_bytes", "sphattn_vocab_loss_bwd", "sphattn_clip_grads_workspace_bytes", "sphattn_clip_grads",
+             "sphattn_vocab_distill_workspace_bytes", "sphattn_vocab_distill_fwd", "sphattn_vocab_distill_bwd_workspace_bytes", "sphattn_vocab_distill_bwd",
+             "sphattn_head_norm_rotary_fwd", "sphattn_head_norm_rotary_bwd_workspace_bytes", "sphattn_head_norm_rotary_bwd",
+             "sphattn_gated_ffn_workspace_bytes", "sphattn_gated_ffn_fwd", "sphattn_gated_ffn_bwd_workspace_bytes", "sphattn_gated_ffn_bwd",
              "sphattn_strerror")
     _marshal.bind(_raise_on, *(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in names))
     return _marshal
@@ -1005,8 +1008,12 @@ def sphattn_vocab_distill_fwd(X, W, ids, teacher, scale=1.0, temperature=1.0, re
     lib = load_library()
     red = REDUCTIONS[reduction]
     scale, temperature = _finite("scale", scale), _temperature(temperature)
-    T, V, D, K, code, id_bytes = _taught(X, W, ids, teacher)
     keep = bool(keep) or kept is not None
+    if losses is None and lse is None and kept is None and mean is None and workspace is None and stream is None:
+        done = _fast.distill_forward(X, W, ids, teacher, scale, temperature, red, keep, False)
+        if done is not None:
+            return done
+    T, V, D, K, code, id_bytes = _taught(X, W, ids, teacher)
     _brought(stream, losses=losses, lse=lse, workspace=workspace, **({"mean": mean} if red else {}), **({"kept": kept} if keep else {}))
     _on_device(X=X, W=W, ids=ids, teacher=teacher, losses=losses, lse=lse, kept=kept, mean=mean, workspace=workspace)
     losses = torch.empty(T, dtype=torch.float32, device=X.device) if losses is None else losses
@@ -1210,8 +1217,12 @@ def sphattn_head_norm_rotary_fwd(Xq, Xk=None, wq=None, wk=None, positions=None, 
     those given, which may have any strides that leave each row a place of its own (a slice of a cache)."""
     import torch
     lib = load_library()
-    B, N, Hq, Hk, d, code = _projection(Xq, Xk, wq, wk)
     eps = _eps(eps)
+    if stream is None:
+        done = _fast.heads_forward(Xq, Xk, wq, wk, positions, inv_freq, sections, bool(interleaved), bool(norm), eps, Q, K, False)
+        if done is not None:
+            return done
+    B, N, Hq, Hk, d, code = _projection(Xq, Xk, wq, wk)
     rotary = _rotary_of(positions, inv_freq, sections, interleaved, B, N, d)
     _brought(stream, Q=Q, **({"K": K} if Hk else {}))
     if K is not None and not Hk:
@@ -1303,6 +1314,10 @@ def sphattn_gated_ffn_fwd(X, Wg, Wu, activation="silu", H=None, workspace=None, 
     import torch
     lib = load_library()
     gate = GATES[activation]
+    if H is None and workspace is None and stream is None:
+        done = _fast.ffn_forward(X, Wg, Wu, gate, False)
+        if done is not None:
+            return done
     T, D, F, code = _gated(X, Wg, Wu)
     need = lib.sphattn_gated_ffn_workspace_bytes(T, D, F, code)
     _brought(stream, H=H, **({"workspace": workspace} if need else {}))

@@ -19,7 +19,7 @@ import math
 import torch
 from torch.autograd.function import once_differentiable
 
-from . import (REDUCTIONS, _cross_fwd_z, _fast_calls, sphattn_bwd, sphattn_embed_bwd, sphattn_embed_fwd, sphattn_fwd_z, sphattn_gated_ffn_bwd,
+from . import (GATES, REDUCTIONS, _cross_fwd_z, _fast_calls, sphattn_bwd, sphattn_embed_bwd, sphattn_embed_fwd, sphattn_fwd_z, sphattn_gated_ffn_bwd,
                sphattn_gated_ffn_fwd, sphattn_grn_bwd, sphattn_head_norm_rotary_bwd, sphattn_head_norm_rotary_fwd, sphattn_vocab_distill_bwd,
                sphattn_vocab_distill_fwd, sphattn_vocab_loss_bwd, sphattn_vocab_loss_fwd)
 
@@ -148,6 +148,11 @@ def head_norm_rotary(Xq, Xk=None, wq=None, wk=None, positions=None, inv_freq=Non
     """Differentiable norms of queries Xq [B,N,Hq,d] and keys Xk [B,N,Hk,d] (or None) for each head, times wq and wk [d], rotated by their
     positions, laid out for spherical_attention: (Q [B,Hq,N,d], K [B,Hk,N,d] or None).  Xq and Xk may be slices of one projection's
     output.  Arguments as sphattn_head_norm_rotary_fwd; no gradients of positions and inv_freq."""
+    eps = float(eps)
+    if math.isfinite(eps):                         # (else the Python path says so)
+        done = _fast_calls().heads_forward(Xq, Xk, wq, wk, positions, inv_freq, sections, bool(interleaved), bool(norm), eps, None, None, True)
+        if done is not None:
+            return done
     return _HeadNormRotary.apply(Xq, Xk, wq, wk, positions, inv_freq, sections, interleaved, norm, eps)
 
 
@@ -174,7 +179,8 @@ class _GatedFeedForward(torch.autograd.Function):
 def gated_feed_forward(X, Wg, Wu, activation="silu"):
     """Differentiable act(X Wg^T) * (X Wu^T): X [..., D], Wg and Wu [F,D] of one type (fp32, bf16 or fp16), activation "silu", "gelu" or "relu".  Nothing but
     the inputs is kept for the gradients."""
-    return _GatedFeedForward.apply(X, Wg, Wu, activation)
+    done = _fast_calls().ffn_forward(X, Wg, Wu, GATES[activation], True)
+    return done if done is not None else _GatedFeedForward.apply(X, Wg, Wu, activation)
 
 
 class _VocabDistillation(torch.autograd.Function):
@@ -206,4 +212,9 @@ def vocab_distillation(X, W, ids, teacher, scale=1.0, temperature=1.0, reduction
     """Differentiable divergence of softmax(scale / temperature X W^T) over a vocabulary from a teacher's best logits, times temperature^2, in fp32: X [..., D]
     and W [V,D] of one type (fp32, bf16 or fp16), ids [..., K] (int32 or int64; negative: no entry), teacher [..., K] (fp32, its logits of those ids, no
     gradient).  reduction "mean" (over the rows with an entry; 0 if there is none), "sum" or "none"."""
+    scale, temperature = float(scale), float(temperature)
+    if math.isfinite(scale) and 2.0 ** -20 <= temperature <= 2.0 ** 20:      # (else the Python path says so)
+        done = _fast_calls().distill_forward(X, W, ids, teacher, scale, temperature, REDUCTIONS[reduction], True, True)
+        if done is not None:
+            return done
     return _VocabDistillation.apply(X, W, ids, teacher, scale, temperature, reduction)

@@ -29,6 +29,7 @@
 #include <string>
 #include <vector>
 
+#include "../../include/sphattn_layer.h"
 #include "../../include/sphattn_train.h"
 
 namespace {
@@ -50,6 +51,17 @@ struct EntryPoints {
     decltype(&sphattn_vocab_loss_bwd) loss_bwd = nullptr;
     decltype(&sphattn_clip_grads_workspace_bytes) clip_bytes = nullptr;
     decltype(&sphattn_clip_grads) clip = nullptr;
+    decltype(&sphattn_vocab_distill_workspace_bytes) distill_bytes = nullptr;
+    decltype(&sphattn_vocab_distill_fwd) distill = nullptr;
+    decltype(&sphattn_vocab_distill_bwd_workspace_bytes) distill_bwd_bytes = nullptr;
+    decltype(&sphattn_vocab_distill_bwd) distill_bwd = nullptr;
+    decltype(&sphattn_head_norm_rotary_fwd) heads = nullptr;
+    decltype(&sphattn_head_norm_rotary_bwd_workspace_bytes) heads_bwd_bytes = nullptr;
+    decltype(&sphattn_head_norm_rotary_bwd) heads_bwd = nullptr;
+    decltype(&sphattn_gated_ffn_workspace_bytes) ffn_bytes = nullptr;
+    decltype(&sphattn_gated_ffn_fwd) ffn = nullptr;
+    decltype(&sphattn_gated_ffn_bwd_workspace_bytes) ffn_bwd_bytes = nullptr;
+    decltype(&sphattn_gated_ffn_bwd) ffn_bwd = nullptr;
     decltype(&sphattn_strerror) text = nullptr;
 } entry;
 PyObject* raise_on = nullptr;                      // the binding's function that raises for an error code
@@ -557,6 +569,320 @@ PyObject* loss_backward(PyObject*, PyObject* const* args, Py_ssize_t n)
     return rc != 0 ? raised(rc) : tuple_of({&d[0], &d[1]});
 }
 
+// ---- distillation -------------------------------------------------------------------------------------
+
+struct Distilled { at::Tensor losses, lse, kept, mean; };
+
+Distilled distill(const at::Tensor& X, const at::Tensor& W, const at::Tensor& ids, const at::Tensor& teacher, double scale, double tau, int reduction, bool keep, int& rc)
+{
+    const int K = (int)ids.size(-1), V = (int)W.size(0), D = (int)W.size(1), T = (int)(X.numel() / D);
+    const at::IntArrayRef rows = X.sizes().slice(0, X.dim() - 1);
+    Distilled out{floats(rows, X), floats(rows, X), keep ? floats(ids.sizes(), X) : at::Tensor(), reduction ? floats({}, X) : at::Tensor()};
+    const size_t bytes = entry.distill_bytes(T, V, D, K, code_of(W));
+    const at::Tensor ws = bytes_of(bytes, X);
+    rc = entry.distill(data(X), data(W), data(ids), (int)ids.element_size(), (const float*)data(teacher), (float*)data(out.losses), (float*)data(out.lse),
+                       keep ? (float*)data(out.kept) : nullptr, reduction ? (float*)data(out.mean) : nullptr, T, V, D, K, (float)scale, (float)tau, reduction,
+                       code_of(W), data(ws), bytes, stream_of(X));
+    return out;
+}
+
+struct VocabDistillation : torch::autograd::Function<VocabDistillation> {
+    static at::Tensor forward(torch::autograd::AutogradContext* ctx, const at::Tensor& X, const at::Tensor& W, const at::Tensor& ids, const at::Tensor& teacher,
+                              double scale, double tau, int64_t reduction, int* rc)
+    {
+        Distilled out = distill(X, W, ids, teacher, scale, tau, (int)reduction, true, *rc);
+        ctx->save_for_backward({X, W, ids, teacher, out.lse, out.kept});
+        ctx->saved_data["scale"] = scale;
+        ctx->saved_data["tau"] = tau;
+        ctx->saved_data["reduction"] = reduction;
+        return reduction ? out.mean : out.losses;
+    }
+    static torch::autograd::variable_list backward(torch::autograd::AutogradContext* ctx, torch::autograd::variable_list grads)
+    {
+        const auto saved = ctx->get_saved_variables();
+        const at::Tensor &X = saved[0], &W = saved[1], &ids = saved[2];
+        int rc = 0;
+        at::Tensor dX, dW;
+        {
+            const at::NoGradGuard off;
+            const at::Tensor dloss = grads[0].contiguous();
+            const int K = (int)ids.size(-1), V = (int)W.size(0), D = (int)W.size(1), T = (int)(X.numel() / D);
+            if (ctx->needs_input_grad(0)) dX = at::empty_like(X);
+            if (ctx->needs_input_grad(1)) dW = at::empty_like(W);
+            const size_t bytes = entry.distill_bwd_bytes(T, V, D, K, code_of(W));
+            const at::Tensor ws = bytes_of(bytes, X);
+            rc = entry.distill_bwd(data(X), data(W), data(ids), (int)ids.element_size(), (const float*)data(saved[3]), (const float*)data(saved[4]),
+                                   (const float*)data(saved[5]), (const float*)data(dloss), dX.defined() ? data(dX) : nullptr, dW.defined() ? data(dW) : nullptr,
+                                   T, V, D, K, (float)ctx->saved_data["scale"].toDouble(), (float)ctx->saved_data["tau"].toDouble(),
+                                   (int)ctx->saved_data["reduction"].toInt(), code_of(W), data(ws), bytes, stream_of(X));
+        }
+        throw_on(rc);
+        return once({dX, dW, at::Tensor(), at::Tensor(), at::Tensor(), at::Tensor(), at::Tensor(), at::Tensor()});
+    }
+};
+
+// distill_forward(X, W, ids, teacher, scale, tau, reduction, keep, differentiable) -> (losses, lse[, kept][, mean]), or if differentiable what
+// vocab_distillation returns
+PyObject* distill_forward(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    if (!arguments(n, 9)) return nullptr;
+    const at::Tensor *X = tensor(args[0]), *W = tensor(args[1]), *ids = tensor(args[2]), *teacher = tensor(args[3]);
+    const double scale = PyFloat_AsDouble(args[4]), tau = PyFloat_AsDouble(args[5]);
+    const long reduction = PyLong_AsLong(args[6]);
+    if (PyErr_Occurred()) return nullptr;
+    if (!X || !W || !ids || !teacher || !ready()) Py_RETURN_NONE;
+    const bool differentiable = args[8] == Py_True, keep = args[7] == Py_True;
+    Distilled out;
+    int rc = 0;
+    try {
+        if (!X->is_cuda() || W->dim() != 2 || X->dim() < 1 || ids->dim() != X->dim() || (!differentiable && X->dim() != 2) || code_of(*X) < 0) Py_RETURN_NONE;
+        const at::Device device = X->device();
+        if (W->scalar_type() != X->scalar_type() || !plain(*X, device) || !plain(*W, device) || !are_ids(*ids, device) ||
+            !fits(*teacher, ids->sizes(), at::kFloat, device) || X->sizes().slice(0, X->dim() - 1) != ids->sizes().slice(0, X->dim() - 1) ||
+            X->size(-1) != W->size(1) || W->size(0) < 1 || W->size(0) > INT_MAX || W->size(1) < 1 || W->size(1) > INT_MAX || ids->size(-1) < 1 ||
+            ids->size(-1) > INT_MAX || X->numel() / W->size(1) > INT_MAX)
+            Py_RETURN_NONE;
+        const Unlocked unlocked;
+        if (differentiable) out.losses = VocabDistillation::apply(*X, *W, *ids, *teacher, scale, tau, (int64_t)reduction, &rc);
+        else out = distill(*X, *W, *ids, *teacher, scale, tau, (int)reduction, keep, rc);
+    } catch (...) {
+        PyErr_Clear();
+        Py_RETURN_NONE;
+    }
+    if (rc != 0) return raised(rc);
+    if (differentiable) return wrapped(std::move(out.losses));
+    if (keep) return reduction ? tuple_of({&out.losses, &out.lse, &out.kept, &out.mean}) : tuple_of({&out.losses, &out.lse, &out.kept});
+    return reduction ? tuple_of({&out.losses, &out.lse, &out.mean}) : tuple_of({&out.losses, &out.lse});
+}
+
+// ---- sphattn_layer.h -------------------------------------------------------------------------------
+
+// How a call of head_norm_rotary is rotated and normalised, and its sizes.
+struct HeadsHow {
+    int axes = 0, sections[3] = {0, 0, 0}, interleaved = 0, norm = 1;   // axes 0: nothing is rotated
+    float eps = 0.f;
+};
+
+sphattn_heads by_token(const at::Tensor& t) { return sphattn_heads{data(t), t.stride(0), t.stride(1), t.stride(2)}; }
+sphattn_heads by_head(const at::Tensor& t) { return sphattn_heads{data(t), t.stride(0), t.stride(2), t.stride(1)}; }
+
+sphattn_rotary rotary_of(const HeadsHow& how, const at::Tensor* positions, const at::Tensor* inv_freq, int64_t B)
+{
+    sphattn_rotary r{};
+    if (!how.axes) return r;
+    r.positions = data(positions), r.id_bytes = (int)positions->element_size(), r.axes = how.axes, r.interleaved = how.interleaved;
+    r.axis = positions->dim() == 3 ? positions->stride(0) : 0;
+    r.batch = positions->dim() > 1 && positions->size(-2) > 1 ? positions->stride(-2) : 0;
+    r.inv_freq = (const float*)data(inv_freq);
+    for (int i = 0; i < 3; ++i) r.sections[i] = how.sections[i];
+    return r;
+}
+
+void rotate_heads(const at::Tensor& Xq, const at::Tensor* Xk, const at::Tensor* wq, const at::Tensor* wk, const at::Tensor* positions, const at::Tensor* inv_freq,
+                  const HeadsHow& how, at::Tensor& Q, at::Tensor& K, int& rc)
+{
+    const int64_t B = Xq.size(0), N = Xq.size(1), Hq = Xq.size(2), d = Xq.size(3), Hk = Xk ? Xk->size(2) : 0;
+    if (!Q.defined()) Q = at::empty({B, Hq, N, d}, Xq.options());
+    if (Xk && !K.defined()) K = at::empty({B, Hk, N, d}, Xq.options());
+    const sphattn_heads xq = by_token(Xq), q = by_head(Q);
+    sphattn_heads xk{}, k{};
+    if (Xk) xk = by_token(*Xk), k = by_head(K);
+    const sphattn_rotary r = rotary_of(how, positions, inv_freq, B);
+    rc = entry.heads(&xq, Xk ? &xk : nullptr, data(wq), data(wk), &q, Xk ? &k : nullptr, &r, (int)B, (int)N, (int)Hq, (int)Hk, (int)d, how.norm, how.eps,
+                     code_of(Xq), stream_of(Xq));
+}
+
+// Rows of neighbouring elements, anywhere
+bool rows_fit(const at::Tensor& t, at::IntArrayRef shape, at::ScalarType type, at::Device device)
+{
+    return t.scalar_type() == type && t.device() == device && t.layout() == at::kStrided && t.sizes() == shape && t.stride(3) == 1;
+}
+
+struct HeadNormRotary : torch::autograd::Function<HeadNormRotary> {
+    static torch::autograd::variable_list forward(torch::autograd::AutogradContext* ctx, const at::Tensor& Xq, const at::Tensor& Xk, const at::Tensor& wq,
+                                                  const at::Tensor& wk, const std::optional<at::Tensor>& positions, const std::optional<at::Tensor>& inv_freq,
+                                                  const HeadsHow* how, int* rc)
+    {
+        at::Tensor Q, K;
+        rotate_heads(Xq, &Xk, &wq, &wk, positions ? &*positions : nullptr, inv_freq ? &*inv_freq : nullptr, *how, Q, K, *rc);
+        ctx->save_for_backward({Xq, Xk, wq, wk, positions.value_or(at::Tensor()), inv_freq.value_or(at::Tensor())});
+        ctx->saved_data["how"] = std::vector<int64_t>{how->axes, how->sections[0], how->sections[1], how->sections[2], how->interleaved, how->norm};
+        ctx->saved_data["eps"] = (double)how->eps;
+        return {Q, K};
+    }
+    static torch::autograd::variable_list backward(torch::autograd::AutogradContext* ctx, torch::autograd::variable_list grads)
+    {
+        const auto saved = ctx->get_saved_variables();
+        const at::Tensor &Xq = saved[0], &Xk = saved[1];
+        at::Tensor d[4];
+        int rc = 0;
+        {
+            const at::NoGradGuard off;
+            const auto list = ctx->saved_data["how"].toIntVector();
+            HeadsHow how;
+            how.axes = (int)list[0], how.interleaved = (int)list[4], how.norm = (int)list[5], how.eps = (float)ctx->saved_data["eps"].toDouble();
+            for (int i = 0; i < 3; ++i) how.sections[i] = (int)list[1 + i];
+            for (int i = 0; i < 2; ++i)
+                if (grads[i].stride(3) != 1) grads[i] = grads[i].contiguous();
+            sphattn_heads view[2];
+            for (int i = 0; i < 4; ++i) {
+                if (!ctx->needs_input_grad(i)) continue;
+                d[i] = at::empty(saved[i].sizes(), saved[i].options());
+                if (i < 2) view[i] = by_token(d[i]);
+            }
+            const sphattn_heads xq = by_token(Xq), xk = by_token(Xk), q = by_head(grads[0]), k = by_head(grads[1]);
+            const sphattn_rotary r = rotary_of(how, &saved[4], &saved[5], Xq.size(0));
+            const bool sums = d[2].defined() || d[3].defined();
+            const size_t bytes = sums ? entry.heads_bwd_bytes((int)Xq.size(3)) : 0;
+            const at::Tensor ws = sums ? bytes_of(bytes, Xq) : at::Tensor();
+            rc = entry.heads_bwd(&xq, &xk, data(saved[2]), data(saved[3]), &q, &k, d[0].defined() ? &view[0] : nullptr, d[1].defined() ? &view[1] : nullptr,
+                                 d[2].defined() ? data(d[2]) : nullptr, d[3].defined() ? data(d[3]) : nullptr, &r, (int)Xq.size(0), (int)Xq.size(1), (int)Xq.size(2),
+                                 (int)Xk.size(2), (int)Xq.size(3), how.norm, how.eps, code_of(Xq), sums ? data(ws) : nullptr, bytes, stream_of(Xq));
+        }
+        throw_on(rc);
+        return once({d[0], d[1], d[2], d[3], at::Tensor(), at::Tensor(), at::Tensor(), at::Tensor()});
+    }
+};
+
+// heads_forward(Xq, Xk, wq, wk, positions, inv_freq, sections, interleaved, norm, eps, Q, K, differentiable) -> (Q, K)
+PyObject* heads_forward(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    if (!arguments(n, 13)) return nullptr;
+    const at::Tensor *Xq = tensor(args[0]), *Xk, *wq, *wk, *positions, *inv_freq, *given_q, *given_k;
+    const double eps = PyFloat_AsDouble(args[9]);
+    if (PyErr_Occurred()) return nullptr;
+    if (!Xq || !optional(args[1], Xk) || !optional(args[2], wq) || !optional(args[3], wk) || !optional(args[4], positions) || !optional(args[5], inv_freq) ||
+        !optional(args[10], given_q) || !optional(args[11], given_k) || !ready() || !(eps >= 0))
+        Py_RETURN_NONE;
+    HeadsHow how;
+    how.interleaved = args[7] == Py_True, how.norm = args[8] == Py_True, how.eps = (float)eps;
+    const bool differentiable = args[12] == Py_True;
+    Py_ssize_t listed = -1;                        // sections
+    if (args[6] != Py_None) {
+        if (!PyList_CheckExact(args[6]) || (listed = PyList_GET_SIZE(args[6])) < 1 || listed > 3) Py_RETURN_NONE;
+        for (Py_ssize_t i = 0; i < listed; ++i) {
+            PyObject* x = PyList_GET_ITEM(args[6], i);
+            const long v = PyLong_CheckExact(x) ? PyLong_AsLong(x) : -1;
+            PyErr_Clear();
+            if (v < 0 || v > 1 << 20) Py_RETURN_NONE;
+            how.sections[i] = (int)v;
+        }
+    }
+    at::Tensor Q, K;
+    int rc = 0;
+    try {
+        if (!Xq->is_cuda() || Xq->dim() != 4 || code_of(*Xq) < 0 || (Xk && Xk->dim() != 4) || (!Xk && (wk || given_k))) Py_RETURN_NONE;
+        const at::Device device = Xq->device();
+        const at::ScalarType type = Xq->scalar_type();
+        const int64_t B = Xq->size(0), N = Xq->size(1), Hq = Xq->size(2), d = Xq->size(3), Hk = Xk ? Xk->size(2) : 0, most = INT_MAX;
+        if (B > most || N > most || Hq > most || Hk > most || d < 1 || d > most || (Xk && Hk < 1)) Py_RETURN_NONE;
+        const int64_t xq[4] = {B, N, Hq, d}, xk[4] = {B, N, Hk, d}, q[4] = {B, Hq, N, d}, k[4] = {B, Hk, N, d}, w[1] = {d}, f[1] = {d / 2};
+        if (!rows_fit(*Xq, xq, type, device) || (Xk && !rows_fit(*Xk, xk, type, device)) || (wq && !fits(*wq, w, type, device)) || (wk && !fits(*wk, w, type, device)) ||
+            (given_q && !rows_fit(*given_q, q, type, device)) || (given_k && !rows_fit(*given_k, k, type, device)))
+            Py_RETURN_NONE;
+        if (positions) {
+            const at::Tensor& p = *positions;
+            if ((p.scalar_type() != at::kLong && p.scalar_type() != at::kInt) || p.device() != device || p.layout() != at::kStrided || p.dim() < 1 || p.dim() > 3 ||
+                p.size(-1) != N || (N > 1 && p.stride(-1) != 1) || (p.dim() > 1 && p.size(-2) != B && p.size(-2) != 1) || !inv_freq ||
+                !fits(*inv_freq, f, at::kFloat, device))
+                Py_RETURN_NONE;
+            how.axes = p.dim() == 3 ? (int)p.size(0) : 1;
+            if (how.axes < 1 || how.axes > 3 || (listed < 0 ? how.axes > 1 : listed != how.axes)) Py_RETURN_NONE;
+            if (listed < 0) how.sections[0] = (int)(d / 2);
+            if (how.sections[0] + how.sections[1] + how.sections[2] != d / 2) Py_RETURN_NONE;
+        } else if (inv_freq || listed >= 0) {
+            Py_RETURN_NONE;
+        }
+        if (differentiable && (!Xk || !wq || !wk)) Py_RETURN_NONE;
+        const Unlocked unlocked;
+        if (differentiable) {
+            auto out = HeadNormRotary::apply(*Xq, *Xk, *wq, *wk, positions ? std::optional<at::Tensor>(*positions) : std::nullopt,
+                                             inv_freq ? std::optional<at::Tensor>(*inv_freq) : std::nullopt, (const HeadsHow*)&how, &rc);
+            Q = out[0], K = out[1];
+        } else {
+            if (given_q) Q = *given_q;
+            if (given_k) K = *given_k;
+            rotate_heads(*Xq, Xk, wq, wk, positions, inv_freq, how, Q, K, rc);
+            if (rc == 0)                           // (autograd is told, as by torch's own operations in place)
+                for (const at::Tensor* o : {given_q, given_k})
+                    if (o && !o->is_inference()) o->unsafeGetTensorImpl()->bump_version();
+        }
+    } catch (...) {
+        PyErr_Clear();
+        Py_RETURN_NONE;
+    }
+    return rc != 0 ? raised(rc) : tuple_of({&Q, &K});
+}
+
+at::Tensor gated(const at::Tensor& X, const at::Tensor& Wg, const at::Tensor& Wu, int gate, int& rc)
+{
+    const int F = (int)Wg.size(0), D = (int)Wg.size(1), T = (int)(X.numel() / D);
+    std::vector<int64_t> shape = X.sizes().vec();
+    shape.back() = F;
+    at::Tensor H = at::empty(shape, X.options());
+    const size_t bytes = entry.ffn_bytes(T, D, F, code_of(X));
+    const at::Tensor ws = bytes ? bytes_of(bytes, X) : at::Tensor();
+    rc = entry.ffn(data(X), data(Wg), data(Wu), data(H), T, D, F, gate, code_of(X), bytes ? data(ws) : nullptr, bytes, stream_of(X));
+    return H;
+}
+
+struct GatedFeedForward : torch::autograd::Function<GatedFeedForward> {
+    static at::Tensor forward(torch::autograd::AutogradContext* ctx, const at::Tensor& X, const at::Tensor& Wg, const at::Tensor& Wu, int64_t gate, int* rc)
+    {
+        at::Tensor H = gated(X, Wg, Wu, (int)gate, *rc);
+        ctx->save_for_backward({X, Wg, Wu});
+        ctx->saved_data["gate"] = gate;
+        return H;
+    }
+    static torch::autograd::variable_list backward(torch::autograd::AutogradContext* ctx, torch::autograd::variable_list grads)
+    {
+        const auto saved = ctx->get_saved_variables();
+        const at::Tensor &X = saved[0], &Wg = saved[1];
+        at::Tensor d[3];
+        int rc = 0;
+        {
+            const at::NoGradGuard off;
+            const at::Tensor dH = grads[0].contiguous();
+            const int F = (int)Wg.size(0), D = (int)Wg.size(1), T = (int)(X.numel() / D);
+            for (int i = 0; i < 3; ++i)
+                if (ctx->needs_input_grad(i)) d[i] = at::empty_like(saved[i]);
+            const size_t bytes = entry.ffn_bwd_bytes(T, D, F, code_of(X));
+            const at::Tensor ws = bytes_of(bytes, X);
+            auto or_null = [](const at::Tensor& t) { return t.defined() ? data(t) : nullptr; };
+            rc = entry.ffn_bwd(data(X), data(Wg), data(saved[2]), data(dH), or_null(d[0]), or_null(d[1]), or_null(d[2]), T, D, F, (int)ctx->saved_data["gate"].toInt(),
+                               code_of(X), data(ws), bytes, stream_of(X));
+        }
+        throw_on(rc);
+        return once({d[0], d[1], d[2], at::Tensor(), at::Tensor()});
+    }
+};
+
+// ffn_forward(X, Wg, Wu, gate, differentiable) -> H
+PyObject* ffn_forward(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    if (!arguments(n, 5)) return nullptr;
+    const at::Tensor *X = tensor(args[0]), *Wg = tensor(args[1]), *Wu = tensor(args[2]);
+    const long gate = PyLong_AsLong(args[3]);
+    if (PyErr_Occurred()) return nullptr;
+    if (!X || !Wg || !Wu || !ready()) Py_RETURN_NONE;
+    at::Tensor H;
+    int rc = 0;
+    try {
+        const bool differentiable = args[4] == Py_True;
+        if (!X->is_cuda() || code_of(*X) < 0 || X->dim() < 1 || (!differentiable && X->dim() != 2) || Wg->dim() != 2) Py_RETURN_NONE;
+        const at::Device device = X->device();
+        if (!plain(*X, device) || !fits(*Wg, Wg->sizes(), X->scalar_type(), device) || !fits(*Wu, Wg->sizes(), X->scalar_type(), device) ||
+            X->size(-1) != Wg->size(1) || Wg->size(1) < 1 || Wg->size(1) > INT_MAX || Wg->size(0) < 1 || Wg->size(0) > INT_MAX || X->numel() / Wg->size(1) > INT_MAX)
+            Py_RETURN_NONE;
+        const Unlocked unlocked;
+        H = differentiable ? GatedFeedForward::apply(*X, *Wg, *Wu, (int64_t)gate, &rc) : gated(*X, *Wg, *Wu, (int)gate, rc);
+    } catch (...) {
+        PyErr_Clear();
+        Py_RETURN_NONE;
+    }
+    return rc != 0 ? raised(rc) : wrapped(std::move(H));
+}
+
 // clip(grads, out, max_norm) -> norm: two lists, or one twice
 PyObject* clip(PyObject*, PyObject* const* args, Py_ssize_t n)
 {
@@ -604,7 +930,7 @@ PyObject* clip(PyObject*, PyObject* const* args, Py_ssize_t n)
 // bind(raise_on, addresses of the entry points in the order of EntryPoints)
 PyObject* bind(PyObject*, PyObject* args)
 {
-    constexpr Py_ssize_t COUNT = 17;
+    constexpr Py_ssize_t COUNT = 28;
     unsigned long long a[COUNT];
     if (!arguments(PyTuple_GET_SIZE(args), COUNT + 1)) return nullptr;
     for (Py_ssize_t i = 0; i < COUNT; ++i) {
@@ -617,7 +943,9 @@ PyObject* bind(PyObject*, PyObject* args)
     raise_on = handler;
     auto set = [&, i = 0](auto&... to) mutable { ((to = (std::decay_t<decltype(to)>)a[i++]), ...); };
     set(entry.cross, entry.cross_cut, entry.cross_bytes, entry.bwd, entry.bwd_cut, entry.bwd_bytes, entry.fp8, entry.embed, entry.embed_bwd_bytes,
-        entry.embed_bwd, entry.loss_bytes, entry.loss, entry.loss_bwd_bytes, entry.loss_bwd, entry.clip_bytes, entry.clip, entry.text);
+        entry.embed_bwd, entry.loss_bytes, entry.loss, entry.loss_bwd_bytes, entry.loss_bwd, entry.clip_bytes, entry.clip,
+        entry.distill_bytes, entry.distill, entry.distill_bwd_bytes, entry.distill_bwd, entry.heads, entry.heads_bwd_bytes, entry.heads_bwd, entry.ffn_bytes,
+        entry.ffn, entry.ffn_bwd_bytes, entry.ffn_bwd, entry.text);
     Py_RETURN_NONE;
 }
 
@@ -629,6 +957,9 @@ PyMethodDef methods[] = {{"forward", (PyCFunction)(void*)forward, METH_FASTCALL,
                          {"loss_forward", (PyCFunction)(void*)loss_forward, METH_FASTCALL, nullptr},
                          {"loss_backward", (PyCFunction)(void*)loss_backward, METH_FASTCALL, nullptr},
                          {"clip", (PyCFunction)(void*)clip, METH_FASTCALL, nullptr},
+                         {"distill_forward", (PyCFunction)(void*)distill_forward, METH_FASTCALL, nullptr},
+                         {"heads_forward", (PyCFunction)(void*)heads_forward, METH_FASTCALL, nullptr},
+                         {"ffn_forward", (PyCFunction)(void*)ffn_forward, METH_FASTCALL, nullptr},
                          {"bind", bind, METH_VARARGS, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", "Checks, outputs, workspace and launch of a call (see marshal.cpp).", -1, methods};

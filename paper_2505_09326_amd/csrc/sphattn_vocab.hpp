@@ -996,7 +996,7 @@ void taught_kernel(const void* __restrict__ ids, int id_bytes, const float* __re
         for (int step = size / 2; step > 0; step /= 2) {
             __syncthreads();
             for (int i = lane; i < padded / 2; i += 64) {
-                const int lo = i / step * step * 2 + i % step, hi = lo + step;
+                const int lo = 2 * i - (i & (step - 1)), hi = lo + step;
                 const uint64_t a = keys[lo], b = keys[hi];
                 if ((a > b) == ((lo & size) == 0)) keys[lo] = b, keys[hi] = a;
             }
