@@ -96,7 +96,7 @@ int sphattn_vocab_loss_bwd(const void* X, const void* W, const void* targets, in
  *   ids, teacher : [T,K], in any order.  A negative id is no entry, whatever its logit; a logit of minus infinity has p 0.  A row in which nothing else
  *   is left does not count: its loss and lse are 0 and its gradients are zeros.  An id that is there twice has both p.  An id >= V is a mistake that
  *   only the device can see: the row's loss and lse are NaN, and so are the gradients that it takes part in.
- *   losses, lse : [T] fp32.  kept : [T,K] fp32 or NULL (no gradients are wanted): what the backward call takes, entries in an order of the library's.
+ *   losses, lse : [T] fp32.  kept : [T,K] fp32 or NULL (no gradients are wanted): what the backward call takes, entries in an order of the library's (0 for what is no entry).
  *   mean, reduction, dtypes, sizes, precision and workspaces as for sphattn_vocab_loss_fwd (the logits have its errors), all_rows 0.
  * 1 <= K <= 1024 (SPHATTN_ERR_SHAPE); 2^-20 <= tau <= 2^20 and scale / tau finite (SPHATTN_ERR_VALUE).
  */

@@ -962,7 +962,8 @@ inline int taught_lds_bytes(int padded) { return kTaughtWaves * padded * 12; }
 
 __global__ __launch_bounds__(kTaughtThreads)
 void taught_kernel(const void* __restrict__ ids, int id_bytes, const float* __restrict__ teacher, int T, int V, int K, int padded, float over_tau,
-                   int* __restrict__ targets, int* __restrict__ sorted, float* __restrict__ weights, unsigned short* __restrict__ starts, int shift, int blocks)
+                   int* __restrict__ targets, int* __restrict__ sorted, float* __restrict__ weights, unsigned short* __restrict__ starts, int shift, int blocks,
+                   float* __restrict__ logits)    // forward: those of no entry are 0, the rest is the tiles'
 {
     extern __shared__ __attribute__((aligned(16))) unsigned char smem_raw[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -1007,6 +1008,7 @@ void taught_kernel(const void* __restrict__ ids, int id_bytes, const float* __re
         const uint64_t key = keys[k];
         sorted[row + k] = counts ? (int)(key >> 32) : 0x7fffffff;
         weights[row + k] = p[(uint32_t)key] / sum;
+        if (starts && (!counts || (int)(key >> 32) == 0x7fffffff)) logits[row + k] = 0.f;
     }
     if (lane == 0) targets[t] = !counts ? -1 : bad ? 0x7fffffff : 0;
     if (!starts) return;

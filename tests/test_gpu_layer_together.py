@@ -1,0 +1,142 @@
+"""Embedding, heads, attention, feed-forward, distillation and clipping together, as a training step uses them: examples/distill_masked_genes.py, its gradients
+against the same model in 64 bits, the step captured into a graph, and calls of several streams at once."""
+import importlib.util
+import math
+import os
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.fixture(scope="module")
+def example():
+    spec = importlib.util.spec_from_file_location("distill_masked_genes", os.path.join(ROOT, "examples", "distill_masked_genes.py"))
+    module = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(module)
+    return module
+
+
+def test_the_example_runs(example):
+    losses, norms = example.train(steps=3, batch=2, length=100, genes=600, types=6, inner=136)
+    assert len(losses) == len(norms) == 3 and all(math.isfinite(x) and x > 0 for x in losses + norms)
+
+
+def _plain(weights, tokens, counts, ids, teacher, heads, key_heads, example):
+    """The example's loss from elementary operations on the weights' own type."""
+    table, Wqkv, wq, wk, Wo, Wg, Wu, Wd = weights
+    t, (B, N), D = table.dtype, tokens.shape, table.shape[1]
+    width = D // heads
+    inv_freq, sections = example.frequencies(width, tokens.device)
+    X = table[tokens] * (math.sqrt(D) * torch.log1p(counts).to(t))[..., None]
+    q, k, v = (X @ Wqkv).view(B, N, -1, width).split([heads, key_heads, key_heads], 2)
+    at = torch.cat([(tokens % example.CHROMOSOMES)[..., None].expand(B, N, sections[0]), (tokens // example.CHROMOSOMES)[..., None].expand(B, N, sections[1])], -1)
+    angle = (at * inv_freq.to(t))[:, :, None]
+
+    def turned(x, w):
+        y = x / (x.square().mean(-1, keepdim=True) + 1e-6).sqrt() * w
+        a, b = y.chunk(2, -1)
+        return torch.cat([a * angle.cos() - b * angle.sin(), b * angle.cos() + a * angle.sin()], -1).transpose(1, 2)
+    Q, K = turned(q, wq), turned(k, wk).repeat_interleave(heads // key_heads, 1)
+    S = (Q.unsqueeze(3) * K.unsqueeze(2)).sum(-1)
+    S = S / S.square().sum(-1, keepdim=True).sqrt()
+    O = (S.unsqueeze(-1) * v.transpose(1, 2).repeat_interleave(heads // key_heads, 1).unsqueeze(2)).sum(3)
+    X = X + O.transpose(1, 2).reshape(B, N, D) @ Wo
+    A = X @ Wg.t()
+    X = X + (A * torch.sigmoid(A) * (X @ Wu.t())) @ Wd
+    tau = example.TEMPERATURE
+    logp = torch.log_softmax(X @ table.t() / tau, -1)
+    there = ids >= 0
+    p = torch.softmax(torch.where(there, teacher.to(t) / tau, -math.inf), -1)
+    counted = there.any(-1)
+    p = torch.where(there, p, 0.0)
+    term = torch.where(there, torch.special.xlogy(p, p) - p * logp.gather(-1, ids.clamp_min(0)), 0.0).sum(-1)
+    return tau ** 2 * torch.where(counted, term, 0.0).sum() / counted.sum()
+
+
+def _setup(example, dtype, seed=3):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    heads, key_heads = 4, 2
+    weights = example.new_weights(500, heads, key_heads, 64, 200, g, DEV, dtype)
+    return weights, example.cells(2, 40, 500, 5, 9, g, DEV), heads, key_heads, g
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_gradients_of_the_whole_step(example, dtype):
+    """Between a weight and the loss its signal is rounded to the type some twelve times on the way there and some twelve on the way back (a layer's
+    tensors once each), by half a step at most each: 24 half steps of the gradient's norm, and its terms in 64 bits on the same weights."""
+    from paper_2505_09326_amd.autograd import vocab_distillation
+    weights, (tokens, counts, ids, teacher), heads, key_heads, _ = _setup(example, dtype)
+    X = example.student(weights, tokens, counts, heads, key_heads)
+    loss = vocab_distillation(X, weights[0], ids, teacher, temperature=example.TEMPERATURE, reduction="mean") * 256.0
+    grads = torch.autograd.grad(loss, weights)
+    exact = [w.detach().double().requires_grad_(True) for w in weights]
+    want_loss = _plain(exact, tokens, counts, ids, teacher, heads, key_heads, example) * 256.0
+    want = torch.autograd.grad(want_loss, exact)
+    half = torch.finfo(dtype).eps / 2
+    assert abs(float(loss) - float(want_loss)) <= 24 * half * abs(float(want_loss))
+    for i, (a, b) in enumerate(zip(grads, want)):
+        assert float((a.double() - b).norm()) <= 24 * half * float(b.norm()), i
+
+
+def test_a_step_captured_into_a_graph(example):
+    import paper_2505_09326_amd as sph
+    from paper_2505_09326_amd.autograd import vocab_distillation
+    weights, (tokens, counts, ids, teacher), heads, key_heads, g = _setup(example, torch.bfloat16)
+
+    def step():
+        loss = vocab_distillation(example.student(weights, tokens, counts, heads, key_heads), weights[0], ids, teacher, temperature=2.0)
+        grads = list(torch.autograd.grad(loss, weights))
+        return loss.detach(), sph.sphattn_clip_grads(grads, 1.0), *grads
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        for _ in range(2):
+            step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    for i in range(3):
+        with torch.no_grad():
+            for w in weights:
+                w.mul_(1.01)
+            fresh = example.cells(2, 40, 500, 5, 9, g, DEV)
+            for a, b in zip((tokens, counts, ids, teacher), fresh):
+                a.copy_(b)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in out]
+        for a, b in zip(got, step()):
+            assert torch.equal(a, b), i
+
+
+def test_calls_of_several_streams_and_threads(example):
+    """The same calls on streams of their own, from threads of their own, give the bits of one after the other."""
+    import threading
+    from paper_2505_09326_amd.autograd import vocab_distillation
+    setups = [_setup(example, torch.bfloat16, seed) for seed in range(4)]
+
+    def step(s):
+        weights, (tokens, counts, ids, teacher), heads, key_heads, _ = s
+        loss = vocab_distillation(example.student(weights, tokens, counts, heads, key_heads), weights[0], ids, teacher, temperature=2.0)
+        return [loss.detach(), *torch.autograd.grad(loss, weights)]
+    want = [step(s) for s in setups]
+    torch.cuda.synchronize()
+    got = [None] * 4
+
+    def work(i):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            for _ in range(3):
+                got[i] = step(setups[i])
+            torch.cuda.current_stream().synchronize()
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    for a, b in zip(got, want):
+        for x, y in zip(a, b):
+            assert torch.equal(x, y)

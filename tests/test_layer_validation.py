@@ -89,3 +89,97 @@ def test_head_norm_rotary_binding_checks():
             bad()
     with pytest.raises(ValueError):
         autograd.head_norm_rotary(x, x)                        # not on a GPU
+
+
+def test_gated_ffn_errors(lib):
+    T, D, F = 100, 64, 96
+    size, back_size = lib.sphattn_gated_ffn_workspace_bytes, lib.sphattn_gated_ffn_bwd_workspace_bytes
+    for f in (size, back_size):
+        assert f(T, D, F, 1) > 0 and f(T, D, F, 0) > f(T, D, F, 1)
+        assert f(-1, D, F, 1) == f(T, 0, F, 1) == f(T, D, 0, 1) == f(T, D, F, 2) == f(2 ** 20 + 1, D, F, 1) == f(2 ** 20, D, 2 ** 18, 1) == f(T, 65537, F, 1) == 0
+    assert size(64, D, F, 0) == 0 and back_size(64, D, F, 1) > 0 and back_size(T, D, F, 3) > back_size(T, D, F, 1)
+    need = size(T, D, F, 1)
+
+    def fwd(X=0x1000000, Wg=0x2000000, Wu=0x3000000, H=0x4000000, T=T, D=D, F=F, gate=0, dtype=1, ws=WS, size=need):
+        return lib.sphattn_gated_ffn_fwd(P(X), P(Wg), P(Wu), P(H), T, D, F, gate, dtype, P(ws), size, None)
+    assert fwd(X=0) == -1 and fwd(Wg=0) == -1 and fwd(Wu=0) == -1 and fwd(H=0) == -1
+    assert fwd(T=-1) == -2 and fwd(D=0) == -2 and fwd(F=2 ** 18 + 1) == -2 and fwd(T=2 ** 20, F=2 ** 17) == -2
+    assert fwd(dtype=2) == -4 and fwd(X=0x1000001) == -5 and fwd(H=0x4000002, dtype=0) == -5 and fwd(gate=3) == -11 and fwd(gate=-1) == -11
+    assert fwd(ws=0) == -9 and fwd(ws=WS + 8) == -9 and fwd(size=need - 1) == -9
+    assert fwd(H=0x1000000) == -7 and fwd(H=0x2000000 + 64) == -7 and fwd(H=WS) == -7 and fwd(X=WS + 16) == -7
+    assert fwd(T=0, X=0, H=0, ws=0, size=0) == 0
+    need = back_size(T, D, F, 1)
+
+    def bwd(X=0x1000000, Wg=0x2000000, Wu=0x3000000, dH=0x4000000, dX=0x5000000, dWg=0x6000000, dWu=0x7000000, gate=0, dtype=1, ws=WS, size=need, T=T):
+        return lib.sphattn_gated_ffn_bwd(P(X), P(Wg), P(Wu), P(dH), P(dX), P(dWg), P(dWu), T, D, F, gate, dtype, P(ws), size, None)
+    assert bwd(X=0) == -1 and bwd(dH=0) == -1 and bwd(dX=0, dWg=0, dWu=0) == -1
+    assert bwd(T=-1) == -2 and bwd(dtype=7) == -4 and bwd(dWu=0x7000001) == -5 and bwd(gate=9) == -11
+    assert bwd(ws=0) == -9 and bwd(size=need - 1) == -9
+    assert bwd(dX=0x1000000) == -7 and bwd(dWg=0x7000000) == -7 and bwd(dWu=0x4000000) == -7 and bwd(dX=WS) == -7 and bwd(dWg=0x2000000 + 2) == -7
+
+
+def test_gated_ffn_binding_checks():
+    X, W, H = torch.zeros(10, 8), torch.zeros(12, 8), torch.zeros(10, 12)
+    fwd, bwd = pkg.sphattn_gated_ffn_fwd, pkg.sphattn_gated_ffn_bwd
+    for bad in (lambda: fwd(X, W, W), lambda: fwd(X[0], W, W), lambda: fwd(X, W[:, :4], W), lambda: fwd(X, W, W.half()), lambda: fwd(X.double(), W, W),
+                lambda: fwd(X.t().contiguous().t(), W, W), lambda: fwd(X, W, W, stream=0), lambda: bwd(X, W, W, H[:9]), lambda: bwd(X, W, W, H.half()),
+                lambda: bwd(X, W, W, H, want_dX=False, want_dWg=False, want_dWu=False), lambda: bwd(X, W, W, H, stream=0)):
+        with pytest.raises(ValueError):
+            bad()
+    with pytest.raises(KeyError):
+        fwd(X, W, W, "tanh")
+    with pytest.raises(TypeError):
+        autograd.gated_feed_forward(X, W.half(), W)
+
+
+def test_distillation_errors(lib):
+    T, V, D, K = 100, 500, 64, 20
+    sizes = [lib.sphattn_vocab_distill_workspace_bytes, lib.sphattn_vocab_distill_bwd_workspace_bytes]
+    for size in sizes:
+        assert size(T, V, D, K, 1) > 0 and size(T, V, D, K, 0) > size(T, V, D, K, 1)
+        assert size(-1, V, D, K, 1) == size(T, 0, D, K, 1) == size(T, V, D, 0, 1) == size(T, V, D, 1025, 1) == size(T, V, D, K, 2) == size(T, 2 ** 24 + 1, D, K, 1) == 0
+    for T2 in (1, 2 ** 20):                        # no size of the ranges overflows on the way
+        for V2 in (1, 50003, 2 ** 24):
+            for K2 in (1, 1024):
+                assert sizes[0](T2, V2, D, K2, 1) > 2 * (T2 + V2) * D + 12 * T2 * K2 and sizes[1](T2, V2, D, K2, 1) > 8 * T2 * K2
+                assert sizes[0](T2, V2, D, K2, 1) < 4 * (T2 + V2) * D + 16 * T2 * K2 + T2 * V2 // 8 + (1 << 30)
+    need = sizes[0](T, V, D, K, 1)
+
+    def fwd(X=0x1000000, W=0x2000000, ids=0x3000000, id_bytes=8, teacher=0x3800000, losses=0x4000000, lse=0x4100000, kept=0x4200000, mean=0x4300000, T=T, V=V, K=K,
+            scale=1.0, tau=1.0, reduction=2, dtype=1, ws=WS, size=need):
+        return lib.sphattn_vocab_distill_fwd(P(X), P(W), P(ids), id_bytes, P(teacher), P(losses), P(lse), P(kept), P(mean), T, V, D, K, scale, tau, reduction,
+                                             dtype, P(ws), size, None)
+    assert fwd(X=0) == -1 and fwd(W=0) == -1 and fwd(ids=0) == -1 and fwd(teacher=0) == -1 and fwd(losses=0) == -1 and fwd(lse=0) == -1
+    assert fwd(T=-1) == -2 and fwd(V=0) == -2 and fwd(K=0) == -2 and fwd(K=1025) == -2
+    assert fwd(dtype=2) == -4 and fwd(id_bytes=2) == -4 and fwd(teacher=0x3800002) == -5 and fwd(kept=0x4200002) == -5 and fwd(ids=0x3000004) == -5
+    assert fwd(scale=float("inf")) == -11 and fwd(reduction=3) == -11
+    for tau in (0.0, -1.0, float("nan"), float("inf"), 2.0 ** -21, 2.0 ** 21):
+        assert fwd(tau=tau) == -11
+    assert fwd(scale=3e38, tau=2.0 ** -20) == -11
+    assert fwd(ws=0) == -9 and fwd(ws=WS + 4) == -9 and fwd(size=need - 1) == -9
+    assert fwd(kept=0x3800000) == -7 and fwd(lse=0x4000000) == -7 and fwd(losses=0x3000000) == -7 and fwd(W=WS) == -7 and fwd(kept=WS + need - 4) == -7
+    need = sizes[1](T, V, D, K, 1)
+
+    def bwd(X=0x1000000, lse=0x4100000, kept=0x4200000, dloss=0x4300000, dX=0x5000000, dW=0x6000000, tau=1.0, reduction=2, ws=WS, size=need, teacher=0x3800000):
+        return lib.sphattn_vocab_distill_bwd(P(X), P(0x2000000), P(0x3000000), 8, P(teacher), P(lse), P(kept), P(dloss), P(dX), P(dW), T, V, D, K, 1.0, tau,
+                                             reduction, 1, P(ws), size, None)
+    assert bwd(lse=0) == -1 and bwd(kept=0) == -1 and bwd(dloss=0) == -1 and bwd(dX=0, dW=0) == -1 and bwd(teacher=0) == -1
+    assert bwd(dX=0x5000001) == -5 and bwd(tau=0.0) == -11 and bwd(reduction=-1) == -11 and bwd(ws=0) == -9 and bwd(size=need - 1) == -9
+    assert bwd(dX=0x1000000) == -7 and bwd(dW=0x2000000 + 64) == -7 and bwd(dW=0x4200000) == -7 and bwd(dX=0x6000000) == -7
+
+
+def test_distillation_binding_checks():
+    X, W, ids, teacher, one = torch.zeros(6, 8), torch.zeros(12, 8), torch.zeros((6, 3), dtype=torch.int64), torch.zeros(6, 3), torch.ones(6)
+    fwd, bwd = pkg.sphattn_vocab_distill_fwd, pkg.sphattn_vocab_distill_bwd
+    for bad in (lambda: fwd(X, W, ids, teacher), lambda: fwd(X, W, ids[:5], teacher), lambda: fwd(X, W, ids, teacher[:, :2]), lambda: fwd(X, W, ids.float(), teacher),
+                lambda: fwd(X, W, ids, teacher.double()), lambda: fwd(X, W.half(), ids, teacher), lambda: fwd(X, W, ids[0], teacher), lambda: fwd(X, W[:, :4], ids, teacher),
+                lambda: fwd(X, W, ids, teacher, float("nan")), lambda: fwd(X, W, ids, teacher, 1.0, 0.0), lambda: fwd(X, W, ids, teacher, 1.0, float("nan")),
+                lambda: fwd(X, W, ids, teacher, stream=0), lambda: fwd(X, W, ids.t().contiguous().t(), teacher), lambda: bwd(X, W, ids, teacher, one, teacher, one),
+                lambda: bwd(X, W, ids, teacher, one, teacher[:3], one), lambda: bwd(X, W, ids, teacher, one, teacher, one[:2]),
+                lambda: bwd(X, W, ids, teacher, one, teacher, one, reduction="mean"), lambda: bwd(X, W, ids, teacher, one, teacher, one, want_dX=False, want_dW=False),
+                lambda: bwd(X, W, ids, teacher, one, teacher, one, stream=0), lambda: autograd.vocab_distillation(X, W, ids[:5], teacher[:5]),
+                lambda: autograd.vocab_distillation(X, W, ids, teacher[:5]), lambda: autograd.vocab_distillation(X, W, ids, teacher, temperature=-1.0)):
+        with pytest.raises(ValueError):
+            bad()
+    with pytest.raises(KeyError):
+        fwd(X, W, ids, teacher, reduction="most")
