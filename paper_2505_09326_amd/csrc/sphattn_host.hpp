@@ -70,7 +70,7 @@ public:
     explicit Carve(void* base) : base_((unsigned char*)base) {}
     template <typename T> T* take(size_t count)
     {
-        T* p = base_ ? (T*)(base_ + used_) : nullptr;
+        T* p = base_ ? (T*)((uintptr_t)base_ + used_) : nullptr;
         used_ += (count * sizeof(T) + 255) / 256 * 256;
         return p;
     }
