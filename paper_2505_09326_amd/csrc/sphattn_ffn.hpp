@@ -32,13 +32,16 @@ __device__ __forceinline__ void gate(float a, float& act, float& slope)
         act = a <= 0.f ? 0.f : a;
         slope = a > 0.f ? 1.f : 0.f;
     } else if constexpr (G == Gate::Silu) {
-        const float e = exp_of(fminf(-a, 87.f));   // (where it ends, a / (1 + e) is below 1e-35)
-        float s;
-        if constexpr (EXACT) s = 1.f / (1.f + e);
-        else s = __builtin_amdgcn_rcpf(1.f + e);
-        act = a * s;
-        slope = s * __builtin_fmaf(a, e * s, 1.f);
-        if (a != a) act = slope = a;               // (the minimum has lost it)
+        if constexpr (EXACT) {
+            const float e = exp_of(fminf(-a, 87.f)), s = 1.f / (1.f + e);   // (where it ends, a / (1 + e) is below 1e-35)
+            act = a * s;
+            slope = s * __builtin_fmaf(a, e * s, 1.f);
+            if (a != a) act = slope = a;           // (the minimum has lost it)
+        } else {                                   // (an infinite exponential gives zeros; 1 - s is off by 2^-24 where s is near 1)
+            const float s = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(a * -kLog2e));
+            act = a * s;
+            slope = __builtin_fmaf(act, 1.f - s, s);
+        }
     } else {
         const float half = exp_of(fmaxf(-0.5f * a * a, -87.f));
         float below;                               // the normal distribution's share below a
@@ -404,13 +407,19 @@ void ffn_dw_kernel(FfnSum a, FfnSum b, int each)
     ffn_sum_tile<T, S, false>(second ? b : a, (int)blockIdx.x - (second ? each : 0), (SPH_LDS unsigned char*)smem_raw);
 }
 
-// Slices added up in order, scaled and rounded: a wave 256 columns of a row, eight slices' loads under way
+// Slices added up in order, scaled and rounded, of up to three results: a wave 256 columns of a row, eight slices' loads under way
+struct FfnJoin { FfnSum sum[3]; int columns[3]; long long until[2]; };   // waves below until[0] on the first, below until[1] on the second
+
 template <Store S>
 __global__ __launch_bounds__(256)
-void ffn_join_kernel(FfnSum a, int columns)
+void ffn_join_kernel(FfnJoin j)
 {
     const int lane = threadIdx.x & 63;
-    const long long unit = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = unit / columns;
+    const long long wave = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int m = wave < j.until[0] ? 0 : wave < j.until[1] ? 1 : 2;
+    const FfnSum& a = j.sum[m];
+    const int columns = max(j.columns[m], 1);
+    const long long unit = wave - (m == 0 ? 0 : j.until[m - 1]), q = unit / columns;
     if (q >= a.out_rows) return;
     const int c = (int)(unit - q * columns) * 256 + lane * 4;
     if (c >= a.out_cols) return;

@@ -25,7 +25,7 @@ struct HeadsArgs {
     const float* inv_freq; int until[2];           // frequencies below until[0] go by the first axis, below until[1] by the second, the rest by the third
     int interleaved, norm;
     float eps;
-    int B, N, share;                               // groups of lanes that share a token's heads
+    int B, N, log_share;                           // groups of lanes that share a token's heads: 1 << log_share
     float* partial;                                // backward: [workgroups][2][d] sums of dw, or NULL
 };
 
@@ -149,19 +149,43 @@ struct HeadsLane {
     }
     // The fraction of a turn is taken in fp64: position times frequency is exact there up to 2^29, and what fp32 would leave of
     // an angle of a far position is no angle any more.
-    __device__ __forceinline__ void angles(const HeadsArgs& a, long long b, long long n, float (&cos)[4], float (&sin)[4]) const
+    // (loaded before a token's rows are, used behind that)
+    struct Place { long long at[4]; };
+    __device__ __forceinline__ Place place(const HeadsArgs& a, long long b, long long n) const
     {
+        Place p;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const long long at = axis[i] * a.pos_axis + b * a.pos_batch + n;
-            const double p = a.id_bytes == 4 ? (double)((const int*)a.positions)[at] : (double)((const long long*)a.positions)[at];
-            const double t = p * turns[i];
+            p.at[i] = a.id_bytes == 4 ? (long long)((const int*)a.positions)[at] : ((const long long*)a.positions)[at];
+        }
+        return p;
+    }
+    __device__ __forceinline__ void angles(const Place& p, float (&cos)[4], float (&sin)[4]) const
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const double t = (double)p.at[i] * turns[i];
             sincospif(2.f * (float)(t - __builtin_rint(t)), &sin[i], &cos[i]);
         }
     }
 };
 
-// Groups of d / 8 lanes take tokens, or (share > 1, where tokens are few) every share-th head of one.
+// Which token and which of its heads a group of lanes takes.  (32-bit numbers: a division of 64 bits is 150 instructions; there are less than 2^31 tokens, and
+// they are shared only where they are few)
+struct HeadsUnit {
+    long long b, n;
+    int first;
+    __device__ __forceinline__ HeadsUnit(const HeadsArgs& a, unsigned u)
+    {
+        const unsigned token = u >> a.log_share, batch = token / (unsigned)a.N;
+        b = batch;
+        n = token - batch * (unsigned)a.N;
+        first = (int)(u - (token << a.log_share));
+    }
+};
+
+// Groups of d / 8 lanes take tokens, or (where tokens are few) every share-th head of one.
 template <Store S, int D, bool ROTATE>
 __global__ __launch_bounds__(kHeadsThreads)
 void heads_fwd_kernel(HeadsArgs a)
@@ -170,24 +194,30 @@ void heads_fwd_kernel(HeadsArgs a)
     const int l = threadIdx.x % LANES;
     HeadsLane<S, D> lane;
     lane.begin(a, l);
-    const long long units = (long long)a.B * a.N * a.share, step = (long long)gridDim.x * (kHeadsThreads / LANES);
-    for (long long u = (long long)blockIdx.x * (kHeadsThreads / LANES) + threadIdx.x / LANES; u < units; u += step) {
-        const long long token = u / a.share, b = token / a.N, n = token - b * a.N;
-        const int first = (int)(u - token * a.share);
+    const unsigned units = (unsigned)a.B * (unsigned)a.N << a.log_share, step = gridDim.x * (kHeadsThreads / LANES);
+    const int share = 1 << a.log_share;
+    for (unsigned u = blockIdx.x * (kHeadsThreads / LANES) + threadIdx.x / LANES; u < units; u += step) {
+        const HeadsUnit unit(a, u);
+        typename HeadsLane<S, D>::Place place;
+        if constexpr (ROTATE) place = lane.place(a, unit.b, unit.n);
+        HeadRow<S, D> rows[AHEAD];
+        auto fetch = [&](const HeadSide& side, int h0) {
+            const unsigned char* from = side.x.data + unit.b * side.x.batch + unit.n * side.x.token;
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) rows[i] = load_row<S, D>(from + min(h0 + i * share, side.heads - 1) * side.x.head, l);
+        };
+        fetch(a.side[0], unit.first);
         float cos[4], sin[4];
-        if constexpr (ROTATE) lane.angles(a, b, n, cos, sin);
+        if constexpr (ROTATE) lane.angles(place, cos, sin);
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
             const HeadSide& side = a.side[s];
-            const unsigned char* from = side.x.data + b * side.x.batch + n * side.x.token;
-            unsigned char* to = side.o.data + b * side.o.batch + n * side.o.token;
-            for (int h0 = first; h0 < side.heads; h0 += AHEAD * a.share) {
-                HeadRow<S, D> rows[AHEAD];
-#pragma unroll
-                for (int i = 0; i < AHEAD; ++i) rows[i] = load_row<S, D>(from + min(h0 + i * a.share, side.heads - 1) * side.x.head, l);
+            unsigned char* to = side.o.data + unit.b * side.o.batch + unit.n * side.o.token;
+            for (int h0 = unit.first; h0 < side.heads; h0 += AHEAD * share) {
+                if (s > 0 || h0 > unit.first) fetch(side, h0);
 #pragma unroll
                 for (int i = 0; i < AHEAD; ++i) {
-                    const int h = h0 + i * a.share;
+                    const int h = h0 + i * share;
                     float x[8];
                     widen_row<S, D>(rows[i], x);
                     float r = 1.f;
@@ -218,29 +248,31 @@ void heads_bwd_kernel(HeadsArgs a)
     float dw[2][8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) dw[0][k] = dw[1][k] = 0.f;
-    const long long units = (long long)a.B * a.N * a.share, step = (long long)gridDim.x * (kHeadsThreads / LANES);
-    for (long long u = (long long)blockIdx.x * (kHeadsThreads / LANES) + threadIdx.x / LANES; u < units; u += step) {
-        const long long token = u / a.share, b = token / a.N, n = token - b * a.N;
-        const int first = (int)(u - token * a.share);
+    const unsigned units = (unsigned)a.B * (unsigned)a.N << a.log_share, step = gridDim.x * (kHeadsThreads / LANES);
+    const int share = 1 << a.log_share;
+    for (unsigned u = blockIdx.x * (kHeadsThreads / LANES) + threadIdx.x / LANES; u < units; u += step) {
+        const HeadsUnit unit(a, u);
+        const long long b = unit.b, n = unit.n;
+        const int first = unit.first;
         float cos[4], sin[4];
-        if constexpr (ROTATE) lane.angles(a, b, n, cos, sin);
+        if constexpr (ROTATE) lane.angles(lane.place(a, b, n), cos, sin);
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
             const HeadSide& side = a.side[s];
             const unsigned char* from = side.x.data + b * side.x.batch + n * side.x.token;
             const unsigned char* grad = side.o.data + b * side.o.batch + n * side.o.token;
             unsigned char* to = side.dx.data ? side.dx.data + b * side.dx.batch + n * side.dx.token : nullptr;
-            for (int h0 = first; h0 < side.heads; h0 += AHEAD * a.share) {
+            for (int h0 = first; h0 < side.heads; h0 += AHEAD * share) {
                 HeadRow<S, D> rows[AHEAD], grads[AHEAD];
 #pragma unroll
                 for (int i = 0; i < AHEAD; ++i) {
-                    const int h = min(h0 + i * a.share, side.heads - 1);
+                    const int h = min(h0 + i * share, side.heads - 1);
                     rows[i] = load_row<S, D>(from + h * side.x.head, l);
                     grads[i] = load_row<S, D>(grad + h * side.o.head, l);
                 }
 #pragma unroll
                 for (int i = 0; i < AHEAD; ++i) {
-                    const int h = h0 + i * a.share;
+                    const int h = h0 + i * share;
                     float x[8], dy[8];
                     widen_row<S, D>(rows[i], x);
                     widen_row<S, D>(grads[i], dy);
@@ -303,6 +335,7 @@ void heads_dw_kernel(const float* __restrict__ partial, int groups, int D, void*
     __shared__ float shared[64][16];
     const int col = (int)blockIdx.x * 16 + (threadIdx.x & 15), row = threadIdx.x >> 4;
     float x = 0.f;
+#pragma unroll 8
     for (int g = row; g < groups; g += 64) x += partial[(size_t)g * 2 * D + col];
     shared[row][threadIdx.x & 15] = x;
     __syncthreads();

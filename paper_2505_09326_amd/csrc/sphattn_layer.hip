@@ -112,12 +112,12 @@ int heads_check(HeadsCall& c, const sphattn_heads* Xq, const sphattn_heads* Xk, 
 
 // Groups of lanes per token: one takes all heads of its token, for which it forms the angles once, where tokens alone make two waves for every
 // SIMD; else as many more as that takes.  (waves: 256 CUs with four SIMDs)
-int heads_share(long long tokens, int heads, int d)
+int heads_log_share(long long tokens, int heads, int d)
 {
-    int share = 1;
-    while (share * 4 <= heads && tokens * share * (d / 8) < 64ll * 4 * kCus * 2) share *= 2;
-    while (share < heads && tokens * share * (d / 8) < 64ll * kCus) share *= 2;
-    return share;
+    int log = 0;
+    while (4 << log <= heads && (tokens << log) * (d / 8) < 64ll * 4 * kCus * 2) ++log;
+    while (1 << log < heads && (tokens << log) * (d / 8) < 64ll * kCus) ++log;
+    return log;
 }
 
 template <Store S, bool FORWARD>
@@ -142,7 +142,7 @@ int run_heads(const HeadsArgs& a, int d, int groups, hipStream_t s)
 long long heads_groups(const HeadsArgs& a, int d)
 {
     const int per = kHeadsThreads / (d / 8);
-    return ((long long)a.B * a.N * a.share + per - 1) / per;
+    return (((long long)a.B * a.N << a.log_share) + per - 1) / per;
 }
 
 // ---- gated feed-forward ------------------------------------------------------------------------------------
@@ -180,7 +180,7 @@ struct Ffn {
     unsigned short *x, *g, *u, *x_sum, *g_sum, *u_sum;
     unsigned short *dA, *dB, *dA_all, *dB_all;
     float *x_bound, *w_norm, *row_up, *row_down, *all_up;   // fp16
-    float* part;                                   // of dX, then of dW
+    float *part, *part_w;                          // slices of dX and of dW
     size_t bytes;
 };
 
@@ -216,8 +216,8 @@ Ffn ffn_plan(int T, int D, int F, int dtype, bool back, void* workspace)
         const int products = f32 ? 6 : 1;
         p.dx = sum_choice(T > 0 ? T : 1, p.ld, 2ll * F, 1, products);
         p.dw = T > 0 ? sum_choice(F, p.ld, T, 2, products) : SumChoice{false, 1};
-        const size_t of_dx = p.dx.slices > 1 ? (size_t)p.dx.slices * T * p.ld : 0, of_dw = p.dw.slices > 1 ? (size_t)p.dw.slices * 2 * F * p.ld : 0;
-        p.part = c.take<float>(of_dx > of_dw ? of_dx : of_dw);
+        p.part = c.take<float>(p.dx.slices > 1 ? (size_t)p.dx.slices * T * p.ld : 0);
+        p.part_w = c.take<float>(p.dw.slices > 1 ? (size_t)p.dw.slices * 2 * F * p.ld : 0);
     }
     p.bytes = c.used();
     return p;
@@ -311,11 +311,20 @@ int launch_sum(FfnSum& a, FfnSum* b, hipStream_t stream)
 }
 
 template <Store S>
-int join_slices(const FfnSum& a, hipStream_t stream)
+int join_slices(const FfnSum (&sums)[3], int n, hipStream_t stream)
 {
-    const int columns = (a.out_cols + 255) / 256;
-    const long long waves = (long long)a.out_rows * columns;
-    hipLaunchKernelGGL((ffn_join_kernel<S>), dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, stream, a, columns);
+    FfnJoin j{};
+    long long waves = 0;
+    for (int i = 0; i < 3; ++i) {
+        if (i < n) {
+            j.sum[i] = sums[i];
+            j.columns[i] = (sums[i].out_cols + 255) / 256;
+            waves += (long long)sums[i].out_rows * j.columns[i];
+        }
+        if (i < 2) j.until[i] = waves;
+    }
+    if (waves > 1ll << 26) return SPHATTN_ERR_LAUNCH;                 // (slices are for results that fit memory many times over: 2^26 waves are 2^34 elements)
+    hipLaunchKernelGGL((ffn_join_kernel<S>), dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, stream, j);
     return launched();
 }
 
@@ -345,6 +354,8 @@ int run_ffn_bwd(const Ffn& p, const void* X, const void* Wg, const void* Wu, con
     auto columns = [&](const Operand& o, const unsigned short* sum, int rows) {
         return F32 ? Operand{(const unsigned char*)sum, (long long)rows * p.ld * 2, p.ld * 2, p.ld} : Operand{o.data, 0, o.ld, p.ld};
     };
+    FfnSum cut[3];                                 // in slices
+    int n_cut = 0;
     if (rc == SPHATTN_OK && dX && p.T > 0) {
         FfnSum s{};
         s.P = columns(a.G, p.g_sum, p.F), s.P2 = columns(a.U, p.u_sum, p.F);
@@ -352,7 +363,7 @@ int run_ffn_bwd(const Ffn& p, const void* X, const void* Wg, const void* Wu, con
         s.k = p.F, s.slices = p.dx.slices, s.out = dX, s.out_ld = s.out_cols = p.D, s.out_rows = p.T, s.part = p.part, s.part_ld = p.ld;
         if (F16) s.row_down = p.row_down;
         rc = p.dx.big ? launch_sum<Big, S, true>(s, nullptr, stream) : launch_sum<Mid, S, true>(s, nullptr, stream);
-        if (rc == SPHATTN_OK && s.slices > 1) rc = join_slices<S>(s, stream);
+        if (s.slices > 1) cut[n_cut++] = s;
     }
     if (rc == SPHATTN_OK && dw) {
         FfnSum s[2]{};
@@ -364,14 +375,15 @@ int run_ffn_bwd(const Ffn& p, const void* X, const void* Wg, const void* Wu, con
             s[n].P = columns(a.X, p.x_sum, p.T);
             s[n].Q = Operand{(const unsigned char*)q, part, p.ldf * 2, p.ldf};
             s[n].k = p.T, s[n].slices = p.dw.slices, s[n].out = out, s[n].out_ld = s[n].out_cols = p.D, s[n].out_rows = p.F;
-            s[n].part = p.part ? p.part + (size_t)n * p.dw.slices * p.F * p.ld : nullptr, s[n].part_ld = p.ld;
+            s[n].part = p.part_w ? p.part_w + (size_t)n * p.dw.slices * p.F * p.ld : nullptr, s[n].part_ld = p.ld;
             if (F16 && p.T > 0) s[n].down = p.all_up + 1;
             ++n;
         }
         FfnSum* second = n == 2 ? &s[1] : nullptr;
         rc = p.dw.big ? launch_sum<Big, S, false>(s[0], second, stream) : launch_sum<Mid, S, false>(s[0], second, stream);
-        for (int m = 0; m < n && rc == SPHATTN_OK && s[m].slices > 1; ++m) rc = join_slices<S>(s[m], stream);
+        for (int m = 0; m < n && s[m].slices > 1; ++m) cut[n_cut++] = s[m];
     }
+    if (rc == SPHATTN_OK && n_cut) rc = join_slices<S>(cut, n_cut, stream);
     return rc;
 }
 
@@ -407,7 +419,7 @@ int sphattn_head_norm_rotary_fwd(const sphattn_heads* Xq, const sphattn_heads* X
     if (B == 0 || N == 0) return SPHATTN_OK;
     c.a.side[0].o = rows_of(Q, c.e);
     c.a.side[1].o = Hk ? rows_of(K, c.e) : HeadRows{};
-    c.a.share = heads_share((long long)B * N, Hq > Hk ? Hq : Hk, d);
+    c.a.log_share = heads_log_share((long long)B * N, Hq > Hk ? Hq : Hk, d);
     const long long groups = heads_groups(c.a, d);
     const int n = (int)(groups < 1 << 22 ? groups : 1 << 22);         // (a launch has less than 2^32 threads)
     switch (dtype) {
@@ -450,7 +462,7 @@ int sphattn_head_norm_rotary_bwd(const sphattn_heads* Xq, const sphattn_heads* X
     HeadsArgs& a = c.a;
     a.side[0].o = rows_of(dQ, c.e), a.side[0].dx = rows_of(dXq, c.e);
     a.side[1].o = Hk ? rows_of(dK, c.e) : HeadRows{}, a.side[1].dx = Hk ? rows_of(dXk, c.e) : HeadRows{};
-    a.share = heads_share((long long)B * N, Hq > Hk ? Hq : Hk, d);
+    a.log_share = heads_log_share((long long)B * N, Hq > Hk ? Hq : Hk, d);
     a.partial = sums ? (float*)workspace : nullptr;
     const long long groups = heads_groups(a, d);
     const int n = (int)(groups < kHeadsMostGroups ? groups : kHeadsMostGroups);
