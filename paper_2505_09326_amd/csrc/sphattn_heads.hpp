@@ -200,13 +200,15 @@ void heads_fwd_kernel(HeadsArgs a)
         const HeadsUnit unit(a, u);
         typename HeadsLane<S, D>::Place place;
         if constexpr (ROTATE) place = lane.place(a, unit.b, unit.n);
-        HeadRow<S, D> rows[AHEAD];
-        auto fetch = [&](const HeadSide& side, int h0) {
+        HeadRow<S, D> rows[2][AHEAD];
+        auto fetch = [&](int s, int h0) {
+            const HeadSide& side = a.side[s];
             const unsigned char* from = side.x.data + unit.b * side.x.batch + unit.n * side.x.token;
 #pragma unroll
-            for (int i = 0; i < AHEAD; ++i) rows[i] = load_row<S, D>(from + min(h0 + i * share, side.heads - 1) * side.x.head, l);
+            for (int i = 0; i < AHEAD; ++i) rows[s][i] = load_row<S, D>(from + min(h0 + i * share, side.heads - 1) * side.x.head, l);
         };
-        fetch(a.side[0], unit.first);
+        fetch(0, unit.first);
+        if (unit.first < a.side[1].heads) fetch(1, unit.first);
         float cos[4], sin[4];
         if constexpr (ROTATE) lane.angles(place, cos, sin);
 #pragma unroll
@@ -214,12 +216,12 @@ void heads_fwd_kernel(HeadsArgs a)
             const HeadSide& side = a.side[s];
             unsigned char* to = side.o.data + unit.b * side.o.batch + unit.n * side.o.token;
             for (int h0 = unit.first; h0 < side.heads; h0 += AHEAD * share) {
-                if (s > 0 || h0 > unit.first) fetch(side, h0);
+                if (h0 > unit.first) fetch(s, h0);
 #pragma unroll
                 for (int i = 0; i < AHEAD; ++i) {
                     const int h = h0 + i * share;
                     float x[8];
-                    widen_row<S, D>(rows[i], x);
+                    widen_row<S, D>(rows[s][i], x);
                     float r = 1.f;
                     if (a.norm) {
                         float ss = 0.f;

@@ -241,7 +241,8 @@ Teacher teacher_plan(int T, int V, int K, bool back, bool keep, size_t behind, v
 
 int launch_teacher(const Teacher& p, const void* ids, int id_bytes, const float* teacher, int T, int V, hipStream_t stream)
 {
-    hipLaunchKernelGGL(taught_kernel, dim3((unsigned)(T + kTaughtWaves - 1) / kTaughtWaves), dim3(kTaughtThreads), (size_t)taught_lds_bytes(p.padded), stream,
+    const auto kern = p.padded <= 64 ? taught_kernel<true> : taught_kernel<false>;
+    hipLaunchKernelGGL(kern, dim3((unsigned)(T + kTaughtWaves - 1) / kTaughtWaves), dim3(kTaughtThreads), (size_t)taught_lds_bytes(p.padded), stream,
                        ids, id_bytes, teacher, T, V, p.K, p.padded, 1.f / p.tau, p.targets, p.sorted, p.weights, p.starts, p.shift, p.blocks, p.logits);
     return launched();
 }
