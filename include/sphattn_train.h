@@ -109,7 +109,7 @@ int sphattn_vocab_distill_fwd(const void* X, const void* W, const void* ids, int
 /*
  * Gradients of that:  G[t,v] = g[t] tau^2 (exp(l[t,v] - lse[t]) - sum of p[t,k] over the entries with ids[t,k] == v) for rows that count, 0 for others
  *                     dX = (scale / tau) G W      dW = (scale / tau) G^T X
- *   lse, kept : from the forward call.  The rest as for sphattn_vocab_loss_bwd.
+ *   lse, kept : from the forward call.  The rest as for sphattn_vocab_loss_bwd; G of up to 256 rows is rounded to twice the storage type's bits.
  */
 size_t sphattn_vocab_distill_bwd_workspace_bytes(int T, int V, int D, int K, int dtype);
 int sphattn_vocab_distill_bwd(const void* X, const void* W, const void* ids, int id_bytes, const float* teacher,

@@ -8,7 +8,9 @@
 // against writing and reading 16 T F bytes (fp32: what 16 bits of A and U leave of dA and dB would be most of the error), and nothing has to be
 // kept between the two calls.  dX is one sum over 2 F (Form::Sum), dWg and dWu are two over T.
 //
-// dA and dB are rounded once to the storage type, which is what the matrix instructions take; sums are in fp32 throughout.  fp16: they are scaled by powers
+// dA and dB are rounded once to the storage type, which is what the matrix instructions take; sums are in fp32 throughout.  That rounding is as large as the results'
+// own, of 1.7e-3 in bf16 it makes 2.3e-3 against 64 bits on average over the terms; where there are few of them, up to 2^18 values, chance makes 2.6e-3 and more of it,
+// and they are kept in two 16-bit parts: twice the products, beside which launches and the weights' bytes are the time there.  fp16: they are scaled by powers
 // of two that keep them in the type's range whatever the gradients' size, by each row for dX and by the largest row for dW.
 // fp32: A and U as three products of two fp16 parts with a power of two per row, the gradients as six of three bf16 parts, as the vocabulary loss has them.
 #pragma once
@@ -70,7 +72,7 @@ struct FfnArgs {
     int k, tiles_p, T, F;
     void* H;                                       // forward: [T,F]
     const void* dH;                                // backward: [T,F]
-    unsigned short *dA, *dB; long long part; int ld;   // [T,ld], in parts (fp32)
+    unsigned short *dA, *dB; long long part; int ld;   // [T,ld], in parts (fp32 three, few values two)
     const float *row_up, *all_up; unsigned short *dA_all, *dB_all;   // fp16: factors of dA and dB, and the second pair
 };
 
@@ -111,8 +113,60 @@ __device__ __forceinline__ void whole_projections(f32x4 (&acc)[T::FP][T::FQ], co
     }
 }
 
-// A tile of BP / 2 columns of F and BQ rows: H, or dA and dB
-template <class T, Store S, bool BACK>
+// relu's slope where A is all but 0: which side it is on is for the sum in 64 bits to say, not for what fp32 has lost of it (with 2^20 values of A about one is on the other
+// side, and one slope is 1e-3 of dX).  The values below 2^-19 of their row's largest here, some ten times the sums' errors, are looked at by the whole wave one at a time: one
+// tile in twenty has one.
+template <class T, Store S>
+__device__ __forceinline__ void settle_signs(f32x4 (&acc)[T::FP][T::FQ], const FfnArgs& a, int fw, int qw)
+{
+    constexpr int R = T::FP / 2 * 4;               // values of a row in a lane
+    static_assert(R * T::FQ <= 64, "");
+    const int lane = threadIdx.x & 63, n16 = lane & 15, g = lane >> 4;
+    uint64_t open = 0, above = 0;                  // by value: not settled; greater than 0
+#pragma unroll
+    for (int j = 0; j < T::FQ; ++j) {
+        float top = 0.f;
+#pragma unroll
+        for (int v = 0; v < R; ++v) top = fmaxf(top, __builtin_fabsf(acc[v / 4 * 2][j][v & 3]));
+        top = max_across_groups(top) * 0x1p-19f;
+        top = top < __builtin_inff() ? top : 0.f;  // (nothing is near 0 beside an infinite value)
+#pragma unroll
+        for (int v = 0; v < R; ++v) {
+            const float x = acc[v / 4 * 2][j][v & 3];
+            const bool near = __builtin_fabsf(x) < top && x != 0.f && fw + v / 4 * 16 + 4 * g + (v & 3) < a.F && qw + 16 * j + n16 < a.T;
+            open |= (uint64_t)near << (j * R + v);
+        }
+    }
+    if (!__ballot(open != 0)) return;
+    const uint64_t found = open;
+    for (uint64_t lanes; (lanes = __ballot(open != 0)) != 0;) {
+        const int who = __builtin_ctzll(lanes);
+        const int which = __builtin_amdgcn_readlane(open ? __builtin_ctzll(open) : 0, who), j = which / R, v = which % R;
+        const size_t f = fw + v / 4 * 16 + 4 * (who >> 4) + (v & 3), q = qw + 16 * j + (who & 15);
+        double sum = 0.0;
+        if constexpr (S == Store::F32) {
+            for (int k = lane; k < a.D; k += 64) sum += (double)a.x_whole[q * a.D + k] * (double)a.g_whole[f * a.D + k];
+        } else {
+            for (int k = lane; k < a.D; k += 64) sum += (double)load_el<S>(a.X.data + q * a.X.ld, k) * (double)load_el<S>(a.G.data + f * a.G.ld, k);
+        }
+#pragma unroll
+        for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+        if (lane == who) {
+            open &= open - 1;
+            above |= (uint64_t)(sum > 0.0) << which;
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < T::FQ; ++j)
+#pragma unroll
+        for (int v = 0; v < R; ++v) {
+            const float x = acc[v / 4 * 2][j][v & 3], size = __builtin_fabsf(x);
+            acc[v / 4 * 2][j][v & 3] = !(found >> (j * R + v) & 1) ? x : above >> (j * R + v) & 1 ? size : -size;
+        }
+}
+
+// A tile of BP / 2 columns of F and BQ rows: H, or dA and dB.  TWO: these in two 16-bit parts
+template <class T, Store S, bool BACK, bool TWO = false>
 __global__ __launch_bounds__(T::THREADS, T::FP * T::FQ > 32 ? 1 : 2)
 void ffn_gate_kernel(FfnArgs a, int act)
 {
@@ -145,6 +199,8 @@ void ffn_gate_kernel(FfnArgs a, int act)
         }
         if (__ballot(endless)) whole_projections<T>(prod.acc, a, fw, qw);
     }
+    if constexpr (BACK)
+        if (act == (int)Gate::Relu) settle_signs<T, S>(prod.acc, a, fw, qw);
     static_assert(T::FP % 4 == 0, "");
     constexpr int E = store_bytes<S>();
     const void* const rows = BACK ? a.dH : a.H;
@@ -223,18 +279,24 @@ void ffn_gate_kernel(FfnArgs a, int act)
                             }
                         }
                     } else {
-                        const i32x4 wa = pack(y, up), wb = pack(z, up);
-                        if (in) {
-                            *(i32x4*)(a.dA + at) = wa;
-                            *(i32x4*)(a.dB + at) = wb;
-                        }
+                        auto put = [&](unsigned short* to, const float (&v)[2][4], float by) {
+                            const i32x4 w = pack(v, by);
+                            if (in) *(i32x4*)(to + at) = w;
+                            if constexpr (TWO) {
+                                auto rest = [&](const float (&x)[4]) {
+                                    return i32x2{pack2_rest<HALF>(x[0] * by, x[1] * by, pack2<HALF>(x[0] * by, x[1] * by)),
+                                                 pack2_rest<HALF>(x[2] * by, x[3] * by, pack2<HALF>(x[2] * by, x[3] * by))};
+                                };
+                                const i32x4 r = join_fragments(rest(v[0]), rest(v[1]));
+                                if (in) *(i32x4*)(to + a.part + at) = r;
+                            }
+                        };
+                        put(a.dA, y, up);
+                        put(a.dB, z, up);
                         if constexpr (HALF) {
                             if (a.dA_all) {
-                                const i32x4 va = pack(y, up_all), vb = pack(z, up_all);
-                                if (in) {
-                                    *(i32x4*)(a.dA_all + at) = va;
-                                    *(i32x4*)(a.dB_all + at) = vb;
-                                }
+                                put(a.dA_all, y, up_all);
+                                put(a.dB_all, z, up_all);
                             }
                         }
                     }
@@ -341,7 +403,7 @@ struct FfnSum {
 };
 
 // dX [T,D] = dA Wg + dB Wu
-template <class T, Store S, bool DX>
+template <class T, Store S, bool DX, bool TWO>
 __device__ __forceinline__ void ffn_sum_tile(const FfnSum& a, int id, SPH_LDS unsigned char* smem)
 {
     constexpr bool F32 = S == Store::F32;
@@ -351,7 +413,7 @@ __device__ __forceinline__ void ffn_sum_tile(const FfnSum& a, int id, SPH_LDS un
     const int per_slice = __builtin_amdgcn_readfirstlane(((a.k + kStepK - 1) / kStepK + a.slices - 1) / a.slices) * kStepK;
     const int slice = __builtin_amdgcn_readfirstlane(tile.slice);
     const int k0 = min(a.k, slice * per_slice), k1 = min(a.k, k0 + per_slice);
-    Product<T, S == Store::F16, true, !DX, F32 ? 6 : 1, DX ? Form::Sum : Form::One> prod;
+    Product<T, S == Store::F16, true, !DX, F32 ? 6 : TWO ? 2 : 1, DX ? Form::Sum : Form::One> prod;
     prod.run(a.P, a.Q, p0, q0, k0, k1, smem, a.P2, a.Q2);
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n16 = lane & 15, g = lane >> 4;
@@ -389,22 +451,22 @@ __device__ __forceinline__ void ffn_sum_tile(const FfnSum& a, int id, SPH_LDS un
     }
 }
 
-template <class T, Store S>
+template <class T, Store S, bool TWO>
 __global__ __launch_bounds__(T::THREADS, T::FP * T::FQ > 32 ? 1 : 2)
 void ffn_dx_kernel(FfnSum a)
 {
     extern __shared__ __attribute__((aligned(16))) unsigned char smem_raw[];
-    ffn_sum_tile<T, S, true>(a, blockIdx.x, (SPH_LDS unsigned char*)smem_raw);
+    ffn_sum_tile<T, S, true, TWO>(a, blockIdx.x, (SPH_LDS unsigned char*)smem_raw);
 }
 
 // dWg and dWu: `each` workgroups for the first, the rest for the second
-template <class T, Store S>
+template <class T, Store S, bool TWO>
 __global__ __launch_bounds__(T::THREADS, T::FP * T::FQ > 32 ? 1 : 2)
 void ffn_dw_kernel(FfnSum a, FfnSum b, int each)
 {
     extern __shared__ __attribute__((aligned(16))) unsigned char smem_raw[];
     const bool second = (int)blockIdx.x >= each;
-    ffn_sum_tile<T, S, false>(second ? b : a, (int)blockIdx.x - (second ? each : 0), (SPH_LDS unsigned char*)smem_raw);
+    ffn_sum_tile<T, S, false, TWO>(second ? b : a, (int)blockIdx.x - (second ? each : 0), (SPH_LDS unsigned char*)smem_raw);
 }
 
 // Slices added up in order, scaled and rounded, of up to three results: a wave 256 columns of a row, eight slices' loads under way

@@ -147,6 +147,7 @@ long long heads_groups(const HeadsArgs& a, int d)
 
 // ---- gated feed-forward ------------------------------------------------------------------------------------
 
+constexpr long long kFfnFew = 1 << 18;             // values of dA up to which they are kept in two parts
 constexpr int kFfnRows = 64;                       // up to here the weights go from memory straight into registers
 
 bool ffn_shape(int T, int D, int F)
@@ -157,11 +158,11 @@ bool ffn_shape(int T, int D, int F)
 // The tile and slices of a sum over k for `count` results of rows x cols, by the time that its rounds take: in a round of 256 Big tiles each takes 27 ns
 // per k, in one of 512 Mid tiles 20, and every slice is written and read again as fp32.
 struct SumChoice { bool big; int slices; };
-SumChoice sum_choice(long long rows, long long cols, long long k, int count, int products)
+SumChoice sum_choice(long long rows, long long cols, long long k, int count, int products, bool may_big)
 {
     SumChoice c{false, 1};
     double best = 0.0;
-    for (int b = 1; b >= 0; --b) {
+    for (int b = may_big; b >= 0; --b) {
         const int tile = b ? 256 : 128, at_once = b ? kCus : 2 * kCus;
         const long long tiles = count * ((rows + tile - 1) / tile) * ((cols + tile - 1) / tile);
         for (int s = 1; s <= 64 && (s == 1 || (k / s >= 256 && (double)s * count * rows * cols <= 2.5e8)); s *= 2) {
@@ -175,6 +176,7 @@ SumChoice sum_choice(long long rows, long long cols, long long k, int count, int
 
 struct Ffn {
     int T, D, F, ld, ldf, parts, g_parts;          // ld, ldf: elements per packed row of D, of F; parts: of X and W, of dA and dB
+    bool two;                                      // few values of dA and dB in 16 bits: two parts
     SumChoice dx, dw;
     int *x_exp, *g_exp, *u_exp;                    // fp32
     unsigned short *x, *g, *u, *x_sum, *g_sum, *u_sum;
@@ -188,7 +190,8 @@ Ffn ffn_plan(int T, int D, int F, int dtype, bool back, void* workspace)
 {
     Ffn p{};
     p.T = T, p.D = D, p.F = F, p.ld = (int)up_to(D, 8), p.ldf = (int)up_to(F, 8);
-    p.parts = dtype == SPHATTN_F32 ? 2 : 1, p.g_parts = dtype == SPHATTN_F32 ? 3 : 1;
+    p.two = back && dtype != SPHATTN_F32 && (long long)T * F <= kFfnFew;
+    p.parts = dtype == SPHATTN_F32 ? 2 : 1, p.g_parts = dtype == SPHATTN_F32 ? 3 : p.two ? 2 : 1;
     if (!back && T <= kFfnRows) return p;
     const bool f32 = dtype == SPHATTN_F32, f16 = dtype == SPHATTN_F16;
     Carve c(workspace);
@@ -213,9 +216,9 @@ Ffn ffn_plan(int T, int D, int F, int dtype, bool back, void* workspace)
         p.row_up = c.take<float>(f16 ? T : 0);
         p.row_down = c.take<float>(f16 ? T : 0);
         p.all_up = c.take<float>(f16 ? 2 : 0);
-        const int products = f32 ? 6 : 1;
-        p.dx = sum_choice(T > 0 ? T : 1, p.ld, 2ll * F, 1, products);
-        p.dw = T > 0 ? sum_choice(F, p.ld, T, 2, products) : SumChoice{false, 1};
+        const int products = f32 ? 6 : p.two ? 2 : 1;
+        p.dx = sum_choice(T > 0 ? T : 1, p.ld, 2ll * F, 1, products, !p.two);
+        p.dw = T > 0 ? sum_choice(F, p.ld, T, 2, products, !p.two) : SumChoice{false, 1};
         p.part = c.take<float>(p.dx.slices > 1 ? (size_t)p.dx.slices * T * p.ld : 0);
         p.part_w = c.take<float>(p.dw.slices > 1 ? (size_t)p.dw.slices * 2 * F * p.ld : 0);
     }
@@ -223,10 +226,10 @@ Ffn ffn_plan(int T, int D, int F, int dtype, bool back, void* workspace)
     return p;
 }
 
-template <class T, Store S, bool BACK>
+template <class T, Store S, bool BACK, bool TWO = false>
 int launch_gate(FfnArgs& a, int act, hipStream_t stream)
 {
-    const auto kern = ffn_gate_kernel<T, S, BACK>;
+    const auto kern = ffn_gate_kernel<T, S, BACK, TWO>;
     static std::atomic<uint64_t> done{0};
     if (T::LDS > 65536 && !raise_lds_limit(kern, T::LDS, done)) return SPHATTN_ERR_LAUNCH;
     a.tiles_p = (a.F + T::BP / 2 - 1) / (T::BP / 2);
@@ -290,7 +293,7 @@ int run_ffn_fwd(const Ffn& p, const void* X, const void* Wg, const void* Wu, voi
     return run_gate<S, false>(a, act, stream);
 }
 
-template <class T, Store S, bool DX>
+template <class T, Store S, bool DX, bool TWO = false>
 int launch_sum(FfnSum& a, FfnSum* b, hipStream_t stream)
 {
     a.tiles_p = (a.P.size + T::BP - 1) / T::BP;
@@ -298,11 +301,11 @@ int launch_sum(FfnSum& a, FfnSum* b, hipStream_t stream)
     if (each > 1 << 21) return SPHATTN_ERR_SHAPE;                     // (a launch has less than 2^32 threads)
     static std::atomic<uint64_t> done{0};
     if constexpr (DX) {
-        const auto kern = ffn_dx_kernel<T, S>;
+        const auto kern = ffn_dx_kernel<T, S, TWO>;
         if (T::LDS > 65536 && !raise_lds_limit(kern, T::LDS, done)) return SPHATTN_ERR_LAUNCH;
         hipLaunchKernelGGL(kern, dim3((unsigned)each), dim3(T::THREADS), T::LDS, stream, a);
     } else {
-        const auto kern = ffn_dw_kernel<T, S>;
+        const auto kern = ffn_dw_kernel<T, S, TWO>;
         if (T::LDS > 65536 && !raise_lds_limit(kern, T::LDS, done)) return SPHATTN_ERR_LAUNCH;
         if (b) b->tiles_p = a.tiles_p;
         hipLaunchKernelGGL(kern, dim3((unsigned)(b ? 2 * each : each)), dim3(T::THREADS), T::LDS, stream, a, b ? *b : a, (int)each);
@@ -347,9 +350,16 @@ int run_ffn_bwd(const Ffn& p, const void* X, const void* Wg, const void* Wu, con
             hipLaunchKernelGGL(ffn_factors_kernel, dim3(1), dim3(1024), 0, stream, p.x_bound, p.w_norm, p.T, p.F, p.row_up, p.row_down, p.all_up);
             a.row_up = p.row_up, a.all_up = p.all_up, a.dA_all = dw ? p.dA_all : nullptr, a.dB_all = p.dB_all;
         }
-        rc = run_gate<S, true>(a, act, stream);
+        if constexpr (F32) rc = run_gate<S, true>(a, act, stream);
+        else rc = p.two ? launch_gate<Mid, S, true, true>(a, act, stream) : run_gate<S, true>(a, act, stream);
     }
-    const long long part = F32 ? (long long)p.T * p.ldf * 2 : 0;
+    const long long part = p.g_parts > 1 ? (long long)p.T * p.ldf * 2 : 0;
+    auto sum = [&](auto is_dx, FfnSum& s, FfnSum* second, bool big) {
+        constexpr bool DX = decltype(is_dx)::value;
+        if constexpr (!F32)
+            if (p.two) return launch_sum<Mid, S, DX, true>(s, second, stream);
+        return big ? launch_sum<Big, S, DX>(s, second, stream) : launch_sum<Mid, S, DX>(s, second, stream);
+    };
     // (fp32: what dA and dB are multiplied with are parts of their own)
     auto columns = [&](const Operand& o, const unsigned short* sum, int rows) {
         return F32 ? Operand{(const unsigned char*)sum, (long long)rows * p.ld * 2, p.ld * 2, p.ld} : Operand{o.data, 0, o.ld, p.ld};
@@ -362,7 +372,7 @@ int run_ffn_bwd(const Ffn& p, const void* X, const void* Wg, const void* Wu, con
         s.Q = Operand{(const unsigned char*)p.dA, part, p.ldf * 2, p.T}, s.Q2 = Operand{(const unsigned char*)p.dB, part, p.ldf * 2, p.T};
         s.k = p.F, s.slices = p.dx.slices, s.out = dX, s.out_ld = s.out_cols = p.D, s.out_rows = p.T, s.part = p.part, s.part_ld = p.ld;
         if (F16) s.row_down = p.row_down;
-        rc = p.dx.big ? launch_sum<Big, S, true>(s, nullptr, stream) : launch_sum<Mid, S, true>(s, nullptr, stream);
+        rc = sum(std::true_type{}, s, nullptr, p.dx.big);
         if (s.slices > 1) cut[n_cut++] = s;
     }
     if (rc == SPHATTN_OK && dw) {
@@ -380,7 +390,7 @@ int run_ffn_bwd(const Ffn& p, const void* X, const void* Wg, const void* Wu, con
             ++n;
         }
         FfnSum* second = n == 2 ? &s[1] : nullptr;
-        rc = p.dw.big ? launch_sum<Big, S, false>(s[0], second, stream) : launch_sum<Mid, S, false>(s[0], second, stream);
+        rc = sum(std::false_type{}, s[0], second, p.dw.big);
         for (int m = 0; m < n && s[m].slices > 1; ++m) cut[n_cut++] = s[m];
     }
     if (rc == SPHATTN_OK && n_cut) rc = join_slices<S>(cut, n_cut, stream);

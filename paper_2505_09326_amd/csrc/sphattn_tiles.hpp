@@ -89,11 +89,11 @@ struct Product {
             return across ? Stream{A.data + part * A.part + (long long)k0 * A.ld, k_end - k0}
                           : Stream{A.data + part * A.part + (long long)a0 * A.ld + (long long)k0 * 2, rows * A.ld - k0 * 2};
         };
-        // parts of P and Q by pair, small products first: (1,0) (0,1) (0,0), or of three parts (2,0) (0,2) (1,1) (1,0) (0,1) (0,0)
-        static_assert(PAIRS == 1 || PAIRS == 3 || PAIRS == 6, "");
+        // parts of P and Q by pair, small products first: of Q's two (0,1) (0,0), of two of each (1,0) (0,1) (0,0), of three (2,0) (0,2) (1,1) (1,0) (0,1) (0,0)
+        static_assert(PAIRS == 1 || PAIRS == 2 || PAIRS == 3 || PAIRS == 6, "");
         int pair = 0, step = 0, copied = 0;        // of the next copies
         auto part_p = [&]() { return PAIRS == 3 ? pair == 0 : PAIRS == 6 ? (pair == 0 ? 2 : pair == 2 || pair == 3) : 0; };
-        auto part_q = [&]() { return PAIRS == 3 ? pair == 1 : PAIRS == 6 ? (pair == 1 ? 2 : pair == 2 || pair == 4) : 0; };
+        auto part_q = [&]() { return PAIRS == 2 ? pair == 0 : PAIRS == 3 ? pair == 1 : PAIRS == 6 ? (pair == 1 ? 2 : pair == 2 || pair == 4) : 0; };
         constexpr int ROWS_P = FORM == Form::Two ? T::BP / 2 : T::BP;
         Stream sp = start(PX, P, p0, ROWS_P, part_p()), sq = start(QX, Q, q0, T::BQ, part_q());
         Stream sp2 = FORM == Form::Two ? start(PX, P2, p0, ROWS_P, part_p()) : sp;
@@ -309,6 +309,20 @@ __device__ __forceinline__ i32x4 join_fragments(i32x2 a, i32x2 b)
     // (odd rows of sixteen lanes of the first operand and even rows of the second change places)
     asm volatile("s_nop 1\n\tv_permlane16_swap_b32 %0, %2\n\tv_permlane16_swap_b32 %1, %3\n\ts_nop 1" : "+v"(a0), "+v"(a1), "+v"(b0), "+v"(b1));
     return i32x4{a0, a1, b0, b1};
+}
+
+// What two values' rounding to the 16-bit type has left of them, rounded (of what is not finite there: nothing)
+template <bool HALF>
+__device__ __forceinline__ int pack2_rest(float a, float b, int rounded)
+{
+    float x, y;
+    if constexpr (HALF) {
+        const f16x2 h = __builtin_bit_cast(f16x2, rounded);
+        x = (float)h[0], y = (float)h[1];
+    } else {
+        x = __builtin_bit_cast(float, rounded << 16), y = __builtin_bit_cast(float, rounded & (int)0xffff0000);
+    }
+    return pack2<HALF>(__builtin_fabsf(x) < __builtin_inff() ? a - x : 0.f, __builtin_fabsf(y) < __builtin_inff() ? b - y : 0.f);
 }
 
 // D = A (16 x 4) B (4 x 16) + C on element ea of a's registers and eb of b's

@@ -169,12 +169,13 @@ Vocab vocab_fwd_plan(int T, int V, int D, int dtype, void* workspace)
     return p;
 }
 
-Vocab vocab_bwd_plan(int T, int V, int D, int dtype, void* workspace)
+// two: G of 16-bit storage in two parts
+Vocab vocab_bwd_plan(int T, int V, int D, int dtype, void* workspace, bool two = false)
 {
     Vocab p{};
     p.T = T, p.V = V, p.D = D, p.parts = dtype == SPHATTN_F32 ? 2 : 1, p.ld = (int)up_to(D, 8);
     const bool few = rows_form(T, dtype);
-    p.g_parts = dtype != SPHATTN_F32 ? 1 : few ? 2 : 3;            // (few rows: fp32 as it is)
+    p.g_parts = dtype != SPHATTN_F32 ? 1 + two : few ? 2 : 3;      // (few rows: fp32 as it is)
     const long long row_bytes = 2ll * p.g_parts * (T > 0 ? T : 1);
     size_t limit = (size_t)row_bytes * V <= kOnePieceBytes ? kOnePieceBytes : kPieceBytes;
     if ((size_t)row_bytes * p.ld > limit) limit = (size_t)row_bytes * p.ld;
@@ -215,8 +216,12 @@ struct Teacher {
     int *targets, *sorted;
     float *weights, *logits;                       // (logits: the caller's)
     unsigned short* starts;
+    float2* lse;                                   // in two parts, base 2
     size_t bytes;
 };
+
+// Rows up to which G of 16-bit storage is kept in two parts
+bool taught_few(int T, int dtype) { return dtype != SPHATTN_F32 && T > 0 && T <= 256; }
 
 bool teacher_shape(int T, int V, int D, int K) { return vocab_shape(T, V, D) && K >= 1 && K <= kTaughtMost; }
 
@@ -233,7 +238,7 @@ Teacher teacher_plan(int T, int V, int K, bool back, bool keep, size_t behind, v
     p.targets = c.take<int>(T);
     p.sorted = c.take<int>((size_t)T * K);
     p.weights = c.take<float>((size_t)T * K);
-    if (!back) p.starts = c.take<unsigned short>((size_t)T * (p.blocks + 1));
+    if (!back) p.starts = c.take<unsigned short>((size_t)T * (p.blocks + 1)), p.lse = c.take<float2>(T);
     if (keep) p.logits = c.take<float>((size_t)T * K);
     p.bytes = behind + c.used();
     return p;
@@ -247,10 +252,10 @@ int launch_teacher(const Teacher& p, const void* ids, int id_bytes, const float*
     return launched();
 }
 
-template <class T, Store S, Stage ST>
+template <class T, Store S, Stage ST, bool TWO = false>
 int launch_tiles(VocabArgs& a, int p, int q, hipStream_t stream)
 {
-    const auto kern = vocab_tile_kernel<T, S, ST>;
+    const auto kern = vocab_tile_kernel<T, S, ST, TWO>;
     constexpr int LDS = reads_fp32<T, S, ST>() ? T::WAVES_P * T::BQ * 8 : T::LDS;   // (sums per row only)
     static std::atomic<uint64_t> done{0};
     if (LDS > 65536 && !raise_lds_limit(kern, LDS, done)) return SPHATTN_ERR_LAUNCH;
@@ -356,20 +361,20 @@ int run_vocab_fwd(const Vocab& p, const void* X, const void* W, const void* targ
     while (log_rows < 6 && (p.T >> log_rows) > (at_once ? 0 : kCus / 2)) ++log_rows;
     hipLaunchKernelGGL(vocab_join_kernel, dim3((unsigned)(p.T + (1 << log_rows) - 1) >> log_rows), dim3(kJoinLossThreads), 0, stream, p.partial, p.T, tiles,
                        log_rows, teacher ? (const float*)nullptr : p.target_logit, targets, id_bytes, k.compact ? p.place : (const int*)nullptr, all_rows, losses, lse,
-                       at_once ? mean : (float*)nullptr, reduction == SPHATTN_LOSS_MEAN, p.T, p.V);
+                       at_once ? mean : (float*)nullptr, reduction == SPHATTN_LOSS_MEAN, p.T, p.V, teacher ? teacher->lse : (float2*)nullptr);
     if (teacher)
         hipLaunchKernelGGL(taught_loss_kernel, dim3((unsigned)(p.T + 3) / 4), dim3(256), 0, stream, teacher->targets, teacher->sorted, teacher->weights, teacher->logits,
-                           lse, p.T, teacher->K, teacher->tau * teacher->tau, losses);
+                           teacher->lse, p.T, teacher->K, teacher->tau * teacher->tau, losses);
     if (mean && !at_once)
         hipLaunchKernelGGL(vocab_mean_kernel, dim3(1), dim3(1024), 0, stream, losses, targets, id_bytes, p.T, mean, reduction == SPHATTN_LOSS_MEAN);
     return launched();
 }
 
 // The teacher's weights taken off a piece of G
-template <Store S, bool WHOLE>
-int launch_taught_g(const Teacher& p, const VocabArgs& a, const int* rows, int n, hipStream_t stream)
+template <Store S, int PARTS>
+int launch_taught_g(const Teacher& p, const VocabArgs& a, const int* rows, const float* lse, int n, hipStream_t stream)
 {
-    hipLaunchKernelGGL((taught_g_kernel<S, WHOLE>), dim3((unsigned)(a.Q.size + 3) / 4), dim3(256), 0, stream, a.info, rows, p.sorted, p.weights, p.logits, a.g_lse2, a.g,
+    hipLaunchKernelGGL((taught_g_kernel<S, PARTS>), dim3((unsigned)(a.Q.size + 3) / 4), dim3(256), 0, stream, a.info, rows, p.sorted, p.weights, p.logits, lse, a.g_lse2, a.g,
                        a.unless_even, p.K, a.v0, n, a.G, a.G_part, a.G_ld);
     return launched();
 }
@@ -391,7 +396,7 @@ int run_rows_bwd(const Vocab& p, const void* X, const void* W, PackArgs k, void*
         a.g_target = p.g_target, a.g_lse2 = p.g_lse2, a.g = p.g, a.G = p.G, a.G_ld = p.piece;
         int tiles;
         int rc = launch_scores<S, Stage::G>(a, n, p.T, tiles, stream);
-        if (rc == SPHATTN_OK && teacher) rc = launch_taught_g<S, true>(*teacher, a, p.rows, n, stream);
+        if (rc == SPHATTN_OK && teacher) rc = launch_taught_g<S, 1>(*teacher, a, p.rows, k.lse, n, stream);
         if (rc != SPHATTN_OK) return rc;
         if (dX) {
             a.slices = p.slices, a.out = p.dx, a.out_ld = p.ld, a.accumulate = i > 0;
@@ -448,8 +453,30 @@ int run_vocab_bwd(const Vocab& p, const void* X, const void* W, const void* targ
         a.g_target = p.g_target, a.g_lse2 = p.g_lse2, a.g = own && !twice ? p.g_own : p.g;
         a.G = p.G, a.G_part = (long long)p.T * p.piece, a.G_ld = p.piece;
         int tiles;
-        if (p.T > 0) rc = launch_scores<S, Stage::G>(a, n, p.T, tiles, stream);
-        if (rc == SPHATTN_OK && teacher && p.T > 0) rc = launch_taught_g<S, false>(*teacher, a, p.rows, n, stream);
+        // G of the piece, and the sums with it
+        const bool in_two = S != Store::F32 && p.g_parts == 2;
+        auto form_g = [&] {
+            if constexpr (S != Store::F32) {
+                if (in_two) {
+                    int done = p.T <= 16 ? launch_tiles<One, S, Stage::G, true>(a, n, p.T, stream) : p.T <= 64 ? launch_tiles<Low, S, Stage::G, true>(a, n, p.T, stream)
+                                                                                                             : launch_tiles<Mid, S, Stage::G, true>(a, n, p.T, stream);
+                    if (done == SPHATTN_OK) done = launch_taught_g<S, 2>(*teacher, a, p.rows, lse, n, stream);
+                    return done;
+                }
+            }
+            int done = launch_scores<S, Stage::G>(a, n, p.T, tiles, stream);
+            if (done == SPHATTN_OK && teacher) done = launch_taught_g<S, S == Store::F32 ? 3 : 1>(*teacher, a, p.rows, lse, n, stream);
+            return done;
+        };
+        auto sums = [&](auto stage, VocabArgs& b, bool big, int q) {
+            constexpr Stage ST = decltype(stage)::value;
+            if constexpr (S != Store::F32)
+                if (in_two) return big ? launch_tiles<Big, S, ST, true>(b, p.ld, q, stream) : launch_tiles<Mid, S, ST, true>(b, p.ld, q, stream);
+            return big ? launch_tiles<Big, S, ST>(b, p.ld, q, stream) : launch_tiles<Mid, S, ST>(b, p.ld, q, stream);
+        };
+        constexpr std::integral_constant<Stage, Stage::Dx> of_dx{};
+        constexpr std::integral_constant<Stage, Stage::Dw> of_dw{};
+        if (p.T > 0) rc = form_g();
         if (rc != SPHATTN_OK) break;
         VocabArgs bx{}, bw{};
         const bool with_dx = dX && p.T > 0, with_dw = dW != nullptr;
@@ -462,20 +489,18 @@ int run_vocab_bwd(const Vocab& p, const void* X, const void* W, const void* targ
         bw.out = dW ? (unsigned char*)dW + (size_t)v0 * p.D * store_bytes<S>() : nullptr, bw.out_ld = p.D, bw.out_cols = p.D, bw.out_rows = n;
         const bool dw_big = big_tiles(p.ld, n);
         if (twice && p.T > 0) {
-            rc = dw_big ? launch_tiles<Big, S, Stage::Dw>(bw, p.ld, n, stream) : launch_tiles<Mid, S, Stage::Dw>(bw, p.ld, n, stream);
+            rc = sums(of_dw, bw, dw_big, n);
             a.g = p.g_own, a.unless_even = 1;
-            if (rc == SPHATTN_OK) rc = launch_scores<S, Stage::G>(a, n, p.T, tiles, stream);
-            if (rc == SPHATTN_OK && teacher) rc = launch_taught_g<S, false>(*teacher, a, p.rows, n, stream);
-            if (rc == SPHATTN_OK) rc = p.dx_big ? launch_tiles<Big, S, Stage::Dx>(bx, p.ld, p.T, stream) : launch_tiles<Mid, S, Stage::Dx>(bx, p.ld, p.T, stream);
+            if (rc == SPHATTN_OK) rc = form_g();
+            if (rc == SPHATTN_OK) rc = sums(of_dx, bx, p.dx_big, p.T);
             continue;
         }
-        if (with_dx && with_dw && !p.dx_big && !dw_big) {
+        if (with_dx && with_dw && !p.dx_big && !dw_big && !in_two) {
             rc = launch_gradients<Mid, S>(bx, bw, p.ld, p.T, n, stream);
             continue;
         }
-        if (with_dx) rc = p.dx_big ? launch_tiles<Big, S, Stage::Dx>(bx, p.ld, p.T, stream) : launch_tiles<Mid, S, Stage::Dx>(bx, p.ld, p.T, stream);
-        if (rc == SPHATTN_OK && with_dw)
-            rc = dw_big ? launch_tiles<Big, S, Stage::Dw>(bw, p.ld, n, stream) : launch_tiles<Mid, S, Stage::Dw>(bw, p.ld, n, stream);
+        if (with_dx) rc = sums(of_dx, bx, p.dx_big, p.T);
+        if (rc == SPHATTN_OK && with_dw) rc = sums(of_dw, bw, dw_big, n);
     }
     if (rc == SPHATTN_OK && dX && p.T > 0)
         hipLaunchKernelGGL((vocab_dx_kernel<S>), dim3((unsigned)(p.T + 3) / 4, (unsigned)(p.D + kDxCols - 1) / kDxCols), dim3(256), 0, stream, p.dx, p.slices, p.ld,
@@ -660,7 +685,7 @@ int sphattn_vocab_distill_fwd(const void* X, const void* W, const void* ids, int
 
 size_t sphattn_vocab_distill_bwd_workspace_bytes(int T, int V, int D, int K, int dtype)
 {
-    return teacher_shape(T, V, D, K) && element_bytes(dtype) ? teacher_plan(T, V, K, true, false, vocab_bwd_plan(T, V, D, dtype, nullptr).bytes, nullptr).bytes : 0;
+    return teacher_shape(T, V, D, K) && element_bytes(dtype) ? teacher_plan(T, V, K, true, false, vocab_bwd_plan(T, V, D, dtype, nullptr, taught_few(T, dtype)).bytes, nullptr).bytes : 0;
 }
 
 int sphattn_vocab_distill_bwd(const void* X, const void* W, const void* ids, int id_bytes, const float* teacher,
@@ -673,7 +698,7 @@ int sphattn_vocab_distill_bwd(const void* X, const void* W, const void* ids, int
     if ((T > 0 && (!lse || !kept || !dloss)) || (!dX && !dW)) return SPHATTN_ERR_NULL;
     const size_t e = (size_t)element_bytes(dtype), entries = (size_t)T * K;
     if (off(lse, 4) || off(kept, 4) || off(dloss, 4) || off(dX, e) || off(dW, e)) return SPHATTN_ERR_ALIGN;
-    const Vocab p = vocab_bwd_plan(T, V, D, dtype, workspace);
+    const Vocab p = vocab_bwd_plan(T, V, D, dtype, workspace, taught_few(T, dtype));
     Teacher k = teacher_plan(T, V, K, true, false, p.bytes, workspace);
     if (!workspace || off(workspace, 16) || workspace_bytes < k.bytes) return SPHATTN_ERR_WORKSPACE;
     const Range written[] = {{dX, (size_t)T * D * e}, {dW, (size_t)V * D * e}, {workspace, k.bytes}};

@@ -375,7 +375,8 @@ struct TaughtIds {
     }
 };
 
-template <class T, Store S, Stage ST>
+// TWO: G in two 16-bit parts
+template <class T, Store S, Stage ST, bool TWO = false>
 __device__ __forceinline__ void vocab_tile(const VocabArgs& a, int block, SPH_LDS unsigned char* smem)
 {
     constexpr bool PX = ST == Stage::Dx || ST == Stage::Dw, QX = ST == Stage::Dw;
@@ -406,7 +407,7 @@ __device__ __forceinline__ void vocab_tile(const VocabArgs& a, int block, SPH_LD
 
     constexpr bool ROWS = reads_fp32<T, S, ST>();
     constexpr bool SUMS = ST == Stage::Dx || ST == Stage::Dw, F32 = S == Store::F32;
-    std::conditional_t<ROWS, RowsProduct<T>, Product<T, S == Store::F16 || (F32 && !SUMS), PX, QX, !F32 ? 1 : SUMS ? 6 : 3>> prod;
+    std::conditional_t<ROWS, RowsProduct<T>, Product<T, S == Store::F16 || (F32 && !SUMS), PX, QX, !F32 ? (SUMS && TWO ? 2 : 1) : SUMS ? 6 : 3>> prod;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n16 = lane & 15, g = lane >> 4, wp = wave % T::WAVES_P, wq = wave / T::WAVES_P;
     const int pw = p0 + wp * T::FP * 16, qw = q0 + wq * T::FQ * 16;     // this wave's corner
@@ -549,6 +550,14 @@ __device__ __forceinline__ void vocab_tile(const VocabArgs& a, int block, SPH_LD
                     const i32x4 o = join_fragments(i32x2{pack2<S == Store::F16>(d[0][0], d[0][1]), pack2<S == Store::F16>(d[0][2], d[0][3])},
                                                    i32x2{pack2<S == Store::F16>(d[1][0], d[1][1]), pack2<S == Store::F16>(d[1][2], d[1][3])});
                     if (q < rows) *(i32x4*)to = o;
+                    if constexpr (TWO) {
+                        auto rest = [&](const float (&x)[4]) {
+                            return i32x2{pack2_rest<S == Store::F16>(x[0], x[1], pack2<S == Store::F16>(x[0], x[1])),
+                                         pack2_rest<S == Store::F16>(x[2], x[3], pack2<S == Store::F16>(x[2], x[3]))};
+                        };
+                        const i32x4 r = join_fragments(rest(d[0]), rest(d[1]));
+                        if (q < rows) *(i32x4*)(to + a.G_part) = r;
+                    }
                 }
             }
         }
@@ -602,12 +611,12 @@ __device__ __forceinline__ void vocab_tile(const VocabArgs& a, int block, SPH_LD
     }
 }
 
-template <class T, Store S, Stage ST>
+template <class T, Store S, Stage ST, bool TWO = false>
 __global__ __launch_bounds__(T::THREADS, T::FP * T::FQ > 32 ? 1 : 2)
 void vocab_tile_kernel(VocabArgs a)
 {
     extern __shared__ __attribute__((aligned(16))) unsigned char smem_raw[];
-    vocab_tile<T, S, ST>(a, blockIdx.x, (SPH_LDS unsigned char*)smem_raw);
+    vocab_tile<T, S, ST, TWO>(a, blockIdx.x, (SPH_LDS unsigned char*)smem_raw);
 }
 
 // dX and dW of a piece, which do not depend on each other, in one launch: dX's tiles first.  For small problems one launch less, and where
@@ -803,12 +812,15 @@ void vocab_pack_kernel(PackArgs a)
     }
     if (a.g_target && lane == 0) {
         a.g_target[m] = a.no_target ? -(1 << 30) : load_id(a.r.targets, a.r.id_bytes, t);
-        a.g_lse2[m] = a.lse[t] * kLog2e;
+        const float lse = a.lse[t], lse2 = lse * kLog2e;
+        a.g_lse2[m] = lse2;
+        // (a teacher's: what the product's rounding has left out of the exponent, as a factor)
+        const float soft = a.no_target ? __builtin_amdgcn_exp2f(-__builtin_fmaf(lse, kLog2e, -lse2)) : 1.f;
         const float g = a.r.reduce == Reduce::None ? a.r.dloss[t] * a.r.scale : 1.f;
-        a.g[m] = g * up;
+        a.g[m] = g * up * soft;
         if (a.g_own) {
             const float own = even ? up : gradient_factor(g);
-            a.g_own[m] = g * own;
+            a.g_own[m] = g * own * soft;
             a.own_down[m] = 1.f / own;
         }
     }
@@ -832,7 +844,8 @@ __device__ __forceinline__ LogSum join_sums(LogSum a, LogSum b)
 __global__ __launch_bounds__(kJoinLossThreads)
 void vocab_join_kernel(const float2* __restrict__ partial, int partial_ld, int tiles, int log_rows, const float* __restrict__ target_logit,
                        const void* __restrict__ targets, int id_bytes, const int* __restrict__ place,
-                       int all_rows, float* __restrict__ losses, float* __restrict__ lse, float* __restrict__ mean, int divide, int T, int V)
+                       int all_rows, float* __restrict__ losses, float* __restrict__ lse, float* __restrict__ mean, int divide, int T, int V,
+                       float2* __restrict__ in_two)   // lse in base 2 as the largest logit and the rest, or NULL
 {
     constexpr int W = kJoinLossThreads / 64;
     __shared__ LogSum shared[W][64];
@@ -857,7 +870,8 @@ void vocab_join_kernel(const float2* __restrict__ partial, int partial_ld, int t
         float l = 0.f;
         if (m >= 0 && (all_rows || y >= 0)) {
             for (int w = 1; w < W; ++w) s = join_sums(s, shared[w][row]);
-            const float l2 = (__builtin_fabsf(s.top) < __builtin_inff() ? s.top : 0.f) + __builtin_amdgcn_logf(s.sum);
+            const float top = __builtin_fabsf(s.top) < __builtin_inff() ? s.top : 0.f, rest = __builtin_amdgcn_logf(s.sum), l2 = top + rest;
+            if (in_two) in_two[t] = float2{top, rest};
             l = y >= V ? __builtin_nanf("") : l2 * kLn2;
             if (y >= 0 && target_logit) of_row = y >= V ? __builtin_nanf("") : (l2 - target_logit[m]) * kLn2;
         }
@@ -952,7 +966,9 @@ void vocab_dx_kernel(const float* __restrict__ part, int slices, int ld, int til
 //   G = g tau^2 (exp(l - lse) - sum of p_k over the entries of that id)      l = (c / tau) x . w
 //
 // The products are those of the cross entropy, with the logits of K ids kept per row where that keeps one, and with K weights taken off G where that
-// takes off one: behind the tiles, in fp32 from the kept logits, so that a value of G is rounded once.  What a row counts for is given on
+// takes off one: behind the tiles, in fp32 from the kept logits, so that a value of G is rounded once.  A row's few large values of G are most of it, and with few rows
+// their rounding to 16 bits may be more than the results' own (two rows of bf16: 3.4e-3 against 1.7e-3): up to 256 rows G is kept in two 16-bit parts, twice the products
+// for dX and dW, beside which W's bytes are most of the time there.  What a row counts for is given on
 // as a target: -1 for a row without an entry, 0 for others, INT_MAX for one with an id that is none.
 
 // Entries in order of their ids, equal ids in theirs, the softmax of their logits, and where each block of ids begins.  A wave per row.  Up to 64 entries
@@ -1049,7 +1065,7 @@ void taught_kernel(const void* __restrict__ ids, int id_bytes, const float* __re
 // The rows' losses from the kept logits: a wave per row
 __global__ __launch_bounds__(256)
 void taught_loss_kernel(const int* __restrict__ targets, const int* __restrict__ sorted, const float* __restrict__ weights, const float* __restrict__ logits,
-                        const float* __restrict__ lse, int T, int K, float tau2, float* __restrict__ losses)
+                        const float2* __restrict__ lse, int T, int K, float tau2, float* __restrict__ losses)
 {
     const int lane = threadIdx.x & 63;
     const long long t = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -1057,12 +1073,12 @@ void taught_loss_kernel(const int* __restrict__ targets, const int* __restrict__
     float sum = 0.f;
     const int y = targets[t];
     if (y >= 0) {
-        const float lse2 = lse[t] * kLog2e;
+        const float2 l = lse[t];                   // (the largest logit's difference to one that is near it has no rounding)
         for (int k = lane; k < K; k += 64) {
             const size_t at = (size_t)t * K + k;
             const float w = weights[at];
             // (below the normal numbers the logarithm's instruction takes 0 for it, and the term is nothing)
-            if (sorted[at] != 0x7fffffff && !(w < 0x1p-126f)) sum = __builtin_fmaf(w, __builtin_amdgcn_logf(w) + (lse2 - logits[at]), sum);
+            if (sorted[at] != 0x7fffffff && !(w < 0x1p-126f)) sum = __builtin_fmaf(w, __builtin_amdgcn_logf(w) + ((l.x - logits[at]) + l.y), sum);
         }
 #pragma unroll
         for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
@@ -1071,30 +1087,35 @@ void taught_loss_kernel(const int* __restrict__ targets, const int* __restrict__
 }
 
 // G of a piece of the vocabulary at the teacher's ids: a wave per row that counts.  Equal ids are one value, the first's to write.
-template <Store S, bool WHOLE>                     // WHOLE: fp32 as it is, not in parts
+template <Store S, int PARTS>                      // (fp32 in one part: as it is)
 __global__ __launch_bounds__(256)
 void taught_g_kernel(const VocabInfo* __restrict__ info, const int* __restrict__ rows, const int* __restrict__ sorted, const float* __restrict__ weights,
-                     const float* __restrict__ logits, const float* __restrict__ g_lse2, const float* __restrict__ g, int unless_even, int K, int v0, int n,
+                     const float* __restrict__ logits, const float* __restrict__ lse, const float* __restrict__ g_lse2, const float* __restrict__ g, int unless_even, int K, int v0, int n,
                      void* __restrict__ G, long long part, int ld)
 {
     const int lane = threadIdx.x & 63;
     const long long m = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (m >= info->rows || (unless_even && info->even)) return;
     const size_t row = (size_t)rows[m] * K;
-    const float lse2 = g_lse2[m], gm = g[m];
+    // (g has the factor that the exponent's rounding asks for, which the teacher's weights are without)
+    const float lse2 = g_lse2[m], gm = g[m], g_weights = gm * __builtin_amdgcn_exp2f(__builtin_fmaf(lse[rows[m]], kLog2e, -lse2));
     for (int k = lane; k < K; k += 64) {
         const int id = sorted[row + k];
         if (id < v0 || id - v0 >= n || (k > 0 && sorted[row + k - 1] == id)) continue;
         float w = weights[row + k];
         for (int i = k + 1; i < K && sorted[row + i] == id; ++i) w += weights[row + i];
-        const float d = (__builtin_amdgcn_exp2f(logits[row + k] - lse2) - w) * gm;
+        const float d = __builtin_fmaf(__builtin_amdgcn_exp2f(logits[row + k] - lse2), gm, -w * g_weights);
         const size_t at = (size_t)m * ld + (id - v0);
-        if constexpr (S == Store::F32 && !WHOLE) {
+        if constexpr (PARTS == 3) {
             const float x[4] = {d, 0.f, 0.f, 0.f};
             i32x2 parts[3];
             split3(x, parts);
 #pragma unroll
             for (int i = 0; i < 3; ++i) ((unsigned short*)G)[at + i * part] = (unsigned short)parts[i][0];
+        } else if constexpr (PARTS == 2) {
+            const int rounded = pack2<S == Store::F16>(d, 0.f);
+            ((unsigned short*)G)[at] = (unsigned short)rounded;
+            ((unsigned short*)G)[at + part] = (unsigned short)pack2_rest<S == Store::F16>(d, 0.f, rounded);
         } else {
             store_el<S>(G, at, d);
         }
