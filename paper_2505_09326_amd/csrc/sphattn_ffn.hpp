@@ -9,10 +9,12 @@
 // kept between the two calls.  dX is one sum over 2 F (Form::Sum), dWg and dWu are two over T.
 //
 // dA and dB are rounded once to the storage type, which is what the matrix instructions take; sums are in fp32 throughout.  That rounding is as large as the results'
-// own, of 1.7e-3 in bf16 it makes 2.3e-3 against 64 bits on average over the terms; where there are few of them, up to 2^18 values, chance makes 2.6e-3 and more of it,
+// own, of 1.7e-3 in bf16 it makes 2.3e-3 against 64 bits on average over the terms; where there are few of them, up to 2^18 values, chance made 2.5e-3 and more of it,
 // and they are kept in two 16-bit parts: twice the products, beside which launches and the weights' bytes are the time there.  fp16: they are scaled by powers
 // of two that keep them in the type's range whatever the gradients' size, by each row for dX and by the largest row for dW.
 // fp32: A and U as three products of two fp16 parts with a power of two per row, the gradients as six of three bf16 parts, as the vocabulary loss has them.
+// Bound by the matrix pipes: 8192 rows, D = 2048, F = 8192 in bf16 forward 487 us (1129 TFLOP/s; a library product of 8192^3 1227), dA and dB 560, dX 440 (1250), dWg and dWu
+// 422 (1303).  What the gate's tiles lose to that is their end, exponentials and stores beside which no other tile's products run (8 rounds).
 #pragma once
 #include "sphattn_tiles.hpp"
 
@@ -113,9 +115,9 @@ __device__ __forceinline__ void whole_projections(f32x4 (&acc)[T::FP][T::FQ], co
     }
 }
 
-// relu's slope where A is all but 0: which side it is on is for the sum in 64 bits to say, not for what fp32 has lost of it (with 2^20 values of A about one is on the other
-// side, and one slope is 1e-3 of dX).  The values below 2^-19 of their row's largest here, some ten times the sums' errors, are looked at by the whole wave one at a time: one
-// tile in twenty has one.
+// relu's slope where A is all but 0: which side it is on is for the sum in 64 bits to say, not for what fp32 has lost of it (of 249 x 6144 values
+// one was on the other side: 1.2e-3 of dX, 1.7e-3 of dWg).  The values below 2^-19 of their row's largest here, some ten times the sums' errors, are looked at by the whole wave one
+// at a time; as A is spread, about one tile in twenty has one.
 template <class T, Store S>
 __device__ __forceinline__ void settle_signs(f32x4 (&acc)[T::FP][T::FQ], const FfnArgs& a, int fw, int qw)
 {
@@ -313,7 +315,7 @@ void ffn_gate_kernel(FfnArgs a, int act)
 
 // H for at most 64 rows, where reading the weights is most of the time: they go from memory straight into registers, once.  A workgroup takes sixteen
 // columns of F, its waves a share of D each, in runs of 256 bytes of a row; lane (i, g) holds 16 bytes of row i of each operand (any order of k
-// will do if both have it).  fp32 on the fp32 matrix instruction, as it is.
+// will do if both have it).  fp32 on the fp32 matrix instruction, as it is.  (One row of 1024 x 4096 in bf16 5.1 us, both weights at 3.3 TB/s.)
 template <int FQ> constexpr int ffn_row_waves() { return FQ == 4 ? 4 : 8; }
 
 template <Store S, int FQ, bool WIDE>

@@ -3,7 +3,8 @@
 //   r = 1 / sqrt(mean(x^2) + eps)      y = x r w      o = R y      R turns each pair of dimensions by position times frequency
 //   dy = R^T do      dw = sum dy x r      dx = r (dy w - x r mean(dy w x r))
 //
-// Bound by memory: every row is read and written once (backward: two read, one written).  A row is d elements on d / 8 lanes, a lane
+// Bound by memory: every row is read and written once (backward: two read, one written): 16384 tokens of 32 heads of 128 in bf16 51.5 us, 5.2 TB/s, what a copy of that size
+// past the last-level cache reaches (5.15); with gradients 16384 tokens of 20 heads 31 forward and 50 backward.  One token: 5 us, a chain of two loads, an angle and a root.  A row is d elements on d / 8 lanes, a lane
 // holding four neighbouring dimensions of each half, so that both kinds of pairs lie in one lane and a rotation exchanges nothing between lanes.
 // cos and sin are formed once per token and lane, for all heads that the lane's group of lanes takes of that token.
 #pragma once
@@ -171,7 +172,7 @@ struct HeadsLane {
     }
 };
 
-// Which token and which of its heads a group of lanes takes.  (32-bit numbers: a division of 64 bits is 150 instructions; there are less than 2^31 tokens, and
+// Which token and which of its heads a group of lanes takes.  (32-bit numbers: a division of 64 bits is a long program; there are less than 2^31 tokens, and
 // they are shared only where they are few)
 struct HeadsUnit {
     long long b, n;

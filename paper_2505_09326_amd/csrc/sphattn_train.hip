@@ -394,8 +394,11 @@ int run_rows_bwd(const Vocab& p, const void* X, const void* W, PackArgs k, void*
         a.P = Operand{(const unsigned char*)W + (size_t)v0 * p.D * 4, 0, 0, n}, a.Q = Operand{(const unsigned char*)X, 0, 0, p.T};
         a.info = p.info, a.rows = p.rows, a.k = p.D, a.T = p.T, a.slices = 1, a.V = p.V, a.v0 = v0, a.scale2 = scale * kLog2e;
         a.g_target = p.g_target, a.g_lse2 = p.g_lse2, a.g = p.g, a.G = p.G, a.G_ld = p.piece;
-        int tiles;
-        int rc = launch_scores<S, Stage::G>(a, n, p.T, tiles, stream);
+        int tiles, rc;
+        if (!teacher) rc = launch_scores<S, Stage::G>(a, n, p.T, tiles, stream);
+        else if (p.T <= 16) rc = launch_tiles<One, S, Stage::G, true>(a, n, p.T, stream);
+        else if (p.T <= 32) rc = launch_tiles<Few, S, Stage::G, true>(a, n, p.T, stream);
+        else rc = launch_tiles<Low, S, Stage::G, true>(a, n, p.T, stream);
         if (rc == SPHATTN_OK && teacher) rc = launch_taught_g<S, 1>(*teacher, a, p.rows, k.lse, n, stream);
         if (rc != SPHATTN_OK) return rc;
         if (dX) {

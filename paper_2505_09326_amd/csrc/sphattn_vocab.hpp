@@ -92,7 +92,9 @@ __device__ __forceinline__ int dx_slices(int rows, int T, int slices, int tile_q
 // (17 rows, 50000 x 1024: logits 68 us, W at 3.0 TB/s, dX 57, dW 62, a training step 277; with parts in memory 489.  64 rows, 60000 x 1472: 165, 149, 179,
 // and 655 against 840, which the instruction's rate is less than half of: X's fragments are loaded in the step that multiplies them.  3 rows, 20000 x
 // 512: 17.6, 11, 12.)
-template <class T>
+// BLOCKED: a step's products are added up by themselves and then to the rest, which leaves less rounding than one long chain (a teacher's one id, one row of width 768: with the
+// chain the loss was 3.3e-6 and its gradients 1.7e-6 from 64 bits, with this all below 1e-6); the cross entropy has the chain, and its results as they were.
+template <class T, bool BLOCKED = false>
 struct RowsProduct {
     f32x4 acc[T::FP][T::FQ];
 
@@ -126,6 +128,13 @@ struct RowsProduct {
 #pragma unroll
             for (int j = 0; j < T::FQ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
         fetch(0);
+        f32x4 all[T::FP][T::FQ];
+        if constexpr (BLOCKED) {
+#pragma unroll
+            for (int i = 0; i < T::FP; ++i)
+#pragma unroll
+                for (int j = 0; j < T::FQ; ++j) all[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
         for (int k = 0; k < D; k += 16 * CH) {
             i32x4 w[CH][T::FP], x[CH][T::FQ];
 #pragma unroll
@@ -144,6 +153,21 @@ struct RowsProduct {
                     for (int i = 0; i < T::FP; ++i)
 #pragma unroll
                         for (int j = 0; j < T::FQ; ++j) acc[i][j] = mfma_f32(w[c][i], x[c][j], r, acc[i][j]);
+            if constexpr (BLOCKED) {
+#pragma unroll
+                for (int i = 0; i < T::FP; ++i)
+#pragma unroll
+                    for (int j = 0; j < T::FQ; ++j) {
+                        all[i][j] += acc[i][j];
+                        acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+                    }
+            }
+        }
+        if constexpr (BLOCKED) {
+#pragma unroll
+            for (int i = 0; i < T::FP; ++i)
+#pragma unroll
+                for (int j = 0; j < T::FQ; ++j) acc[i][j] = all[i][j];
         }
     }
 };
@@ -375,7 +399,7 @@ struct TaughtIds {
     }
 };
 
-// TWO: G in two 16-bit parts
+// TWO: G of a teacher's few rows, in two 16-bit parts or (fp32) from sums in blocks
 template <class T, Store S, Stage ST, bool TWO = false>
 __device__ __forceinline__ void vocab_tile(const VocabArgs& a, int block, SPH_LDS unsigned char* smem)
 {
@@ -407,7 +431,7 @@ __device__ __forceinline__ void vocab_tile(const VocabArgs& a, int block, SPH_LD
 
     constexpr bool ROWS = reads_fp32<T, S, ST>();
     constexpr bool SUMS = ST == Stage::Dx || ST == Stage::Dw, F32 = S == Store::F32;
-    std::conditional_t<ROWS, RowsProduct<T>, Product<T, S == Store::F16 || (F32 && !SUMS), PX, QX, !F32 ? (SUMS && TWO ? 2 : 1) : SUMS ? 6 : 3>> prod;
+    std::conditional_t<ROWS, RowsProduct<T, TWO || ST == Stage::Taught>, Product<T, S == Store::F16 || (F32 && !SUMS), PX, QX, !F32 ? (SUMS && TWO ? 2 : 1) : SUMS ? 6 : 3>> prod;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n16 = lane & 15, g = lane >> 4, wp = wave % T::WAVES_P, wq = wave / T::WAVES_P;
     const int pw = p0 + wp * T::FP * 16, qw = q0 + wq * T::FQ * 16;     // this wave's corner
@@ -967,8 +991,8 @@ void vocab_dx_kernel(const float* __restrict__ part, int slices, int ld, int til
 //
 // The products are those of the cross entropy, with the logits of K ids kept per row where that keeps one, and with K weights taken off G where that
 // takes off one: behind the tiles, in fp32 from the kept logits, so that a value of G is rounded once.  A row's few large values of G are most of it, and with few rows
-// their rounding to 16 bits may be more than the results' own (two rows of bf16: 3.4e-3 against 1.7e-3): up to 256 rows G is kept in two 16-bit parts, twice the products
-// for dX and dW, beside which W's bytes are most of the time there.  What a row counts for is given on
+// chance may make more of their rounding to 16 bits than of the results' own (of many rows the two are 2.3e-3 in bf16 where the results' own is 1.7e-3): up to 256 rows G is kept in
+// two 16-bit parts, twice the products for dX and dW, beside which W's bytes are most of the time there.  What a row counts for is given on
 // as a target: -1 for a row without an entry, 0 for others, INT_MAX for one with an id that is none.
 
 // Entries in order of their ids, equal ids in theirs, the softmax of their logits, and where each block of ids begins.  A wave per row.  Up to 64 entries
