@@ -532,7 +532,7 @@ int sphattn_gated_ffn_bwd(const void* X, const void* Wg, const void* Wu, const v
 {
     const int rc = ffn_check(X, Wg, Wu, T, D, F, gate, dtype);
     if (rc != SPHATTN_OK) return rc;
-    if ((T > 0 && !dH) || (!dX && !dWg && !dWu)) return SPHATTN_ERR_NULL;
+    if (T > 0 && (!dH || (!dX && !dWg && !dWu))) return SPHATTN_ERR_NULL;   // (an array of no rows has no address)
     const size_t e = (size_t)element_bytes(dtype);
     if (off(dH, e) || off(dX, e) || off(dWg, e) || off(dWu, e)) return SPHATTN_ERR_ALIGN;
     const Ffn p = ffn_plan(T, D, F, dtype, true, workspace);
@@ -541,6 +541,7 @@ int sphattn_gated_ffn_bwd(const void* X, const void* Wg, const void* Wu, const v
     const Range written[] = {{dX, x}, {dWg, w}, {dWu, w}, {workspace, p.bytes}};
     const Range read[] = {{X, x}, {Wg, w}, {Wu, w}, {dH, (size_t)T * F * e}};
     if (any_meet(written, read)) return SPHATTN_ERR_ALIAS;
+    if (T == 0 && !dWg && !dWu) return SPHATTN_OK;
     const hipStream_t s = (hipStream_t)stream;
     switch (dtype) {
     case SPHATTN_F32: return run_ffn_bwd<Store::F32>(p, X, Wg, Wu, dH, dX, dWg, dWu, gate, s);

@@ -698,7 +698,7 @@ int sphattn_vocab_distill_bwd(const void* X, const void* W, const void* ids, int
 {
     const int rc = distill_check(X, W, ids, id_bytes, teacher, T, V, D, K, scale, temperature, reduction, dtype);
     if (rc != SPHATTN_OK) return rc;
-    if ((T > 0 && (!lse || !kept || !dloss)) || (!dX && !dW)) return SPHATTN_ERR_NULL;
+    if (T > 0 && (!lse || !kept || !dloss || (!dX && !dW))) return SPHATTN_ERR_NULL;   // (an array of no rows has no address)
     const size_t e = (size_t)element_bytes(dtype), entries = (size_t)T * K;
     if (off(lse, 4) || off(kept, 4) || off(dloss, 4) || off(dX, e) || off(dW, e)) return SPHATTN_ERR_ALIGN;
     const Vocab p = vocab_bwd_plan(T, V, D, dtype, workspace, taught_few(T, dtype));
@@ -708,6 +708,7 @@ int sphattn_vocab_distill_bwd(const void* X, const void* W, const void* ids, int
     const Range read[] = {{X, (size_t)T * D * e}, {W, (size_t)V * D * e}, {ids, entries * id_bytes}, {teacher, entries * 4}, {lse, (size_t)T * 4}, {kept, entries * 4},
                           {dloss, reduction == SPHATTN_LOSS_NONE ? (size_t)T * 4 : 4}};
     if (any_meet(written, read)) return SPHATTN_ERR_ALIAS;
+    if (T == 0 && !dW) return SPHATTN_OK;
     const hipStream_t s = (hipStream_t)stream;
     k.tau = temperature;
     k.logits = const_cast<float*>(kept);

@@ -201,6 +201,8 @@ def test_no_rows(pkg):
         assert H.shape == (0, 50)
         dX, dWg, dWu = pkg.sphattn_gated_ffn_bwd(X, Wg, Wu, H)
         assert dX.shape == X.shape and (dWg == 0).all() and (dWu == 0).all()
+        only = pkg.sphattn_gated_ffn_bwd(X, Wg, Wu, H, want_dWg=False, want_dWu=False)
+        assert only[0].shape == X.shape and only[1] is only[2] is None
 
 
 @pytest.mark.parametrize("scale", [2.0 ** -13, 1.0, 512.0])

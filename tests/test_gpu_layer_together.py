@@ -77,7 +77,7 @@ def test_gradients_of_the_whole_step(example, dtype):
     want_loss = _plain(exact, tokens, counts, ids, teacher, heads, key_heads, example) * 256.0
     want = torch.autograd.grad(want_loss, exact)
     half = torch.finfo(dtype).eps / 2
-    assert abs(float(loss) - float(want_loss)) <= 24 * half * abs(float(want_loss))
+    assert abs(float(loss.detach()) - float(want_loss.detach())) <= 24 * half * abs(float(want_loss.detach()))
     for i, (a, b) in enumerate(zip(grads, want)):
         assert float((a.double() - b).norm()) <= 24 * half * float(b.norm()), i
 

@@ -217,6 +217,8 @@ def test_no_rows_and_alignment(pkg):
         assert empty[0].shape == (0,) and empty[3] == 0
         dX, dW = pkg.sphattn_vocab_distill_bwd(X[:0], W, ids[:0], teacher[:0], empty[1], empty[2], torch.ones((), device=DEV), reduction="mean")
         assert dX.shape == (0, 33) and (dW == 0).all()
+        dX, dW = pkg.sphattn_vocab_distill_bwd(X[:0], W, ids[:0], teacher[:0], empty[1], empty[2], torch.ones((), device=DEV), reduction="mean", want_dW=False)
+        assert dX.shape == (0, 33) and dW is None
         want = pkg.sphattn_vocab_distill_fwd(X, W, ids, teacher, keep=True)
         move = lambda t: torch.cat([t.new_zeros(3), t.flatten()])[3:].view(t.shape)
         got = pkg.sphattn_vocab_distill_fwd(move(X), move(W), move(ids), move(teacher), keep=True)
