@@ -272,3 +272,22 @@ def test_graph_replays(pkg, dtype, T):
         torch.cuda.synchronize()
         for a, b in zip(out, call()):
             assert torch.equal(a, b), i
+
+
+def test_more_values_than_32_bits_count(pkg):
+    """H and dH of 2^32 elements and more: their last rows are those of a call of their own."""
+    T, D, F = 33000, 64, 131072
+    g = torch.Generator(device=DEV).manual_seed(31)
+    X = torch.randn(T, D, generator=g, device=DEV).bfloat16()
+    Wg, Wu = (torch.randn(F, D, generator=g, device=DEV).mul_(D ** -0.5).bfloat16() for _ in range(2))
+    few = slice(T - 80, T)
+    H = pkg.sphattn_gated_ffn_fwd(X, Wg, Wu)
+    assert torch.equal(H[few], pkg.sphattn_gated_ffn_fwd(X[few], Wg, Wu))
+    dH = H                                                     # (any values will do; zeros but for the last rows)
+    dH[:T - 80].zero_()
+    dX, dWg, dWu = pkg.sphattn_gated_ffn_bwd(X, Wg, Wu, dH)
+    want = pkg.sphattn_gated_ffn_bwd(X[few], Wg, Wu, dH[few].contiguous())
+    assert (dX[:T - 80] == 0).all()
+    for got, w in zip((dX[few], dWg, dWu), want):              # (the order of the sums is another: fp32's rounding, and a step of bf16 where that decides)
+        off = (got.double() - w.double()).abs()
+        assert (off <= 2.0 ** -7 * w.double().abs() + (2 * F + 40) * U * float(w.abs().max())).all()
