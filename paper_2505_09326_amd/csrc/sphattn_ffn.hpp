@@ -13,7 +13,7 @@
 // and they are kept in two 16-bit parts: twice the products, beside which launches and the weights' bytes are the time there.  fp16: they are scaled by powers
 // of two that keep them in the type's range whatever the gradients' size, by each row for dX and by the largest row for dW.
 // fp32: A and U as three products of two fp16 parts with a power of two per row, the gradients as six of three bf16 parts, as the vocabulary loss has them.
-// Bound by the matrix pipes: 8192 rows, D = 2048, F = 8192 in bf16 forward 487 us (1129 TFLOP/s; a library product of 8192^3 1227), dA and dB 560, dX 440 (1250), dWg and dWu
+// Bound by the matrix pipes: 8192 rows, D = 2048, F = 8192 in bf16 forward 487 us (1129 TFLOP/s; a library product of 8192^3 1227), dA and dB 545, dX 436 (1261), dWg and dWu
 // 422 (1303).  What the gate's tiles lose to that is their end, exponentials and stores beside which no other tile's products run (8 rounds).
 #pragma once
 #include "sphattn_tiles.hpp"
@@ -207,7 +207,23 @@ void ffn_gate_kernel(FfnArgs a, int act)
     constexpr int E = store_bytes<S>();
     const void* const rows = BACK ? a.dH : a.H;
     const bool wide = (((uintptr_t)rows | (uintptr_t)((size_t)a.F * E)) & 15) == 0;
-    // 16-bit: two fragments at a time, whose lanes exchange halves, so that each has eight neighbouring columns of one and 16 bytes to load or store
+    // 16-bit: two fragments at a time, whose lanes exchange halves, so that each has eight neighbouring columns of one and 16 bytes to load or store.
+    // dH of the whole corner is asked for at once: a row block at a time, each behind the last one's arithmetic, took dA and dB of 8192 x 2048 x 8192 from 545 us to 560.
+    constexpr int PIECES = F32 ? T::FP / 2 : T::FP / 4;
+    i32x4 dh[T::FQ][PIECES];
+    if constexpr (BACK) {
+#pragma unroll
+        for (int j = 0; j < T::FQ; ++j) {
+            const size_t row = (size_t)min(qw + 16 * j + n16, a.T - 1) * a.F;
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) {
+                const int at = F32 ? fw + 16 * i + 4 * g : fw + 16 * (2 * i + (g & 1)) + 8 * (g >> 1);
+                dh[j][i] = i32x4{0, 0, 0, 0};
+                if (at < a.F)
+                    dh[j][i] = wide ? load16<S, true>(a.dH, row + at, per16<S>(), per16<S>()) : load16<S, false>(a.dH, row + at, a.F - at, (size_t)a.T * a.F - row - at);
+            }
+        }
+    }
     auto corner = [&](auto gate_of) {
         constexpr Gate G = decltype(gate_of)::value;
 #pragma unroll
@@ -222,15 +238,11 @@ void ffn_gate_kernel(FfnArgs a, int act)
                 const int f = F32 ? fw + 16 * i + 4 * g : fw + 16 * (i + (g & 1)) + 8 * (g >> 1);
                 float d[2][4];
                 if constexpr (BACK) {
-                    auto load = [&](int at) {
-                        if (at >= a.F) return i32x4{0, 0, 0, 0};
-                        return wide ? load16<S, true>(a.dH, row + at, per16<S>(), per16<S>()) : load16<S, false>(a.dH, row + at, a.F - at, (size_t)a.T * a.F - row - at);
-                    };
                     if constexpr (F32) {
-                        widen16<S>(load(f), d[0]);
-                        widen16<S>(load(f + 16), d[1]);
+                        widen16<S>(dh[j][i], d[0]);
+                        widen16<S>(dh[j][i + 1], d[1]);
                     } else {
-                        const i32x4 w = load(f), h = join_fragments(i32x2{w[0], w[1]}, i32x2{w[2], w[3]});   // (the exchange is its own inverse)
+                        const i32x4 w = dh[j][i / 2], h = join_fragments(i32x2{w[0], w[1]}, i32x2{w[2], w[3]});   // (the exchange is its own inverse)
                         float x[8];
                         widen16<S>(h, x);
 #pragma unroll
