@@ -325,7 +325,7 @@ void ffn_gate_kernel(FfnArgs a, int act)
 
 // ---- few rows -----------------------------------------------------------------------------------------------
 
-// H for at most 64 rows, where reading the weights is most of the time: they go from memory straight into registers, once.  A workgroup takes sixteen
+// H for few rows, at most 64, where reading the weights is most of the time: they go from memory straight into registers, once.  A workgroup takes sixteen
 // columns of F, its waves a share of D each, in runs of 256 bytes of a row; lane (i, g) holds 16 bytes of row i of each operand (any order of k
 // will do if both have it).  fp32 on the fp32 matrix instruction, as it is.  (One row of 1024 x 4096 in bf16 5.1 us, both weights at 3.3 TB/s.)
 template <int FQ> constexpr int ffn_row_waves() { return FQ == 4 ? 4 : 8; }

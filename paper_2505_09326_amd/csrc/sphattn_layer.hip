@@ -148,7 +148,10 @@ long long heads_groups(const HeadsArgs& a, int d)
 // ---- gated feed-forward ------------------------------------------------------------------------------------
 
 constexpr long long kFfnFew = 1 << 18;             // values of dA up to which they are kept in two parts
-constexpr int kFfnRows = 64;                       // up to here the weights go from memory straight into registers
+// Whether forward reads the weights straight into registers: up to 32 rows, and up to 64 where the tiles' way is longer, in fp32 (parts) and for small weights.  (33 and
+// 64 rows in bf16: 1024 x 4096 6.9 and 8.3 us, in tiles 11.3; 2000 x 5001 16.2 and 19.8, 19.0 and 21.4; 2048 x 8192 25.2 and 30.5, 21.3 and 22.2; 4096 x 12000 52.6 and 68.9, 45;
+// 64 rows of 2048 x 8192 in fp32 74, 65 in tiles 123.)
+bool ffn_rows_form(int T, int D, int F, int dtype) { return T <= 32 || (T <= 64 && (dtype == SPHATTN_F32 || (long long)F * D < 1 << 24)); }
 
 bool ffn_shape(int T, int D, int F)
 {
@@ -192,7 +195,7 @@ Ffn ffn_plan(int T, int D, int F, int dtype, bool back, void* workspace)
     p.T = T, p.D = D, p.F = F, p.ld = (int)up_to(D, 8), p.ldf = (int)up_to(F, 8);
     p.two = back && dtype != SPHATTN_F32 && (long long)T * F <= kFfnFew;
     p.parts = dtype == SPHATTN_F32 ? 2 : 1, p.g_parts = dtype == SPHATTN_F32 ? 3 : p.two ? 2 : 1;
-    if (!back && T <= kFfnRows) return p;
+    if (!back && ffn_rows_form(T, D, F, dtype)) return p;
     const bool f32 = dtype == SPHATTN_F32, f16 = dtype == SPHATTN_F16;
     Carve c(workspace);
     p.x_exp = c.take<int>(f32 ? T : 0);
@@ -285,9 +288,11 @@ int launch_rows(const void* X, const void* Wg, const void* Wu, void* H, int T, i
 template <Store S>
 int run_ffn_fwd(const Ffn& p, const void* X, const void* Wg, const void* Wu, void* H, int act, hipStream_t stream)
 {
-    if (p.T <= 16) return launch_rows<S, 1>(X, Wg, Wu, H, p.T, p.D, p.F, act, stream);
-    if (p.T <= 32) return launch_rows<S, 2>(X, Wg, Wu, H, p.T, p.D, p.F, act, stream);
-    if (p.T <= kFfnRows) return launch_rows<S, 4>(X, Wg, Wu, H, p.T, p.D, p.F, act, stream);
+    if (p.bytes == 0) {                            // (the plan of the rows' form)
+        if (p.T <= 16) return launch_rows<S, 1>(X, Wg, Wu, H, p.T, p.D, p.F, act, stream);
+        if (p.T <= 32) return launch_rows<S, 2>(X, Wg, Wu, H, p.T, p.D, p.F, act, stream);
+        return launch_rows<S, 4>(X, Wg, Wu, H, p.T, p.D, p.F, act, stream);
+    }
     FfnArgs a = ffn_pack<S>(p, X, Wg, Wu, stream);
     a.H = H;
     return run_gate<S, false>(a, act, stream);

@@ -102,6 +102,7 @@ def _near(got, want, tol, what):
 
 CASES = [  # T, D, F
     (1, 64, 64), (1, 1024, 4096), (1, 515, 1371), (2, 1, 1), (16, 128, 17), (17, 96, 130), (32, 2048, 100), (33, 72, 255), (64, 40, 300),
+    (33, 8192, 2048), (64, 2050, 8191),                        # (few rows of large weights: in tiles in 16 bits)
     (65, 64, 64), (129, 200, 65), (300, 515, 333), (257, 1000, 1200), (1000, 256, 96), (2500, 64, 136), (700, 2048, 640), (2048, 512, 1024)]
 
 
@@ -291,3 +292,15 @@ def test_more_values_than_32_bits_count(pkg):
     for got, w in zip((dX[few], dWg, dWu), want):              # (the order of the sums is another: fp32's rounding, and a step of bf16 where that decides)
         off = (got.double() - w.double()).abs()
         assert (off <= 2.0 ** -7 * w.double().abs() + (2 * F + 40) * U * float(w.abs().max())).all()
+
+
+@pytest.mark.parametrize("T,D,F", [(249, 320, 6144), (1649, 71, 1024), (3000, 64, 1300)])
+def test_relu_beside_zero(pkg, T, D, F):
+    """Of so many values of A some are so near 0 that sums in fp32 put them on the other side; one such slope is 1 / sqrt(T F / 2), 4e-4 and more, of dX.  With all slopes
+    right the gradients are off by some 2^-21 of their terms: 2^-17 of their norms is far from either."""
+    X, Wg, Wu, dH = _inputs(T, D, F, "f32", 249)
+    near = X.double() @ Wg.double().t().contiguous()
+    sides = int(((near > 0) != (X @ Wg.t() > 0)).sum())        # (how many a library's product has there: for the reader)
+    grads = pkg.sphattn_gated_ffn_bwd(X, Wg, Wu, dH, "relu")
+    for name, got, (want, _) in zip(("dX", "dWg", "dWu"), grads, _exact(X, Wg, Wu, "relu", dH, parts=True)):
+        assert float((got.double() - want).norm() / want.norm()) < 2.0 ** -17, (name, sides)
