@@ -23,10 +23,13 @@ namespace sphattn {
 enum class Gate { Silu, Gelu, Relu };
 
 // act(a) and its slope.  The exponential's argument is rounded to fp32: |a| 2^-24 of the exponential, which EXACT (fp32 storage) makes up for.
+// Exponentials are of numbers that are not positive and end in 0, below 2^-126: what a far gate is multiplied with vanishes, however large the gate (a mask of the type's
+// lowest value has act and slope 0), and an infinite one is NaN where the formula's 0 times infinity is.
 template <Gate G, bool EXACT>
 __device__ __forceinline__ void gate(float a, float& act, float& slope)
 {
-    auto exp_of = [](float x) {                    // e^x, x <= 87
+    auto exp_of = [](float x) {                    // e^x, x <= 0
+        x = fmaxf(x, -200.f);                      // (the correction has no infinite argument)
         const float y = x * kLog2e;
         float e = __builtin_amdgcn_exp2f(y);
         if constexpr (EXACT) e = __builtin_fmaf(e, kLn2 * (__builtin_fmaf(x, kLog2e, -y) + x * 1.925963033e-8f), e);   // (log2(e) and what fp32 leaves of it)
@@ -37,17 +40,18 @@ __device__ __forceinline__ void gate(float a, float& act, float& slope)
         slope = a > 0.f ? 1.f : 0.f;
     } else if constexpr (G == Gate::Silu) {
         if constexpr (EXACT) {
-            const float e = exp_of(fminf(-a, 87.f)), s = 1.f / (1.f + e);   // (where it ends, a / (1 + e) is below 1e-35)
+            // 1 / (1 + e^-a) and what is left of 1
+            const float e = exp_of(-__builtin_fabsf(a)), large = 1.f / (1.f + e), small = e * large;
+            const float s = a < 0.f ? small : large, rest = a < 0.f ? large : small;
             act = a * s;
-            slope = s * __builtin_fmaf(a, e * s, 1.f);
-            if (a != a) act = slope = a;           // (the minimum has lost it)
+            slope = s * __builtin_fmaf(a, rest, 1.f);
         } else {                                   // (an infinite exponential gives zeros; 1 - s is off by 2^-24 where s is near 1)
             const float s = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(a * -kLog2e));
             act = a * s;
             slope = __builtin_fmaf(act, 1.f - s, s);
         }
     } else {
-        const float half = exp_of(fmaxf(-0.5f * a * a, -87.f));
+        const float half = exp_of(-0.5f * a * a);
         float below;                               // the normal distribution's share below a
         if constexpr (EXACT) below = 0.5f * erfcf(a * -0.70710678118654752f);
         else {
