@@ -78,7 +78,7 @@ int sphattn_gated_ffn_fwd(const void* X, const void* Wg, const void* Wu, void* H
 
 /*
  * Gradients of that, from its inputs alone (A = X Wg^T and U = X Wu^T are formed again):
- *   dA = dH U act'(A)    dB = dH act(A)    dX = dA Wg + dB Wu    dWg = dA^T X    dWu = dB^T X        (relu: act' is 1 where A is greater than 0 in 64 bits, else 0)
+ *   dA = dH U act'(A)    dB = dH act(A)    dX = dA Wg + dB Wu    dWg = dA^T X    dWu = dB^T X        (relu: act' is 1 where A is greater than 0, else 0, as a sum in fp64 has it)
  *   dH : [T,F].  dX : [T,D], dWg, dWu : [F,D]; each may be NULL (not wanted), not all (SPHATTN_ERR_NULL; T = 0: all).  T = 0: dWg and dWu are zeros.
  * dA and dB are rounded once to the storage type (up to 2^18 of them to twice its bits; SPHATTN_F32: not; every factor of the sums keeps its 24 bits, terms are off by 2^-24 at
  * most), sums in fp32, the results rounded once.  fp16: dA and dB are scaled by powers of two, for dX by row and for dW by the largest row, from what

@@ -84,6 +84,7 @@ struct FfnArgs {
     const void* dH;                                // backward: [T,F]
     unsigned short *dA, *dB; long long part; int ld;   // [T,ld], in parts (fp32 three, few values two)
     const float *row_up, *all_up; unsigned short *dA_all, *dB_all;   // fp16: factors of dA and dB, and the second pair
+    const float *x_norm, *g_norm;                  // relu's slopes: the norms of X's and Wg's rows
 };
 
 // Eight (fp32: four) neighbouring elements of a row of F: what of it is in the row
@@ -123,55 +124,122 @@ __device__ __forceinline__ void whole_projections(f32x4 (&acc)[T::FP][T::FQ], co
     }
 }
 
-// relu's slope where A is all but 0: which side it is on is for the sum in 64 bits to say, not for what fp32 has lost of it (of 249 x 6144 values
-// one was on the other side: 1.2e-3 of dX, 1.7e-3 of dWg).  The values below 2^-19 of their row's largest here, some ten times the sums' errors, are looked at by the whole wave one
-// at a time; as A is spread, about one tile in twenty has one.
+// relu's slope beside 0: which side A is on is for the sum in 64 bits to say, not for what fp32 has lost of it (of 249 x 6144 values one was on the other side: 1.2e-3
+// of dX, 1.7e-3 of dWg).  What a sum may be off by goes by its terms, |x| |w| at most, however small it is itself: a matrix instruction was never more than 4.8 2^-24 of its terms'
+// and its addend's size off (10^6 sums of six kinds), and the partial sums of one that ends near 0 are half of the terms' size at most, so that n of them make (2.5 n + 5) 2^-24.
+// Values below that, an exact 0 among them, are formed again: few of a fragment four at a time, each by sixteen lanes, more of them with all of the fragment by the fp64 matrix
+// instruction, so that no data (sparse rows, weights that take an offset of X away) costs more than that.  (8192 rows, D = 2048: 3.4e-4 of values whose weights are normally distributed.)
+constexpr float kSlopeSteps = 3.f, kSlopeRest = 8.f, kSlopeParts = 13.f;   // 2^-24 of |x| |w| each: per instruction, at least, for what parts of fp32 leave out
+// Of a fragment's 256 values: gradients of 2048 x 1024 x 2048 in bf16 with 16, 32 and 256 of them 201, 283 and 1607 us four at a time, 295, 281 and 280 with the instruction (without any
+// 108); in fp32 441, 559 and 2376, 604, 605 and 594 (326)
+constexpr int kSlopeMany = 32;
+typedef __attribute__((ext_vector_type(4))) double f64x4;
+
 template <class T, Store S>
-__device__ __forceinline__ void settle_signs(f32x4 (&acc)[T::FP][T::FQ], const FfnArgs& a, int fw, int qw)
+__device__ __forceinline__ void settle_signs(f32x4 (&acc)[T::FP][T::FQ], const FfnArgs& a, int fw, int qw, bool whole)
 {
     constexpr int R = T::FP / 2 * 4;               // values of a row in a lane
     static_assert(R * T::FQ <= 64, "");
+    constexpr bool F32 = S == Store::F32;
+    constexpr int N = per16<S>();
     const int lane = threadIdx.x & 63, n16 = lane & 15, g = lane >> 4;
-    uint64_t open = 0, above = 0;                  // by value: not settled; greater than 0
+    // (fp32 as it is: four k an instruction)
+    const float steps = F32 && whole ? (float)((a.D + 3) / 4) : (float)((a.k + kStepK - 1) / kStepK);
+    const float off = 0x1p-24f * (kSlopeSteps * steps + kSlopeRest + (F32 ? kSlopeParts : 0.f));
+    uint64_t open = 0;                             // by value: not settled
+    float x_norm[T::FQ];
 #pragma unroll
-    for (int j = 0; j < T::FQ; ++j) {
-        float top = 0.f;
+    for (int j = 0; j < T::FQ; ++j) x_norm[j] = qw + 16 * j + n16 < a.T ? a.x_norm[qw + 16 * j + n16] : 0.f;
 #pragma unroll
-        for (int v = 0; v < R; ++v) top = fmaxf(top, __builtin_fabsf(acc[v / 4 * 2][j][v & 3]));
-        top = max_across_groups(top) * 0x1p-19f;
-        top = top < __builtin_inff() ? top : 0.f;  // (nothing is near 0 beside an infinite value)
+    for (int i = 0; i < R / 4; ++i) {
+        const int f = fw + 16 * i + 4 * g;
+        const f32x4 g_norm = *(const f32x4*)(a.g_norm + f);   // (the array goes on to a tile's end)
 #pragma unroll
-        for (int v = 0; v < R; ++v) {
-            const float x = acc[v / 4 * 2][j][v & 3];
-            const bool near = __builtin_fabsf(x) < top && x != 0.f && fw + v / 4 * 16 + 4 * g + (v & 3) < a.F && qw + 16 * j + n16 < a.T;
-            open |= (uint64_t)near << (j * R + v);
+        for (int r = 0; r < 4; ++r) {
+            const float norm = f + r < a.F ? g_norm[r] : 0.f;
+#pragma unroll
+            for (int j = 0; j < T::FQ; ++j) {
+                // (and what is lost below the normal numbers; a row of zeros has sums of 0)
+                const float size = __builtin_fabsf(acc[2 * i][j][r]), top = __builtin_fmaf(x_norm[j] * norm, off, 0x1p-132f);
+                const bool near = size <= top && size < __builtin_inff() && fminf(x_norm[j], norm) > 0.f;
+                open |= (uint64_t)near << (j * R + 4 * i + r);
+            }
         }
     }
     if (!__ballot(open != 0)) return;
+    asm("" : "+v"(open));                          // (seen through, each of its bits is kept as a comparison's own result, in scratch)
     const uint64_t found = open;
-    for (uint64_t lanes; (lanes = __ballot(open != 0)) != 0;) {
-        const int who = __builtin_ctzll(lanes);
-        const int which = __builtin_amdgcn_readlane(open ? __builtin_ctzll(open) : 0, who), j = which / R, v = which % R;
-        const size_t f = fw + v / 4 * 16 + 4 * (who >> 4) + (v & 3), q = qw + 16 * j + (who & 15);
-        double sum = 0.0;
-        if constexpr (S == Store::F32) {
-            for (int k = lane; k < a.D; k += 64) sum += (double)a.x_whole[q * a.D + k] * (double)a.g_whole[f * a.D + k];
-        } else {
-            for (int k = lane; k < a.D; k += 64) sum += (double)load_el<S>(a.X.data + q * a.X.ld, k) * (double)load_el<S>(a.G.data + f * a.G.ld, k);
+    uint64_t above = 0;                            // by value: greater than 0
+    // 16 bytes of row q of X or row f of Wg, zeros behind its end
+    const int end = F32 ? a.D : a.k;
+    auto piece = [&](bool of_x, int row, int k, float (&x)[N]) {
+        i32x4 w = {0, 0, 0, 0};
+        if (k < end) {
+            if constexpr (F32) w = load16<S, false>(of_x ? a.x_whole : a.g_whole, (size_t)row * end + k, end - k, (size_t)((of_x ? a.T : a.F) - row) * end - k);
+            else w = *(const i32x4*)((of_x ? a.X : a.G).data + (size_t)row * (of_x ? a.X : a.G).ld + (size_t)k * 2);
+        }
+        widen16<S>(w, x);
+    };
+#pragma unroll 1
+    for (int n = 0; n < R / 4 * T::FQ; ++n) {      // fragments with many
+        const uint32_t mine = (uint32_t)(open >> (n * 4)) & 15;
+        int count = 0;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) count += __builtin_popcountll(__ballot(mine >> r & 1));
+        if (count <= kSlopeMany) continue;
+        // (the instruction leaves row 4 r + g of its first operand in register r of lane group g: there goes column 4 g + r)
+        const int f = min(fw + n % (R / 4) * 16 + 4 * (n16 & 3) + (n16 >> 2), a.F - 1), q = min(qw + n / (R / 4) * 16 + n16, a.T - 1);
+        f64x4 sum = {0.0, 0.0, 0.0, 0.0};
+#pragma unroll 1
+        for (int k = g * N; k < end + g * N; k += 4 * N) {
+            float w[N], x[N];
+            piece(false, f, k, w);
+            piece(true, q, k, x);
+#pragma unroll
+            for (int i = 0; i < N; ++i) sum = __builtin_amdgcn_mfma_f64_16x16x4f64((double)w[i], (double)x[i], sum, 0, 0, 0);
         }
 #pragma unroll
-        for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
-        if (lane == who) {
-            open &= open - 1;
-            above |= (uint64_t)(sum > 0.0) << which;
+        for (int r = 0; r < 4; ++r) above |= (uint64_t)(sum[r] > 0.0) << (n * 4 + r);
+        open &= ~((uint64_t)15 << (n * 4));
+    }
+    for (uint64_t lanes; (lanes = __ballot(open != 0)) != 0;) {
+        const int first = open ? __builtin_ctzll(open) : 0;
+        int who[4], which[4], my_who = -1, my_which = 0;
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+            who[m] = lanes ? __builtin_ctzll(lanes) : -1;
+            lanes &= lanes - 1;
+            which[m] = __builtin_amdgcn_readlane(first, max(who[m], 0));
+            my_who = g == m ? who[m] : my_who;
+            my_which = g == m ? which[m] : my_which;
         }
+        const int j = my_which / R, v = my_which % R, at = max(my_who, 0);
+        const int f = min(fw + v / 4 * 16 + 4 * (at >> 4) + (v & 3), a.F - 1), q = min(qw + 16 * j + (at & 15), a.T - 1);
+        double sum = 0.0;
+#pragma unroll 2
+        for (int k = n16 * N; k < end; k += 16 * N) {
+            float w[N], x[N];
+            piece(false, f, k, w);
+            piece(true, q, k, x);
+#pragma unroll
+            for (int i = 0; i < N; ++i) sum = __builtin_fma((double)w[i], (double)x[i], sum);
+        }
+#pragma unroll
+        for (int d = 8; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+        const uint64_t positive = __ballot(sum > 0.0);
+#pragma unroll
+        for (int m = 0; m < 4; ++m)
+            if (lane == who[m]) {
+                open &= open - 1;
+                above |= (positive >> (16 * m) & 1) << which[m];
+            }
     }
 #pragma unroll
     for (int j = 0; j < T::FQ; ++j)
 #pragma unroll
         for (int v = 0; v < R; ++v) {
             const float x = acc[v / 4 * 2][j][v & 3], size = __builtin_fabsf(x);
-            acc[v / 4 * 2][j][v & 3] = !(found >> (j * R + v) & 1) ? x : above >> (j * R + v) & 1 ? size : -size;
+            acc[v / 4 * 2][j][v & 3] = !(found >> (j * R + v) & 1) ? x : above >> (j * R + v) & 1 ? fmaxf(size, 0x1p-126f) : -size;
         }
 }
 
@@ -191,6 +259,7 @@ void ffn_gate_kernel(FfnArgs a, int act)
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n16 = lane & 15, g = lane >> 4;
     const int fw = f0 + wave % T::WAVES_P * (T::FP / 2) * 16, qw = q0 + wave / T::WAVES_P * T::FQ * 16;   // this wave's corner
+    bool whole = false;
     if constexpr (F32) {
         int qe[T::FQ];
         bool endless = false;
@@ -207,10 +276,11 @@ void ffn_gate_kernel(FfnArgs a, int act)
                 for (int j = 0; j < T::FQ; ++j) prod.acc[i][j][r] = __builtin_ldexpf(prod.acc[i][j][r], pe[r] + qe[j]);
             }
         }
-        if (__ballot(endless)) whole_projections<T>(prod.acc, a, fw, qw);
+        whole = __ballot(endless) != 0;
+        if (whole) whole_projections<T>(prod.acc, a, fw, qw);
     }
     if constexpr (BACK)
-        if (act == (int)Gate::Relu) settle_signs<T, S>(prod.acc, a, fw, qw);
+        if (act == (int)Gate::Relu) settle_signs<T, S>(prod.acc, a, fw, qw, whole);
     static_assert(T::FP % 4 == 0, "");
     constexpr int E = store_bytes<S>();
     const void* const rows = BACK ? a.dH : a.H;
@@ -555,41 +625,50 @@ void ffn_pack_kernel(FfnPack a)
 // fp16.  dA and dB are at most |dH| |x| |w| 1.13 for the rows' norms (act's slope is 1.13 at most), which a power of two brings to 2^13 .. 2^14: by each
 // row t for dX, by the largest row for dW.  A dot product of D terms is about sqrt(D) below the product of the norms; from there down the type has
 // 2^-14 for normal numbers, so with D = 2048 a row's values keep their bits to 2^-22 of their usual size.
-// Norms of X's rows with the largest |dH| of each, and of Wg's and Wu's: a wave per row.
-template <bool WIDE>
+// Norms of X's rows, of Wg's and (fp16) of Wu's, and what X's come to with the largest |dH| of each: a wave per row, of the first `rows` of all of them.  Other types than fp16 take
+// the squares' sum in fp64, whose range theirs do not leave.
+template <Store S, bool WIDE>
 __global__ __launch_bounds__(256)
-void ffn_norms_kernel(const void* __restrict__ X, const void* __restrict__ dH, const void* __restrict__ Wg, const void* __restrict__ Wu, int T, int D, int F,
-                      float* __restrict__ x_bound, float* __restrict__ w_norm)
+void ffn_norms_kernel(const void* __restrict__ X, const void* __restrict__ dH, const void* __restrict__ Wg, const void* __restrict__ Wu, int T, int D, int F, long long rows,
+                      float* __restrict__ x_bound, float* __restrict__ x_norm, float* __restrict__ w_norm)
 {
-    constexpr Store S = Store::F16;
+    constexpr int N = per16<S>();
+    using Sum = std::conditional_t<S == Store::F16, float, double>;
     const int lane = threadIdx.x & 63;
     const long long unit = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if (unit >= (long long)T + 2 * F) return;
+    if (unit >= rows) return;
     const bool on_x = unit < T;
     const long long f = unit - T;
     const void* from = on_x ? X : f < F ? Wg : Wu;
     const size_t row = (size_t)(on_x ? unit : f < F ? f : f - F) * D, end = (size_t)(on_x ? T : F) * D;
-    float sum = 0.f, top = 1.f;
-    for (int c = lane * 8; c < D; c += 512) {
-        float x[8];
+    Sum sum = 0;
+    float top = 0.f;
+    for (int c = lane * N; c < D; c += 64 * N) {
+        float x[N];
         widen16<S>(load16<S, WIDE>(from, row + c, D - c, end - row - c), x);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum = __builtin_fmaf(x[i], x[i], sum);
+        for (int i = 0; i < N; ++i) {
+            if constexpr (S == Store::F16) sum = __builtin_fmaf(x[i], x[i], sum);
+            else sum = __builtin_fma((double)x[i], (double)x[i], sum);
+        }
     }
-    if (on_x) {
+    if (on_x && x_bound) {
         const size_t at = (size_t)unit * F;
-        top = 0.f;
-        for (int c = lane * 8; c < F; c += 512) {
-            float x[8];
+        for (int c = lane * N; c < F; c += 64 * N) {
+            float x[N];
             widen16<S>(load16<S, false>(dH, at + c, F - c, (size_t)T * F - at - c), x);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) top = fmaxf(top, __builtin_fabsf(x[i]));
+            for (int i = 0; i < N; ++i) top = fmaxf(top, __builtin_fabsf(x[i]));
         }
         top = max_over_wave(top);
     }
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
-    if (lane == 0) (on_x ? x_bound[unit] : w_norm[f]) = __builtin_sqrtf(sum) * top;
+    if (lane != 0) return;
+    const float norm = S == Store::F16 ? __builtin_sqrtf((float)sum) : (float)__builtin_sqrt((double)sum);
+    if (!on_x) w_norm[f] = norm;
+    if (on_x && x_bound) x_bound[unit] = norm * top;
+    if (on_x && x_norm) x_norm[unit] = norm;
 }
 
 // The rows' factors and the one for all; one workgroup.  A row whose bound is infinite or 0 keeps its values as they are.

@@ -184,7 +184,8 @@ struct Ffn {
     int *x_exp, *g_exp, *u_exp;                    // fp32
     unsigned short *x, *g, *u, *x_sum, *g_sum, *u_sum;
     unsigned short *dA, *dB, *dA_all, *dB_all;
-    float *x_bound, *w_norm, *row_up, *row_down, *all_up;   // fp16
+    float *x_norm, *w_norm;                        // fp16 and relu's slopes; w_norm: Wg's rows, fp16 Wu's behind them
+    float *x_bound, *row_up, *row_down, *all_up;   // fp16
     float *part, *part_w;                          // slices of dX and of dW
     size_t bytes;
 };
@@ -214,8 +215,9 @@ Ffn ffn_plan(int T, int D, int F, int dtype, bool back, void* workspace)
         p.dB = c.take<unsigned short>(n);
         p.dA_all = c.take<unsigned short>(f16 ? n : 0);
         p.dB_all = c.take<unsigned short>(f16 ? n : 0);
+        p.x_norm = c.take<float>(T);
+        p.w_norm = c.take<float>(up_to(f16 ? 2ll * F : F, 256));
         p.x_bound = c.take<float>(f16 ? T : 0);
-        p.w_norm = c.take<float>(f16 ? (size_t)2 * F : 0);
         p.row_up = c.take<float>(f16 ? T : 0);
         p.row_down = c.take<float>(f16 ? T : 0);
         p.all_up = c.take<float>(f16 ? 2 : 0);
@@ -347,11 +349,15 @@ int run_ffn_bwd(const Ffn& p, const void* X, const void* Wg, const void* Wu, con
     if (p.T > 0) {
         a = ffn_pack<S>(p, X, Wg, Wu, stream);
         a.dH = dH, a.dA = p.dA, a.dB = p.dB, a.part = (long long)p.T * p.ldf, a.ld = p.ldf;
+        if (F16 || act == SPHATTN_GATE_RELU) {
+            const long long rows = (long long)p.T + (F16 ? 2 : 1) * (long long)p.F;
+            const bool wide = !off(X, 16) && !off(Wg, 16) && !off(Wu, 16) && p.D % per16<S>() == 0;
+            const auto kern = wide ? ffn_norms_kernel<S, true> : ffn_norms_kernel<S, false>;
+            hipLaunchKernelGGL(kern, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, stream, X, dH, Wg, Wu, p.T, p.D, p.F, rows, F16 ? p.x_bound : (float*)nullptr,
+                               act == SPHATTN_GATE_RELU ? p.x_norm : (float*)nullptr, p.w_norm);
+            a.x_norm = p.x_norm, a.g_norm = p.w_norm;
+        }
         if (F16) {
-            const dim3 grid((unsigned)(((long long)p.T + 2 * p.F + 3) / 4));
-            if (!off(X, 16) && !off(Wg, 16) && !off(Wu, 16) && p.D % 8 == 0)
-                hipLaunchKernelGGL((ffn_norms_kernel<true>), grid, dim3(256), 0, stream, X, dH, Wg, Wu, p.T, p.D, p.F, p.x_bound, p.w_norm);
-            else hipLaunchKernelGGL((ffn_norms_kernel<false>), grid, dim3(256), 0, stream, X, dH, Wg, Wu, p.T, p.D, p.F, p.x_bound, p.w_norm);
             hipLaunchKernelGGL(ffn_factors_kernel, dim3(1), dim3(1024), 0, stream, p.x_bound, p.w_norm, p.T, p.F, p.row_up, p.row_down, p.all_up);
             a.row_up = p.row_up, a.all_up = p.all_up, a.dA_all = dw ? p.dA_all : nullptr, a.dB_all = p.dB_all;
         }
