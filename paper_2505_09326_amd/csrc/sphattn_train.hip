@@ -248,7 +248,7 @@ int launch_teacher(const Teacher& p, const void* ids, int id_bytes, const float*
 {
     const auto kern = p.padded <= 64 ? taught_kernel<true> : taught_kernel<false>;
     hipLaunchKernelGGL(kern, dim3((unsigned)(T + kTaughtWaves - 1) / kTaughtWaves), dim3(kTaughtThreads), (size_t)taught_lds_bytes(p.padded), stream,
-                       ids, id_bytes, teacher, T, V, p.K, p.padded, 1.f / p.tau, p.targets, p.sorted, p.weights, p.starts, p.shift, p.blocks, p.logits);
+                       ids, id_bytes, teacher, T, V, p.K, p.padded, p.tau, p.targets, p.sorted, p.weights, p.starts, p.shift, p.blocks, p.logits);
     return launched();
 }
 

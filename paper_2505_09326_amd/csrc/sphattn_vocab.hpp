@@ -1003,7 +1003,7 @@ inline int taught_lds_bytes(int padded) { return kTaughtWaves * (padded <= 64 ? 
 
 template <bool LANES>
 __global__ __launch_bounds__(kTaughtThreads)
-void taught_kernel(const void* __restrict__ ids, int id_bytes, const float* __restrict__ teacher, int T, int V, int K, int padded, float over_tau,
+void taught_kernel(const void* __restrict__ ids, int id_bytes, const float* __restrict__ teacher, int T, int V, int K, int padded, float tau,
                    int* __restrict__ targets, int* __restrict__ sorted, float* __restrict__ weights, unsigned short* __restrict__ starts, int shift, int blocks,
                    float* __restrict__ logits)    // forward: those of no entry are 0, the rest is the tiles'
 {
@@ -1023,8 +1023,7 @@ void taught_kernel(const void* __restrict__ ids, int id_bytes, const float* __re
     for (int k = lane; k < padded; k += 64) {
         const bool in = t < T && k < K;
         const int id = in ? load_id(ids, id_bytes, row + k) : -1;
-        const float logit = in ? teacher[row + k] : 0.f;
-        const float x = id >= 0 ? logit * over_tau : -__builtin_inff();
+        const float x = id >= 0 ? teacher[row + k] : -__builtin_inff();
         bad |= id >= V;
         none |= x != x;
         top = fmaxf(top, x);
@@ -1035,8 +1034,10 @@ void taught_kernel(const void* __restrict__ ids, int id_bytes, const float* __re
     top = max_over_wave(top);
     none = __ballot(none) != 0;
     bad = __ballot(bad) != 0;
-    for (int k = lane; k < padded; k += 64) {      // (an infinite top: its difference to itself is no number, as in the formula)
-        const float e = p[k] == -__builtin_inff() ? 0.f : expf(p[k] - top);
+    // (by tau behind the difference: what all of a row's logits have in common takes no bits from p, and none is past fp32's range with it.  An infinite top: its difference to itself is
+    // no number, as in the formula)
+    for (int k = lane; k < padded; k += 64) {
+        const float e = p[k] == -__builtin_inff() ? 0.f : expf((p[k] - top) / tau);
         p[k] = e;
         sum += e;
     }
