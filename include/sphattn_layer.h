@@ -81,8 +81,8 @@ int sphattn_gated_ffn_fwd(const void* X, const void* Wg, const void* Wu, void* H
  *   dA = dH U act'(A)    dB = dH act(A)    dX = dA Wg + dB Wu    dWg = dA^T X    dWu = dB^T X        (relu: act' is 1 where A is greater than 0, else 0, as a sum in fp64 has it)
  *   dH : [T,F].  dX : [T,D], dWg, dWu : [F,D]; each may be NULL (not wanted), not all (SPHATTN_ERR_NULL; T = 0: all).  T = 0: dWg and dWu are zeros.
  * dA and dB are rounded once to the storage type (up to 2^18 of them to twice its bits; SPHATTN_F32: not; every factor of the sums keeps its 24 bits, terms are off by 2^-24 at
- * most), sums in fp32, the results rounded once.  fp16: dA and dB are scaled by powers of two, for dX by row and for dW by the largest row, from what
- * the norms of X's and W's rows and a row's largest dH allow at most: values down to 2^-27 of that keep the type's bits.
+ * most), sums in fp32, the results rounded once.  fp16: dA and dB are scaled by powers of two, for dX by row and for dW by column, from what
+ * the norms of X's and W's rows and the largest dH of the row or column allow at most: values down to 2^-27 of that keep the type's bits.
  * Where they have more than 16 bits an infinite element of dA, dB, X or W may make NaN of a sum that it would make infinite.
  */
 size_t sphattn_gated_ffn_bwd_workspace_bytes(int T, int D, int F, int dtype);

@@ -83,7 +83,8 @@ struct FfnArgs {
     void* H;                                       // forward: [T,F]
     const void* dH;                                // backward: [T,F]
     unsigned short *dA, *dB; long long part; int ld;   // [T,ld], in parts (fp32 three, few values two)
-    const float *row_up, *all_up; unsigned short *dA_all, *dB_all;   // fp16: factors of dA and dB, and the second pair
+    // fp16: factors of dA and dB by row, and the second pair with powers of two by column, dA's in the lower half of an int
+    const float* row_up; const int* col_up; unsigned short *dA_all, *dB_all;
     const float *x_norm, *g_norm;                  // relu's slopes: the norms of X's and Wg's rows
 };
 
@@ -302,14 +303,21 @@ void ffn_gate_kernel(FfnArgs a, int act)
             }
         }
     }
+    i32x4 col_up[T::FP / 2];                       // (the array goes on to a tile's end: what stands there changes nothing, the values are 0)
+    if constexpr (BACK && HALF) {
+        if (a.dA_all) {
+#pragma unroll
+            for (int i = 0; i < T::FP / 2; ++i) col_up[i] = *(const i32x4*)(a.col_up + fw + 16 * i + 4 * g);
+        }
+    }
     auto corner = [&](auto gate_of) {
         constexpr Gate G = decltype(gate_of)::value;
 #pragma unroll
         for (int j = 0; j < T::FQ; ++j) {
             const int q = qw + 16 * j + n16;
             const size_t row = (size_t)min(q, a.T - 1) * a.F;
-            float up = 1.f, up_all = 1.f;
-            if constexpr (BACK && HALF) up = a.row_up[min(q, a.T - 1)], up_all = *a.all_up;
+            float up = 1.f;
+            if constexpr (BACK && HALF) up = a.row_up[min(q, a.T - 1)];
 #pragma unroll
             for (int i = 0; i < T::FP / 2; i += 2) {
                 // where this lane's piece of the two fragments stands (fp32: a piece of each)
@@ -387,8 +395,16 @@ void ffn_gate_kernel(FfnArgs a, int act)
                         put(a.dB, z, up);
                         if constexpr (HALF) {
                             if (a.dA_all) {
-                                put(a.dA_all, y, up_all);
-                                put(a.dB_all, z, up_all);
+#pragma unroll
+                                for (int s = 0; s < 2; ++s)
+#pragma unroll
+                                    for (int r = 0; r < 4; ++r) {
+                                        const int e = col_up[i + s][r];
+                                        y[s][r] = __builtin_ldexpf(y[s][r], e << 16 >> 16);
+                                        z[s][r] = __builtin_ldexpf(z[s][r], e >> 16);
+                                    }
+                                put(a.dA_all, y, 1.f);
+                                put(a.dB_all, z, 1.f);
                             }
                         }
                     }
@@ -491,7 +507,7 @@ struct FfnSum {
     int k, tiles_p, slices;
     void* out; int out_ld, out_cols, out_rows;     // in the storage type, where there is one slice
     float* part; int part_ld;                      // else [slices][out_rows][part_ld]
-    const float *row_down, *down;                  // fp16: by row, or one
+    const float* row_down;                         // fp16
 };
 
 // dX [T,D] = dA Wg + dB Wu
@@ -524,7 +540,7 @@ __device__ __forceinline__ void ffn_sum_tile(const FfnSum& a, int id, SPH_LDS un
             continue;
         }
         float by = 1.f;
-        if constexpr (S == Store::F16) by = a.row_down ? a.row_down[min(q, a.out_rows - 1)] : a.down ? *a.down : 1.f;
+        if constexpr (S == Store::F16) by = a.row_down ? a.row_down[min(q, a.out_rows - 1)] : 1.f;
         const size_t row = (size_t)q * a.out_ld;
 #pragma unroll
         for (int i = 0; i < T::FP; i += 2) {
@@ -589,7 +605,7 @@ void ffn_join_kernel(FfnJoin j)
         for (int i = 0; i < AHEAD; ++i)
             if (s0 + i < a.slices) x += y[i];
     }
-    if constexpr (S == Store::F16) x *= a.row_down ? a.row_down[q] : a.down ? *a.down : 1.f;
+    if constexpr (S == Store::F16) x *= a.row_down ? a.row_down[q] : 1.f;
     const size_t at = (size_t)q * a.out_ld + c;
     const int left = a.out_cols - c;
     if (left >= 4) {
@@ -607,9 +623,32 @@ void ffn_join_kernel(FfnJoin j)
 
 // ---- around the products ------------------------------------------------------------------------------------
 
-// X, Wg and Wu as the products take them (those with an `out`): a wave per row
-struct FfnPack { PackRows m[3]; int until[2]; };   // workgroups below until[0] on the first, below until[1] on the second
+// X, Wg and Wu as the products take them (those with an `out`), and the norms of their rows (those with a `norm`): a wave per row.  Other types than fp16 take the squares' sum in
+// fp64, whose range theirs do not leave.
+struct FfnPack { PackRows m[3]; float* norm[3]; int until[2]; };   // workgroups below until[0] on the first, below until[1] on the second
 constexpr int kFfnPackThreads = 256, kFfnPackRows = kFfnPackThreads / 64;
+
+template <Store S>
+__device__ __forceinline__ float row_norm(const PackRows& a, long long row, int lane)
+{
+    constexpr int N = per16<S>();
+    const size_t from = (size_t)row * a.D, end = (size_t)a.n * a.D;
+    const bool wide = ((uintptr_t)a.in & 15) == 0 && a.D % N == 0;
+    std::conditional_t<S == Store::F16, float, double> sum = 0;
+    for (int c = lane * N; c < a.D; c += 64 * N) {
+        float x[N];
+        widen16<S>(wide ? load16<S, true>(a.in, from + c, N, N) : load16<S, false>(a.in, from + c, a.D - c, end - from - c), x);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if constexpr (S == Store::F16) sum = __builtin_fmaf(x[i], x[i], sum);
+            else sum = __builtin_fma((double)x[i], (double)x[i], sum);
+        }
+    }
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+    if constexpr (S == Store::F16) return __builtin_sqrtf(sum);
+    else return (float)__builtin_sqrt(sum);
+}
 
 template <Store S>
 __global__ __launch_bounds__(kFfnPackThreads)
@@ -619,90 +658,126 @@ void ffn_pack_kernel(FfnPack a)
     const int m = block < a.until[0] ? 0 : block < a.until[1] ? 1 : 2;
     const PackRows& rows = a.m[m];
     const long long row = (long long)(block - (m == 0 ? 0 : a.until[m - 1])) * kFfnPackRows + wave;
-    if (row < rows.n) pack_row<S>(rows, row, row, lane);
+    if (row >= rows.n) return;
+    if (a.norm[m]) {
+        const float norm = row_norm<S>(rows, row, lane);
+        if (lane == 0) a.norm[m][row] = norm;
+    }
+    pack_row<S>(rows, row, row, lane);
 }
 
-// fp16.  dA and dB are at most |dH| |x| |w| 1.13 for the rows' norms (act's slope is 1.13 at most), which a power of two brings to 2^13 .. 2^14: by each
-// row t for dX, by the largest row for dW.  A dot product of D terms is about sqrt(D) below the product of the norms; from there down the type has
-// 2^-14 for normal numbers, so with D = 2048 a row's values keep their bits to 2^-22 of their usual size.
-// Norms of X's rows, of Wg's and (fp16) of Wu's, and what X's come to with the largest |dH| of each: a wave per row, of the first `rows` of all of them.  Other types than fp16 take
-// the squares' sum in fp64, whose range theirs do not leave.
-template <Store S, bool WIDE>
+// fp16.  dA and dB are at most |dH| |x| |w| 1.13 for the rows' norms (act's slope is 1.13 at most), which a power of two brings to 2^13 .. 2^14: for dX by row t, of the largest
+// |dH| of the row and the largest |w|; for dW, where dA and dB are a pair of their own, by column f, of the largest |dH| |x| of the column and its own |w| (one power for all of
+// it lost the bits of units whose gradient is 2^-27 of that of others, as those of gates that are all but closed).  A dot product of D terms is about sqrt(D) below the product of
+// the norms; from there down the type has 2^-14 for normal numbers, so with D = 2048 values keep their bits to 2^-22 of their row's or column's usual size.
+// The largest |dH| of each row in each 512 columns, and the largest |dH| |x| of each column in each `rows` rows: a workgroup for both.  NaN counts for nothing, and neither does a row of X that is not finite.
+constexpr int kTopCols = 512, kTopRows = 64, kTopMost = 64;   // (parts of a column at most)
+template <bool EIGHT>                               // columns or more
 __global__ __launch_bounds__(256)
-void ffn_norms_kernel(const void* __restrict__ X, const void* __restrict__ dH, const void* __restrict__ Wg, const void* __restrict__ Wu, int T, int D, int F, long long rows,
-                      float* __restrict__ x_bound, float* __restrict__ x_norm, float* __restrict__ w_norm)
+void ffn_tops_kernel(const void* __restrict__ dH, const float* __restrict__ x_norm, int T, int F, int rows, float* __restrict__ row_top, float* __restrict__ col_top)
 {
-    constexpr int N = per16<S>();
-    using Sum = std::conditional_t<S == Store::F16, float, double>;
-    const int lane = threadIdx.x & 63;
-    const long long unit = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if (unit >= rows) return;
-    const bool on_x = unit < T;
-    const long long f = unit - T;
-    const void* from = on_x ? X : f < F ? Wg : Wu;
-    const size_t row = (size_t)(on_x ? unit : f < F ? f : f - F) * D, end = (size_t)(on_x ? T : F) * D;
-    Sum sum = 0;
-    float top = 0.f;
-    for (int c = lane * N; c < D; c += 64 * N) {
-        float x[N];
-        widen16<S>(load16<S, WIDE>(from, row + c, D - c, end - row - c), x);
+    constexpr Store S = Store::F16;
+    constexpr int AHEAD = 16;                      // rows whose loads are under way
+    __shared__ float shared[4][kTopCols];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int tiles = (F + kTopCols - 1) / kTopCols, tile = (int)(blockIdx.x % tiles), part = (int)(blockIdx.x / tiles);
+    const int end = (int)min((long long)T, (long long)(part + 1) * rows);
+    // (a row's last eight columns in the place of what goes past its end: the same maxima)
+    const int c = min(tile * kTopCols + lane * 8, max(F - 8, 0));
+    float col[8];
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            if constexpr (S == Store::F16) sum = __builtin_fmaf(x[i], x[i], sum);
-            else sum = __builtin_fma((double)x[i], (double)x[i], sum);
+    for (int i = 0; i < 8; ++i) col[i] = 0.f;
+    for (long long t0 = (long long)part * rows + wave * AHEAD; t0 < end; t0 += 4 * AHEAD) {
+        const int last = min(AHEAD, (int)(end - t0)) - 1;      // (and the last row more than once)
+        const unsigned short* const from = (const unsigned short*)dH + (size_t)t0 * F + c;
+        i32x4 w[AHEAD];
+        float norm[AHEAD], top[AHEAD];
+#pragma unroll
+        for (int a = 0; a < AHEAD; ++a) {
+            const int r = min(a, last);
+            if constexpr (EIGHT) __builtin_memcpy(&w[a], from + (uint32_t)(r * F), 16);
+            else w[a] = load16<S, false>(from, (size_t)r * F, F, (size_t)(T - t0 - r) * F);
+            norm[a] = x_norm[t0 + r];
         }
-    }
-    if (on_x && x_bound) {
-        const size_t at = (size_t)unit * F;
-        for (int c = lane * N; c < F; c += 64 * N) {
-            float x[N];
-            widen16<S>(load16<S, false>(dH, at + c, F - c, (size_t)T * F - at - c), x);
 #pragma unroll
-            for (int i = 0; i < N; ++i) top = fmaxf(top, __builtin_fabsf(x[i]));
+        for (int a = 0; a < AHEAD; ++a) {
+            float x[8];
+            widen16<S>(w[a], x);
+            top[a] = 0.f;
+            norm[a] = norm[a] < __builtin_inff() ? norm[a] : 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float size = __builtin_fabsf(x[i]);
+                top[a] = fmaxf(top[a], size);
+                col[i] = fmaxf(col[i], size * norm[a]);
+            }
         }
-        top = max_over_wave(top);
+        // sixteen maxima over the wave: half of the rows go to the lanes across at each exchange, in the end row r is with lanes 4 r .. 4 r + 3
+        auto halve = [&](auto half) {
+            constexpr int H = decltype(half)::value;
+            const bool upper = (lane & 4 * H) != 0;
+#pragma unroll
+            for (int i = 0; i < H; ++i) {
+                const float other = __shfl_xor(upper ? top[i] : top[i + H], 4 * H);
+                top[i] = fmaxf(upper ? top[i + H] : top[i], other);
+            }
+        };
+        static_assert(AHEAD == 16, "");
+        halve(std::integral_constant<int, 8>{});
+        halve(std::integral_constant<int, 4>{});
+        halve(std::integral_constant<int, 2>{});
+        halve(std::integral_constant<int, 1>{});
+        top[0] = fmaxf(top[0], __shfl_xor(top[0], 2));
+        top[0] = fmaxf(top[0], __shfl_xor(top[0], 1));
+        if ((lane & 3) == 0 && t0 + (lane >> 2) < end) row_top[(size_t)tile * T + t0 + (lane >> 2)] = top[0];
     }
 #pragma unroll
-    for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
-    if (lane != 0) return;
-    const float norm = S == Store::F16 ? __builtin_sqrtf((float)sum) : (float)__builtin_sqrt((double)sum);
-    if (!on_x) w_norm[f] = norm;
-    if (on_x && x_bound) x_bound[unit] = norm * top;
-    if (on_x && x_norm) x_norm[unit] = norm;
+    for (int i = 0; i < 8; ++i) shared[wave][lane * 8 + i] = col[i];
+    __syncthreads();
+    for (int i = threadIdx.x; i < kTopCols; i += 256) {
+        const int own = tile * kTopCols + i / 8 * 8, f = min(own, max(F - 8, 0)) + i % 8;   // (the column of this place; each is written by the lane that it belongs to)
+        if (f >= own && f < F) col_top[(size_t)part * F + f] = fmaxf(fmaxf(shared[0][i], shared[1][i]), fmaxf(shared[2][i], shared[3][i]));
+    }
 }
 
-// The rows' factors and the one for all; one workgroup.  A row whose bound is infinite or 0 keeps its values as they are.
-__global__ __launch_bounds__(1024)
-void ffn_factors_kernel(const float* __restrict__ x_bound, const float* __restrict__ w_norm, int T, int F, float* __restrict__ row_up, float* __restrict__ row_down,
-                        float* __restrict__ all)       // all: up, down
+// The rows' factors and the columns': a thread each, rows first.  One whose bound is infinite or 0 keeps its values as they are.
+constexpr int kFactorThreads = 1024;
+__global__ __launch_bounds__(kFactorThreads)
+void ffn_factors_kernel(const float* __restrict__ x_norm, const float* __restrict__ w_norm, const float* __restrict__ row_top, const float* __restrict__ col_top, int T, int F, int parts,
+                        float* __restrict__ row_up, float* __restrict__ row_down, int* __restrict__ col_up, float* __restrict__ down_a, float* __restrict__ down_b)
 {
-    __shared__ float shared[16];
+    __shared__ float shared[kFactorThreads / 64];
     const int tid = threadIdx.x;
-    auto over_all = [&](float x) {
-        x = max_over_wave(x);
-        __syncthreads();
-        if ((tid & 63) == 0) shared[tid >> 6] = x;
-        __syncthreads();
-        for (int w = 0; w < 16; ++w) x = fmaxf(x, shared[w]);
-        return x;
+    auto power = [](float x) { return x > 0.f && x < __builtin_inff() ? max(-100, min(100, 13 - (__builtin_amdgcn_frexp_expf(x) - 1))) : 0; };
+    auto largest = [](const float* from, int n, int apart) {   // of every apart-th, eight loads under way
+        float top = 0.f;
+        for (int i0 = 0; i0 < n; i0 += 8) {
+            float x[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = from[(size_t)min(i0 + i, n - 1) * apart];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) top = fmaxf(top, x[i]);
+        }
+        return top;
     };
-    float w = 0.f;
-    for (int f = tid; f < 2 * F; f += 1024) w = w_norm[f] < __builtin_inff() ? fmaxf(w, w_norm[f]) : w;
-    w = over_all(w);
-    auto factor = [](float x) {
-        return x > 0.f && x < __builtin_inff() ? __builtin_ldexpf(1.f, max(-100, min(100, 13 - (__builtin_amdgcn_frexp_expf(x) - 1)))) : 1.f;
-    };
-    float top = 0.f;
-    for (int t = tid; t < T; t += 1024) {
-        const float b = x_bound[t] * w * 1.13f, up = factor(b);
-        top = b < __builtin_inff() ? fmaxf(top, b) : top;
-        row_up[t] = up;
-        row_down[t] = 1.f / up;
-    }
-    top = over_all(top);
-    if (tid == 0) {
-        all[0] = factor(top);
-        all[1] = 1.f / all[0];
+    const long long unit = (long long)blockIdx.x * kFactorThreads + tid, f = unit - T;
+    const float top = unit < T ? largest(row_top + unit, (F + kTopCols - 1) / kTopCols, T) : f < F ? largest(col_top + f, parts, F) : 0.f;
+    float w = 0.f;                                 // (each workgroup for itself: a launch less)
+#pragma unroll 4
+    for (int i = tid; i < 2 * F; i += kFactorThreads) w = w_norm[i] < __builtin_inff() ? fmaxf(w, w_norm[i]) : w;
+    w = max_over_wave(w);
+    if ((tid & 63) == 0) shared[tid >> 6] = w;
+    __syncthreads();
+    for (int i = 0; i < kFactorThreads / 64; ++i) w = fmaxf(w, shared[i]);
+    if (unit < T) {
+        const int e = power(x_norm[unit] * top * w * 1.13f);
+        row_up[unit] = __builtin_ldexpf(1.f, e);
+        row_down[unit] = __builtin_ldexpf(1.f, -e);
+    } else if (f < F) {
+        const int a = power(top * w_norm[F + f] * 1.13f), b = power(top * w_norm[f] * 1.13f);
+        col_up[f] = (a & 0xffff) | b << 16;
+        down_a[f] = __builtin_ldexpf(1.f, -a);
+        down_b[f] = __builtin_ldexpf(1.f, -b);
     }
 }
 

@@ -185,7 +185,9 @@ struct Ffn {
     unsigned short *x, *g, *u, *x_sum, *g_sum, *u_sum;
     unsigned short *dA, *dB, *dA_all, *dB_all;
     float *x_norm, *w_norm;                        // fp16 and relu's slopes; w_norm: Wg's rows, fp16 Wu's behind them
-    float *x_bound, *row_up, *row_down, *all_up;   // fp16
+    // fp16: the largest of dH by row and by column in parts, factors by row and by column
+    float *row_top, *col_top, *row_up, *row_down, *down_a, *down_b;
+    int *col_up, top_rows, top_parts;
     float *part, *part_w;                          // slices of dX and of dW
     size_t bytes;
 };
@@ -217,10 +219,15 @@ Ffn ffn_plan(int T, int D, int F, int dtype, bool back, void* workspace)
         p.dB_all = c.take<unsigned short>(f16 ? n : 0);
         p.x_norm = c.take<float>(T);
         p.w_norm = c.take<float>(up_to(f16 ? 2ll * F : F, 256));
-        p.x_bound = c.take<float>(f16 ? T : 0);
+        p.top_rows = (int)up_to((T + kTopMost - 1) / kTopMost, kTopRows);
+        p.top_parts = T > 0 ? (T + p.top_rows - 1) / p.top_rows : 0;
+        p.row_top = c.take<float>(f16 ? (size_t)((F + kTopCols - 1) / kTopCols) * T : 0);
+        p.col_top = c.take<float>(f16 ? (size_t)p.top_parts * F : 0);
         p.row_up = c.take<float>(f16 ? T : 0);
         p.row_down = c.take<float>(f16 ? T : 0);
-        p.all_up = c.take<float>(f16 ? 2 : 0);
+        p.col_up = c.take<int>(f16 ? up_to(F, 256) : 0);
+        p.down_a = c.take<float>(f16 ? F : 0);
+        p.down_b = c.take<float>(f16 ? F : 0);
         const int products = f32 ? 6 : p.two ? 2 : 1;
         p.dx = sum_choice(T > 0 ? T : 1, p.ld, 2ll * F, 1, products, !p.two);
         p.dw = T > 0 ? sum_choice(F, p.ld, T, 2, products, !p.two) : SumChoice{false, 1};
@@ -250,27 +257,30 @@ int run_gate(FfnArgs& a, int act, hipStream_t stream)
     return big_tiles(2ll * a.F, a.T) ? launch_gate<Big, S, BACK>(a, act, stream) : launch_gate<Mid, S, BACK>(a, act, stream);
 }
 
-// X, Wg and Wu as the products take them; what can be read as it is stays where it is
+// X, Wg and Wu as the products take them (what can be read as it is stays where it is), and the norms of X's and Wg's rows, of Wu's too
 template <Store S>
-FfnArgs ffn_pack(const Ffn& p, const void* X, const void* Wg, const void* Wu, hipStream_t stream)
+FfnArgs ffn_pack(const Ffn& p, const void* X, const void* Wg, const void* Wu, bool norms, bool norms_u, hipStream_t stream)
 {
     FfnArgs a{};
     FfnPack k{};
     int groups = 0;
-    auto take = [&](int m, const void* in, int n, unsigned short* out, unsigned short* sum_out, int* exp) {
+    auto take = [&](int m, const void* in, int n, unsigned short* out, unsigned short* sum_out, int* exp, float* norm) {
         Operand o{(const unsigned char*)in, 0, p.D * 2, n};
-        if (!ready(in, p.D, S)) {
-            k.m[m] = PackRows{in, out, n, p.D, p.ld, (long long)n * p.ld, sum_out, exp};
+        const bool copy = !ready(in, p.D, S);
+        if (copy || norm) {
+            k.m[m] = PackRows{in, copy ? out : nullptr, n, p.D, p.ld, (long long)n * p.ld, sum_out, exp};
+            k.norm[m] = norm;
             groups += (n + kFfnPackRows - 1) / kFfnPackRows;
-            o = Operand{(const unsigned char*)out, k.m[m].part * 2, p.ld * 2, n};
         }
+        if (copy) o = Operand{(const unsigned char*)out, k.m[m].part * 2, p.ld * 2, n};
         if (m < 2) k.until[m] = groups;
         return o;
     };
-    a.X = take(0, X, p.T, p.x, p.x_sum, p.x_exp);
-    a.G = take(1, Wg, p.F, p.g, p.g_sum, p.g_exp);
-    a.U = take(2, Wu, p.F, p.u, p.u_sum, p.u_exp);
+    a.X = take(0, X, p.T, p.x, p.x_sum, p.x_exp, norms ? p.x_norm : nullptr);
+    a.G = take(1, Wg, p.F, p.g, p.g_sum, p.g_exp, norms ? p.w_norm : nullptr);
+    a.U = take(2, Wu, p.F, p.u, p.u_sum, p.u_exp, norms_u ? p.w_norm + p.F : nullptr);
     if (groups) hipLaunchKernelGGL((ffn_pack_kernel<S>), dim3((unsigned)groups), dim3(kFfnPackThreads), 0, stream, k);
+    a.x_norm = p.x_norm, a.g_norm = p.w_norm;
     a.g_exp = p.g_exp, a.u_exp = p.u_exp, a.x_exp = p.x_exp;
     a.g_whole = (const float*)Wg, a.u_whole = (const float*)Wu, a.x_whole = (const float*)X, a.D = p.D;
     a.k = p.ld, a.T = p.T, a.F = p.F;
@@ -295,7 +305,7 @@ int run_ffn_fwd(const Ffn& p, const void* X, const void* Wg, const void* Wu, voi
         if (p.T <= 32) return launch_rows<S, 2>(X, Wg, Wu, H, p.T, p.D, p.F, act, stream);
         return launch_rows<S, 4>(X, Wg, Wu, H, p.T, p.D, p.F, act, stream);
     }
-    FfnArgs a = ffn_pack<S>(p, X, Wg, Wu, stream);
+    FfnArgs a = ffn_pack<S>(p, X, Wg, Wu, false, false, stream);
     a.H = H;
     return run_gate<S, false>(a, act, stream);
 }
@@ -347,19 +357,15 @@ int run_ffn_bwd(const Ffn& p, const void* X, const void* Wg, const void* Wu, con
     a.X = Operand{nullptr, 0, p.ld * 2, 0};
     int rc = SPHATTN_OK;
     if (p.T > 0) {
-        a = ffn_pack<S>(p, X, Wg, Wu, stream);
+        a = ffn_pack<S>(p, X, Wg, Wu, F16 || act == SPHATTN_GATE_RELU, F16, stream);
         a.dH = dH, a.dA = p.dA, a.dB = p.dB, a.part = (long long)p.T * p.ldf, a.ld = p.ldf;
-        if (F16 || act == SPHATTN_GATE_RELU) {
-            const long long rows = (long long)p.T + (F16 ? 2 : 1) * (long long)p.F;
-            const bool wide = !off(X, 16) && !off(Wg, 16) && !off(Wu, 16) && p.D % per16<S>() == 0;
-            const auto kern = wide ? ffn_norms_kernel<S, true> : ffn_norms_kernel<S, false>;
-            hipLaunchKernelGGL(kern, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, stream, X, dH, Wg, Wu, p.T, p.D, p.F, rows, F16 ? p.x_bound : (float*)nullptr,
-                               act == SPHATTN_GATE_RELU ? p.x_norm : (float*)nullptr, p.w_norm);
-            a.x_norm = p.x_norm, a.g_norm = p.w_norm;
-        }
         if (F16) {
-            hipLaunchKernelGGL(ffn_factors_kernel, dim3(1), dim3(1024), 0, stream, p.x_bound, p.w_norm, p.T, p.F, p.row_up, p.row_down, p.all_up);
-            a.row_up = p.row_up, a.all_up = p.all_up, a.dA_all = dw ? p.dA_all : nullptr, a.dB_all = p.dB_all;
+            const long long tiles = (p.F + kTopCols - 1) / kTopCols, units = (long long)p.T + p.F;
+            const auto tops = p.F >= 8 ? ffn_tops_kernel<true> : ffn_tops_kernel<false>;
+            hipLaunchKernelGGL(tops, dim3((unsigned)(tiles * p.top_parts)), dim3(256), 0, stream, dH, p.x_norm, p.T, p.F, p.top_rows, p.row_top, p.col_top);
+            hipLaunchKernelGGL(ffn_factors_kernel, dim3((unsigned)((units + kFactorThreads - 1) / kFactorThreads)), dim3(kFactorThreads), 0, stream, p.x_norm, p.w_norm, p.row_top,
+                               p.col_top, p.T, p.F, p.top_parts, p.row_up, p.row_down, p.col_up, p.down_a, p.down_b);
+            a.row_up = p.row_up, a.col_up = p.col_up, a.dA_all = dw ? p.dA_all : nullptr, a.dB_all = p.dB_all;
         }
         if constexpr (F32) rc = run_gate<S, true>(a, act, stream);
         else rc = p.two ? launch_gate<Mid, S, true, true>(a, act, stream) : run_gate<S, true>(a, act, stream);
@@ -397,7 +403,7 @@ int run_ffn_bwd(const Ffn& p, const void* X, const void* Wg, const void* Wu, con
             s[n].Q = Operand{(const unsigned char*)q, part, p.ldf * 2, p.ldf};
             s[n].k = p.T, s[n].slices = p.dw.slices, s[n].out = out, s[n].out_ld = s[n].out_cols = p.D, s[n].out_rows = p.F;
             s[n].part = p.part_w ? p.part_w + (size_t)n * p.dw.slices * p.F * p.ld : nullptr, s[n].part_ld = p.ld;
-            if (F16 && p.T > 0) s[n].down = p.all_up + 1;
+            if (F16 && p.T > 0) s[n].row_down = m ? p.down_b : p.down_a;
             ++n;
         }
         FfnSum* second = n == 2 ? &s[1] : nullptr;
