@@ -823,6 +823,14 @@ def _scratch(workspace, need, like):
     return torch.empty(need, dtype=torch.uint8, device=like.device), need
 
 
+def _written(given):
+    """Autograd is told of the caller's tensors (None: none) that a call has written, as by torch's own operations in place."""
+    import torch
+    for t in given:
+        if t is not None and not t.is_inference():
+            torch.autograd.graph.increment_version(t)
+
+
 def _finite(name, x):
     x = float(x)
     if not math.isfinite(x):
@@ -1016,6 +1024,7 @@ def sphattn_vocab_distill_fwd(X, W, ids, teacher, scale=1.0, temperature=1.0, re
     T, V, D, K, code, id_bytes = _taught(X, W, ids, teacher)
     _brought(stream, losses=losses, lse=lse, workspace=workspace, **({"mean": mean} if red else {}), **({"kept": kept} if keep else {}))
     _on_device(X=X, W=W, ids=ids, teacher=teacher, losses=losses, lse=lse, kept=kept, mean=mean, workspace=workspace)
+    given = losses, lse, kept, mean if red else None
     losses = torch.empty(T, dtype=torch.float32, device=X.device) if losses is None else losses
     lse = torch.empty(T, dtype=torch.float32, device=X.device) if lse is None else lse
     if keep and kept is None:
@@ -1029,6 +1038,7 @@ def sphattn_vocab_distill_fwd(X, W, ids, teacher, scale=1.0, temperature=1.0, re
     ws, ws_bytes = _scratch(workspace, lib.sphattn_vocab_distill_workspace_bytes(T, V, D, K, code), X)
     _raise_on(lib.sphattn_vocab_distill_fwd(X.data_ptr(), W.data_ptr(), ids.data_ptr(), id_bytes, teacher.data_ptr(), losses.data_ptr(), lse.data_ptr(),
                                             _ptr(kept), _ptr(mean), T, V, D, K, scale, temperature, red, code, ws.data_ptr(), ws_bytes, _stream_of(X, stream)))
+    _written(given)
     return (losses, lse) + ((kept,) if keep else ()) + ((mean,) if red else ())
 
 
@@ -1048,6 +1058,7 @@ def sphattn_vocab_distill_bwd(X, W, ids, teacher, lse, kept, dloss, scale=1.0, t
     _f32("dloss", dloss, () if red else (T,), optional=False)
     _brought(stream, workspace=workspace, **({"dX": dX} if want_dX else {}), **({"dW": dW} if want_dW else {}))
     _on_device(X=X, W=W, ids=ids, teacher=teacher, lse=lse, kept=kept, dloss=dloss, dX=dX, dW=dW, workspace=workspace)
+    given = dX if want_dX else None, dW if want_dW else None
     if want_dX and dX is None:
         dX = torch.empty_like(X)
     if want_dW and dW is None:
@@ -1059,6 +1070,7 @@ def sphattn_vocab_distill_bwd(X, W, ids, teacher, lse, kept, dloss, scale=1.0, t
     _raise_on(lib.sphattn_vocab_distill_bwd(X.data_ptr(), W.data_ptr(), ids.data_ptr(), id_bytes, teacher.data_ptr(), lse.data_ptr(), kept.data_ptr(),
                                             dloss.data_ptr(), _ptr(dX), _ptr(dW), T, V, D, K, scale, temperature, red, code, ws.data_ptr(), ws_bytes,
                                             _stream_of(X, stream)))
+    _written(given)
     return dX, dW
 
 
@@ -1118,9 +1130,7 @@ def sphattn_clip_grads(grads, max_norm, out=None, norm=None, workspace=None, str
     _raise_on(lib.sphattn_clip_grads(pointers(*[g.data_ptr() for g in grads]), pointers(*[o.data_ptr() for o in outs]),
                                      sizes(*[g.numel() for g in grads]), types(*[codes[g.dtype] for g in grads]), n, max_norm,
                                      norm.data_ptr(), ws.data_ptr(), ws_bytes, _stream_of(norm, stream)))
-    for o in outs:                                 # autograd is told, as by torch's own operations in place
-        if not o.is_inference():
-            torch.autograd.graph.increment_version(o)
+    _written(outs)
     return norm
 
 
@@ -1230,7 +1240,7 @@ def sphattn_head_norm_rotary_fwd(Xq, Xk=None, wq=None, wk=None, positions=None, 
     _need_heads("Q", Q, (B, Hq, N, d), Xq.dtype, optional=True)
     _need_heads("K", K, (B, Hk, N, d), Xq.dtype, optional=True)
     _on_device(Xq=Xq, Xk=Xk, wq=wq, wk=wk, positions=positions, inv_freq=inv_freq, Q=Q, K=K)
-    given = [t for t in (Q, K) if t is not None]
+    given = Q, K
     if Q is None:
         Q = torch.empty((B, Hq, N, d), dtype=Xq.dtype, device=Xq.device)
     if K is None and Hk:
@@ -1238,9 +1248,7 @@ def sphattn_head_norm_rotary_fwd(Xq, Xk=None, wq=None, wk=None, positions=None, 
     _raise_on(lib.sphattn_head_norm_rotary_fwd(_heads_of(Xq, True), _heads_of(Xk, True), _ptr(wq), _ptr(wk), _heads_of(Q, False), _heads_of(K, False),
                                                None if rotary is None else ctypes.byref(rotary), B, N, Hq, Hk, d, int(bool(norm)), eps, code,
                                                _stream_of(Xq, stream)))
-    for t in given:                                # autograd is told, as by torch's own operations in place
-        if not t.is_inference():
-            torch.autograd.graph.increment_version(t)
+    _written(given)
     return Q, K
 
 
@@ -1274,16 +1282,14 @@ def sphattn_head_norm_rotary_bwd(Xq, Xk, wq, wk, dQ, dK, positions=None, inv_fre
     _need("dwk", out[3], (d,), (Xq.dtype,), optional=True)
     _on_device(Xq=Xq, Xk=Xk, wq=wq, wk=wk, dQ=dQ, dK=dK, positions=positions, inv_freq=inv_freq, dXq=out[0], dXk=out[1], dwq=out[2], dwk=out[3],
                workspace=workspace)
-    given = [t for t in out if t is not None]
+    given = out
     out = [torch.empty(s, dtype=Xq.dtype, device=Xq.device) if w and t is None else t for t, s, w in zip(out, shapes, wants)]
     ws, ws_bytes = _scratch(workspace, sphattn_head_norm_rotary_bwd_workspace_bytes(d), Xq) if wants[2] or wants[3] else (None, 0)
     _raise_on(lib.sphattn_head_norm_rotary_bwd(_heads_of(Xq, True), _heads_of(Xk, True), _ptr(wq), _ptr(wk), _heads_of(dQ, False), _heads_of(dK, False),
                                                _heads_of(out[0], True), _heads_of(out[1], True), _ptr(out[2]), _ptr(out[3]),
                                                None if rotary is None else ctypes.byref(rotary), B, N, Hq, Hk, d, int(bool(norm)), eps, code, _ptr(ws),
                                                ws_bytes, _stream_of(Xq, stream)))
-    for t in given:
-        if not t.is_inference():
-            torch.autograd.graph.increment_version(t)
+    _written(given)
     return tuple(out)
 
 
@@ -1322,11 +1328,13 @@ def sphattn_gated_ffn_fwd(X, Wg, Wu, activation="silu", H=None, workspace=None, 
     need = lib.sphattn_gated_ffn_workspace_bytes(T, D, F, code)
     _brought(stream, H=H, **({"workspace": workspace} if need else {}))
     _on_device(X=X, Wg=Wg, Wu=Wu, H=H, workspace=workspace)
+    given = H,
     if H is None:
         H = torch.empty((T, F), dtype=X.dtype, device=X.device)
     _need("H", H, (T, F), (X.dtype,))
     ws, ws_bytes = _scratch(workspace, need, X) if need else (None, 0)
     _raise_on(lib.sphattn_gated_ffn_fwd(X.data_ptr(), Wg.data_ptr(), Wu.data_ptr(), H.data_ptr(), T, D, F, gate, code, _ptr(ws), ws_bytes, _stream_of(X, stream)))
+    _written(given)
     return H
 
 
@@ -1345,10 +1353,12 @@ def sphattn_gated_ffn_bwd(X, Wg, Wu, dH, activation="silu", dX=None, dWg=None, d
     out = [t if w else None for t, w in zip((dX, dWg, dWu), wants)]
     _brought(stream, workspace=workspace, **{n: t for n, t, w in zip(("dX", "dWg", "dWu"), out, wants) if w})
     _on_device(X=X, Wg=Wg, Wu=Wu, dH=dH, dX=out[0], dWg=out[1], dWu=out[2], workspace=workspace)
+    given = out
     out = [torch.empty_like(x) if w and t is None else t for t, x, w in zip(out, (X, Wg, Wu), wants)]
     for name, t, shape in zip(("dX", "dWg", "dWu"), out, ((T, D), (F, D), (F, D))):
         _need(name, t, shape, (X.dtype,), optional=True)
     ws, ws_bytes = _scratch(workspace, lib.sphattn_gated_ffn_bwd_workspace_bytes(T, D, F, code), X)
     _raise_on(lib.sphattn_gated_ffn_bwd(X.data_ptr(), Wg.data_ptr(), Wu.data_ptr(), dH.data_ptr(), *(_ptr(t) for t in out), T, D, F, gate, code, ws.data_ptr(),
                                         ws_bytes, _stream_of(X, stream)))
+    _written(given)
     return tuple(out)
