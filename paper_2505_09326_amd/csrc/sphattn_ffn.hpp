@@ -344,7 +344,7 @@ void ffn_gate_kernel(FfnArgs a, int act)
                         float value, slope;
                         gate<G, F32>(prod.acc[2 * (i + s)][j][r], value, slope);
                         if constexpr (BACK) {
-                            y[s][r] = d[s][r] * u * slope;
+                            y[s][r] = d[s][r] * (u * slope);       // (dH U may be past fp32's range beside a closed gate)
                             z[s][r] = d[s][r] * value;
                         } else {
                             y[s][r] = value * u;

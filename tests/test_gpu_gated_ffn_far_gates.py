@@ -111,3 +111,17 @@ def test_infinite_rows_are_the_formula(pkg, T, act, dtype):
     # (either way of forming the sums is off by (72 + 4) u and 3 2^-22 of their terms at most, act's slope by 1.13 of that)
     tol = 2 * (76 * U + 3 * 2.0 ** -22) * 1.13 * size * other * 2 + torch.finfo(TYPES[dtype]).eps * clean.double().abs()
     assert ((got - clean.double()).abs() <= tol)[rows].all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("act", ["silu", "gelu", "relu"])
+@pytest.mark.parametrize("T", [3, 200, 4200])
+def test_closed_gates_beside_large_gradients(pkg, T, act, dtype):
+    """dH U of 1e40 where the slope is 0: 0, and where it is 1 but dH 0 too."""
+    t = TYPES[dtype]
+    X, Wg, Wu = _one_product(torch.full((72,), -1000.0, device=DEV), T, dtype)
+    Wg[5], Wu[:, 0] = 1000.0, 1e20
+    dH = torch.full((T, 72), 1e20, device=DEV, dtype=t)
+    dH[:, 5] = 0
+    for g in pkg.sphattn_gated_ffn_bwd(X, Wg, Wu, dH, act):
+        assert (g == 0).all()
