@@ -42,8 +42,9 @@ typedef struct {
  *   wq, wk : [d], the type of X, or NULL (ones).
  *   Q, K   : where the rows go, by strides: [B,Hq,N,d] for the attention, or a place in a cache.  They overlap no input
  *            (SPHATTN_ERR_ALIAS) and each other nowhere (not checked: both may lie in one buffer).  What is between the rows is not touched.
- *   rotary : NULL: nothing is rotated.  Angles are formed in fp64, a position's fraction of a turn to 2^-21 of one at 2^31.
- * In fp32, rounded once.  d 64 or 128 (SPHATTN_ERR_HEAD_DIM); B, N >= 0 (0: nothing is done), B N <= 2^31 - 1, Hq >= 1, Hk >= 0, Hq + Hk <= 65536, sections
+ *   rotary : NULL: nothing is rotated.  Turns (position inv_freq / 2 pi) are formed in fp64, off by 2^-51 of themselves, their fraction is rounded to fp32: at 2^31 and a radian
+ *            per position 2^-22 of a turn, larger frequencies in proportion.
+ * In fp32, rounded once, whatever the size of a row's elements.  d 64 or 128 (SPHATTN_ERR_HEAD_DIM); B, N >= 0 (0: nothing is done), B N <= 2^31 - 1, Hq >= 1, Hk >= 0, Hq + Hk <= 65536, sections
  * as said (SPHATTN_ERR_SHAPE); eps >= 0 and finite, norm 0 or 1 (SPHATTN_ERR_VALUE).
  */
 int sphattn_head_norm_rotary_fwd(const sphattn_heads* Xq, const sphattn_heads* Xk, const void* wq, const void* wk, const sphattn_heads* Q, const sphattn_heads* K,

