@@ -366,23 +366,24 @@ void heads_bwd_kernel(HeadsArgs a)
     }
 }
 
-// dw from the workgroups' sums: a workgroup takes sixteen columns, 16 lanes' worth of rows at a time
+// dw from the workgroups' sums, in fp64: a workgroup takes sixteen columns, 16 lanes' worth of rows at a time
 template <Store S>
 __global__ __launch_bounds__(1024)
 void heads_dw_kernel(const float* __restrict__ partial, int groups, int D, void* __restrict__ dwq, void* __restrict__ dwk)
 {
-    __shared__ float shared[64][16];
+    __shared__ double shared[64][16];
     const int col = (int)blockIdx.x * 16 + (threadIdx.x & 15), row = threadIdx.x >> 4;
-    float x = 0.f;
+    double x = 0.0;
 #pragma unroll 8
     for (int g = row; g < groups; g += 64) x += partial[(size_t)g * 2 * D + col];
     shared[row][threadIdx.x & 15] = x;
     __syncthreads();
     if (threadIdx.x >= 16) return;
-    x = 0.f;
+    x = 0.0;
+#pragma unroll 16
     for (int r = 0; r < 64; ++r) x += shared[r][threadIdx.x];
     void* out = col < D ? dwq : dwk;
-    if (out) store_el<S>(out, col < D ? col : col - D, x);
+    if (out) store_el<S>(out, col < D ? col : col - D, (float)x);
 }
 
 }  // namespace sphattn

@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from test_gpu_head_norm_rotary import _case, _freq
+from test_gpu_head_norm_rotary import _angle, _case, _exact
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -67,3 +67,17 @@ def test_elements_of_very_different_size(pkg, dtype):
     x[0, 6, 0, 7], x[0, 7, 1, 9] = float("inf"), float("nan")
     got = pkg.sphattn_head_norm_rotary_fwd(x, eps=0.0)[0]
     assert got[0, :, 5].isnan().all() and got[0, 0, 6, 7].isnan() and (got[0, 0, 6, :7] == 0).all() and got[0, 1, 7].isnan().all() and got[0, 1, 6].isfinite().all()
+
+
+@pytest.mark.parametrize("seed", [1, 2, 3])
+def test_weights_gradients_over_many_rows(pkg, seed):
+    """Sums over 54081 and 18027 rows in fp32.  Of each sum's norm: its terms' roundings, six of 0.29 2^-24 each in the mean (x r, the product with dy and dy's rotation), 0.7 2^-24; adding them, a
+    chain of nine heads and five levels of lanes and waves, 0.29 2^-24 of what is there at each, sqrt(14) of them, 1.1; the angles' 2^-26 of a turn, 0.5; in fp64 behind that and the
+    result's rounding, 0.3.  Together 1.5 2^-24 in the mean, and this asks for 2.7."""
+    B, N, Hq, Hk, d = 3, 2003, 9, 3, 64
+    Xq, Xk, wq, wk, dQ, dK, positions, inv_freq, sections = _case(B, N, Hq, Hk, d, "f32", 3, torch.int64, seed)
+    grads = pkg.sphattn_head_norm_rotary_bwd(Xq, Xk, wq, wk, dQ, dK, positions, inv_freq, sections, True)
+    angle = _angle(positions, inv_freq, sections, B, N)
+    for got, x, w, g in ((grads[2], Xq, wq, dQ), (grads[3], Xk, wk, dK)):
+        want = _exact(x, w, angle, True, True, float(torch.tensor(1e-6).float()), g)[2]
+        assert float((got.double() - want).norm() / want.norm()) < 2.7 * 2.0 ** -24
